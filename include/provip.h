@@ -392,6 +392,108 @@ int provip_prune_visual_heads(const void *Q, const void *K, const void *V, const
                               float *conf_out_or_null, void *ws, size_t ws_bytes,
                               unsigned flags, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Behind the pruning: attention over the pruned prompts, a paged key/value
+ * cache for their rows, and decoding from it (the paper has no counterpart:
+ * these are the LLM-side operators that its pruned sequences go through)
+ *
+ * Row strides are in elements, at least a row, and multiples of 16 bytes; the
+ * heads of a row lie next to each other. Requires d_h == 128 and at most 64
+ * query heads a group (H_q / H_kv). algo: PROVIP_ALGO_AUTO, _SIMT, or _TCGEN05
+ * (bf16 only). Softmax statistics and all sums are kept in fp32; the tensor
+ * cores' form rounds the probabilities to bf16 for their product with V.
+ * scale is the factor of the logits (1 / sqrt(d_h) as a rule), > 0.
+ * A key that a row does not see never touches it, whatever it holds
+ * (infinities and NaN too). A row that sees no key gets out = 0, lse = -inf.
+ * ---------------------------------------------------------------------- */
+
+/* Attention over whole prompts: B sequences of different lengths, packed or
+ * padded. Sequence b has query rows q_start[b] .. + q_len[b] of Q and own keys
+ * k_start[b] .. + k_len[b] of K and V (packed: the running sums of the
+ * lengths; the padded layout [B, L_max] of the pruning calls: b * L_max and
+ * seq_len, or seq_len_out of a compaction). Every row also sees the prefix_len
+ * rows of K_prefix / V_prefix, if any (the prompt of one image or video in front
+ * of many questions about it). Row i of a sequence, head h:
+ *   o = sum_j softmax_j(scale q . k_j) v_j,  lse = log sum_j exp(scale q . k_j)
+ * over the prefix and own keys j < k_len, causal != 0: with j <= i + k_len -
+ * q_len only (the last row sees the last key), from key/value head
+ * h / (H_q / H_kv).
+ *   Q [T_q, H_q, d_h] rows q_stride apart; K, V [T_k, H_kv, d_h] (may be slices
+ *   of one buffer); K_prefix, V_prefix [prefix_len, H_kv, d_h] or NULL.
+ *   q_start, q_len, k_start, k_len [B] int32 (device); q_len <= q_len_max,
+ *   k_len <= k_len_max (host bounds, which size the launch).
+ *   out [T_q, H_q, d_h] rows out_stride apart, lse_or_null [T_q, H_q] fp32;
+ *   rows outside every sequence are left untouched, and so are those of a
+ *   sequence whose start or length is out of range (it is reported). Sequences
+ *   must not share query rows. */
+size_t provip_prompt_attention_workspace_size(int T_q, int B, int H_q, int H_kv, int q_len_max,
+                                              int k_len_max, int prefix_len, int dtype, int algo);
+int provip_prompt_attention(const void *Q, long long q_stride, const void *K, long long k_stride,
+                            const void *V, long long v_stride, int T_q, int T_k, int B, int H_q,
+                            int H_kv, int d_h, const int *q_start, const int *q_len,
+                            const int *k_start, const int *k_len, int q_len_max, int k_len_max,
+                            const void *K_prefix_or_null, long long kp_stride,
+                            const void *V_prefix_or_null, long long vp_stride, int prefix_len,
+                            int causal, float scale, int dtype, int algo, void *out,
+                            long long out_stride, float *lse_or_null, void *ws, size_t ws_bytes,
+                            void *stream);
+
+/* Block tables and slot maps of a paged cache, on the GPU, for one step of B
+ * requests. A cache is n_pages pages of page_size rows (a power of two, 8 to
+ * 256); free_pages[0 .. free_count) is the stack of pages nobody holds;
+ * request b holds kv_len[b] tokens in the first ceil(kv_len / page_size) pages
+ * of its table row. new_len[b] < 0 ends it: its pages go onto the stack (all
+ * ended requests' before anything is taken, in request and table order) and its
+ * length becomes 0. new_len[b] >= 0 adds that many tokens: the pages that they
+ * need beyond those held come off the top of the stack, in request order. A
+ * request that needs pages when too few are left gets none, and so does every
+ * later one that needs any; its length stays.
+ *   kv_len, new_len [B], free_count [1] int32; free_pages [n_free_max] int32 (in
+ *   place), block_table [B, max_pages] int32 (in place; only new entries are
+ *   written).
+ *   row_start_out [B + 1]: where each request's new tokens start among all new
+ *   tokens, packed in request order (its own q_start), and their number;
+ *   slot_map_out [T_max]: page * page_size + row in the page for every packed
+ *   new token, -1 for those of a request that got no pages and past the last;
+ *   kv_len_out [B] and free_count_out [1]: lengths and free pages afterwards
+ *   (may be kv_len and free_count themselves).
+ * Reported, and left as they are: a request with kv_len < 0, with more pages
+ * than max_pages or rows past T_max; a stack that outgrows n_free_max. */
+int provip_page_tables(const int *kv_len, const int *new_len, int B, int page_size,
+                       int *free_pages, int n_free_max, const int *free_count, int *block_table,
+                       int max_pages, int T_max, int *kv_len_out, int *row_start_out,
+                       int *slot_map_out, int *free_count_out, void *stream);
+
+/* Key/value rows of T tokens into the pages, byte-exactly: row t of K and V
+ * [T, H_kv, d_h] (k_stride, v_stride elements apart) goes to slot slot_map[t]
+ * [T] int32 of k_pages and v_pages [n_pages, page_size, H_kv, d_h]. Negative
+ * slots are skipped, slots past the pool reported and skipped; no two rows may
+ * have the same slot. Rows are multiples of 16 bytes. */
+int provip_kv_append(const void *K, long long k_stride, const void *V, long long v_stride, int T,
+                     int H_kv, int d_h, const int *slot_map, int n_pages, int page_size, int dtype,
+                     void *k_pages, void *v_pages, void *stream);
+
+/* Attention of one token per request over the paged cache: request b's row of
+ * Q [B, H_q, d_h] (q_stride elements apart) sees the prefix_len tokens in the
+ * pages of prefix_table (shared by the whole batch and read once for it; NULL
+ * with prefix_len 0) and the kv_len[b] tokens in the pages of its row of
+ * block_table [B, max_pages] (its own new token among them, appended before).
+ *   k_pages, v_pages [n_pages, page_size, H_kv, d_h], page_size a power of two
+ *   from 8 to 256; pages past a length are not read. kv_len [B] int32 (device),
+ *   at most kv_len_max <= max_pages * page_size (host bound).
+ *   out [B, H_q, d_h] rows out_stride apart, lse_or_null [B, H_q] fp32.
+ * A kv_len out of range is reported and taken as 0, a page outside the pool is
+ * reported and the result of its request (of every one, for a prefix page) is
+ * meaningless. */
+size_t provip_decode_attention_workspace_size(int B, int H_q, int H_kv, int kv_len_max,
+                                              int prefix_len, int dtype, int algo);
+int provip_decode_attention(const void *Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
+                            const void *k_pages, const void *v_pages, int n_pages, int page_size,
+                            const int *block_table, int max_pages, const int *kv_len,
+                            int kv_len_max, const int *prefix_table_or_null, int prefix_len,
+                            float scale, int dtype, int algo, void *out, long long out_stride,
+                            float *lse_or_null, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

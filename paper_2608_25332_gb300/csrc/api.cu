@@ -1160,3 +1160,299 @@ extern "C" int provip_head_scores_noalloc(const void* Q, const void* K, int B, i
                             row_mask_or_null, N_t_max, vis_start, N_v, seq_len, dtype, ralgo,
                             scores, scratch, kNoAllocScratchBytes, stream);
 }
+
+// ===========================================================================
+// attention behind the pruning and its paged cache
+// ===========================================================================
+namespace {
+
+constexpr int kPlanSms = 152;  // parts are planned for a GB300's SMs (sizes do not depend on the device)
+
+// parts to share n_keys keys out over, so that `units` pieces of work become about `want`;
+// a part has at least min_keys keys
+int attn_parts(long long units, int n_keys, long long want, int min_keys, int most) {
+  if (n_keys <= 0) return 0;
+  long long n = units > 0 ? (want + units - 1) / units : 1;
+  const long long by_keys = ((long long)n_keys + min_keys - 1) / min_keys;
+  if (n > by_keys) n = by_keys;
+  if (n > most) n = most;
+  return n < 1 ? 1 : (int)n;
+}
+
+int attn_algo(int algo, int dtype) {
+  (void)dtype;
+  return algo == PROVIP_ALGO_AUTO ? PROVIP_ALGO_SIMT : algo;
+}
+
+// row tiles of 64 packed rows; a part has four 64-key tiles or more
+int prompt_parts(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int prefix_len) {
+  const long long tiles = ((long long)q_len_max * (H_q / H_kv) + 63) / 64;
+  const int keys = prefix_len > 0x7fffffff - k_len_max ? 0x7fffffff : prefix_len + k_len_max;
+  const int n = attn_parts(tiles * H_kv * B, keys, 2 * kPlanSms, 256, 32);
+  return n < 1 ? 1 : n;
+}
+
+void decode_parts(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int* n_own, int* n_prefix) {
+  const int R = H_q / H_kv;
+  *n_own = attn_parts((long long)B * H_kv * (R <= 2 ? 1 : (R + 3) / 4), kv_len_max, 4 * kPlanSms, 64, 64);
+  *n_prefix = attn_parts(((long long)B * R + 63) / 64 * H_kv, prefix_len, 2 * kPlanSms, 256, 64);
+  if (*n_own + *n_prefix == 0) *n_own = 1;
+}
+
+size_t attn_ws(Carve& c, int n_part, int T_q, int H_q, float** part_o, float** part_lse) {
+  if (n_part <= 1) return 0;
+  *part_o = c.take<float>((size_t)n_part * T_q * H_q * kHeadDim);
+  *part_lse = c.take<float>((size_t)n_part * T_q * H_q);
+  return c.off;
+}
+
+// what the two attention calls check alike
+int attn_validate(const char* what, const void* Q, long long q_stride, const void* K, long long k_stride,
+                  const void* V, long long v_stride, int H_q, int H_kv, int d_h, float scale, int dtype, int algo,
+                  const void* out, long long out_stride) {
+  if (!Q || !K || !V || !out) return fail(PROVIP_ERR_INVALID_ARG, "%s: null tensor", what);
+  if (H_q < 1 || H_kv < 1 || H_q % H_kv) return fail(PROVIP_ERR_INVALID_ARG, "%s: H_q %d, H_kv %d", what, H_q, H_kv);
+  if (d_h != kHeadDim) return fail(PROVIP_ERR_UNSUPPORTED, "%s: d_h must be 128", what);
+  if (H_q / H_kv > 64) return fail(PROVIP_ERR_UNSUPPORTED, "%s: more than 64 query heads a group", what);
+  if (!dtype_ok(dtype)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: dtype %d", what, dtype);
+  if (!(scale > 0.f) || isinf(scale)) return fail(PROVIP_ERR_INVALID_ARG, "%s: scale must be positive", what);
+  if (algo != PROVIP_ALGO_AUTO && algo != PROVIP_ALGO_SIMT && algo != PROVIP_ALGO_TCGEN05)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: algo %d", what, algo);
+  if (algo == PROVIP_ALGO_TCGEN05 && dtype != PROVIP_BF16)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: tcgen05 path needs bf16", what);
+  if (q_stride < (long long)H_q * d_h || k_stride < (long long)H_kv * d_h || v_stride < (long long)H_kv * d_h ||
+      out_stride < (long long)H_q * d_h)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: row stride shorter than a row", what);
+  const int es = esize(dtype);
+  if ((q_stride * es) % 16 || (k_stride * es) % 16 || (v_stride * es) % 16 || (out_stride * es) % 16)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: row strides must be multiples of 16 bytes", what);
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out))
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: tensor not 16-byte aligned", what);
+  return PROVIP_OK;
+}
+
+int page_shift_of(int page_size) {
+  for (int s = 3; s <= 8; ++s)
+    if (page_size == 1 << s) return s;
+  return -1;
+}
+
+}  // namespace
+
+extern "C" size_t provip_prompt_attention_workspace_size(int T_q, int B, int H_q, int H_kv, int q_len_max,
+                                                         int k_len_max, int prefix_len, int dtype, int algo) {
+  if (T_q < 0 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || q_len_max < 0 || k_len_max < 0 || prefix_len < 0)
+    return 0;
+  (void)attn_algo(algo, dtype);
+  Carve c(nullptr);
+  float *po, *pl;
+  return attn_ws(c, prompt_parts(B, H_q, H_kv, q_len_max, k_len_max, prefix_len), T_q, H_q, &po, &pl);
+}
+
+extern "C" int provip_prompt_attention(const void* Q, long long q_stride, const void* K, long long k_stride,
+                                       const void* V, long long v_stride, int T_q, int T_k, int B, int H_q, int H_kv,
+                                       int d_h, const int* q_start, const int* q_len, const int* k_start,
+                                       const int* k_len, int q_len_max, int k_len_max,
+                                       const void* K_prefix_or_null, long long kp_stride,
+                                       const void* V_prefix_or_null, long long vp_stride, int prefix_len, int causal,
+                                       float scale, int dtype, int algo, void* out, long long out_stride,
+                                       float* lse_or_null, void* ws, size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_range("provip_prompt_attention");
+  const char* what = "prompt_attention";
+  if (T_q < 0 || T_k < 0 || B < 1 || q_len_max < 0 || q_len_max > T_q || k_len_max < 0 || k_len_max > T_k ||
+      prefix_len < 0)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: bad sizes", what);
+  if (B > 65535) return fail(PROVIP_ERR_UNSUPPORTED, "%s: more than 65535 sequences", what);
+  if (T_q == 0 || q_len_max == 0) return PROVIP_OK;  // no row
+  // a call without own keys may pass no tensor for them
+  const void *k = K, *v = V;
+  if (T_k == 0) {
+    k = v = Q;
+    k_stride = v_stride = (long long)H_kv * d_h;
+  }
+  int rc = attn_validate(what, Q, q_stride, k, k_stride, v, v_stride, H_q, H_kv, d_h, scale, dtype, algo, out,
+                         out_stride);
+  if (rc) return rc;
+  if (!q_start || !q_len || !k_start || !k_len) return fail(PROVIP_ERR_INVALID_ARG, "%s: null starts or lengths", what);
+  if (prefix_len > 0) {
+    rc = attn_validate(what, Q, q_stride, K_prefix_or_null, kp_stride, V_prefix_or_null, vp_stride, H_q, H_kv, d_h,
+                       scale, dtype, algo, out, out_stride);
+    if (rc) return rc;
+    if (prefix_len > 0x7fffffff - k_len_max) return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many keys", what);
+  }
+  const int n_part = prompt_parts(B, H_q, H_kv, q_len_max, k_len_max, prefix_len);
+  if ((long long)q_len_max * (H_q / H_kv) > 0x7fffffffll - 64 || (long long)H_kv * n_part > 65535)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
+  if ((rc = check_ws(provip_prompt_attention_workspace_size(T_q, B, H_q, H_kv, q_len_max, k_len_max, prefix_len, dtype,
+                                                            algo),
+                     ws, ws_bytes, what)))
+    return rc;
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  AttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q;
+  a.K = k;
+  a.V = v;
+  a.Kp = K_prefix_or_null;
+  a.Vp = V_prefix_or_null;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.kp_stride = kp_stride;
+  a.vp_stride = vp_stride;
+  a.o_stride = out_stride;
+  a.T_q = T_q;
+  a.T_k = T_k;
+  a.B = B;
+  a.H_q = H_q;
+  a.H_kv = H_kv;
+  a.q_start = q_start;
+  a.q_len = q_len;
+  a.k_start = k_start;
+  a.k_len = k_len;
+  a.q_len_max = q_len_max;
+  a.k_len_max = k_len_max;
+  a.prefix_len = prefix_len;
+  a.causal = causal ? 1 : 0;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.out = out;
+  a.lse = lse_or_null;
+  a.n_part = n_part;
+  a.err = d->status;
+  Carve c(ws);
+  attn_ws(c, n_part, T_q, H_q, &a.part_o, &a.part_lse);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = attn_prompt_simt_launch(a, dtype, s);
+  if (e == cudaSuccess && n_part > 1) e = attn_join_launch(a, dtype, s);
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "prompt_attention launch");
+}
+
+extern "C" size_t provip_decode_attention_workspace_size(int B, int H_q, int H_kv, int kv_len_max, int prefix_len,
+                                                         int dtype, int algo) {
+  if (B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || kv_len_max < 0 || prefix_len < 0) return 0;
+  (void)attn_algo(algo, dtype);
+  int n_own, n_prefix;
+  decode_parts(B, H_q, H_kv, kv_len_max, prefix_len, &n_own, &n_prefix);
+  Carve c(nullptr);
+  float *po, *pl;
+  return attn_ws(c, n_own + n_prefix, B, H_q, &po, &pl);
+}
+
+extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
+                                       const void* k_pages, const void* v_pages, int n_pages, int page_size,
+                                       const int* block_table, int max_pages, const int* kv_len, int kv_len_max,
+                                       const int* prefix_table_or_null, int prefix_len, float scale, int dtype,
+                                       int algo, void* out, long long out_stride, float* lse_or_null, void* ws,
+                                       size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_range("provip_decode_attention");
+  const char* what = "decode_attention";
+  if (B < 1 || n_pages < 1 || max_pages < 0 || kv_len_max < 0 || prefix_len < 0)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: bad sizes", what);
+  if (B > 65535) return fail(PROVIP_ERR_UNSUPPORTED, "%s: more than 65535 requests", what);
+  const long long row = (long long)H_kv * d_h;
+  int rc = attn_validate(what, Q, q_stride, k_pages, row, v_pages, row, H_q, H_kv, d_h, scale, dtype, algo, out,
+                         out_stride);
+  if (rc) return rc;
+  const int shift = page_shift_of(page_size);
+  if (shift < 0) return fail(PROVIP_ERR_UNSUPPORTED, "%s: page_size %d is no power of two from 8 to 256", what, page_size);
+  if (!kv_len || (!block_table && max_pages > 0) || (!prefix_table_or_null && prefix_len > 0))
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: null lengths or tables", what);
+  if (kv_len_max > (long long)max_pages * page_size)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: kv_len_max %d does not fit %d pages", what, kv_len_max, max_pages);
+  if (prefix_len > 0x7fffffff - kv_len_max || (long long)n_pages * page_size > 0x7fffffffll)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many keys", what);
+  int n_own, n_prefix;
+  decode_parts(B, H_q, H_kv, kv_len_max, prefix_len, &n_own, &n_prefix);
+  if ((long long)B * (H_q / H_kv) > 0x7fffffffll - 64 || (long long)H_kv * (n_prefix + 1) > 65535)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
+  if ((rc = check_ws(provip_decode_attention_workspace_size(B, H_q, H_kv, kv_len_max, prefix_len, dtype, algo), ws,
+                     ws_bytes, what)))
+    return rc;
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  AttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q;
+  a.K = a.Kp = k_pages;
+  a.V = a.Vp = v_pages;
+  a.q_stride = q_stride;
+  a.k_stride = a.v_stride = a.kp_stride = a.vp_stride = row;
+  a.o_stride = out_stride;
+  a.T_q = B;
+  a.B = B;
+  a.H_q = H_q;
+  a.H_kv = H_kv;
+  a.k_len = kv_len;
+  a.q_len_max = 1;
+  a.k_len_max = kv_len_max;
+  a.prefix_len = prefix_len;
+  a.paged = 1;
+  a.page_size = page_size;
+  a.page_shift = shift;
+  a.n_pages = n_pages;
+  a.max_pages = max_pages;
+  a.block_table = block_table;
+  a.prefix_table = prefix_table_or_null;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.out = out;
+  a.lse = lse_or_null;
+  a.n_part = n_own + n_prefix;
+  a.err = d->status;
+  Carve c(ws);
+  attn_ws(c, a.n_part, B, H_q, &a.part_o, &a.part_lse);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = attn_decode_simt_launch(a, n_own, dtype, s);
+  if (e == cudaSuccess && a.n_part > 1) e = attn_join_launch(a, dtype, s);
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "decode_attention launch");
+}
+
+extern "C" int provip_page_tables(const int* kv_len, const int* new_len, int B, int page_size, int* free_pages,
+                                  int n_free_max, const int* free_count, int* block_table, int max_pages, int T_max,
+                                  int* kv_len_out, int* row_start_out, int* slot_map_out, int* free_count_out,
+                                  void* stream) {
+  NvtxRange nvtx_range("provip_page_tables");
+  if (!kv_len || !new_len || !free_count || !kv_len_out || !row_start_out || !free_count_out)
+    return fail(PROVIP_ERR_INVALID_ARG, "page_tables: null pointer argument");
+  if (B < 1 || n_free_max < 0 || max_pages < 0 || T_max < 0)
+    return fail(PROVIP_ERR_INVALID_ARG, "page_tables: bad sizes");
+  if ((!free_pages && n_free_max > 0) || (!block_table && max_pages > 0) || (!slot_map_out && T_max > 0))
+    return fail(PROVIP_ERR_INVALID_ARG, "page_tables: null tables");
+  const int shift = page_shift_of(page_size);
+  if (shift < 0)
+    return fail(PROVIP_ERR_UNSUPPORTED, "page_tables: page_size %d is no power of two from 8 to 256", page_size);
+  DevInfo* d;
+  int rc = dev_info(&d);
+  if (rc) return rc;
+  PageTablesArgs a = {kv_len,    new_len,    B,     shift,      free_pages,    n_free_max,   free_count,
+                      block_table, max_pages, T_max, kv_len_out, row_start_out, slot_map_out, free_count_out,
+                      d->status};
+  cudaError_t e = page_tables_launch(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "page_tables launch");
+}
+
+extern "C" int provip_kv_append(const void* K, long long k_stride, const void* V, long long v_stride, int T, int H_kv,
+                                int d_h, const int* slot_map, int n_pages, int page_size, int dtype, void* k_pages,
+                                void* v_pages, void* stream) {
+  NvtxRange nvtx_range("provip_kv_append");
+  if (T < 0 || H_kv < 1 || d_h < 1 || n_pages < 1 || page_size < 1)
+    return fail(PROVIP_ERR_INVALID_ARG, "kv_append: bad sizes");
+  if (T == 0) return PROVIP_OK;
+  if (!K || !V || !slot_map || !k_pages || !v_pages) return fail(PROVIP_ERR_INVALID_ARG, "kv_append: null pointer argument");
+  if (!dtype_ok(dtype)) return fail(PROVIP_ERR_UNSUPPORTED, "kv_append: dtype %d", dtype);
+  const long long row = (long long)H_kv * d_h, es = esize(dtype);
+  if (k_stride < row || v_stride < row) return fail(PROVIP_ERR_INVALID_ARG, "kv_append: row stride shorter than a row");
+  if ((row * es) % 16 || (k_stride * es) % 16 || (v_stride * es) % 16)
+    return fail(PROVIP_ERR_UNSUPPORTED, "kv_append: rows and row strides must be multiples of 16 bytes");
+  if (!aligned16(K) || !aligned16(V) || !aligned16(k_pages) || !aligned16(v_pages))
+    return fail(PROVIP_ERR_UNSUPPORTED, "kv_append: tensor not 16-byte aligned");
+  if (row * es > (1ll << 30)) return fail(PROVIP_ERR_UNSUPPORTED, "kv_append: row too long");
+  DevInfo* d;
+  int rc = dev_info(&d);
+  if (rc) return rc;
+  KvAppendArgs a = {static_cast<const char*>(K), static_cast<const char*>(V), k_stride * es, v_stride * es, T, row * es,
+                    slot_map, (long long)n_pages * page_size, static_cast<char*>(k_pages), static_cast<char*>(v_pages),
+                    d->status};
+  cudaError_t e = kv_append_launch(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "kv_append launch");
+}

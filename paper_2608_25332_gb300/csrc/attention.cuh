@@ -1,0 +1,140 @@
+// Attention behind the pruning: what its kernels share.
+//
+// Rows. The rows of one key/value head g are (token, query head of g's group) pairs,
+// token-major: row r of a sequence is token r / R, head g * R + r % R with R = H_q / H_kv.
+// All R heads of a group read the same keys, so a tile of packed rows reads them once.
+//
+// Keys. A sequence's keys are a prefix that every sequence of the call shares, then its
+// own; token i of q_len sees every prefix key and, of its own k_len keys, all of them or
+// (causal) the first k_len - q_len + i + 1 (the last token sees the last key). Keys come as
+// rows of a tensor or as slots of a paged cache (page_size rows a page, the pages of a
+// sequence listed in its block table).
+//
+// Sums. Scores are kept in the base-2 domain: s = q . k * log2(e) * scale; a row's partial
+// result over a part of its keys is o = sum 2^(s - m) v / l and its base-2 log-sum-exp
+// m + log2 l, so parts join as sum_p w_p o_p / sum_p w_p with w_p = 2^(lse_p - max).
+#pragma once
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace provip {
+
+constexpr float kLn2 = 0.693147180559945309f;
+
+// where a sequence's queries, keys and values lie (validated)
+struct AttnSeq {
+  int q0, q_len;         // first query token, tokens
+  int k_len;             // own keys
+  long long k0;          // first own key row (contiguous keys)
+  const int* pages;      // own block table (paged keys)
+  bool ok;
+};
+
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int b) {
+  AttnSeq s;
+  s.pages = nullptr;
+  s.k0 = 0;
+  if (a.paged) {  // one token per request
+    s.q0 = b;
+    s.q_len = 1;
+    s.k_len = a.k_len[b];
+    s.pages = a.block_table + (size_t)b * a.max_pages;
+    s.ok = s.k_len >= 0 && s.k_len <= a.k_len_max && s.k_len <= (long long)a.max_pages * a.page_size;
+    if (!s.ok) s.k_len = 0;  // reported; the shared prefix is still attended to
+  } else {
+    s.q0 = a.q_start[b];
+    s.q_len = a.q_len[b];
+    s.k_len = a.k_len[b];
+    s.k0 = a.k_start[b];
+    s.ok = s.q0 >= 0 && s.q_len >= 0 && s.q_len <= a.q_len_max && s.q_len <= a.T_q - s.q0 && s.k0 >= 0 &&
+           s.k_len >= 0 && s.k_len <= a.k_len_max && s.k_len <= a.T_k - s.k0;
+    if (!s.ok) s.q_len = 0;  // reported; the sequence's rows are left untouched
+  }
+  return s;
+}
+
+// own keys that token i sees
+__device__ __forceinline__ int attn_visible(const AttnArgs& a, int q_len, int k_len, int i) {
+  return a.causal ? min(max(k_len - q_len + i + 1, 0), k_len) : k_len;
+}
+
+// row of the pool (paged) that holds key j of a page list; a page outside the pool is
+// reported and read as page 0
+__device__ __forceinline__ long long attn_slot(const AttnArgs& a, const int* pages, int j) {
+  int p = __ldg(pages + (j >> a.page_shift));
+  if ((unsigned)p >= (unsigned)a.n_pages) {
+    set_error(a.err, kErrBadDeviceArg);
+    p = 0;
+  }
+  return ((long long)p << a.page_shift) + (j & (a.page_size - 1));
+}
+
+// row pointers of prefix key j and of own key j, key/value head g
+template <typename T>
+__device__ __forceinline__ const T* attn_prefix_row(const AttnArgs& a, bool v, int j, int g) {
+  const T* base = static_cast<const T*>(v ? a.Vp : a.Kp) + (size_t)g * kHeadDim;
+  return base + (a.paged ? attn_slot(a, a.prefix_table, j) : (long long)j) * (v ? a.vp_stride : a.kp_stride);
+}
+template <typename T>
+__device__ __forceinline__ const T* attn_own_row(const AttnArgs& a, const AttnSeq& s, bool v, int j, int g) {
+  const T* base = static_cast<const T*>(v ? a.V : a.K) + (size_t)g * kHeadDim;
+  return base + (a.paged ? attn_slot(a, s.pages, j) : s.k0 + j) * (v ? a.v_stride : a.k_stride);
+}
+
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float* o);
+template <>
+__device__ __forceinline__ void load4<float>(const float* p, float* o) {
+  const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+  o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+}
+template <>
+__device__ __forceinline__ void load4<__nv_bfloat16>(const __nv_bfloat16* p, float* o) {
+  const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+  const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
+  const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
+  o[0] = x.x; o[1] = x.y; o[2] = y.x; o[3] = y.y;
+}
+__device__ __forceinline__ void store4(float* p, const float* v) {
+  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(v[0], v[1]), y = __floats2bfloat162_rn(v[2], v[3]);
+  uint2 u;
+  u.x = *reinterpret_cast<const uint32_t*>(&x);
+  u.y = *reinterpret_cast<const uint32_t*>(&y);
+  *reinterpret_cast<uint2*>(p) = u;
+}
+
+// One row over keys [lo, hi) of its list (prefix keys, then own ones), key by key, by one
+// warp: the plain definition, which no key outside the range touches. The tile kernels
+// weigh every value row of a tile, the hidden ones by zero; zero times an infinite or NaN
+// value is NaN, so a row that did not come out finite is computed again here. lane holds
+// elements 4 lane .. 4 lane + 3; returns the base-2 log-sum-exp (-inf: no weight at all).
+template <typename T>
+__device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s, int n_prefix, int token, int h,
+                                             int lo, int hi, float* o) {
+  const int lane = threadIdx.x & 31, g = h / (a.H_q / a.H_kv);
+  float q[4], m = -INFINITY, l = 0.f;
+  load4(static_cast<const T*>(a.Q) + (size_t)(s.q0 + token) * a.q_stride + (size_t)h * kHeadDim + lane * 4, q);
+  o[0] = o[1] = o[2] = o[3] = 0.f;
+  for (int j = lo; j < hi; ++j) {
+    float k[4], v[4];
+    const bool pre = j < n_prefix;
+    load4((pre ? attn_prefix_row<T>(a, false, j, g) : attn_own_row<T>(a, s, false, j - n_prefix, g)) + lane * 4, k);
+    load4((pre ? attn_prefix_row<T>(a, true, j, g) : attn_own_row<T>(a, s, true, j - n_prefix, g)) + lane * 4, v);
+    const float x = warp_sum(fmaf(q[0], k[0], fmaf(q[1], k[1], fmaf(q[2], k[2], q[3] * k[3])))) * a.scale_log2;
+    if (x == -INFINITY) continue;
+    const float mn = fmaxf(m, x), r = exp2f(m - mn), p = exp2f(x - mn);
+    l = l * r + p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * r + p * v[e];
+    m = mn;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = l == 0.f ? 0.f : o[e] / l;
+  return l == 0.f ? -INFINITY : m + log2f(l);
+}
+
+}  // namespace provip

@@ -1,0 +1,448 @@
+// Attention behind the pruning on the CUDA cores: fp32 tensors (FFMA, no reduced
+// precision), and bf16 on request.
+#include "attention.cuh"
+
+namespace provip {
+namespace {
+
+// ---------------------------------------------------------------------------
+// tiles of 64 rows by 64 keys
+//
+// A CTA holds 64 packed rows of a key/value head (Q in shared memory as fp32, 8 rows of
+// scores and of the output in each thread's registers) and passes over its keys once in
+// tiles of 64 with a running maximum and sum. Bound by the FFMA pipe: a thread's 8 x 4
+// scores take 12 16-byte loads from shared memory per 128 FFMA, its 8 x 8 outputs 16 per 256.
+// ---------------------------------------------------------------------------
+constexpr int kBM = 64, kBN = 64, kThr = 128;
+constexpr int kPitch = kHeadDim + 4;  // floats a row: rows 4 banks apart, 16 bytes aligned
+constexpr int kPPitch = kBN + 4;
+constexpr size_t kTileSmem = sizeof(float) * ((size_t)(kBM + 2 * kBN) * kPitch + (size_t)kBM * kPPitch);
+
+template <typename T>
+__device__ __forceinline__ void fill_row(float* dst, const T* src, int lane32) {
+  float v[4];
+  load4(src + lane32 * 4, v);
+  *reinterpret_cast<float4*>(dst + lane32 * 4) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void zero_row(float* dst, int lane32) {
+  *reinterpret_cast<float4*>(dst + lane32 * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+// blockIdx: x row tile, y = key/value head * parts + part, z sequence. PREFIX: the rows of
+// every request's token against the prefix alone (paged), parts part0 .. part0 + n - 1.
+template <typename T, bool PREFIX>
+__global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant__ AttnArgs a, int part0, int n_parts) {
+  extern __shared__ __align__(16) float sm[];
+  float* qs = sm;
+  float* ks = qs + kBM * kPitch;
+  float* vs = ks + kBN * kPitch;
+  float* ps = vs + kBN * kPitch;
+  const int R = a.H_q / a.H_kv, g = blockIdx.y / n_parts, part = blockIdx.y % n_parts, b = blockIdx.z;
+  AttnSeq s;
+  if (PREFIX) {
+    s.q0 = 0;
+    s.q_len = a.B;
+    s.k_len = 0;
+    s.k0 = 0;
+    s.pages = nullptr;
+    s.ok = true;
+  } else {
+    s = attn_seq(a, b);
+    if (!s.ok && threadIdx.x == 0) set_error(a.err, kErrBadDeviceArg);
+  }
+  const int n_rows = s.q_len * R, r0 = blockIdx.x * kBM;
+  if (r0 >= n_rows) return;
+  const int rows = min(kBM, n_rows - r0);
+  const int P = a.prefix_len;
+  // keys of the list that some row of the tile sees, and this part's share of their tiles
+  const int n_keys = P + (PREFIX ? 0 : attn_visible(a, s.q_len, s.k_len, (r0 + rows - 1) / R));
+  const int n_tiles = (n_keys + kBN - 1) / kBN, per = (n_tiles + n_parts - 1) / n_parts;
+  const int k_lo = min(part * per * kBN, n_keys), k_hi = min((part + 1) * per * kBN, n_keys);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;  // rows ty*8.., columns tx + 16 j / 4 tx..
+
+  for (int r = warp; r < kBM; r += kThr / 32) {
+    if (r < rows) {
+      const int t = (r0 + r) / R, h = g * R + (r0 + r) % R;
+      fill_row(qs + r * kPitch, static_cast<const T*>(a.Q) + (size_t)(s.q0 + t) * a.q_stride + (size_t)h * kHeadDim, lane);
+    } else {
+      zero_row(qs + r * kPitch, lane);
+    }
+  }
+  int lim[8];  // keys of the list that each row sees
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + ty * 8 + i;
+    lim[i] = r < n_rows ? P + (PREFIX ? 0 : attn_visible(a, s.q_len, s.k_len, r / R)) : 0;
+  }
+  float o[8][8], m[8], l[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[i][j] = 0.f;
+  }
+  for (int k0 = k_lo; k0 < k_hi; k0 += kBN) {
+    __syncthreads();
+    for (int j = warp; j < kBN; j += kThr / 32) {
+      const int key = k0 + j;
+      if (key < k_hi) {
+        const bool pre = key < P;
+        fill_row(ks + j * kPitch, pre ? attn_prefix_row<T>(a, false, key, g) : attn_own_row<T>(a, s, false, key - P, g), lane);
+        fill_row(vs + j * kPitch, pre ? attn_prefix_row<T>(a, true, key, g) : attn_own_row<T>(a, s, true, key - P, g), lane);
+      } else {
+        zero_row(ks + j * kPitch, lane);
+        zero_row(vs + j * kPitch, lane);
+      }
+    }
+    __syncthreads();
+    float x[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
+#pragma unroll 2
+    for (int d = 0; d < kHeadDim; d += 4) {
+      float4 kv[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(ks + (tx + 16 * j) * kPitch + d);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 qv = *reinterpret_cast<const float4*>(qs + (ty * 8 + i) * kPitch + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, x[i][j]))));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[i][j] = k0 + tx + 16 * j < min(lim[i], k_hi) ? x[i][j] * a.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, x[i][j]);
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+      const float mn = fmaxf(m[i], mx), base = mn == -INFINITY ? 0.f : mn;
+      const float r = exp2f(m[i] - base);
+      m[i] = mn;
+      float t = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = exp2f(x[i][j] - base);
+        t += p;
+        ps[(ty * 8 + i) * kPPitch + tx + 16 * j] = p;
+      }
+      l[i] = l[i] * r + t;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[i][j] *= r;
+    }
+    __syncwarp();  // a row's probabilities are written and read by the same 16 lanes
+#pragma unroll 1
+    for (int k = 0; k < kBN; k += 4) {
+      float4 p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = *reinterpret_cast<const float4*>(ps + (ty * 8 + i) * kPPitch + k);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const float4 v0 = *reinterpret_cast<const float4*>(vs + (k + kk) * kPitch + tx * 4);
+        const float4 v1 = *reinterpret_cast<const float4*>(vs + (k + kk) * kPitch + 64 + tx * 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float w = kk == 0 ? p[i].x : kk == 1 ? p[i].y : kk == 2 ? p[i].z : p[i].w;
+          o[i][0] = fmaf(w, v0.x, o[i][0]);
+          o[i][1] = fmaf(w, v0.y, o[i][1]);
+          o[i][2] = fmaf(w, v0.z, o[i][2]);
+          o[i][3] = fmaf(w, v0.w, o[i][3]);
+          o[i][4] = fmaf(w, v1.x, o[i][4]);
+          o[i][5] = fmaf(w, v1.y, o[i][5]);
+          o[i][6] = fmaf(w, v1.z, o[i][6]);
+          o[i][7] = fmaf(w, v1.w, o[i][7]);
+        }
+      }
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+    const int r = r0 + ty * 8 + i;
+    const bool live = r < n_rows;
+    const int t = r / R, h = g * R + r % R;
+    const size_t row = (size_t)(s.q0 + t) * a.H_q + h;
+    bool fine = true;
+    const float den = l[i] == 0.f ? 1.f : l[i];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      o[i][j] /= den;
+      fine = fine && isfinite(o[i][j]);
+    }
+    float lse = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
+    if (live && fine && !isnan(lse)) {
+      if (a.n_part > 1) {
+        float* po = a.part_o + ((size_t)(part0 + part) * a.T_q * a.H_q + row) * kHeadDim;
+        store4(po + tx * 4, o[i]);
+        store4(po + 64 + tx * 4, o[i] + 4);
+        if (tx == 0) a.part_lse[(size_t)(part0 + part) * a.T_q * a.H_q + row] = lse;
+      } else {
+        if (l[i] == 0.f && lim[i] > 0) {
+          lse = NAN;  // every score is -inf: 0 / 0, as the formula has it
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[i][j] = NAN;
+        }
+        T* op = static_cast<T*>(a.out) + (size_t)(s.q0 + t) * a.o_stride + (size_t)h * kHeadDim;
+        store4(op + tx * 4, o[i]);
+        store4(op + 64 + tx * 4, o[i] + 4);
+        if (tx == 0 && a.lse) a.lse[row] = lse * kLn2;
+      }
+    }
+    // rows that are not finite, one at a time by the whole warp
+    unsigned bad = __ballot_sync(0xffffffffu, live && !(fine && !isnan(lse)));
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      if (!((bad >> (16 * half)) & 0xffffu)) continue;
+      const int rb = __shfl_sync(0xffffffffu, r, 16 * half), tb = rb / R, hb = g * R + rb % R;
+      const int hi = min(__shfl_sync(0xffffffffu, lim[i], 16 * half), k_hi);
+      float ob[4];
+      float lb = attn_row_plain<T>(a, s, P, tb, hb, k_lo, hi, ob);
+      const size_t rowb = (size_t)(s.q0 + tb) * a.H_q + hb;
+      if (a.n_part > 1) {
+        store4(a.part_o + ((size_t)(part0 + part) * a.T_q * a.H_q + rowb) * kHeadDim + lane * 4, ob);
+        if (lane == 0) a.part_lse[(size_t)(part0 + part) * a.T_q * a.H_q + rowb] = lb;
+      } else {
+        if (lb == -INFINITY) lb = ob[0] = ob[1] = ob[2] = ob[3] = NAN;
+        store4(static_cast<T*>(a.out) + (size_t)(s.q0 + tb) * a.o_stride + (size_t)hb * kHeadDim + lane * 4, ob);
+        if (lane == 0 && a.lse) a.lse[rowb] = lb * kLn2;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// one token against its request's own pages
+//
+// A CTA takes one part of a request's keys for up to RT heads of a group. Each warp
+// passes over its keys, four elements of a row per lane and four keys' rows in flight, with
+// its own running maximum and sum; the warps are joined in shared memory at the end. Bound
+// by HBM: every key and
+// value row is read once for the RT heads.
+// ---------------------------------------------------------------------------
+constexpr int kDecThr = 256;
+
+// blockIdx: x = key/value head * heads' tiles + tile, y part, z request
+template <typename T, int RT>
+__global__ void __launch_bounds__(kDecThr) attn_token_simt(const __grid_constant__ AttnArgs a, int n_own) {
+  constexpr int kUnroll = 4, kWarps = kDecThr / 32;
+  const int R = a.H_q / a.H_kv, n_rt = (R + RT - 1) / RT;
+  const int g = blockIdx.x / n_rt, h0 = g * R + (blockIdx.x % n_rt) * RT, part = blockIdx.y, b = blockIdx.z;
+  const int nh = min(RT, g * R + R - h0);
+  const AttnSeq s = attn_seq(a, b);
+  if (!s.ok && threadIdx.x == 0) set_error(a.err, kErrBadDeviceArg);
+  const int per = (s.k_len + n_own - 1) / n_own;
+  const int k_lo = min(part * per, s.k_len), k_hi = min(k_lo + per, s.k_len);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  float q[RT][4], o[RT][4], m[RT], l[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[r][e] = o[r][e] = 0.f;
+    if (r < nh) {
+      load4(static_cast<const T*>(a.Q) + (size_t)b * a.q_stride + (size_t)(h0 + r) * kHeadDim + lane * 4, q[r]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[r][e] *= a.scale_log2;
+    }
+  }
+  for (int j0 = k_lo + warp * kUnroll; j0 < k_hi; j0 += kWarps * kUnroll) {
+    float k[kUnroll][4], v[kUnroll][4];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int j = min(j0 + u, k_hi - 1);
+      load4(attn_own_row<T>(a, s, false, j, g) + lane * 4, k[u]);
+      load4(attn_own_row<T>(a, s, true, j, g) + lane * 4, v[u]);
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      float x[kUnroll], mx = m[r];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        x[u] = warp_sum(fmaf(q[r][0], k[u][0], fmaf(q[r][1], k[u][1], fmaf(q[r][2], k[u][2], q[r][3] * k[u][3]))));
+        if (j0 + u >= k_hi) x[u] = -INFINITY;
+        mx = fmaxf(mx, x[u]);
+      }
+      const float base = mx == -INFINITY ? 0.f : mx, c = exp2f(m[r] - base);
+      m[r] = mx;
+      l[r] *= c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[r][e] *= c;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (j0 + u < k_hi) {
+          const float p = exp2f(x[u] - base);
+          l[r] += p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[r][e] = fmaf(p, v[u][e], o[r][e]);
+        }
+      }
+    }
+  }
+  __shared__ float so[kWarps][kHeadDim];
+  __shared__ float sml[kWarps][2];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    if (r >= nh) break;
+    __syncthreads();
+    store4(&so[warp][lane * 4], o[r]);
+    if (lane == 0) {
+      sml[warp][0] = m[r];
+      sml[warp][1] = l[r];
+    }
+    __syncthreads();
+    if (threadIdx.x < kHeadDim) {
+      float mx = -INFINITY, acc = 0.f, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, sml[w][0]);
+      const float base = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float c = exp2f(sml[w][0] - base);
+        sum = fmaf(sml[w][1], c, sum);
+        if (sml[w][1] != 0.f) acc = fmaf(so[w][threadIdx.x], c, acc);
+      }
+      const size_t row = (size_t)b * a.H_q + h0 + r;
+      float val = sum == 0.f ? 0.f : acc / sum, lse = sum == 0.f ? -INFINITY : mx + log2f(sum);
+      if (a.n_part > 1) {
+        a.part_o[((size_t)part * a.T_q * a.H_q + row) * kHeadDim + threadIdx.x] = val;
+        if (threadIdx.x == 0) a.part_lse[(size_t)part * a.T_q * a.H_q + row] = lse;
+      } else {
+        if (sum == 0.f && s.k_len > 0) val = lse = NAN;  // every score is -inf
+        T* op = static_cast<T*>(a.out) + (size_t)b * a.o_stride + (size_t)(h0 + r) * kHeadDim;
+        op[threadIdx.x] = static_cast<T>(val);
+        if (threadIdx.x == 0 && a.lse) a.lse[row] = lse * kLn2;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// parts of a row -> the row: a warp per (token, head)
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(256) attn_join(const __grid_constant__ AttnArgs a) {
+  pdl_wait_prior();
+  const int lane = threadIdx.x & 31;
+  const long long n_rows = (long long)a.T_q * a.H_q, row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= n_rows) return;
+  const int t = (int)(row / a.H_q), h = (int)(row % a.H_q);
+  int n_vis = a.prefix_len;
+  if (a.paged) {
+    n_vis += attn_seq(a, t).k_len;
+  } else {
+    // the sequence that holds token t; rows outside every sequence are left untouched
+    bool found = false;
+    for (int b0 = 0; b0 < a.B && !found; b0 += 32) {
+      AttnSeq s;
+      bool mine = false;
+      if (b0 + lane < a.B) {
+        s = attn_seq(a, b0 + lane);
+        mine = s.ok && t >= s.q0 && t - s.q0 < s.q_len;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, mine);
+      if (hit) {
+        found = true;
+        n_vis += __shfl_sync(0xffffffffu, mine ? attn_visible(a, s.q_len, s.k_len, t - s.q0) : 0, __ffs(hit) - 1);
+      }
+    }
+    if (!found) return;
+  }
+  float mx = -INFINITY;
+  for (int p = lane; p < a.n_part; p += 32) mx = fmaxf(mx, a.part_lse[(size_t)p * n_rows + row]);
+  mx = warp_max(mx);
+  const float base = mx == -INFINITY ? 0.f : mx;
+  float o[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < a.n_part; ++p) {
+    const float w = exp2f(a.part_lse[(size_t)p * n_rows + row] - base);
+    const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((size_t)p * n_rows + row) * kHeadDim + lane * 4);
+    sum += w;
+    if (w != 0.f) {
+      o[0] = fmaf(w, v.x, o[0]);
+      o[1] = fmaf(w, v.y, o[1]);
+      o[2] = fmaf(w, v.z, o[2]);
+      o[3] = fmaf(w, v.w, o[3]);
+    }
+  }
+  const float den = sum == 0.f ? (n_vis > 0 ? NAN : 1.f) : sum;  // every score -inf: 0 / 0, as the formula has it
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] /= den;
+  store4(static_cast<T*>(a.out) + (size_t)t * a.o_stride + (size_t)h * kHeadDim + lane * 4, o);
+  if (lane == 0 && a.lse)
+    a.lse[row] = sum == 0.f ? (n_vis > 0 ? NAN : -INFINITY) : (mx + log2f(sum)) * kLn2;
+}
+
+template <typename T, bool PREFIX>
+cudaError_t tile_launch(const AttnArgs& a, dim3 grid, int part0, int n_parts, cudaStream_t s) {
+  static std::atomic<bool> configured[64];  // per device, zero-initialised
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    cudaError_t e = cudaFuncSetAttribute(attn_tile_simt<T, PREFIX>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)kTileSmem);
+    if (e != cudaSuccess) return e;
+    configured[dev] = true;
+  }
+  attn_tile_simt<T, PREFIX><<<grid, kThr, kTileSmem, s>>>(a, part0, n_parts);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t token_launch(const AttnArgs& a, int n_own, cudaStream_t s) {
+  const int R = a.H_q / a.H_kv;
+  // heads that share a key row's load: as many as the group has, four at most
+  const dim3 grid((unsigned)(a.H_kv * (R == 1 ? 1 : R == 2 ? 1 : (R + 3) / 4)), (unsigned)n_own, (unsigned)a.B);
+  if (R == 1)
+    attn_token_simt<T, 1><<<grid, kDecThr, 0, s>>>(a, n_own);
+  else if (R == 2)
+    attn_token_simt<T, 2><<<grid, kDecThr, 0, s>>>(a, n_own);
+  else
+    attn_token_simt<T, 4><<<grid, kDecThr, 0, s>>>(a, n_own);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t prompt_simt(const AttnArgs& a, cudaStream_t s) {
+  const long long rows = (long long)a.q_len_max * (a.H_q / a.H_kv);
+  return tile_launch<T, false>(a, dim3((unsigned)((rows + kBM - 1) / kBM), (unsigned)(a.H_kv * a.n_part), (unsigned)a.B),
+                               0, a.n_part, s);
+}
+template <typename T>
+cudaError_t decode_simt(const AttnArgs& a, int n_own, cudaStream_t s) {
+  cudaError_t e = n_own > 0 ? token_launch<T>(a, n_own, s) : cudaSuccess;
+  if (e != cudaSuccess || a.n_part == n_own) return e;
+  const long long rows = (long long)a.B * (a.H_q / a.H_kv);
+  const int n = a.n_part - n_own;
+  return tile_launch<T, true>(a, dim3((unsigned)((rows + kBM - 1) / kBM), (unsigned)(a.H_kv * n), 1), n_own, n, s);
+}
+
+}  // namespace
+
+cudaError_t attn_prompt_simt_launch(const AttnArgs& a, int dtype, cudaStream_t s) {
+  return dtype == 0 ? prompt_simt<float>(a, s) : prompt_simt<__nv_bfloat16>(a, s);
+}
+
+cudaError_t attn_decode_simt_launch(const AttnArgs& a, int n_own, int dtype, cudaStream_t s) {
+  return dtype == 0 ? decode_simt<float>(a, n_own, s) : decode_simt<__nv_bfloat16>(a, n_own, s);
+}
+
+cudaError_t attn_join_launch(const AttnArgs& a, int dtype, cudaStream_t s) {
+  const dim3 grid((unsigned)(((long long)a.T_q * a.H_q + 7) / 8));
+  return dtype == 0 ? launch_pdl(attn_join<float>, grid, dim3(256), 0, s, a)
+                    : launch_pdl(attn_join<__nv_bfloat16>, grid, dim3(256), 0, s, a);
+}
+
+}  // namespace provip

@@ -283,6 +283,79 @@ cudaError_t merge_argmax_pair_launch(const SimArgs& a, const int* keep_idx, int 
                                      const int* pruned, const void* perm, const MergePairPlan& plan,
                                      float* ws_best, int* ws_bidx, cudaStream_t s);
 
+// ---------------------------------------------------------------------------
+// attention behind the pruning (attention.cuh has the conventions)
+// ---------------------------------------------------------------------------
+struct AttnArgs {
+  const void* Q;             // rows [T_q][H_q][d_h], q_stride elements apart
+  const void* K;             // own keys: rows [T_k][H_kv][d_h], or the pool's slots (paged)
+  const void* V;
+  const void* Kp;            // prefix keys: rows of their own, or the pool's slots (paged)
+  const void* Vp;
+  long long q_stride, k_stride, v_stride, kp_stride, vp_stride, o_stride;
+  int T_q, T_k, B, H_q, H_kv;
+  const int* q_start;        // contiguous keys: [B] first token and tokens of each sequence,
+  const int* q_len;          // first own key row and own keys
+  const int* k_start;
+  const int* k_len;          // both: own keys [B]
+  int q_len_max, k_len_max;
+  int prefix_len, causal;
+  int paged;                 // one token per request, keys through tables
+  int page_size, page_shift, n_pages, max_pages;
+  const int* block_table;    // [B][max_pages]
+  const int* prefix_table;   // pages of the prefix
+  float scale_log2;          // scale * log2(e)
+  void* out;                 // rows [T_q][H_q][d_h], o_stride elements apart
+  float* lse;                // [T_q][H_q] natural log, or null
+  // partial results, when a row's keys are shared out over n_part parts: of part p,
+  // part_o[(p T_q + t) H_q + h][d_h] and part_lse[(p T_q + t) H_q + h] (base 2)
+  int n_part;
+  float* part_o;
+  float* part_lse;
+  unsigned* err;
+};
+// CUDA-core forms. Prompt: 64-row tiles, split over the keys n_part ways.
+cudaError_t attn_prompt_simt_launch(const AttnArgs& a, int dtype, cudaStream_t s);
+// One token per request: own keys in parts 0 .. n_own - 1, the prefix's in the others
+// (64-row tiles over the tokens of every request).
+cudaError_t attn_decode_simt_launch(const AttnArgs& a, int n_own, int dtype, cudaStream_t s);
+// joins n_part parts of every row into out and lse
+cudaError_t attn_join_launch(const AttnArgs& a, int dtype, cudaStream_t s);
+
+// ---------------------------------------------------------------------------
+// paged key/value cache
+// ---------------------------------------------------------------------------
+struct PageTablesArgs {
+  const int* kv_len;         // [B]
+  const int* new_len;        // [B]
+  int B, page_shift;
+  int* free_pages;           // [n_free_max]: stack, the top at free_count - 1
+  int n_free_max;
+  const int* free_count;
+  int* block_table;          // [B][max_pages]
+  int max_pages, T_max;
+  int* kv_len_out;           // [B]
+  int* row_start_out;        // [B + 1]
+  int* slot_map_out;         // [T_max]
+  int* free_count_out;
+  unsigned* err;
+};
+cudaError_t page_tables_launch(const PageTablesArgs& a, cudaStream_t s);
+
+struct KvAppendArgs {
+  const char* K;             // T rows of row_bytes, strides in bytes
+  const char* V;
+  long long k_stride, v_stride;
+  int T;
+  long long row_bytes;
+  const int* slot_map;       // [T]
+  long long n_slots;
+  char* k_pages;
+  char* v_pages;
+  unsigned* err;
+};
+cudaError_t kv_append_launch(const KvAppendArgs& a, cudaStream_t s);
+
 // host helper: encode a 2-D bf16 row table [rows, cols] (row stride in bytes)
 // as a tensor map with 64 x box_rows boxes and 128-byte swizzle.
 int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,

@@ -33,6 +33,8 @@ PRUNE_HOST_ROWS = 4
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int
+_L = ctypes.c_longlong
+_F = ctypes.c_float
 _Z = ctypes.c_size_t
 
 # name -> (restype, argtypes); mirrors include/provip.h
@@ -73,6 +75,14 @@ _SIGS = {
     "provip_prune_visual_heads": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _I, _I, _I, _P,
                                        _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z,
                                        ctypes.c_uint, _P]),
+    "provip_prompt_attention_workspace_size": (_Z, [_I] * 9),
+    "provip_prompt_attention": (_I, [_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I, _I, _P, _L, _P,
+                                     _L, _I, _I, _F, _I, _I, _P, _L, _P, _P, _Z, _P]),
+    "provip_page_tables": (_I, [_P, _P, _I, _I, _P, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P]),
+    "provip_kv_append": (_I, [_P, _L, _P, _L, _I, _I, _I, _P, _I, _I, _I, _P, _P, _P]),
+    "provip_decode_attention_workspace_size": (_Z, [_I] * 7),
+    "provip_decode_attention": (_I, [_P, _L, _I, _I, _I, _I, _P, _P, _I, _I, _P, _I, _P, _I, _P, _I, _F, _I, _I, _P, _L,
+                                     _P, _P, _Z, _P]),
 }
 
 
@@ -532,3 +542,180 @@ def provip_prune_visual_heads(Q, K, V, hidden, pos, text_start, text_len, seq_le
                                                    else int(text_len.max().item())))
     step = VisualHeadsPruneStep(Q, K, V, hidden, pos, Ntm, N_v, keep, N_vis, algo)
     return step(Q, K, V, hidden, pos, text_start, text_len, seq_len, vis_start, crit_mask)
+
+
+# ---------------------------------------------------------------------------
+# behind the pruning: attention over prompts, paged cache, decoding
+# ---------------------------------------------------------------------------
+def _rows(t, H, dtype, what):
+    """pointer and row stride (elements) of a [T, H, 128] tensor whose heads lie next to each
+    other; a slice of a fused query/key/value buffer is fine"""
+    if not t.is_cuda:
+        raise ProvipError(ERR_INVALID_ARG, "tensor must live on the GPU")
+    if t.dtype != dtype:
+        raise ProvipError(ERR_INVALID_ARG, f"{what}: dtype {t.dtype}, not {dtype}")
+    n, h, d = t.shape
+    s0, s1, s2 = t.stride()
+    if h != H or d != 128:
+        raise ProvipError(ERR_INVALID_ARG, f"{what}: shape {tuple(t.shape)}, not [rows, {H}, 128]")
+    if n and (s2 != 1 or (s1 != 128 and h > 1)):
+        raise ProvipError(ERR_INVALID_ARG, f"{what}: the heads of a row must lie next to each other")
+    return t.data_ptr(), (s0 if n > 1 else h * 128)
+
+
+def _ints(t, n, what):
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+        raise ProvipError(ERR_INVALID_ARG, f"{what} must be a contiguous int32 GPU tensor of {n} entries")
+    return t.data_ptr()
+
+
+def _dtype_of(dtype):
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ProvipError(ERR_UNSUPPORTED, f"unsupported dtype {dtype}")
+    return F32 if dtype == torch.float32 else BF16
+
+
+class PromptAttention:
+    """Pre-allocated outputs + workspace for repeated provip_prompt_attention calls (one shape):
+    T_q query rows of B sequences, at most q_len_max rows and k_len_max own keys each, behind
+    prefix_len shared keys. With T_q = B * L_max, q_start = b * L_max and the lengths of a
+    pruning step it takes that step's padded layout."""
+
+    def __init__(self, T_q, B, H_q, H_kv, q_len_max, k_len_max, prefix_len=0, causal=True, scale=None,
+                 dtype=torch.bfloat16, device="cuda", algo=ALGO_AUTO, want_lse=True):
+        self.shape = (int(T_q), int(B), int(H_q), int(H_kv), int(q_len_max), int(k_len_max), int(prefix_len))
+        self.causal, self.algo, self.dtype, self._dt = int(bool(causal)), int(algo), dtype, _dtype_of(dtype)
+        self.scale = 128 ** -0.5 if scale is None else float(scale)
+        dev = torch.device(device)
+        self.out = torch.empty((T_q, H_q, 128), dtype=dtype, device=dev)
+        self.lse = torch.empty((T_q, H_q), dtype=torch.float32, device=dev) if want_lse else None
+        self.ws = workspace(lib().provip_prompt_attention_workspace_size(*self.shape, self._dt, self.algo), dev)
+
+    def __call__(self, Q, K, V, q_start, q_len, k_start, k_len, K_prefix=None, V_prefix=None):
+        """Q [T_q, H_q, 128], K and V [T_k, H_kv, 128], the prefix's [prefix_len, H_kv, 128];
+        starts and lengths int32 [B] on the device. Returns dict(out, lse)."""
+        T_q, B, H_q, H_kv, qm, km, P = self.shape
+        if Q.shape[0] != T_q or K.shape[0] != V.shape[0]:
+            raise ProvipError(ERR_INVALID_ARG, "prompt_attention: Q, K or V has another number of rows")
+        q, qs = _rows(Q, H_q, self.dtype, "Q")
+        k, ks = _rows(K, H_kv, self.dtype, "K")
+        v, vs = _rows(V, H_kv, self.dtype, "V")
+        kp = vp = None
+        kps = vps = 0
+        if P:
+            if K_prefix is None or V_prefix is None or K_prefix.shape[0] < P or V_prefix.shape[0] < P:
+                raise ProvipError(ERR_INVALID_ARG, f"prompt_attention: the prefix needs {P} rows")
+            kp, kps = _rows(K_prefix, H_kv, self.dtype, "K_prefix")
+            vp, vps = _rows(V_prefix, H_kv, self.dtype, "V_prefix")
+        rc = lib().provip_prompt_attention(
+            q, qs, k, ks, v, vs, T_q, K.shape[0], B, H_q, H_kv, 128, _ints(q_start, B, "q_start"),
+            _ints(q_len, B, "q_len"), _ints(k_start, B, "k_start"), _ints(k_len, B, "k_len"), qm, km, kp, kps, vp, vps, P,
+            self.causal, self.scale, self._dt, self.algo, self.out.data_ptr(), H_q * 128,
+            None if self.lse is None else self.lse.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream(Q.device))
+        _check(rc, "provip_prompt_attention")
+        return dict(out=self.out, lse=self.lse)
+
+
+def provip_prompt_attention(Q, K, V, q_start, q_len, k_start, k_len, q_len_max, k_len_max, K_prefix=None,
+                            V_prefix=None, causal=True, scale=None, algo=ALGO_AUTO, want_lse=True):
+    """One call of PromptAttention, its outputs and workspace allocated here."""
+    step = PromptAttention(Q.shape[0], q_len.numel(), Q.shape[1], K.shape[1], q_len_max, k_len_max,
+                           0 if K_prefix is None else K_prefix.shape[0], causal, scale, Q.dtype, Q.device, algo, want_lse)
+    return step(Q, K, V, q_start, q_len, k_start, k_len, K_prefix, V_prefix)
+
+
+class PageTables:
+    """Pre-allocated outputs for repeated provip_page_tables calls: B requests, pages of
+    page_size rows, at most T_max new tokens a step."""
+
+    def __init__(self, B, page_size, T_max, device="cuda"):
+        dev = torch.device(device)
+        self.B, self.page_size, self.T_max = int(B), int(page_size), int(T_max)
+        self.kv_len = torch.empty(B, dtype=torch.int32, device=dev)
+        self.row_start = torch.empty(B + 1, dtype=torch.int32, device=dev)
+        self.slot_map = torch.empty(T_max, dtype=torch.int32, device=dev)
+        self.free_count = torch.empty(1, dtype=torch.int32, device=dev)
+
+    def __call__(self, kv_len, new_len, free_pages, free_count, block_table, inplace=False):
+        """kv_len, new_len [B], free_pages (the stack) and block_table [B, max_pages] (both updated),
+        free_count [1]: int32 on the device. inplace: kv_len and free_count are updated too instead
+        of leaving the new ones in self. Returns dict(kv_len, row_start, slot_map, free_count)."""
+        B = self.B
+        kv_out, fc_out = (kv_len, free_count) if inplace else (self.kv_len, self.free_count)
+        if block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ProvipError(ERR_INVALID_ARG, f"block_table must be [{B}, max_pages]")
+        rc = lib().provip_page_tables(
+            _ints(kv_len, B, "kv_len"), _ints(new_len, B, "new_len"), B, self.page_size,
+            _ints(free_pages, 0, "free_pages"), free_pages.numel(), _ints(free_count, 1, "free_count"),
+            _ints(block_table, 0, "block_table"), block_table.shape[1], self.T_max, kv_out.data_ptr(),
+            self.row_start.data_ptr(), self.slot_map.data_ptr(), fc_out.data_ptr(), _stream(kv_len.device))
+        _check(rc, "provip_page_tables")
+        return dict(kv_len=kv_out, row_start=self.row_start, slot_map=self.slot_map, free_count=fc_out)
+
+
+def _pages(t, dtype, what):
+    if not t.is_cuda or not t.is_contiguous() or t.dim() != 4 or t.dtype != dtype:
+        raise ProvipError(ERR_INVALID_ARG, f"{what} must be a contiguous {dtype} GPU tensor [n_pages, page_size, H_kv, d_h]")
+    return t.data_ptr()
+
+
+def provip_kv_append(K, V, slot_map, k_pages, v_pages):
+    """Rows of K and V [T, H_kv, d_h] into the slots slot_map [T] of k_pages and v_pages
+    [n_pages, page_size, H_kv, d_h]; negative slots are skipped."""
+    T, H, d = K.shape
+    if V.shape != K.shape or V.dtype != K.dtype or k_pages.shape[2:] != K.shape[1:] or v_pages.shape != k_pages.shape:
+        raise ProvipError(ERR_INVALID_ARG, "kv_append: K, V and the pages must agree in shape and dtype")
+    if not (K.is_cuda and V.is_cuda):
+        raise ProvipError(ERR_INVALID_ARG, "tensor must live on the GPU")
+    for t in (K, V):
+        if T and (t.stride(2) != 1 or (t.stride(1) != d and H > 1)):
+            raise ProvipError(ERR_INVALID_ARG, "kv_append: the heads of a row must lie next to each other")
+    rc = lib().provip_kv_append(K.data_ptr(), K.stride(0) if T > 1 else H * d, V.data_ptr(),
+                                V.stride(0) if T > 1 else H * d, T, H, d, _ints(slot_map, T, "slot_map"),
+                                k_pages.shape[0], k_pages.shape[1], _dtype_code(K), _pages(k_pages, K.dtype, "k_pages"),
+                                _pages(v_pages, K.dtype, "v_pages"), _stream(K.device))
+    _check(rc, "provip_kv_append")
+
+
+class DecodeAttention:
+    """Pre-allocated outputs + workspace for repeated provip_decode_attention calls: one token of
+    B requests, each behind prefix_len shared tokens and at most kv_len_max of its own."""
+
+    def __init__(self, B, H_q, H_kv, kv_len_max, prefix_len=0, scale=None, dtype=torch.bfloat16, device="cuda",
+                 algo=ALGO_AUTO, want_lse=True):
+        self.shape = (int(B), int(H_q), int(H_kv), int(kv_len_max), int(prefix_len))
+        self.algo, self.dtype, self._dt = int(algo), dtype, _dtype_of(dtype)
+        self.scale = 128 ** -0.5 if scale is None else float(scale)
+        dev = torch.device(device)
+        self.out = torch.empty((B, H_q, 128), dtype=dtype, device=dev)
+        self.lse = torch.empty((B, H_q), dtype=torch.float32, device=dev) if want_lse else None
+        self.ws = workspace(lib().provip_decode_attention_workspace_size(*self.shape, self._dt, self.algo), dev)
+
+    def __call__(self, Q, k_pages, v_pages, block_table, kv_len, prefix_table=None):
+        """Q [B, H_q, 128]; k_pages, v_pages [n_pages, page_size, H_kv, 128]; block_table
+        [B, max_pages], kv_len [B] and the prefix's pages int32 on the device. Returns dict(out, lse)."""
+        B, H_q, H_kv, km, P = self.shape
+        if Q.shape[0] != B or block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ProvipError(ERR_INVALID_ARG, f"decode_attention: Q and block_table must have {B} rows")
+        if k_pages.shape[2:] != (H_kv, 128) or v_pages.shape != k_pages.shape:
+            raise ProvipError(ERR_INVALID_ARG, f"decode_attention: pages must be [n_pages, page_size, {H_kv}, 128]")
+        q, qs = _rows(Q, H_q, self.dtype, "Q")
+        if P and prefix_table is None:
+            raise ProvipError(ERR_INVALID_ARG, "decode_attention: the prefix needs its pages' table")
+        ps = k_pages.shape[1]
+        rc = lib().provip_decode_attention(
+            q, qs, B, H_q, H_kv, 128, _pages(k_pages, self.dtype, "k_pages"), _pages(v_pages, self.dtype, "v_pages"),
+            k_pages.shape[0], ps, _ints(block_table, 0, "block_table"), block_table.shape[1], _ints(kv_len, B, "kv_len"),
+            km, _ints(prefix_table, -(-P // ps), "prefix_table") if P else None, P, self.scale, self._dt, self.algo,
+            self.out.data_ptr(), H_q * 128, None if self.lse is None else self.lse.data_ptr(), self.ws.data_ptr(),
+            self.ws.numel(), _stream(Q.device))
+        _check(rc, "provip_decode_attention")
+        return dict(out=self.out, lse=self.lse)
+
+
+def provip_decode_attention(Q, k_pages, v_pages, block_table, kv_len, kv_len_max, prefix_table=None, prefix_len=0,
+                            scale=None, algo=ALGO_AUTO, want_lse=True):
+    """One call of DecodeAttention, its outputs and workspace allocated here."""
+    step = DecodeAttention(Q.shape[0], Q.shape[1], k_pages.shape[2], kv_len_max, prefix_len, scale, Q.dtype, Q.device,
+                           algo, want_lse)
+    return step(Q, k_pages, v_pages, block_table, kv_len, prefix_table)
