@@ -1179,24 +1179,80 @@ int attn_parts(long long units, int n_keys, long long want, int min_keys, int mo
   return n < 1 ? 1 : (int)n;
 }
 
-int attn_algo(int algo, int dtype) {
-  (void)dtype;
-  return algo == PROVIP_ALGO_AUTO ? PROVIP_ALGO_SIMT : algo;
+bool attn_tc_form(int algo, int dtype) {
+  return algo == PROVIP_ALGO_TCGEN05 || (algo == PROVIP_ALGO_AUTO && dtype == PROVIP_BF16);
 }
 
-// row tiles of 64 packed rows; a part has four 64-key tiles or more
-int prompt_parts(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int prefix_len) {
-  const long long tiles = ((long long)q_len_max * (H_q / H_kv) + 63) / 64;
-  const int keys = prefix_len > 0x7fffffff - k_len_max ? 0x7fffffff : prefix_len + k_len_max;
-  const int n = attn_parts(tiles * H_kv * B, keys, 2 * kPlanSms, 256, 32);
-  return n < 1 ? 1 : n;
-}
+// How a call's work is cut up, from its host-side sizes alone.
+struct AttnCut {
+  bool tc;
+  int n_own, n_prefix, n_part;  // parts of a row's keys (prompt: n_part only)
+  AttnPlan plan;                // tensor cores
+};
 
-void decode_parts(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int* n_own, int* n_prefix) {
+// CUDA cores: row tiles of 64 packed rows, parts of four 64-key tiles or more. Tensor cores:
+// two row tiles of 128 a CTA, one where a sequence's rows fit in it (two CTAs then share an
+// SM); the keys are shared out where the units leave half of the CTAs without work, four
+// 128-key tiles or more a part (a second launch joins the parts, about two tiles' time).
+AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int prefix_len, int dtype, int algo) {
+  AttnCut c;
+  memset(&c, 0, sizeof(c));
   const int R = H_q / H_kv;
-  *n_own = attn_parts((long long)B * H_kv * (R <= 2 ? 1 : (R + 3) / 4), kv_len_max, 4 * kPlanSms, 64, 64);
-  *n_prefix = attn_parts(((long long)B * R + 63) / 64 * H_kv, prefix_len, 2 * kPlanSms, 256, 64);
-  if (*n_own + *n_prefix == 0) *n_own = 1;
+  const int keys = prefix_len > 0x7fffffff - k_len_max ? 0x7fffffff : prefix_len + k_len_max;
+  c.tc = attn_tc_form(algo, dtype);
+  if (!c.tc) {
+    const long long tiles = ((long long)q_len_max * R + 63) / 64;
+    c.n_part = attn_parts(tiles * H_kv * B, keys, 2 * kPlanSms, 256, 32);
+    if (c.n_part < 1) c.n_part = 1;
+    return c;
+  }
+  const int TT = 128 / (R > 128 ? 128 : R);
+  AttnPlan& p = c.plan;
+  p.nq = q_len_max <= TT ? 1 : 2;
+  p.n_blk = (int)(((long long)q_len_max + p.nq * TT - 1) / (p.nq * TT));
+  if (p.n_blk < 1) p.n_blk = 1;
+  const long long units = (long long)p.n_blk * B * H_kv, ctas = kPlanSms * (p.nq == 2 ? 1 : 2);
+  c.n_part = 1;
+  if (2 * units <= ctas) c.n_part = attn_parts(units, keys, ctas / units * units, 512, 32);
+  if (c.n_part < 1) c.n_part = 1;
+  p.n_units = units * c.n_part;
+  // keys and values of a chunk: 48 MB, which leaves the 126 MB L2 room for the rest
+  const long long pair = (long long)keys * 2 * kHeadDim * 2, fit = (48ll << 20) / (pair > 0 ? pair : 1);
+  p.chunk = (int)(fit < 1 ? 1 : fit > (long long)B * H_kv ? (long long)B * H_kv : fit);
+  return c;
+}
+
+// Tensor cores: units of about as many 128-key tiles as a CTA's even share, two at least (a
+// prefix part writes as many bytes of partial results as one tile has).
+AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int dtype, int algo) {
+  AttnCut c;
+  memset(&c, 0, sizeof(c));
+  const int R = H_q / H_kv;
+  c.tc = attn_tc_form(algo, dtype);
+  if (!c.tc) {
+    c.n_own = attn_parts((long long)B * H_kv * (R <= 2 ? 1 : (R + 3) / 4), kv_len_max, 4 * kPlanSms, 64, 64);
+    c.n_prefix = attn_parts(((long long)B * R + 63) / 64 * H_kv, prefix_len, 2 * kPlanSms, 256, 64);
+    if (c.n_own + c.n_prefix == 0) c.n_own = 1;
+    c.n_part = c.n_own + c.n_prefix;
+    return c;
+  }
+  const int TT = 128 / (R > 128 ? 128 : R);
+  const long long own_tiles = ((long long)kv_len_max + 127) / 128, pre_tiles = ((long long)prefix_len + 127) / 128;
+  const long long own_units = (long long)B * H_kv, pre_units = (((long long)B + TT - 1) / TT) * H_kv;
+  long long share = (own_units * own_tiles + pre_units * pre_tiles + 2 * kPlanSms - 1) / (2 * kPlanSms);
+  if (share < 2) share = 2;
+  c.n_own = (int)((own_tiles + share - 1) / share);
+  c.n_prefix = (int)((pre_tiles + share - 1) / share);
+  if (c.n_own > 64) c.n_own = 64;
+  if (c.n_prefix > 64) c.n_prefix = 64;
+  if (c.n_own + c.n_prefix == 0) c.n_own = 1;
+  c.n_part = c.n_own + c.n_prefix;
+  c.plan.nq = 1;
+  c.plan.n_own_parts = c.n_own;
+  c.plan.n_prefix_parts = c.n_prefix;
+  c.plan.n_prefix_units = (int)(pre_units * c.n_prefix);
+  c.plan.n_units = own_units * c.n_own + pre_units * c.n_prefix;
+  return c;
 }
 
 size_t attn_ws(Carve& c, int n_part, int T_q, int H_q, float** part_o, float** part_lse) {
@@ -1243,10 +1299,9 @@ extern "C" size_t provip_prompt_attention_workspace_size(int T_q, int B, int H_q
                                                          int k_len_max, int prefix_len, int dtype, int algo) {
   if (T_q < 0 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || q_len_max < 0 || k_len_max < 0 || prefix_len < 0)
     return 0;
-  (void)attn_algo(algo, dtype);
   Carve c(nullptr);
   float *po, *pl;
-  return attn_ws(c, prompt_parts(B, H_q, H_kv, q_len_max, k_len_max, prefix_len), T_q, H_q, &po, &pl);
+  return attn_ws(c, prompt_cut(B, H_q, H_kv, q_len_max, k_len_max, prefix_len, dtype, algo).n_part, T_q, H_q, &po, &pl);
 }
 
 extern "C" int provip_prompt_attention(const void* Q, long long q_stride, const void* K, long long k_stride,
@@ -1280,8 +1335,10 @@ extern "C" int provip_prompt_attention(const void* Q, long long q_stride, const 
     if (rc) return rc;
     if (prefix_len > 0x7fffffff - k_len_max) return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many keys", what);
   }
-  const int n_part = prompt_parts(B, H_q, H_kv, q_len_max, k_len_max, prefix_len);
-  if ((long long)q_len_max * (H_q / H_kv) > 0x7fffffffll - 64 || (long long)H_kv * n_part > 65535)
+  const AttnCut cut = prompt_cut(B, H_q, H_kv, q_len_max, k_len_max, prefix_len, dtype, algo);
+  const int n_part = cut.n_part;
+  if ((long long)q_len_max * (H_q / H_kv) > 0x7fffffffll - 64 || (long long)H_kv * n_part > 65535 ||
+      cut.plan.n_units > 0x3fffffffll)
     return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
   if ((rc = check_ws(provip_prompt_attention_workspace_size(T_q, B, H_q, H_kv, q_len_max, k_len_max, prefix_len, dtype,
                                                             algo),
@@ -1323,7 +1380,7 @@ extern "C" int provip_prompt_attention(const void* Q, long long q_stride, const 
   Carve c(ws);
   attn_ws(c, n_part, T_q, H_q, &a.part_o, &a.part_lse);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = attn_prompt_simt_launch(a, dtype, s);
+  cudaError_t e = cut.tc ? attn_tc_launch(a, cut.plan, d->sms, s) : attn_prompt_simt_launch(a, dtype, s);
   if (e == cudaSuccess && n_part > 1) e = attn_join_launch(a, dtype, s);
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "prompt_attention launch");
 }
@@ -1331,12 +1388,9 @@ extern "C" int provip_prompt_attention(const void* Q, long long q_stride, const 
 extern "C" size_t provip_decode_attention_workspace_size(int B, int H_q, int H_kv, int kv_len_max, int prefix_len,
                                                          int dtype, int algo) {
   if (B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || kv_len_max < 0 || prefix_len < 0) return 0;
-  (void)attn_algo(algo, dtype);
-  int n_own, n_prefix;
-  decode_parts(B, H_q, H_kv, kv_len_max, prefix_len, &n_own, &n_prefix);
   Carve c(nullptr);
   float *po, *pl;
-  return attn_ws(c, n_own + n_prefix, B, H_q, &po, &pl);
+  return attn_ws(c, decode_cut(B, H_q, H_kv, kv_len_max, prefix_len, dtype, algo).n_part, B, H_q, &po, &pl);
 }
 
 extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
@@ -1362,9 +1416,9 @@ extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B,
     return fail(PROVIP_ERR_INVALID_ARG, "%s: kv_len_max %d does not fit %d pages", what, kv_len_max, max_pages);
   if (prefix_len > 0x7fffffff - kv_len_max || (long long)n_pages * page_size > 0x7fffffffll)
     return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many keys", what);
-  int n_own, n_prefix;
-  decode_parts(B, H_q, H_kv, kv_len_max, prefix_len, &n_own, &n_prefix);
-  if ((long long)B * (H_q / H_kv) > 0x7fffffffll - 64 || (long long)H_kv * (n_prefix + 1) > 65535)
+  const AttnCut cut = decode_cut(B, H_q, H_kv, kv_len_max, prefix_len, dtype, algo);
+  if ((long long)B * (H_q / H_kv) > 0x7fffffffll - 64 || (long long)H_kv * (cut.n_prefix + 1) > 65535 ||
+      cut.plan.n_units > 0x3fffffffll)
     return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
   if ((rc = check_ws(provip_decode_attention_workspace_size(B, H_q, H_kv, kv_len_max, prefix_len, dtype, algo), ws,
                      ws_bytes, what)))
@@ -1397,12 +1451,12 @@ extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B,
   a.scale_log2 = (float)((double)scale * 1.4426950408889634);
   a.out = out;
   a.lse = lse_or_null;
-  a.n_part = n_own + n_prefix;
+  a.n_part = cut.n_part;
   a.err = d->status;
   Carve c(ws);
   attn_ws(c, a.n_part, B, H_q, &a.part_o, &a.part_lse);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = attn_decode_simt_launch(a, n_own, dtype, s);
+  cudaError_t e = cut.tc ? attn_tc_launch(a, cut.plan, d->sms, s) : attn_decode_simt_launch(a, cut.n_own, dtype, s);
   if (e == cudaSuccess && a.n_part > 1) e = attn_join_launch(a, dtype, s);
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "decode_attention launch");
 }

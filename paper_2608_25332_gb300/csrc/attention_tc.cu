@@ -1,0 +1,612 @@
+// Attention behind the pruning on the tensor cores (bf16, fp32 accumulation).
+//
+// A persistent CTA takes units: NQ tiles of 128 packed rows (attention.cuh) of one
+// key/value head against a run of 128-key tiles. Per key tile and row tile:
+//   S = Q K^T   8 tcgen05.mma (M = N = 128, K = 16), both operands in shared memory, S in
+//               tensor memory;
+//   P = 2^(s - m), a thread per row: the 128 scores in registers, running maximum and sum
+//               in fp32, P to bf16 over S's own columns;
+//   O += P V    8 tcgen05.mma, P read from tensor memory, V as it lies in memory (keys by
+//               elements, an operand whose rows run along N), O in tensor memory.
+// P is rounded to bf16 for its product (the only 16-bit operand type that V allows); the
+// sum of a row adds the unrounded values. The maximum that P is taken against follows the
+// true one only once it is 2^8 behind: P stays below 2^8, which costs no accuracy in floating
+// point, and O is rescaled a few times a row instead of at every tile. S of a tile is
+// complete after the product of the tile before (one thread issues both, and a commit covers
+// all that it issued), so a rescale needs no further wait.
+// Roles: warps 0 .. 4 NQ - 1 softmax, then one warp issues the MMAs and one the TMA loads.
+// K and V tiles share a ring of 32 KiB stages. While the softmax works on one row tile, the
+// tensor cores multiply for the other (NQ = 2, one CTA an SM), or for the other CTA of the
+// SM (NQ = 1, two CTAs).
+// Value rows of a tile past the sequence's end (another sequence's, padding, a page's unused
+// slots, a page not loaded) are zeroed in shared memory before the product.
+// Every wait is bounded; a timeout sets the device error word and the roles drain.
+#include "attention.cuh"
+
+namespace provip {
+namespace {
+
+constexpr int kT = 128;                // rows and keys of a tile
+constexpr int kHalf = kT * 128;        // 64 elements of 128 rows: 16 KiB
+constexpr int kStage = 2 * kHalf;      // a Q, K or V tile
+constexpr float kLag = 8.f;            // how far (base 2) the running maximum may be behind
+constexpr int kSoftRegs = 208, kRestRegs = 80;  // registers a thread, NQ = 2
+
+template <int NQ>
+struct Form {
+  static constexpr int kStages = NQ == 2 ? 5 : 2;
+  static constexpr int kSoft = 128 * NQ;               // softmax threads
+  static constexpr int kThreads = NQ == 2 ? 384 : 192;  // + MMA warp + TMA warp (+ 2 idle)
+  static constexpr int kCtas = NQ == 2 ? 1 : 2;
+  static constexpr size_t kSmem = (size_t)(NQ + kStages) * kStage + 1024;
+  static constexpr uint32_t kCols = 256 * NQ;          // S and O of every row tile
+};
+
+struct Maps {
+  CUtensorMap q, k, v, kp, vp;
+};
+
+template <int NQ>
+struct Ctl {
+  uint64_t q_full, q_empty;
+  uint64_t kv_full[Form<NQ>::kStages], kv_empty[Form<NQ>::kStages];
+  uint64_t s_full[NQ], p_full[NQ], o_full[NQ];
+  uint32_t tmem;
+  volatile int fail;
+};
+
+// P V: A (P) from tensor memory
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                               uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// 128-byte swizzled tile whose rows (128 B, 64 elements) run along N (or M) and whose
+// successive rows are successive K: 8-row groups 1024 B apart, 64-element halves kHalf apart
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t start) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((start >> 4) & 0x3FFFu);
+  d |= static_cast<uint64_t>(kHalf >> 4) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= static_cast<uint64_t>(1u) << 46;
+  d |= static_cast<uint64_t>(2u) << 61;
+  return d;
+}
+constexpr uint32_t kIdescS = idesc_bf16_f32(kT, kT);
+constexpr uint32_t kIdescO = idesc_bf16_f32(kT, kT) | (1u << 16);  // B's rows run along N
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// ---------------------------------------------------------------------------
+// units
+// ---------------------------------------------------------------------------
+template <int NQ>
+struct Unit {
+  AttnSeq s;
+  int g, part;       // key/value head; slot of the partial results
+  int tok0;          // first token of the first row tile
+  int n_tok[NQ];     // tokens of each row tile
+  int n_prefix;      // prefix keys of the list, their tiles
+  int n_pt;
+  int t_lo;          // the unit's first tile of the list
+  int nt[NQ];        // tiles of each row tile
+  int ntm;           // the most of them
+};
+
+template <int NQ>
+__device__ __forceinline__ Unit<NQ> unit_of(const AttnArgs& a, const AttnPlan& p, int u) {
+  Unit<NQ> x;
+  const int R = a.H_q / a.H_kv, TT = kT / R;
+  int blk, n_parts, part;
+  bool own = true;
+  if (a.paged && u < p.n_prefix_units) {
+    // the tokens of every request against the prefix
+    part = u % p.n_prefix_parts;
+    u /= p.n_prefix_parts;
+    x.g = u % a.H_kv;
+    blk = u / a.H_kv;
+    n_parts = p.n_prefix_parts;
+    x.part = p.n_own_parts + part;
+    x.s.q0 = 0;
+    x.s.q_len = a.B;
+    x.s.k_len = 0;
+    x.s.k0 = 0;
+    x.s.pages = nullptr;
+    x.s.ok = true;
+    x.n_prefix = a.prefix_len;
+    own = false;
+  } else if (a.paged) {
+    u -= p.n_prefix_units;
+    x.g = u % a.H_kv;
+    u /= a.H_kv;
+    part = u % p.n_own_parts;
+    x.s = attn_seq(a, u / p.n_own_parts);
+    blk = 0;
+    n_parts = p.n_own_parts;
+    x.part = part;
+    x.n_prefix = 0;
+  } else {
+    // (sequence, head) pairs in chunks whose keys and values stay in L2; within a chunk the
+    // last rows, which see the most keys, first
+    const int n_bg = a.B * a.H_kv, per = p.chunk * p.n_blk * a.n_part, c = u / per;
+    const int sz = min(p.chunk, n_bg - c * p.chunk) * a.n_part;
+    const int rem = u - c * per;
+    blk = p.n_blk - 1 - rem / sz;
+    const int in = rem % sz, bg = c * p.chunk + in / a.n_part;
+    part = in % a.n_part;
+    x.g = bg % a.H_kv;
+    x.s = attn_seq(a, bg / a.H_kv);
+    n_parts = a.n_part;
+    x.part = part;
+    x.n_prefix = a.prefix_len;
+  }
+  x.tok0 = blk * NQ * TT;
+  x.n_pt = (x.n_prefix + kT - 1) / kT;
+  int most = 0, tiles[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    x.n_tok[i] = min(max(x.s.q_len - x.tok0 - i * TT, 0), TT);
+    tiles[i] = 0;
+    if (x.n_tok[i] > 0) {
+      const int vis = own ? attn_visible(a, x.s.q_len, x.s.k_len, x.tok0 + i * TT + x.n_tok[i] - 1) : 0;
+      tiles[i] = x.n_pt + (vis + kT - 1) / kT;
+    }
+    most = max(most, tiles[i]);
+  }
+  const int per = (most + n_parts - 1) / n_parts;
+  x.t_lo = min(part * per, most);
+  const int t_hi = min(x.t_lo + per, most);
+  x.ntm = t_hi - x.t_lo;
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) x.nt[i] = min(max(tiles[i] - x.t_lo, 0), x.ntm);
+  return x;
+}
+
+// key of the list that tile t starts with
+template <int NQ>
+__device__ __forceinline__ int list_key(const Unit<NQ>& x, int t) {
+  return t < x.n_pt ? t * kT : x.n_prefix + (t - x.n_pt) * kT;
+}
+
+// the k-th unit of this CTA: every other round runs backwards, so that the long units of
+// one round meet the short ones of the next
+__device__ __forceinline__ int unit_index(int k) {
+  const int G = (int)gridDim.x, i = (int)blockIdx.x;
+  return k * G + ((k & 1) ? G - 1 - i : i);
+}
+
+// ---------------------------------------------------------------------------
+// the kernel
+// ---------------------------------------------------------------------------
+template <int NQ>
+__global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
+    attn_tc(int n_units, const __grid_constant__ AttnArgs a, const __grid_constant__ AttnPlan plan,
+            const __grid_constant__ Maps maps) {
+  using F = Form<NQ>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Ctl<NQ> ctl;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int R = a.H_q / a.H_kv, TT = kT / R;
+  const uint32_t base = smem_u32(smem_raw);
+  uint8_t* qs = smem_raw + (((base + 1023u) & ~1023u) - base);
+  uint8_t* kv = qs + NQ * kStage;
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&maps.q);
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+    mbar_init(&ctl.q_full, 1);
+    mbar_init(&ctl.q_empty, 1);
+    for (int s = 0; s < F::kStages; ++s) {
+      mbar_init(&ctl.kv_full[s], 1);
+      mbar_init(&ctl.kv_empty[s], 1);
+    }
+    for (int i = 0; i < NQ; ++i) {
+      mbar_init(&ctl.s_full[i], 1);
+      mbar_init(&ctl.p_full[i], 4);
+      mbar_init(&ctl.o_full[i], 1);
+    }
+    ctl.fail = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(&ctl.tmem, F::kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_allow_next();  // the joining kernel, which holds no tensor memory, may be scheduled
+  const uint32_t tmem = ctl.tmem;
+
+  if (warp >= 4 * NQ) {
+    if (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
+    if (warp == 4 * NQ) {
+      // ---- MMA issuer ----
+      if (lane == 0) {
+        const uint64_t qd = smem_desc_sw128(smem_u32(qs));
+        uint32_t n_q = 0, n_p[NQ], idx = 0;  // phases of q_full and p_full, loads consumed
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) n_p[i] = 0;
+        bool live = true;
+        for (int k = 0, u; live && (u = unit_index(k)) < n_units; ++k) {
+          const Unit<NQ> x = unit_of<NQ>(a, plan, u);
+          if (x.ntm == 0) continue;
+          live = mbar_wait(&ctl.q_full, n_q++ & 1u, a.err);
+          for (int j = 0; live && j <= x.ntm; ++j) {
+            // loads: K_j is number idx + 2 j, V_j the next
+            const uint32_t lk = idx + 2 * j, lv = lk - 1;
+            const uint32_t sk = lk % F::kStages, sv = lv % F::kStages;
+            if (ctl.fail) live = false;
+            bool got_k = false, got_v = false;
+            const uint64_t kd = smem_desc_sw128(smem_u32(kv + sk * kStage));
+            const uint64_t vd = smem_desc_mn_sw128(smem_u32(kv + sv * kStage));
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+              const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
+              if (live && j > 0 && j - 1 < x.nt[i]) {
+                if (!got_v) live = mbar_wait(&ctl.kv_full[sv], (lv / F::kStages) & 1u, a.err);
+                got_v = true;
+                live = live && mbar_wait(&ctl.p_full[i], n_p[i]++ & 1u, a.err);
+                if (!live) break;
+                tc_fence_after();
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                  tc_mma_bf16_ts(to, ts + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), kIdescO, (j > 1 || ks > 0) ? 1u : 0u);
+                if (j == x.nt[i]) tc_commit(&ctl.o_full[i]);
+              }
+              if (live && j < x.nt[i]) {
+                if (!got_k) live = mbar_wait(&ctl.kv_full[sk], (lk / F::kStages) & 1u, a.err);
+                got_k = true;
+                if (!live) break;
+                tc_fence_after();
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                  const uint64_t off = (uint64_t)((ks >> 2) * kHalf + (ks & 3) * 32) >> 4;
+                  tc_mma_bf16(ts, qd + (uint64_t)(i * kStage >> 4) + off, kd + off, kIdescS, ks > 0 ? 1u : 0u);
+                }
+                tc_commit(&ctl.s_full[i]);
+              }
+            }
+            if (live && j > 0) tc_commit(&ctl.kv_empty[sv]);
+            if (live && j < x.ntm) tc_commit(&ctl.kv_empty[sk]);
+            if (live && j == x.ntm - 1) tc_commit(&ctl.q_empty);
+          }
+          idx += 2 * x.ntm;
+        }
+        if (!live) ctl.fail = 1;
+      }
+    } else if (warp == 4 * NQ + 1) {
+      // ---- TMA producer (the lanes share a tile's pages) ----
+      uint32_t n_q = 0, idx = 0;
+      bool live = true;
+      const int box = a.paged ? min(a.page_size, kT) : kT;
+      // one tile of the list, K or V, into the next stage
+      auto load = [&](const Unit<NQ>& x, int t, bool v) {
+        const uint32_t st = idx % F::kStages, ph = (idx / F::kStages) & 1u;
+        ++idx;
+        uint64_t* full = &ctl.kv_full[st];
+        uint8_t* dst = kv + st * kStage;
+        const bool pre = t < x.n_pt;
+        const int key = pre ? t * kT : (t - x.n_pt) * kT;
+        const int n = min(kT, (pre ? x.n_prefix : x.s.k_len) - key);
+        const int boxes = a.paged ? (n + box - 1) / box : 1;
+        bool ok = true;
+        if (lane == 0) {
+          ok = !ctl.fail && mbar_wait(&ctl.kv_empty[st], ph ^ 1u, a.err);
+          if (ok) mbar_arrive_expect_tx(full, (uint32_t)(boxes * box * 256));
+        }
+        __syncwarp();
+        if (!__shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) return false;
+        const CUtensorMap* map = pre ? (v ? &maps.vp : &maps.kp) : (v ? &maps.v : &maps.k);
+        if (lane < boxes) {
+          int row;
+          if (a.paged)
+            row = (int)attn_slot(a, pre ? a.prefix_table : x.s.pages, key + lane * box);
+          else
+            row = pre ? key : (int)(x.s.k0 + key);
+          tma_load_2d(dst + lane * box * 128, map, x.g * kHeadDim, row, full);
+          tma_load_2d(dst + kHalf + lane * box * 128, map, x.g * kHeadDim + 64, row, full);
+        }
+        __syncwarp();
+        return true;
+      };
+      for (int k = 0, u; live && (u = unit_index(k)) < n_units; ++k) {
+        const Unit<NQ> x = unit_of<NQ>(a, plan, u);
+        if (lane == 0 && !x.s.ok) set_error(a.err, kErrBadDeviceArg);
+        if (x.ntm == 0) continue;
+        live = load(x, x.t_lo, false);
+        if (!live) break;
+        bool ok = true;
+        if (lane == 0) {
+          ok = mbar_wait(&ctl.q_empty, (n_q & 1u) ^ 1u, a.err);
+          if (ok) {
+            int tiles = 0;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) tiles += x.n_tok[i] > 0;
+            mbar_arrive_expect_tx(&ctl.q_full, (uint32_t)(tiles * TT * R * 256));
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+              if (x.n_tok[i] > 0) {
+                const int tok = x.s.q0 + x.tok0 + i * TT;
+                tma_load_3d(qs + i * kStage, &maps.q, 0, x.g * R, tok, &ctl.q_full);
+                tma_load_3d(qs + i * kStage + kHalf, &maps.q, 64, x.g * R, tok, &ctl.q_full);
+              }
+          }
+        }
+        __syncwarp();
+        live = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        ++n_q;
+        for (int j = 0; live && j < x.ntm; ++j) {
+          live = load(x, x.t_lo + j, true);
+          if (live && j + 1 < x.ntm) live = load(x, x.t_lo + j + 1, false);
+        }
+      }
+      if (!live) ctl.fail = 1;
+    }
+  } else {
+    // ---- softmax: a thread per row ----
+    if (NQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int i = NQ == 2 ? warp >> 2 : 0, quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t ts = tmem + i * kT + ((uint32_t)(quad * 32) << 16);
+    const uint32_t to = tmem + (NQ + i) * kT + ((uint32_t)(quad * 32) << 16);
+    const int tok_in = r / R, hd = r - tok_in * R;
+    const float sc = a.scale_log2;
+    uint32_t n_s = 0, n_o = 0, idx = 0;
+    bool failed = false;
+    for (int k = 0, u; !failed && (u = unit_index(k)) < n_units; ++k) {
+      const Unit<NQ> x = unit_of<NQ>(a, plan, u);
+      const int n_tok = NQ == 2 && i ? x.n_tok[NQ - 1] : x.n_tok[0], nt = NQ == 2 && i ? x.nt[NQ - 1] : x.nt[0];
+      const int tok = x.tok0 + i * TT + tok_in;
+      const bool row_live = tok_in < n_tok;
+      const bool warp_live = (quad * 32) / R < n_tok;  // the warp's first row's token
+      const int own = row_live ? attn_visible(a, x.s.q_len, x.s.k_len, tok) : x.s.k_len;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < nt; ++j) {
+        const int t = x.t_lo + j;
+        const bool pre = t < x.n_pt;
+        const int key = pre ? t * kT : (t - x.n_pt) * kT;
+        const int n_keys = (pre ? x.n_prefix : x.s.k_len) - key;   // of the list from here on
+        const int lim = (pre ? x.n_prefix : own) - key;            // that this row sees
+        if (!failed) failed = !mbar_wait(&ctl.s_full[i], n_s & 1u, a.err);
+        ++n_s;
+        failed = __any_sync(0xffffffffu, failed);
+        if (failed) break;
+        __syncwarp();
+        tc_fence_after();
+        if (n_keys < kT) {
+          // rows past the end: zero before the product reads them
+          const uint32_t lv = idx + 2 * j + 1, sv = lv % F::kStages;
+          failed = !mbar_wait(&ctl.kv_full[sv], (lv / F::kStages) & 1u, a.err);
+          failed = __any_sync(0xffffffffu, failed);
+          if (failed) break;
+          __syncwarp();
+          uint8_t* vs = kv + sv * kStage;
+          for (int q = n_keys * 16 + r; q < kT * 16; q += 128)
+            *reinterpret_cast<uint4*>(vs + ((q >> 3) & 1) * kHalf + (q >> 4) * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async_smem();
+        }
+        if (warp_live) {
+          float v[kT];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, v + c * 32);
+          tc_wait_ld();
+          if (__any_sync(0xffffffffu, lim < kT)) {
+#pragma unroll
+            for (int e = 0; e < kT; ++e) v[e] = e < lim ? v[e] : -INFINITY;
+          }
+          float b4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int e = 4; e + 7 < kT; e += 8) {
+#pragma unroll
+            for (int z = 0; z < 4; ++z) b4[z] = max3(b4[z], v[e + z], v[e + 4 + z]);
+          }
+#pragma unroll
+          for (int z = 0; z < 4; ++z) b4[z] = fmaxf(b4[z], v[kT - 4 + z]);
+          const float mx = max3(fmaxf(b4[0], b4[1]), b4[2], b4[3]) * sc;  // sc > 0: the maximum commutes with it
+          const bool up = row_live && (mx > m + kLag || (m == -INFINITY && mx > m));
+          if (__any_sync(0xffffffffu, up)) {
+            const float mn = up ? mx : m;
+            const float f = m == mn ? 1.f : ex2_approx(m - mn);
+            m = mn;
+            l *= f;
+            if (j > 0) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                uint32_t w[32];
+                tmem_ld32(to + c * 32, reinterpret_cast<float*>(w));
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+                tmem_st32(to + c * 32, w);
+              }
+            }
+          }
+          const float mb = m == -INFINITY ? 0.f : m;
+          float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t w[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float p0 = ex2_approx(fmaf(v[c * 64 + 2 * e], sc, -mb));
+              const float p1 = ex2_approx(fmaf(v[c * 64 + 2 * e + 1], sc, -mb));
+              s4[(2 * e) & 3] += p0;
+              s4[(2 * e + 1) & 3] += p1;
+              w[e] = pack_bf16(p0, p1);
+            }
+            tmem_st32(ts + c * 32, w);
+          }
+          l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+          tc_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.p_full[i]);
+      }
+      idx += 2 * x.ntm;
+      if (failed) break;
+      // ---- epilogue: O / l to memory ----
+      if (nt > 0) {
+        failed = !mbar_wait(&ctl.o_full[i], n_o & 1u, a.err);
+        ++n_o;
+        failed = __any_sync(0xffffffffu, failed);
+        if (failed) break;
+        __syncwarp();
+        tc_fence_after();
+      }
+      if (!warp_live) continue;
+      const int h = x.g * R + hd;
+      const size_t n_rows = (size_t)a.T_q * a.H_q, row = (size_t)(x.s.q0 + tok) * a.H_q + h;
+      const bool partial = a.n_part > 1;
+      float* po = partial ? a.part_o + ((size_t)x.part * n_rows + row) * kHeadDim : nullptr;
+      __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tok) * a.o_stride + (size_t)h * kHeadDim;
+      const bool none = l == 0.f;
+      // a row whose keys all score -inf is 0 / 0; a row without keys is 0
+      const int lo = list_key(x, x.t_lo), hi = min(list_key(x, x.t_lo + nt), x.n_prefix + own);
+      const float nil = !partial && hi > lo ? NAN : 0.f;
+      const float inv = none ? 0.f : 1.f / l;
+      float lse = none ? (nil == 0.f ? -INFINITY : NAN) : m + lg2_approx(l);
+      bool fine = !isnan(l);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        if (nt > 0) {
+          tmem_ld32(to + c * 32, o);
+          tc_wait_ld();
+        }
+        float bad = 0.f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          o[e] = none ? nil : o[e] * inv;
+          bad = fmaf(o[e], 0.f, bad);  // NaN once an element is not finite
+        }
+        if (!none && isnan(bad)) fine = false;
+        if (row_live) {
+          if (partial) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) store4(po + c * 32 + e, o + e);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              uint4 w;
+              w.x = pack_bf16(o[e], o[e + 1]);
+              w.y = pack_bf16(o[e + 2], o[e + 3]);
+              w.z = pack_bf16(o[e + 4], o[e + 5]);
+              w.w = pack_bf16(o[e + 6], o[e + 7]);
+              *reinterpret_cast<uint4*>(op + c * 32 + e) = w;
+            }
+          }
+        }
+      }
+      tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
+      if (row_live) {
+        if (partial)
+          a.part_lse[(size_t)x.part * n_rows + row] = lse;
+        else if (a.lse)
+          a.lse[row] = lse * kLn2;
+      }
+      // rows that are not finite: again by the definition
+      unsigned again = __ballot_sync(0xffffffffu, row_live && !fine);
+      while (again) {
+        const int src = __ffs(again) - 1;
+        again &= again - 1;
+        const int tk = __shfl_sync(0xffffffffu, tok, src), hh = __shfl_sync(0xffffffffu, h, src);
+        const int khi = __shfl_sync(0xffffffffu, hi, src);
+        float o[4];
+        float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, o);
+        const size_t rw = (size_t)(x.s.q0 + tk) * a.H_q + hh;
+        if (partial) {
+          store4(a.part_o + ((size_t)x.part * n_rows + rw) * kHeadDim + lane * 4, o);
+          if (lane == 0) a.part_lse[(size_t)x.part * n_rows + rw] = le;
+        } else {
+          if (le == -INFINITY) le = o[0] = o[1] = o[2] = o[3] = NAN;
+          store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tk) * a.o_stride + (size_t)hh * kHeadDim + lane * 4, o);
+          if (lane == 0 && a.lse) a.lse[rw] = le * kLn2;
+        }
+      }
+    }
+    if (failed) ctl.fail = 1;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, F::kCols);
+}
+
+int map_of(CUtensorMap* m, const void* base, uint64_t rows, int H, long long stride, uint32_t box_rows) {
+  return make_tmap_bf16_2d(m, base, rows, (uint64_t)H * kHeadDim, (uint64_t)stride * 2, box_rows);
+}
+
+template <int NQ>
+cudaError_t launch(const AttnArgs& a, const AttnPlan& plan, const Maps& maps, int sms, cudaStream_t s) {
+  using F = Form<NQ>;
+  static std::atomic<bool> configured[64];  // per device, zero-initialised
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    cudaError_t e = cudaFuncSetAttribute(attn_tc<NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
+    cudaFuncAttributes at;
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, attn_tc<NQ>);
+    if (e != cudaSuccess) return e;
+    // the register split draws on what the block is launched with
+    if (NQ == 2 && at.numRegs * F::kThreads < kSoftRegs * F::kSoft + kRestRegs * (F::kThreads - F::kSoft))
+      return cudaErrorInvalidConfiguration;
+    configured[dev] = true;
+  }
+  const long long most = (long long)sms * F::kCtas;
+  const int grid = (int)(plan.n_units < most ? plan.n_units : most);
+  attn_tc<NQ><<<grid, F::kThreads, F::kSmem, s>>>((int)plan.n_units, a, plan, maps);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t attn_tc_launch(const AttnArgs& a, const AttnPlan& plan, int sms, cudaStream_t s) {
+  Maps m;
+  const int R = a.H_q / a.H_kv;
+  const uint32_t box = a.paged ? (uint32_t)(a.page_size < kT ? a.page_size : kT) : (uint32_t)kT;
+  const uint64_t rows = a.paged ? (uint64_t)a.n_pages * a.page_size : (uint64_t)(a.T_k > 0 ? a.T_k : 1);
+  if (make_tmap_bf16_heads(&m.q, a.Q, (uint64_t)a.T_q, (uint64_t)a.H_q, (uint64_t)a.q_stride * 2, (uint32_t)R,
+                           (uint32_t)(kT / R)) ||
+      map_of(&m.k, a.K, rows, a.H_kv, a.k_stride, box) || map_of(&m.v, a.V, rows, a.H_kv, a.v_stride, box))
+    return cudaErrorInvalidValue;
+  m.kp = m.k;
+  m.vp = m.v;
+  if (!a.paged && a.prefix_len > 0 &&
+      (map_of(&m.kp, a.Kp, (uint64_t)a.prefix_len, a.H_kv, a.kp_stride, box) ||
+       map_of(&m.vp, a.Vp, (uint64_t)a.prefix_len, a.H_kv, a.vp_stride, box)))
+    return cudaErrorInvalidValue;
+  return plan.nq == 2 ? launch<2>(a, plan, m, sms, s) : launch<1>(a, plan, m, sms, s);
+}
+
+}  // namespace provip

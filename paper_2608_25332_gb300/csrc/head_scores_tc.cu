@@ -304,8 +304,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,
-                      uint64_t row_stride_bytes, uint32_t box_rows) {
+static EncodeTiledFn encode_tiled() {
   static EncodeTiledFn fn = nullptr;
   if (!fn) {
     void* p = nullptr;
@@ -313,14 +312,35 @@ int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
             cudaSuccess ||
         q != cudaDriverEntryPointSuccess || !p)
-      return -1;
+      return nullptr;
     fn = reinterpret_cast<EncodeTiledFn>(p);
   }
+  return fn;
+}
+
+int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,
+                      uint64_t row_stride_bytes, uint32_t box_rows) {
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return -1;
   const cuuint64_t gdim[2] = {cols, rows};
   const cuuint64_t gstride[1] = {row_stride_bytes};
   const cuuint32_t box[2] = {64, box_rows};
   const cuuint32_t estride[2] = {1, 1};
   CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), gdim, gstride,
+                  box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? 0 : -1;
+}
+
+int make_tmap_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads,
+                         uint64_t row_stride_bytes, uint32_t box_heads, uint32_t box_rows) {
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return -1;
+  const cuuint64_t gdim[3] = {(cuuint64_t)kHeadDim, heads, rows};
+  const cuuint64_t gstride[2] = {kHeadDim * 2, row_stride_bytes};
+  const cuuint32_t box[3] = {64, box_heads, box_rows};
+  const cuuint32_t estride[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), gdim, gstride,
                   box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? 0 : -1;

@@ -319,6 +319,16 @@ cudaError_t attn_prompt_simt_launch(const AttnArgs& a, int dtype, cudaStream_t s
 // One token per request: own keys in parts 0 .. n_own - 1, the prefix's in the others
 // (64-row tiles over the tokens of every request).
 cudaError_t attn_decode_simt_launch(const AttnArgs& a, int n_own, int dtype, cudaStream_t s);
+// Tensor-core form (bf16): how the work is cut into units for its persistent CTAs.
+struct AttnPlan {
+  int nq;                    // row tiles of 128 a CTA
+  long long n_units;
+  int n_blk;                 // prompt: row blocks of the longest sequence
+  int chunk;                 // prompt: (sequence, key/value head) pairs handled together
+  int n_own_parts, n_prefix_parts;  // paged: parts of a request's keys, of the prefix's
+  int n_prefix_units;        // paged: units of the prefix, which come first
+};
+cudaError_t attn_tc_launch(const AttnArgs& a, const AttnPlan& plan, int sms, cudaStream_t s);
 // joins n_part parts of every row into out and lse
 cudaError_t attn_join_launch(const AttnArgs& a, int dtype, cudaStream_t s);
 
@@ -360,5 +370,9 @@ cudaError_t kv_append_launch(const KvAppendArgs& a, cudaStream_t s);
 // as a tensor map with 64 x box_rows boxes and 128-byte swizzle.
 int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,
                       uint64_t row_stride_bytes, uint32_t box_rows);
+// the same for rows of 128-element heads: [rows][heads][128], boxes of box_rows rows by
+// box_heads heads by 64 elements, rows outermost
+int make_tmap_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads,
+                         uint64_t row_stride_bytes, uint32_t box_heads, uint32_t box_rows);
 
 }  // namespace provip
