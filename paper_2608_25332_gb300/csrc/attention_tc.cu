@@ -86,16 +86,21 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
-      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
-      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -103,9 +108,60 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// pairs of fp32 in one instruction
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// 2^x of a whole x <= 0 (-inf too), exactly; 0 where it is subnormal
+__device__ __forceinline__ float ex2_int(float x) {
+  return x < -126.f ? 0.f : __int_as_float((127 + (int)x) << 23);
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// this thread's row times f: the first c pieces of P (32 keys each; a power of two leaves
+// their rounding as it is), and O
+__device__ __noinline__ void scale_p(uint32_t ts, int c, float f) {
+  const __nv_bfloat162 f2 = __floats2bfloat162_rn(f, f);
+  tc_wait_st();
+  for (int z = 0; z < c; ++z) {
+    uint32_t w[16];
+    tmem_ld16(ts + z * 16, w);
+    tc_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const __nv_bfloat162 t = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w[e]), f2);
+      w[e] = *reinterpret_cast<const uint32_t*>(&t);
+    }
+    tmem_st16(ts + z * 16, w);
+  }
+}
+__device__ __noinline__ void scale_o(uint32_t to, float f) {
+  for (int z = 0; z < kHeadDim / 16; ++z) {
+    uint32_t w[16];
+    tmem_ld16(to + z * 16, w);
+    tc_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+    tmem_st16(to + z * 16, w);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -417,57 +473,54 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           fence_proxy_async_smem();
         }
         if (warp_live) {
-          float v[kT];
+          // 32 columns at a time, the next ones' load under way
+          float v[2][32];
+          tmem_ld32(ts, v[0]);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, v + c * 32);
-          tc_wait_ld();
-          if (__any_sync(0xffffffffu, lim < kT)) {
+          for (int c = 0; c < 4; ++c) {
+            float* x32 = v[c & 1];
+            tc_wait_ld();
+            if (c < 3) tmem_ld32(ts + (c + 1) * 32, v[(c + 1) & 1]);
+            if (__any_sync(0xffffffffu, lim < c * 32 + 32)) {
 #pragma unroll
-            for (int e = 0; e < kT; ++e) v[e] = e < lim ? v[e] : -INFINITY;
-          }
-          float b4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-          for (int e = 4; e + 7 < kT; e += 8) {
-#pragma unroll
-            for (int z = 0; z < 4; ++z) b4[z] = max3(b4[z], v[e + z], v[e + 4 + z]);
-          }
-#pragma unroll
-          for (int z = 0; z < 4; ++z) b4[z] = fmaxf(b4[z], v[kT - 4 + z]);
-          const float mx = max3(fmaxf(b4[0], b4[1]), b4[2], b4[3]) * sc;  // sc > 0: the maximum commutes with it
-          const bool up = row_live && (mx > m + kLag || (m == -INFINITY && mx > m));
-          if (__any_sync(0xffffffffu, up)) {
-            const float mn = up ? mx : m;
-            const float f = m == mn ? 1.f : ex2_approx(m - mn);
-            m = mn;
-            l *= f;
-            if (j > 0) {
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                uint32_t w[32];
-                tmem_ld32(to + c * 32, reinterpret_cast<float*>(w));
-                tc_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
-                tmem_st32(to + c * 32, w);
-              }
+              for (int e = 0; e < 32; ++e) x32[e] = c * 32 + e < lim ? x32[e] : -INFINITY;
             }
-          }
-          const float mb = m == -INFINITY ? 0.f : m;
-          float s4[4] = {0.f, 0.f, 0.f, 0.f};
+            float b4[4] = {x32[0], x32[1], x32[2], x32[3]};
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t w[32];
+            for (int e = 4; e < 28; e += 8) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float p0 = ex2_approx(fmaf(v[c * 64 + 2 * e], sc, -mb));
-              const float p1 = ex2_approx(fmaf(v[c * 64 + 2 * e + 1], sc, -mb));
-              s4[(2 * e) & 3] += p0;
-              s4[(2 * e + 1) & 3] += p1;
+              for (int z = 0; z < 4; ++z) b4[z] = max3(b4[z], x32[e + z], x32[e + 4 + z]);
+            }
+#pragma unroll
+            for (int z = 0; z < 4; ++z) b4[z] = fmaxf(b4[z], x32[28 + z]);
+            const float mx = max3(fmaxf(b4[0], b4[1]), b4[2], b4[3]) * sc;  // sc > 0: the maximum commutes with it
+            const bool up = row_live && (mx > m + kLag || (m == -INFINITY && mx > m));
+            if (__any_sync(0xffffffffu, up)) {
+              const float mn = up ? ceilf(mx) : m;
+              const float f = m == mn ? 1.f : ex2_int(m - mn);
+              m = mn;
+              l *= f;
+              if (c > 0) scale_p(ts, c, f);
+              if (j > 0) scale_o(to, f);
+            }
+            const float mb = m == -INFINITY ? 0.f : m;
+            const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
+            uint64_t s2[2] = {0, 0};
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float p0, p1;
+              unpack2(fma2(pack2(x32[2 * e], x32[2 * e + 1]), sc2, mb2), p0, p1);
+              p0 = ex2_approx(p0);
+              p1 = ex2_approx(p1);
+              s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
               w[e] = pack_bf16(p0, p1);
             }
-            tmem_st32(ts + c * 32, w);
+            tmem_st16(ts + c * 16, w);
+            float s0, s1;
+            unpack2(add2(s2[0], s2[1]), s0, s1);
+            l += s0 + s1;
           }
-          l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
           tc_wait_st();
         }
         tc_fence_before();
