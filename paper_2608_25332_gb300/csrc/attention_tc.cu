@@ -30,13 +30,12 @@ constexpr int kT = 128;                // rows and keys of a tile
 constexpr int kHalf = kT * 128;        // 64 elements of 128 rows: 16 KiB
 constexpr int kStage = 2 * kHalf;      // a Q, K or V tile
 constexpr float kLag = 8.f;            // how far (base 2) the running maximum may be behind
-constexpr int kSoftRegs = 208, kRestRegs = 80;  // registers a thread, NQ = 2
 
 template <int NQ>
 struct Form {
   static constexpr int kStages = NQ == 2 ? 5 : 2;
   static constexpr int kSoft = 128 * NQ;               // softmax threads
-  static constexpr int kThreads = NQ == 2 ? 384 : 192;  // + MMA warp + TMA warp (+ 2 idle)
+  static constexpr int kThreads = kSoft + 64;          // + MMA warp + TMA warp
   static constexpr int kCtas = NQ == 2 ? 1 : 2;
   static constexpr size_t kSmem = (size_t)(NQ + kStages) * kStage + 1024;
   static constexpr uint32_t kCols = 256 * NQ;          // S and O of every row tile
@@ -86,21 +85,22 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
       : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
+// true in one lane of a converged warp
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -136,31 +136,34 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// this thread's row times f: the first c pieces of P (32 keys each; a power of two leaves
-// their rounding as it is), and O
-__device__ __noinline__ void scale_p(uint32_t ts, int c, float f) {
-  const __nv_bfloat162 f2 = __floats2bfloat162_rn(f, f);
-  tc_wait_st();
-  for (int z = 0; z < c; ++z) {
-    uint32_t w[16];
-    tmem_ld16(ts + z * 16, w);
-    tc_wait_ld();
+// the maximum of 32 scores, with those from number n on hidden
+__device__ __forceinline__ void mask32(float* x, int n) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const __nv_bfloat162 t = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w[e]), f2);
-      w[e] = *reinterpret_cast<const uint32_t*>(&t);
-    }
-    tmem_st16(ts + z * 16, w);
-  }
+  for (int e = 0; e < 32; ++e) x[e] = e < n ? x[e] : -INFINITY;
 }
+__device__ __forceinline__ float max32(const float* x) {
+  float b[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+  for (int e = 4; e < 28; e += 8) {
+#pragma unroll
+    for (int z = 0; z < 4; ++z) b[z] = max3(b[z], x[e + z], x[e + 4 + z]);
+  }
+#pragma unroll
+  for (int z = 0; z < 4; ++z) b[z] = fmaxf(b[z], x[28 + z]);
+  return max3(fmaxf(b[0], b[1]), b[2], b[3]);
+}
+// whether a maximum m, against which P is taken, has fallen too far behind mx
+__device__ __forceinline__ bool behind(float mx, float m) { return mx > m + kLag || (m == -INFINITY && mx > m); }
+
+// this thread's row of O times f
 __device__ __noinline__ void scale_o(uint32_t to, float f) {
-  for (int z = 0; z < kHeadDim / 16; ++z) {
-    uint32_t w[16];
-    tmem_ld16(to + z * 16, w);
+  for (int z = 0; z < kHeadDim / 32; ++z) {
+    uint32_t w[32];
+    tmem_ld32(to + z * 32, reinterpret_cast<float*>(w));
     tc_wait_ld();
 #pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
-    tmem_st16(to + z * 16, w);
+    for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+    tmem_st32(to + z * 32, w);
   }
 }
 
@@ -262,6 +265,15 @@ __device__ __forceinline__ int unit_index(int k) {
   return k * G + ((k & 1) ? G - 1 - i : i);
 }
 
+// the next unit of this CTA that has tiles (ntm > 0), from its k-th on; ntm = 0: none is left
+template <int NQ>
+__device__ __forceinline__ Unit<NQ> next_unit(const AttnArgs& a, const AttnPlan& p, int n_units, int& k) {
+  Unit<NQ> x;
+  x.ntm = 0;
+  for (int u; x.ntm == 0 && (u = unit_index(k)) < n_units; ++k) x = unit_of<NQ>(a, p, u);
+  return x;
+}
+
 // ---------------------------------------------------------------------------
 // the kernel
 // ---------------------------------------------------------------------------
@@ -306,46 +318,56 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
   const uint32_t tmem = ctl.tmem;
 
   if (warp >= 4 * NQ) {
-    if (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
     if (warp == 4 * NQ) {
-      // ---- MMA issuer ----
-      if (lane == 0) {
-        const uint64_t qd = smem_desc_sw128(smem_u32(qs));
-        uint32_t n_q = 0, n_p[NQ], idx = 0;  // phases of q_full and p_full, loads consumed
+      // ---- MMA issuer: the whole warp walks through the tiles, one lane issues ----
+      const bool lead = elect_one();
+      const uint64_t qd = smem_desc_sw128(smem_u32(qs));
+      const uint64_t kd0 = smem_desc_sw128(smem_u32(kv)), vd0 = smem_desc_mn_sw128(smem_u32(kv));
+      // loads come in the order K_0 V_0 K_1 V_1 ..: stage and phase of the next K and of the next V
+      uint32_t sk = 0, pk = 0, sv = 1, pv = 0, pq = 0, pp[NQ];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) n_p[i] = 0;
-        bool live = true;
-        for (int k = 0, u; live && (u = unit_index(k)) < n_units; ++k) {
-          const Unit<NQ> x = unit_of<NQ>(a, plan, u);
-          if (x.ntm == 0) continue;
-          live = mbar_wait(&ctl.q_full, n_q++ & 1u, a.err);
-          for (int j = 0; live && j <= x.ntm; ++j) {
-            // loads: K_j is number idx + 2 j, V_j the next
-            const uint32_t lk = idx + 2 * j, lv = lk - 1;
-            const uint32_t sk = lk % F::kStages, sv = lv % F::kStages;
-            if (ctl.fail) live = false;
-            bool got_k = false, got_v = false;
-            const uint64_t kd = smem_desc_sw128(smem_u32(kv + sk * kStage));
-            const uint64_t vd = smem_desc_mn_sw128(smem_u32(kv + sv * kStage));
+      for (int i = 0; i < NQ; ++i) pp[i] = 0;
+      auto two_on = [](uint32_t& st, uint32_t& ph) {
+        st += 2;
+        if (st >= F::kStages) {
+          st -= F::kStages;
+          ph ^= 1u;
+        }
+      };
+      bool live = true;
+      int k = 0;
+      Unit<NQ> x = next_unit<NQ>(a, plan, n_units, k);
+      while (live && x.ntm > 0) {
+        Unit<NQ> nx;
+        live = mbar_wait(&ctl.q_full, pq, a.err);
+        pq ^= 1u;
+        for (int j = 0; j <= x.ntm; ++j) {
+          const uint64_t kd = kd0 + (uint64_t)(sk * (kStage >> 4)), vd = vd0 + (uint64_t)(sv * (kStage >> 4));
+          bool got_k = false, got_v = false;
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-              const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
-              if (live && j > 0 && j - 1 < x.nt[i]) {
-                if (!got_v) live = mbar_wait(&ctl.kv_full[sv], (lv / F::kStages) & 1u, a.err);
-                got_v = true;
-                live = live && mbar_wait(&ctl.p_full[i], n_p[i]++ & 1u, a.err);
-                if (!live) break;
-                tc_fence_after();
+          for (int i = 0; i < NQ; ++i) {
+            const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
+            if (live && j > 0 && j <= x.nt[i]) {
+              if (!got_v) live = mbar_wait(&ctl.kv_full[sv], pv, a.err);
+              got_v = true;
+              live = live && mbar_wait(&ctl.p_full[i], pp[i], a.err);
+              pp[i] ^= 1u;
+              __syncwarp();
+              tc_fence_after();
+              if (live && lead) {
+                const uint32_t first = j > 1 ? 1u : 0u;
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
-                  tc_mma_bf16_ts(to, ts + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), kIdescO, (j > 1 || ks > 0) ? 1u : 0u);
+                  tc_mma_bf16_ts(to, ts + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), kIdescO, ks > 0 ? 1u : first);
                 if (j == x.nt[i]) tc_commit(&ctl.o_full[i]);
               }
-              if (live && j < x.nt[i]) {
-                if (!got_k) live = mbar_wait(&ctl.kv_full[sk], (lk / F::kStages) & 1u, a.err);
-                got_k = true;
-                if (!live) break;
-                tc_fence_after();
+            }
+            if (live && j < x.nt[i]) {
+              if (!got_k) live = mbar_wait(&ctl.kv_full[sk], pk, a.err);
+              got_k = true;
+              __syncwarp();
+              tc_fence_after();
+              if (live && lead) {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) {
                   const uint64_t off = (uint64_t)((ks >> 2) * kHalf + (ks & 3) * 32) >> 4;
@@ -354,14 +376,19 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
                 tc_commit(&ctl.s_full[i]);
               }
             }
-            if (live && j > 0) tc_commit(&ctl.kv_empty[sv]);
-            if (live && j < x.ntm) tc_commit(&ctl.kv_empty[sk]);
-            if (live && j == x.ntm - 1) tc_commit(&ctl.q_empty);
           }
-          idx += 2 * x.ntm;
+          if (live && lead) {
+            if (j > 0) tc_commit(&ctl.kv_empty[sv]);
+            if (j < x.ntm) tc_commit(&ctl.kv_empty[sk]);
+            if (j == x.ntm - 1) tc_commit(&ctl.q_empty);
+          }
+          if (j > 0) two_on(sv, pv);
+          if (j < x.ntm) two_on(sk, pk);
+          if (j == 0) nx = next_unit<NQ>(a, plan, n_units, k);  // while the softmax has the first tiles
         }
-        if (!live) ctl.fail = 1;
+        x = nx;
       }
+      if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 1) {
       // ---- TMA producer (the lanes share a tile's pages) ----
       uint32_t n_q = 0, idx = 0;
@@ -432,7 +459,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     }
   } else {
     // ---- softmax: a thread per row ----
-    if (NQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int i = NQ == 2 ? warp >> 2 : 0, quad = warp & 3, r = quad * 32 + lane;
     const uint32_t ts = tmem + i * kT + ((uint32_t)(quad * 32) << 16);
     const uint32_t to = tmem + (NQ + i) * kT + ((uint32_t)(quad * 32) << 16);
@@ -473,54 +499,63 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           fence_proxy_async_smem();
         }
         if (warp_live) {
-          // 32 columns at a time, the next ones' load under way
-          float v[2][32];
-          tmem_ld32(ts, v[0]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float* x32 = v[c & 1];
-            tc_wait_ld();
-            if (c < 3) tmem_ld32(ts + (c + 1) * 32, v[(c + 1) & 1]);
-            if (__any_sync(0xffffffffu, lim < c * 32 + 32)) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) x32[e] = c * 32 + e < lim ? x32[e] : -INFINITY;
+          const bool masked = __any_sync(0xffffffffu, lim < kT);
+          // P is formed against the maximum so far while the tile's own is found; where that
+          // turns out too far behind (and at a row's first tile), it is formed again
+          float mx = -INFINITY;
+          if (j == 0) {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              float x32[32];
+              tmem_ld32(ts + c * 32, x32);
+              tc_wait_ld();
+              if (masked) mask32(x32, lim - c * 32);
+              mx = fmaxf(mx, max32(x32));
             }
-            float b4[4] = {x32[0], x32[1], x32[2], x32[3]};
-#pragma unroll
-            for (int e = 4; e < 28; e += 8) {
-#pragma unroll
-              for (int z = 0; z < 4; ++z) b4[z] = max3(b4[z], x32[e + z], x32[e + 4 + z]);
-            }
-#pragma unroll
-            for (int z = 0; z < 4; ++z) b4[z] = fmaxf(b4[z], x32[28 + z]);
-            const float mx = max3(fmaxf(b4[0], b4[1]), b4[2], b4[3]) * sc;  // sc > 0: the maximum commutes with it
-            const bool up = row_live && (mx > m + kLag || (m == -INFINITY && mx > m));
-            if (__any_sync(0xffffffffu, up)) {
-              const float mn = up ? ceilf(mx) : m;
+          }
+          float t;
+          uint32_t w[64];
+#pragma unroll 1
+          for (bool raise = j == 0;; raise = true) {
+            if (raise) {
+              mx *= sc;  // sc > 0: the maximum commutes with it
+              const float mn = behind(mx, m) ? ceilf(mx) : m;
               const float f = m == mn ? 1.f : ex2_int(m - mn);
               m = mn;
               l *= f;
-              if (c > 0) scale_p(ts, c, f);
               if (j > 0) scale_o(to, f);
             }
             const float mb = m == -INFINITY ? 0.f : m;
             const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
             uint64_t s2[2] = {0, 0};
-            uint32_t w[16];
+            float v[2][32];
+            mx = -INFINITY;
+            tmem_ld32(ts, v[0]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float p0, p1;
-              unpack2(fma2(pack2(x32[2 * e], x32[2 * e + 1]), sc2, mb2), p0, p1);
-              p0 = ex2_approx(p0);
-              p1 = ex2_approx(p1);
-              s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
-              w[e] = pack_bf16(p0, p1);
+            for (int c = 0; c < 4; ++c) {
+              float* x32 = v[c & 1];
+              tc_wait_ld();
+              if (c < 3) tmem_ld32(ts + (c + 1) * 32, v[(c + 1) & 1]);
+              if (masked) mask32(x32, lim - c * 32);
+              mx = fmaxf(mx, max32(x32));
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                float p0, p1;
+                unpack2(fma2(pack2(x32[2 * e], x32[2 * e + 1]), sc2, mb2), p0, p1);
+                p0 = ex2_approx(p0);
+                p1 = ex2_approx(p1);
+                s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
+                w[c * 16 + e] = pack_bf16(p0, p1);
+              }
             }
-            tmem_st16(ts + c * 16, w);
             float s0, s1;
             unpack2(add2(s2[0], s2[1]), s0, s1);
-            l += s0 + s1;
+            t = s0 + s1;
+            if (!__any_sync(0xffffffffu, row_live && behind(mx * sc, m))) break;
           }
+          l += t;
+          tmem_st32(ts, w);
+          tmem_st32(ts + 32, w + 32);
           tc_wait_st();
         }
         tc_fence_before();
@@ -628,12 +663,7 @@ cudaError_t launch(const AttnArgs& a, const AttnPlan& plan, const Maps& maps, in
   cudaGetDevice(&dev);
   if (dev >= 0 && dev < 64 && !configured[dev]) {
     cudaError_t e = cudaFuncSetAttribute(attn_tc<NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
-    cudaFuncAttributes at;
-    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, attn_tc<NQ>);
     if (e != cudaSuccess) return e;
-    // the register split draws on what the block is launched with
-    if (NQ == 2 && at.numRegs * F::kThreads < kSoftRegs * F::kSoft + kRestRegs * (F::kThreads - F::kSoft))
-      return cudaErrorInvalidConfiguration;
     configured[dev] = true;
   }
   const long long most = (long long)sms * F::kCtas;
