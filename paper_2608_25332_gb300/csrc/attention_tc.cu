@@ -102,6 +102,11 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
   return p != 0;
 }
+// every lane waits; the outcome is the warp's (and known to be the same in every lane, which
+// keeps the branches on it and the MMA operands in the uniform registers)
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned* err) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -334,27 +339,24 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           ph ^= 1u;
         }
       };
-      bool live = true;
       int k = 0;
       Unit<NQ> x = next_unit<NQ>(a, plan, n_units, k);
+      bool live = true;
       while (live && x.ntm > 0) {
         Unit<NQ> nx;
-        live = mbar_wait(&ctl.q_full, pq, a.err);
+        live = warp_wait(&ctl.q_full, pq, a.err);
         pq ^= 1u;
-        for (int j = 0; j <= x.ntm; ++j) {
+        for (int j = 0; live && j <= x.ntm; ++j) {
           const uint64_t kd = kd0 + (uint64_t)(sk * (kStage >> 4)), vd = vd0 + (uint64_t)(sv * (kStage >> 4));
-          bool got_k = false, got_v = false;
+          if (j > 0) live = warp_wait(&ctl.kv_full[sv], pv, a.err);
 #pragma unroll
           for (int i = 0; i < NQ; ++i) {
             const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
-            if (live && j > 0 && j <= x.nt[i]) {
-              if (!got_v) live = mbar_wait(&ctl.kv_full[sv], pv, a.err);
-              got_v = true;
-              live = live && mbar_wait(&ctl.p_full[i], pp[i], a.err);
+            if (j > 0 && j <= x.nt[i]) {
+              if (live) live = warp_wait(&ctl.p_full[i], pp[i], a.err);
               pp[i] ^= 1u;
-              __syncwarp();
               tc_fence_after();
-              if (live && lead) {
+              if (lead) {
                 const uint32_t first = j > 1 ? 1u : 0u;
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
@@ -362,12 +364,10 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
                 if (j == x.nt[i]) tc_commit(&ctl.o_full[i]);
               }
             }
-            if (live && j < x.nt[i]) {
-              if (!got_k) live = mbar_wait(&ctl.kv_full[sk], pk, a.err);
-              got_k = true;
-              __syncwarp();
+            if (i == 0 && j < x.ntm && live) live = warp_wait(&ctl.kv_full[sk], pk, a.err);
+            if (j < x.nt[i]) {
               tc_fence_after();
-              if (live && lead) {
+              if (lead) {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) {
                   const uint64_t off = (uint64_t)((ks >> 2) * kHalf + (ks & 3) * 32) >> 4;
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
               }
             }
           }
-          if (live && lead) {
+          if (lead) {
             if (j > 0) tc_commit(&ctl.kv_empty[sv]);
             if (j < x.ntm) tc_commit(&ctl.kv_empty[sk]);
             if (j == x.ntm - 1) tc_commit(&ctl.q_empty);
