@@ -29,13 +29,16 @@ namespace {
 constexpr int kT = 128;                // rows and keys of a tile
 constexpr int kHalf = kT * 128;        // 64 elements of 128 rows: 16 KiB
 constexpr int kStage = 2 * kHalf;      // a Q, K or V tile
+// registers a thread with two row tiles: a row's 128 scores live in them; the sum over the
+// block is what it is launched with (168 a thread)
+constexpr int kSoftRegs = 224, kRestRegs = 56;
 constexpr float kLag = 8.f;            // how far (base 2) the running maximum may be behind
 
 template <int NQ>
 struct Form {
   static constexpr int kStages = NQ == 2 ? 5 : 2;
   static constexpr int kSoft = 128 * NQ;               // softmax threads
-  static constexpr int kThreads = kSoft + 64;          // + MMA warp + TMA warp
+  static constexpr int kThreads = NQ == 2 ? 384 : 192;  // + MMA warp + TMA warp (+ 2 idle)
   static constexpr int kCtas = NQ == 2 ? 1 : 2;
   static constexpr size_t kSmem = (size_t)(NQ + kStages) * kStage + 1024;
   static constexpr uint32_t kCols = 256 * NQ;          // S and O of every row tile
@@ -45,8 +48,27 @@ struct Maps {
   CUtensorMap q, k, v, kp, vp;
 };
 
+// One unit, as the producer works it out and the other roles read it (a board of kBoard
+// units in shared memory, which keeps the decoding out of their registers and way).
+template <int NQ>
+struct Unit {
+  AttnSeq s;
+  int g, part;       // key/value head (-1: no unit is left); slot of the partial results
+  int tok0;          // first token of the first row tile
+  int n_tok[NQ];     // tokens of each row tile
+  int n_prefix;      // prefix keys of the list, their tiles
+  int n_pt;
+  int t_lo;          // the unit's first tile of the list
+  int nt[NQ];        // tiles of each row tile
+  int ntm;           // the most of them
+  uint32_t load0;    // number of its first K load
+};
+constexpr int kBoard = 4;
+
 template <int NQ>
 struct Ctl {
+  Unit<NQ> board[kBoard];
+  uint64_t u_full[kBoard], u_empty[kBoard];
   uint64_t q_full, q_empty;
   uint64_t kv_full[Form<NQ>::kStages], kv_empty[Form<NQ>::kStages];
   uint64_t s_full[NQ], p_full[NQ], o_full[NQ];
@@ -96,6 +118,30 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
       "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+  uint32_t r[64];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,"
+      "%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32,%33,%34,%35,%36,%37,%38,%39,"
+      "%40,%41,%42,%43,%44,%45,%46,%47,"
+      "%48,%49,%50,%51,%52,%53,%54,%55,"
+      "%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr));
+#pragma unroll
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
 // true in one lane of a converged warp
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -141,21 +187,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// the maximum of 32 scores, with those from number n on hidden
-__device__ __forceinline__ void mask32(float* x, int n) {
+// n scores, with those from number `from` on hidden
+template <int N>
+__device__ __forceinline__ void mask_from(float* x, int from) {
 #pragma unroll
-  for (int e = 0; e < 32; ++e) x[e] = e < n ? x[e] : -INFINITY;
+  for (int e = 0; e < N; ++e) x[e] = e < from ? x[e] : -INFINITY;
 }
-__device__ __forceinline__ float max32(const float* x) {
-  float b[4] = {x[0], x[1], x[2], x[3]};
+__device__ __forceinline__ float max16(const float* x) {
+  float b[4];
 #pragma unroll
-  for (int e = 4; e < 28; e += 8) {
-#pragma unroll
-    for (int z = 0; z < 4; ++z) b[z] = max3(b[z], x[e + z], x[e + 4 + z]);
-  }
-#pragma unroll
-  for (int z = 0; z < 4; ++z) b[z] = fmaxf(b[z], x[28 + z]);
-  return max3(fmaxf(b[0], b[1]), b[2], b[3]);
+  for (int z = 0; z < 4; ++z) b[z] = max3(x[z], x[4 + z], x[8 + z]);
+  return fmaxf(max3(b[0], b[1], x[12]), max3(b[2], b[3], max3(x[13], x[14], x[15])));
 }
 // whether a maximum m, against which P is taken, has fallen too far behind mx
 __device__ __forceinline__ bool behind(float mx, float m) { return mx > m + kLag || (m == -INFINITY && mx > m); }
@@ -175,19 +217,6 @@ __device__ __noinline__ void scale_o(uint32_t to, float f) {
 // ---------------------------------------------------------------------------
 // units
 // ---------------------------------------------------------------------------
-template <int NQ>
-struct Unit {
-  AttnSeq s;
-  int g, part;       // key/value head; slot of the partial results
-  int tok0;          // first token of the first row tile
-  int n_tok[NQ];     // tokens of each row tile
-  int n_prefix;      // prefix keys of the list, their tiles
-  int n_pt;
-  int t_lo;          // the unit's first tile of the list
-  int nt[NQ];        // tiles of each row tile
-  int ntm;           // the most of them
-};
-
 template <int NQ>
 __device__ __forceinline__ Unit<NQ> unit_of(const AttnArgs& a, const AttnPlan& p, int u) {
   Unit<NQ> x;
@@ -270,13 +299,84 @@ __device__ __forceinline__ int unit_index(int k) {
   return k * G + ((k & 1) ? G - 1 - i : i);
 }
 
-// the next unit of this CTA that has tiles (ntm > 0), from its k-th on; ntm = 0: none is left
+// O / l of a thread's row, its log-sum-exp: to memory, as the result or as a part. Kept out
+// of line: its addresses would cost the tile loop registers.
 template <int NQ>
-__device__ __forceinline__ Unit<NQ> next_unit(const AttnArgs& a, const AttnPlan& p, int n_units, int& k) {
-  Unit<NQ> x;
-  x.ntm = 0;
-  for (int u; x.ntm == 0 && (u = unit_index(k)) < n_units; ++k) x = unit_of<NQ>(a, p, u);
-  return x;
+__device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, int i, int hid, float m, float l,
+                                         uint32_t to) {
+  const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
+  const int R = a.H_q / a.H_kv, TT = kT / R, tok_in = r / R, hd = r - tok_in * R;
+  const int nt = x.nt[i];
+  const bool row_live = tok_in < x.n_tok[i];
+  const int h = x.g * R + hd, tok = x.tok0 + i * TT + tok_in;
+  const size_t n_rows = (size_t)a.T_q * a.H_q, row = (size_t)(x.s.q0 + tok) * a.H_q + h;
+  const bool partial = a.n_part > 1;
+  float* po = partial ? a.part_o + ((size_t)x.part * n_rows + row) * kHeadDim : nullptr;
+  __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tok) * a.o_stride + (size_t)h * kHeadDim;
+  const bool none = l == 0.f;
+  // a row whose keys all score -inf is 0 / 0; a row without keys is 0
+  const int lo = list_key(x, x.t_lo), hi = min(list_key(x, x.t_lo + nt), x.n_prefix + x.s.k_len - hid);
+  const float nil = !partial && hi > lo ? NAN : 0.f;
+  const float inv = none ? 0.f : 1.f / l;
+  const float lse = none ? (nil == 0.f ? -INFINITY : NAN) : m + lg2_approx(l);
+  bool fine = !isnan(l);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    float o[32];
+    if (nt > 0) {
+      tmem_ld32(to + c * 32, o);
+      tc_wait_ld();
+    }
+    float bad = 0.f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      o[e] = none ? nil : o[e] * inv;
+      bad = fmaf(o[e], 0.f, bad);  // NaN once an element is not finite
+    }
+    if (!none && isnan(bad)) fine = false;
+    if (row_live) {
+      if (partial) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) store4(po + c * 32 + e, o + e);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          uint4 z;
+          z.x = pack_bf16(o[e], o[e + 1]);
+          z.y = pack_bf16(o[e + 2], o[e + 3]);
+          z.z = pack_bf16(o[e + 4], o[e + 5]);
+          z.w = pack_bf16(o[e + 6], o[e + 7]);
+          *reinterpret_cast<uint4*>(op + c * 32 + e) = z;
+        }
+      }
+    }
+  }
+  tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
+  if (row_live) {
+    if (partial)
+      a.part_lse[(size_t)x.part * n_rows + row] = lse;
+    else if (a.lse)
+      a.lse[row] = lse * kLn2;
+  }
+  // rows that are not finite: again by the definition
+  unsigned again = __ballot_sync(0xffffffffu, row_live && !fine);
+  while (again) {
+    const int src = __ffs(again) - 1;
+    again &= again - 1;
+    const int tk = __shfl_sync(0xffffffffu, tok, src), hh = __shfl_sync(0xffffffffu, h, src);
+    const int khi = __shfl_sync(0xffffffffu, hi, src);
+    float o[4];
+    float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, o);
+    const size_t rw = (size_t)(x.s.q0 + tk) * a.H_q + hh;
+    if (partial) {
+      store4(a.part_o + ((size_t)x.part * n_rows + rw) * kHeadDim + lane * 4, o);
+      if (lane == 0) a.part_lse[(size_t)x.part * n_rows + rw] = le;
+    } else {
+      if (le == -INFINITY) le = o[0] = o[1] = o[2] = o[3] = NAN;
+      store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tk) * a.o_stride + (size_t)hh * kHeadDim + lane * 4, o);
+      if (lane == 0 && a.lse) a.lse[rw] = le * kLn2;
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -298,6 +398,10 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
+    for (int n = 0; n < kBoard; ++n) {
+      mbar_init(&ctl.u_full[n], 1);
+      mbar_init(&ctl.u_empty[n], 4 * NQ + 1);
+    }
     mbar_init(&ctl.q_full, 1);
     mbar_init(&ctl.q_empty, 1);
     for (int s = 0; s < F::kStages; ++s) {
@@ -323,6 +427,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
   const uint32_t tmem = ctl.tmem;
 
   if (warp >= 4 * NQ) {
+    if (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
     if (warp == 4 * NQ) {
       // ---- MMA issuer: the whole warp walks through the tiles, one lane issues ----
       const bool lead = elect_one();
@@ -339,20 +444,27 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           ph ^= 1u;
         }
       };
-      int k = 0;
-      Unit<NQ> x = next_unit<NQ>(a, plan, n_units, k);
       bool live = true;
-      while (live && x.ntm > 0) {
-        Unit<NQ> nx;
+      for (uint32_t n = 0; live; ++n) {
+        live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err);
+        const Unit<NQ>& x = ctl.board[n % kBoard];
+        if (!live || x.g < 0) break;
+        const int ntm = x.ntm;
+        int nt[NQ];
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) nt[i] = x.nt[i];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
+        if (ntm == 0) continue;
         live = warp_wait(&ctl.q_full, pq, a.err);
         pq ^= 1u;
-        for (int j = 0; live && j <= x.ntm; ++j) {
+        for (int j = 0; live && j <= ntm; ++j) {
           const uint64_t kd = kd0 + (uint64_t)(sk * (kStage >> 4)), vd = vd0 + (uint64_t)(sv * (kStage >> 4));
           if (j > 0) live = warp_wait(&ctl.kv_full[sv], pv, a.err);
 #pragma unroll
           for (int i = 0; i < NQ; ++i) {
             const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
-            if (j > 0 && j <= x.nt[i]) {
+            if (j > 0 && j <= nt[i]) {
               if (live) live = warp_wait(&ctl.p_full[i], pp[i], a.err);
               pp[i] ^= 1u;
               tc_fence_after();
@@ -361,11 +473,11 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
                   tc_mma_bf16_ts(to, ts + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), kIdescO, ks > 0 ? 1u : first);
-                if (j == x.nt[i]) tc_commit(&ctl.o_full[i]);
+                if (j == nt[i]) tc_commit(&ctl.o_full[i]);
               }
             }
-            if (i == 0 && j < x.ntm && live) live = warp_wait(&ctl.kv_full[sk], pk, a.err);
-            if (j < x.nt[i]) {
+            if (i == 0 && j < ntm && live) live = warp_wait(&ctl.kv_full[sk], pk, a.err);
+            if (j < nt[i]) {
               tc_fence_after();
               if (lead) {
 #pragma unroll
@@ -379,14 +491,12 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           }
           if (lead) {
             if (j > 0) tc_commit(&ctl.kv_empty[sv]);
-            if (j < x.ntm) tc_commit(&ctl.kv_empty[sk]);
-            if (j == x.ntm - 1) tc_commit(&ctl.q_empty);
+            if (j < ntm) tc_commit(&ctl.kv_empty[sk]);
+            if (j == ntm - 1) tc_commit(&ctl.q_empty);
           }
           if (j > 0) two_on(sv, pv);
-          if (j < x.ntm) two_on(sk, pk);
-          if (j == 0) nx = next_unit<NQ>(a, plan, n_units, k);  // while the softmax has the first tiles
+          if (j < ntm) two_on(sk, pk);
         }
-        x = nx;
       }
       if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 1) {
@@ -424,9 +534,24 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         __syncwarp();
         return true;
       };
-      for (int k = 0, u; live && (u = unit_index(k)) < n_units; ++k) {
-        const Unit<NQ> x = unit_of<NQ>(a, plan, u);
-        if (lane == 0 && !x.s.ok) set_error(a.err, kErrBadDeviceArg);
+      for (int k = 0; live; ++k) {
+        const int u = unit_index(k), slot = k % kBoard;
+        Unit<NQ> x;
+        x.g = -1;
+        if (u < n_units) {
+          x = unit_of<NQ>(a, plan, u);
+          if (lane == 0 && !x.s.ok) set_error(a.err, kErrBadDeviceArg);
+        }
+        x.load0 = idx;
+        live = warp_wait(&ctl.u_empty[slot], ((k / kBoard) & 1u) ^ 1u, a.err) && !ctl.fail;
+        live = __all_sync(0xffffffffu, live);
+        if (!live) break;
+        if (lane == 0) {
+          ctl.board[slot] = x;
+          mbar_arrive(&ctl.u_full[slot]);
+        }
+        __syncwarp();
+        if (x.g < 0) break;
         if (x.ntm == 0) continue;
         live = load(x, x.t_lo, false);
         if (!live) break;
@@ -459,190 +584,102 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     }
   } else {
     // ---- softmax: a thread per row ----
-    const int i = NQ == 2 ? warp >> 2 : 0, quad = warp & 3, r = quad * 32 + lane;
-    const uint32_t ts = tmem + i * kT + ((uint32_t)(quad * 32) << 16);
-    const uint32_t to = tmem + (NQ + i) * kT + ((uint32_t)(quad * 32) << 16);
-    const int tok_in = r / R, hd = r - tok_in * R;
+    if (NQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int i = NQ == 2 ? warp >> 2 : 0, r = (warp & 3) * 32 + lane;
+    const uint32_t ts = tmem + i * kT + ((uint32_t)(r & ~31) << 16), to = ts + NQ * kT;
+    const int tok_in = r / R, tok_first = (r & ~31) / R;
     const float sc = a.scale_log2;
-    uint32_t n_s = 0, n_o = 0, idx = 0;
+    uint32_t n_s = 0, n_o = 0;
     bool failed = false;
-    for (int k = 0, u; !failed && (u = unit_index(k)) < n_units; ++k) {
-      const Unit<NQ> x = unit_of<NQ>(a, plan, u);
-      const int n_tok = NQ == 2 && i ? x.n_tok[NQ - 1] : x.n_tok[0], nt = NQ == 2 && i ? x.nt[NQ - 1] : x.nt[0];
-      const int tok = x.tok0 + i * TT + tok_in;
-      const bool row_live = tok_in < n_tok;
-      const bool warp_live = (quad * 32) / R < n_tok;  // the warp's first row's token
-      const int own = row_live ? attn_visible(a, x.s.q_len, x.s.k_len, tok) : x.s.k_len;
+    for (uint32_t n = 0;; ++n) {
+      if (!warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err)) failed = true;
+      const Unit<NQ>& x = ctl.board[n % kBoard];
+      if (failed || x.g < 0) break;
+      const int nt = x.nt[i];
+      const bool row_live = tok_in < x.n_tok[i], warp_live = tok_first < x.n_tok[i];
+      // hidden own keys, of this row and of the warp's first one, which sees the fewest
+      int hid = 0, hid_first;
+      {
+        const int q_len = x.s.q_len, k_len = x.s.k_len, tok = x.tok0 + i * TT;
+        if (row_live) hid = k_len - attn_visible(a, q_len, k_len, tok + tok_in);
+        hid_first = k_len - attn_visible(a, q_len, k_len, tok + tok_first);
+      }
+      int pre_left = x.n_pt - x.t_lo;  // tiles of the prefix from the unit's first tile on
+      int n_keys = pre_left > 0 ? x.n_prefix - x.t_lo * kT : x.s.k_len + pre_left * kT;  // from the tile on
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < nt; ++j) {
-        const int t = x.t_lo + j;
-        const bool pre = t < x.n_pt;
-        const int key = pre ? t * kT : (t - x.n_pt) * kT;
-        const int n_keys = (pre ? x.n_prefix : x.s.k_len) - key;   // of the list from here on
-        const int lim = (pre ? x.n_prefix : own) - key;            // that this row sees
-        if (!failed) failed = !mbar_wait(&ctl.s_full[i], n_s & 1u, a.err);
+        failed = !warp_wait(&ctl.s_full[i], n_s & 1u, a.err);
         ++n_s;
-        failed = __any_sync(0xffffffffu, failed);
         if (failed) break;
-        __syncwarp();
         tc_fence_after();
         if (n_keys < kT) {
           // rows past the end: zero before the product reads them
-          const uint32_t lv = idx + 2 * j + 1, sv = lv % F::kStages;
-          failed = !mbar_wait(&ctl.kv_full[sv], (lv / F::kStages) & 1u, a.err);
-          failed = __any_sync(0xffffffffu, failed);
+          const uint32_t lv = x.load0 + 2 * j + 1, sv = lv % F::kStages;
+          failed = !warp_wait(&ctl.kv_full[sv], (lv / F::kStages) & 1u, a.err);
           if (failed) break;
-          __syncwarp();
           uint8_t* vs = kv + sv * kStage;
           for (int q = n_keys * 16 + r; q < kT * 16; q += 128)
             *reinterpret_cast<uint4*>(vs + ((q >> 3) & 1) * kHalf + (q >> 4) * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async_smem();
+          __syncwarp();
         }
         if (warp_live) {
-          const bool masked = __any_sync(0xffffffffu, lim < kT);
-          // P is formed against the maximum so far while the tile's own is found; where that
-          // turns out too far behind (and at a row's first tile), it is formed again
-          float mx = -INFINITY;
-          if (j == 0) {
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              float x32[32];
-              tmem_ld32(ts + c * 32, x32);
-              tc_wait_ld();
-              if (masked) mask32(x32, lim - c * 32);
-              mx = fmaxf(mx, max32(x32));
-            }
-          }
-          float t;
-          uint32_t w[64];
-#pragma unroll 1
-          for (bool raise = j == 0;; raise = true) {
-            if (raise) {
-              mx *= sc;  // sc > 0: the maximum commutes with it
-              const float mn = behind(mx, m) ? ceilf(mx) : m;
-              const float f = m == mn ? 1.f : ex2_int(m - mn);
-              m = mn;
-              l *= f;
-              if (j > 0) scale_o(to, f);
-            }
-            const float mb = m == -INFINITY ? 0.f : m;
-            const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
-            uint64_t s2[2] = {0, 0};
-            float v[2][32];
-            mx = -INFINITY;
-            tmem_ld32(ts, v[0]);
+          float v[kT];
+          tmem_ld64(ts, v);
+          tmem_ld64(ts + 64, v + 64);
+          tc_wait_ld();
+          // keys that this row sees; the warp's first row sees the fewest
+          const int lim = n_keys - (pre_left > 0 ? 0 : hid);
+          if (n_keys - (pre_left > 0 ? 0 : hid_first) < kT) mask_from<kT>(v, lim);
+          float mx = max16(v);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              float* x32 = v[c & 1];
-              tc_wait_ld();
-              if (c < 3) tmem_ld32(ts + (c + 1) * 32, v[(c + 1) & 1]);
-              if (masked) mask32(x32, lim - c * 32);
-              mx = fmaxf(mx, max32(x32));
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                float p0, p1;
-                unpack2(fma2(pack2(x32[2 * e], x32[2 * e + 1]), sc2, mb2), p0, p1);
-                p0 = ex2_approx(p0);
-                p1 = ex2_approx(p1);
-                s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
-                w[c * 16 + e] = pack_bf16(p0, p1);
-              }
-            }
-            float s0, s1;
-            unpack2(add2(s2[0], s2[1]), s0, s1);
-            t = s0 + s1;
-            if (!__any_sync(0xffffffffu, row_live && behind(mx * sc, m))) break;
+          for (int c = 16; c < kT; c += 16) mx = fmaxf(mx, max16(v + c));
+          mx *= sc;  // sc > 0: the maximum commutes with it
+          if (__any_sync(0xffffffffu, row_live && behind(mx, m))) {
+            const float mn = behind(mx, m) ? ceilf(mx) : m;
+            const float f = m == mn ? 1.f : ex2_int(m - mn);
+            m = mn;
+            l *= f;
+            if (j > 0) scale_o(to, f);
           }
-          l += t;
-          tmem_st32(ts, w);
-          tmem_st32(ts + 32, w + 32);
+          const float mb = m == -INFINITY ? 0.f : m;
+          const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
+          uint64_t s2[2] = {0, 0};
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t w[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float p0, p1;
+              unpack2(fma2(pack2(v[c * 64 + 2 * e], v[c * 64 + 2 * e + 1]), sc2, mb2), p0, p1);
+              p0 = ex2_approx(p0);
+              p1 = ex2_approx(p1);
+              s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
+              w[e] = pack_bf16(p0, p1);
+            }
+            tmem_st32(ts + c * 32, w);
+          }
+          float s0, s1;
+          unpack2(add2(s2[0], s2[1]), s0, s1);
+          l += s0 + s1;
           tc_wait_st();
         }
+        n_keys = --pre_left == 0 ? x.s.k_len : n_keys - kT;  // of the next tile
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.p_full[i]);
       }
-      idx += 2 * x.ntm;
       if (failed) break;
       // ---- epilogue: O / l to memory ----
       if (nt > 0) {
-        failed = !mbar_wait(&ctl.o_full[i], n_o & 1u, a.err);
+        failed = !warp_wait(&ctl.o_full[i], n_o & 1u, a.err);
         ++n_o;
-        failed = __any_sync(0xffffffffu, failed);
         if (failed) break;
-        __syncwarp();
         tc_fence_after();
       }
-      if (!warp_live) continue;
-      const int h = x.g * R + hd;
-      const size_t n_rows = (size_t)a.T_q * a.H_q, row = (size_t)(x.s.q0 + tok) * a.H_q + h;
-      const bool partial = a.n_part > 1;
-      float* po = partial ? a.part_o + ((size_t)x.part * n_rows + row) * kHeadDim : nullptr;
-      __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tok) * a.o_stride + (size_t)h * kHeadDim;
-      const bool none = l == 0.f;
-      // a row whose keys all score -inf is 0 / 0; a row without keys is 0
-      const int lo = list_key(x, x.t_lo), hi = min(list_key(x, x.t_lo + nt), x.n_prefix + own);
-      const float nil = !partial && hi > lo ? NAN : 0.f;
-      const float inv = none ? 0.f : 1.f / l;
-      float lse = none ? (nil == 0.f ? -INFINITY : NAN) : m + lg2_approx(l);
-      bool fine = !isnan(l);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float o[32];
-        if (nt > 0) {
-          tmem_ld32(to + c * 32, o);
-          tc_wait_ld();
-        }
-        float bad = 0.f;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          o[e] = none ? nil : o[e] * inv;
-          bad = fmaf(o[e], 0.f, bad);  // NaN once an element is not finite
-        }
-        if (!none && isnan(bad)) fine = false;
-        if (row_live) {
-          if (partial) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) store4(po + c * 32 + e, o + e);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint4 w;
-              w.x = pack_bf16(o[e], o[e + 1]);
-              w.y = pack_bf16(o[e + 2], o[e + 3]);
-              w.z = pack_bf16(o[e + 4], o[e + 5]);
-              w.w = pack_bf16(o[e + 6], o[e + 7]);
-              *reinterpret_cast<uint4*>(op + c * 32 + e) = w;
-            }
-          }
-        }
-      }
-      tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
-      if (row_live) {
-        if (partial)
-          a.part_lse[(size_t)x.part * n_rows + row] = lse;
-        else if (a.lse)
-          a.lse[row] = lse * kLn2;
-      }
-      // rows that are not finite: again by the definition
-      unsigned again = __ballot_sync(0xffffffffu, row_live && !fine);
-      while (again) {
-        const int src = __ffs(again) - 1;
-        again &= again - 1;
-        const int tk = __shfl_sync(0xffffffffu, tok, src), hh = __shfl_sync(0xffffffffu, h, src);
-        const int khi = __shfl_sync(0xffffffffu, hi, src);
-        float o[4];
-        float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, o);
-        const size_t rw = (size_t)(x.s.q0 + tk) * a.H_q + hh;
-        if (partial) {
-          store4(a.part_o + ((size_t)x.part * n_rows + rw) * kHeadDim + lane * 4, o);
-          if (lane == 0) a.part_lse[(size_t)x.part * n_rows + rw] = le;
-        } else {
-          if (le == -INFINITY) le = o[0] = o[1] = o[2] = o[3] = NAN;
-          store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tk) * a.o_stride + (size_t)hh * kHeadDim + lane * 4, o);
-          if (lane == 0 && a.lse) a.lse[rw] = le * kLn2;
-        }
-      }
+      if (warp_live) finish_rows<NQ>(a, x, i, hid, m, l, to);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
     }
     if (failed) ctl.fail = 1;
   }
@@ -663,7 +700,12 @@ cudaError_t launch(const AttnArgs& a, const AttnPlan& plan, const Maps& maps, in
   cudaGetDevice(&dev);
   if (dev >= 0 && dev < 64 && !configured[dev]) {
     cudaError_t e = cudaFuncSetAttribute(attn_tc<NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
+    cudaFuncAttributes at;
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, attn_tc<NQ>);
     if (e != cudaSuccess) return e;
+    // a register split that the launch does not cover would wait for ever
+    if (NQ == 2 && at.numRegs * F::kThreads < kSoftRegs * F::kSoft + kRestRegs * (F::kThreads - F::kSoft))
+      return cudaErrorInvalidConfiguration;
     configured[dev] = true;
   }
   const long long most = (long long)sms * F::kCtas;
