@@ -9,11 +9,13 @@
 //   O += P V    8 tcgen05.mma, P read from tensor memory, V as it lies in memory (keys by
 //               elements, an operand whose rows run along N), O in tensor memory.
 // P is rounded to bf16 for its product (the only 16-bit operand type that V allows); the
-// sum of a row adds the unrounded values. The maximum that P is taken against follows the
-// true one only once it is 2^8 behind: P stays below 2^8, which costs no accuracy in floating
-// point, and O is rescaled a few times a row instead of at every tile. S of a tile is
-// complete after the product of the tile before (one thread issues both, and a commit covers
-// all that it issued), so a rescale needs no further wait.
+// sum of a row adds the unrounded values. The maximum that P is taken against (a whole
+// number) is raised only where a tile's values add up to more than 2^10: larger values of P
+// cost no accuracy in floating point, O is rescaled a few times a row instead of at every
+// tile, and the other tiles need no maximum at all, whose 64 three-way comparisons had
+// taken a third of a tile's time. S of a tile is complete after the product of the tile before
+// (one thread issues both, and a commit covers all that it issued), so a rescale needs no
+// further wait.
 // Roles: warps 0 .. 4 NQ - 1 softmax, then one warp issues the MMAs and one the TMA loads.
 // K and V tiles share a ring of 32 KiB stages. While the softmax works on one row tile, the
 // tensor cores multiply for the other (NQ = 2, one CTA an SM), or for the other CTA of the
@@ -32,7 +34,7 @@ constexpr int kStage = 2 * kHalf;      // a Q, K or V tile
 // registers a thread with two row tiles: a row's 128 scores live in them; the sum over the
 // block is what it is launched with (168 a thread)
 constexpr int kSoftRegs = 224, kRestRegs = 56;
-constexpr float kLag = 8.f;            // how far (base 2) the running maximum may be behind
+constexpr float kMostSum = 1024.f;     // of a row's 128 values of P before its maximum is raised
 
 template <int NQ>
 struct Form {
@@ -193,15 +195,20 @@ __device__ __forceinline__ void mask_from(float* x, int from) {
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = e < from ? x[e] : -INFINITY;
 }
-__device__ __forceinline__ float max16(const float* x) {
-  float b[4];
+// the largest of 128 in eight chains
+__device__ __forceinline__ float max128(const float* x) {
+  float b[8];
 #pragma unroll
-  for (int z = 0; z < 4; ++z) b[z] = max3(x[z], x[4 + z], x[8 + z]);
-  return fmaxf(max3(b[0], b[1], x[12]), max3(b[2], b[3], max3(x[13], x[14], x[15])));
+  for (int z = 0; z < 8; ++z) b[z] = max3(x[z], x[8 + z], x[16 + z]);
+#pragma unroll
+  for (int e = 24; e < 120; e += 16) {
+#pragma unroll
+    for (int z = 0; z < 8; ++z) b[z] = max3(b[z], x[e + z], x[e + 8 + z]);
+  }
+#pragma unroll
+  for (int z = 0; z < 8; ++z) b[z] = fmaxf(b[z], x[120 + z]);
+  return fmaxf(max3(b[0], b[1], b[2]), max3(max3(b[3], b[4], b[5]), b[6], b[7]));
 }
-// whether a maximum m, against which P is taken, has fallen too far behind mx
-__device__ __forceinline__ bool behind(float mx, float m) { return mx > m + kLag || (m == -INFINITY && mx > m); }
-
 // this thread's row of O times f
 __device__ __noinline__ void scale_o(uint32_t to, float f) {
   for (int z = 0; z < kHeadDim / 32; ++z) {
@@ -624,44 +631,52 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           __syncwarp();
         }
         if (warp_live) {
-          float v[kT];
-          tmem_ld64(ts, v);
-          tmem_ld64(ts + 64, v + 64);
-          tc_wait_ld();
-          // keys that this row sees; the warp's first row sees the fewest
-          const int lim = n_keys - (pre_left > 0 ? 0 : hid);
-          if (n_keys - (pre_left > 0 ? 0 : hid_first) < kT) mask_from<kT>(v, lim);
-          float mx = max16(v);
+          // P is formed against the maximum so far. No maximum is looked for: a tile's sum shows
+          // whether one of its terms is too large (and at a row's first keys there is no
+          // maximum yet); only then it is found and P formed again from the scores, which
+          // are still there
+          const int lim = n_keys - (pre_left > 0 ? 0 : hid);  // keys that this row sees
+          const bool masked = n_keys - (pre_left > 0 ? 0 : hid_first) < kT;  // the warp's first row sees the fewest
+          float t;
+          uint32_t w[kT / 2];
+#pragma unroll 1
+          for (bool raise = __any_sync(0xffffffffu, m == -INFINITY && lim > 0 && row_live);;) {
+            float v[kT];
+            tmem_ld64(ts, v);
+            tmem_ld64(ts + 64, v + 64);
+            tc_wait_ld();
+            if (masked) mask_from<kT>(v, lim);
+            if (raise) {
+              const float mn = fmaxf(m, ceilf(max128(v) * sc));  // sc > 0: the maximum commutes with it
+              const float f = m == mn ? 1.f : ex2_int(m - mn);
+              m = mn;
+              l *= f;
+              if (j > 0) scale_o(to, f);
+              raise = false;
+              continue;
+            }
+            const float mb = m == -INFINITY ? 0.f : m;
+            const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
+            uint64_t s2[2] = {0, 0};
 #pragma unroll
-          for (int c = 16; c < kT; c += 16) mx = fmaxf(mx, max16(v + c));
-          mx *= sc;  // sc > 0: the maximum commutes with it
-          if (__any_sync(0xffffffffu, row_live && behind(mx, m))) {
-            const float mn = behind(mx, m) ? ceilf(mx) : m;
-            const float f = m == mn ? 1.f : ex2_int(m - mn);
-            m = mn;
-            l *= f;
-            if (j > 0) scale_o(to, f);
-          }
-          const float mb = m == -INFINITY ? 0.f : m;
-          const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
-          uint64_t s2[2] = {0, 0};
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t w[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
+            for (int e = 0; e < kT / 2; ++e) {
               float p0, p1;
-              unpack2(fma2(pack2(v[c * 64 + 2 * e], v[c * 64 + 2 * e + 1]), sc2, mb2), p0, p1);
+              unpack2(fma2(pack2(v[2 * e], v[2 * e + 1]), sc2, mb2), p0, p1);
               p0 = ex2_approx(p0);
               p1 = ex2_approx(p1);
               s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
               w[e] = pack_bf16(p0, p1);
             }
-            tmem_st32(ts + c * 32, w);
+            float s0, s1;
+            unpack2(add2(s2[0], s2[1]), s0, s1);
+            t = s0 + s1;
+            // against the tile's own maximum the sum is kT at most, so this ends
+            raise = __any_sync(0xffffffffu, row_live && t > kMostSum);
+            if (!raise) break;
           }
-          float s0, s1;
-          unpack2(add2(s2[0], s2[1]), s0, s1);
-          l += s0 + s1;
+          l += t;
+          tmem_st32(ts, w);
+          tmem_st32(ts + 32, w + 32);
           tc_wait_st();
         }
         n_keys = --pre_left == 0 ? x.s.k_len : n_keys - kT;  // of the next tile
