@@ -306,8 +306,33 @@ __device__ __forceinline__ int unit_index(int k) {
   return k * G + ((k & 1) ? G - 1 - i : i);
 }
 
+// Four lanes hold a 64-byte run of a row each (four 16-byte pieces); afterwards lane q of the
+// four holds piece q of all four rows, so that a store covers whole runs.
+__device__ __forceinline__ uint4 shfl_xor4(uint4 v, int m) {
+  v.x = __shfl_xor_sync(0xffffffffu, v.x, m);
+  v.y = __shfl_xor_sync(0xffffffffu, v.y, m);
+  v.z = __shfl_xor_sync(0xffffffffu, v.z, m);
+  v.w = __shfl_xor_sync(0xffffffffu, v.w, m);
+  return v;
+}
+__device__ __forceinline__ void transpose4(uint4* u) {
+  const bool b0 = threadIdx.x & 1, b1 = threadIdx.x & 2;
+#pragma unroll
+  for (int k = 0; k < 4; k += 2) {
+    const uint4 got = shfl_xor4(b0 ? u[k] : u[k + 1], 1);
+    if (b0) u[k] = got; else u[k + 1] = got;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint4 got = shfl_xor4(b1 ? u[k] : u[k + 2], 2);
+    if (b1) u[k] = got; else u[k + 2] = got;
+  }
+}
+
 // O / l of a thread's row, its log-sum-exp: to memory, as the result or as a part. Kept out
-// of line: its addresses would cost the tile loop registers.
+// of line: its addresses would cost the tile loop registers. Stored 16 bytes a lane along
+// the lanes' own rows, the 32 lines of every store took the SM's load/store unit 4000 clocks a
+// unit; with the pieces of four lanes exchanged it is a quarter.
 template <int NQ>
 __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, int i, int hid, float m, float l,
                                          uint32_t to) {
@@ -318,8 +343,6 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
   const int h = x.g * R + hd, tok = x.tok0 + i * TT + tok_in;
   const size_t n_rows = (size_t)a.T_q * a.H_q, row = (size_t)(x.s.q0 + tok) * a.H_q + h;
   const bool partial = a.n_part > 1;
-  float* po = partial ? a.part_o + ((size_t)x.part * n_rows + row) * kHeadDim : nullptr;
-  __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tok) * a.o_stride + (size_t)h * kHeadDim;
   const bool none = l == 0.f;
   // a row whose keys all score -inf is 0 / 0; a row without keys is 0
   const int lo = list_key(x, x.t_lo), hi = min(list_key(x, x.t_lo + nt), x.n_prefix + x.s.k_len - hid);
@@ -327,7 +350,18 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
   const float inv = none ? 0.f : 1.f / l;
   const float lse = none ? (nil == 0.f ? -INFINITY : NAN) : m + lg2_approx(l);
   bool fine = !isnan(l);
+  char* dst = partial ? reinterpret_cast<char*>(a.part_o + ((size_t)x.part * n_rows + row) * kHeadDim)
+                      : reinterpret_cast<char*>(static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tok) * a.o_stride +
+                                                (size_t)h * kHeadDim);
+  if (!row_live) dst = nullptr;
+  char* to4[4];  // where this lane's piece of the four rows goes
 #pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const unsigned long long d =
+        __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), (lane & ~3) + s);
+    to4[s] = d ? reinterpret_cast<char*>(d) + (lane & 3) * 16 : nullptr;
+  }
+#pragma unroll 1
   for (int c = 0; c < 4; ++c) {
     float o[32];
     if (nt > 0) {
@@ -341,21 +375,29 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
       bad = fmaf(o[e], 0.f, bad);  // NaN once an element is not finite
     }
     if (!none && isnan(bad)) fine = false;
-    if (row_live) {
-      if (partial) {
+    if (partial) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) store4(po + c * 32 + e, o + e);
-      } else {
+      for (int z = 0; z < 2; ++z) {
+        uint4 u[4];
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          uint4 z;
-          z.x = pack_bf16(o[e], o[e + 1]);
-          z.y = pack_bf16(o[e + 2], o[e + 3]);
-          z.z = pack_bf16(o[e + 4], o[e + 5]);
-          z.w = pack_bf16(o[e + 6], o[e + 7]);
-          *reinterpret_cast<uint4*>(op + c * 32 + e) = z;
-        }
+        for (int k = 0; k < 4; ++k)
+          u[k] = make_uint4(__float_as_uint(o[z * 16 + k * 4]), __float_as_uint(o[z * 16 + k * 4 + 1]),
+                            __float_as_uint(o[z * 16 + k * 4 + 2]), __float_as_uint(o[z * 16 + k * 4 + 3]));
+        transpose4(u);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          if (to4[s]) *reinterpret_cast<uint4*>(to4[s] + c * 128 + z * 64) = u[s];
       }
+    } else {
+      uint4 u[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        u[k] = make_uint4(pack_bf16(o[k * 8], o[k * 8 + 1]), pack_bf16(o[k * 8 + 2], o[k * 8 + 3]),
+                          pack_bf16(o[k * 8 + 4], o[k * 8 + 5]), pack_bf16(o[k * 8 + 6], o[k * 8 + 7]));
+      transpose4(u);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (to4[s]) *reinterpret_cast<uint4*>(to4[s] + c * 64) = u[s];
     }
   }
   tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
@@ -365,7 +407,8 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
     else if (a.lse)
       a.lse[row] = lse * kLn2;
   }
-  // rows that are not finite: again by the definition
+  // rows that are not finite: again by the definition (past the other lanes' stores to them)
+  __syncwarp();
   unsigned again = __ballot_sync(0xffffffffu, row_live && !fine);
   while (again) {
     const int src = __ffs(again) - 1;
