@@ -11,14 +11,15 @@ namespace {
 // ---------------------------------------------------------------------------
 // block tables and slot maps
 //
-// One cluster. Its CTAs all scan the requests (1024 at a time, in order) and share out the
-// writes, so one launch does both passes: ended requests' pages onto the free stack, then,
-// past a cluster barrier, pages off it in request order (those of a request that no longer
-// fits are not taken), the tables' new entries and a slot for every new token. Lengths and
-// the free count may be updated in place, so they are written past a last barrier. Bound by
-// latency: two block scans and two cluster barriers.
+// One cluster. Its CTAs all scan the requests (a block of them at a time, in order) and share
+// out the writes, so one launch does both passes: ended requests' pages onto the free stack,
+// then, past a cluster barrier, pages off it in request order (those of a request that no
+// longer fits are not taken), the tables' new entries and a slot for every new token. Lengths
+// and the free count may be updated in place, so they are written past a last barrier. Bound
+// by latency: two block scans and the barriers, with the requests read once where one block
+// holds them all. A decode step (256 requests, a token each) runs on one CTA of 256 threads.
 // ---------------------------------------------------------------------------
-constexpr int kThr = 1024;
+constexpr int kThr = 1024;  // at most
 
 struct Scan {
   int pages[32];
@@ -45,8 +46,9 @@ __device__ __forceinline__ void block_scan(Scan& sc, int& pages, long long& rows
     sc.rows[warp] = r;
   }
   __syncthreads();
-  int wp = sc.pages[lane];
-  long long wr = sc.rows[lane];
+  const bool has = lane < (int)(blockDim.x >> 5);
+  int wp = has ? sc.pages[lane] : 0;
+  long long wr = has ? sc.rows[lane] : 0;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int pu = __shfl_up_sync(0xffffffffu, wp, o);
@@ -98,82 +100,93 @@ __device__ __forceinline__ Request request(const PageTablesArgs& a, int b) {
   return q;
 }
 
+// a barrier over the cluster; one CTA needs only its own
+__device__ __forceinline__ void all_sync(int n_cta) {
+  if (n_cta > 1)
+    cooperative_groups::this_cluster().sync();
+  else
+    __syncthreads();
+}
+
 __global__ void __launch_bounds__(kThr) page_tables_kernel(const PageTablesArgs a) {
-  namespace cg = cooperative_groups;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int rank = (int)cluster.block_rank(), n_cta = (int)cluster.num_blocks();
-  const int gtid = rank * kThr + (int)threadIdx.x, gthr = n_cta * kThr;
+  const int n_cta = (int)gridDim.x, rank = (int)blockIdx.x, thr = (int)blockDim.x;  // the grid is one cluster
+  const int gtid = rank * thr + (int)threadIdx.x, gthr = n_cta * thr;
+  const bool single = a.B <= thr;
   __shared__ Scan sc;
   __shared__ int s_pages[kThr], s_held[kThr], s_kv[kThr], s_take[kThr];
   __shared__ long long s_rows[kThr];
+  __shared__ int s_used;
 
   // ended requests' pages onto the stack
   int count = *a.free_count;
+  Request q = request(a, (int)threadIdx.x);
+  if (threadIdx.x == 0) s_used = 0;
   if (count < 0 || count > a.n_free_max) {
     if (gtid == 0) set_error(a.err, kErrBadDeviceArg);
     count = min(max(count, 0), a.n_free_max);
   }
   long long back = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThr) {
-    const Request q = request(a, b0 + (int)threadIdx.x);
-    int at = q.end ? q.held : 0, all;
+  for (int b0 = 0; b0 < a.B; b0 += thr) {
+    if (b0 > 0) q = request(a, b0 + (int)threadIdx.x);
+    const int mine = q.end ? q.held : 0;
+    if (!__syncthreads_or(mine)) continue;
+    int at = mine, all;
     long long r = 0, r_all;
-    const int mine = at;
     block_scan(sc, at, r, all, r_all);
-    if (all) {
-      s_pages[threadIdx.x] = at;
-      s_take[threadIdx.x] = mine;
-      __syncthreads();
-      for (int i = gtid; i < all; i += gthr) {
-        const int j = last_at_most(s_pages, kThr, i);
-        const long long to = count + back + i;
-        if (to < a.n_free_max)
-          a.free_pages[to] = a.block_table[(size_t)(b0 + j) * a.max_pages + (i - s_pages[j])];
-        else
-          set_error(a.err, kErrBadDeviceArg);
-      }
+    s_pages[threadIdx.x] = at;
+    __syncthreads();
+    for (int i = gtid; i < all; i += gthr) {
+      const int j = last_at_most(s_pages, thr, i);
+      const long long to = count + back + i;
+      if (to < a.n_free_max)
+        a.free_pages[to] = a.block_table[(size_t)(b0 + j) * a.max_pages + (i - s_pages[j])];
+      else
+        set_error(a.err, kErrBadDeviceArg);
     }
     back += all;
   }
   const int total = (int)min((long long)a.n_free_max, count + back);
-  cluster.sync();  // the stack is whole
+  all_sync(n_cta);  // the stack is whole
 
   // pages off its top
   long long pages_done = 0, rows_done = 0;  // of the requests before the chunk
   int used = 0;                             // pages of granted requests
-  Request q = {0, 0, 0, 0, false, false};
   bool ok = false;
   long long row = 0;
-  auto chunk = [&](int b0) {
-    q = request(a, b0 + (int)threadIdx.x);
+  // request b0 + threadIdx.x: its first new row, whether it is granted; its first page
+  auto place = [&](int b0) {
+    if (!single) q = request(a, b0 + (int)threadIdx.x);
     int p = q.need, p_all;
     long long r_all;
     row = q.add;
     block_scan(sc, p, row, p_all, r_all);
     row += rows_done;
     const long long first = pages_done + p;
-    const bool fits = row + q.add <= a.T_max;
-    ok = !q.end && !q.bad && fits && (q.need == 0 || first + q.need <= total);
-    if (b0 + (int)threadIdx.x < a.B && rank == 0 && (q.bad || !fits)) set_error(a.err, kErrBadDeviceArg);
+    ok = !q.end && !q.bad && row + q.add <= a.T_max && (q.need == 0 || first + q.need <= total);
+    pages_done += p_all;
+    rows_done += r_all;
+    return first;
+  };
+  for (int b0 = 0; b0 < a.B; b0 += thr) {
+    const long long p0 = pages_done, r0 = rows_done;
+    const long long first = place(b0);
+    if (b0 + (int)threadIdx.x < a.B && rank == 0 && (q.bad || row + q.add > a.T_max)) set_error(a.err, kErrBadDeviceArg);
     s_pages[threadIdx.x] = (int)min(first, 0x7fffffffll);
     s_rows[threadIdx.x] = row;
     s_held[threadIdx.x] = q.held;
     s_kv[threadIdx.x] = q.kv;
     s_take[threadIdx.x] = ok ? q.need : -1;
-    // granted requests with pages end at the stack's first `total` of the order
-    used = max(used, __reduce_max_sync(0xffffffffu, ok && q.need ? (int)(first + q.need) : 0));
+    // requests with pages are granted in order, so the last one's end is what was used
+    used = max(used, ok && q.need ? (int)(first + q.need) : 0);
     __syncthreads();
-    const long long p0 = pages_done, r0 = rows_done;
-    pages_done += p_all;
-    rows_done += r_all;
     // the tables' new entries
     for (long long i = p0 + gtid; i < min(pages_done, (long long)total); i += gthr) {
-      const int j = last_at_most(s_pages, kThr, (int)i), k = (int)i - s_pages[j];
+      const int j = last_at_most(s_pages, thr, (int)i), k = (int)i - s_pages[j];
       if (k < s_take[j]) a.block_table[(size_t)(b0 + j) * a.max_pages + s_held[j] + k] = a.free_pages[total - 1 - i];
     }
     // a slot for every new token
     for (long long t = r0 + gtid; t < min(rows_done, (long long)a.T_max); t += gthr) {
-      const int j = last_at_most(s_rows, kThr, t);
+      const int j = last_at_most(s_rows, thr, t);
       int slot = -1;
       if (s_take[j] >= 0) {
         const int pos = s_kv[j] + (int)(t - s_rows[j]), pi = pos >> a.page_shift;
@@ -183,39 +196,27 @@ __global__ void __launch_bounds__(kThr) page_tables_kernel(const PageTablesArgs 
       }
       a.slot_map_out[t] = slot;
     }
-    __syncthreads();  // the arrays may change
-  };
-  for (int b0 = 0; b0 < a.B; b0 += kThr) chunk(b0);
+    if (!single) __syncthreads();  // the arrays may change
+  }
   for (long long t = rows_done + gtid; t < a.T_max; t += gthr) a.slot_map_out[t] = -1;
+  if (rank == 0) {
+    used = __reduce_max_sync(0xffffffffu, used);
+    if ((threadIdx.x & 31) == 0 && used) atomicMax(&s_used, used);
+  }
   const long long rows_all = rows_done;
 
-  // lengths, which the calls before and after this one may hold in one place
-  cluster.sync();
+  // lengths and the free count, which calls may keep in one place: past everybody's reads
+  all_sync(n_cta);
   if (rank != 0) return;
-  __shared__ int s_used;
-  if (threadIdx.x == 0) s_used = 0;
-  __syncthreads();
-  atomicMax(&s_used, used);
   pages_done = rows_done = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThr) {
+  for (int b0 = 0; b0 < a.B; b0 += thr) {
     const int b = b0 + (int)threadIdx.x;
-    if (a.B > kThr) {  // this chunk's requests again
-      q = request(a, b);
-      int p = q.need, p_all;
-      long long r_all;
-      row = q.add;
-      block_scan(sc, p, row, p_all, r_all);
-      row += rows_done;
-      ok = !q.end && !q.bad && row + q.add <= a.T_max && (q.need == 0 || pages_done + p + q.need <= total);
-      pages_done += p_all;
-      rows_done += r_all;
-    }
+    if (!single) place(b0);  // this chunk's requests again
     if (b < a.B) {
       a.kv_len_out[b] = q.end && !q.bad ? 0 : ok ? q.kv + q.add : q.kv;
       a.row_start_out[b] = (int)min(row, 0x7fffffffll);
     }
   }
-  __syncthreads();
   if (threadIdx.x == 0) {
     a.row_start_out[a.B] = (int)min(rows_all, 0x7fffffffll);
     *a.free_count_out = total - s_used;
@@ -263,15 +264,20 @@ __global__ void __launch_bounds__(kAppThr) kv_append_kernel(const KvAppendArgs a
 }  // namespace
 
 cudaError_t page_tables_launch(const PageTablesArgs& a, cudaStream_t s) {
+  // few requests and slots: one small CTA, whose barriers are quick; else eight large ones
+  // (the portable cluster's most) from four slots a thread on
+  const int thr = a.B <= 256 && a.T_max <= 1024 ? 256 : kThr;
+  if (a.T_max <= 4 * thr) {
+    page_tables_kernel<<<1, thr, 0, s>>>(a);
+    return cudaGetLastError();
+  }
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
-  // a CTA writes 2048 slots in two rounds; eight is the portable cluster's most
-  const unsigned n = a.T_max <= 2048 ? 1u : 8u;
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = n;
+  attr[0].val.clusterDim.x = 8;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(n);
+  cfg.gridDim = dim3(8);
   cfg.blockDim = dim3(kThr);
   cfg.stream = s;
   cfg.attrs = attr;
