@@ -1188,6 +1188,7 @@ struct AttnCut {
   bool tc;
   int n_own, n_prefix, n_part;  // parts of a row's keys (prompt: n_part only)
   AttnPlan plan;                // tensor cores
+  int n_spans;                  // decoding on the tensor cores: CTAs of the own keys (0: as units of plan)
 };
 
 // CUDA cores: row tiles of 64 packed rows, parts of four 64-key tiles or more. Tensor cores:
@@ -1222,8 +1223,11 @@ AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int p
   return c;
 }
 
-// Tensor cores: units of about as many 128-key tiles as a CTA's even share, two at least (a
-// prefix part writes as many bytes of partial results as one tile has).
+// Tensor cores, up to eight heads a group: the own keys' tiles shared out evenly over two CTAs
+// an SM (two tiles a CTA at least), the prefix's as units of the row form, with the keys shared
+// out until its CTAs have one each, four tiles or more a part (a part writes as many bytes of
+// partial results as one tile has). More heads a group: units of the row form for both, of
+// about as many tiles as a CTA's even share, two at least.
 AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int dtype, int algo) {
   AttnCut c;
   memset(&c, 0, sizeof(c));
@@ -1237,7 +1241,20 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
     return c;
   }
   const int TT = 128 / (R > 128 ? 128 : R);
+  AttnPlan& p = c.plan;
   const long long own_tiles = ((long long)kv_len_max + 127) / 128, pre_tiles = ((long long)prefix_len + 127) / 128;
+  if (R <= kSpanHeads) {
+    const long long tiles = (long long)B * H_kv * (own_tiles > 0 ? own_tiles : 1);
+    c.n_spans = (int)((tiles + 1) / 2 < 2 * kPlanSms ? (tiles + 1) / 2 : 2 * kPlanSms);
+    p.nq = B <= TT ? 1 : 2;
+    const long long units = ((long long)B + p.nq * TT - 1) / (p.nq * TT) * H_kv;
+    c.n_prefix = attn_parts(units, prefix_len, kPlanSms * (p.nq == 2 ? 1 : 2), 512, 64);
+    c.n_part = c.n_prefix;
+    p.n_prefix_parts = c.n_prefix;
+    p.n_prefix_units = (int)(units * c.n_prefix);
+    p.n_units = p.n_prefix_units;
+    return c;
+  }
   const long long own_units = (long long)B * H_kv, pre_units = (((long long)B + TT - 1) / TT) * H_kv;
   long long share = (own_units * own_tiles + pre_units * pre_tiles + 2 * kPlanSms - 1) / (2 * kPlanSms);
   if (share < 2) share = 2;
@@ -1247,11 +1264,11 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
   if (c.n_prefix > 64) c.n_prefix = 64;
   if (c.n_own + c.n_prefix == 0) c.n_own = 1;
   c.n_part = c.n_own + c.n_prefix;
-  c.plan.nq = 1;
-  c.plan.n_own_parts = c.n_own;
-  c.plan.n_prefix_parts = c.n_prefix;
-  c.plan.n_prefix_units = (int)(pre_units * c.n_prefix);
-  c.plan.n_units = own_units * c.n_own + pre_units * c.n_prefix;
+  p.nq = 1;
+  p.n_own_parts = c.n_own;
+  p.n_prefix_parts = c.n_prefix;
+  p.n_prefix_units = (int)(pre_units * c.n_prefix);
+  p.n_units = own_units * c.n_own + pre_units * c.n_prefix;
   return c;
 }
 
@@ -1259,6 +1276,25 @@ size_t attn_ws(Carve& c, int n_part, int T_q, int H_q, float** part_o, float** p
   if (n_part <= 1) return 0;
   *part_o = c.take<float>((size_t)n_part * T_q * H_q * kHeadDim);
   *part_lse = c.take<float>((size_t)n_part * T_q * H_q);
+  return c.off;
+}
+
+// a decode call's workspace
+size_t decode_ws(Carve& c, const AttnCut& cut, int B, int H_q, int H_kv, float** part_o, float** part_lse,
+                 AttnSpans* sp) {
+  if (cut.n_spans == 0) return attn_ws(c, cut.n_part, B, H_q, part_o, part_lse);
+  const size_t rows = (size_t)B * H_q, pieces = 2 * (size_t)cut.n_spans * (H_q / H_kv);
+  sp->n_spans = cut.n_spans;
+  sp->n_prefix = cut.n_prefix;
+  sp->before = c.take<long long>((size_t)B + 1);
+  sp->piece_o = c.take<float>(pieces * kHeadDim);
+  sp->piece_lse = c.take<float>(pieces);
+  if (cut.n_prefix > 0) {
+    sp->whole_o = c.take<float>(rows * kHeadDim);
+    sp->whole_lse = c.take<float>(rows);
+    *part_o = c.take<float>(cut.n_prefix * rows * kHeadDim);
+    *part_lse = c.take<float>(cut.n_prefix * rows);
+  }
   return c.off;
 }
 
@@ -1390,7 +1426,8 @@ extern "C" size_t provip_decode_attention_workspace_size(int B, int H_q, int H_k
   if (B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || kv_len_max < 0 || prefix_len < 0) return 0;
   Carve c(nullptr);
   float *po, *pl;
-  return attn_ws(c, decode_cut(B, H_q, H_kv, kv_len_max, prefix_len, dtype, algo).n_part, B, H_q, &po, &pl);
+  AttnSpans sp;
+  return decode_ws(c, decode_cut(B, H_q, H_kv, kv_len_max, prefix_len, dtype, algo), B, H_q, H_kv, &po, &pl, &sp);
 }
 
 extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
@@ -1454,10 +1491,22 @@ extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B,
   a.n_part = cut.n_part;
   a.err = d->status;
   Carve c(ws);
-  attn_ws(c, a.n_part, B, H_q, &a.part_o, &a.part_lse);
+  AttnSpans sp;
+  memset(&sp, 0, sizeof(sp));
+  decode_ws(c, cut, B, H_q, H_kv, &a.part_o, &a.part_lse, &sp);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cut.tc ? attn_tc_launch(a, cut.plan, d->sms, s) : attn_decode_simt_launch(a, cut.n_own, dtype, s);
-  if (e == cudaSuccess && a.n_part > 1) e = attn_join_launch(a, dtype, s);
+  cudaError_t e = cudaSuccess;
+  if (cut.n_spans > 0) {
+    if (cut.n_prefix > 0) {
+      AttnArgs pre = a;
+      pre.n_part = cut.n_prefix + 1;  // always as parts
+      e = attn_tc_launch(pre, cut.plan, d->sms, s);
+    }
+    if (e == cudaSuccess) e = attn_keys_launch(a, sp, s);
+  } else {
+    e = cut.tc ? attn_tc_launch(a, cut.plan, d->sms, s) : attn_decode_simt_launch(a, cut.n_own, dtype, s);
+    if (e == cudaSuccess && a.n_part > 1) e = attn_join_launch(a, dtype, s);
+  }
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "decode_attention launch");
 }
 

@@ -1,0 +1,592 @@
+// One token per request against its own pages (bf16, up to eight query heads a group): the
+// keys are the rows of the tensor-core tiles.
+//
+// Bound by HBM: every key and value row of a request is read once for the R heads of its
+// group, and there are only R query rows to multiply it with. So the products are transposed,
+// with the tile of 128 keys as the 128 rows of the MMA and the heads as its columns (N = 16,
+// the fewest; columns past R hold anything and are never read):
+//   S^T = K Q^T    8 tcgen05.mma (M = 128 keys, N = 16, K = 16), a thread per key then has R
+//                  scores to weigh, instead of one thread 128;
+//   P^T            2^(s - m) in fp32, summed per thread and head, to bf16 in shared memory
+//                  [head][key] (the second product's only 16-bit operand type);
+//   O^T += V^T P^T 8 tcgen05.mma (M = 128 elements, N = 16, K = 16 keys), V as it lies.
+// No maximum is looked for while no value of P passes 2^10 (a vote of the tile's threads);
+// at a unit's first tile and past that it is found and P formed again.
+//
+// Work. The tiles of all (request, key/value head) units lie end to end; CTA c of G takes
+// tiles [c T / G, (c + 1) T / G), whatever the requests' lengths, so all CTAs end together. A
+// unit inside one CTA's span is finished by it; one that a span's border cuts is written in
+// pieces, at most two a CTA, which a second kernel joins. Two CTAs an SM, each with a ring
+// of three 32 KiB stages that TMA fills across units.
+// Roles: warps 0-3 softmax (thread = key, then element), warp 4 MMAs, warp 5 TMA.
+// Every wait is bounded; a timeout sets the device error word and the roles drain.
+#include "attention_tc.cuh"
+
+namespace provip {
+namespace {
+
+constexpr int kHeads = 8;      // query heads of a group, at most
+constexpr int kCols = 16;      // columns of the MMAs
+constexpr int kStages = 3;
+constexpr int kQBytes = 2 * kHeads * 128;  // a unit's queries: two halves of 64 elements
+constexpr int kPBytes = 2 * kHeads * 128;  // a tile's P^T: two halves of 64 keys
+// an MMA reads 16 rows of an operand of 8: 1 KiB past it, which the layout keeps inside
+constexpr size_t kSmem = (size_t)kStages * kStage + 2 * kQBytes + 2 * kPBytes + 1024 + 1024;
+constexpr int kThr = 192;
+constexpr uint32_t kTmemCols = 64;  // S twice, O
+constexpr float kMostP = 1024.f;
+constexpr uint32_t kIdescS = idesc_bf16_f32(kT, kCols);
+constexpr uint32_t kIdescO = idesc_bf16_f32(kT, kCols) | (1u << 15);  // A's (V's) rows run along M
+constexpr int kBoard = 4;
+
+// a unit's tiles in this CTA's span
+struct Piece {
+  int b, g;          // request, key/value head (-1: none is left)
+  int t_lo, nt;      // tiles of the unit
+  int n_keys;        // keys from the first tile on
+  bool whole;        // every tile of the unit
+  uint32_t tile0;    // number of its first tile in the CTA
+};
+
+struct Ctl {
+  Piece board[kBoard];
+  uint64_t u_full[kBoard], u_empty[kBoard];
+  uint64_t q_full[2], q_empty[2];
+  uint64_t kv_full[kStages], kv_empty[kStages];
+  uint64_t s_full[2], p_full[2], o_done;
+  float red[4][kHeads];
+  uint32_t tmem;
+  volatile int fail;
+};
+
+__device__ __forceinline__ int unit_tiles(int k_len) { return max((k_len + kT - 1) / kT, 1); }
+__device__ __forceinline__ int checked_len(const AttnArgs& a, int b) {
+  const int n = a.k_len[b];
+  return n >= 0 && n <= a.k_len_max && n <= (long long)a.max_pages * a.page_size ? n : -1;
+}
+
+__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool soft_any(bool v) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, 1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)v)
+      : "memory");
+  return any != 0;
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+               "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+               "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
+}
+
+// the warp's sum of the requests' tiles before each of 32 requests, and of all 32
+__device__ __forceinline__ int tiles_before(int t, int lane, int& all) {
+  int s = t;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += u;
+  }
+  all = __shfl_sync(0xffffffffu, s, 31);
+  return s - t;
+}
+
+template <int R>
+__global__ void __launch_bounds__(kThr, 2)
+    attn_keys_tc(int G, const __grid_constant__ AttnArgs a, const __grid_constant__ AttnSpans sp,
+                 const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                 const __grid_constant__ CUtensorMap map_v) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Ctl ctl;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem_raw);
+  uint8_t* kv = smem_raw + (((base + 1023u) & ~1023u) - base);
+  uint8_t* ps = kv + kStages * kStage;
+  uint8_t* qs = ps + 2 * kPBytes;
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&map_q);
+    prefetch_tmap(&map_k);
+    prefetch_tmap(&map_v);
+    for (int n = 0; n < kBoard; ++n) {
+      mbar_init(&ctl.u_full[n], 1);
+      mbar_init(&ctl.u_empty[n], 5);
+    }
+    for (int n = 0; n < 2; ++n) {
+      mbar_init(&ctl.q_full[n], 1);
+      mbar_init(&ctl.q_empty[n], 1);
+      mbar_init(&ctl.s_full[n], 1);
+      mbar_init(&ctl.p_full[n], 4);
+    }
+    mbar_init(&ctl.o_done, 1);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&ctl.kv_full[s], 1);
+      mbar_init(&ctl.kv_empty[s], 1);
+    }
+    ctl.fail = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(&ctl.tmem, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_allow_next();  // the joining kernel, which holds no tensor memory, may be scheduled
+  const uint32_t tmem = ctl.tmem;
+
+  if (warp == 4) {
+    // ---- MMA issuer: the products of tile n + 1 with Q before those of tile n with V ----
+    const bool lead = elect_one();
+    const uint64_t kd0 = smem_desc_sw128(smem_u32(kv)), vd0 = smem_desc_mn_sw128(smem_u32(kv));
+    const uint64_t qd0 = smem_desc_sw128(smem_u32(qs)), pd0 = smem_desc_sw128(smem_u32(ps));
+    uint32_t n = 0;  // tiles done
+    bool live = true;
+    // S^T of tile n from unit buffer qb
+    auto scores = [&](uint32_t t, uint32_t qb) {
+      const uint32_t ld = 2 * t, st = ld % kStages;
+      live = live && warp_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
+      tc_fence_after();
+      if (lead) {
+        const uint64_t kd = kd0 + (uint64_t)(st * (kStage >> 4)), qd = qd0 + (uint64_t)(qb * (kQBytes >> 4));
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          tc_mma_bf16(tmem + (t & 1) * kCols, kd + (uint64_t)(((ks >> 2) * kHalf + (ks & 3) * 32) >> 4),
+                      qd + (uint64_t)(((ks >> 2) * (kQBytes / 2) + (ks & 3) * 32) >> 4), kIdescS, ks > 0 ? 1u : 0u);
+        tc_commit(&ctl.s_full[t & 1]);
+        tc_commit(&ctl.kv_empty[st]);
+      }
+    };
+    auto values = [&](uint32_t t, bool first) {
+      const uint32_t ld = 2 * t + 1, st = ld % kStages;
+      live = live && warp_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
+      live = live && warp_wait(&ctl.p_full[t & 1], (t >> 1) & 1u, a.err);
+      tc_fence_after();
+      if (lead) {
+        const uint64_t vd = vd0 + (uint64_t)(st * (kStage >> 4)), pd = pd0 + (uint64_t)((t & 1) * (kPBytes >> 4));
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          tc_mma_bf16(tmem + 2 * kCols, vd + (uint64_t)(ks * 2048 >> 4),
+                      pd + (uint64_t)(((ks >> 2) * (kPBytes / 2) + (ks & 3) * 32) >> 4), kIdescO,
+                      first && ks == 0 ? 0u : 1u);
+        tc_commit(&ctl.kv_empty[st]);
+        tc_commit(&ctl.o_done);
+      }
+    };
+    for (uint32_t u = 0; live; ++u) {
+      live = warp_wait(&ctl.u_full[u % kBoard], (u / kBoard) & 1u, a.err);
+      const Piece& x = ctl.board[u % kBoard];
+      if (!live || x.g < 0) break;
+      const int nt = x.nt;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
+      live = warp_wait(&ctl.q_full[u & 1], (u >> 1) & 1u, a.err);
+      for (int j = 0; live && j <= nt; ++j) {
+        if (j < nt) {
+          scores(n + j, u & 1);
+          if (j == nt - 1 && lead) tc_commit(&ctl.q_empty[u & 1]);
+        }
+        if (j > 0) values(n + j - 1, j == 1);
+      }
+      n += nt;
+    }
+    if (!live) ctl.fail = 1;
+  } else if (warp == 5) {
+    // ---- producer: the CTA's span, cut into pieces, and their loads ----
+    const int box = min(a.page_size, kT);
+    bool live = true;
+    uint32_t n_ld = 0, u = 0, tile0 = 0;
+    // all tiles, and tiles before this CTA's span
+    long long T = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      int t = 0, all;
+      if (b0 + lane < a.B) {
+        const int k = checked_len(a, b0 + lane);
+        if (k < 0 && blockIdx.x == 0) set_error(a.err, kErrBadDeviceArg);
+        t = unit_tiles(k);
+      }
+      const int before = tiles_before(t, lane, all);
+      if (blockIdx.x == 0 && b0 + lane < a.B) sp.before[b0 + lane] = T + before;
+      T += all;
+    }
+    if (blockIdx.x == 0 && lane == 0) sp.before[a.B] = T;
+    T *= a.H_kv;
+    long long f = T * blockIdx.x / G;
+    const long long f_end = T * (blockIdx.x + 1) / G;
+    // the request that holds tile f: its tiles, and those before it
+    int b = 0, k_len = 0, nt_b = 1;
+    long long f_b = 0;
+    if (f < f_end) {
+      long long done = 0;
+      for (int b0 = 0; b0 < a.B; b0 += 32) {
+        int k = 0, t = 0, all;
+        if (b0 + lane < a.B) {
+          k = max(checked_len(a, b0 + lane), 0);
+          t = unit_tiles(k);
+        }
+        const int before = tiles_before(t, lane, all);
+        if ((done + all) * a.H_kv > f) {
+          const unsigned in = __ballot_sync(0xffffffffu, t > 0 && (done + before) * a.H_kv <= f);
+          const int src = 31 - __clz(in);
+          b = b0 + src;
+          k_len = __shfl_sync(0xffffffffu, k, src);
+          nt_b = __shfl_sync(0xffffffffu, t, src);
+          f_b = (done + __shfl_sync(0xffffffffu, before, src)) * a.H_kv;
+          break;
+        }
+        done += all;
+      }
+    }
+    // one tile, K or V, into the next stage
+    auto load = [&](const Piece& x, int j, bool v) {
+      const uint32_t st = n_ld % kStages, ph = (n_ld / kStages) & 1u;
+      ++n_ld;
+      const int n = min(kT, x.n_keys - j * kT), boxes = n > 0 ? (n + box - 1) / box : 0;
+      bool ok = true;
+      if (lane == 0) {
+        ok = !ctl.fail && mbar_wait(&ctl.kv_empty[st], ph ^ 1u, a.err);
+        if (ok) mbar_arrive_expect_tx(&ctl.kv_full[st], (uint32_t)(boxes * box * 256));
+      }
+      __syncwarp();
+      if (!__shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) return false;
+      uint8_t* dst = kv + st * kStage;
+      const CUtensorMap* map = v ? &map_v : &map_k;
+      if (lane < boxes) {
+        const int row = (int)attn_slot(a, a.block_table + (size_t)x.b * a.max_pages, (x.t_lo + j) * kT + lane * box);
+        tma_load_2d(dst + lane * box * 128, map, x.g * kHeadDim, row, &ctl.kv_full[st]);
+        tma_load_2d(dst + kHalf + lane * box * 128, map, x.g * kHeadDim + 64, row, &ctl.kv_full[st]);
+      }
+      __syncwarp();
+      return true;
+    };
+    for (; live; ++u) {
+      Piece x;
+      x.g = -1;
+      if (f < f_end) {
+        const int in = (int)(f - f_b);
+        x.b = b;
+        x.g = in / nt_b;
+        x.t_lo = in % nt_b;
+        x.nt = (int)min((long long)(nt_b - x.t_lo), f_end - f);
+        x.n_keys = k_len - x.t_lo * kT;
+        x.whole = x.nt == nt_b;
+        x.tile0 = tile0;
+        tile0 += x.nt;
+        f += x.nt;
+        if (f - f_b == (long long)nt_b * a.H_kv && f < f_end) {
+          // the next request (never past the last: f < f_end <= T)
+          f_b = f;
+          ++b;
+          k_len = max(checked_len(a, b), 0);
+          nt_b = unit_tiles(k_len);
+        }
+      }
+      live = warp_wait(&ctl.u_empty[u % kBoard], ((u / kBoard) & 1u) ^ 1u, a.err);
+      if (!live) break;
+      if (lane == 0) {
+        ctl.board[u % kBoard] = x;
+        mbar_arrive(&ctl.u_full[u % kBoard]);
+      }
+      __syncwarp();
+      if (x.g < 0) break;
+      live = load(x, 0, false);
+      if (!live) break;
+      bool ok = true;
+      if (lane == 0) {
+        ok = mbar_wait(&ctl.q_empty[u & 1], ((u >> 1) & 1u) ^ 1u, a.err);
+        if (ok) {
+          mbar_arrive_expect_tx(&ctl.q_full[u & 1], R * 256);
+          uint8_t* q = qs + (u & 1) * kQBytes;
+          tma_load_3d(q, &map_q, 0, x.g * R, x.b, &ctl.q_full[u & 1]);
+          tma_load_3d(q + kQBytes / 2, &map_q, 64, x.g * R, x.b, &ctl.q_full[u & 1]);
+        }
+      }
+      __syncwarp();
+      live = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+      for (int j = 0; live && j < x.nt; ++j) {
+        live = load(x, j, true);
+        if (live && j + 1 < x.nt) live = load(x, j + 1, false);
+      }
+    }
+    if (!live) ctl.fail = 1;
+  } else {
+    // ---- softmax: a thread per key; in the epilogue a thread per element ----
+    const int r = threadIdx.x;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const uint32_t to = tmem + 2 * kCols + lanes;
+    const float sc = a.scale_log2;
+    // this key's place in a row of P^T: 16-byte chunks swizzled by the row
+    const uint32_t p_half = (uint32_t)(r >> 6) * (kPBytes / 2), p_chunk = (uint32_t)(r >> 3) & 7u, p_in = (uint32_t)(r & 7) * 2;
+    // a wait that gave up: no more waits in the unit, but every barrier of the four warps is
+    // met, and all of them leave before the next one
+    bool failed = false;
+    for (uint32_t u = 0;; ++u) {
+      if (!failed) failed = !mbar_wait(&ctl.u_full[u % kBoard], (u / kBoard) & 1u, a.err);
+      failed = soft_any(failed);
+      const Piece& x = ctl.board[u % kBoard];
+      if (failed || x.g < 0) break;
+      const int nt = x.nt;
+      float m[R], l[R];
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        m[h] = -INFINITY;
+        l[h] = 0.f;
+      }
+      for (int j = 0; j < nt; ++j) {
+        const uint32_t n = x.tile0 + j, buf = n & 1;
+        const bool key = r < x.n_keys - j * kT;
+        if (!failed) failed = !mbar_wait(&ctl.s_full[buf], (n >> 1) & 1u, a.err);
+        __syncwarp();
+        tc_fence_after();
+        if (x.n_keys - j * kT < kT) {
+          // value rows past the end: zero before the product reads them
+          const uint32_t ld = 2 * n + 1, st = ld % kStages;
+          if (!failed) failed = !mbar_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
+          if (!key) {
+            uint8_t* vs = kv + st * kStage + r * 128;
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+              *reinterpret_cast<uint4*>(vs + (q >> 3) * kHalf + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          __syncwarp();
+        }
+        float s[8], p[R];
+        tmem_ld8(tmem + buf * kCols + lanes, s);
+        tc_wait_ld();
+#pragma unroll
+        for (int h = 0; h < R; ++h) s[h] = key ? s[h] * sc : -INFINITY;
+        bool raise = j == 0;
+        for (;;) {
+          if (raise) {
+            // each head's largest score of the tile, over its 128 threads
+#pragma unroll
+            for (int h = 0; h < R; ++h) {
+              const float w = warp_max(s[h]);
+              if (lane == 0) ctl.red[warp][h] = w;
+            }
+            soft_sync();
+            float f[8];
+            bool any = false;
+#pragma unroll
+            for (int h = 0; h < R; ++h) {
+              const float mx = fmaxf(fmaxf(ctl.red[0][h], ctl.red[1][h]), fmaxf(ctl.red[2][h], ctl.red[3][h]));
+              const float mn = fmaxf(m[h], ceilf(mx));
+              f[h] = m[h] == mn ? 1.f : ex2_int(m[h] - mn);
+              any = any || f[h] != 1.f;
+              m[h] = mn;
+              l[h] *= f[h];
+            }
+#pragma unroll
+            for (int h = R; h < 8; ++h) f[h] = 1.f;
+            if (j > 0 && any) {
+              // O^T times f, once the product before is complete (the next waits for this P)
+              if (!failed) failed = !mbar_wait(&ctl.o_done, (n - 1) & 1u, a.err);
+              __syncwarp();
+              tc_fence_after();
+              float o[8];
+              tmem_ld8(to, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int h = 0; h < 8; ++h) o[h] *= f[h];
+              tmem_st8(to, o);
+              tc_wait_st();
+            }
+          }
+          bool far = false;
+#pragma unroll
+          for (int h = 0; h < R; ++h) {
+            p[h] = ex2_approx(s[h] - (m[h] == -INFINITY ? 0.f : m[h]));
+            far = far || p[h] > kMostP;
+          }
+          // against the tile's own maximum no value passes 1, so this ends
+          raise = soft_any(far);
+          if (!raise) break;
+        }
+        uint8_t* pb = ps + buf * kPBytes + p_half + p_in;
+#pragma unroll
+        for (int h = 0; h < R; ++h) {
+          l[h] += p[h];
+          *reinterpret_cast<__nv_bfloat16*>(pb + h * 128 + ((p_chunk ^ (uint32_t)h) & 7u) * 16) = __float2bfloat16_rn(p[h]);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.p_full[buf]);
+      }
+      // ---- epilogue: O^T / l, element r of every head ----
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        const float w = warp_sum(l[h]);
+        if (lane == 0) ctl.red[warp][h] = w;
+      }
+      if (!failed) failed = !mbar_wait(&ctl.o_done, (x.tile0 + nt - 1) & 1u, a.err);
+      __syncwarp();
+      tc_fence_after();
+      soft_sync();
+      float o[8];
+      tmem_ld8(to, o);
+      tc_wait_ld();
+      tc_fence_before();  // O^T is read before the next unit's first product, which waits for p_full
+      const size_t row0 = (size_t)x.b * a.H_q + x.g * R;
+      const bool last = x.whole && a.prefix_len == 0;
+      const size_t slot = x.whole ? 0 : 2 * (size_t)blockIdx.x + (x.t_lo == 0 ? 1 : 0);
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        const float t = (ctl.red[0][h] + ctl.red[1][h]) + (ctl.red[2][h] + ctl.red[3][h]);
+        float val = t == 0.f ? 0.f : o[h] / t, lse = t == 0.f ? -INFINITY : m[h] + lg2_approx(t);
+        if (last) {
+          if (t == 0.f && x.n_keys > 0) val = lse = NAN;  // every score is -inf: 0 / 0, as the formula has it
+          __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim;
+          op[r] = __float2bfloat16_rn(val);
+          if (r == 0 && a.lse) a.lse[row0 + h] = lse * kLn2;
+        } else {
+          float* po = x.whole ? sp.whole_o + (row0 + h) * kHeadDim : sp.piece_o + (slot * R + h) * kHeadDim;
+          po[r] = val;
+          if (r == 0) (x.whole ? sp.whole_lse[row0 + h] : sp.piece_lse[slot * R + h]) = lse;
+        }
+      }
+      soft_sync();  // red is free again
+      if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
+    }
+    if (failed) ctl.fail = 1;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, kTmemCols);
+}
+
+// ---------------------------------------------------------------------------
+// pieces and prefix parts -> rows: a warp per row
+// ---------------------------------------------------------------------------
+struct Sum {
+  float m = -INFINITY, w = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float lse, const float* po, int lane) {
+    const float mn = fmaxf(m, lse), base = mn == -INFINITY ? 0.f : mn;
+    const float c = exp2f(m - base), p = exp2f(lse - base);
+    const float4 v = *reinterpret_cast<const float4*>(po + lane * 4);
+    w = w * c + p;
+    o[0] = o[0] * c + (p == 0.f ? 0.f : p * v.x);
+    o[1] = o[1] * c + (p == 0.f ? 0.f : p * v.y);
+    o[2] = o[2] * c + (p == 0.f ? 0.f : p * v.z);
+    o[3] = o[3] * c + (p == 0.f ? 0.f : p * v.w);
+    m = mn;
+  }
+};
+
+// with a prefix: a warp per (request, head); without: per border of two spans and head, for
+// the unit that the border is the first to cut
+__global__ void __launch_bounds__(256) attn_join_spans(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnSpans sp,
+                                                       int G) {
+  pdl_wait_prior();
+  const int lane = threadIdx.x & 31, R = a.H_q / a.H_kv;
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long T = sp.before[a.B] * a.H_kv;
+  int b, g, h;
+  long long F;  // the unit's first tile
+  int nt;
+  if (a.prefix_len > 0) {
+    if (w >= (long long)a.B * a.H_q) return;
+    b = (int)(w / a.H_q);
+    h = (int)(w % a.H_q);
+    g = h / R;
+    nt = (int)(sp.before[b + 1] - sp.before[b]);
+    F = sp.before[b] * a.H_kv + (long long)g * nt;
+  } else {
+    const long long c = 1 + w / R;
+    if (c >= G) return;
+    const long long f = T * c / G;
+    if (f >= T) return;
+    int lo = 0, hi = a.B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sp.before[mid] * a.H_kv <= f) lo = mid; else hi = mid - 1;
+    }
+    b = lo;
+    nt = (int)(sp.before[b + 1] - sp.before[b]);
+    g = (int)((f - sp.before[b] * a.H_kv) / nt);
+    F = sp.before[b] * a.H_kv + (long long)g * nt;
+    if (f == F || T * (c - 1) / G > F) return;
+    h = g * R + (int)(w % R);
+  }
+  Sum s;
+  const long long n_rows = (long long)a.T_q * a.H_q, row = (long long)b * a.H_q + h;
+  for (int p = 0; p < sp.n_prefix; ++p) s.add(a.part_lse[p * n_rows + row], a.part_o + (p * n_rows + row) * kHeadDim, lane);
+  // the span that holds tile f is the last one that starts at or before it
+  const long long c0 = ((F + 1) * G - 1) / T, c1 = ((F + nt) * G - 1) / T;
+  if (c0 == c1) {
+    s.add(sp.whole_lse[row], sp.whole_o + row * kHeadDim, lane);
+  } else {
+    for (long long c = c0; c <= c1; ++c) {
+      if (c > c0 && T * c / G == T * (c + 1) / G) continue;  // an empty span
+      const long long slot = (2 * c + (c == c0 ? 1 : 0)) * R + (h - g * R);
+      s.add(sp.piece_lse[slot], sp.piece_o + slot * kHeadDim, lane);
+    }
+  }
+  const int n_keys = a.prefix_len + max(checked_len(a, b), 0);
+  const float den = s.w == 0.f ? (n_keys > 0 ? NAN : 1.f) : s.w;  // every score -inf: 0 / 0, as the formula has it
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s.o[e] /= den;
+  store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)b * a.o_stride + (size_t)h * kHeadDim + lane * 4, s.o);
+  if (lane == 0 && a.lse) a.lse[row] = s.w == 0.f ? (n_keys > 0 ? NAN : -INFINITY) : (s.m + log2f(s.w)) * kLn2;
+}
+
+template <int R>
+cudaError_t launch(const AttnArgs& a, const AttnSpans& sp, const CUtensorMap& q, const CUtensorMap& k,
+                   const CUtensorMap& v, cudaStream_t s) {
+  static std::atomic<bool> configured[64];  // per device, zero-initialised
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    cudaError_t e = cudaFuncSetAttribute(attn_keys_tc<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (e != cudaSuccess) return e;
+    configured[dev] = true;
+  }
+  attn_keys_tc<R><<<sp.n_spans, kThr, kSmem, s>>>(sp.n_spans, a, sp, q, k, v);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t attn_keys_launch(const AttnArgs& a, const AttnSpans& sp, cudaStream_t s) {
+  CUtensorMap q, k, v;
+  const int R = a.H_q / a.H_kv;
+  const uint32_t box = (uint32_t)(a.page_size < kT ? a.page_size : kT);
+  const uint64_t rows = (uint64_t)a.n_pages * a.page_size;
+  if (make_tmap_bf16_heads(&q, a.Q, (uint64_t)a.T_q, (uint64_t)a.H_q, (uint64_t)a.q_stride * 2, (uint32_t)R, 1) ||
+      make_tmap_bf16_2d(&k, a.K, rows, (uint64_t)a.H_kv * kHeadDim, (uint64_t)a.k_stride * 2, box) ||
+      make_tmap_bf16_2d(&v, a.V, rows, (uint64_t)a.H_kv * kHeadDim, (uint64_t)a.v_stride * 2, box))
+    return cudaErrorInvalidValue;
+  cudaError_t e;
+  switch (R) {
+    case 1: e = launch<1>(a, sp, q, k, v, s); break;
+    case 2: e = launch<2>(a, sp, q, k, v, s); break;
+    case 3: e = launch<3>(a, sp, q, k, v, s); break;
+    case 4: e = launch<4>(a, sp, q, k, v, s); break;
+    case 5: e = launch<5>(a, sp, q, k, v, s); break;
+    case 6: e = launch<6>(a, sp, q, k, v, s); break;
+    case 7: e = launch<7>(a, sp, q, k, v, s); break;
+    case 8: e = launch<8>(a, sp, q, k, v, s); break;
+    default: return cudaErrorInvalidValue;
+  }
+  if (e != cudaSuccess) return e;
+  const long long warps = a.prefix_len > 0 ? (long long)a.B * a.H_q : (long long)(sp.n_spans - 1) * R;
+  if (warps == 0) return cudaSuccess;
+  return launch_pdl(attn_join_spans, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a, sp, sp.n_spans);
+}
+
+}  // namespace provip

@@ -329,6 +329,18 @@ struct AttnPlan {
   int n_prefix_units;        // paged: units of the prefix, which come first
 };
 cudaError_t attn_tc_launch(const AttnArgs& a, const AttnPlan& plan, int sms, cudaStream_t s);
+// One token per request, at most eight heads a group: the tiles of the requests' own keys
+// shared out over n_spans CTAs. Of a unit (request, key/value head) that one CTA finishes, the
+// result goes to out (no prefix) or whole_*[B H_q rows]; of one that is cut, CTA c writes
+// slot 2 c (the unit began before its span) or 2 c + 1 of piece_*[2 n_spans][H_q / H_kv].
+struct AttnSpans {
+  int n_spans;
+  int n_prefix;              // parts of the prefix, in part_* of AttnArgs
+  long long* before;         // [B + 1] 128-key tiles of the requests before each
+  float *whole_o, *whole_lse, *piece_o, *piece_lse;
+};
+constexpr int kSpanHeads = 8;
+cudaError_t attn_keys_launch(const AttnArgs& a, const AttnSpans& sp, cudaStream_t s);
 // joins n_part parts of every row into out and lse
 cudaError_t attn_join_launch(const AttnArgs& a, int dtype, cudaStream_t s);
 
