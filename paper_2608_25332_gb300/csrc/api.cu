@@ -1287,6 +1287,7 @@ size_t decode_ws(Carve& c, const AttnCut& cut, int B, int H_q, int H_kv, float**
   sp->n_spans = cut.n_spans;
   sp->n_prefix = cut.n_prefix;
   sp->before = c.take<long long>((size_t)B + 1);
+  sp->cut = c.take<int2>(cut.n_spans);
   sp->piece_o = c.take<float>(pieces * kHeadDim);
   sp->piece_lse = c.take<float>(pieces);
   if (cut.n_prefix > 0) {

@@ -53,7 +53,8 @@ struct Ctl {
   uint64_t u_full[kBoard], u_empty[kBoard];
   uint64_t q_full[2], q_empty[2];
   uint64_t kv_full[kStages], kv_empty[kStages];
-  uint64_t s_full[2], p_full[2], o_done;
+  uint64_t s_full[2], p_full[2];
+  uint64_t o_done[2];  // by the tile's parity: scores of tile n are issued past the product of n - 2, not of n - 1
   float red[4][kHeads];
   uint32_t tmem;
   volatile int fail;
@@ -131,8 +132,8 @@ __global__ void __launch_bounds__(kThr, 2)
       mbar_init(&ctl.q_empty[n], 1);
       mbar_init(&ctl.s_full[n], 1);
       mbar_init(&ctl.p_full[n], 4);
+      mbar_init(&ctl.o_done[n], 1);
     }
-    mbar_init(&ctl.o_done, 1);
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&ctl.kv_full[s], 1);
       mbar_init(&ctl.kv_empty[s], 1);
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(kThr, 2)
                       pd + (uint64_t)(((ks >> 2) * (kPBytes / 2) + (ks & 3) * 32) >> 4), kIdescO,
                       first && ks == 0 ? 0u : 1u);
         tc_commit(&ctl.kv_empty[st]);
-        tc_commit(&ctl.o_done);
+        tc_commit(&ctl.o_done[t & 1]);
       }
     };
     for (uint32_t u = 0; live; ++u) {
@@ -211,17 +212,33 @@ __global__ void __launch_bounds__(kThr, 2)
     const int box = min(a.page_size, kT);
     bool live = true;
     uint32_t n_ld = 0, u = 0, tile0 = 0;
-    // all tiles, and tiles before this CTA's span
+    // lengths of 256 requests in the lanes' registers (beyond, they are read twice)
+    constexpr int kHeld = 8;
+    int held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0;
+    auto len_of = [&](int i) { return i < kHeld ? held[i] : i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0; };
+    // all tiles, and the tiles of the requests before each
     long long T = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-      int t = 0, all;
-      if (b0 + lane < a.B) {
-        const int k = checked_len(a, b0 + lane);
-        if (k < 0 && blockIdx.x == 0) set_error(a.err, kErrBadDeviceArg);
-        t = unit_tiles(k);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      if (i * 32 >= a.B) break;
+      int all;
+      const int t = i * 32 + lane < a.B ? unit_tiles(held[i]) : 0, before = tiles_before(t, lane, all);
+      if (blockIdx.x == 0 && i * 32 + lane < a.B) {
+        sp.before[i * 32 + lane] = T + before;
+        if (held[i] < 0) set_error(a.err, kErrBadDeviceArg);
       }
-      const int before = tiles_before(t, lane, all);
-      if (blockIdx.x == 0 && b0 + lane < a.B) sp.before[b0 + lane] = T + before;
+      T += all;
+    }
+    for (int i = kHeld; i * 32 < a.B; ++i) {
+      const int k = len_of(i);
+      int all;
+      const int t = i * 32 + lane < a.B ? unit_tiles(k) : 0, before = tiles_before(t, lane, all);
+      if (blockIdx.x == 0 && i * 32 + lane < a.B) {
+        sp.before[i * 32 + lane] = T + before;
+        if (k < 0) set_error(a.err, kErrBadDeviceArg);
+      }
       T += all;
     }
     if (blockIdx.x == 0 && lane == 0) sp.before[a.B] = T;
@@ -233,24 +250,42 @@ __global__ void __launch_bounds__(kThr, 2)
     long long f_b = 0;
     if (f < f_end) {
       long long done = 0;
-      for (int b0 = 0; b0 < a.B; b0 += 32) {
-        int k = 0, t = 0, all;
-        if (b0 + lane < a.B) {
-          k = max(checked_len(a, b0 + lane), 0);
-          t = unit_tiles(k);
-        }
-        const int before = tiles_before(t, lane, all);
-        if ((done + all) * a.H_kv > f) {
-          const unsigned in = __ballot_sync(0xffffffffu, t > 0 && (done + before) * a.H_kv <= f);
-          const int src = 31 - __clz(in);
-          b = b0 + src;
-          k_len = __shfl_sync(0xffffffffu, k, src);
+      auto look = [&](int i, int k) {
+        int all;
+        const int t = i * 32 + lane < a.B ? unit_tiles(k) : 0, before = tiles_before(t, lane, all);
+        const bool here = (done + all) * a.H_kv > f;
+        if (here) {
+          const int src = 31 - __clz(__ballot_sync(0xffffffffu, t > 0 && (done + before) * a.H_kv <= f));
+          b = i * 32 + src;
+          k_len = max(__shfl_sync(0xffffffffu, k, src), 0);
           nt_b = __shfl_sync(0xffffffffu, t, src);
           f_b = (done + __shfl_sync(0xffffffffu, before, src)) * a.H_kv;
-          break;
         }
         done += all;
+        return here;
+      };
+      bool here = false;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (!here && i * 32 < a.B) here = look(i, held[i]);
+      for (int i = kHeld; !here && i * 32 < a.B; ++i) here = look(i, len_of(i));
+    }
+    // what a border cuts: the first border inside a unit tells the joining kernel
+    if (lane == 0) {
+      int unit = -1;
+      long long last = -1;  // a span without tiles
+      if (f < f_end) {
+        last = 0;
+        const int in = (int)(f - f_b);
+        const long long F = f_b + in / nt_b * nt_b;
+        // no other span starts inside the unit before this one: the tile before it lies in a
+        // span that starts at or before the unit
+        if (f > F && T * ((f * G - 1) / T) / G <= F) {
+          unit = b * a.H_kv + in / nt_b;
+          last = ((F + nt_b) * G - 1) / T;  // the span that holds the unit's last tile
+        }
       }
+      sp.cut[blockIdx.x] = make_int2(unit, (int)last);
     }
     // one tile, K or V, into the next stage
     auto load = [&](const Piece& x, int j, bool v) {
@@ -395,7 +430,7 @@ __global__ void __launch_bounds__(kThr, 2)
             for (int h = R; h < 8; ++h) f[h] = 1.f;
             if (j > 0 && any) {
               // O^T times f, once the product before is complete (the next waits for this P)
-              if (!failed) failed = !mbar_wait(&ctl.o_done, (n - 1) & 1u, a.err);
+              if (!failed) failed = !mbar_wait(&ctl.o_done[buf ^ 1], ((n - 1) >> 1) & 1u, a.err);
               __syncwarp();
               tc_fence_after();
               float o[8];
@@ -434,7 +469,8 @@ __global__ void __launch_bounds__(kThr, 2)
         const float w = warp_sum(l[h]);
         if (lane == 0) ctl.red[warp][h] = w;
       }
-      if (!failed) failed = !mbar_wait(&ctl.o_done, (x.tile0 + nt - 1) & 1u, a.err);
+      const uint32_t last_n = x.tile0 + nt - 1;
+      if (!failed) failed = !mbar_wait(&ctl.o_done[last_n & 1], (last_n >> 1) & 1u, a.err);
       __syncwarp();
       tc_fence_after();
       soft_sync();
@@ -473,75 +509,88 @@ __global__ void __launch_bounds__(kThr, 2)
 // ---------------------------------------------------------------------------
 // pieces and prefix parts -> rows: a warp per row
 // ---------------------------------------------------------------------------
-struct Sum {
-  float m = -INFINITY, w = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  __device__ __forceinline__ void add(float lse, const float* po, int lane) {
-    const float mn = fmaxf(m, lse), base = mn == -INFINITY ? 0.f : mn;
-    const float c = exp2f(m - base), p = exp2f(lse - base);
-    const float4 v = *reinterpret_cast<const float4*>(po + lane * 4);
-    w = w * c + p;
-    o[0] = o[0] * c + (p == 0.f ? 0.f : p * v.x);
-    o[1] = o[1] * c + (p == 0.f ? 0.f : p * v.y);
-    o[2] = o[2] * c + (p == 0.f ? 0.f : p * v.z);
-    o[3] = o[3] * c + (p == 0.f ? 0.f : p * v.w);
-    m = mn;
-  }
+// Weighs and adds n parts of a row: lse(p) and the 512 bytes at part(p). The weights first, a
+// part per lane, so that the parts' loads do not wait for one another.
+struct Joined {
+  float o[4], w, m;
 };
+template <typename Lse, typename Part>
+__device__ __forceinline__ Joined join_parts(int n, Lse lse, Part part) {
+  const int lane = threadIdx.x & 31;
+  Joined s = {{0.f, 0.f, 0.f, 0.f}, 0.f, -INFINITY};
+  for (int p0 = 0; p0 < n; p0 += 32) {
+    const float x = p0 + lane < n ? lse(p0 + lane) : -INFINITY;
+    const float mn = fmaxf(s.m, warp_max(x)), base = mn == -INFINITY ? 0.f : mn;
+    const float c = exp2f(s.m - base), mine = p0 + lane < n ? exp2f(x - base) : 0.f;
+    s.m = mn;
+    s.w = s.w * c + warp_sum(mine);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s.o[e] *= c;
+#pragma unroll 8
+    for (int p = 0; p < min(n - p0, 32); ++p) {
+      const float w = __shfl_sync(0xffffffffu, mine, p);
+      const float4 v = *reinterpret_cast<const float4*>(part(p0 + p) + lane * 4);
+      if (w != 0.f) {
+        s.o[0] = fmaf(w, v.x, s.o[0]);
+        s.o[1] = fmaf(w, v.y, s.o[1]);
+        s.o[2] = fmaf(w, v.z, s.o[2]);
+        s.o[3] = fmaf(w, v.w, s.o[3]);
+      }
+    }
+  }
+  return s;
+}
 
 // with a prefix: a warp per (request, head); without: per border of two spans and head, for
 // the unit that the border is the first to cut
-__global__ void __launch_bounds__(256) attn_join_spans(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnSpans sp,
-                                                       int G) {
+__global__ void __launch_bounds__(256) attn_join_spans(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnSpans sp) {
   pdl_wait_prior();
-  const int lane = threadIdx.x & 31, R = a.H_q / a.H_kv;
+  const int lane = threadIdx.x & 31, R = a.H_q / a.H_kv, G = sp.n_spans;
   const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const long long T = sp.before[a.B] * a.H_kv;
-  int b, g, h;
-  long long F;  // the unit's first tile
-  int nt;
+  long long row, c0, c1;  // the spans that hold the unit's first and last tile
+  int hd;
   if (a.prefix_len > 0) {
     if (w >= (long long)a.B * a.H_q) return;
-    b = (int)(w / a.H_q);
-    h = (int)(w % a.H_q);
-    g = h / R;
-    nt = (int)(sp.before[b + 1] - sp.before[b]);
-    F = sp.before[b] * a.H_kv + (long long)g * nt;
+    row = w;
+    const int b = (int)(w / a.H_q), h = (int)(w % a.H_q);
+    hd = h % R;
+    const long long T = sp.before[a.B] * a.H_kv, nt = sp.before[b + 1] - sp.before[b];
+    const long long F = sp.before[b] * a.H_kv + h / R * nt;
+    c0 = ((F + 1) * G - 1) / T;  // the last span that starts at or before the tile
+    c1 = ((F + nt) * G - 1) / T;
   } else {
     const long long c = 1 + w / R;
     if (c >= G) return;
-    const long long f = T * c / G;
-    if (f >= T) return;
-    int lo = 0, hi = a.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (sp.before[mid] * a.H_kv <= f) lo = mid; else hi = mid - 1;
-    }
-    b = lo;
-    nt = (int)(sp.before[b + 1] - sp.before[b]);
-    g = (int)((f - sp.before[b] * a.H_kv) / nt);
-    F = sp.before[b] * a.H_kv + (long long)g * nt;
-    if (f == F || T * (c - 1) / G > F) return;
-    h = g * R + (int)(w % R);
+    const int2 cut = sp.cut[c];
+    if (cut.x < 0) return;
+    hd = (int)(w % R);
+    row = (long long)(cut.x / a.H_kv) * a.H_q + (cut.x % a.H_kv) * R + hd;
+    c0 = c - 1;
+    // (the border cuts the unit, so the tile before it lies in the nearest span that has any)
+    while (c0 > 0 && sp.cut[c0].y < 0) --c0;
+    c1 = cut.y;
   }
-  Sum s;
-  const long long n_rows = (long long)a.T_q * a.H_q, row = (long long)b * a.H_q + h;
-  for (int p = 0; p < sp.n_prefix; ++p) s.add(a.part_lse[p * n_rows + row], a.part_o + (p * n_rows + row) * kHeadDim, lane);
-  // the span that holds tile f is the last one that starts at or before it
-  const long long c0 = ((F + 1) * G - 1) / T, c1 = ((F + nt) * G - 1) / T;
-  if (c0 == c1) {
-    s.add(sp.whole_lse[row], sp.whole_o + row * kHeadDim, lane);
-  } else {
-    for (long long c = c0; c <= c1; ++c) {
-      if (c > c0 && T * c / G == T * (c + 1) / G) continue;  // an empty span
-      const long long slot = (2 * c + (c == c0 ? 1 : 0)) * R + (h - g * R);
-      s.add(sp.piece_lse[slot], sp.piece_o + slot * kHeadDim, lane);
-    }
-  }
+  const long long n_rows = (long long)a.T_q * a.H_q;
+  const int n_pre = sp.n_prefix, n_own = (int)(c1 - c0) + 1;
+  auto slot = [&](int p) { return (2 * (c0 + p) + (p == 0 ? 1 : 0)) * R + hd; };
+  auto empty = [&](int p) { return p > 0 && sp.cut[c0 + p].y < 0; };  // a span without tiles
+  const Joined s = join_parts(
+      n_pre + n_own,
+      [&](int p) {
+        return p < n_pre ? a.part_lse[p * n_rows + row]
+               : n_own == 1 ? sp.whole_lse[row] : empty(p - n_pre) ? -INFINITY : sp.piece_lse[slot(p - n_pre)];
+      },
+      [&](int p) {
+        return p < n_pre ? a.part_o + (p * n_rows + row) * kHeadDim
+               : n_own == 1 ? sp.whole_o + row * kHeadDim : sp.piece_o + slot(p - n_pre) * kHeadDim;
+      });
+  const int b = (int)(row / a.H_q), h = (int)(row % a.H_q);
   const int n_keys = a.prefix_len + max(checked_len(a, b), 0);
   const float den = s.w == 0.f ? (n_keys > 0 ? NAN : 1.f) : s.w;  // every score -inf: 0 / 0, as the formula has it
+  float o[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) s.o[e] /= den;
-  store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)b * a.o_stride + (size_t)h * kHeadDim + lane * 4, s.o);
+  for (int e = 0; e < 4; ++e) o[e] = s.o[e] / den;
+  store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)b * a.o_stride + (size_t)h * kHeadDim + lane * 4, o);
   if (lane == 0 && a.lse) a.lse[row] = s.w == 0.f ? (n_keys > 0 ? NAN : -INFINITY) : (s.m + log2f(s.w)) * kLn2;
 }
 
@@ -586,7 +635,7 @@ cudaError_t attn_keys_launch(const AttnArgs& a, const AttnSpans& sp, cudaStream_
   if (e != cudaSuccess) return e;
   const long long warps = a.prefix_len > 0 ? (long long)a.B * a.H_q : (long long)(sp.n_spans - 1) * R;
   if (warps == 0) return cudaSuccess;
-  return launch_pdl(attn_join_spans, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a, sp, sp.n_spans);
+  return launch_pdl(attn_join_spans, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a, sp);
 }
 
 }  // namespace provip

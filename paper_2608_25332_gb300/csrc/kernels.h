@@ -337,6 +337,8 @@ struct AttnSpans {
   int n_spans;
   int n_prefix;              // parts of the prefix, in part_* of AttnArgs
   long long* before;         // [B + 1] 128-key tiles of the requests before each
+  int2* cut;                 // [n_spans] the unit that a span's start is the first to cut (-1: none) and the
+                             // span of its last tile (-1: the span is empty)
   float *whole_o, *whole_lse, *piece_o, *piece_lse;
 };
 constexpr int kSpanHeads = 8;
