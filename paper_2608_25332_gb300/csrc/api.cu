@@ -1189,6 +1189,7 @@ struct AttnCut {
   int n_own, n_prefix, n_part;  // parts of a row's keys (prompt: n_part only)
   AttnPlan plan;                // tensor cores
   int n_spans;                  // decoding on the tensor cores: CTAs of the own keys (0: as units of plan)
+  bool by_unit;                 // a unit each
 };
 
 // CUDA cores: row tiles of 64 packed rows, parts of four 64-key tiles or more. Tensor cores:
@@ -1224,9 +1225,10 @@ AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int p
 }
 
 // Tensor cores, up to eight heads a group: the own keys' tiles shared out evenly over two CTAs
-// an SM (two tiles a CTA at least), the prefix's as units of the row form, with the keys shared
-// out until its CTAs have one each, four tiles or more a part (a part writes as many bytes of
-// partial results as one tile has). More heads a group: units of the row form for both, of
+// an SM (two tiles a CTA at least; where every unit has its CTA and four tiles at most, a unit
+// each), the prefix's as units of the row form, with the keys shared out until its CTAs have
+// their share of the SMs, four tiles or more a part (a part writes as many bytes of partial
+// results as one tile has). More heads a group: units of the row form for both, of
 // about as many tiles as a CTA's even share, two at least.
 AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int dtype, int algo) {
   AttnCut c;
@@ -1245,10 +1247,13 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
   const long long own_tiles = ((long long)kv_len_max + 127) / 128, pre_tiles = ((long long)prefix_len + 127) / 128;
   if (R <= kSpanHeads) {
     const long long tiles = (long long)B * H_kv * (own_tiles > 0 ? own_tiles : 1);
-    c.n_spans = (int)((tiles + 1) / 2 < 2 * kPlanSms ? (tiles + 1) / 2 : 2 * kPlanSms);
+    c.by_unit = (long long)B * H_kv <= 2 * kPlanSms && own_tiles <= 4;
+    c.n_spans = c.by_unit ? B * H_kv : (int)((tiles + 1) / 2 < 2 * kPlanSms ? (tiles + 1) / 2 : 2 * kPlanSms);
     p.nq = B <= TT ? 1 : 2;
     const long long units = ((long long)B + p.nq * TT - 1) / (p.nq * TT) * H_kv;
-    c.n_prefix = attn_parts(units, prefix_len, kPlanSms * (p.nq == 2 ? 1 : 2), 512, 64);
+    // the two kernels run side by side, on SMs in proportion to their tiles (of about equal cost)
+    const long long pre = units * pre_tiles, ctas = pre > 0 ? kPlanSms * pre / (pre + tiles) : 0;
+    c.n_prefix = attn_parts(units, prefix_len, ctas / units * units, 512, 64);
     c.n_part = c.n_prefix;
     p.n_prefix_parts = c.n_prefix;
     p.n_prefix_units = (int)(units * c.n_prefix);
@@ -1285,6 +1290,7 @@ size_t decode_ws(Carve& c, const AttnCut& cut, int B, int H_q, int H_kv, float**
   if (cut.n_spans == 0) return attn_ws(c, cut.n_part, B, H_q, part_o, part_lse);
   const size_t rows = (size_t)B * H_q, pieces = 2 * (size_t)cut.n_spans * (H_q / H_kv);
   sp->n_spans = cut.n_spans;
+  sp->by_unit = cut.by_unit ? 1 : 0;
   sp->n_prefix = cut.n_prefix;
   sp->before = c.take<long long>((size_t)B + 1);
   sp->cut = c.take<int2>(cut.n_spans);

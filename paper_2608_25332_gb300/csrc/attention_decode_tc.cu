@@ -14,7 +14,8 @@
 // at a unit's first tile and past that it is found and P formed again.
 //
 // Work. The tiles of all (request, key/value head) units lie end to end; CTA c of G takes
-// tiles [c T / G, (c + 1) T / G), whatever the requests' lengths, so all CTAs end together. A
+// tiles [c T / G, (c + 1) T / G), whatever the requests' lengths, so all CTAs end together (a
+// few short requests: a unit each, which needs no scan of the lengths and no join). A
 // unit inside one CTA's span is finished by it; one that a span's border cuts is written in
 // pieces, at most two a CTA, which a second kernel joins. Two CTAs an SM, each with a ring
 // of three 32 KiB stages that TMA fills across units.
@@ -93,6 +94,18 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* v) {
                "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
                "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
                : "memory");
+}
+
+// first tile of span c of G over T tiles
+__device__ __forceinline__ long long span_start(long long T, int c, int G) {
+  // (a 64-bit division takes a few hundred instructions)
+  if (T < (1 << 22)) return (long long)((unsigned)T * (unsigned)c / (unsigned)G);
+  return T * c / G;
+}
+// the last span that starts at or before tile f
+__device__ __forceinline__ int span_of(long long f, long long T, int G) {
+  if (T < (1 << 22)) return (int)((((unsigned)f + 1u) * (unsigned)G - 1u) / (unsigned)T);
+  return (int)(((f + 1) * G - 1) / T);
 }
 
 // the warp's sum of the requests' tiles before each of 32 requests, and of all 32
@@ -212,43 +225,43 @@ __global__ void __launch_bounds__(kThr, 2)
     const int box = min(a.page_size, kT);
     bool live = true;
     uint32_t n_ld = 0, u = 0, tile0 = 0;
-    // lengths of 256 requests in the lanes' registers (beyond, they are read twice)
-    constexpr int kHeld = 8;
-    int held[kHeld];
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0;
-    auto len_of = [&](int i) { return i < kHeld ? held[i] : i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0; };
-    // all tiles, and the tiles of the requests before each
-    long long T = 0;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      if (i * 32 >= a.B) break;
-      int all;
-      const int t = i * 32 + lane < a.B ? unit_tiles(held[i]) : 0, before = tiles_before(t, lane, all);
-      if (blockIdx.x == 0 && i * 32 + lane < a.B) {
-        sp.before[i * 32 + lane] = T + before;
-        if (held[i] < 0) set_error(a.err, kErrBadDeviceArg);
-      }
-      T += all;
-    }
-    for (int i = kHeld; i * 32 < a.B; ++i) {
-      const int k = len_of(i);
-      int all;
-      const int t = i * 32 + lane < a.B ? unit_tiles(k) : 0, before = tiles_before(t, lane, all);
-      if (blockIdx.x == 0 && i * 32 + lane < a.B) {
-        sp.before[i * 32 + lane] = T + before;
-        if (k < 0) set_error(a.err, kErrBadDeviceArg);
-      }
-      T += all;
-    }
-    if (blockIdx.x == 0 && lane == 0) sp.before[a.B] = T;
-    T *= a.H_kv;
-    long long f = T * blockIdx.x / G;
-    const long long f_end = T * (blockIdx.x + 1) / G;
-    // the request that holds tile f: its tiles, and those before it
+    long long f = 0, f_end = 1, f_b = 0, T = 0;  // this CTA's tiles; the first of request b
     int b = 0, k_len = 0, nt_b = 1;
-    long long f_b = 0;
-    if (f < f_end) {
+    if (sp.by_unit) {
+      // a unit each: nothing to share out
+      b = (int)blockIdx.x / a.H_kv;
+      k_len = checked_len(a, b);
+      if (k_len < 0 && lane == 0) set_error(a.err, kErrBadDeviceArg);
+      k_len = max(k_len, 0);
+      nt_b = unit_tiles(k_len);
+      f = (long long)((int)blockIdx.x - b * a.H_kv) * nt_b;
+      f_end = f + nt_b;
+    } else {
+      // lengths of 256 requests in the lanes' registers (beyond, they are read twice)
+      constexpr int kHeld = 8;
+      int held[kHeld];
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0;
+      auto len_of = [&](int i) { return i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0; };
+      // all tiles, and the tiles of the requests before each
+      auto count = [&](int i, int k) {
+        int all;
+        const int t = i * 32 + lane < a.B ? unit_tiles(k) : 0, before = tiles_before(t, lane, all);
+        if (blockIdx.x == 0 && i * 32 + lane < a.B) {
+          sp.before[i * 32 + lane] = T + before;
+          if (k < 0) set_error(a.err, kErrBadDeviceArg);
+        }
+        T += all;
+      };
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (i * 32 < a.B) count(i, held[i]);
+      for (int i = kHeld; i * 32 < a.B; ++i) count(i, len_of(i));
+      if (blockIdx.x == 0 && lane == 0) sp.before[a.B] = T;
+      T *= a.H_kv;
+      f = span_start(T, (int)blockIdx.x, G);
+      f_end = span_start(T, (int)blockIdx.x + 1, G);
+      // the request that holds tile f: its tiles, and those before it
       long long done = 0;
       auto look = [&](int i, int k) {
         int all;
@@ -264,34 +277,23 @@ __global__ void __launch_bounds__(kThr, 2)
         done += all;
         return here;
       };
-      bool here = false;
+      bool here = f >= f_end;  // a span without tiles looks for nothing
 #pragma unroll
       for (int i = 0; i < kHeld; ++i)
         if (!here && i * 32 < a.B) here = look(i, held[i]);
       for (int i = kHeld; !here && i * 32 < a.B; ++i) here = look(i, len_of(i));
     }
-    // what a border cuts: the first border inside a unit tells the joining kernel
-    if (lane == 0) {
-      int unit = -1;
-      long long last = -1;  // a span without tiles
-      if (f < f_end) {
-        last = 0;
-        const int in = (int)(f - f_b);
-        const long long F = f_b + in / nt_b * nt_b;
-        // no other span starts inside the unit before this one: the tile before it lies in a
-        // span that starts at or before the unit
-        if (f > F && T * ((f * G - 1) / T) / G <= F) {
-          unit = b * a.H_kv + in / nt_b;
-          last = ((F + nt_b) * G - 1) / T;  // the span that holds the unit's last tile
-        }
-      }
-      sp.cut[blockIdx.x] = make_int2(unit, (int)last);
-    }
-    // one tile, K or V, into the next stage
+    const long long f0 = f, f0_b = f_b;
+    const int b0 = b, nt0_b = nt_b;
+    // One tile, K or V, into the next stage. A lane's page is looked up once for both, and
+    // before the wait for the stage.
+    int row = 0;
     auto load = [&](const Piece& x, int j, bool v) {
       const uint32_t st = n_ld % kStages, ph = (n_ld / kStages) & 1u;
       ++n_ld;
       const int n = min(kT, x.n_keys - j * kT), boxes = n > 0 ? (n + box - 1) / box : 0;
+      if (!v && lane < boxes)
+        row = (int)attn_slot(a, a.block_table + (size_t)x.b * a.max_pages, (x.t_lo + j) * kT + lane * box);
       bool ok = true;
       if (lane == 0) {
         ok = !ctl.fail && mbar_wait(&ctl.kv_empty[st], ph ^ 1u, a.err);
@@ -302,7 +304,6 @@ __global__ void __launch_bounds__(kThr, 2)
       uint8_t* dst = kv + st * kStage;
       const CUtensorMap* map = v ? &map_v : &map_k;
       if (lane < boxes) {
-        const int row = (int)attn_slot(a, a.block_table + (size_t)x.b * a.max_pages, (x.t_lo + j) * kT + lane * box);
         tma_load_2d(dst + lane * box * 128, map, x.g * kHeadDim, row, &ctl.kv_full[st]);
         tma_load_2d(dst + kHalf + lane * box * 128, map, x.g * kHeadDim + 64, row, &ctl.kv_full[st]);
       }
@@ -357,6 +358,22 @@ __global__ void __launch_bounds__(kThr, 2)
         live = load(x, j, true);
         if (live && j + 1 < x.nt) live = load(x, j + 1, false);
       }
+    }
+    // what a border cuts: the first border inside a unit tells the joining kernel
+    if (!sp.by_unit && lane == 0) {
+      int unit = -1, last = -1;  // a span without tiles
+      if (f0 < f_end) {
+        last = 0;
+        const int in = (int)(f0 - f0_b);
+        const long long F = f0_b + in / nt0_b * nt0_b;
+        // no other span starts inside the unit before this one: the tile before it lies in a
+        // span that starts at or before the unit
+        if (f0 > F && span_start(T, span_of(f0 - 1, T, G), G) <= F) {
+          unit = b0 * a.H_kv + in / nt0_b;
+          last = span_of(F + nt0_b - 1, T, G);  // the span that holds the unit's last tile
+        }
+      }
+      sp.cut[blockIdx.x] = make_int2(unit, last);
     }
     if (!live) ctl.fail = 1;
   } else {
@@ -504,6 +521,9 @@ __global__ void __launch_bounds__(kThr, 2)
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, kTmemCols);
+  // where this kernel runs beside the prefix's, it does not complete before it: the joining
+  // kernel waits for this one alone
+  if (blockIdx.x == 0 && threadIdx.x == 0) pdl_wait_prior();
 }
 
 // ---------------------------------------------------------------------------
@@ -547,32 +567,34 @@ __global__ void __launch_bounds__(256) attn_join_spans(const __grid_constant__ A
   pdl_wait_prior();
   const int lane = threadIdx.x & 31, R = a.H_q / a.H_kv, G = sp.n_spans;
   const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  long long row, c0, c1;  // the spans that hold the unit's first and last tile
-  int hd;
+  long long row;
+  int hd, c0 = 0, c1 = 0;  // the spans that hold the unit's first and last tile
   if (a.prefix_len > 0) {
     if (w >= (long long)a.B * a.H_q) return;
     row = w;
     const int b = (int)(w / a.H_q), h = (int)(w % a.H_q);
     hd = h % R;
-    const long long T = sp.before[a.B] * a.H_kv, nt = sp.before[b + 1] - sp.before[b];
-    const long long F = sp.before[b] * a.H_kv + h / R * nt;
-    c0 = ((F + 1) * G - 1) / T;  // the last span that starts at or before the tile
-    c1 = ((F + nt) * G - 1) / T;
+    if (!sp.by_unit) {
+      const long long T = sp.before[a.B] * a.H_kv, first = sp.before[b], nt = sp.before[b + 1] - first;
+      const long long F = first * a.H_kv + h / R * nt;
+      c0 = span_of(F, T, G);
+      c1 = span_of(F + nt - 1, T, G);
+    }
   } else {
-    const long long c = 1 + w / R;
+    const int c = (int)(1 + w / R);
     if (c >= G) return;
     const int2 cut = sp.cut[c];
     if (cut.x < 0) return;
     hd = (int)(w % R);
     row = (long long)(cut.x / a.H_kv) * a.H_q + (cut.x % a.H_kv) * R + hd;
-    c0 = c - 1;
     // (the border cuts the unit, so the tile before it lies in the nearest span that has any)
+    c0 = c - 1;
     while (c0 > 0 && sp.cut[c0].y < 0) --c0;
     c1 = cut.y;
   }
   const long long n_rows = (long long)a.T_q * a.H_q;
-  const int n_pre = sp.n_prefix, n_own = (int)(c1 - c0) + 1;
-  auto slot = [&](int p) { return (2 * (c0 + p) + (p == 0 ? 1 : 0)) * R + hd; };
+  const int n_pre = sp.n_prefix, n_own = c1 - c0 + 1;
+  auto slot = [&](int p) { return (size_t)(2 * (c0 + p) + (p == 0 ? 1 : 0)) * R + hd; };
   auto empty = [&](int p) { return p > 0 && sp.cut[c0 + p].y < 0; };  // a span without tiles
   const Joined s = join_parts(
       n_pre + n_own,
@@ -605,6 +627,8 @@ cudaError_t launch(const AttnArgs& a, const AttnSpans& sp, const CUtensorMap& q,
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
+  // beside the prefix's kernel, where there is one (whose results it does not read)
+  if (sp.n_prefix > 0) return launch_pdl(attn_keys_tc<R>, dim3(sp.n_spans), dim3(kThr), kSmem, s, sp.n_spans, a, sp, q, k, v);
   attn_keys_tc<R><<<sp.n_spans, kThr, kSmem, s>>>(sp.n_spans, a, sp, q, k, v);
   return cudaGetLastError();
 }
@@ -633,7 +657,7 @@ cudaError_t attn_keys_launch(const AttnArgs& a, const AttnSpans& sp, cudaStream_
     default: return cudaErrorInvalidValue;
   }
   if (e != cudaSuccess) return e;
-  const long long warps = a.prefix_len > 0 ? (long long)a.B * a.H_q : (long long)(sp.n_spans - 1) * R;
+  const long long warps = a.prefix_len > 0 ? (long long)a.B * a.H_q : sp.by_unit ? 0 : (long long)(sp.n_spans - 1) * R;
   if (warps == 0) return cudaSuccess;
   return launch_pdl(attn_join_spans, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a, sp);
 }

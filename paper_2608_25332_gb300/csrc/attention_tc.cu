@@ -28,17 +28,17 @@
 namespace provip {
 namespace {
 
-// registers a thread with two row tiles: a row's 128 scores live in them; the sum over the
-// block is what it is launched with (168 a thread)
-constexpr int kSoftRegs = 224, kRestRegs = 56;
 constexpr float kMostSum = 1024.f;     // of a row's 128 values of P before its maximum is raised
 
 template <int NQ>
 struct Form {
   static constexpr int kStages = NQ == 2 ? 5 : 2;
   static constexpr int kSoft = 128 * NQ;               // softmax threads
-  static constexpr int kThreads = NQ == 2 ? 384 : 192;  // + MMA warp + TMA warp (+ 2 idle)
+  static constexpr int kThreads = kSoft + 128;         // + MMA warp + TMA warp + 2 idle ones
   static constexpr int kCtas = NQ == 2 ? 1 : 2;
+  // registers a thread: a row's 128 scores live in the softmax warps'; the sum over the block
+  // is what it is launched with (168 a thread and 128)
+  static constexpr int kSoftRegs = NQ == 2 ? 224 : 208, kRestRegs = NQ == 2 ? 56 : 48;
   static constexpr size_t kSmem = (size_t)(NQ + kStages) * kStage + 1024;
   static constexpr uint32_t kCols = 256 * NQ;          // S and O of every row tile
 };
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
   const uint32_t tmem = ctl.tmem;
 
   if (warp >= 4 * NQ) {
-    if (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kRestRegs));
     if (warp == 4 * NQ) {
       // ---- MMA issuer: the whole warp walks through the tiles, one lane issues ----
       const bool lead = elect_one();
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     }
   } else {
     // ---- softmax: a thread per row ----
-    if (NQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kSoftRegs));
     const int i = NQ == 2 ? warp >> 2 : 0, r = (warp & 3) * 32 + lane;
     const uint32_t ts = tmem + i * kT + ((uint32_t)(r & ~31) << 16), to = ts + NQ * kT;
     const int tok_in = r / R, tok_first = (r & ~31) / R;
@@ -651,7 +651,7 @@ cudaError_t launch(const AttnArgs& a, const AttnPlan& plan, const Maps& maps, in
     if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, attn_tc<NQ>);
     if (e != cudaSuccess) return e;
     // a register split that the launch does not cover would wait for ever
-    if (NQ == 2 && at.numRegs * F::kThreads < kSoftRegs * F::kSoft + kRestRegs * (F::kThreads - F::kSoft))
+    if (at.numRegs * F::kThreads < F::kSoftRegs * F::kSoft + F::kRestRegs * (F::kThreads - F::kSoft))
       return cudaErrorInvalidConfiguration;
     configured[dev] = true;
   }

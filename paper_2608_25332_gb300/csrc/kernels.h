@@ -335,6 +335,7 @@ cudaError_t attn_tc_launch(const AttnArgs& a, const AttnPlan& plan, int sms, cud
 // slot 2 c (the unit began before its span) or 2 c + 1 of piece_*[2 n_spans][H_q / H_kv].
 struct AttnSpans {
   int n_spans;
+  int by_unit;               // CTA c takes unit c, nothing is cut
   int n_prefix;              // parts of the prefix, in part_* of AttnArgs
   long long* before;         // [B + 1] 128-key tiles of the requests before each
   int2* cut;                 // [n_spans] the unit that a span's start is the first to cut (-1: none) and the
