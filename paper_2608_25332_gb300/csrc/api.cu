@@ -1211,16 +1211,18 @@ AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int p
   const int TT = 128 / (R > 128 ? 128 : R);
   AttnPlan& p = c.plan;
   p.nq = q_len_max <= TT ? 1 : 2;
-  p.n_blk = (int)(((long long)q_len_max + p.nq * TT - 1) / (p.nq * TT));
-  if (p.n_blk < 1) p.n_blk = 1;
-  const long long units = (long long)p.n_blk * B * H_kv, ctas = kPlanSms * (p.nq == 2 ? 1 : 2);
+  long long n_blk = ((long long)q_len_max + p.nq * TT - 1) / (p.nq * TT);
+  if (n_blk < 1) n_blk = 1;
+  const long long units = n_blk * B * H_kv, ctas = kPlanSms * (p.nq == 2 ? 1 : 2);
   c.n_part = 1;
   if (2 * units <= ctas) c.n_part = attn_parts(units, keys, ctas / units * units, 512, 32);
   if (c.n_part < 1) c.n_part = 1;
   p.n_units = units * c.n_part;
-  // keys and values of a chunk: 48 MB, which leaves the 126 MB L2 room for the rest
-  const long long pair = (long long)keys * 2 * kHeadDim * 2, fit = (48ll << 20) / (pair > 0 ? pair : 1);
-  p.chunk = (int)(fit < 1 ? 1 : fit > (long long)B * H_kv ? (long long)B * H_kv : fit);
+  // keys and values of a chunk: 80 MB, which leaves the 126 MB L2 room for the rest
+  const long long pair = (long long)keys * 2 * kHeadDim * 2, fit = (80ll << 20) / (pair > 0 ? pair : 1);
+  p.chunk_heads = (int)(fit < 1 ? 1 : fit < H_kv ? fit : H_kv);
+  const long long seqs = fit / H_kv;
+  p.chunk_seqs = (int)(seqs < 1 ? 1 : seqs > 256 ? 256 : seqs);
   return c;
 }
 
@@ -1251,8 +1253,8 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
     c.n_spans = c.by_unit ? B * H_kv : (int)((tiles + 1) / 2 < 2 * kPlanSms ? (tiles + 1) / 2 : 2 * kPlanSms);
     p.nq = B <= TT ? 1 : 2;
     const long long units = ((long long)B + p.nq * TT - 1) / (p.nq * TT) * H_kv;
-    // the two kernels run side by side, on SMs in proportion to their tiles (of about equal cost)
-    const long long pre = units * pre_tiles, ctas = pre > 0 ? kPlanSms * pre / (pre + tiles) : 0;
+    // the two kernels run side by side, on SMs in proportion to their tiles (two row tiles: twice the cost)
+    const long long pre = 2 * units * pre_tiles, ctas = pre > 0 ? kPlanSms * pre / (pre + tiles) : 0;
     c.n_prefix = attn_parts(units, prefix_len, ctas / units * units, 512, 64);
     c.n_part = c.n_prefix;
     p.n_prefix_parts = c.n_prefix;

@@ -16,7 +16,8 @@
 // taken a third of a tile's time. S of a tile is complete after the product of the tile before
 // (one thread issues both, and a commit covers all that it issued), so a rescale needs no
 // further wait.
-// Roles: warps 0 .. 4 NQ - 1 softmax, then one warp issues the MMAs and one the TMA loads.
+// Roles: warps 0 .. 4 NQ - 1 softmax, then one warp issues the MMAs, one the TMA loads, and one
+// works the units out.
 // K and V tiles share a ring of 32 KiB stages. While the softmax works on one row tile, the
 // tensor cores multiply for the other (NQ = 2, one CTA an SM), or for the other CTA of the
 // SM (NQ = 1, two CTAs).
@@ -34,7 +35,7 @@ template <int NQ>
 struct Form {
   static constexpr int kStages = NQ == 2 ? 5 : 2;
   static constexpr int kSoft = 128 * NQ;               // softmax threads
-  static constexpr int kThreads = kSoft + 128;         // + MMA warp + TMA warp + 2 idle ones
+  static constexpr int kThreads = kSoft + 128;         // + MMA, TMA and unit warps, an idle one
   static constexpr int kCtas = NQ == 2 ? 1 : 2;
   // registers a thread: a row's 128 scores live in the softmax warps'; the sum over the block
   // is what it is launched with (168 a thread and 128)
@@ -47,8 +48,8 @@ struct Maps {
   CUtensorMap q, k, v, kp, vp;
 };
 
-// One unit, as the producer works it out and the other roles read it (a board of kBoard
-// units in shared memory, which keeps the decoding out of their registers and way).
+// One unit, as its warp works it out and the other roles read it (a board of kBoard units in
+// shared memory, which keeps the decoding out of their registers and way).
 template <int NQ>
 struct Unit {
   AttnSeq s;
@@ -113,19 +114,41 @@ __device__ __noinline__ void scale_o(uint32_t to, float f) {
 // ---------------------------------------------------------------------------
 // units
 // ---------------------------------------------------------------------------
+// the tiles of a unit whose sequence, head, part and first token are known
 template <int NQ>
-__device__ __forceinline__ Unit<NQ> unit_of(const AttnArgs& a, const AttnPlan& p, int u) {
-  Unit<NQ> x;
+__device__ __forceinline__ void set_tiles(const AttnArgs& a, Unit<NQ>& x, int part, int n_parts) {
   const int R = a.H_q / a.H_kv, TT = kT / R;
-  int blk, n_parts, part;
-  bool own = true;
-  if (a.paged && u < p.n_prefix_units) {
-    // the tokens of every request against the prefix
-    part = u % p.n_prefix_parts;
-    u /= p.n_prefix_parts;
-    x.g = u % a.H_kv;
-    blk = u / a.H_kv;
+  x.n_pt = (x.n_prefix + kT - 1) / kT;
+  int most = 0, tiles[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    x.n_tok[i] = min(max(x.s.q_len - x.tok0 - i * TT, 0), TT);
+    tiles[i] = 0;
+    if (x.n_tok[i] > 0) {
+      const int vis = attn_visible(a, x.s.q_len, x.s.k_len, x.tok0 + i * TT + x.n_tok[i] - 1);
+      tiles[i] = x.n_pt + (vis + kT - 1) / kT;
+    }
+    most = max(most, tiles[i]);
+  }
+  const int per = (most + n_parts - 1) / n_parts;
+  x.t_lo = min(part * per, most);
+  x.ntm = min(x.t_lo + per, most) - x.t_lo;
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) x.nt[i] = min(max(tiles[i] - x.t_lo, 0), x.ntm);
+}
+
+// paged: the units of the prefix (the tokens of every request against it), then those of the
+// requests' own keys
+template <int NQ>
+__device__ __forceinline__ Unit<NQ> paged_unit(const AttnArgs& a, const AttnPlan& p, int u) {
+  Unit<NQ> x;
+  int part, n_parts;
+  if (u < p.n_prefix_units) {
     n_parts = p.n_prefix_parts;
+    part = u % n_parts;
+    u /= n_parts;
+    x.g = u % a.H_kv;
+    x.tok0 = u / a.H_kv * NQ * (kT / (a.H_q / a.H_kv));
     x.part = p.n_own_parts + part;
     x.s.q0 = 0;
     x.s.q_len = a.B;
@@ -134,52 +157,108 @@ __device__ __forceinline__ Unit<NQ> unit_of(const AttnArgs& a, const AttnPlan& p
     x.s.pages = nullptr;
     x.s.ok = true;
     x.n_prefix = a.prefix_len;
-    own = false;
-  } else if (a.paged) {
+  } else {
     u -= p.n_prefix_units;
+    n_parts = p.n_own_parts;
     x.g = u % a.H_kv;
     u /= a.H_kv;
-    part = u % p.n_own_parts;
-    x.s = attn_seq(a, u / p.n_own_parts);
-    blk = 0;
-    n_parts = p.n_own_parts;
+    part = u % n_parts;
+    x.s = attn_seq(a, u / n_parts);
+    x.tok0 = 0;
     x.part = part;
     x.n_prefix = 0;
-  } else {
-    // (sequence, head) pairs in chunks whose keys and values stay in L2; within a chunk the
-    // last rows, which see the most keys, first
-    const int n_bg = a.B * a.H_kv, per = p.chunk * p.n_blk * a.n_part, c = u / per;
-    const int sz = min(p.chunk, n_bg - c * p.chunk) * a.n_part;
-    const int rem = u - c * per;
-    blk = p.n_blk - 1 - rem / sz;
-    const int in = rem % sz, bg = c * p.chunk + in / a.n_part;
-    part = in % a.n_part;
-    x.g = bg % a.H_kv;
-    x.s = attn_seq(a, bg / a.H_kv);
-    n_parts = a.n_part;
-    x.part = part;
-    x.n_prefix = a.prefix_len;
   }
-  x.tok0 = blk * NQ * TT;
-  x.n_pt = (x.n_prefix + kT - 1) / kT;
-  int most = 0, tiles[NQ];
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    x.n_tok[i] = min(max(x.s.q_len - x.tok0 - i * TT, 0), TT);
-    tiles[i] = 0;
-    if (x.n_tok[i] > 0) {
-      const int vis = own ? attn_visible(a, x.s.q_len, x.s.k_len, x.tok0 + i * TT + x.n_tok[i] - 1) : 0;
-      tiles[i] = x.n_pt + (vis + kT - 1) / kT;
-    }
-    most = max(most, tiles[i]);
-  }
-  const int per = (most + n_parts - 1) / n_parts;
-  x.t_lo = min(part * per, most);
-  const int t_hi = min(x.t_lo + per, most);
-  x.ntm = t_hi - x.t_lo;
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) x.nt[i] = min(max(tiles[i] - x.t_lo, 0), x.ntm);
+  set_tiles(a, x, part, n_parts);
   return x;
+}
+
+// Contiguous keys: the units that have rows, in an order that the producer walks through. The
+// sequences (and, where one's keys are too many, its heads) come in chunks whose keys and
+// values stay in L2; within a chunk level by level, level l holding the l-th block of rows from
+// each sequence's end, which sees the most keys, so that long units come first. The blocks of a
+// chunk's sequences (256 at most) lie in the lanes' registers.
+struct Walk {
+  static constexpr int kHeld = 8;
+  int nb[kHeld];   // blocks of sequence b0 + 32 i + lane
+  int b0, n_seq;   // the chunk's sequences
+  int g0, n_g;     // and heads
+  int level, more; // the level, and how many like it follow (sequences of the same number of blocks)
+  int base, cnt;   // units before this level, and of it
+};
+__device__ __forceinline__ void walk_level(const AttnArgs& a, Walk& w) {
+  int n = 0;
+  unsigned least = 0x7fffffffu;
+#pragma unroll
+  for (int i = 0; i < Walk::kHeld; ++i) {
+    if (i * 32 >= w.n_seq) break;
+    const bool has = w.nb[i] > w.level;
+    n += __popc(__ballot_sync(0xffffffffu, has));
+    if (has) least = min(least, (unsigned)w.nb[i]);
+  }
+  w.cnt = n * w.n_g * a.n_part;
+  w.more = n ? (int)__reduce_min_sync(0xffffffffu, least) - w.level - 1 : 0;
+}
+template <int NQ>
+__device__ __forceinline__ void walk_chunk(const AttnArgs& a, const AttnPlan& p, Walk& w) {
+  const int lane = threadIdx.x & 31, rows = NQ * (kT / (a.H_q / a.H_kv));
+  w.n_seq = min(p.chunk_seqs, a.B - w.b0);
+  w.n_g = min(p.chunk_heads, a.H_kv - w.g0);
+#pragma unroll
+  for (int i = 0; i < Walk::kHeld; ++i) {
+    w.nb[i] = 0;
+    if (i * 32 + lane < w.n_seq) {
+      const AttnSeq s = attn_seq(a, w.b0 + i * 32 + lane);
+      if (!s.ok) set_error(a.err, kErrBadDeviceArg);
+      w.nb[i] = (s.q_len + rows - 1) / rows;
+    }
+  }
+  w.level = 0;
+  walk_level(a, w);
+}
+// unit u, which comes after the one asked for before; false: there is none
+template <int NQ>
+__device__ __forceinline__ bool walk_to(const AttnArgs& a, const AttnPlan& p, Walk& w, int u, Unit<NQ>& x) {
+  while (u >= w.base + w.cnt) {
+    if (w.cnt > 0) {
+      const int skip = min((u - w.base) / w.cnt, w.more + 1);
+      w.base += skip * w.cnt;
+      w.level += skip;
+      w.more -= skip;
+      if (w.more < 0) walk_level(a, w);
+    } else {
+      w.g0 += w.n_g;
+      if (w.g0 >= a.H_kv) {
+        w.g0 = 0;
+        w.b0 += w.n_seq;
+        if (w.b0 >= a.B) return false;
+      }
+      walk_chunk<NQ>(a, p, w);
+    }
+  }
+  int in = u - w.base;
+  const int part = in % a.n_part;
+  in /= a.n_part;
+  x.g = w.g0 + in % w.n_g;
+  in /= w.n_g;  // the in-th sequence that has this level
+  int b = 0, nb = 0;
+#pragma unroll
+  for (int i = 0; i < Walk::kHeld; ++i) {
+    if (i * 32 >= w.n_seq) break;
+    const unsigned has = __ballot_sync(0xffffffffu, w.nb[i] > w.level);
+    const int n = __popc(has);
+    if (in >= 0 && in < n) {
+      const int src = (int)__fns(has, 0, in + 1);
+      b = w.b0 + i * 32 + src;
+      nb = __shfl_sync(0xffffffffu, w.nb[i], src);
+    }
+    in -= n;
+  }
+  x.s = attn_seq(a, b);
+  x.n_prefix = a.prefix_len;
+  x.part = part;
+  x.tok0 = (nb - 1 - w.level) * NQ * (kT / (a.H_q / a.H_kv));
+  set_tiles(a, x, part, a.n_part);
+  return true;
 }
 
 // key of the list that tile t starts with
@@ -250,6 +329,9 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
         __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), (lane & ~3) + s);
     to4[s] = d ? reinterpret_cast<char*>(d) + (lane & 3) * 16 : nullptr;
   }
+  const uint64_t inv2 = pack2(inv, inv), nil2 = pack2(nil, nil);
+  uint64_t sum[2] = {0, 0};
+  // (unrolled, this code is fetched once a unit and its misses cost more than the loop)
 #pragma unroll 1
   for (int c = 0; c < 4; ++c) {
     float o[32];
@@ -257,13 +339,12 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
       tmem_ld32(to + c * 32, o);
       tc_wait_ld();
     }
-    float bad = 0.f;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      o[e] = none ? nil : o[e] * inv;
-      bad = fmaf(o[e], 0.f, bad);  // NaN once an element is not finite
+    for (int e = 0; e < 32; e += 2) {
+      const uint64_t v = none ? nil2 : fma2(pack2(o[e], o[e + 1]), inv2, 0);
+      sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], v);  // not finite once an element is not
+      unpack2(v, o[e], o[e + 1]);
     }
-    if (!none && isnan(bad)) fine = false;
     if (partial) {
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
@@ -288,6 +369,11 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
       for (int s = 0; s < 4; ++s)
         if (to4[s]) *reinterpret_cast<uint4*>(to4[s] + c * 64) = u[s];
     }
+  }
+  {
+    float s0, s1;
+    unpack2(add2(sum[0], sum[1]), s0, s1);
+    if (!none && !isfinite(s0 + s1)) fine = false;
   }
   tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
   if (row_live) {
@@ -339,7 +425,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     prefetch_tmap(&maps.v);
     for (int n = 0; n < kBoard; ++n) {
       mbar_init(&ctl.u_full[n], 1);
-      mbar_init(&ctl.u_empty[n], 4 * NQ + 1);
+      mbar_init(&ctl.u_empty[n], 4 * NQ + 2);
     }
     mbar_init(&ctl.q_full, 1);
     mbar_init(&ctl.q_empty, 1);
@@ -473,23 +559,12 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         __syncwarp();
         return true;
       };
-      for (int k = 0; live; ++k) {
-        const int u = unit_index(k), slot = k % kBoard;
-        Unit<NQ> x;
-        x.g = -1;
-        if (u < n_units) {
-          x = unit_of<NQ>(a, plan, u);
-          if (lane == 0 && !x.s.ok) set_error(a.err, kErrBadDeviceArg);
-        }
-        x.load0 = idx;
-        live = warp_wait(&ctl.u_empty[slot], ((k / kBoard) & 1u) ^ 1u, a.err) && !ctl.fail;
-        live = __all_sync(0xffffffffu, live);
+      for (uint32_t n = 0; live; ++n) {
+        live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err);
         if (!live) break;
-        if (lane == 0) {
-          ctl.board[slot] = x;
-          mbar_arrive(&ctl.u_full[slot]);
-        }
+        const Unit<NQ> x = ctl.board[n % kBoard];
         __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
         if (x.g < 0) break;
         if (x.ntm == 0) continue;
         live = load(x, x.t_lo, false);
@@ -518,6 +593,37 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           live = load(x, x.t_lo + j, true);
           if (live && j + 1 < x.ntm) live = load(x, x.t_lo + j + 1, false);
         }
+      }
+      if (!live) ctl.fail = 1;
+    } else if (warp == 4 * NQ + 2) {
+      // ---- units of this CTA onto the board, ahead of those who work on them ----
+      Walk w;
+      if (!a.paged) {
+        w.b0 = w.g0 = w.base = 0;
+        walk_chunk<NQ>(a, plan, w);
+      }
+      uint32_t loads = 0;
+      bool live = true;
+      for (int k = 0; live; ++k) {
+        const int u = unit_index(k), slot = k % kBoard;
+        Unit<NQ> x;
+        bool more = u < n_units;  // (contiguous keys: at most)
+        if (more && a.paged) {
+          x = paged_unit<NQ>(a, plan, u);
+          if (lane == 0 && !x.s.ok) set_error(a.err, kErrBadDeviceArg);
+        } else if (more) {
+          more = walk_to<NQ>(a, plan, w, u, x);
+        }
+        if (!more) x.g = -1;
+        x.load0 = loads;
+        if (more) loads += 2 * x.ntm;
+        live = warp_wait(&ctl.u_empty[slot], ((k / kBoard) & 1u) ^ 1u, a.err);
+        if (live && lane == 0) {
+          ctl.board[slot] = x;
+          mbar_arrive(&ctl.u_full[slot]);
+        }
+        __syncwarp();
+        if (!more) break;
       }
       if (!live) ctl.fail = 1;
     }

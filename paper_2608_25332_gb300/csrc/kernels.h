@@ -322,9 +322,8 @@ cudaError_t attn_decode_simt_launch(const AttnArgs& a, int n_own, int dtype, cud
 // Tensor-core form (bf16): how the work is cut into units for its persistent CTAs.
 struct AttnPlan {
   int nq;                    // row tiles of 128 a CTA
-  long long n_units;
-  int n_blk;                 // prompt: row blocks of the longest sequence
-  int chunk;                 // prompt: (sequence, key/value head) pairs handled together
+  long long n_units;         // prompt: at most, by the host's bounds
+  int chunk_seqs, chunk_heads;  // prompt: sequences (256 at most) and heads handled together
   int n_own_parts, n_prefix_parts;  // paged: parts of a request's keys, of the prefix's
   int n_prefix_units;        // paged: units of the prefix, which come first
 };
