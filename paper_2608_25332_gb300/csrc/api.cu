@@ -1286,6 +1286,14 @@ size_t attn_ws(Carve& c, int n_part, int T_q, int H_q, float** part_o, float** p
   return c.off;
 }
 
+void attn_heads(AttnArgs& a, int H_q, int H_kv) {
+  a.H_q = H_q;
+  a.H_kv = H_kv;
+  a.group = H_q / H_kv;
+  a.tile_tokens = 128 / a.group;
+  a.group_inv = (65536 + a.group - 1) / a.group;
+}
+
 // a decode call's workspace
 size_t decode_ws(Carve& c, const AttnCut& cut, int B, int H_q, int H_kv, float** part_o, float** part_lse,
                  AttnSpans* sp) {
@@ -1407,8 +1415,7 @@ extern "C" int provip_prompt_attention(const void* Q, long long q_stride, const 
   a.T_q = T_q;
   a.T_k = T_k;
   a.B = B;
-  a.H_q = H_q;
-  a.H_kv = H_kv;
+  attn_heads(a, H_q, H_kv);
   a.q_start = q_start;
   a.q_len = q_len;
   a.k_start = k_start;
@@ -1481,8 +1488,7 @@ extern "C" int provip_decode_attention(const void* Q, long long q_stride, int B,
   a.o_stride = out_stride;
   a.T_q = B;
   a.B = B;
-  a.H_q = H_q;
-  a.H_kv = H_kv;
+  attn_heads(a, H_q, H_kv);
   a.k_len = kv_len;
   a.q_len_max = 1;
   a.k_len_max = kv_len_max;

@@ -117,7 +117,7 @@ __device__ __noinline__ void scale_o(uint32_t to, float f) {
 // the tiles of a unit whose sequence, head, part and first token are known
 template <int NQ>
 __device__ __forceinline__ void set_tiles(const AttnArgs& a, Unit<NQ>& x, int part, int n_parts) {
-  const int R = a.H_q / a.H_kv, TT = kT / R;
+  const int TT = a.tile_tokens;
   x.n_pt = (x.n_prefix + kT - 1) / kT;
   int most = 0, tiles[NQ];
 #pragma unroll
@@ -148,7 +148,7 @@ __device__ __forceinline__ Unit<NQ> paged_unit(const AttnArgs& a, const AttnPlan
     part = u % n_parts;
     u /= n_parts;
     x.g = u % a.H_kv;
-    x.tok0 = u / a.H_kv * NQ * (kT / (a.H_q / a.H_kv));
+    x.tok0 = u / a.H_kv * NQ * a.tile_tokens;
     x.part = p.n_own_parts + part;
     x.s.q0 = 0;
     x.s.q_len = a.B;
@@ -200,7 +200,7 @@ __device__ __forceinline__ void walk_level(const AttnArgs& a, Walk& w) {
 }
 template <int NQ>
 __device__ __forceinline__ void walk_chunk(const AttnArgs& a, const AttnPlan& p, Walk& w) {
-  const int lane = threadIdx.x & 31, rows = NQ * (kT / (a.H_q / a.H_kv));
+  const int lane = threadIdx.x & 31, rows = NQ * a.tile_tokens;
   w.n_seq = min(p.chunk_seqs, a.B - w.b0);
   w.n_g = min(p.chunk_heads, a.H_kv - w.g0);
 #pragma unroll
@@ -256,7 +256,7 @@ __device__ __forceinline__ bool walk_to(const AttnArgs& a, const AttnPlan& p, Wa
   x.s = attn_seq(a, b);
   x.n_prefix = a.prefix_len;
   x.part = part;
-  x.tok0 = (nb - 1 - w.level) * NQ * (kT / (a.H_q / a.H_kv));
+  x.tok0 = (nb - 1 - w.level) * NQ * a.tile_tokens;
   set_tiles(a, x, part, a.n_part);
   return true;
 }
@@ -274,115 +274,91 @@ __device__ __forceinline__ int unit_index(int k) {
   return k * G + ((k & 1) ? G - 1 - i : i);
 }
 
-// Four lanes hold a 64-byte run of a row each (four 16-byte pieces); afterwards lane q of the
-// four holds piece q of all four rows, so that a store covers whole runs.
-__device__ __forceinline__ uint4 shfl_xor4(uint4 v, int m) {
-  v.x = __shfl_xor_sync(0xffffffffu, v.x, m);
-  v.y = __shfl_xor_sync(0xffffffffu, v.y, m);
-  v.z = __shfl_xor_sync(0xffffffffu, v.z, m);
-  v.w = __shfl_xor_sync(0xffffffffu, v.w, m);
-  return v;
-}
-__device__ __forceinline__ void transpose4(uint4* u) {
-  const bool b0 = threadIdx.x & 1, b1 = threadIdx.x & 2;
-#pragma unroll
-  for (int k = 0; k < 4; k += 2) {
-    const uint4 got = shfl_xor4(b0 ? u[k] : u[k + 1], 1);
-    if (b0) u[k] = got; else u[k + 1] = got;
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const uint4 got = shfl_xor4(b1 ? u[k] : u[k + 2], 2);
-    if (b1) u[k] = got; else u[k + 2] = got;
+// 32 bytes of a thread's row: one store where the rows allow it
+__device__ __forceinline__ void store32(char* p, const uint32_t* r, bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
   }
 }
 
 // O / l of a thread's row, its log-sum-exp: to memory, as the result or as a part. Kept out
-// of line: its addresses would cost the tile loop registers. Stored 16 bytes a lane along
-// the lanes' own rows, the 32 lines of every store took the SM's load/store unit 4000 clocks a
-// unit; with the pieces of four lanes exchanged it is a quarter.
+// of line: its addresses would cost the tile loop registers. Bound by the instructions of a
+// single warp a scheduler; stores of whole 32-byte sectors need no exchange between lanes.
 template <int NQ>
-__device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, int i, int hid, float m, float l,
-                                         uint32_t to) {
+__device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, int i, int tok_in, int hid, float m,
+                                         float l, uint32_t to) {
   const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
-  const int R = a.H_q / a.H_kv, TT = kT / R, tok_in = r / R, hd = r - tok_in * R;
+  const int R = a.group, hd = r - tok_in * R;
   const int nt = x.nt[i];
   const bool row_live = tok_in < x.n_tok[i];
-  const int h = x.g * R + hd, tok = x.tok0 + i * TT + tok_in;
+  const int h = x.g * R + hd, tok = x.tok0 + i * a.tile_tokens + tok_in;
   const size_t n_rows = (size_t)a.T_q * a.H_q, row = (size_t)(x.s.q0 + tok) * a.H_q + h;
   const bool partial = a.n_part > 1;
-  const bool none = l == 0.f;
-  // a row whose keys all score -inf is 0 / 0; a row without keys is 0
+  // the part's keys of the list that this row sees
   const int lo = list_key(x, x.t_lo), hi = min(list_key(x, x.t_lo + nt), x.n_prefix + x.s.k_len - hid);
-  const float nil = !partial && hi > lo ? NAN : 0.f;
-  const float inv = none ? 0.f : 1.f / l;
-  const float lse = none ? (nil == 0.f ? -INFINITY : NAN) : m + lg2_approx(l);
-  bool fine = !isnan(l);
+  const float inv = 1.f / l, lse = m + lg2_approx(l);
   char* dst = partial ? reinterpret_cast<char*>(a.part_o + ((size_t)x.part * n_rows + row) * kHeadDim)
                       : reinterpret_cast<char*>(static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tok) * a.o_stride +
                                                 (size_t)h * kHeadDim);
-  if (!row_live) dst = nullptr;
-  char* to4[4];  // where this lane's piece of the four rows goes
-#pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const unsigned long long d =
-        __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), (lane & ~3) + s);
-    to4[s] = d ? reinterpret_cast<char*>(d) + (lane & 3) * 16 : nullptr;
-  }
-  const uint64_t inv2 = pack2(inv, inv), nil2 = pack2(nil, nil);
-  uint64_t sum[2] = {0, 0};
-  // (unrolled, this code is fetched once a unit and its misses cost more than the loop)
+  const bool wide = !__any_sync(0xffffffffu, (reinterpret_cast<uintptr_t>(dst) & 31u) != 0);
+  float sum = 0.f;
+  if (nt == 0) {
+    // no keys at all for the tile (in this part)
+    if (row_live) {
+      const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      for (int e = 0; e < kHeadDim * (partial ? 4 : 2); e += 32) store32(dst + e, zero, wide);
+      if (partial)
+        a.part_lse[(size_t)x.part * n_rows + row] = -INFINITY;
+      else if (a.lse)
+        a.lse[row] = -INFINITY;
+    }
+    return;
+  } else {
+    const uint64_t inv2 = pack2(inv, inv);
+    uint64_t s2[2] = {0, 0};
 #pragma unroll 1
-  for (int c = 0; c < 4; ++c) {
-    float o[32];
-    if (nt > 0) {
-      tmem_ld32(to + c * 32, o);
+    for (int c = 0; c < 2; ++c) {
+      float o[64];
+      tmem_ld64(to + c * 64, o);
       tc_wait_ld();
-    }
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      const uint64_t v = none ? nil2 : fma2(pack2(o[e], o[e + 1]), inv2, 0);
-      sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], v);  // not finite once an element is not
-      unpack2(v, o[e], o[e + 1]);
-    }
-    if (partial) {
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        uint4 u[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          u[k] = make_uint4(__float_as_uint(o[z * 16 + k * 4]), __float_as_uint(o[z * 16 + k * 4 + 1]),
-                            __float_as_uint(o[z * 16 + k * 4 + 2]), __float_as_uint(o[z * 16 + k * 4 + 3]));
-        transpose4(u);
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-          if (to4[s]) *reinterpret_cast<uint4*>(to4[s] + c * 128 + z * 64) = u[s];
+      for (int e = 0; e < 64; e += 2) {
+        const uint64_t v = fma2(pack2(o[e], o[e + 1]), inv2, 0);
+        s2[(e >> 1) & 1] = add2(s2[(e >> 1) & 1], v);  // not finite once an element is not
+        unpack2(v, o[e], o[e + 1]);
       }
-    } else {
-      uint4 u[4];
+      if (!row_live) continue;
+      if (partial) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        u[k] = make_uint4(pack_bf16(o[k * 8], o[k * 8 + 1]), pack_bf16(o[k * 8 + 2], o[k * 8 + 3]),
-                          pack_bf16(o[k * 8 + 4], o[k * 8 + 5]), pack_bf16(o[k * 8 + 6], o[k * 8 + 7]));
-      transpose4(u);
+        for (int e = 0; e < 64; e += 8) store32(dst + (c * 64 + e) * 4, reinterpret_cast<const uint32_t*>(o) + e, wide);
+      } else {
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        if (to4[s]) *reinterpret_cast<uint4*>(to4[s] + c * 64) = u[s];
+        for (int e = 0; e < 64; e += 16) {
+          uint32_t w[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) w[k] = pack_bf16(o[e + 2 * k], o[e + 2 * k + 1]);
+          store32(dst + (c * 64 + e) * 2, w, wide);
+        }
+      }
     }
-  }
-  {
     float s0, s1;
-    unpack2(add2(sum[0], sum[1]), s0, s1);
-    if (!none && !isfinite(s0 + s1)) fine = false;
+    unpack2(add2(s2[0], s2[1]), s0, s1);
+    sum = s0 + s1;
   }
   tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
-  if (row_live) {
+  const bool fine = l != 0.f && isfinite(sum) && isfinite(lse);
+  if (row_live && fine) {
     if (partial)
       a.part_lse[(size_t)x.part * n_rows + row] = lse;
     else if (a.lse)
       a.lse[row] = lse * kLn2;
   }
-  // rows that are not finite: again by the definition (past the other lanes' stores to them)
+  // rows that are not finite or have no weight: again by the definition
   __syncwarp();
   unsigned again = __ballot_sync(0xffffffffu, row_live && !fine);
   while (again) {
@@ -397,7 +373,8 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
       store4(a.part_o + ((size_t)x.part * n_rows + rw) * kHeadDim + lane * 4, o);
       if (lane == 0) a.part_lse[(size_t)x.part * n_rows + rw] = le;
     } else {
-      if (le == -INFINITY) le = o[0] = o[1] = o[2] = o[3] = NAN;
+      // every score is -inf: 0 / 0, as the formula has it (a row without keys is 0)
+      if (le == -INFINITY && khi > lo) le = o[0] = o[1] = o[2] = o[3] = NAN;
       store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)(x.s.q0 + tk) * a.o_stride + (size_t)hh * kHeadDim + lane * 4, o);
       if (lane == 0 && a.lse) a.lse[rw] = le * kLn2;
     }
@@ -415,7 +392,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
   extern __shared__ uint8_t smem_raw[];
   __shared__ Ctl<NQ> ctl;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int R = a.H_q / a.H_kv, TT = kT / R;
+  const int R = a.group, TT = a.tile_tokens;
   const uint32_t base = smem_u32(smem_raw);
   uint8_t* qs = smem_raw + (((base + 1023u) & ~1023u) - base);
   uint8_t* kv = qs + NQ * kStage;
@@ -632,7 +609,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kSoftRegs));
     const int i = NQ == 2 ? warp >> 2 : 0, r = (warp & 3) * 32 + lane;
     const uint32_t ts = tmem + i * kT + ((uint32_t)(r & ~31) << 16), to = ts + NQ * kT;
-    const int tok_in = r / R, tok_first = (r & ~31) / R;
+    const int tok_in = (r * a.group_inv) >> 16, tok_first = ((r & ~31) * a.group_inv) >> 16;  // / R
     const float sc = a.scale_log2;
     uint32_t n_s = 0, n_o = 0;
     bool failed = false;
@@ -688,10 +665,12 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
               const float mn = fmaxf(m, ceilf(max128(v) * sc));  // sc > 0: the maximum commutes with it
               const float f = m == mn ? 1.f : ex2_int(m - mn);
               m = mn;
-              l *= f;
-              if (j > 0) scale_o(to, f);
-              raise = false;
-              continue;
+              if (j > 0) {
+                l *= f;
+                scale_o(to, f);
+                raise = false;
+                continue;  // the scores are read again rather than kept over the call
+              }
             }
             const float mb = m == -INFINITY ? 0.f : m;
             const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
@@ -730,7 +709,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         if (failed) break;
         tc_fence_after();
       }
-      if (warp_live) finish_rows<NQ>(a, x, i, hid, m, l, to);
+      if (warp_live) finish_rows<NQ>(a, x, i, tok_in, hid, m, l, to);
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
     }

@@ -294,6 +294,8 @@ struct AttnArgs {
   const void* Vp;
   long long q_stride, k_stride, v_stride, kp_stride, vp_stride, o_stride;
   int T_q, T_k, B, H_q, H_kv;
+  int group, tile_tokens;    // query heads a key/value head; tokens of a tile of 128 packed rows
+  int group_inv;             // 65536 / group, rounded up: x / group = x * group_inv >> 16 for x < 128
   const int* q_start;        // contiguous keys: [B] first token and tokens of each sequence,
   const int* q_len;          // first own key row and own keys
   const int* k_start;
