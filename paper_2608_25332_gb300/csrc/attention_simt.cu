@@ -10,22 +10,44 @@ namespace {
 //
 // A CTA holds 64 packed rows of a key/value head (Q in shared memory as fp32, 8 rows of
 // scores and of the output in each thread's registers) and passes over its keys once in
-// tiles of 64 with a running maximum and sum. Bound by the FFMA pipe: a thread's 8 x 4
-// scores take 12 16-byte loads from shared memory per 128 FFMA, its 8 x 8 outputs 16 per 256.
+// tiles of 64 with a running maximum and sum. Bound by the FFMA pipe: pairs of products in one
+// instruction, a thread's 8 x 4 scores take 12 16-byte loads from shared memory per 64 of
+// them, its 8 x 8 outputs 16 per 128. P takes the place of the keys it came from, so that two
+// CTAs fit an SM and one multiplies while the other waits for its next tile (cp.async).
 // ---------------------------------------------------------------------------
 constexpr int kBM = 64, kBN = 64, kThr = 128;
-constexpr int kPitch = kHeadDim + 4;  // floats a row: rows 4 banks apart, 16 bytes aligned
+constexpr int kPitch = kHeadDim + 4;  // floats a row of Q and K: rows 4 banks apart, 16 bytes aligned
+constexpr int kVPitch = kHeadDim;     // V is read along its rows
 constexpr int kPPitch = kBN + 4;
-constexpr size_t kTileSmem = sizeof(float) * ((size_t)(kBM + 2 * kBN) * kPitch + (size_t)kBM * kPPitch);
+constexpr size_t kTileSmem = sizeof(float) * ((size_t)(kBM + kBN) * kPitch + (size_t)kBN * kVPitch);
+static_assert(kBM * kPPitch <= kBN * kPitch, "P fits in the place of K");
 
-template <typename T>
-__device__ __forceinline__ void fill_row(float* dst, const T* src, int lane32) {
-  float v[4];
-  load4(src + lane32 * 4, v);
-  *reinterpret_cast<float4*>(dst + lane32 * 4) = make_float4(v[0], v[1], v[2], v[3]);
+// four elements of a row; zeros for a null source
+__device__ __forceinline__ void fill4(float* dst, const float* src, bool have) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(have ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void zero_row(float* dst, int lane32) {
-  *reinterpret_cast<float4*>(dst + lane32 * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+__device__ __forceinline__ void fill4(float* dst, const __nv_bfloat16* src, bool have) {
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (have) load4(src, v);
+  *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void fill_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void fill_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
 }
 
 // blockIdx: x row tile, y = key/value head * parts + part, z sequence. PREFIX: the rows of
@@ -35,8 +57,8 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
   extern __shared__ __align__(16) float sm[];
   float* qs = sm;
   float* ks = qs + kBM * kPitch;
+  float* ps = ks;
   float* vs = ks + kBN * kPitch;
-  float* ps = vs + kBN * kPitch;
   const int R = a.H_q / a.H_kv, g = blockIdx.y / n_parts, part = blockIdx.y % n_parts, b = blockIdx.z;
   AttnSeq s;
   if (PREFIX) {
@@ -61,13 +83,27 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;  // rows ty*8.., columns tx + 16 j / 4 tx..
 
-  for (int r = warp; r < kBM; r += kThr / 32) {
-    if (r < rows) {
-      const int t = (r0 + r) / R, h = g * R + (r0 + r) % R;
-      fill_row(qs + r * kPitch, static_cast<const T*>(a.Q) + (size_t)(s.q0 + t) * a.q_stride + (size_t)h * kHeadDim, lane);
-    } else {
-      zero_row(qs + r * kPitch, lane);
+  // keys k0 .. k0 + 63 of the list (past k_hi: zeros) to dst
+  auto fill = [&](float* dst, int pitch, int k0, bool v) {
+#pragma unroll 4
+    for (int j = warp; j < kBN; j += kThr / 32) {
+      const int key = k0 + j;
+      const bool have = key < k_hi, pre = key < P;
+      const T* src = static_cast<const T*>(v ? a.V : a.K);
+      if (have) src = pre ? attn_prefix_row<T>(a, v, key, g) : attn_own_row<T>(a, s, v, key - P, g);
+      fill4(dst + j * pitch + lane * 4, src + (have ? lane * 4 : 0), have);
     }
+    fill_commit();
+  };
+  for (int r = warp; r < kBM; r += kThr / 32) {
+    const bool have = r < rows;
+    const int t = have ? (r0 + r) / R : 0, h = g * R + (have ? (r0 + r) % R : 0);
+    fill4(qs + r * kPitch + lane * 4, static_cast<const T*>(a.Q) + (size_t)(s.q0 + t) * a.q_stride + (size_t)h * kHeadDim + lane * 4,
+          have);
+  }
+  if (k_lo < k_hi) {
+    fill(ks, kPitch, k_lo, false);  // (with Q)
+    fill(vs, kVPitch, k_lo, true);
   }
   int lim[8];  // keys of the list that each row sees
 #pragma unroll
@@ -75,46 +111,45 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
     const int r = r0 + ty * 8 + i;
     lim[i] = r < n_rows ? P + (PREFIX ? 0 : attn_visible(a, s.q_len, s.k_len, r / R)) : 0;
   }
-  float o[8][8], m[8], l[8];
+  uint64_t o2[8][4];
+  float m[8], l[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[i][j] = 0.f;
+    for (int j = 0; j < 4; ++j) o2[i][j] = 0;
   }
   for (int k0 = k_lo; k0 < k_hi; k0 += kBN) {
-    __syncthreads();
-    for (int j = warp; j < kBN; j += kThr / 32) {
-      const int key = k0 + j;
-      if (key < k_hi) {
-        const bool pre = key < P;
-        fill_row(ks + j * kPitch, pre ? attn_prefix_row<T>(a, false, key, g) : attn_own_row<T>(a, s, false, key - P, g), lane);
-        fill_row(vs + j * kPitch, pre ? attn_prefix_row<T>(a, true, key, g) : attn_own_row<T>(a, s, true, key - P, g), lane);
-      } else {
-        zero_row(ks + j * kPitch, lane);
-        zero_row(vs + j * kPitch, lane);
+    fill_wait<1>();
+    __syncthreads();  // K is there
+    uint64_t x2[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x2[i][j] = 0;
+#pragma unroll 2
+    for (int d = 0; d < kHeadDim; d += 4) {
+      ulonglong2 kv[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * j) * kPitch + d);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const ulonglong2 qv = *reinterpret_cast<const ulonglong2*>(qs + (ty * 8 + i) * kPitch + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x2[i][j] = fma_pair(qv.y, kv[j].y, fma_pair(qv.x, kv[j].x, x2[i][j]));
       }
     }
-    __syncthreads();
     float x[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
-#pragma unroll 2
-    for (int d = 0; d < kHeadDim; d += 4) {
-      float4 kv[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(ks + (tx + 16 * j) * kPitch + d);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 qv = *reinterpret_cast<const float4*>(qs + (ty * 8 + i) * kPitch + d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          x[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, x[i][j]))));
+      for (int j = 0; j < 4; ++j) {
+        float e, f;
+        unpair(x2[i][j], e, f);
+        x[i][j] = e + f;
       }
-    }
+    __syncthreads();  // K is read: P takes its place
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float mx = -INFINITY;
@@ -136,10 +171,12 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
         ps[(ty * 8 + i) * kPPitch + tx + 16 * j] = p;
       }
       l[i] = l[i] * r + t;
+      const uint64_t r2 = pair(r, r);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[i][j] *= r;
+      for (int j = 0; j < 4; ++j) o2[i][j] = fma_pair(o2[i][j], r2, 0);
     }
-    __syncwarp();  // a row's probabilities are written and read by the same 16 lanes
+    fill_wait<0>();
+    __syncthreads();  // V is there (and a row's probabilities, written and read by the same 16 lanes)
 #pragma unroll 1
     for (int k = 0; k < kBN; k += 4) {
       float4 p[8];
@@ -147,24 +184,26 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       for (int i = 0; i < 8; ++i) p[i] = *reinterpret_cast<const float4*>(ps + (ty * 8 + i) * kPPitch + k);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const float4 v0 = *reinterpret_cast<const float4*>(vs + (k + kk) * kPitch + tx * 4);
-        const float4 v1 = *reinterpret_cast<const float4*>(vs + (k + kk) * kPitch + 64 + tx * 4);
+        const ulonglong2 v0 = *reinterpret_cast<const ulonglong2*>(vs + (k + kk) * kVPitch + tx * 4);
+        const ulonglong2 v1 = *reinterpret_cast<const ulonglong2*>(vs + (k + kk) * kVPitch + 64 + tx * 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float w = kk == 0 ? p[i].x : kk == 1 ? p[i].y : kk == 2 ? p[i].z : p[i].w;
-          o[i][0] = fmaf(w, v0.x, o[i][0]);
-          o[i][1] = fmaf(w, v0.y, o[i][1]);
-          o[i][2] = fmaf(w, v0.z, o[i][2]);
-          o[i][3] = fmaf(w, v0.w, o[i][3]);
-          o[i][4] = fmaf(w, v1.x, o[i][4]);
-          o[i][5] = fmaf(w, v1.y, o[i][5]);
-          o[i][6] = fmaf(w, v1.z, o[i][6]);
-          o[i][7] = fmaf(w, v1.w, o[i][7]);
+          const uint64_t w2 = pair(w, w);
+          o2[i][0] = fma_pair(w2, v0.x, o2[i][0]);
+          o2[i][1] = fma_pair(w2, v0.y, o2[i][1]);
+          o2[i][2] = fma_pair(w2, v1.x, o2[i][2]);
+          o2[i][3] = fma_pair(w2, v1.y, o2[i][3]);
         }
       }
     }
-    __syncwarp();
+    __syncthreads();  // P and V are read
+    if (k0 + kBN < k_hi) {
+      fill(ks, kPitch, k0 + kBN, false);
+      fill(vs, kVPitch, k0 + kBN, true);
+    }
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");  // a part without keys leaves Q's copies under way
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
 #pragma unroll
@@ -175,27 +214,30 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
     const size_t row = (size_t)(s.q0 + t) * a.H_q + h;
     bool fine = true;
     const float den = l[i] == 0.f ? 1.f : l[i];
+    float o[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpair(o2[i][j], o[2 * j], o[2 * j + 1]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      o[i][j] /= den;
-      fine = fine && isfinite(o[i][j]);
+      o[j] /= den;
+      fine = fine && isfinite(o[j]);
     }
     float lse = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
     if (live && fine && !isnan(lse)) {
       if (a.n_part > 1) {
         float* po = a.part_o + ((size_t)(part0 + part) * a.T_q * a.H_q + row) * kHeadDim;
-        store4(po + tx * 4, o[i]);
-        store4(po + 64 + tx * 4, o[i] + 4);
+        store4(po + tx * 4, o);
+        store4(po + 64 + tx * 4, o + 4);
         if (tx == 0) a.part_lse[(size_t)(part0 + part) * a.T_q * a.H_q + row] = lse;
       } else {
         if (l[i] == 0.f && lim[i] > 0) {
           lse = NAN;  // every score is -inf: 0 / 0, as the formula has it
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[i][j] = NAN;
+          for (int j = 0; j < 8; ++j) o[j] = NAN;
         }
         T* op = static_cast<T*>(a.out) + (size_t)(s.q0 + t) * a.o_stride + (size_t)h * kHeadDim;
-        store4(op + tx * 4, o[i]);
-        store4(op + 64 + tx * 4, o[i] + 4);
+        store4(op + tx * 4, o);
+        store4(op + 64 + tx * 4, o + 4);
         if (tx == 0 && a.lse) a.lse[row] = lse * kLn2;
       }
     }
