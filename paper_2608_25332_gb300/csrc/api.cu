@@ -1192,7 +1192,7 @@ struct AttnCut {
   bool by_unit;                 // a unit each
 };
 
-// CUDA cores: row tiles of 64 packed rows, parts of four 64-key tiles or more. Tensor cores:
+// CUDA cores: row tiles of 64 packed rows, parts of two 64-key tiles or more. Tensor cores:
 // two row tiles of 128 a CTA, one where a sequence's rows fit in it (two CTAs then share an
 // SM); the keys are shared out where the units leave half of the CTAs without work, four
 // 128-key tiles or more a part (a second launch joins the parts, about two tiles' time).
@@ -1204,7 +1204,7 @@ AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int p
   c.tc = attn_tc_form(algo, dtype);
   if (!c.tc) {
     const long long tiles = ((long long)q_len_max * R + 63) / 64;
-    c.n_part = attn_parts(tiles * H_kv * B, keys, 2 * kPlanSms, 256, 32);
+    c.n_part = attn_parts(tiles * H_kv * B, keys, 3 * kPlanSms, 128, 32);
     if (c.n_part < 1) c.n_part = 1;
     return c;
   }

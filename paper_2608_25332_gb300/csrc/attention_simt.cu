@@ -83,15 +83,27 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;  // rows ty*8.., columns tx + 16 j / 4 tx..
 
-  // keys k0 .. k0 + 63 of the list (past k_hi: zeros) to dst
+  // Keys k0 .. k0 + 63 of the list (past k_hi: zeros) to dst, from this lane's column of the
+  // prefix's and the own rows (a key of the list is added to either base; worked out per row, the
+  // addresses had cost as much as a third of the products).
+  const size_t col = (size_t)g * kHeadDim + lane * 4;
+  const T *k_pre = static_cast<const T*>(a.Kp) + col, *v_pre = static_cast<const T*>(a.Vp) + col;
+  const T* k_own = static_cast<const T*>(a.K) + col + (s.k0 - P) * a.k_stride;
+  const T* v_own = static_cast<const T*>(a.V) + col + (s.k0 - P) * a.v_stride;
   auto fill = [&](float* dst, int pitch, int k0, bool v) {
+    const T *pre = v ? v_pre : k_pre, *own = v ? v_own : k_own;
+    const long long sp = v ? a.vp_stride : a.kp_stride, so = v ? a.v_stride : a.k_stride;
 #pragma unroll 4
     for (int j = warp; j < kBN; j += kThr / 32) {
       const int key = k0 + j;
-      const bool have = key < k_hi, pre = key < P;
-      const T* src = static_cast<const T*>(v ? a.V : a.K);
-      if (have) src = pre ? attn_prefix_row<T>(a, v, key, g) : attn_own_row<T>(a, s, v, key - P, g);
-      fill4(dst + j * pitch + lane * 4, src + (have ? lane * 4 : 0), have);
+      const bool have = key < k_hi;
+      const T* src = pre;
+      if (PREFIX) {
+        if (have) src = pre + attn_slot(a, a.prefix_table, key) * sp;
+      } else if (have) {
+        src = key < P ? pre + key * sp : own + key * so;
+      }
+      fill4(dst + j * pitch + lane * 4, have ? src : static_cast<const T*>(a.Q), have);
     }
     fill_commit();
   };

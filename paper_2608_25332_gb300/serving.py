@@ -1,0 +1,104 @@
+"""Questions about one pruned image or video, from the pruning step to the answers.
+
+After the pruning layers a sample's sequence is [system rows | kept visual rows | text]. Where
+several questions are asked about the same image or video, the system and visual rows are
+the same for all of them: their keys and values are computed, pruned and stored once, and
+every question's prompt and every decoded token attends over them and over its own rows.
+
+``QuestionCache`` keeps that state for the LLM layers behind the pruning: one paged pool of
+key/value rows per layer, one set of block tables for all layers. The LLM itself is the
+caller's: it hands each layer's queries, keys and values in and gets the attention's output
+back. All calls enqueue on the current stream; nothing synchronises with the host.
+
+    cache = QuestionCache(layers, B, H_q, H_kv, page_size, n_pages, max_len, dtype)
+    cache.set_prefix(K, V)                # per layer: rows of a compaction, system + visual
+    cache.begin(new_len)                  # prompts: the questions' lengths, 0 for an idle slot
+    for each layer: out = cache.prompt(layer, Q, K, V)      # packed rows of all questions
+    while ...:
+        cache.begin(ones)                 # 1: one more token, -1: the question is answered
+        for each layer: out = cache.decode(layer, Q, K, V)  # one row per request
+"""
+from __future__ import annotations
+
+import torch
+
+from . import provip as P
+
+
+class QuestionCache:
+    """Paged keys and values of B concurrent questions over one shared prefix.
+
+    layers: LLM layers behind the pruning; n_pages pages of page_size rows per layer, for the
+    prefix and the questions; max_len: own tokens of a question at most (prompt and answer);
+    max_new: new tokens of one step over all questions at most (default B * max_len).
+    """
+
+    def __init__(self, layers, B, H_q, H_kv, page_size, n_pages, max_len, dtype=torch.bfloat16, device="cuda",
+                 max_new=None, algo=P.ALGO_AUTO):
+        dev = torch.device(device)
+        self.B, self.H_q, self.H_kv, self.page_size, self.max_len = int(B), int(H_q), int(H_kv), int(page_size), int(max_len)
+        self.dtype, self.device, self.algo = dtype, dev, algo
+        self.pools = [tuple(torch.zeros(n_pages, page_size, H_kv, 128, dtype=dtype, device=dev) for _ in range(2))
+                      for _ in range(layers)]
+        self.free = torch.arange(n_pages, dtype=torch.int32, device=dev)
+        self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=dev)
+        self.tables = torch.zeros(B, -(-max_len // page_size), dtype=torch.int32, device=dev)
+        self.kv_len = torch.zeros(B, dtype=torch.int32, device=dev)
+        self.planner = P.PageTables(B, page_size, B * max_len if max_new is None else max_new, dev)
+        self.prefix, self.prefix_len, self.prefix_table = [], 0, None
+        self.plan = None
+        self._steps = {}
+
+    def set_prefix(self, K, V):
+        """K, V: a [n, H_kv, 128] tensor per layer (for instance rows [:vis_start + keep] of a
+        compaction's K_out[b] and V_out[b]). Their pages come off the free stack and stay."""
+        n = K[0].shape[0]
+        need = -(-n // self.page_size)
+        one = P.PageTables(1, self.page_size, n, self.device)
+        table = torch.zeros(1, need, dtype=torch.int32, device=self.device)
+        zero = torch.zeros(1, dtype=torch.int32, device=self.device)
+        plan = one(zero, torch.full_like(zero, n), self.free, self.n_free, table)
+        self.n_free.copy_(plan["free_count"])
+        for (kp, vp), k, v in zip(self.pools, K, V):
+            P.provip_kv_append(k, v, plan["slot_map"], kp, vp)
+        self.prefix, self.prefix_len, self.prefix_table = list(zip(K, V)), n, table[0]
+        self._steps.clear()
+
+    def begin(self, new_len):
+        """The next step's new tokens per question (int32 [B] on the device): pages and slots for
+        them; -1 returns an answered question's pages (its slot can take another question).
+        A question that the free pages do not suffice for keeps its length: read kv_len where
+        that can happen."""
+        self.new_len = new_len
+        self.plan = self.planner(self.kv_len, new_len, self.free, self.n_free, self.tables, inplace=True)
+        return self.plan
+
+    def prompt(self, layer, Q, K, V, max_rows=None):
+        """Prompts of the step begun: the questions' rows packed in request order, Q [T, H_q, 128],
+        K and V [T, H_kv, 128] (T >= the step's new tokens). Every row sees the prefix and the
+        rows of its question up to itself. max_rows: the longest question (default max_len)."""
+        T, longest = Q.shape[0], min(self.max_len, Q.shape[0]) if max_rows is None else int(max_rows)
+        key = ("prompt", T, longest)
+        step = self._steps.get(key)
+        if step is None:
+            step = self._steps[key] = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len,
+                                                        True, None, self.dtype, self.device, self.algo, want_lse=False)
+        start, n = self.plan["row_start"], self.new_len.clamp(min=0)
+        kp, vp = self.pools[layer]
+        P.provip_kv_append(K, V, self.plan["slot_map"][:T], kp, vp)
+        pre = self.prefix[layer] if self.prefix_len else (None, None)
+        return step(Q, K, V, start, n, start, n, *pre)["out"]
+
+    def decode(self, layer, Q, K, V):
+        """One token per question: Q [B, H_q, 128], K and V [B, H_kv, 128] in request order, all of
+        the step's new lengths 1 (or -1, whose rows are skipped: their output is that of an empty
+        question)."""
+        step = self._steps.get("decode")
+        if step is None:
+            step = self._steps["decode"] = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len,
+                                                             None, self.dtype, self.device, self.algo, want_lse=False)
+        kp, vp = self.pools[layer]
+        # packed rows skip the ended questions; request b's token is row row_start[b]
+        slots = torch.where(self.new_len > 0, self.plan["slot_map"][:self.B][self.plan["row_start"][:-1].clamp(max=self.B - 1)], -1)
+        P.provip_kv_append(K, V, slots, kp, vp)
+        return step(Q, kp, vp, self.tables, self.kv_len, self.prefix_table if self.prefix_len else None)["out"]
