@@ -61,16 +61,20 @@ struct Unit {
   int t_lo;          // the unit's first tile of the list
   int nt[NQ];        // tiles of each row tile
   int ntm;           // the most of them
-  uint32_t load0;    // number of its first K load
+  uint32_t load0, step0;  // numbers of its first K load and of its first step
 };
 constexpr int kBoard = 4;
+// The MMAs' step j of a unit multiplies P of tile j - 1 with V and Q with K of tile j: the two
+// loads it needs share a barrier, and so do the two stages it hands back. (A step has one load
+// at least, so the producer is at most a ring of stages, five, ahead.)
+constexpr int kSteps = 8;
 
 template <int NQ>
 struct Ctl {
   Unit<NQ> board[kBoard];
   uint64_t u_full[kBoard], u_empty[kBoard];
   uint64_t q_full, q_empty;
-  uint64_t kv_full[Form<NQ>::kStages], kv_empty[Form<NQ>::kStages];
+  uint64_t full[kSteps], empty[kSteps];
   uint64_t s_full[NQ], p_full[NQ], o_full[NQ];
   uint32_t tmem;
   volatile int fail;
@@ -406,9 +410,9 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     }
     mbar_init(&ctl.q_full, 1);
     mbar_init(&ctl.q_empty, 1);
-    for (int s = 0; s < F::kStages; ++s) {
-      mbar_init(&ctl.kv_full[s], 1);
-      mbar_init(&ctl.kv_empty[s], 1);
+    for (int s = 0; s < kSteps; ++s) {
+      mbar_init(&ctl.full[s], 1);
+      mbar_init(&ctl.empty[s], 1);
     }
     for (int i = 0; i < NQ; ++i) {
       mbar_init(&ctl.s_full[i], 1);
@@ -435,17 +439,11 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       const bool lead = elect_one();
       const uint64_t qd = smem_desc_sw128(smem_u32(qs));
       const uint64_t kd0 = smem_desc_sw128(smem_u32(kv)), vd0 = smem_desc_mn_sw128(smem_u32(kv));
-      // loads come in the order K_0 V_0 K_1 V_1 ..: stage and phase of the next K and of the next V
-      uint32_t sk = 0, pk = 0, sv = 1, pv = 0, pq = 0, pp[NQ];
+      // loads come in the order K_0 V_0 K_1 V_1 ..: stages of the next K and of the next V
+      uint32_t sk = 0, sv = 1, step = 0, pq = 0, pp[NQ];
 #pragma unroll
       for (int i = 0; i < NQ; ++i) pp[i] = 0;
-      auto two_on = [](uint32_t& st, uint32_t& ph) {
-        st += 2;
-        if (st >= F::kStages) {
-          st -= F::kStages;
-          ph ^= 1u;
-        }
-      };
+      auto two_on = [](uint32_t& st) { st = st + 2 < F::kStages ? st + 2 : st + 2 - F::kStages; };
       bool live = true;
       for (uint32_t n = 0; live; ++n) {
         live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err);
@@ -460,9 +458,9 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         if (ntm == 0) continue;
         live = warp_wait(&ctl.q_full, pq, a.err);
         pq ^= 1u;
-        for (int j = 0; live && j <= ntm; ++j) {
+        for (int j = 0; live && j <= ntm; ++j, ++step) {
+          live = warp_wait(&ctl.full[step % kSteps], (step / kSteps) & 1u, a.err);
           const uint64_t kd = kd0 + (uint64_t)(sk * (kStage >> 4)), vd = vd0 + (uint64_t)(sv * (kStage >> 4));
-          if (j > 0) live = warp_wait(&ctl.kv_full[sv], pv, a.err);
 #pragma unroll
           for (int i = 0; i < NQ; ++i) {
             const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
@@ -478,7 +476,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
                 if (j == nt[i]) tc_commit(&ctl.o_full[i]);
               }
             }
-            if (i == 0 && j < ntm && live) live = warp_wait(&ctl.kv_full[sk], pk, a.err);
             if (j < nt[i]) {
               tc_fence_after();
               if (lead) {
@@ -492,39 +489,48 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
             }
           }
           if (lead) {
-            if (j > 0) tc_commit(&ctl.kv_empty[sv]);
-            if (j < ntm) tc_commit(&ctl.kv_empty[sk]);
+            tc_commit(&ctl.empty[step % kSteps]);
             if (j == ntm - 1) tc_commit(&ctl.q_empty);
           }
-          if (j > 0) two_on(sv, pv);
-          if (j < ntm) two_on(sk, pk);
+          if (j > 0) two_on(sv);
+          if (j < ntm) two_on(sk);
         }
       }
       if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 1) {
       // ---- TMA producer (the lanes share a tile's pages) ----
-      uint32_t n_q = 0, idx = 0;
+      uint32_t n_q = 0, st = 0, step = 0;
+      uint32_t user[F::kStages];  // the step that the stage's tile is for, and one more
+#pragma unroll
+      for (int i = 0; i < F::kStages; ++i) user[i] = 0;
       bool live = true;
       const int box = a.paged ? min(a.page_size, kT) : kT;
-      // one tile of the list, K or V, into the next stage
+      auto bytes_of = [&](const Unit<NQ>& x, int t) {
+        if (!a.paged) return kStage;
+        const int n = min(kT, t < x.n_pt ? x.n_prefix - t * kT : x.s.k_len - (t - x.n_pt) * kT);
+        return (n + box - 1) / box * box * 256;
+      };
+      // one tile of the list, K or V, into the next stage, for the step under way
       auto load = [&](const Unit<NQ>& x, int t, bool v) {
-        const uint32_t st = idx % F::kStages, ph = (idx / F::kStages) & 1u;
-        ++idx;
-        uint64_t* full = &ctl.kv_full[st];
-        uint8_t* dst = kv + st * kStage;
-        const bool pre = t < x.n_pt;
-        const int key = pre ? t * kT : (t - x.n_pt) * kT;
-        const int n = min(kT, (pre ? x.n_prefix : x.s.k_len) - key);
-        const int boxes = a.paged ? (n + box - 1) / box : 1;
         bool ok = true;
-        if (lane == 0) {
-          ok = !ctl.fail && mbar_wait(&ctl.kv_empty[st], ph ^ 1u, a.err);
-          if (ok) mbar_arrive_expect_tx(full, (uint32_t)(boxes * box * 256));
-        }
+        uint32_t before = 0;
+#pragma unroll
+        for (int i = 0; i < F::kStages; ++i)
+          if (st == i) {
+            before = user[i];
+            user[i] = step + 1;
+          }
+        if (lane == 0 && before > 0)
+          ok = mbar_wait(&ctl.empty[(before - 1) % kSteps], ((before - 1) / kSteps) & 1u, a.err);
         __syncwarp();
         if (!__shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) return false;
+        uint64_t* full = &ctl.full[step % kSteps];
+        uint8_t* dst = kv + st * kStage;
+        st = st + 1 < F::kStages ? st + 1 : 0;
+        const bool pre = t < x.n_pt;
+        const int key = pre ? t * kT : (t - x.n_pt) * kT;
         const CUtensorMap* map = pre ? (v ? &maps.vp : &maps.kp) : (v ? &maps.v : &maps.k);
-        if (lane < boxes) {
+        if (lane * box * 256 < bytes_of(x, t)) {
           int row;
           if (a.paged)
             row = (int)attn_slot(a, pre ? a.prefix_table : x.s.pages, key + lane * box);
@@ -544,8 +550,12 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
         if (x.g < 0) break;
         if (x.ntm == 0) continue;
+        // (a step's barrier is free: the stages handed over so far come from later steps than its last)
+        if (lane == 0) mbar_arrive_expect_tx(&ctl.full[step % kSteps], bytes_of(x, x.t_lo));
+        __syncwarp();
         live = load(x, x.t_lo, false);
         if (!live) break;
+        ++step;
         bool ok = true;
         if (lane == 0) {
           ok = mbar_wait(&ctl.q_empty, (n_q & 1u) ^ 1u, a.err);
@@ -566,9 +576,13 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         __syncwarp();
         live = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
         ++n_q;
-        for (int j = 0; live && j < x.ntm; ++j) {
+        for (int j = 0; live && j < x.ntm; ++j, ++step) {
+          const bool more = j + 1 < x.ntm;
+          if (lane == 0)
+            mbar_arrive_expect_tx(&ctl.full[step % kSteps], bytes_of(x, x.t_lo + j) + (more ? bytes_of(x, x.t_lo + j + 1) : 0));
+          __syncwarp();
           live = load(x, x.t_lo + j, true);
-          if (live && j + 1 < x.ntm) live = load(x, x.t_lo + j + 1, false);
+          if (live && more) live = load(x, x.t_lo + j + 1, false);
         }
       }
       if (!live) ctl.fail = 1;
@@ -579,7 +593,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         w.b0 = w.g0 = w.base = 0;
         walk_chunk<NQ>(a, plan, w);
       }
-      uint32_t loads = 0;
+      uint32_t loads = 0, steps = 0;
       bool live = true;
       for (int k = 0; live; ++k) {
         const int u = unit_index(k), slot = k % kBoard;
@@ -593,7 +607,11 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         }
         if (!more) x.g = -1;
         x.load0 = loads;
-        if (more) loads += 2 * x.ntm;
+        x.step0 = steps;
+        if (more && x.ntm > 0) {
+          loads += 2 * x.ntm;
+          steps += x.ntm + 1;
+        }
         live = warp_wait(&ctl.u_empty[slot], ((k / kBoard) & 1u) ^ 1u, a.err);
         if (live && lane == 0) {
           ctl.board[slot] = x;
@@ -636,8 +654,8 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         tc_fence_after();
         if (n_keys < kT) {
           // rows past the end: zero before the product reads them
-          const uint32_t lv = x.load0 + 2 * j + 1, sv = lv % F::kStages;
-          failed = !warp_wait(&ctl.kv_full[sv], (lv / F::kStages) & 1u, a.err);
+          const uint32_t sv = (x.load0 + 2 * j + 1) % F::kStages, st = x.step0 + j + 1;
+          failed = !warp_wait(&ctl.full[st % kSteps], (st / kSteps) & 1u, a.err);
           if (failed) break;
           uint8_t* vs = kv + sv * kStage;
           for (int q = n_keys * 16 + r; q < kT * 16; q += 128)
