@@ -1248,17 +1248,19 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
   AttnPlan& p = c.plan;
   const long long own_tiles = ((long long)kv_len_max + 127) / 128, pre_tiles = ((long long)prefix_len + 127) / 128;
   if (R <= kSpanHeads) {
-    const long long tiles = (long long)B * H_kv * (own_tiles > 0 ? own_tiles : 1);
-    c.by_unit = (long long)B * H_kv <= 2 * kPlanSms && own_tiles <= 4;
-    c.n_spans = c.by_unit ? B * H_kv : (int)((tiles + 1) / 2 < 2 * kPlanSms ? (tiles + 1) / 2 : 2 * kPlanSms);
+    const long long units = (long long)B * H_kv, tiles = units * (own_tiles > 0 ? own_tiles : 1);
     p.nq = B <= TT ? 1 : 2;
-    const long long units = ((long long)B + p.nq * TT - 1) / (p.nq * TT) * H_kv;
-    // the two kernels run side by side, on SMs in proportion to their tiles (two row tiles: twice the cost)
-    const long long pre = 2 * units * pre_tiles, ctas = pre > 0 ? kPlanSms * pre / (pre + tiles) : 0;
-    c.n_prefix = attn_parts(units, prefix_len, ctas / units * units, 512, 64);
+    const long long pre_units = ((long long)B + p.nq * TT - 1) / (p.nq * TT) * H_kv;
+    // the two kernels run side by side, on SMs in proportion to their tiles (one of the prefix's
+    // with two row tiles takes a CTA about as long as three of the own keys' take an SM)
+    const long long pre = (p.nq == 2 ? 3 : 2) * pre_units * pre_tiles;
+    c.n_prefix = attn_parts(pre_units, prefix_len, pre > 0 ? kPlanSms * pre / (pre + tiles) / pre_units * pre_units : 0, 512, 64);
+    const long long left = kPlanSms - pre_units * c.n_prefix, slots = 2 * (left > 32 ? left : 32);
+    c.by_unit = units <= slots && own_tiles <= 4;
+    c.n_spans = (int)(c.by_unit ? units : (tiles + 1) / 2 < slots ? (tiles + 1) / 2 : slots);
     c.n_part = c.n_prefix;
     p.n_prefix_parts = c.n_prefix;
-    p.n_prefix_units = (int)(units * c.n_prefix);
+    p.n_prefix_units = (int)(pre_units * c.n_prefix);
     p.n_units = p.n_prefix_units;
     return c;
   }

@@ -137,4 +137,47 @@ __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s
   return l == 0.f ? -INFINITY : m + log2f(l);
 }
 
+// Weighs n more parts of a row and adds them to s (by one warp): lse(p) in base 2 and 128 floats at part(p).
+// A round's loads are all under way before the first is used.
+struct Joined {
+  float o[4], w, m;  // weighted sum of lane's elements, sum of the weights 2^(lse - m)
+};
+template <typename Lse, typename Part>
+__device__ __forceinline__ void join_parts(Joined& s, int n, Lse lse, Part part) {
+  constexpr int kRound = 12;
+  const int lane = threadIdx.x & 31;
+  for (int p0 = 0; p0 < n; p0 += kRound) {
+    float x[kRound];
+    float4 v[kRound];
+#pragma unroll
+    for (int p = 0; p < kRound; ++p) {
+      x[p] = -INFINITY;
+      v[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (p0 + p < n) {
+        x[p] = lse(p0 + p);
+        v[p] = *reinterpret_cast<const float4*>(part(p0 + p) + lane * 4);
+      }
+    }
+    float mn = s.m;
+#pragma unroll
+    for (int p = 0; p < kRound; ++p) mn = fmaxf(mn, x[p]);
+    const float base = mn == -INFINITY ? 0.f : mn, c = exp2f(s.m - base);
+    s.m = mn;
+    s.w *= c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s.o[e] *= c;
+#pragma unroll
+    for (int p = 0; p < kRound; ++p) {
+      const float w = exp2f(x[p] - base);
+      s.w += w;
+      if (w != 0.f) {  // (a part without weight may hold anything)
+        s.o[0] = fmaf(w, v[p].x, s.o[0]);
+        s.o[1] = fmaf(w, v[p].y, s.o[1]);
+        s.o[2] = fmaf(w, v[p].z, s.o[2]);
+        s.o[3] = fmaf(w, v[p].w, s.o[3]);
+      }
+    }
+  }
+}
+
 }  // namespace provip

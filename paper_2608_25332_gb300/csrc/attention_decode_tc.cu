@@ -108,6 +108,28 @@ __device__ __forceinline__ int span_of(long long f, long long T, int G) {
   return (int)(((f + 1) * G - 1) / T);
 }
 
+// The warp's reduction of eight values a lane, in nine exchanges instead of forty: afterwards
+// lane 4 h has that of value h.
+template <typename Op>
+__device__ __forceinline__ float reduce8(const float* x, Op op) {
+  const int lane = threadIdx.x & 31;
+  float v[4], u[2], w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool up = lane & 16;
+    v[i] = op(up ? x[i + 4] : x[i], __shfl_xor_sync(0xffffffffu, up ? x[i] : x[i + 4], 16));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const bool up = lane & 8;
+    u[i] = op(up ? v[i + 2] : v[i], __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + 2], 8));
+  }
+  const bool up = lane & 4;
+  w = op(up ? u[1] : u[0], __shfl_xor_sync(0xffffffffu, up ? u[0] : u[1], 4));
+  w = op(w, __shfl_xor_sync(0xffffffffu, w, 2));
+  return op(w, __shfl_xor_sync(0xffffffffu, w, 1));
+}
+
 // the warp's sum of the requests' tiles before each of 32 requests, and of all 32
 __device__ __forceinline__ int tiles_before(int t, int lane, int& all) {
   int s = t;
@@ -165,7 +187,9 @@ __global__ void __launch_bounds__(kThr, 2)
   const uint32_t tmem = ctl.tmem;
 
   if (warp == 4) {
-    // ---- MMA issuer: the products of tile n + 1 with Q before those of tile n with V ----
+    // ---- MMA issuer. A tile's product with V goes before the next one's with Q: with three
+    // stages, the next K is only asked for once the last V but one is done with, and to wait
+    // for it first had made the time of a tile the latency of a load ----
     const bool lead = elect_one();
     const uint64_t kd0 = smem_desc_sw128(smem_u32(kv)), vd0 = smem_desc_mn_sw128(smem_u32(kv));
     const uint64_t qd0 = smem_desc_sw128(smem_u32(qs)), pd0 = smem_desc_sw128(smem_u32(ps));
@@ -211,11 +235,11 @@ __global__ void __launch_bounds__(kThr, 2)
       if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
       live = warp_wait(&ctl.q_full[u & 1], (u >> 1) & 1u, a.err);
       for (int j = 0; live && j <= nt; ++j) {
+        if (j > 0) values(n + j - 1, j == 1);
         if (j < nt) {
           scores(n + j, u & 1);
           if (j == nt - 1 && lead) tc_commit(&ctl.q_empty[u & 1]);
         }
-        if (j > 0) values(n + j - 1, j == 1);
       }
       n += nt;
     }
@@ -421,15 +445,14 @@ __global__ void __launch_bounds__(kThr, 2)
         tmem_ld8(tmem + buf * kCols + lanes, s);
         tc_wait_ld();
 #pragma unroll
-        for (int h = 0; h < R; ++h) s[h] = key ? s[h] * sc : -INFINITY;
+        for (int h = 0; h < 8; ++h) s[h] = key && h < R ? s[h] * sc : -INFINITY;
         bool raise = j == 0;
         for (;;) {
           if (raise) {
             // each head's largest score of the tile, over its 128 threads
-#pragma unroll
-            for (int h = 0; h < R; ++h) {
-              const float w = warp_max(s[h]);
-              if (lane == 0) ctl.red[warp][h] = w;
+            {
+              const float w = reduce8(s, [](float x, float y) { return fmaxf(x, y); });
+              if ((lane & 3) == 0) ctl.red[warp][lane >> 2] = w;
             }
             soft_sync();
             float f[8];
@@ -481,10 +504,12 @@ __global__ void __launch_bounds__(kThr, 2)
         if (lane == 0) mbar_arrive(&ctl.p_full[buf]);
       }
       // ---- epilogue: O^T / l, element r of every head ----
+      {
+        float l8[8];
 #pragma unroll
-      for (int h = 0; h < R; ++h) {
-        const float w = warp_sum(l[h]);
-        if (lane == 0) ctl.red[warp][h] = w;
+        for (int h = 0; h < 8; ++h) l8[h] = h < R ? l[h] : 0.f;
+        const float w = reduce8(l8, [](float x, float y) { return x + y; });
+        if ((lane & 3) == 0) ctl.red[warp][lane >> 2] = w;
       }
       const uint32_t last_n = x.tile0 + nt - 1;
       if (!failed) failed = !mbar_wait(&ctl.o_done[last_n & 1], (last_n >> 1) & 1u, a.err);
@@ -501,16 +526,21 @@ __global__ void __launch_bounds__(kThr, 2)
 #pragma unroll
       for (int h = 0; h < R; ++h) {
         const float t = (ctl.red[0][h] + ctl.red[1][h]) + (ctl.red[2][h] + ctl.red[3][h]);
-        float val = t == 0.f ? 0.f : o[h] / t, lse = t == 0.f ? -INFINITY : m[h] + lg2_approx(t);
+        // no weight: 0, or where every score is -inf 0 / 0, as the formula has it
+        const float nil = last && x.n_keys > 0 ? NAN : 0.f, val = t == 0.f ? nil : o[h] / t;
         if (last) {
-          if (t == 0.f && x.n_keys > 0) val = lse = NAN;  // every score is -inf: 0 / 0, as the formula has it
           __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim;
           op[r] = __float2bfloat16_rn(val);
-          if (r == 0 && a.lse) a.lse[row0 + h] = lse * kLn2;
         } else {
           float* po = x.whole ? sp.whole_o + (row0 + h) * kHeadDim : sp.piece_o + (slot * R + h) * kHeadDim;
           po[r] = val;
-          if (r == 0) (x.whole ? sp.whole_lse[row0 + h] : sp.piece_lse[slot * R + h]) = lse;
+        }
+        if (r == 0) {
+          const float lse = t != 0.f ? m[h] + lg2_approx(t) : nil == 0.f ? -INFINITY : NAN;
+          if (!last)
+            (x.whole ? sp.whole_lse[row0 + h] : sp.piece_lse[slot * R + h]) = lse;
+          else if (a.lse)
+            a.lse[row0 + h] = lse * kLn2;
         }
       }
       soft_sync();  // red is free again
@@ -529,85 +559,59 @@ __global__ void __launch_bounds__(kThr, 2)
 // ---------------------------------------------------------------------------
 // pieces and prefix parts -> rows: a warp per row
 // ---------------------------------------------------------------------------
-// Weighs and adds n parts of a row: lse(p) and the 512 bytes at part(p). The weights first, a
-// part per lane, so that the parts' loads do not wait for one another.
-struct Joined {
-  float o[4], w, m;
-};
-template <typename Lse, typename Part>
-__device__ __forceinline__ Joined join_parts(int n, Lse lse, Part part) {
-  const int lane = threadIdx.x & 31;
-  Joined s = {{0.f, 0.f, 0.f, 0.f}, 0.f, -INFINITY};
-  for (int p0 = 0; p0 < n; p0 += 32) {
-    const float x = p0 + lane < n ? lse(p0 + lane) : -INFINITY;
-    const float mn = fmaxf(s.m, warp_max(x)), base = mn == -INFINITY ? 0.f : mn;
-    const float c = exp2f(s.m - base), mine = p0 + lane < n ? exp2f(x - base) : 0.f;
-    s.m = mn;
-    s.w = s.w * c + warp_sum(mine);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s.o[e] *= c;
-#pragma unroll 8
-    for (int p = 0; p < min(n - p0, 32); ++p) {
-      const float w = __shfl_sync(0xffffffffu, mine, p);
-      const float4 v = *reinterpret_cast<const float4*>(part(p0 + p) + lane * 4);
-      if (w != 0.f) {
-        s.o[0] = fmaf(w, v.x, s.o[0]);
-        s.o[1] = fmaf(w, v.y, s.o[1]);
-        s.o[2] = fmaf(w, v.z, s.o[2]);
-        s.o[3] = fmaf(w, v.w, s.o[3]);
-      }
-    }
-  }
-  return s;
-}
-
 // with a prefix: a warp per (request, head); without: per border of two spans and head, for
 // the unit that the border is the first to cut
 __global__ void __launch_bounds__(256) attn_join_spans(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnSpans sp) {
   pdl_wait_prior();
   const int lane = threadIdx.x & 31, R = a.H_q / a.H_kv, G = sp.n_spans;
   const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long n_rows = (long long)a.T_q * a.H_q;
   long long row;
-  int hd, c0 = 0, c1 = 0;  // the spans that hold the unit's first and last tile
+  int b, h, hd, c0 = 0, c1 = 0;  // c0, c1: the spans that hold the unit's first and last tile
   if (a.prefix_len > 0) {
-    if (w >= (long long)a.B * a.H_q) return;
+    if (w >= n_rows) return;
     row = w;
-    const int b = (int)(w / a.H_q), h = (int)(w % a.H_q);
+    b = (int)((unsigned)w / (unsigned)a.H_q);  // (B H_q fits 31 bits)
+    h = (int)w - b * a.H_q;
     hd = h % R;
-    if (!sp.by_unit) {
-      const long long T = sp.before[a.B] * a.H_kv, first = sp.before[b], nt = sp.before[b + 1] - first;
-      const long long F = first * a.H_kv + h / R * nt;
-      c0 = span_of(F, T, G);
-      c1 = span_of(F + nt - 1, T, G);
-    }
   } else {
-    const int c = (int)(1 + w / R);
+    const int c = 1 + (int)((unsigned)w / (unsigned)R);
     if (c >= G) return;
     const int2 cut = sp.cut[c];
     if (cut.x < 0) return;
-    hd = (int)(w % R);
-    row = (long long)(cut.x / a.H_kv) * a.H_q + (cut.x % a.H_kv) * R + hd;
+    hd = (int)w - (c - 1) * R;
+    b = cut.x / a.H_kv;
+    h = cut.x % a.H_kv * R + hd;
+    row = (long long)b * a.H_q + h;
     // (the border cuts the unit, so the tile before it lies in the nearest span that has any)
     c0 = c - 1;
     while (c0 > 0 && sp.cut[c0].y < 0) --c0;
     c1 = cut.y;
   }
-  const long long n_rows = (long long)a.T_q * a.H_q;
-  const int n_pre = sp.n_prefix, n_own = c1 - c0 + 1;
-  auto slot = [&](int p) { return (size_t)(2 * (c0 + p) + (p == 0 ? 1 : 0)) * R + hd; };
-  auto empty = [&](int p) { return p > 0 && sp.cut[c0 + p].y < 0; };  // a span without tiles
-  const Joined s = join_parts(
-      n_pre + n_own,
-      [&](int p) {
-        return p < n_pre ? a.part_lse[p * n_rows + row]
-               : n_own == 1 ? sp.whole_lse[row] : empty(p - n_pre) ? -INFINITY : sp.piece_lse[slot(p - n_pre)];
-      },
-      [&](int p) {
-        return p < n_pre ? a.part_o + (p * n_rows + row) * kHeadDim
-               : n_own == 1 ? sp.whole_o + row * kHeadDim : sp.piece_o + slot(p - n_pre) * kHeadDim;
-      });
-  const int b = (int)(row / a.H_q), h = (int)(row % a.H_q);
-  const int n_keys = a.prefix_len + max(checked_len(a, b), 0);
+  // what is needed later is asked for now
+  const int k_len = checked_len(a, b);
+  const bool scan = a.prefix_len > 0 && !sp.by_unit;
+  const long long all = scan ? sp.before[a.B] : 0, first = scan ? sp.before[b] : 0, next = scan ? sp.before[b + 1] : 0;
+  Joined s = {{0.f, 0.f, 0.f, 0.f}, 0.f, -INFINITY};
+  join_parts(
+      s, sp.n_prefix, [&](int p) { return a.part_lse[p * n_rows + row]; },
+      [&](int p) { return a.part_o + (p * n_rows + row) * kHeadDim; });
+  if (scan) {
+    const long long T = all * a.H_kv, nt = next - first, F = first * a.H_kv + h / R * nt;
+    c0 = span_of(F, T, G);
+    c1 = span_of(F + nt - 1, T, G);
+  }
+  if (c0 == c1) {
+    join_parts(
+        s, 1, [&](int) { return sp.whole_lse[row]; }, [&](int) { return sp.whole_o + row * kHeadDim; });
+  } else {
+    auto slot = [&](int p) { return (size_t)(2 * (c0 + p) + (p == 0 ? 1 : 0)) * R + hd; };
+    auto empty = [&](int p) { return p > 0 && sp.cut[c0 + p].y < 0; };  // a span without tiles (its slot: anything)
+    join_parts(
+        s, c1 - c0 + 1, [&](int p) { return empty(p) ? -INFINITY : sp.piece_lse[slot(p)]; },
+        [&](int p) { return sp.piece_o + slot(p) * kHeadDim; });
+  }
+  const int n_keys = a.prefix_len + max(k_len, 0);
   const float den = s.w == 0.f ? (n_keys > 0 ? NAN : 1.f) : s.w;  // every score -inf: 0 / 0, as the formula has it
   float o[4];
 #pragma unroll

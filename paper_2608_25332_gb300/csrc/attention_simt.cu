@@ -414,29 +414,16 @@ __global__ void __launch_bounds__(256) attn_join(const __grid_constant__ AttnArg
     }
     if (!found) return;
   }
-  float mx = -INFINITY;
-  for (int p = lane; p < a.n_part; p += 32) mx = fmaxf(mx, a.part_lse[(size_t)p * n_rows + row]);
-  mx = warp_max(mx);
-  const float base = mx == -INFINITY ? 0.f : mx;
-  float o[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < a.n_part; ++p) {
-    const float w = exp2f(a.part_lse[(size_t)p * n_rows + row] - base);
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((size_t)p * n_rows + row) * kHeadDim + lane * 4);
-    sum += w;
-    if (w != 0.f) {
-      o[0] = fmaf(w, v.x, o[0]);
-      o[1] = fmaf(w, v.y, o[1]);
-      o[2] = fmaf(w, v.z, o[2]);
-      o[3] = fmaf(w, v.w, o[3]);
-    }
-  }
-  const float den = sum == 0.f ? (n_vis > 0 ? NAN : 1.f) : sum;  // every score -inf: 0 / 0, as the formula has it
+  Joined s = {{0.f, 0.f, 0.f, 0.f}, 0.f, -INFINITY};
+  join_parts(
+      s, a.n_part, [&](int p) { return a.part_lse[(size_t)p * n_rows + row]; },
+      [&](int p) { return a.part_o + ((size_t)p * n_rows + row) * kHeadDim; });
+  const float den = s.w == 0.f ? (n_vis > 0 ? NAN : 1.f) : s.w;  // every score -inf: 0 / 0, as the formula has it
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] /= den;
-  store4(static_cast<T*>(a.out) + (size_t)t * a.o_stride + (size_t)h * kHeadDim + lane * 4, o);
+  for (int e = 0; e < 4; ++e) s.o[e] /= den;
+  store4(static_cast<T*>(a.out) + (size_t)t * a.o_stride + (size_t)h * kHeadDim + lane * 4, s.o);
   if (lane == 0 && a.lse)
-    a.lse[row] = sum == 0.f ? (n_vis > 0 ? NAN : -INFINITY) : (mx + log2f(sum)) * kLn2;
+    a.lse[row] = s.w == 0.f ? (n_vis > 0 ? NAN : -INFINITY) : (s.m + log2f(s.w)) * kLn2;
 }
 
 template <typename T, bool PREFIX>
