@@ -7,8 +7,10 @@
 // the fewest; columns past R hold anything and are never read):
 //   S^T = K Q^T    8 tcgen05.mma (M = 128 keys, N = 16, K = 16), a thread per key then has R
 //                  scores to weigh, instead of one thread 128;
-//   P^T            2^(s - m) in fp32, summed per thread and head, to bf16 in shared memory
-//                  [head][key] (the second product's only 16-bit operand type);
+//   P^T            2^(s - m) in fp32, to bf16 in shared memory [head][key] (the second
+//                  product's only 16-bit operand type); per thread and head the sum of the
+//                  values in fp32 for the log-sum-exp, and that of the rounded ones, by which
+//                  O is divided so that its weights add up to one;
 //   O^T += V^T P^T 8 tcgen05.mma (M = 128 elements, N = 16, K = 16 keys), V as it lies.
 // No maximum is looked for while no value of P passes 2^10 (a vote of the tile's threads);
 // at a unit's first tile and past that it is found and P formed again.
@@ -56,7 +58,7 @@ struct Ctl {
   uint64_t kv_full[kStages], kv_empty[kStages];
   uint64_t s_full[2], p_full[2];
   uint64_t o_done[2];  // by the tile's parity: scores of tile n are issued past the product of n - 2, not of n - 1
-  float red[4][kHeads];
+  float red[4][kHeads], red_w[4][kHeads];
   uint32_t tmem;
   volatile int fail;
 };
@@ -417,11 +419,11 @@ __global__ void __launch_bounds__(kThr, 2)
       const Piece& x = ctl.board[u % kBoard];
       if (failed || x.g < 0) break;
       const int nt = x.nt;
-      float m[R], l[R];
+      float m[R], l[R], lw[R];
 #pragma unroll
       for (int h = 0; h < R; ++h) {
         m[h] = -INFINITY;
-        l[h] = 0.f;
+        l[h] = lw[h] = 0.f;
       }
       for (int j = 0; j < nt; ++j) {
         const uint32_t n = x.tile0 + j, buf = n & 1;
@@ -460,11 +462,12 @@ __global__ void __launch_bounds__(kThr, 2)
 #pragma unroll
             for (int h = 0; h < R; ++h) {
               const float mx = fmaxf(fmaxf(ctl.red[0][h], ctl.red[1][h]), fmaxf(ctl.red[2][h], ctl.red[3][h]));
-              const float mn = fmaxf(m[h], ceilf(mx));
-              f[h] = m[h] == mn ? 1.f : ex2_int(m[h] - mn);
+              const float mn = fmaxf(m[h], mx);
+              f[h] = m[h] == mn ? 1.f : ex2_approx(m[h] - mn);
               any = any || f[h] != 1.f;
               m[h] = mn;
               l[h] *= f[h];
+              lw[h] *= f[h];
             }
 #pragma unroll
             for (int h = R; h < 8; ++h) f[h] = 1.f;
@@ -495,8 +498,10 @@ __global__ void __launch_bounds__(kThr, 2)
         uint8_t* pb = ps + buf * kPBytes + p_half + p_in;
 #pragma unroll
         for (int h = 0; h < R; ++h) {
+          const __nv_bfloat16 w = __float2bfloat16_rn(p[h]);
           l[h] += p[h];
-          *reinterpret_cast<__nv_bfloat16*>(pb + h * 128 + ((p_chunk ^ (uint32_t)h) & 7u) * 16) = __float2bfloat16_rn(p[h]);
+          lw[h] += __bfloat162float(w);
+          *reinterpret_cast<__nv_bfloat16*>(pb + h * 128 + ((p_chunk ^ (uint32_t)h) & 7u) * 16) = w;
         }
         fence_proxy_async_smem();
         tc_fence_before();
@@ -505,11 +510,18 @@ __global__ void __launch_bounds__(kThr, 2)
       }
       // ---- epilogue: O^T / l, element r of every head ----
       {
-        float l8[8];
+        auto add = [](float x, float y) { return x + y; };
+        float l8[8], w8[8];
 #pragma unroll
-        for (int h = 0; h < 8; ++h) l8[h] = h < R ? l[h] : 0.f;
-        const float w = reduce8(l8, [](float x, float y) { return x + y; });
-        if ((lane & 3) == 0) ctl.red[warp][lane >> 2] = w;
+        for (int h = 0; h < 8; ++h) {
+          l8[h] = h < R ? l[h] : 0.f;
+          w8[h] = h < R ? lw[h] : 0.f;
+        }
+        const float t = reduce8(l8, add), w = reduce8(w8, add);
+        if ((lane & 3) == 0) {
+          ctl.red[warp][lane >> 2] = t;
+          ctl.red_w[warp][lane >> 2] = w;
+        }
       }
       const uint32_t last_n = x.tile0 + nt - 1;
       if (!failed) failed = !mbar_wait(&ctl.o_done[last_n & 1], (last_n >> 1) & 1u, a.err);
@@ -527,7 +539,8 @@ __global__ void __launch_bounds__(kThr, 2)
       for (int h = 0; h < R; ++h) {
         const float t = (ctl.red[0][h] + ctl.red[1][h]) + (ctl.red[2][h] + ctl.red[3][h]);
         // no weight: 0, or where every score is -inf 0 / 0, as the formula has it
-        const float nil = last && x.n_keys > 0 ? NAN : 0.f, val = t == 0.f ? nil : o[h] / t;
+        const float w = (ctl.red_w[0][h] + ctl.red_w[1][h]) + (ctl.red_w[2][h] + ctl.red_w[3][h]);
+        const float nil = last && x.n_keys > 0 ? NAN : 0.f, val = t == 0.f ? nil : o[h] / w;
         if (last) {
           __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim;
           op[r] = __float2bfloat16_rn(val);

@@ -9,13 +9,13 @@
 //   O += P V    8 tcgen05.mma, P read from tensor memory, V as it lies in memory (keys by
 //               elements, an operand whose rows run along N), O in tensor memory.
 // P is rounded to bf16 for its product (the only 16-bit operand type that V allows); the
-// sum of a row adds the unrounded values. The maximum that P is taken against (a whole
-// number) is raised only where a tile's values add up to more than 2^10: larger values of P
-// cost no accuracy in floating point, O is rescaled a few times a row instead of at every
-// tile, and the other tiles need no maximum at all, whose 64 three-way comparisons had
-// taken a third of a tile's time. S of a tile is complete after the product of the tile before
-// (one thread issues both, and a commit covers all that it issued), so a rescale needs no
-// further wait.
+// sum of a row adds the unrounded values. The maximum that P is taken against is raised, to
+// the true one (whose P is then 1 and rounds to itself), only where a tile's values add up to
+// more than 2^10: larger values of P cost no accuracy in floating point, O is rescaled a few
+// times a row instead of at every tile, and the other tiles need no maximum at all, whose 64
+// three-way comparisons had taken a third of a tile's time. S of a tile is complete after the
+// product of the tile before (one thread issues both, and a commit covers all that it issued),
+// so a rescale needs no further wait.
 // Roles: warps 0 .. 4 NQ - 1 softmax, then one warp issues the MMAs, one the TMA loads, and one
 // works the units out.
 // K and V tiles share a ring of 32 KiB stages. While the softmax works on one row tile, the
@@ -680,8 +680,8 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
             tc_wait_ld();
             if (masked) mask_from<kT>(v, lim);
             if (raise) {
-              const float mn = fmaxf(m, ceilf(max128(v) * sc));  // sc > 0: the maximum commutes with it
-              const float f = m == mn ? 1.f : ex2_int(m - mn);
+              const float mn = fmaxf(m, max128(v) * sc);  // sc > 0: the maximum commutes with it
+              const float f = m == mn ? 1.f : ex2_approx(m - mn);
               m = mn;
               if (j > 0) {
                 l *= f;

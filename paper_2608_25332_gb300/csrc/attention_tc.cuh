@@ -109,10 +109,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// 2^x of a whole x <= 0 (-inf too), exactly; 0 where it is subnormal
-__device__ __forceinline__ float ex2_int(float x) {
-  return x < -126.f ? 0.f : __int_as_float((127 + (int)x) << 23);
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);

@@ -242,7 +242,7 @@ def run_decode(seed, lens, H_q, H_kv, prefix, page, dtype, algo, kv_max=None, ch
     pool = torch.full((2, pages, page, H_kv, DH), math.nan, dtype=dtype, device=DEV) if not top else \
         torch.empty((2, pages, page, H_kv, DH), dtype=dtype, device=DEV)
     prefix_table = order[:pre].clone()
-    width = max(max(held), 1) + 2
+    width = max(max(held), -(-(kv_max or 1) // page)) + 2
     table = torch.full((B, width), -1, dtype=torch.int32, device=DEV)
     at = pre
     seqs = []
@@ -389,3 +389,144 @@ def test_without_lse(dtype):
     a = (Q, K, V, i32([0]), i32([64]), i32([0]), i32([64]), 64, 64)
     x, y = P.provip_prompt_attention(*a), P.provip_prompt_attention(*a, want_lse=False)
     assert y["lse"] is None and torch.equal(x["out"], y["out"])
+
+
+# ---------------------------------------------------------------------------
+# sizes at which the work is cut up differently
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+def test_more_sequences_than_the_lanes_hold(dtype, algo):
+    """600 sequences (256 at a time are walked through), some without rows"""
+    lens = [(7 * i) % 5 + (130 if i in (3, 299, 599) else 0) for i in range(600)]
+    run_prompt(40, lens, lens, 2, 1, 0, True, dtype, algo)
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("rows", [3, 300])
+def test_bounds_far_above_the_lengths(rows, dtype, algo):
+    """host bounds that promise long keys: most parts of a row are empty"""
+    g = gen(41)
+    H_q, H_kv, Tk = 4, 2, 200000
+    K, V = (torch.full((Tk, H_kv, DH), math.nan, dtype=dtype, device=DEV) for _ in range(2))
+    lens, starts_ = [rows, 77 + rows], [5, 100000]
+    for s, n in zip(starts_, lens):
+        K[s:s + n], V[s:s + n] = randn(g, n, H_kv, DH, dtype=dtype), randn(g, n, H_kv, DH, dtype=dtype)
+    Q = randn(g, 2 * rows, H_q, DH, dtype=dtype)
+    r = P.provip_prompt_attention(Q, K, V, i32([0, rows]), i32([rows, rows]), i32(starts_), i32(lens), rows, Tk, algo=algo)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(H_q):
+            k, v = (x[starts_[b]:starts_[b] + lens[b], h // 2] for x in (K, V))
+            ref = attend(Q[b * rows:(b + 1) * rows, h], k, v, hidden_mask(rows, lens[b], 0, True, DEV), DH ** -0.5, dtype, tc(dtype, algo))
+            check(r["out"][b * rows:(b + 1) * rows, h], r["lse"][b * rows:(b + 1) * rows, h], ref, f"sequence {b} head {h}")
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+def test_values_that_grow_along_the_keys(dtype, algo):
+    """the running maximum rises many times, by more than any lag: every tile rescales"""
+    g = gen(42)
+    n = 1500
+    Q, K, V = (randn(g, n, 2, DH, dtype=dtype) for _ in range(3))
+    q, k = Q.float(), K.float()
+    q[..., 0], k[..., 0] = 4.0, torch.arange(n, device=DEV)[:, None] * 0.25  # logits up to 130 above the first
+    Q, K = q.to(dtype), k.to(dtype)
+    r = P.provip_prompt_attention(Q, K, V, i32([0]), i32([n]), i32([0]), i32([n]), n, n, algo=algo)
+    torch.cuda.synchronize()
+    for h in range(2):
+        ref = attend(Q[:, h], K[:, h], V[:, h], hidden_mask(n, n, 0, True, DEV), DH ** -0.5, dtype, tc(dtype, algo))
+        check(r["out"][:, h], r["lse"][:, h], ref, f"head {h}")
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+def test_decode_values_that_grow_along_the_keys(dtype, algo):
+    g = gen(43)
+    n, page, H = 1100, 16, 2
+    pages = -(-n // page)
+    K, V = randn(g, pages, page, H, DH, dtype=dtype), randn(g, pages, page, H, DH, dtype=dtype)
+    k = K.float().reshape(-1, H, DH)
+    k[..., 0] = torch.arange(pages * page, device=DEV)[:, None] * 0.25
+    K = k.to(dtype).reshape(pages, page, H, DH)
+    Q = randn(g, 1, 4, DH, dtype=dtype)
+    Q[..., 0] = 4.0
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
+    r = P.provip_decode_attention(Q, K, V, table, i32([n]), n, algo=algo)
+    torch.cuda.synchronize()
+    for h in range(4):
+        kk, vv = (x.reshape(-1, H, DH)[:n, h // 2] for x in (K, V))
+        ref = attend(Q[:, h], kk, vv, torch.zeros(1, n, dtype=torch.bool, device=DEV), DH ** -0.5, dtype, tc(dtype, algo))
+        check(r["out"][:, h], r["lse"][:, h], ref, f"head {h}")
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+def test_decode_more_requests_than_the_lanes_hold(dtype, algo):
+    run_decode(44, [(13 * i) % 40 + (700 if i % 211 == 5 else 0) for i in range(700)], 2, 1, 0, 16, dtype, algo, check_heads=[1])
+    run_decode(45, [(13 * i) % 40 for i in range(300)], 3, 1, 50, 8, dtype, algo, kv_max=2000, check_heads=[2])
+
+
+@pytest.mark.parametrize("lens", [[300], [1500, 20, 700], [129] * 40, [1, 2000]], ids=lambda v: "_".join(map(str, v[:4])))
+def test_decode_bits_stay(lens):
+    """twenty calls in a row, nothing waiting between them: units of several tiles, and units
+    that the CTAs' spans cut"""
+    step, args = run_decode(46, lens, 4, 4, 0, 16, BF16, P.ALGO_AUTO, check_heads=[0])
+    want = {k: v.clone() for k, v in step(*args).items()}
+    got = []
+    for _ in range(20):
+        r = step(*args)
+        got.append((r["out"].clone(), r["lse"].clone()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want["out"]) and torch.equal(l, want["lse"]) for o, l in got)
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("pad", [0, 8, 24])
+def test_guard_bytes_and_row_strides(pad, dtype, algo):
+    """outputs with rows further apart (16-byte, not 32-byte multiples among them) and the
+    workspace inside red zones; what lies between and around the rows stays"""
+    import ctypes
+    g = gen(47)
+    L = P.lib()
+    dt = P._dtype_of(dtype)
+    H_q, H_kv, lens = 6, 2, [130, 0, 7]
+    T = sum(lens)
+    Q, K, V = (randn(g, T, h, DH, dtype=dtype) for h in (H_q, H_kv, H_kv))
+    st, ln = i32(starts(lens)[:-1]), i32(lens)
+    want = P.provip_prompt_attention(Q, K, V, st, ln, st, ln, 130, 130, algo=algo)
+    stride, zone = H_q * DH + pad, 512
+    buf = torch.full((zone + T * stride + zone,), 3.0, dtype=dtype, device=DEV)
+    lse = torch.full((zone + T * H_q + zone,), 3.0, device=DEV)
+    need = L.provip_prompt_attention_workspace_size(T, 3, H_q, H_kv, 130, 130, 0, dt, algo)
+    ws = torch.full((need + 2048,), 0xA5, dtype=torch.uint8, device=DEV)
+    at = lambda t, n: ctypes.c_void_p(t.data_ptr() + n * t.element_size())
+    rc = L.provip_prompt_attention(Q.data_ptr(), H_q * DH, K.data_ptr(), H_kv * DH, V.data_ptr(), H_kv * DH, T, T, 3, H_q, H_kv, DH,
+                                   st.data_ptr(), ln.data_ptr(), st.data_ptr(), ln.data_ptr(), 130, 130, None, 0, None, 0, 0, 1,
+                                   DH ** -0.5, dt, algo, at(buf, zone), stride, at(lse, zone), at(ws, 1024), need,
+                                   P._stream(torch.device(DEV)))
+    torch.cuda.synchronize()
+    assert rc == 0
+    rows = buf[zone:zone + T * stride].view(T, stride)
+    assert torch.equal(rows[:, :H_q * DH].reshape(T, H_q, DH), want["out"]) and (rows[:, H_q * DH:] == 3).all()
+    assert (buf[:zone] == 3).all() and (buf[-zone:] == 3).all()
+    assert torch.equal(lse[zone:-zone].view(T, H_q), want["lse"]) and (lse[:zone] == 3).all() and (lse[-zone:] == 3).all()
+    assert (ws[:1024] == 0xA5).all() and (ws[1024 + need:] == 0xA5).all()
+    # decoding
+    page, B = 16, 3
+    kp, vp = randn(g, 40, page, H_kv, DH, dtype=dtype), randn(g, 40, page, H_kv, DH, dtype=dtype)
+    table, kl = torch.arange(30, dtype=torch.int32, device=DEV).view(B, 10), i32([160, 0, 33])
+    pt = torch.arange(30, 40, dtype=torch.int32, device=DEV)
+    Qd = randn(g, B, H_q, DH, dtype=dtype)
+    for prefix in (0, 150):
+        want = P.provip_decode_attention(Qd, kp, vp, table, kl, 160, pt if prefix else None, prefix, algo=algo)
+        need = L.provip_decode_attention_workspace_size(B, H_q, H_kv, 160, prefix, dt, algo)
+        buf.fill_(3.0)
+        lse.fill_(3.0)
+        ws = torch.full((need + 2048,), 0xA5, dtype=torch.uint8, device=DEV)
+        rc = L.provip_decode_attention(Qd.data_ptr(), H_q * DH, B, H_q, H_kv, DH, kp.data_ptr(), vp.data_ptr(), 40, page, table.data_ptr(), 10,
+                                       kl.data_ptr(), 160, pt.data_ptr() if prefix else None, prefix, DH ** -0.5, dt, algo, at(buf, zone),
+                                       stride, at(lse, zone), at(ws, 1024), need, P._stream(torch.device(DEV)))
+        torch.cuda.synchronize()
+        assert rc == 0
+        rows = buf[zone:zone + B * stride].view(B, stride)
+        assert torch.equal(rows[:, :H_q * DH].reshape(B, H_q, DH), want["out"]) and (rows[:, H_q * DH:] == 3).all()
+        assert (buf[:zone] == 3).all() and (buf[zone + B * stride:] == 3).all()
+        assert torch.equal(lse[zone:zone + B * H_q].view(B, H_q), want["lse"]) and (lse[zone + B * H_q:] == 3).all()
+        assert (ws[:1024] == 0xA5).all() and (ws[1024 + need:] == 0xA5).all()
