@@ -1254,8 +1254,12 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
     // the two kernels run side by side, on SMs in proportion to their tiles (one of the prefix's
     // with two row tiles takes a CTA about as long as three of the own keys' take an SM)
     const long long pre = (p.nq == 2 ? 3 : 2) * pre_units * pre_tiles;
-    c.n_prefix = attn_parts(pre_units, prefix_len, pre > 0 ? kPlanSms * pre / (pre + tiles) / pre_units * pre_units : 0, 512, 64);
-    const long long left = kPlanSms - pre_units * c.n_prefix, slots = 2 * (left > 32 ? left : 32);
+    const long long own_sms = units < 64 ? (units + 1) / 2 : 32;  // at least
+    long long pre_sms = pre > 0 ? kPlanSms * pre / (pre + tiles) : 0;
+    if (pre_sms > kPlanSms - own_sms) pre_sms = kPlanSms - own_sms;
+    const long long pre_ctas = pre_sms * (p.nq == 2 ? 1 : 2);
+    c.n_prefix = attn_parts(pre_units, prefix_len, pre_ctas / pre_units * pre_units, 512, 64);
+    const long long left = kPlanSms - pre_units * c.n_prefix / (p.nq == 2 ? 1 : 2), slots = 2 * (left > own_sms ? left : own_sms);
     c.by_unit = units <= slots && own_tiles <= 4;
     c.n_spans = (int)(c.by_unit ? units : (tiles + 1) / 2 < slots ? (tiles + 1) / 2 : slots);
     c.n_part = c.n_prefix;

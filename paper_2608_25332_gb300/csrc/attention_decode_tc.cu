@@ -58,16 +58,16 @@ struct Ctl {
   uint64_t kv_full[kStages], kv_empty[kStages];
   uint64_t s_full[2], p_full[2];
   uint64_t o_done[2];  // by the tile's parity: scores of tile n are issued past the product of n - 2, not of n - 1
-  float red[4][kHeads], red_w[4][kHeads];
+  float red[4][kHeads], red_w[4][kHeads], inv[kHeads];
   uint32_t tmem;
   volatile int fail;
 };
 
 __device__ __forceinline__ int unit_tiles(int k_len) { return max((k_len + kT - 1) / kT, 1); }
-__device__ __forceinline__ int checked_len(const AttnArgs& a, int b) {
-  const int n = a.k_len[b];
+__device__ __forceinline__ int fitting_len(const AttnArgs& a, int n) {
   return n >= 0 && n <= a.k_len_max && n <= (long long)a.max_pages * a.page_size ? n : -1;
 }
+__device__ __forceinline__ int checked_len(const AttnArgs& a, int b) { return fitting_len(a, a.k_len[b]); }
 
 __device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ bool soft_any(bool v) {
@@ -156,6 +156,13 @@ __global__ void __launch_bounds__(kThr, 2)
   uint8_t* kv = smem_raw + (((base + 1023u) & ~1023u) - base);
   uint8_t* ps = kv + kStages * kStage;
   uint8_t* qs = ps + 2 * kPBytes;
+  // lengths of 256 requests in the producer's registers, asked for while the block is set up
+  constexpr int kHeld = 8;
+  int held[kHeld];
+  if (warp == 5 && !sp.by_unit) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < a.B ? a.k_len[i * 32 + lane] : 0;
+  }
   if (threadIdx.x == 0) {
     prefetch_tmap(&map_q);
     prefetch_tmap(&map_k);
@@ -263,11 +270,9 @@ __global__ void __launch_bounds__(kThr, 2)
       f = (long long)((int)blockIdx.x - b * a.H_kv) * nt_b;
       f_end = f + nt_b;
     } else {
-      // lengths of 256 requests in the lanes' registers (beyond, they are read twice)
-      constexpr int kHeld = 8;
-      int held[kHeld];
+      // (past 256 requests the lengths are read twice)
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0;
+      for (int i = 0; i < kHeld; ++i) held[i] = fitting_len(a, held[i]);
       auto len_of = [&](int i) { return i * 32 + lane < a.B ? checked_len(a, i * 32 + lane) : 0; };
       // all tiles, and the tiles of the requests before each
       auto count = [&](int i, int k) {
@@ -311,15 +316,21 @@ __global__ void __launch_bounds__(kThr, 2)
     }
     const long long f0 = f, f0_b = f_b;
     const int b0 = b, nt0_b = nt_b;
-    // One tile, K or V, into the next stage. A lane's page is looked up once for both, and
-    // before the wait for the stage.
-    int row = 0;
+    // One tile, K or V, into the next stage. A lane's page is looked up once for both, a tile
+    // ahead.
+    int row = 0, next = 0;
+    auto row_of = [&](const Piece& x, int j) {
+      if (j >= x.nt || lane * box >= min(kT, x.n_keys - j * kT)) return 0;
+      return (int)attn_slot(a, a.block_table + (size_t)x.b * a.max_pages, (x.t_lo + j) * kT + lane * box);
+    };
     auto load = [&](const Piece& x, int j, bool v) {
       const uint32_t st = n_ld % kStages, ph = (n_ld / kStages) & 1u;
       ++n_ld;
       const int n = min(kT, x.n_keys - j * kT), boxes = n > 0 ? (n + box - 1) / box : 0;
-      if (!v && lane < boxes)
-        row = (int)attn_slot(a, a.block_table + (size_t)x.b * a.max_pages, (x.t_lo + j) * kT + lane * box);
+      if (!v) {
+        row = next;
+        next = row_of(x, j + 1);
+      }
       bool ok = true;
       if (lane == 0) {
         ok = !ctl.fail && mbar_wait(&ctl.kv_empty[st], ph ^ 1u, a.err);
@@ -366,6 +377,7 @@ __global__ void __launch_bounds__(kThr, 2)
       }
       __syncwarp();
       if (x.g < 0) break;
+      next = row_of(x, 0);
       live = load(x, 0, false);
       if (!live) break;
       bool ok = true;
@@ -425,30 +437,19 @@ __global__ void __launch_bounds__(kThr, 2)
         m[h] = -INFINITY;
         l[h] = lw[h] = 0.f;
       }
+      bool none = false;  // a head without a finite maximum so far
       for (int j = 0; j < nt; ++j) {
         const uint32_t n = x.tile0 + j, buf = n & 1;
         const bool key = r < x.n_keys - j * kT;
         if (!failed) failed = !mbar_wait(&ctl.s_full[buf], (n >> 1) & 1u, a.err);
         __syncwarp();
         tc_fence_after();
-        if (x.n_keys - j * kT < kT) {
-          // value rows past the end: zero before the product reads them
-          const uint32_t ld = 2 * n + 1, st = ld % kStages;
-          if (!failed) failed = !mbar_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
-          if (!key) {
-            uint8_t* vs = kv + st * kStage + r * 128;
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-              *reinterpret_cast<uint4*>(vs + (q >> 3) * kHalf + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          __syncwarp();
-        }
         float s[8], p[R];
         tmem_ld8(tmem + buf * kCols + lanes, s);
         tc_wait_ld();
 #pragma unroll
         for (int h = 0; h < 8; ++h) s[h] = key && h < R ? s[h] * sc : -INFINITY;
-        bool raise = j == 0;
+        bool raise = j == 0 || none;
         for (;;) {
           if (raise) {
             // each head's largest score of the tile, over its 128 threads
@@ -459,6 +460,7 @@ __global__ void __launch_bounds__(kThr, 2)
             soft_sync();
             float f[8];
             bool any = false;
+            none = false;
 #pragma unroll
             for (int h = 0; h < R; ++h) {
               const float mx = fmaxf(fmaxf(ctl.red[0][h], ctl.red[1][h]), fmaxf(ctl.red[2][h], ctl.red[3][h]));
@@ -466,6 +468,7 @@ __global__ void __launch_bounds__(kThr, 2)
               f[h] = m[h] == mn ? 1.f : ex2_approx(m[h] - mn);
               any = any || f[h] != 1.f;
               m[h] = mn;
+              none = none || mn == -INFINITY;
               l[h] *= f[h];
               lw[h] *= f[h];
             }
@@ -503,6 +506,17 @@ __global__ void __launch_bounds__(kThr, 2)
           lw[h] += __bfloat162float(w);
           *reinterpret_cast<__nv_bfloat16*>(pb + h * 128 + ((p_chunk ^ (uint32_t)h) & 7u) * 16) = w;
         }
+        if (x.n_keys - j * kT < kT) {
+          // value rows past the end: zero before the product reads them (neighbours in a warp
+          // write neighbouring 16 bytes: a row each had cost a microsecond of bank conflicts)
+          const uint32_t ld = 2 * n + 1, st = ld % kStages;
+          if (!failed) failed = !mbar_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
+          uint8_t* vs = kv + st * kStage;
+          for (int q = max(x.n_keys - j * kT, 0) * 8 + r; q < kT * 8; q += 128) {
+            *reinterpret_cast<uint4*>(vs + q * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(vs + kHalf + q * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
@@ -523,6 +537,27 @@ __global__ void __launch_bounds__(kThr, 2)
           ctl.red_w[warp][lane >> 2] = w;
         }
       }
+      soft_sync();
+      const size_t row0 = (size_t)x.b * a.H_q + x.g * R;
+      const bool last = x.whole && a.prefix_len == 0;
+      const size_t slot = x.whole ? 0 : 2 * (size_t)blockIdx.x + (x.t_lo == 0 ? 1 : 0);
+      // The sums over the warps, the divisor and the log-sum-exp of each head, a thread a head,
+      // while the last product runs. No weight: 0, or where every score is -inf 0 / 0, as
+      // the formula has it.
+      if (r < R) {
+        const float t = (ctl.red[0][r] + ctl.red[1][r]) + (ctl.red[2][r] + ctl.red[3][r]);
+        const float w = (ctl.red_w[0][r] + ctl.red_w[1][r]) + (ctl.red_w[2][r] + ctl.red_w[3][r]);
+        float mh = m[0];
+#pragma unroll
+        for (int h = 1; h < R; ++h) mh = r == h ? m[h] : mh;
+        const bool nil = last && x.n_keys > 0;
+        const float lse = t != 0.f ? mh + lg2_approx(t) : nil ? NAN : -INFINITY;
+        ctl.inv[r] = t != 0.f ? 1.f / w : nil ? NAN : 0.f;
+        if (!last)
+          (x.whole ? sp.whole_lse[row0 + r] : sp.piece_lse[slot * R + r]) = lse;
+        else if (a.lse)
+          a.lse[row0 + r] = lse * kLn2;
+      }
       const uint32_t last_n = x.tile0 + nt - 1;
       if (!failed) failed = !mbar_wait(&ctl.o_done[last_n & 1], (last_n >> 1) & 1u, a.err);
       __syncwarp();
@@ -532,15 +567,10 @@ __global__ void __launch_bounds__(kThr, 2)
       tmem_ld8(to, o);
       tc_wait_ld();
       tc_fence_before();  // O^T is read before the next unit's first product, which waits for p_full
-      const size_t row0 = (size_t)x.b * a.H_q + x.g * R;
-      const bool last = x.whole && a.prefix_len == 0;
-      const size_t slot = x.whole ? 0 : 2 * (size_t)blockIdx.x + (x.t_lo == 0 ? 1 : 0);
 #pragma unroll
       for (int h = 0; h < R; ++h) {
-        const float t = (ctl.red[0][h] + ctl.red[1][h]) + (ctl.red[2][h] + ctl.red[3][h]);
-        // no weight: 0, or where every score is -inf 0 / 0, as the formula has it
-        const float w = (ctl.red_w[0][h] + ctl.red_w[1][h]) + (ctl.red_w[2][h] + ctl.red_w[3][h]);
-        const float nil = last && x.n_keys > 0 ? NAN : 0.f, val = t == 0.f ? nil : o[h] / w;
+        // (an element without weight may hold anything)
+        const float inv = ctl.inv[h], val = inv == 0.f ? 0.f : o[h] * inv;
         if (last) {
           __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim;
           op[r] = __float2bfloat16_rn(val);
@@ -548,15 +578,7 @@ __global__ void __launch_bounds__(kThr, 2)
           float* po = x.whole ? sp.whole_o + (row0 + h) * kHeadDim : sp.piece_o + (slot * R + h) * kHeadDim;
           po[r] = val;
         }
-        if (r == 0) {
-          const float lse = t != 0.f ? m[h] + lg2_approx(t) : nil == 0.f ? -INFINITY : NAN;
-          if (!last)
-            (x.whole ? sp.whole_lse[row0 + h] : sp.piece_lse[slot * R + h]) = lse;
-          else if (a.lse)
-            a.lse[row0 + h] = lse * kLn2;
-        }
       }
-      soft_sync();  // red is free again
       if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
     }
     if (failed) ctl.fail = 1;

@@ -176,7 +176,7 @@ __device__ __forceinline__ Unit<NQ> paged_unit(const AttnArgs& a, const AttnPlan
   return x;
 }
 
-// Contiguous keys: the units that have rows, in an order that the producer walks through. The
+// Contiguous keys: the units that have rows, in an order that their warp walks through. The
 // sequences (and, where one's keys are too many, its heads) come in chunks whose keys and
 // values stay in L2; within a chunk level by level, level l holding the l-th block of rows from
 // each sequence's end, which sees the most keys, so that long units come first. The blocks of a

@@ -458,6 +458,29 @@ def test_decode_values_that_grow_along_the_keys(dtype, algo):
 
 
 @pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("prefix", [0, 64])
+def test_decode_first_scores_minus_infinity(prefix, dtype, algo):
+    """the first tiles have no weight, and the scores behind them lie where 2^score underflows"""
+    g = gen(48)
+    n, page, H = 700, 16, 2
+    pages = -(-n // page)
+    K, V = randn(g, pages, page, H, DH, dtype=dtype), randn(g, pages, page, H, DH, dtype=dtype)
+    k = K.reshape(-1, H, DH)
+    k[..., 0] = -2000.0
+    k[:prefix + 300, :, 0] = -math.inf
+    Q = randn(g, 1, 4, DH, dtype=dtype)
+    Q[..., 0] = 4.0
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)
+    kw = dict(algo=algo, prefix_table=table[:prefix // page], prefix_len=prefix) if prefix else dict(algo=algo)
+    r = P.provip_decode_attention(Q, K, V, table[None, prefix // page:].contiguous(), i32([n - prefix]), n - prefix, **kw)
+    torch.cuda.synchronize()
+    for h in range(4):
+        kk, vv = (x.reshape(-1, H, DH)[prefix + 300:n, h // 2] for x in (K, V))  # the keys that have a weight
+        ref = attend(Q[:, h], kk, vv, torch.zeros(1, len(kk), dtype=torch.bool, device=DEV), DH ** -0.5, dtype, tc(dtype, algo))
+        check(r["out"][:, h], r["lse"][:, h], ref, f"head {h}")
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
 def test_decode_more_requests_than_the_lanes_hold(dtype, algo):
     run_decode(44, [(13 * i) % 40 + (700 if i % 211 == 5 else 0) for i in range(700)], 2, 1, 0, 16, dtype, algo, check_heads=[1])
     run_decode(45, [(13 * i) % 40 for i in range(300)], 3, 1, 50, 8, dtype, algo, kv_max=2000, check_heads=[2])
