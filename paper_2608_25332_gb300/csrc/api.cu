@@ -1193,8 +1193,10 @@ struct AttnCut {
 };
 
 // CUDA cores: row tiles of 64 packed rows, parts of two 64-key tiles or more. Tensor cores:
-// two row tiles of 128 a CTA, one where a sequence's rows fit in it (two CTAs then share an
-// SM); the keys are shared out where the units leave half of the CTAs without work, four
+// two row tiles of 128 a CTA, one where a sequence's rows fit in it and the CTAs are more than
+// the SMs (two CTAs then share an SM; with an SM to itself a CTA is better off with the ring of five
+// stages that comes with two row tiles: 32 heads of 100 rows and 500 keys 17.8 -> 14.4 us, 2 prompts
+// of 20-128 rows behind 5000 keys 52 -> 47; 16 behind 1000 keys 71 -> 65 the other way); the keys are shared out where the units leave half of the CTAs without work, four
 // 128-key tiles or more a part (a second launch joins the parts, about two tiles' time).
 AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int prefix_len, int dtype, int algo) {
   AttnCut c;
@@ -1210,7 +1212,7 @@ AttnCut prompt_cut(int B, int H_q, int H_kv, int q_len_max, int k_len_max, int p
   }
   const int TT = 128 / (R > 128 ? 128 : R);
   AttnPlan& p = c.plan;
-  p.nq = q_len_max <= TT ? 1 : 2;
+  p.nq = q_len_max <= TT && (long long)B * H_kv > kPlanSms ? 1 : 2;
   long long n_blk = ((long long)q_len_max + p.nq * TT - 1) / (p.nq * TT);
   if (n_blk < 1) n_blk = 1;
   const long long units = n_blk * B * H_kv, ctas = kPlanSms * (p.nq == 2 ? 1 : 2);
@@ -1249,16 +1251,20 @@ AttnCut decode_cut(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int
   const long long own_tiles = ((long long)kv_len_max + 127) / 128, pre_tiles = ((long long)prefix_len + 127) / 128;
   if (R <= kSpanHeads) {
     const long long units = (long long)B * H_kv, tiles = units * (own_tiles > 0 ? own_tiles : 1);
-    p.nq = B <= TT ? 1 : 2;
+    // one row tile: two row tiles' ring of five stages all the same, where there is more than a
+    // tile to fill it (2 requests of 40 heads behind 5000 keys 51 -> 44 us, 64 of 32 behind 1000 56 -> 40;
+    // 30 of 40 behind 35 keys 26 -> 24 the other way)
+    const bool two = B > TT;
+    p.nq = two || pre_tiles > 1 ? 2 : 1;
     const long long pre_units = ((long long)B + p.nq * TT - 1) / (p.nq * TT) * H_kv;
     // the two kernels run side by side, on SMs in proportion to their tiles (one of the prefix's
     // with two row tiles takes a CTA about as long as three of the own keys' take an SM)
-    const long long pre = (p.nq == 2 ? 3 : 2) * pre_units * pre_tiles;
+    const long long pre = (two ? 3 : 2) * pre_units * pre_tiles;
     const long long own_sms = units < 64 ? (units + 1) / 2 : 32;  // at least
     long long pre_sms = pre > 0 ? kPlanSms * pre / (pre + tiles) : 0;
     if (pre_sms > kPlanSms - own_sms) pre_sms = kPlanSms - own_sms;
     const long long pre_ctas = pre_sms * (p.nq == 2 ? 1 : 2);
-    c.n_prefix = attn_parts(pre_units, prefix_len, pre_ctas / pre_units * pre_units, 512, 64);
+    c.n_prefix = attn_parts(pre_units, prefix_len, pre_ctas / pre_units * pre_units, two ? 512 : 256, 64);
     const long long left = kPlanSms - pre_units * c.n_prefix / (p.nq == 2 ? 1 : 2), slots = 2 * (left > own_sms ? left : own_sms);
     c.by_unit = units <= slots && own_tiles <= 4;
     c.n_spans = (int)(c.by_unit ? units : (tiles + 1) / 2 < slots ? (tiles + 1) / 2 : slots);
