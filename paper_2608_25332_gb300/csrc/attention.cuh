@@ -124,7 +124,8 @@ __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s
     const bool pre = j < n_prefix;
     load4((pre ? attn_prefix_row<T>(a, false, j, g) : attn_own_row<T>(a, s, false, j - n_prefix, g)) + lane * 4, k);
     load4((pre ? attn_prefix_row<T>(a, true, j, g) : attn_own_row<T>(a, s, true, j - n_prefix, g)) + lane * 4, v);
-    const float x = warp_sum(fmaf(q[0], k[0], fmaf(q[1], k[1], fmaf(q[2], k[2], q[3] * k[3])))) * a.scale_log2;
+    // (rounded as the maximum is: no fma with the subtraction below)
+    const float x = __fmul_rn(warp_sum(fmaf(q[0], k[0], fmaf(q[1], k[1], fmaf(q[2], k[2], q[3] * k[3])))), a.scale_log2);
     if (x == -INFINITY) continue;
     const float mn = fmaxf(m, x), r = exp2f(m - mn), p = exp2f(x - mn);
     l = l * r + p;

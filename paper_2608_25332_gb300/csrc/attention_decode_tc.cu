@@ -445,10 +445,12 @@ __global__ void __launch_bounds__(kThr, 2)
         __syncwarp();
         tc_fence_after();
         float s[8], p[R];
+        // (rounded before the maximum is subtracted: with the two in one fma, scores past 2^28 would
+        // pass their own maximum by more than the loop below allows)
         tmem_ld8(tmem + buf * kCols + lanes, s);
         tc_wait_ld();
 #pragma unroll
-        for (int h = 0; h < 8; ++h) s[h] = key && h < R ? s[h] * sc : -INFINITY;
+        for (int h = 0; h < 8; ++h) s[h] = key && h < R ? __fmul_rn(s[h], sc) : -INFINITY;
         bool raise = j == 0 || none;
         for (;;) {
           if (raise) {

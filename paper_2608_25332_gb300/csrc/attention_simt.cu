@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[i][j] = k0 + tx + 16 * j < min(lim[i], k_hi) ? x[i][j] * a.scale_log2 : -INFINITY;
+        x[i][j] = k0 + tx + 16 * j < min(lim[i], k_hi) ? __fmul_rn(x[i][j], a.scale_log2) : -INFINITY;  // as in the maximum
         mx = fmaxf(mx, x[i][j]);
       }
 #pragma unroll

@@ -675,13 +675,14 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           float t;
           uint32_t w[kT / 2];
 #pragma unroll 1
-          for (bool raise = __any_sync(0xffffffffu, m == -INFINITY && lim > 0 && row_live);;) {
+          for (bool raise = __any_sync(0xffffffffu, m == -INFINITY && lim > 0 && row_live), raised = false;;) {
             float v[kT];
             tmem_ld64(ts, v);
             tmem_ld64(ts + 64, v + 64);
             tc_wait_ld();
             if (masked) mask_from<kT>(v, lim);
             if (raise) {
+              raised = true;
               const float mn = fmaxf(m, max128(v) * sc);  // sc > 0: the maximum commutes with it
               const float f = m == mn ? 1.f : ex2_approx(m - mn);
               m = mn;
@@ -707,8 +708,10 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
             float s0, s1;
             unpack2(add2(s2[0], s2[1]), s0, s1);
             t = s0 + s1;
-            // against the tile's own maximum the sum is kT at most, so this ends
-            raise = __any_sync(0xffffffffu, row_live && t > kMostSum);
+            // Against the tile's own maximum the sum is about kT at most. (Where scores pass 2^28 the
+            // rounding of m alone may make more of it, up to infinity: not raised again. Such
+            // a sum cancels with O's, or the row is not finite and computed again.)
+            raise = !raised && __any_sync(0xffffffffu, row_live && t > kMostSum);
             if (!raise) break;
           }
           l += t;

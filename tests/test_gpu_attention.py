@@ -458,6 +458,42 @@ def test_decode_values_that_grow_along_the_keys(dtype, algo):
 
 
 @pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("power", [10, 14, 15, 16, 20, 30, 50])
+def test_scores_of_any_size(power, dtype, algo):
+    """Scores of 2^(2 power) and more, all exact and far apart, where a rounding of the maximum is
+    worth many powers of two: the weight lies on the keys that share the largest. (How evenly is
+    not said: parts are joined by log-sum-exps in 32 bits, whose last place is worth more than the
+    parts' numbers of such keys.)"""
+    g = gen(49)
+    n, page, H = 400, 16, 2
+    pages = n // page
+    c = torch.arange(n, device=DEV) % 7 + 1
+    c[::3] = 1 + torch.arange(len(c[::3]), device=DEV) // 60
+    K = torch.zeros(pages, page, H, DH, dtype=dtype, device=DEV)
+    K.view(n, H, DH)[..., 0] = (c * 2.0 ** power).to(dtype)[:, None]
+    V = randn(g, pages, page, H, DH, dtype=dtype)
+    Q = torch.zeros(4, 4, DH, dtype=dtype, device=DEV)
+    Q[..., 0] = 2.0 ** power
+    Q[2:, :, 0] = -(2.0 ** power)  # these rows' largest is that of c = 1
+    args = (K.view(n, H, DH), V.view(n, H, DH))
+    whole = P.provip_prompt_attention(Q, *args, i32([0]), i32([4]), i32([0]), i32([n]), 4, n, causal=False, algo=algo)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None].expand(4, -1).contiguous()
+    step = P.provip_decode_attention(Q, K, V, table, i32([n] * 4), n, algo=algo)
+    torch.cuda.synchronize()
+    for r in (whole, step):
+        for t in range(4):
+            top = c == (c.max() if t < 2 else c.min())
+            x = (1 if t < 2 else -1) * float(c[top][0]) * 2.0 ** (2 * power) * DH ** -0.5
+            for h in range(4):
+                v = args[1][top, h // 2].double()
+                # a mean of them, with bf16 weights and a bf16 output
+                o, slack = r["out"][t, h].double(), 2.0 ** -7 * v.abs().amax(0) + 2.0 ** -12
+                assert ((o >= v.amin(0) - slack) & (o <= v.amax(0) + slack)).all(), (t, h)
+                lse = x + math.log(int(top.sum()))
+                assert abs(float(r["lse"][t, h]) - lse) <= abs(lse) * 2.0 ** -21, (t, h)
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
 @pytest.mark.parametrize("prefix", [0, 64])
 def test_decode_first_scores_minus_infinity(prefix, dtype, algo):
     """the first tiles have no weight, and the scores behind them lie where 2^score underflows"""
