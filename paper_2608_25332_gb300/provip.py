@@ -155,8 +155,8 @@ def _ptr_host_ok(t):
 def _stream(device):
     """The device's current stream as torch has it. (torch.cuda.current_stream builds an object
     around the same handle, 2 us of a 10 us call; it is the way where the handle has no
-    accessor.)"""
-    if _raw_stream is None:
+    accessor, and for a device given by its name or number.)"""
+    if _raw_stream is None or not isinstance(device, torch.device):
         return torch.cuda.current_stream(device).cuda_stream
     return _raw_stream(device.index if device.index is not None else torch.cuda.current_device())
 
