@@ -46,7 +46,7 @@ class QuestionCache:
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=dev)
         self.planner = P.PageTables(B, page_size, B * max_len if max_new is None else max_new, dev)
         self.prefix, self.prefix_len, self.prefix_table = [], 0, None
-        self.plan = None
+        self.plan = self.slots = None
         self._steps = {}
 
     def set_prefix(self, K, V):
@@ -69,7 +69,7 @@ class QuestionCache:
         them; -1 returns an answered question's pages (its slot can take another question).
         A question that the free pages do not suffice for keeps its length: read kv_len where
         that can happen."""
-        self.new_len = new_len
+        self.new_len, self.slots = new_len, None
         self.plan = self.planner(self.kv_len, new_len, self.free, self.n_free, self.tables, inplace=True)
         return self.plan
 
@@ -98,7 +98,17 @@ class QuestionCache:
             step = self._steps["decode"] = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len,
                                                              None, self.dtype, self.device, self.algo, want_lse=False)
         kp, vp = self.pools[layer]
-        # packed rows skip the ended questions; request b's token is row row_start[b]
-        slots = torch.where(self.new_len > 0, self.plan["slot_map"][:self.B][self.plan["row_start"][:-1].clamp(max=self.B - 1)], -1)
-        P.provip_kv_append(K, V, slots, kp, vp)
+        if self.slots is None:  # (the same for every layer of the step)
+            self.slots = self._token_slots()
+        P.provip_kv_append(K, V, self.slots, kp, vp)
         return step(Q, kp, vp, self.tables, self.kv_len, self.prefix_table if self.prefix_len else None)["out"]
+
+    def _token_slots(self):
+        """Slots of the questions' new tokens in request order, -1 for a question without one.
+        Packed rows skip such questions: the token of question b is row row_start[b], which for
+        those behind the step's last row may lie past the map's end (it has max_new slots)."""
+        rows, slots = self.plan["row_start"][:-1], self.plan["slot_map"]
+        n = slots.numel()
+        if n == 0:
+            return torch.full_like(rows, -1)
+        return torch.where((self.new_len > 0) & (rows < n), slots[rows.clamp(max=n - 1)], -1)

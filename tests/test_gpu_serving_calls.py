@@ -1,0 +1,89 @@
+"""QuestionCache's calls on the GPU, at the steps and sizes where they could go wrong, against
+attention over the rows themselves in 64 bits (bounds: attention_ref.py)."""
+import pytest
+import torch
+
+from attention_ref import DH, attend
+from paper_2608_25332_gb300 import provip as P
+from paper_2608_25332_gb300.serving import QuestionCache
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DTYPES = [torch.float32, torch.bfloat16]
+H_Q, H_KV, PAGE = 8, 2, 16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    import __graft_entry__
+    __graft_entry__.build()
+    P.provip_device_status(clear=True)
+    yield
+    rc, bits = P.provip_device_status(clear=True)
+    assert rc == 0 and bits == 0, f"device status {rc} {bits}"
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+class Run:
+    """A cache of one layer and what its questions hold."""
+
+    def __init__(self, dtype, B=8, n_pages=60, max_len=70, prefix=37, **kw):
+        self.g, self.dtype, self.B = torch.Generator(device=DEV).manual_seed(5), dtype, B
+        self.cache = QuestionCache(1, B, H_Q, H_KV, PAGE, n_pages, max_len, dtype, DEV, **kw)
+        self.rows = [[self.rand(0, H_KV)] * 2 for _ in range(B)]
+        self.set_prefix(prefix)
+
+    def rand(self, n, h):
+        return torch.randn(n, h, DH, generator=self.g, device=DEV).to(self.dtype)
+
+    def set_prefix(self, n):
+        self.prefix = [self.rand(n, H_KV) for _ in range(2)]
+        given = [x.clone() for x in self.prefix]
+        self.cache.set_prefix([given[0]], [given[1]])
+        return given
+
+    def begin(self, new):
+        self.new = new
+        self.cache.begin(i32(new))
+        self.rows = [[x[:0] for x in r] if n < 0 else r for n, r in zip(new, self.rows)]
+
+    def near(self, out, b, q):
+        k, v = (torch.cat([p, r]) for p, r in zip(self.prefix, self.rows[b]))
+        for h in range(H_Q):
+            kv = h * H_KV // H_Q
+            o, _, bound, _ = attend(q[None, h], k[:, kv], v[:, kv], torch.zeros(1, len(k), dtype=torch.bool, device=DEV), DH ** -0.5,
+                                    self.dtype, self.dtype == torch.bfloat16)
+            assert ((out[None, h].double() - o).abs() <= bound).all(), (b, h)
+
+    def prompt(self, pad=0):
+        T, at = sum(max(n, 0) for n in self.new), 0
+        q, k, v = self.rand(T + pad, H_Q), self.rand(T + pad, H_KV), self.rand(T + pad, H_KV)
+        out = self.cache.prompt(0, q, k, v)
+        for b, n in enumerate(self.new):
+            for i in range(at, at + max(n, 0)):
+                self.rows[b] = [torch.cat([r, x[i:i + 1]]) for r, x in zip(self.rows[b], (k, v))]
+                self.near(out[i], b, q[i])
+            at += max(n, 0)
+
+    def decode(self):
+        q, k, v = self.rand(self.B, H_Q), self.rand(self.B, H_KV), self.rand(self.B, H_KV)
+        out = self.cache.decode(0, q, k, v)
+        for b, n in enumerate(self.new):
+            if n > 0:
+                self.rows[b] = [torch.cat([r, x[b:b + 1]]) for r, x in zip(self.rows[b], (k, v))]
+            self.near(out[b], b, q[b])
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new", [[1, 1, 1, 1, 0, 0, 0, 0], [1, -1, 1, 0, 0, 1, -1, 0], [0] * 8])
+def test_decode_with_fewer_slots_than_questions(new, dtype):
+    """a step's slots are fewer than the questions, and idle or ended ones follow its last row"""
+    r = Run(dtype, max_new=4)
+    r.begin([1, 0, 2, 0, 1, 0, 0, 0])
+    r.prompt()
+    r.begin(new)
+    r.decode()

@@ -1,0 +1,89 @@
+"""QuestionCache's calls against attention over the rows themselves (CPU: the binding's calls
+are the model's, cache_model.py)."""
+import pytest
+import torch
+
+from cache_model import DH, Model
+from paper_2608_25332_gb300.serving import QuestionCache
+
+H_Q, H_KV, PAGE, LAYERS = 4, 2, 8, 2
+
+
+class Run:
+    """A cache and what its questions hold."""
+
+    def __init__(self, monkeypatch, B=8, n_pages=60, max_len=40, prefix=11, **kw):
+        self.model, self.g, self.B = Model(monkeypatch), torch.Generator().manual_seed(1), B
+        self.cache = QuestionCache(LAYERS, B, H_Q, H_KV, PAGE, n_pages, max_len, torch.float32, "cpu", **kw)
+        self.rows = [[[torch.zeros(0, H_KV, DH)] * 2 for _ in range(B)] for _ in range(LAYERS)]
+        self.prefix = [[torch.zeros(0, H_KV, DH)] * 2 for _ in range(LAYERS)]
+        if prefix:
+            self.set_prefix(prefix)
+
+    def rand(self, n, h):
+        return torch.randn(n, h, DH, generator=self.g)
+
+    def set_prefix(self, n):
+        self.prefix = [[self.rand(n, H_KV) for _ in range(2)] for _ in range(LAYERS)]
+        given = [[p[i].clone() for p in self.prefix] for i in range(2)]
+        self.cache.set_prefix(*given)
+        return given
+
+    def begin(self, new):
+        self.new = new
+        self.cache.begin(torch.tensor(new, dtype=torch.int32))
+        self.rows = [[[x[:0] for x in r] if n < 0 else r for n, r in zip(new, layer)] for layer in self.rows]
+
+    def want(self, layer, b, q):
+        k, v = (torch.cat([p, r]) for p, r in zip(self.prefix[layer], self.rows[layer][b]))
+        return Model.attend(q, k, v, DH ** -0.5)
+
+    def prompt(self, pad=0, **kw):
+        T = sum(max(n, 0) for n in self.new)
+        for layer in range(LAYERS):
+            q, k, v = self.rand(T + pad, H_Q), self.rand(T + pad, H_KV), self.rand(T + pad, H_KV)
+            out, at = self.cache.prompt(layer, q, k, v, **kw), 0
+            for b, n in enumerate(self.new):
+                for i in range(at, at + max(n, 0)):
+                    self.rows[layer][b] = [torch.cat([r, x[i:i + 1]]) for r, x in zip(self.rows[layer][b], (k, v))]
+                    assert torch.allclose(out[i], self.want(layer, b, q[i])), (layer, b, i)
+                at += max(n, 0)
+        assert not self.model.reports
+
+    def decode(self):
+        for layer in range(LAYERS):
+            q, k, v = self.rand(self.B, H_Q), self.rand(self.B, H_KV), self.rand(self.B, H_KV)
+            out = self.cache.decode(layer, q, k, v)
+            for b, n in enumerate(self.new):
+                if n > 0:
+                    self.rows[layer][b] = [torch.cat([r, x[b:b + 1]]) for r, x in zip(self.rows[layer][b], (k, v))]
+                assert torch.allclose(out[b], self.want(layer, b, q[b])), (layer, b)
+        assert not self.model.reports
+
+
+def test_prompts_and_decoding(monkeypatch):
+    r = Run(monkeypatch)
+    r.begin([3, 0, 9, 1, 0, 17, 2, 0])
+    r.prompt()
+    for _ in range(3):
+        r.begin([1, 0, 1, 1, 0, 1, 1, 0])
+        r.decode()
+    r.begin([1, 0, -1, 1, 0, -1, 1, 0])
+    r.decode()
+
+
+@pytest.mark.parametrize("max_new", [4, 5, 8])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1, 0, 0, 0, 0], [1, -1, 1, 0, 0, 1, -1, 0], [0] * 8, [0, 0, 0, 0, 1, 1, 1, 1]])
+def test_decode_with_fewer_slots_than_questions(monkeypatch, max_new, new):
+    """a step's slots are fewer than the questions, and idle or ended ones follow its last row"""
+    r = Run(monkeypatch, max_new=max_new)
+    r.begin([1, 0, 2, 0, 1, 0, 0, 0])
+    r.prompt()
+    r.begin(new)
+    r.decode()
+
+
+def test_decode_without_slots(monkeypatch):
+    r = Run(monkeypatch, max_new=0)
+    r.begin([0] * 8)
+    r.decode()
