@@ -70,20 +70,26 @@ class QuestionCache:
         A question that the free pages do not suffice for keeps its length: read kv_len where
         that can happen."""
         self.new_len, self.slots = new_len, None
+        # rows of prompt(): -1, which is reported, for a question that holds tokens already
+        self.prompt_len = torch.where((new_len > 0) & (self.kv_len > 0), -1, new_len.clamp(min=0))
         self.plan = self.planner(self.kv_len, new_len, self.free, self.n_free, self.tables, inplace=True)
         return self.plan
 
     def prompt(self, layer, Q, K, V, max_rows=None):
         """Prompts of the step begun: the questions' rows packed in request order, Q [T, H_q, 128],
         K and V [T, H_kv, 128] (T >= the step's new tokens). Every row sees the prefix and the
-        rows of its question up to itself. max_rows: the longest question (default max_len)."""
+        step's rows of its question up to itself, so a question with new rows must hold no token
+        yet (one that was not begun, or ended by -1): what it holds lies in pages, which the
+        prompts' attention does not read. A question that does is reported in the device status,
+        its rows go into the cache, and their output is left untouched. max_rows: the longest
+        question (default max_len)."""
         T, longest = Q.shape[0], min(self.max_len, Q.shape[0]) if max_rows is None else int(max_rows)
         key = ("prompt", T, longest)
         step = self._steps.get(key)
         if step is None:
             step = self._steps[key] = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len,
                                                         True, None, self.dtype, self.device, self.algo, want_lse=False)
-        start, n = self.plan["row_start"], self.new_len.clamp(min=0)
+        start, n = self.plan["row_start"], self.prompt_len
         kp, vp = self.pools[layer]
         P.provip_kv_append(K, V, self.plan["slot_map"][:T], kp, vp)
         pre = self.prefix[layer] if self.prefix_len else (None, None)

@@ -87,3 +87,28 @@ def test_decode_with_fewer_slots_than_questions(new, dtype):
     r.prompt()
     r.begin(new)
     r.decode()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_prompt_behind_tokens_of_its_question_is_reported(dtype):
+    """prompt() sees the step's own rows and the prefix, none of the pages: a second turn is
+    reported, the other questions' rows are as ever"""
+    r = Run(dtype, B=3)
+    r.begin([5, 40, 0])
+    r.prompt()
+    r.begin([4, 0, 30])
+    q, k, v = r.rand(34, H_Q), r.rand(34, H_KV), r.rand(34, H_KV)
+    out = r.cache.prompt(0, q, k, v)
+    torch.cuda.synchronize()
+    rc, bits = P.provip_device_status(clear=True)
+    assert rc == P.ERR_INVALID_ARG and bits == P.DEVSTAT_BAD_ARG
+    for i in range(4, 34):
+        r.rows[2] = [torch.cat([x, y[i:i + 1]]) for x, y in zip(r.rows[2], (k, v))]
+        r.near(out[i], 2, q[i])
+    r.rows[0] = [torch.cat([x, y[:4]]) for x, y in zip(r.rows[0], (k, v))]
+    r.begin([1, 1, 1])  # the rows are in the cache all the same
+    r.decode()
+    r.begin([-1, 1, 0])  # an ended question's slot takes a prompt again
+    r.decode()
+    r.begin([21, 0, 0])
+    r.prompt()

@@ -87,3 +87,29 @@ def test_decode_without_slots(monkeypatch):
     r = Run(monkeypatch, max_new=0)
     r.begin([0] * 8)
     r.decode()
+
+
+def test_a_prompt_behind_tokens_of_its_question_is_reported(monkeypatch):
+    """prompt() sees the step's own rows and the prefix, none of the pages: a second turn is
+    reported and its rows are left untouched, the other questions' are as ever"""
+    r = Run(monkeypatch, B=3)
+    r.begin([5, 9, 0])
+    r.prompt()
+    r.begin([4, 0, 3])
+    q, k, v = r.rand(7, H_Q), r.rand(7, H_KV), r.rand(7, H_KV)
+    for layer in range(LAYERS):
+        out = r.cache.prompt(layer, q, k, v)
+        assert r.model.reports == ["sequence"]
+        r.model.reports.clear()
+        if layer == 0:
+            assert torch.isnan(out[:4]).all()
+        for i in range(4, 7):
+            r.rows[layer][2] = [torch.cat([x, y[i:i + 1]]) for x, y in zip(r.rows[layer][2], (k, v))]
+            assert torch.allclose(out[i], r.want(layer, 2, q[i]))
+        r.rows[layer][0] = [torch.cat([x, y[:4]]) for x, y in zip(r.rows[layer][0], (k, v))]
+    r.begin([1, 1, 1])  # the rows are in the cache all the same
+    r.decode()
+    r.begin([-1, 1, 0])  # an ended question's slot takes a prompt again
+    r.decode()
+    r.begin([6, 0, 0])
+    r.prompt()
