@@ -51,7 +51,8 @@ class QuestionCache:
 
     def set_prefix(self, K, V):
         """K, V: a [n, H_kv, 128] tensor per layer (for instance rows [:vis_start + keep] of a
-        compaction's K_out[b] and V_out[b]). Their pages come off the free stack and stay."""
+        compaction's K_out[b] and V_out[b]), copied here: they may change afterwards. Their pages
+        come off the free stack and stay."""
         n = K[0].shape[0]
         need = -(-n // self.page_size)
         one = P.PageTables(1, self.page_size, n, self.device)
@@ -61,7 +62,9 @@ class QuestionCache:
         self.n_free.copy_(plan["free_count"])
         for (kp, vp), k, v in zip(self.pools, K, V):
             P.provip_kv_append(k, v, plan["slot_map"], kp, vp)
-        self.prefix, self.prefix_len, self.prefix_table = list(zip(K, V)), n, table[0]
+        # prompts read rows of their own, not the caller's, which the next pruning may overwrite
+        self.prefix = [(k.clone(), v.clone()) for k, v in zip(K, V)]
+        self.prefix_len, self.prefix_table = n, table[0]
         self._steps.clear()
 
     def begin(self, new_len):

@@ -112,3 +112,17 @@ def test_a_prompt_behind_tokens_of_its_question_is_reported(dtype):
     r.decode()
     r.begin([21, 0, 0])
     r.prompt()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prompts_and_decoding_see_the_same_prefix(dtype):
+    """the rows given to set_prefix may be the outputs of a pruning step, which its next call
+    overwrites"""
+    r = Run(dtype, B=3)
+    r.begin([-1, -1, -1])
+    for x in r.set_prefix(53):
+        x.fill_(7.0)
+    r.begin([3, 0, 20])
+    r.prompt()
+    r.begin([1, 0, 1])
+    r.decode()

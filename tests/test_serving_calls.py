@@ -113,3 +113,17 @@ def test_a_prompt_behind_tokens_of_its_question_is_reported(monkeypatch):
     r.decode()
     r.begin([6, 0, 0])
     r.prompt()
+
+
+def test_prompts_and_decoding_see_the_same_prefix(monkeypatch):
+    """the rows given to set_prefix may be the outputs of a pruning step, which its next call
+    overwrites"""
+    r = Run(monkeypatch, prefix=0)
+    given = r.set_prefix(13)
+    for i in range(2):
+        for x in given[i]:
+            x.fill_(7.0)
+    r.begin([3, 0, 9, 1, 0, 17, 2, 0])
+    r.prompt()
+    r.begin([1, 0, 1, 1, 0, 1, 1, 0])
+    r.decode()
