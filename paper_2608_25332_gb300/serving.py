@@ -52,11 +52,16 @@ class QuestionCache:
     def set_prefix(self, K, V):
         """K, V: a [n, H_kv, 128] tensor per layer (for instance rows [:vis_start + keep] of a
         compaction's K_out[b] and V_out[b]), copied here: they may change afterwards. Their pages
-        come off the free stack and stay."""
+        come off the free stack and stay; more rows than the pool holds are refused. Where the
+        questions leave too few pages, the prefix gets none: every decode() then reports it in the
+        device status, and its result is meaningless."""
         n = K[0].shape[0]
-        need = -(-n // self.page_size)
+        need, pages = -(-n // self.page_size), self.free.numel()
+        if need > pages:
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: {n} rows take {need} pages, the pool has {pages}")
         one = P.PageTables(1, self.page_size, n, self.device)
-        table = torch.zeros(1, need, dtype=torch.int32, device=self.device)
+        # (-1: no page. Where the questions hold too many, the prefix gets none and decoding reports it)
+        table = torch.full((1, need), -1, dtype=torch.int32, device=self.device)
         zero = torch.zeros(1, dtype=torch.int32, device=self.device)
         plan = one(zero, torch.full_like(zero, n), self.free, self.n_free, table)
         self.n_free.copy_(plan["free_count"])

@@ -126,3 +126,20 @@ def test_prompts_and_decoding_see_the_same_prefix(dtype):
     r.prompt()
     r.begin([1, 0, 1])
     r.decode()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_prefix_that_the_pool_cannot_hold(dtype):
+    """refused where no pool state could hold it; where others hold the pages, reported by every
+    decoding instead of attending over a page of someone else's"""
+    r = Run(dtype, B=2, n_pages=6, prefix=3)
+    with pytest.raises(P.ProvipError, match="pages"):
+        r.set_prefix(6 * PAGE + 1)
+    r = Run(dtype, B=2, n_pages=7, prefix=3)
+    r.begin([40, 0])
+    r.set_prefix(5 * PAGE)
+    r.begin([1, 0])
+    r.cache.decode(0, r.rand(2, H_Q), r.rand(2, H_KV), r.rand(2, H_KV))
+    torch.cuda.synchronize()
+    rc, bits = P.provip_device_status(clear=True)
+    assert rc == P.ERR_INVALID_ARG and bits == P.DEVSTAT_BAD_ARG

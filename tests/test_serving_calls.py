@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from cache_model import DH, Model
+from paper_2608_25332_gb300 import provip as P
 from paper_2608_25332_gb300.serving import QuestionCache
 
 H_Q, H_KV, PAGE, LAYERS = 4, 2, 8, 2
@@ -127,3 +128,20 @@ def test_prompts_and_decoding_see_the_same_prefix(monkeypatch):
     r.prompt()
     r.begin([1, 0, 1, 1, 0, 1, 1, 0])
     r.decode()
+
+
+def test_a_prefix_that_the_pool_cannot_hold(monkeypatch):
+    """refused where no pool state could hold it; where others hold the pages, reported by every
+    decoding instead of attending over a page of someone else's"""
+    r = Run(monkeypatch, n_pages=6, prefix=0)
+    with pytest.raises(P.ProvipError, match="pages"):
+        r.set_prefix(6 * PAGE + 1)
+    assert r.cache.prefix_len == 0 and int(r.cache.n_free) == 6
+    r.prefix = [[torch.zeros(0, H_KV, DH)] * 2 for _ in range(LAYERS)]
+    r.begin([20, 0, 0, 0, 0, 0, 0, 0])  # three of the six pages
+    r.prompt()
+    r.set_prefix(4 * PAGE)
+    r.begin([1, 0, 0, 0, 0, 0, 0, 0])
+    r.cache.decode(0, r.rand(8, H_Q), r.rand(8, H_KV), r.rand(8, H_KV))
+    assert "page" in r.model.reports
+    assert int(r.cache.n_free) == 3
