@@ -46,30 +46,37 @@ class QuestionCache:
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=dev)
         self.planner = P.PageTables(B, page_size, B * max_len if max_new is None else max_new, dev)
         self.prefix, self.prefix_len, self.prefix_table = [], 0, None
+        self._prefix_held = torch.zeros(2, dtype=torch.int32, device=dev)  # rows of the prefix in its pages, 0
         self.plan = self.slots = None
         self._steps = {}
 
     def set_prefix(self, K, V):
         """K, V: a [n, H_kv, 128] tensor per layer (for instance rows [:vis_start + keep] of a
         compaction's K_out[b] and V_out[b]), copied here: they may change afterwards. Their pages
-        come off the free stack and stay; more rows than the pool holds are refused. Where the
-        questions leave too few pages, the prefix gets none: every decode() then reports it in the
-        device status, and its result is meaningless."""
+        come off the free stack, and those of the prefix before go back onto it (its questions
+        should have ended); more rows than the pool holds are refused. Where the questions leave
+        too few pages, the prefix gets none: every decode() then reports it in the device status,
+        and its result is meaningless."""
         n = K[0].shape[0]
         need, pages = -(-n // self.page_size), self.free.numel()
         if need > pages:
             raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: {n} rows take {need} pages, the pool has {pages}")
-        one = P.PageTables(1, self.page_size, n, self.device)
-        # (-1: no page. Where the questions hold too many, the prefix gets none and decoding reports it)
-        table = torch.full((1, need), -1, dtype=torch.int32, device=self.device)
-        zero = torch.zeros(1, dtype=torch.int32, device=self.device)
-        plan = one(zero, torch.full_like(zero, n), self.free, self.n_free, table)
+        # two requests of the tables: the prefix before, which ends, and this one. (-1: no page.
+        # Where the questions hold too many, the prefix gets none and decoding reports it)
+        before = 0 if self.prefix_table is None else self.prefix_table.numel()
+        table = torch.full((2, max(need, before)), -1, dtype=torch.int32, device=self.device)
+        if before:
+            table[0, :before] = self.prefix_table
+        new = torch.full((2,), n, dtype=torch.int32, device=self.device)
+        new[0].fill_(-1)
+        plan = P.PageTables(2, self.page_size, n, self.device)(self._prefix_held, new, self.free, self.n_free, table)
         self.n_free.copy_(plan["free_count"])
+        self._prefix_held[0].copy_(plan["kv_len"][1])
         for (kp, vp), k, v in zip(self.pools, K, V):
             P.provip_kv_append(k, v, plan["slot_map"], kp, vp)
         # prompts read rows of their own, not the caller's, which the next pruning may overwrite
         self.prefix = [(k.clone(), v.clone()) for k, v in zip(K, V)]
-        self.prefix_len, self.prefix_table = n, table[0]
+        self.prefix_len, self.prefix_table = n, table[1, :need]
         self._steps.clear()
 
     def begin(self, new_len):

@@ -143,3 +143,17 @@ def test_a_prefix_that_the_pool_cannot_hold(dtype):
     torch.cuda.synchronize()
     rc, bits = P.provip_device_status(clear=True)
     assert rc == P.ERR_INVALID_ARG and bits == P.DEVSTAT_BAD_ARG
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_another_prefix_returns_the_first_ones_pages(dtype):
+    r = Run(dtype, B=3, n_pages=12, prefix=30)
+    for n in (100, 5, 12 * PAGE, 1, 0, 33):  # (12 pages: all, those of the prefix before among them)
+        r.set_prefix(n)
+        held = -(-n // PAGE)
+        assert int(r.cache.n_free) == 12 - held
+        assert sorted(r.cache.free[:12 - held].tolist() + r.cache.prefix_table[:held].tolist()) == list(range(12))
+    r.begin([3, 0, 19])
+    r.prompt()
+    r.begin([1, 0, 1])
+    r.decode()

@@ -145,3 +145,28 @@ def test_a_prefix_that_the_pool_cannot_hold(monkeypatch):
     r.cache.decode(0, r.rand(8, H_Q), r.rand(8, H_KV), r.rand(8, H_KV))
     assert "page" in r.model.reports
     assert int(r.cache.n_free) == 3
+
+
+def test_another_prefix_returns_the_first_ones_pages(monkeypatch):
+    r = Run(monkeypatch, n_pages=12, prefix=30)
+    assert int(r.cache.n_free) == 8
+    for n in (70, 5, 96, 1, 0, 33, 33):  # (96: every page of the pool, those of the prefix before among them)
+        r.set_prefix(n)
+        assert int(r.cache.n_free) == 12 - -(-n // PAGE)
+        assert sorted(r.cache.free[:int(r.cache.n_free)].tolist() + r.cache.prefix_table[:-(-n // PAGE)].tolist()) == list(range(12))
+    r.begin([3, 0, 9, 1, 0, 10, 2, 0])  # the seven pages that are left
+    r.prompt()
+    r.begin([1, 0, 1, 1, 0, 1, 1, 0])
+    r.decode()
+    r.begin([-1, 0, -1, -1, 0, -1, -1, 0])
+    r.set_prefix(90)
+    r.begin([0, 2, 0, 0, 0, 0, 0, 0])  # the pool is all the prefix's
+    assert r.cache.kv_len.tolist() == [0] * 8 and int(r.cache.n_free) == 0
+    r.model.reports.clear()
+    # a prefix that got no pages has none to return
+    r.set_prefix(0)
+    r.begin([40, 0, 0, 0, 0, 0, 0, 0])
+    r.set_prefix(60)
+    assert int(r.cache.n_free) == 7 and r.cache.prefix_table.tolist()[:8] == [-1] * 8
+    r.set_prefix(56)
+    assert int(r.cache.n_free) == 0 and -1 not in r.cache.prefix_table.tolist()[:7]
