@@ -48,7 +48,7 @@ class QuestionCache:
         self.prefix, self.prefix_len, self.prefix_table = [], 0, None
         self._prefix_held = torch.zeros(2, dtype=torch.int32, device=dev)  # rows of the prefix in its pages, 0
         self.plan = self.slots = None
-        self._steps = {}
+        self._prompt = self._decode = None  # the steps' buffers: of the last size only
 
     def set_prefix(self, K, V):
         """K, V: a [n, H_kv, 128] tensor per layer (for instance rows [:vis_start + keep] of a
@@ -75,9 +75,11 @@ class QuestionCache:
         for (kp, vp), k, v in zip(self.pools, K, V):
             P.provip_kv_append(k, v, plan["slot_map"], kp, vp)
         # prompts read rows of their own, not the caller's, which the next pruning may overwrite
+        self._drop(*(x for kv in self.prefix for x in kv))
         self.prefix = [(k.clone(), v.clone()) for k, v in zip(K, V)]
         self.prefix_len, self.prefix_table = n, table[1, :need]
-        self._steps.clear()
+        self._drop(self._prompt, self._decode)
+        self._prompt = self._decode = None
 
     def begin(self, new_len):
         """The next step's new tokens per question (int32 [B] on the device): pages and slots for
@@ -97,32 +99,39 @@ class QuestionCache:
         yet (one that was not begun, or ended by -1): what it holds lies in pages, which the
         prompts' attention does not read. A question that does is reported in the device status,
         its rows go into the cache, and their output is left untouched. max_rows: the longest
-        question (default max_len)."""
+        question (default max_len). The result is overwritten by the next call (another layer's)."""
         T, longest = Q.shape[0], min(self.max_len, Q.shape[0]) if max_rows is None else int(max_rows)
-        key = ("prompt", T, longest)
-        step = self._steps.get(key)
-        if step is None:
-            step = self._steps[key] = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len,
-                                                        True, None, self.dtype, self.device, self.algo, want_lse=False)
+        if self._prompt is None or self._prompt.shape[0] != T or self._prompt.shape[4] != longest:
+            self._drop(self._prompt)
+            self._prompt = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len, True, None,
+                                             self.dtype, self.device, self.algo, want_lse=False)
         start, n = self.plan["row_start"], self.prompt_len
         kp, vp = self.pools[layer]
         P.provip_kv_append(K, V, self.plan["slot_map"][:T], kp, vp)
         pre = self.prefix[layer] if self.prefix_len else (None, None)
-        return step(Q, K, V, start, n, start, n, *pre)["out"]
+        return self._prompt(Q, K, V, start, n, start, n, *pre)["out"]
 
     def decode(self, layer, Q, K, V):
         """One token per question: Q [B, H_q, 128], K and V [B, H_kv, 128] in request order, all of
         the step's new lengths 1 (or -1, whose rows are skipped: their output is that of an empty
-        question)."""
-        step = self._steps.get("decode")
-        if step is None:
-            step = self._steps["decode"] = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len,
-                                                             None, self.dtype, self.device, self.algo, want_lse=False)
+        question). The result is overwritten by the next call."""
+        if self._decode is None:
+            self._decode = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len, None, self.dtype,
+                                             self.device, self.algo, want_lse=False)
         kp, vp = self.pools[layer]
         if self.slots is None:  # (the same for every layer of the step)
             self.slots = self._token_slots()
         P.provip_kv_append(K, V, self.slots, kp, vp)
-        return step(Q, kp, vp, self.tables, self.kv_len, self.prefix_table if self.prefix_len else None)["out"]
+        return self._decode(Q, kp, vp, self.tables, self.kv_len, self.prefix_table if self.prefix_len else None)["out"]
+
+    @staticmethod
+    def _drop(*held):
+        """Tensors, or steps with theirs, that the cache lets go of: their memory is handed out again
+        behind what the current stream has under way, whichever stream it was allocated on."""
+        for x in held:
+            for t in (x,) if isinstance(x, torch.Tensor) else () if x is None else (x.out, x.ws):
+                if t.is_cuda:
+                    t.record_stream(torch.cuda.current_stream(t.device))
 
     def _token_slots(self):
         """Slots of the questions' new tokens in request order, -1 for a question without one.

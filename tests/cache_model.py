@@ -2,6 +2,7 @@
 from their contract in include/provip.h, so that what calls them can be tested without a
 GPU. A condition that a kernel would report in the device status is listed in ``reports``."""
 import math
+import weakref
 
 import torch
 
@@ -25,9 +26,13 @@ class Model:
 
     def _bound(self, cls):
         def make(*a, **kw):
-            self.made.append(cls.__name__)
-            return cls(self, *a, **kw)
+            step = cls(self, *a, **kw)
+            self.made.append((cls.__name__, weakref.ref(step)))
+            return step
         return make
+
+    def kept(self, name):
+        return sum(n == name and step() is not None for n, step in self.made)
 
     @staticmethod
     def _rows(n, t, what):
@@ -95,12 +100,13 @@ class Model:
     class PromptAttention:
         def __init__(self, model, T_q, B, H_q, H_kv, q_len_max, k_len_max, prefix_len=0, causal=True, scale=None, dtype=None,
                      device="cpu", algo=0, want_lse=True):
-            self.model, self.shape, self.causal = model, (T_q, B, q_len_max, k_len_max, prefix_len), causal
+            self.model, self.shape, self.causal = model, (T_q, B, H_q, H_kv, q_len_max, k_len_max, prefix_len), causal
             self.scale = DH ** -0.5 if scale is None else scale
             self.out = torch.full((T_q, H_q, DH), math.nan, dtype=torch.float64)
+            self.ws = self.out[:0]
 
         def __call__(self, Q, K, V, q_start, q_len, k_start, k_len, K_prefix=None, V_prefix=None):
-            T_q, B, qm, km, n = self.shape
+            T_q, B, _, _, qm, km, n = self.shape
             if Q.shape[0] != T_q or qm > T_q or km > K.shape[0] or (n and (K_prefix is None or K_prefix.shape[0] < n)):
                 raise P.ProvipError(P.ERR_INVALID_ARG, "prompt_attention")
             for t in (q_start, q_len, k_start, k_len):
@@ -124,6 +130,7 @@ class Model:
             self.model, self.shape = model, (B, kv_len_max, prefix_len)
             self.scale = DH ** -0.5 if scale is None else scale
             self.out = torch.full((B, H_q, DH), math.nan, dtype=torch.float64)
+            self.ws = self.out[:0]
 
         def __call__(self, Q, k_pages, v_pages, block_table, kv_len, prefix_table=None):
             B, km, n = self.shape

@@ -157,3 +157,46 @@ def test_another_prefix_returns_the_first_ones_pages(dtype):
     r.prompt()
     r.begin([1, 0, 1])
     r.decode()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prompts_of_many_sizes_keep_one_set_of_buffers(dtype):
+    r = Run(dtype, B=2, n_pages=200, max_len=1200)
+    for n in (700, 1100, 1200):
+        r.begin([n, 0])
+        q, k, v = r.rand(n, H_Q), r.rand(n, H_KV), r.rand(n, H_KV)
+        r.cache.prompt(0, q, k, v)
+        r.begin([-1, 0])
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    for n in range(1000, 1100):
+        r.begin([n, 0])
+        r.cache.prompt(0, q[:n], k[:n], v[:n])
+        r.begin([-1, 0])
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() <= held
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_buffers_that_are_dropped_wait_for_their_stream(dtype):
+    """A step's workspace was allocated on another stream than the one that uses it last: once
+    it is dropped, the allocating stream gets its memory only behind that use."""
+    r = Run(dtype, B=1, n_pages=400, max_len=64, prefix=5000)  # few rows, many keys: parts in the workspace
+    r.begin([4])
+    q, k, v = r.rand(4, H_Q), r.rand(4, H_KV), r.rand(4, H_KV)
+    want = r.cache.prompt(0, q, k, v).clone()
+    new = [i32([x]) for x in (-1, 4, -1, 5)]
+    q5 = r.rand(5, H_Q)
+    side = torch.cuda.Stream(DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        r.cache.begin(new[0])
+        r.cache.begin(new[1])
+        torch.cuda._sleep(200_000_000)  # about a tenth of a second
+        got = r.cache.prompt(0, q, k, v)
+        r.cache.begin(new[2])
+        r.cache.begin(new[3])
+        r.cache.prompt(0, q5, q5[:, :H_KV], q5[:, :H_KV])  # drops the step of four rows
+    junk = [torch.full((1 << p,), 0xFF, dtype=torch.uint8, device=DEV) for p in range(9, 24) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(junk)

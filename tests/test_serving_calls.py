@@ -170,3 +170,14 @@ def test_another_prefix_returns_the_first_ones_pages(monkeypatch):
     assert int(r.cache.n_free) == 7 and r.cache.prefix_table.tolist()[:8] == [-1] * 8
     r.set_prefix(56)
     assert int(r.cache.n_free) == 0 and -1 not in r.cache.prefix_table.tolist()[:7]
+
+
+def test_prompts_of_many_sizes_keep_one_set_of_buffers(monkeypatch):
+    r = Run(monkeypatch, B=2)
+    for n in list(range(1, 12)) + [3, 3, 20]:
+        r.begin([n, 0])
+        r.prompt()
+        assert r.model.kept("PromptAttention") == 1
+        r.begin([-1, 0])
+        r.decode()
+    assert r.model.kept("DecodeAttention") == 1
