@@ -86,7 +86,7 @@ class QuestionCache:
         them; -1 returns an answered question's pages (its slot can take another question).
         A question that the free pages do not suffice for keeps its length: read kv_len where
         that can happen."""
-        self.new_len, self.slots = new_len, None
+        self.new_len, self.slots = new_len.clone(), None  # (the caller may write the next step's into it)
         # rows of prompt(): -1, which is reported, for a question that holds tokens already
         self.prompt_len = torch.where((new_len > 0) & (self.kv_len > 0), -1, new_len.clamp(min=0))
         self.plan = self.planner(self.kv_len, new_len, self.free, self.n_free, self.tables, inplace=True)

@@ -181,3 +181,20 @@ def test_prompts_of_many_sizes_keep_one_set_of_buffers(monkeypatch):
         r.begin([-1, 0])
         r.decode()
     assert r.model.kept("DecodeAttention") == 1
+
+
+def test_the_lengths_of_a_step_may_change_after_begin(monkeypatch):
+    """a caller may write the next step's lengths into the same tensor before this one's layers"""
+    r = Run(monkeypatch, B=3)
+    lens = torch.tensor([2, 0, 5], dtype=torch.int32)
+    r.new = lens.tolist()
+    r.cache.begin(lens)
+    lens.fill_(-1)
+    r.prompt()
+    lens.copy_(torch.tensor([1, 0, 1]))
+    r.new = lens.tolist()
+    r.cache.begin(lens)
+    lens.fill_(0)
+    r.decode()
+    r.begin([1, 0, 1])
+    r.decode()
