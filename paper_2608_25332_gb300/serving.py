@@ -29,24 +29,26 @@ class QuestionCache:
     """Paged keys and values of B concurrent questions over one shared prefix.
 
     layers: LLM layers behind the pruning; n_pages pages of page_size rows per layer, for the
-    prefix and the questions; max_len: own tokens of a question at most (prompt and answer);
-    max_new: new tokens of one step over all questions at most (default B * max_len).
+    prefix and the questions; max_len: own tokens of a question at most (prompt and answer),
+    rounded up to whole pages; max_new: new tokens of one step over all questions at most (default
+    B * max_len).
     """
 
     def __init__(self, layers, B, H_q, H_kv, page_size, n_pages, max_len, dtype=torch.bfloat16, device="cuda",
                  max_new=None, algo=P.ALGO_AUTO):
         dev = torch.device(device)
-        self.B, self.H_q, self.H_kv, self.page_size, self.max_len = int(B), int(H_q), int(H_kv), int(page_size), int(max_len)
+        self.B, self.H_q, self.H_kv, self.page_size = int(B), int(H_q), int(H_kv), int(page_size)
+        self.max_len = -(-int(max_len) // self.page_size) * self.page_size  # what the tables may hand out
         self.dtype, self.device, self.algo = dtype, dev, algo
         self.pools = [tuple(torch.zeros(n_pages, page_size, H_kv, 128, dtype=dtype, device=dev) for _ in range(2))
                       for _ in range(layers)]
         self.free = torch.arange(n_pages, dtype=torch.int32, device=dev)
         self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=dev)
-        self.tables = torch.zeros(B, -(-max_len // page_size), dtype=torch.int32, device=dev)
+        self.tables = torch.zeros(B, self.max_len // self.page_size, dtype=torch.int32, device=dev)
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=dev)
-        self.planner = P.PageTables(B, page_size, B * max_len if max_new is None else max_new, dev)
+        self.planner = P.PageTables(B, page_size, B * self.max_len if max_new is None else max_new, dev)
         self.prefix, self.prefix_len, self.prefix_table = [], 0, None
-        self._prefix_held = torch.zeros(2, dtype=torch.int32, device=dev)  # rows of the prefix in its pages, 0
+        self._prefix_held = torch.zeros(2, dtype=torch.int32, device=dev)  # rows that the prefix has in pages; 0
         self.plan = self.slots = None
         self._prompt = self._decode = None  # the steps' buffers: of the last size only
 

@@ -200,3 +200,15 @@ def test_buffers_that_are_dropped_wait_for_their_stream(dtype):
     junk = [torch.full((1 << p,), 0xFF, dtype=torch.uint8, device=DEV) for p in range(9, 24) for _ in range(4)]
     torch.cuda.synchronize()
     assert torch.equal(got, want) and len(junk)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_question_may_fill_its_last_page(dtype):
+    """the tables hand out whole pages: with max_len 20 and pages of 16 a question holds 32 tokens"""
+    r = Run(dtype, B=2, max_len=20)
+    r.begin([30, 0])
+    r.prompt()
+    for _ in range(2):
+        r.begin([1, 0])
+        r.decode()
+    assert r.cache.kv_len.tolist() == [32, 0]

@@ -198,3 +198,16 @@ def test_the_lengths_of_a_step_may_change_after_begin(monkeypatch):
     r.decode()
     r.begin([1, 0, 1])
     r.decode()
+
+
+def test_a_question_may_fill_its_last_page(monkeypatch):
+    """the tables hand out whole pages: with max_len 20 and pages of 8 a question holds 24 tokens"""
+    r = Run(monkeypatch, B=2, max_len=20)
+    r.begin([22, 0])
+    r.prompt()
+    for _ in range(2):
+        r.begin([1, 0])
+        r.decode()
+    assert r.cache.kv_len.tolist() == [24, 0]
+    r.begin([1, 0])  # its table is full
+    assert r.cache.kv_len.tolist() == [24, 0] and r.model.reports
