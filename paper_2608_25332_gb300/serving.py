@@ -109,7 +109,8 @@ class QuestionCache:
                                              self.dtype, self.device, self.algo, want_lse=False)
         start, n = self.plan["row_start"], self.prompt_len
         kp, vp = self.pools[layer]
-        P.provip_kv_append(K, V, self.plan["slot_map"][:T], kp, vp)
+        rows = min(T, self.planner.T_max)  # (rows behind the last question have no slot)
+        P.provip_kv_append(K[:rows], V[:rows], self.plan["slot_map"][:rows], kp, vp)
         pre = self.prefix[layer] if self.prefix_len else (None, None)
         return self._prompt(Q, K, V, start, n, start, n, *pre)["out"]
 

@@ -211,3 +211,13 @@ def test_a_question_may_fill_its_last_page(monkeypatch):
     assert r.cache.kv_len.tolist() == [24, 0]
     r.begin([1, 0])  # its table is full
     assert r.cache.kv_len.tolist() == [24, 0] and r.model.reports
+
+
+@pytest.mark.parametrize("pad", [0, 1, 9])
+def test_prompts_with_rows_behind_the_last_question(monkeypatch, pad):
+    """padding rows, more in all than the step's slots"""
+    r = Run(monkeypatch, B=3, max_new=12)
+    r.begin([4, 0, 8])
+    r.prompt(pad=pad)
+    r.begin([1, 1, 1])
+    r.decode()
