@@ -59,7 +59,9 @@ class QuestionCache:
         should have ended); more rows than the pool holds are refused. Where the questions leave
         too few pages, the prefix gets none: every decode() then reports it in the device status,
         and its result is meaningless."""
-        n = K[0].shape[0]
+        n = K[0].shape[0] if len(K) else 0
+        if len(K) != len(self.pools) or len(V) != len(K) or any(x.shape[0] != n for x in (*K, *V)):
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: K and V must be {len(self.pools)} tensors each, of as many rows")
         need, pages = -(-n // self.page_size), self.free.numel()
         if need > pages:
             raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: {n} rows take {need} pages, the pool has {pages}")

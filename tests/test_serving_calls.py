@@ -221,3 +221,15 @@ def test_prompts_with_rows_behind_the_last_question(monkeypatch, pad):
     r.prompt(pad=pad)
     r.begin([1, 1, 1])
     r.decode()
+
+
+def test_a_prefix_is_given_for_every_layer(monkeypatch):
+    r = Run(monkeypatch, B=2)
+    one, two = r.rand(5, H_KV), r.rand(6, H_KV)
+    for k, v in (([one], [one]), ([one] * 2, [one]), ([one] * 3, [one] * 3), ([one, two], [one, one]), ([one, one], [one, two]), ([], [])):
+        with pytest.raises(P.ProvipError):
+            r.cache.set_prefix(k, v)
+    r.begin([3, 2])  # nothing has changed
+    r.prompt()
+    r.begin([1, 1])
+    r.decode()
