@@ -119,15 +119,17 @@ class QuestionCache:
     def decode(self, layer, Q, K, V):
         """One token per question: Q [B, H_q, 128], K and V [B, H_kv, 128] in request order, all of
         the step's new lengths 1 (or -1, whose rows are skipped: their output is that of an empty
-        question). The result is overwritten by the next call."""
+        question; a longer one is reported in the device status and taken for an empty question).
+        The result is overwritten by the next call."""
         if self._decode is None:
             self._decode = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len, None, self.dtype,
                                              self.device, self.algo, want_lse=False)
         kp, vp = self.pools[layer]
         if self.slots is None:  # (the same for every layer of the step)
             self.slots = self._token_slots()
+            self.decode_len = torch.where(self.new_len > 1, -1, self.kv_len)  # -1: reported
         P.provip_kv_append(K, V, self.slots, kp, vp)
-        return self._decode(Q, kp, vp, self.tables, self.kv_len, self.prefix_table if self.prefix_len else None)["out"]
+        return self._decode(Q, kp, vp, self.tables, self.decode_len, self.prefix_table if self.prefix_len else None)["out"]
 
     @staticmethod
     def _drop(*held):

@@ -233,3 +233,19 @@ def test_a_prefix_is_given_for_every_layer(monkeypatch):
     r.prompt()
     r.begin([1, 1])
     r.decode()
+
+
+def test_decoding_more_than_one_token_of_a_question_is_reported(monkeypatch):
+    """its other new tokens have slots, but no rows: what lies there is not attended to"""
+    r = Run(monkeypatch, B=3)
+    r.begin([2, 3, 1])
+    r.prompt()
+    r.begin([1, 2, 1])
+    q, k, v = r.rand(3, H_Q), r.rand(3, H_KV), r.rand(3, H_KV)
+    for layer in range(LAYERS):
+        out = r.cache.decode(layer, q, k, v)
+        assert r.model.reports == ["kv_len"]
+        r.model.reports.clear()
+        for b in (0, 2):
+            r.rows[layer][b] = [torch.cat([x, y[b:b + 1]]) for x, y in zip(r.rows[layer][b], (k, v))]
+            assert torch.allclose(out[b], r.want(layer, b, q[b]))
