@@ -49,7 +49,10 @@ class QuestionCache:
         self.planner = P.PageTables(B, page_size, B * self.max_len if max_new is None else max_new, dev)
         self.prefix, self.prefix_len, self.prefix_table = [], 0, None
         self._prefix_held = torch.zeros(2, dtype=torch.int32, device=dev)  # rows that the prefix has in pages; 0
-        self.plan = self.slots = None
+        # a step's own tensors: its new tokens, prompt()'s rows, decode()'s slots and lengths (at one
+        # place for good, so that a layer's calls can be captured in a graph)
+        self.new_len, self.prompt_len, self.slots, self.decode_len = (torch.zeros_like(self.kv_len) for _ in range(4))
+        self.plan = None
         self._prompt = self._decode = None  # the steps' buffers: of the last size only
 
     def set_prefix(self, K, V):
@@ -90,10 +93,12 @@ class QuestionCache:
         them; -1 returns an answered question's pages (its slot can take another question).
         A question that the free pages do not suffice for keeps its length: read kv_len where
         that can happen."""
-        self.new_len, self.slots = new_len.clone(), None  # (the caller may write the next step's into it)
-        # rows of prompt(): -1, which is reported, for a question that holds tokens already
-        self.prompt_len = torch.where((new_len > 0) & (self.kv_len > 0), -1, new_len.clamp(min=0))
-        self.plan = self.planner(self.kv_len, new_len, self.free, self.n_free, self.tables, inplace=True)
+        self.new_len.copy_(new_len)  # (the caller may write the next step's into it)
+        # -1, which is reported: more than prompt() and decode() can do
+        self.prompt_len.copy_(torch.where((self.new_len > 0) & (self.kv_len > 0), -1, self.new_len.clamp(min=0)))
+        self.plan = self.planner(self.kv_len, self.new_len, self.free, self.n_free, self.tables, inplace=True)
+        self.decode_len.copy_(torch.where(self.new_len > 1, -1, self.kv_len))
+        self.slots.copy_(self._token_slots())
         return self.plan
 
     def prompt(self, layer, Q, K, V, max_rows=None):
@@ -125,9 +130,6 @@ class QuestionCache:
             self._decode = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len, None, self.dtype,
                                              self.device, self.algo, want_lse=False)
         kp, vp = self.pools[layer]
-        if self.slots is None:  # (the same for every layer of the step)
-            self.slots = self._token_slots()
-            self.decode_len = torch.where(self.new_len > 1, -1, self.kv_len)  # -1: reported
         P.provip_kv_append(K, V, self.slots, kp, vp)
         return self._decode(Q, kp, vp, self.tables, self.decode_len, self.prefix_table if self.prefix_len else None)["out"]
 

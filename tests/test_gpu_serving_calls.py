@@ -212,3 +212,28 @@ def test_a_question_may_fill_its_last_page(dtype):
         r.begin([1, 0])
         r.decode()
     assert r.cache.kv_len.tolist() == [32, 0]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_captured_layer_sees_the_steps_begun_after_it(dtype):
+    r = Run(dtype, B=4)
+    r.begin([3, 0, 20, 1])
+    r.prompt()
+    q, k, v = r.rand(4, H_Q), r.rand(4, H_KV), r.rand(4, H_KV)
+    r.begin([1, 0, 1, 1])
+    r.cache.decode(0, q, k, v)  # (its buffers)
+    r.rows = [[torch.cat([x, y[b:b + 1]]) for x, y in zip(rows, (k, v))] if r.new[b] > 0 else rows for b, rows in enumerate(r.rows)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = r.cache.decode(0, q, k, v)
+    for new in ([1, 0, 1, 1], [0, 0, -1, 1], [1, -1, 0, 1]):
+        r.begin(new)
+        for x, h in ((q, H_Q), (k, H_KV), (v, H_KV)):
+            x.copy_(r.rand(4, h))
+        graph.replay()
+        torch.cuda.synchronize()
+        for b, n in enumerate(new):
+            if n > 0:
+                r.rows[b] = [torch.cat([x, y[b:b + 1]]) for x, y in zip(r.rows[b], (k, v))]
+            r.near(out[b], b, q[b])
