@@ -581,6 +581,7 @@ __global__ void __launch_bounds__(kThr, 2)
           po[r] = val;
         }
       }
+      __syncwarp();  // every lane has read the unit
       if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
     }
     if (failed) ctl.fail = 1;

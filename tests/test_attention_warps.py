@@ -1,0 +1,23 @@
+"""Order within a warp in the attention kernels, read from their source (CPU only)."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2608_25332_gb300", "csrc")
+FILES = ["attention_tc.cu", "attention_decode_tc.cu"]
+
+
+def code(file):
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, file)).read())
+
+
+@pytest.mark.parametrize("file", FILES)
+def test_a_units_slot_is_handed_back_behind_a_warp_barrier(file):
+    """One lane hands the slot back for the warp: the other lanes' reads of it come before a
+    barrier of the warp, which is the statement before."""
+    src = code(file)
+    found = [m.start() for m in re.finditer(r"if \(lane == 0\) mbar_arrive\(&ctl\.u_empty", src)]
+    assert len(found) == (3 if file == "attention_tc.cu" else 2)
+    for at in found:
+        assert src[:at].rstrip().endswith("__syncwarp();"), src[at - 200:at + 60]
