@@ -338,19 +338,21 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
         s2[(e >> 1) & 1] = add2(s2[(e >> 1) & 1], v);  // not finite once an element is not
         unpack2(v, o[e], o[e + 1]);
       }
-      if (!row_live) continue;
-      if (partial) {
+      if (row_live) {
+        if (partial) {
 #pragma unroll
-        for (int e = 0; e < 64; e += 8) store32(dst + (c * 64 + e) * 4, reinterpret_cast<const uint32_t*>(o) + e, wide);
-      } else {
+          for (int e = 0; e < 64; e += 8) store32(dst + (c * 64 + e) * 4, reinterpret_cast<const uint32_t*>(o) + e, wide);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 64; e += 16) {
-          uint32_t w[8];
+          for (int e = 0; e < 64; e += 16) {
+            uint32_t w[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) w[k] = pack_bf16(o[e + 2 * k], o[e + 2 * k + 1]);
-          store32(dst + (c * 64 + e) * 2, w, wide);
+            for (int k = 0; k < 8; ++k) w[k] = pack_bf16(o[e + 2 * k], o[e + 2 * k + 1]);
+            store32(dst + (c * 64 + e) * 2, w, wide);
+          }
         }
       }
+      __syncwarp();  // the next round's load is the whole warp's
     }
     float s0, s1;
     unpack2(add2(s2[0], s2[1]), s0, s1);

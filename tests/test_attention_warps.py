@@ -21,3 +21,23 @@ def test_a_units_slot_is_handed_back_behind_a_warp_barrier(file):
     assert len(found) == (3 if file == "attention_tc.cu" else 2)
     for at in found:
         assert src[:at].rstrip().endswith("__syncwarp();"), src[at - 200:at + 60]
+
+
+@pytest.mark.parametrize("file", FILES)
+def test_no_lane_leaves_a_round_before_the_warps_tensor_memory_access(file):
+    """A lane that goes to the loop's next round by itself would meet an access that the whole warp
+    has to make together (.sync.aligned) alone: rounds with one have no condition of a lane's own
+    that ends them."""
+    src = code(file)
+    for m in re.finditer(r"\bfor \([^;{]*;[^;{]*;[^{]*\) \{", src):
+        depth, j = 0, src.index("{", m.start())
+        for j in range(j, len(src)):
+            depth += (src[j] == "{") - (src[j] == "}")
+            if depth == 0:
+                break
+        body = src[m.end():j]
+        if "tmem_ld" in body or "tmem_st" in body:
+            # (raise, live and the unit's fields are the warp's)
+            ends = re.findall(r"if \(([^;{}]*)\) (?:continue|break|return)\b", body)
+            for cond in ends:
+                assert "row_live" not in cond and "lane" not in cond, (file, cond)
