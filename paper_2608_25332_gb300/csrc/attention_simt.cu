@@ -235,7 +235,8 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       fine = fine && isfinite(o[j]);
     }
     float lse = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
-    if (live && fine && !isnan(lse)) {
+    fine = fine || isnan(l[i]);  // a NaN score, which masked ones are not: every element is NaN
+    if (live && fine) {
       if (a.n_part > 1) {
         float* po = a.part_o + ((size_t)(part0 + part) * a.T_q * a.H_q + row) * kHeadDim;
         store4(po + tx * 4, o);
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       }
     }
     // rows that are not finite, one at a time by the whole warp
-    unsigned bad = __ballot_sync(0xffffffffu, live && !(fine && !isnan(lse)));
+    unsigned bad = __ballot_sync(0xffffffffu, live && !fine);
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {
       if (!((bad >> (16 * half)) & 0xffffu)) continue;

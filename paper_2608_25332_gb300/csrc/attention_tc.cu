@@ -359,7 +359,8 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
     sum = s0 + s1;
   }
   tc_fence_before();  // O is read before the next unit's first product, which waits for p_full
-  const bool fine = l != 0.f && isfinite(sum) && isfinite(lse);
+  // a NaN sum is the row's own: no masked score, rescaling or overflow makes one (O times 1 / l is NaN throughout)
+  const bool fine = isnan(l) || (l != 0.f && isfinite(sum) && isfinite(lse));
   if (row_live && fine) {
     if (partial)
       a.part_lse[(size_t)x.part * n_rows + row] = lse;
@@ -689,7 +690,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
               const float f = m == mn ? 1.f : ex2_approx(m - mn);
               m = mn;
               if (j > 0) {
-                l *= f;
+                l = l == INFINITY ? l : l * f;  // (NaN is kept for a row that sees a NaN score)
                 scale_o(to, f);
                 raise = false;
                 continue;  // the scores are read again rather than kept over the call

@@ -1,0 +1,73 @@
+"""Attention over values and scores that are NaN, infinite or near the largest number, against
+the definition in 64 bits (bounds: attention_ref.py)."""
+import math
+
+import pytest
+import torch
+
+from attention_ref import DH, attend, check, hidden_mask
+from paper_2608_25332_gb300 import provip as P
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+FORMS = [(F32, P.ALGO_AUTO), (BF16, P.ALGO_SIMT), (BF16, P.ALGO_AUTO)]
+IDS = ["f32", "bf16_simt", "bf16"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    import __graft_entry__
+    __graft_entry__.build()
+    P.provip_device_status(clear=True)
+    yield
+    rc, bits = P.provip_device_status(clear=True)
+    assert rc == 0 and bits == 0, f"device status {rc} {bits}"
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def randn(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g, device=DEV).to(dtype)
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def tc(dtype, algo):
+    return dtype == BF16 and algo != P.ALGO_SIMT
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("n,lq,H", [(1500, 1500, 8), (3000, 20, 2)])
+def test_a_nan_key_costs_no_more_than_another(n, lq, H, dtype, algo):
+    """every row sees the key, so every row is NaN, which its own sum shows: nothing is computed
+    again (key by key, that took a thousand times as long). The second size has its keys
+    shared out over parts."""
+    g = gen(1)
+    Q, K, V = randn(g, lq, H, DH, dtype=dtype), randn(g, n, H, DH, dtype=dtype), randn(g, n, H, DH, dtype=dtype)
+    step = P.PromptAttention(lq, 1, H, H, lq, n, 0, True, None, dtype, DEV, algo)
+    args = i32([0]), i32([lq]), i32([0]), i32([n])
+
+    def best():
+        t = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            r = step(Q, K, V, *args)
+            b.record()
+            b.synchronize()
+            t.append(a.elapsed_time(b))
+        return min(t[1:]), r
+
+    clean, r = best()
+    assert torch.isfinite(r["out"]).all() and torch.isfinite(r["lse"]).all()
+    K[5, H - 1, 3] = math.nan
+    poisoned, r = best()
+    row = torch.arange(lq, device=DEV) + n - lq >= 5
+    assert torch.isnan(r["out"][row, H - 1]).all() and torch.isnan(r["lse"][row, H - 1]).all()
+    assert torch.isfinite(r["out"][:, :H - 1]).all() and torch.isfinite(r["out"][~row]).all() and torch.isfinite(r["lse"][~row]).all()
+    assert poisoned < 4 * clean + 0.05, (clean, poisoned)
