@@ -255,6 +255,7 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       }
     }
     // rows that are not finite, one at a time by the whole warp
+    __syncwarp();  // their stores above come first
     unsigned bad = __ballot_sync(0xffffffffu, live && !fine);
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {

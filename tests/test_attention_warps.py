@@ -41,3 +41,15 @@ def test_no_lane_leaves_a_round_before_the_warps_tensor_memory_access(file):
             ends = re.findall(r"if \(([^;{}]*)\) (?:continue|break|return)\b", body)
             for cond in ends:
                 assert "row_live" not in cond and "lane" not in cond, (file, cond)
+
+
+def test_rows_computed_again_follow_the_warps_stores():
+    """Rows that are not finite are stored by one set of lanes and again by another: a barrier of
+    the warp lies between."""
+    for file in ("attention_tc.cu", "attention_simt.cu"):
+        src = code(file)
+        again = [m.start() for m in re.finditer(r"attn_row_plain<[^;]*\(a, ", src)]
+        assert again
+        for at in again:
+            vote = src.rindex("__ballot_sync(", 0, at)
+            assert src[:src.rindex(";", 0, vote)].rstrip().endswith("__syncwarp()"), file
