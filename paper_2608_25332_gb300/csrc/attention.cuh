@@ -111,16 +111,18 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
 // warp: the plain definition, which no key outside the range touches. The tile kernels
 // weigh every value row of a tile, the hidden ones by zero; zero times an infinite or NaN
 // value is NaN, so a row that did not come out finite is computed again here. lane holds
-// elements 4 lane .. 4 lane + 3; returns the base-2 log-sum-exp (-inf: no weight at all).
+// elements 4 lane .. 4 lane + 3; returns the base-2 log-sum-exp (-inf: no weight at all). beat, if
+// any, is given the time every 64 keys.
 template <typename T>
 __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s, int n_prefix, int token, int h,
-                                             int lo, int hi, float* o) {
+                                             int lo, int hi, float* o, unsigned long long* beat) {
   const int lane = threadIdx.x & 31, g = h / (a.H_q / a.H_kv);
   float q[4], m = -INFINITY, l = 0.f;
   load4(static_cast<const T*>(a.Q) + (size_t)(s.q0 + token) * a.q_stride + (size_t)h * kHeadDim + lane * 4, q);
   o[0] = o[1] = o[2] = o[3] = 0.f;
   for (int j = lo; j < hi; ++j) {
     float k[4], v[4];
+    if (beat && lane == 0 && ((j - lo) & 63) == 0) *static_cast<volatile unsigned long long*>(beat) = global_timer_ns();
     const bool pre = j < n_prefix;
     load4((pre ? attn_prefix_row<T>(a, false, j, g) : attn_own_row<T>(a, s, false, j - n_prefix, g)) + lane * 4, k);
     load4((pre ? attn_prefix_row<T>(a, true, j, g) : attn_own_row<T>(a, s, true, j - n_prefix, g)) + lane * 4, v);

@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       const int rb = __shfl_sync(0xffffffffu, r, 16 * half), tb = rb / R, hb = g * R + rb % R;
       const int hi = min(__shfl_sync(0xffffffffu, lim[i], 16 * half), k_hi);
       float ob[4];
-      float lb = attn_row_plain<T>(a, s, P, tb, hb, k_lo, hi, ob);
+      float lb = attn_row_plain<T>(a, s, P, tb, hb, k_lo, hi, ob, nullptr);
       const size_t rowb = (size_t)(s.q0 + tb) * a.H_q + hb;
       if (a.n_part > 1) {
         store4(a.part_o + ((size_t)(part0 + part) * a.T_q * a.H_q + rowb) * kHeadDim + lane * 4, ob);

@@ -23,7 +23,8 @@
 // SM (NQ = 1, two CTAs).
 // Value rows of a tile past the sequence's end (another sequence's, padding, a page's unused
 // slots, a page not loaded) are zeroed in shared memory before the product.
-// Every wait is bounded; a timeout sets the device error word and the roles drain.
+// Every wait is bounded, from the last sign of rows computed again on (mbar_wait_beat); a timeout sets
+// the device error word and the roles drain.
 #include "attention_tc.cuh"
 
 namespace provip {
@@ -76,6 +77,7 @@ struct Ctl {
   uint64_t q_full, q_empty;
   uint64_t full[kSteps], empty[kSteps];
   uint64_t s_full[NQ], p_full[NQ], o_full[NQ];
+  unsigned long long beat;  // when rows were last known to be computed again (mbar_wait_beat)
   uint32_t tmem;
   volatile int fail;
 };
@@ -297,7 +299,7 @@ __device__ __forceinline__ void store32(char* p, const uint32_t* r, bool wide) {
 // as pairs of 16 bytes they had made the pass of 8 prompts 3% longer.
 template <int NQ>
 __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, int i, int tok_in, int hid, float m,
-                                         float l, uint32_t to) {
+                                         float l, uint32_t to, unsigned long long* beat) {
   const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
   const int R = a.group, hd = r - tok_in * R;
   const int nt = x.nt[i];
@@ -376,7 +378,7 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
     const int tk = __shfl_sync(0xffffffffu, tok, src), hh = __shfl_sync(0xffffffffu, h, src);
     const int khi = __shfl_sync(0xffffffffu, hi, src);
     float o[4];
-    float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, o);
+    float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, o, beat);
     const size_t rw = (size_t)(x.s.q0 + tk) * a.H_q + hh;
     if (partial) {
       store4(a.part_o + ((size_t)x.part * n_rows + rw) * kHeadDim + lane * 4, o);
@@ -425,6 +427,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       mbar_init(&ctl.o_full[i], 1);
     }
     ctl.fail = 0;
+    ctl.beat = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       auto two_on = [](uint32_t& st) { st = st + 2 < F::kStages ? st + 2 : st + 2 - F::kStages; };
       bool live = true;
       for (uint32_t n = 0; live; ++n) {
-        live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err);
+        live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err, &ctl.beat);
         const Unit<NQ>& x = ctl.board[n % kBoard];
         if (!live || x.g < 0) break;
         const int ntm = x.ntm;
@@ -461,16 +464,16 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
         if (ntm == 0) continue;
-        live = warp_wait(&ctl.q_full, pq, a.err);
+        live = warp_wait(&ctl.q_full, pq, a.err, &ctl.beat);
         pq ^= 1u;
         for (int j = 0; live && j <= ntm; ++j, ++step) {
-          live = warp_wait(&ctl.full[step % kSteps], (step / kSteps) & 1u, a.err);
+          live = warp_wait(&ctl.full[step % kSteps], (step / kSteps) & 1u, a.err, &ctl.beat);
           const uint64_t kd = kd0 + (uint64_t)(sk * (kStage >> 4)), vd = vd0 + (uint64_t)(sv * (kStage >> 4));
 #pragma unroll
           for (int i = 0; i < NQ; ++i) {
             const uint32_t ts = tmem + i * kT, to = tmem + (NQ + i) * kT;
             if (j > 0 && j <= nt[i]) {
-              if (live) live = warp_wait(&ctl.p_full[i], pp[i], a.err);
+              if (live) live = warp_wait(&ctl.p_full[i], pp[i], a.err, &ctl.beat);
               pp[i] ^= 1u;
               tc_fence_after();
               if (lead) {
@@ -526,7 +529,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
             user[i] = step + 1;
           }
         if (lane == 0 && before > 0)
-          ok = mbar_wait(&ctl.empty[(before - 1) % kSteps], ((before - 1) / kSteps) & 1u, a.err);
+          ok = mbar_wait_beat(&ctl.empty[(before - 1) % kSteps], ((before - 1) / kSteps) & 1u, a.err, &ctl.beat);
         __syncwarp();
         if (!__shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) return false;
         uint64_t* full = &ctl.full[step % kSteps];
@@ -548,7 +551,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         return true;
       };
       for (uint32_t n = 0; live; ++n) {
-        live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err);
+        live = warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err, &ctl.beat);
         if (!live) break;
         const Unit<NQ> x = ctl.board[n % kBoard];
         __syncwarp();
@@ -563,7 +566,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         ++step;
         bool ok = true;
         if (lane == 0) {
-          ok = mbar_wait(&ctl.q_empty, (n_q & 1u) ^ 1u, a.err);
+          ok = mbar_wait_beat(&ctl.q_empty, (n_q & 1u) ^ 1u, a.err, &ctl.beat);
           if (ok) {
             int tiles = 0;
 #pragma unroll
@@ -617,7 +620,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           loads += 2 * x.ntm;
           steps += x.ntm + 1;
         }
-        live = warp_wait(&ctl.u_empty[slot], ((k / kBoard) & 1u) ^ 1u, a.err);
+        live = warp_wait(&ctl.u_empty[slot], ((k / kBoard) & 1u) ^ 1u, a.err, &ctl.beat);
         if (live && lane == 0) {
           ctl.board[slot] = x;
           mbar_arrive(&ctl.u_full[slot]);
@@ -637,7 +640,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     uint32_t n_s = 0, n_o = 0;
     bool failed = false;
     for (uint32_t n = 0;; ++n) {
-      if (!warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err)) failed = true;
+      if (!warp_wait(&ctl.u_full[n % kBoard], (n / kBoard) & 1u, a.err, &ctl.beat)) failed = true;
       const Unit<NQ>& x = ctl.board[n % kBoard];
       if (failed || x.g < 0) break;
       const int nt = x.nt[i];
@@ -653,14 +656,14 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       int n_keys = pre_left > 0 ? x.n_prefix - x.t_lo * kT : x.s.k_len + pre_left * kT;  // from the tile on
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < nt; ++j) {
-        failed = !warp_wait(&ctl.s_full[i], n_s & 1u, a.err);
+        failed = !warp_wait(&ctl.s_full[i], n_s & 1u, a.err, &ctl.beat);
         ++n_s;
         if (failed) break;
         tc_fence_after();
         if (n_keys < kT) {
           // rows past the end: zero before the product reads them
           const uint32_t sv = (x.load0 + 2 * j + 1) % F::kStages, st = x.step0 + j + 1;
-          failed = !warp_wait(&ctl.full[st % kSteps], (st / kSteps) & 1u, a.err);
+          failed = !warp_wait(&ctl.full[st % kSteps], (st / kSteps) & 1u, a.err, &ctl.beat);
           if (failed) break;
           uint8_t* vs = kv + sv * kStage;
           for (int q = n_keys * 16 + r; q < kT * 16; q += 128)
@@ -730,12 +733,12 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       if (failed) break;
       // ---- epilogue: O / l to memory ----
       if (nt > 0) {
-        failed = !warp_wait(&ctl.o_full[i], n_o & 1u, a.err);
+        failed = !warp_wait(&ctl.o_full[i], n_o & 1u, a.err, &ctl.beat);
         ++n_o;
         if (failed) break;
         tc_fence_after();
       }
-      if (warp_live) finish_rows<NQ>(a, x, i, tok_in, hid, m, l, to);
+      if (warp_live) finish_rows<NQ>(a, x, i, tok_in, hid, m, l, to, &ctl.beat);
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
     }

@@ -53,3 +53,22 @@ def test_rows_computed_again_follow_the_warps_stores():
         for at in again:
             vote = src.rindex("__ballot_sync(", 0, at)
             assert src[:src.rindex(";", 0, vote)].rstrip().endswith("__syncwarp()"), file
+
+
+@pytest.mark.parametrize("file", ["attention_tc.cu"])
+def test_waits_outlast_rows_that_are_computed_again(file):
+    """A warp that computes rows again by the definition may take longer than a wait's limit (a
+    microsecond a key and row): the others' waits start again while it gets on."""
+    src = code(file)
+    assert not re.search(r"\bmbar_wait\(", src), "waits without the sign of rows under way"
+    assert "attn_row_plain" not in src or re.search(r"attn_row_plain<[^;]*&?(?:ctl\.)?beat\)", src)
+    tc = code("attention_tc.cuh")
+    wait = tc[tc.index("bool wait_over("):tc.index("bool warp_wait(")]
+    # gives up only where the last sign of them is a whole limit ago too (read before the time is,
+    # so that it is never ahead of it)
+    assert re.search(r"last = \*[^;]*\(beat\), now = global_timer_ns\(\);", wait)
+    assert re.search(r"if \(\(long long\)\(now - t0\) <= most \|\| \(long long\)\(now - last\) <= most\) return false;", wait)
+    assert "&& wait_over(t0, err, beat)) return false;" in wait and wait.count("return false;") == 2
+    plain = code("attention.cuh")
+    plain = plain[plain.index("attn_row_plain("):]
+    assert re.search(r"& 63\) == 0\) [^;]*\(beat\) = global_timer_ns\(\);", plain[:plain.index("\n}\n")])

@@ -71,3 +71,24 @@ def test_a_nan_key_costs_no_more_than_another(n, lq, H, dtype, algo):
     assert torch.isnan(r["out"][row, H - 1]).all() and torch.isnan(r["lse"][row, H - 1]).all()
     assert torch.isfinite(r["out"][:, :H - 1]).all() and torch.isfinite(r["out"][~row]).all() and torch.isfinite(r["lse"][~row]).all()
     assert poisoned < 4 * clean + 0.05, (clean, poisoned)
+
+
+def test_rows_computed_again_over_a_long_list():
+    """One infinite value that every row of a head sees: its rows are computed again key by key,
+    which takes longer than any one wait's limit, and nothing gives up on them."""
+    g = gen(2)
+    n, lq, H = 160000, 128, 80
+    Q = randn(g, lq, H, DH, dtype=BF16)
+    K = torch.empty(n, H, DH, dtype=BF16, device=DEV).normal_(generator=g)
+    V = torch.empty(n, H, DH, dtype=BF16, device=DEV).normal_(generator=g)
+    V[7, 1, 0] = math.inf
+    r = P.provip_prompt_attention(Q, K, V, i32([0]), i32([lq]), i32([0]), i32([n]), lq, n)
+    torch.cuda.synchronize()
+    assert P.provip_device_status() == (0, 0)
+    assert (r["out"][:, 1, 0] == math.inf).all()
+    V[7, 1, 0] = 0.0
+    for h in (1, 79):
+        ref = attend(Q[:, h], K[:, h], V[:, h], hidden_mask(lq, n, 0, True, DEV), DH ** -0.5, BF16, True)
+        out = r["out"][:, h].clone()
+        out[:, 0] = torch.where(out[:, 0] == math.inf, ref[0][:, 0].to(BF16), out[:, 0])
+        check(out, r["lse"][:, h], ref, f"head {h}")
