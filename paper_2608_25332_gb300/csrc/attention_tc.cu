@@ -23,8 +23,8 @@
 // SM (NQ = 1, two CTAs).
 // Value rows of a tile past the sequence's end (another sequence's, padding, a page's unused
 // slots, a page not loaded) are zeroed in shared memory before the product.
-// Every wait is bounded, from the last sign of rows computed again on (mbar_wait_beat); a timeout sets
-// the device error word and the roles drain.
+// Every wait is bounded, from the last sign of rows computed again on (mbar_wait_beat); one that gives
+// up sets the device error word and ends its role, and the other roles' waits then run out likewise.
 #include "attention_tc.cuh"
 
 namespace provip {
@@ -79,7 +79,6 @@ struct Ctl {
   uint64_t s_full[NQ], p_full[NQ], o_full[NQ];
   unsigned long long beat;  // when rows were last known to be computed again (mbar_wait_beat)
   uint32_t tmem;
-  volatile int fail;
 };
 
 constexpr uint32_t kIdescS = idesc_bf16_f32(kT, kT);
@@ -426,7 +425,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       mbar_init(&ctl.p_full[i], 4);
       mbar_init(&ctl.o_full[i], 1);
     }
-    ctl.fail = 0;
     ctl.beat = 0;
     fence_mbar_init();
   }
@@ -504,7 +502,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           if (j < ntm) two_on(sk);
         }
       }
-      if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 1) {
       // ---- TMA producer (the lanes share a tile's pages) ----
       uint32_t n_q = 0, st = 0, step = 0;
@@ -593,7 +590,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           if (live && more) live = load(x, x.t_lo + j + 1, false);
         }
       }
-      if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 2) {
       // ---- units of this CTA onto the board, ahead of those who work on them ----
       Walk w;
@@ -628,7 +624,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         __syncwarp();
         if (!more) break;
       }
-      if (!live) ctl.fail = 1;
     }
   } else {
     // ---- softmax: a thread per row ----
@@ -742,7 +737,6 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
     }
-    if (failed) ctl.fail = 1;
   }
   tc_fence_before();
   __syncthreads();

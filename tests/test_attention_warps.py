@@ -72,3 +72,14 @@ def test_waits_outlast_rows_that_are_computed_again(file):
     plain = code("attention.cuh")
     plain = plain[plain.index("attn_row_plain("):]
     assert re.search(r"& 63\) == 0\) [^;]*\(beat\) = global_timer_ns\(\);", plain[:plain.index("\n}\n")])
+
+
+@pytest.mark.parametrize("file", FILES)
+def test_a_flag_in_shared_memory_is_read(file):
+    """what a role leaves for the others is read by one of them"""
+    src = code(file)
+    struct = src[src.index("struct Ctl {"):]
+    struct = struct[:struct.index("\n};")]
+    for name in re.findall(r"\b(?:int|uint32_t|float) (\w+)(?:\[\w+\])*;", struct):
+        uses = re.findall(r"\bctl\." + name + r"\b(?!\s*(?:\[[^\]]*\])*\s*=[^=])", src)
+        assert uses, f"{file}: {name} is written and never read"
