@@ -109,17 +109,18 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
 
 // One row over keys [lo, hi) of its list (prefix keys, then own ones), key by key, by one
 // warp: the plain definition, which no key outside the range touches. The tile kernels
-// weigh every value row of a tile, the hidden ones by zero; zero times an infinite or NaN
-// value is NaN, so a row that did not come out finite is computed again here. lane holds
-// elements 4 lane .. 4 lane + 3; returns the base-2 log-sum-exp (-inf: no weight at all). beat, if
-// any, is given the time every 64 keys.
+// weigh every value row of a tile, the hidden ones by zero, and divide at the end; zero times an
+// infinite or NaN value is NaN, and a sum of values may pass the largest float where their mean does
+// not, so a row that did not come out finite is computed again here, with its sums in 64 bits. lane
+// holds elements 4 lane .. 4 lane + 3; returns the base-2 log-sum-exp (-inf: no weight at all).
+// beat, if any, is given the time every 64 keys.
 template <typename T>
 __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s, int n_prefix, int token, int h,
                                              int lo, int hi, float* o, unsigned long long* beat) {
   const int lane = threadIdx.x & 31, g = h / (a.H_q / a.H_kv);
-  float q[4], m = -INFINITY, l = 0.f;
+  float q[4], m = -INFINITY;
+  double l = 0., acc[4] = {0., 0., 0., 0.};
   load4(static_cast<const T*>(a.Q) + (size_t)(s.q0 + token) * a.q_stride + (size_t)h * kHeadDim + lane * 4, q);
-  o[0] = o[1] = o[2] = o[3] = 0.f;
   for (int j = lo; j < hi; ++j) {
     float k[4], v[4];
     if (beat && lane == 0 && ((j - lo) & 63) == 0) *static_cast<volatile unsigned long long*>(beat) = global_timer_ns();
@@ -129,21 +130,31 @@ __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s
     // (rounded as the maximum is: no fma with the subtraction below)
     const float x = __fmul_rn(warp_sum(fmaf(q[0], k[0], fmaf(q[1], k[1], fmaf(q[2], k[2], q[3] * k[3])))), a.scale_log2);
     if (x == -INFINITY) continue;
-    const float mn = fmaxf(m, x), r = exp2f(m - mn), p = exp2f(x - mn);
-    l = l * r + p;
+    if (x > m) {
+      const float r = exp2f(m - x);
+      m = x;
+      l *= r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = o[e] * r + p * v[e];
-    m = mn;
+      for (int e = 0; e < 4; ++e) acc[e] *= r;
+    }
+    const double w = exp2f(x - m);
+    l += w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = fma(w, (double)v[e], acc[e]);
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = l == 0.f ? 0.f : o[e] / l;
-  return l == 0.f ? -INFINITY : m + log2f(l);
+  for (int e = 0; e < 4; ++e) o[e] = l == 0. ? 0.f : (float)(acc[e] / l);
+  return l == 0. ? -INFINITY : m + log2f((float)l);
 }
 
 // Weighs n more parts of a row and adds them to s (by one warp): lse(p) in base 2 and 128 floats at part(p).
-// A round's loads are all under way before the first is used.
+// A round's loads are all under way before the first is used. The weights carry a factor of 2^-10:
+// a row has fewer than 2^10 parts (128 shared out, or 64 and the pieces of 304 spans), so they add up
+// to less than one and no sum of parts passes the largest float where their mean does not.
+constexpr float kJoinUnit = 1.f / 1024.f;
 struct Joined {
-  float o[4], w, m;  // weighted sum of lane's elements, sum of the weights 2^(lse - m)
+  float o[4], w, m;  // weighted sum of lane's elements, sum of the weights 2^(lse - m) kJoinUnit
+  __device__ __forceinline__ float lse() const { return m + log2f(w * (1.f / kJoinUnit)); }  // (base 2)
 };
 template <typename Lse, typename Part>
 __device__ __forceinline__ void join_parts(Joined& s, int n, Lse lse, Part part) {
@@ -171,7 +182,7 @@ __device__ __forceinline__ void join_parts(Joined& s, int n, Lse lse, Part part)
     for (int e = 0; e < 4; ++e) s.o[e] *= c;
 #pragma unroll
     for (int p = 0; p < kRound; ++p) {
-      const float w = exp2f(x[p] - base);
+      const float w = exp2f(x[p] - base) * kJoinUnit;
       s.w += w;
       if (w != 0.f) {  // (a part without weight may hold anything)
         s.o[0] = fmaf(w, v[p].x, s.o[0]);

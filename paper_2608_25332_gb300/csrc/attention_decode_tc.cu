@@ -655,7 +655,7 @@ __global__ void __launch_bounds__(256) attn_join_spans(const __grid_constant__ A
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = s.o[e] / den;
   store4(static_cast<__nv_bfloat16*>(a.out) + (size_t)b * a.o_stride + (size_t)h * kHeadDim + lane * 4, o);
-  if (lane == 0 && a.lse) a.lse[row] = s.w == 0.f ? (n_keys > 0 ? NAN : -INFINITY) : (s.m + log2f(s.w)) * kLn2;
+  if (lane == 0 && a.lse) a.lse[row] = s.w == 0.f ? (n_keys > 0 ? NAN : -INFINITY) : s.lse() * kLn2;
 }
 
 template <int R>

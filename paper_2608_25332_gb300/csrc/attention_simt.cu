@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(256) attn_join(const __grid_constant__ AttnArg
   for (int e = 0; e < 4; ++e) s.o[e] /= den;
   store4(static_cast<T*>(a.out) + (size_t)t * a.o_stride + (size_t)h * kHeadDim + lane * 4, s.o);
   if (lane == 0 && a.lse)
-    a.lse[row] = s.w == 0.f ? (n_vis > 0 ? NAN : -INFINITY) : (s.m + log2f(s.w)) * kLn2;
+    a.lse[row] = s.w == 0.f ? (n_vis > 0 ? NAN : -INFINITY) : s.lse() * kLn2;
 }
 
 template <typename T, bool PREFIX>

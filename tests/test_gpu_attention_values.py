@@ -92,3 +92,28 @@ def test_rows_computed_again_over_a_long_list():
         out = r["out"][:, h].clone()
         out[:, 0] = torch.where(out[:, 0] == math.inf, ref[0][:, 0].to(BF16), out[:, 0])
         check(out, r["lse"][:, h], ref, f"head {h}")
+
+
+def huge(g, *shape, dtype):
+    """values of 0.5 to 1 times 3e38, of one sign in the first half of a head's elements: no sum of two
+    of those is a finite float, every mean of them is"""
+    v = (0.5 + 0.5 * torch.rand(*shape, generator=g, device=DEV)) * 3e38
+    v[..., DH // 2:] *= torch.where(torch.rand(*shape[:-1], DH // 2, generator=g, device=DEV) < 0.5, -1.0, 1.0)
+    return v.to(dtype)
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("lq,lk,prefix,H_q,H_kv", [(300, 300, 0, 4, 2), (20, 3000, 0, 2, 2), (40, 40, 2500, 7, 1), (1, 2, 0, 1, 1)])
+def test_values_whose_sums_pass_the_largest_float(lq, lk, prefix, H_q, H_kv, dtype, algo):
+    """a row is a mean of values: it is finite where they are (the second and third sizes have
+    their keys shared out over parts)"""
+    g = gen(3)
+    Q, K, V = randn(g, lq, H_q, DH, dtype=dtype), randn(g, lk, H_kv, DH, dtype=dtype), huge(g, lk, H_kv, DH, dtype=dtype)
+    pre = (randn(g, prefix, H_kv, DH, dtype=dtype), huge(g, prefix, H_kv, DH, dtype=dtype)) if prefix else (None, None)
+    r = P.provip_prompt_attention(Q, K, V, i32([0]), i32([lq]), i32([0]), i32([lk]), lq, lk, *pre, algo=algo)
+    torch.cuda.synchronize()
+    for h in range(H_q):
+        kv = h * H_kv // H_q
+        k, v = (torch.cat([p[:, kv], x[:, kv]]) if prefix else x[:, kv] for p, x in zip(pre, (K, V)))
+        ref = attend(Q[:, h], k, v, hidden_mask(lq, lk, prefix, True, DEV), DH ** -0.5, dtype, tc(dtype, algo))
+        check(r["out"][:, h], r["lse"][:, h], ref, f"head {h}")
