@@ -405,6 +405,8 @@ int provip_prune_visual_heads(const void *Q, const void *K, const void *V, const
  * scale is the factor of the logits (1 / sqrt(d_h) as a rule), > 0.
  * A key that a row does not see never touches it, whatever it holds
  * (infinities and NaN too). A row that sees no key gets out = 0, lse = -inf.
+ * A row whose scores and values are finite is finite: where a sum of values
+ * passes the largest float it is computed again, with sums in 64 bits.
  * ---------------------------------------------------------------------- */
 
 /* Attention over whole prompts: B sequences of different lengths, packed or

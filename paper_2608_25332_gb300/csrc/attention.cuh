@@ -111,22 +111,28 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
 // warp: the plain definition, which no key outside the range touches. The tile kernels
 // weigh every value row of a tile, the hidden ones by zero, and divide at the end; zero times an
 // infinite or NaN value is NaN, and a sum of values may pass the largest float where their mean does
-// not, so a row that did not come out finite is computed again here, with its sums in 64 bits. lane
-// holds elements 4 lane .. 4 lane + 3; returns the base-2 log-sum-exp (-inf: no weight at all).
-// beat, if any, is given the time every 64 keys.
-template <typename T>
+// not, so a row that did not come out finite is computed again here, with its sums in 64 bits. A lane
+// gets E elements from col on (four: 4 lane); returns the base-2 log-sum-exp (-inf: no weight at
+// all). beat, if any, is given the time every 64 keys.
+template <typename T, int E = 4>
 __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s, int n_prefix, int token, int h,
-                                             int lo, int hi, float* o, unsigned long long* beat) {
+                                             int lo, int hi, int col, float* o, unsigned long long* beat) {
   const int lane = threadIdx.x & 31, g = h / (a.H_q / a.H_kv);
   float q[4], m = -INFINITY;
-  double l = 0., acc[4] = {0., 0., 0., 0.};
+  double l = 0., acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.;
   load4(static_cast<const T*>(a.Q) + (size_t)(s.q0 + token) * a.q_stride + (size_t)h * kHeadDim + lane * 4, q);
   for (int j = lo; j < hi; ++j) {
-    float k[4], v[4];
+    float k[4], v[E];
     if (beat && lane == 0 && ((j - lo) & 63) == 0) *static_cast<volatile unsigned long long*>(beat) = global_timer_ns();
     const bool pre = j < n_prefix;
     load4((pre ? attn_prefix_row<T>(a, false, j, g) : attn_own_row<T>(a, s, false, j - n_prefix, g)) + lane * 4, k);
-    load4((pre ? attn_prefix_row<T>(a, true, j, g) : attn_own_row<T>(a, s, true, j - n_prefix, g)) + lane * 4, v);
+    const T* pv = (pre ? attn_prefix_row<T>(a, true, j, g) : attn_own_row<T>(a, s, true, j - n_prefix, g)) + col;
+    if (E == 4)
+      load4(pv, v);
+    else
+      v[0] = (float)*pv;
     // (rounded as the maximum is: no fma with the subtraction below)
     const float x = __fmul_rn(warp_sum(fmaf(q[0], k[0], fmaf(q[1], k[1], fmaf(q[2], k[2], q[3] * k[3])))), a.scale_log2);
     if (x == -INFINITY) continue;
@@ -135,16 +141,35 @@ __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s
       m = x;
       l *= r;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] *= r;
+      for (int e = 0; e < E; ++e) acc[e] *= r;
     }
     const double w = exp2f(x - m);
     l += w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fma(w, (double)v[e], acc[e]);
+    for (int e = 0; e < E; ++e) acc[e] = fma(w, (double)v[e], acc[e]);
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = l == 0. ? 0.f : (float)(acc[e] / l);
+  for (int e = 0; e < E; ++e) o[e] = l == 0. ? 0.f : (float)(acc[e] / l);
   return l == 0. ? -INFINITY : m + log2f((float)l);
+}
+
+// Element col (a lane's own) of a request's row over its own keys [lo, hi), where it came out infinite
+// or NaN (odd) though the row's weights are finite: with values that are all finite it was their sum
+// that passed the largest float, and *v is the element with its sums in 64 bits (true); a value that
+// is not shows in the element as it is. By a warp, the head's (paged keys).
+template <typename T>
+__device__ __noinline__ bool attn_element_again(const AttnArgs& a, int b, int h, int lo, int hi, int col, bool odd,
+                                                float* v, unsigned long long* beat) {
+  const AttnSeq s = attn_seq(a, b);
+#pragma unroll 8
+  for (int j = lo; j < hi; ++j) {
+    if (beat && (threadIdx.x & 31) == 0 && ((j - lo) & 1023) == 0)
+      *static_cast<volatile unsigned long long*>(beat) = global_timer_ns();
+    odd = odd && isfinite((float)attn_own_row<T>(a, s, true, j, h / (a.H_q / a.H_kv))[col]);
+  }
+  if (!__any_sync(0xffffffffu, odd)) return false;
+  attn_row_plain<T, 1>(a, s, 0, 0, h, lo, hi, col, v, beat);
+  return odd;
 }
 
 // Weighs n more parts of a row and adds them to s (by one warp): lse(p) in base 2 and 128 floats at part(p).

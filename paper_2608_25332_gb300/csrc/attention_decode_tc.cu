@@ -22,7 +22,8 @@
 // pieces, at most two a CTA, which a second kernel joins. Two CTAs an SM, each with a ring
 // of three 32 KiB stages that TMA fills across units.
 // Roles: warps 0-3 softmax (thread = key, then element), warp 4 MMAs, warp 5 TMA.
-// Every wait is bounded; a timeout sets the device error word and the roles drain.
+// Every wait is bounded, from the last sign of elements computed again on (mbar_wait_beat); a timeout
+// sets the device error word and the roles drain.
 #include "attention_tc.cuh"
 
 namespace provip {
@@ -57,7 +58,8 @@ struct Ctl {
   uint64_t q_full[2], q_empty[2];
   uint64_t kv_full[kStages], kv_empty[kStages];
   uint64_t s_full[2], p_full[2];
-  uint64_t o_done[2];  // by the tile's parity: scores of tile n are issued past the product of n - 2, not of n - 1
+  uint64_t o_done[2];  // by the tile's parity
+  unsigned long long beat;  // when elements were last known to be computed again (mbar_wait_beat)
   float red[4][kHeads], red_w[4][kHeads], inv[kHeads];
   uint32_t tmem;
   volatile int fail;
@@ -144,6 +146,29 @@ __device__ __forceinline__ int tiles_before(int t, int lane, int& all) {
   return s - t;
 }
 
+// Elements of a finished piece that are infinite or NaN though their weights are finite: again
+// (attn_element_again). Reads them back from where this thread has stored them, which keeps all of
+// it out of the unit's loop (inside, 64 requests of 32 heads on 4 had taken 26.4 us instead of 25.9).
+template <int R>
+__device__ __noinline__ void elements_again(const AttnArgs& a, const AttnSpans& sp, const Piece& x, const float* inv,
+                                            unsigned long long* beat) {
+  const int r = threadIdx.x, lo = x.t_lo * kT, hi = lo + min(x.nt * kT, x.n_keys);
+  const bool last = x.whole && a.prefix_len == 0;
+  const size_t row0 = (size_t)x.b * a.H_q + x.g * R, slot = 2 * (size_t)blockIdx.x + (x.t_lo == 0 ? 1 : 0);
+  for (int h = 0; h < R; ++h) {
+    __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim + r;
+    float* po = x.whole ? sp.whole_o + (row0 + h) * kHeadDim + r : sp.piece_o + (slot * R + h) * kHeadDim + r;
+    const bool odd = isfinite(inv[h]) && !isfinite(last ? __bfloat162float(*op) : *po);
+    float v;
+    if (__any_sync(0xffffffffu, odd) && attn_element_again<__nv_bfloat16>(a, x.b, x.g * R + h, lo, hi, r, odd, &v, beat)) {
+      if (last)
+        *op = __float2bfloat16_rn(v);
+      else
+        *po = v;
+    }
+  }
+}
+
 template <int R>
 __global__ void __launch_bounds__(kThr, 2)
     attn_keys_tc(int G, const __grid_constant__ AttnArgs a, const __grid_constant__ AttnSpans sp,
@@ -183,6 +208,7 @@ __global__ void __launch_bounds__(kThr, 2)
       mbar_init(&ctl.kv_empty[s], 1);
     }
     ctl.fail = 0;
+    ctl.beat = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -207,7 +233,7 @@ __global__ void __launch_bounds__(kThr, 2)
     // S^T of tile n from unit buffer qb
     auto scores = [&](uint32_t t, uint32_t qb) {
       const uint32_t ld = 2 * t, st = ld % kStages;
-      live = live && warp_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
+      live = live && warp_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err, &ctl.beat);
       tc_fence_after();
       if (lead) {
         const uint64_t kd = kd0 + (uint64_t)(st * (kStage >> 4)), qd = qd0 + (uint64_t)(qb * (kQBytes >> 4));
@@ -221,8 +247,8 @@ __global__ void __launch_bounds__(kThr, 2)
     };
     auto values = [&](uint32_t t, bool first) {
       const uint32_t ld = 2 * t + 1, st = ld % kStages;
-      live = live && warp_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
-      live = live && warp_wait(&ctl.p_full[t & 1], (t >> 1) & 1u, a.err);
+      live = live && warp_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err, &ctl.beat);
+      live = live && warp_wait(&ctl.p_full[t & 1], (t >> 1) & 1u, a.err, &ctl.beat);
       tc_fence_after();
       if (lead) {
         const uint64_t vd = vd0 + (uint64_t)(st * (kStage >> 4)), pd = pd0 + (uint64_t)((t & 1) * (kPBytes >> 4));
@@ -236,13 +262,13 @@ __global__ void __launch_bounds__(kThr, 2)
       }
     };
     for (uint32_t u = 0; live; ++u) {
-      live = warp_wait(&ctl.u_full[u % kBoard], (u / kBoard) & 1u, a.err);
+      live = warp_wait(&ctl.u_full[u % kBoard], (u / kBoard) & 1u, a.err, &ctl.beat);
       const Piece& x = ctl.board[u % kBoard];
       if (!live || x.g < 0) break;
       const int nt = x.nt;
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
-      live = warp_wait(&ctl.q_full[u & 1], (u >> 1) & 1u, a.err);
+      live = warp_wait(&ctl.q_full[u & 1], (u >> 1) & 1u, a.err, &ctl.beat);
       for (int j = 0; live && j <= nt; ++j) {
         if (j > 0) values(n + j - 1, j == 1);
         if (j < nt) {
@@ -333,7 +359,7 @@ __global__ void __launch_bounds__(kThr, 2)
       }
       bool ok = true;
       if (lane == 0) {
-        ok = !ctl.fail && mbar_wait(&ctl.kv_empty[st], ph ^ 1u, a.err);
+        ok = !ctl.fail && mbar_wait_beat(&ctl.kv_empty[st], ph ^ 1u, a.err, &ctl.beat);
         if (ok) mbar_arrive_expect_tx(&ctl.kv_full[st], (uint32_t)(boxes * box * 256));
       }
       __syncwarp();
@@ -369,7 +395,7 @@ __global__ void __launch_bounds__(kThr, 2)
           nt_b = unit_tiles(k_len);
         }
       }
-      live = warp_wait(&ctl.u_empty[u % kBoard], ((u / kBoard) & 1u) ^ 1u, a.err);
+      live = warp_wait(&ctl.u_empty[u % kBoard], ((u / kBoard) & 1u) ^ 1u, a.err, &ctl.beat);
       if (!live) break;
       if (lane == 0) {
         ctl.board[u % kBoard] = x;
@@ -382,7 +408,7 @@ __global__ void __launch_bounds__(kThr, 2)
       if (!live) break;
       bool ok = true;
       if (lane == 0) {
-        ok = mbar_wait(&ctl.q_empty[u & 1], ((u >> 1) & 1u) ^ 1u, a.err);
+        ok = mbar_wait_beat(&ctl.q_empty[u & 1], ((u >> 1) & 1u) ^ 1u, a.err, &ctl.beat);
         if (ok) {
           mbar_arrive_expect_tx(&ctl.q_full[u & 1], R * 256);
           uint8_t* q = qs + (u & 1) * kQBytes;
@@ -426,7 +452,7 @@ __global__ void __launch_bounds__(kThr, 2)
     // met, and all of them leave before the next one
     bool failed = false;
     for (uint32_t u = 0;; ++u) {
-      if (!failed) failed = !mbar_wait(&ctl.u_full[u % kBoard], (u / kBoard) & 1u, a.err);
+      if (!failed) failed = !mbar_wait_beat(&ctl.u_full[u % kBoard], (u / kBoard) & 1u, a.err, &ctl.beat);
       failed = soft_any(failed);
       const Piece& x = ctl.board[u % kBoard];
       if (failed || x.g < 0) break;
@@ -441,7 +467,7 @@ __global__ void __launch_bounds__(kThr, 2)
       for (int j = 0; j < nt; ++j) {
         const uint32_t n = x.tile0 + j, buf = n & 1;
         const bool key = r < x.n_keys - j * kT;
-        if (!failed) failed = !mbar_wait(&ctl.s_full[buf], (n >> 1) & 1u, a.err);
+        if (!failed) failed = !mbar_wait_beat(&ctl.s_full[buf], (n >> 1) & 1u, a.err, &ctl.beat);
         __syncwarp();
         tc_fence_after();
         float s[8], p[R];
@@ -478,7 +504,7 @@ __global__ void __launch_bounds__(kThr, 2)
             for (int h = R; h < 8; ++h) f[h] = 1.f;
             if (j > 0 && any) {
               // O^T times f, once the product before is complete (the next waits for this P)
-              if (!failed) failed = !mbar_wait(&ctl.o_done[buf ^ 1], ((n - 1) >> 1) & 1u, a.err);
+              if (!failed) failed = !mbar_wait_beat(&ctl.o_done[buf ^ 1], ((n - 1) >> 1) & 1u, a.err, &ctl.beat);
               __syncwarp();
               tc_fence_after();
               float o[8];
@@ -512,7 +538,7 @@ __global__ void __launch_bounds__(kThr, 2)
           // value rows past the end: zero before the product reads them (neighbours in a warp
           // write neighbouring 16 bytes: a row each had cost a microsecond of bank conflicts)
           const uint32_t ld = 2 * n + 1, st = ld % kStages;
-          if (!failed) failed = !mbar_wait(&ctl.kv_full[st], (ld / kStages) & 1u, a.err);
+          if (!failed) failed = !mbar_wait_beat(&ctl.kv_full[st], (ld / kStages) & 1u, a.err, &ctl.beat);
           uint8_t* vs = kv + st * kStage;
           for (int q = max(x.n_keys - j * kT, 0) * 8 + r; q < kT * 8; q += 128) {
             *reinterpret_cast<uint4*>(vs + q * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -561,7 +587,7 @@ __global__ void __launch_bounds__(kThr, 2)
           a.lse[row0 + r] = lse * kLn2;
       }
       const uint32_t last_n = x.tile0 + nt - 1;
-      if (!failed) failed = !mbar_wait(&ctl.o_done[last_n & 1], (last_n >> 1) & 1u, a.err);
+      if (!failed) failed = !mbar_wait_beat(&ctl.o_done[last_n & 1], (last_n >> 1) & 1u, a.err, &ctl.beat);
       __syncwarp();
       tc_fence_after();
       soft_sync();
@@ -569,10 +595,12 @@ __global__ void __launch_bounds__(kThr, 2)
       tmem_ld8(to, o);
       tc_wait_ld();
       tc_fence_before();  // O^T is read before the next unit's first product, which waits for p_full
+      float not_fine = 0.f;  // NaN once a value is not finite
 #pragma unroll
       for (int h = 0; h < R; ++h) {
         // (an element without weight may hold anything)
         const float inv = ctl.inv[h], val = inv == 0.f ? 0.f : o[h] * inv;
+        not_fine = fmaf(val, 0.f, not_fine);
         if (last) {
           __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim;
           op[r] = __float2bfloat16_rn(val);
@@ -581,6 +609,7 @@ __global__ void __launch_bounds__(kThr, 2)
           po[r] = val;
         }
       }
+      if (__any_sync(0xffffffffu, isnan(not_fine))) elements_again<R>(a, sp, x, ctl.inv, &ctl.beat);
       __syncwarp();  // every lane has read the unit
       if (lane == 0) mbar_arrive(&ctl.u_empty[u % kBoard]);
     }

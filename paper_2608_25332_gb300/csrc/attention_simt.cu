@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kThr, 2) attn_tile_simt(const __grid_constant_
       const int rb = __shfl_sync(0xffffffffu, r, 16 * half), tb = rb / R, hb = g * R + rb % R;
       const int hi = min(__shfl_sync(0xffffffffu, lim[i], 16 * half), k_hi);
       float ob[4];
-      float lb = attn_row_plain<T>(a, s, P, tb, hb, k_lo, hi, ob, nullptr);
+      float lb = attn_row_plain<T>(a, s, P, tb, hb, k_lo, hi, lane * 4, ob, nullptr);
       const size_t rowb = (size_t)(s.q0 + tb) * a.H_q + hb;
       if (a.n_part > 1) {
         store4(a.part_o + ((size_t)(part0 + part) * a.T_q * a.H_q + rowb) * kHeadDim + lane * 4, ob);
@@ -372,6 +372,9 @@ __global__ void __launch_bounds__(kDecThr) attn_token_simt(const __grid_constant
       }
       const size_t row = (size_t)b * a.H_q + h0 + r;
       float val = sum == 0.f ? 0.f : acc / sum, lse = sum == 0.f ? -INFINITY : mx + log2f(sum);
+      const bool odd = sum != 0.f && isfinite(sum) && !isfinite(val);
+      float v;
+      if (__any_sync(0xffffffffu, odd) && attn_element_again<T>(a, b, h0 + r, k_lo, k_hi, threadIdx.x, odd, &v, nullptr)) val = v;
       if (a.n_part > 1) {
         a.part_o[((size_t)part * a.T_q * a.H_q + row) * kHeadDim + threadIdx.x] = val;
         if (threadIdx.x == 0) a.part_lse[(size_t)part * a.T_q * a.H_q + row] = lse;

@@ -377,7 +377,7 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
     const int tk = __shfl_sync(0xffffffffu, tok, src), hh = __shfl_sync(0xffffffffu, h, src);
     const int khi = __shfl_sync(0xffffffffu, hi, src);
     float o[4];
-    float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, o, beat);
+    float le = attn_row_plain<__nv_bfloat16>(a, x.s, x.n_prefix, tk, hh, lo, khi, lane * 4, o, beat);
     const size_t rw = (size_t)(x.s.q0 + tk) * a.H_q + hh;
     if (partial) {
       store4(a.part_o + ((size_t)x.part * n_rows + rw) * kHeadDim + lane * 4, o);

@@ -102,9 +102,6 @@ __device__ __forceinline__ bool mbar_wait_beat(uint64_t* bar, uint32_t parity, u
 }
 // every lane waits; the outcome is the warp's (and known to be the same in every lane, which
 // keeps the branches on it and the MMA operands in the uniform registers)
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned* err) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
-}
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned* err, const unsigned long long* beat) {
   return __all_sync(0xffffffffu, mbar_wait_beat(bar, parity, err, beat));
 }

@@ -55,7 +55,7 @@ def test_rows_computed_again_follow_the_warps_stores():
             assert src[:src.rindex(";", 0, vote)].rstrip().endswith("__syncwarp()"), file
 
 
-@pytest.mark.parametrize("file", ["attention_tc.cu"])
+@pytest.mark.parametrize("file", FILES)
 def test_waits_outlast_rows_that_are_computed_again(file):
     """A warp that computes rows again by the definition may take longer than a wait's limit (a
     microsecond a key and row): the others' waits start again while it gets on."""

@@ -117,3 +117,66 @@ def test_values_whose_sums_pass_the_largest_float(lq, lk, prefix, H_q, H_kv, dty
         k, v = (torch.cat([p[:, kv], x[:, kv]]) if prefix else x[:, kv] for p, x in zip(pre, (K, V)))
         ref = attend(Q[:, h], k, v, hidden_mask(lq, lk, prefix, True, DEV), DH ** -0.5, dtype, tc(dtype, algo))
         check(r["out"][:, h], r["lse"][:, h], ref, f"head {h}")
+
+
+def decode_case(g, lens, H_q, H_kv, prefix, dtype, values, page=16):
+    """the arguments of a decode call, and its keys and values a request"""
+    held, pre = [-(-n // page) for n in lens], -(-prefix // page)
+    order = torch.randperm(sum(held) + pre + 2, generator=g, device=DEV).to(torch.int32)
+    K, V = (torch.full((len(order), page, H_kv, DH), math.nan, dtype=dtype, device=DEV) for _ in range(2))
+    table = torch.full((len(lens), max(held) + 1), -1, dtype=torch.int32, device=DEV)
+    at = pre
+    seqs = []
+    for b, n in [(-1, prefix)] + list(enumerate(lens)):
+        pages = order[:pre] if b < 0 else order[at:at + held[b]]
+        k, v, j = randn(g, n, H_kv, DH, dtype=dtype), values(g, n, H_kv, DH, dtype=dtype), torch.arange(n, device=DEV)
+        K[pages.long()[j // page], j % page], V[pages.long()[j // page], j % page] = k, v
+        seqs.append((k, v))
+        if b >= 0:
+            table[b, :held[b]] = pages
+            at += held[b]
+    Q = randn(g, len(lens), H_q, DH, dtype=dtype)
+    kw = dict(prefix_table=order[:pre].clone(), prefix_len=prefix) if prefix else {}
+    return (Q, K, V, table, i32(lens), max(lens)), kw, [tuple(torch.cat(x) for x in zip(seqs[0], s)) for s in seqs[1:]]
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("lens,prefix,H_q,H_kv", [([2, 130, 700], 0, 4, 4), ([3000], 0, 7, 1), ([300] * 40, 0, 8, 4), ([1, 90], 700, 14, 2),
+                                                  ([5, 260], 300, 16, 1)])
+def test_decoding_values_whose_sums_pass_the_largest_float(lens, prefix, H_q, H_kv, dtype, algo):
+    """requests a CTA each, spans that cut them, a prefix, and groups of more than eight heads"""
+    args, kw, seqs = decode_case(gen(4), lens, H_q, H_kv, prefix, dtype, huge)
+    r = P.provip_decode_attention(*args, algo=algo, **kw)
+    torch.cuda.synchronize()
+    for b, (k, v) in enumerate(seqs):
+        for h in range(H_q):
+            kv = h * H_kv // H_q
+            ref = attend(args[0][b:b + 1, h], k[:, kv], v[:, kv], torch.zeros(1, len(k), dtype=torch.bool, device=DEV), DH ** -0.5, dtype,
+                         tc(dtype, algo))
+            check(r["out"][b:b + 1, h], r["lse"][b:b + 1, h], ref, f"request {b} head {h}")
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_decoding_infinite_values_that_are_seen(prefix, dtype, algo):
+    """they show in their element, and in no other"""
+    def values(g, *shape, dtype):
+        v = huge(g, *shape, dtype=dtype)
+        if shape[0]:
+            v[0, :, 3], v[0, :, 40] = math.inf, math.nan
+        return v
+
+    args, kw, seqs = decode_case(gen(5), [2, 130, 700], 14, 2, prefix, dtype, values)
+    r = P.provip_decode_attention(*args, algo=algo, **kw)
+    torch.cuda.synchronize()
+    assert (r["out"][..., 3] == math.inf).all() and torch.isnan(r["out"][..., 40]).all()
+    fine = torch.arange(DH, device=DEV)
+    fine = fine[(fine != 3) & (fine != 40)]
+    for b, (k, v) in enumerate(seqs):
+        for h in range(14):
+            v2 = v[:, h // 7].clone()
+            v2[:, [3, 40]] = 0.0
+            o, lse, bound, _ = attend(args[0][b:b + 1, h], k[:, h // 7], v2, torch.zeros(1, len(k), dtype=torch.bool, device=DEV),
+                                      DH ** -0.5, dtype, tc(dtype, algo))
+            out = r["out"][b:b + 1, h].double()
+            assert torch.isfinite(out[:, fine]).all() and ((out - o).abs() <= bound)[:, fine].all(), (b, h)
