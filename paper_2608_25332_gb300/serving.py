@@ -93,7 +93,10 @@ class QuestionCache:
         them; -1 returns an answered question's pages (its slot can take another question).
         A question that the free pages do not suffice for keeps its length: read kv_len where
         that can happen."""
-        self.new_len.copy_(new_len)  # (the caller may write the next step's into it)
+        if new_len.dtype is not torch.int32 or new_len.device != self.kv_len.device or not new_len.is_contiguous() or \
+                new_len.numel() < self.B:
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"begin: new_len must be a contiguous int32 tensor of {self.B} entries on {self.kv_len.device}")
+        self.new_len.copy_(new_len.view(-1)[:self.B])  # (the caller may write the next step's into it)
         # -1, which is reported: more than prompt() and decode() can do
         self.prompt_len.copy_(torch.where((self.new_len > 0) & (self.kv_len > 0), -1, self.new_len.clamp(min=0)))
         self.plan = self.planner(self.kv_len, self.new_len, self.free, self.n_free, self.tables, inplace=True)

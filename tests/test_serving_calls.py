@@ -249,3 +249,15 @@ def test_decoding_more_than_one_token_of_a_question_is_reported(monkeypatch):
         for b in (0, 2):
             r.rows[layer][b] = [torch.cat([x, y[b:b + 1]]) for x, y in zip(r.rows[layer][b], (k, v))]
             assert torch.allclose(out[b], r.want(layer, b, q[b]))
+
+
+def test_the_lengths_of_a_step_are_checked(monkeypatch):
+    """int32, one for every question: a shorter tensor is not spread over them"""
+    r = Run(monkeypatch, B=3)
+    for bad in (torch.tensor([1]), torch.tensor([1], dtype=torch.int32), torch.tensor([1, 1, 1]), torch.ones(2, dtype=torch.int32),
+                torch.ones(6, dtype=torch.int32)[::2], torch.tensor(1, dtype=torch.int32)):
+        with pytest.raises(P.ProvipError):
+            r.cache.begin(bad)
+    r.new = [2, 0, 1]
+    r.cache.begin(torch.tensor([2, 0, 1, 7], dtype=torch.int32))  # (more may follow)
+    r.prompt()
