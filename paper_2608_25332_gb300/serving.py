@@ -117,6 +117,7 @@ class QuestionCache:
             self._drop(self._prompt)
             self._prompt = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len, True, None,
                                              self.dtype, self.device, self.algo, want_lse=False)
+        self._check_rows("prompt", T, K, V)
         start, n = self.plan["row_start"], self.prompt_len
         kp, vp = self.pools[layer]
         rows = min(T, self.planner.T_max)  # (rows behind the last question have no slot)
@@ -129,12 +130,20 @@ class QuestionCache:
         the step's new lengths 1 (or -1, whose rows are skipped: their output is that of an empty
         question; a longer one is reported in the device status and taken for an empty question).
         The result is overwritten by the next call."""
+        if Q.shape[0] != self.B:
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"decode: Q must have {self.B} rows")
+        self._check_rows("decode", self.B, K, V)
         if self._decode is None:
             self._decode = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len, None, self.dtype,
                                              self.device, self.algo, want_lse=False)
         kp, vp = self.pools[layer]
         P.provip_kv_append(K, V, self.slots, kp, vp)
         return self._decode(Q, kp, vp, self.tables, self.decode_len, self.prefix_table if self.prefix_len else None)["out"]
+
+    @staticmethod
+    def _check_rows(what, n, *tensors):
+        if any(x.shape[0] != n for x in tensors):
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"{what}: K and V must have as many rows as Q, {n}")
 
     @staticmethod
     def _drop(*held):

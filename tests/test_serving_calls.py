@@ -261,3 +261,19 @@ def test_the_lengths_of_a_step_are_checked(monkeypatch):
     r.new = [2, 0, 1]
     r.cache.begin(torch.tensor([2, 0, 1, 7], dtype=torch.int32))  # (more may follow)
     r.prompt()
+
+
+def test_a_steps_rows_are_checked(monkeypatch):
+    """with fewer rows of K or V than of Q some tokens would not be stored"""
+    r = Run(monkeypatch, B=3)
+    r.begin([2, 0, 1])
+    q, k, v = r.rand(3, H_Q), r.rand(3, H_KV), r.rand(3, H_KV)
+    for kk, vv in ((k[:2], v[:2]), (k[:2], v), (k, v[:2])):
+        with pytest.raises(P.ProvipError):
+            r.cache.prompt(0, q, kk, vv)
+    r.prompt()
+    r.begin([1, 1, 1])
+    for qq, kk, vv in ((q, k[:2], v[:2]), (q, k, v[:2]), (q[:2], k, v), (q[:2], k[:2], v[:2])):
+        with pytest.raises(P.ProvipError):
+            r.cache.decode(0, qq, kk, vv)
+    r.decode()
