@@ -154,22 +154,26 @@ __device__ __noinline__ float attn_row_plain(const AttnArgs& a, const AttnSeq& s
 }
 
 // Element col (a lane's own) of a request's row over its own keys [lo, hi), where it came out infinite
-// or NaN (odd) though the row's weights are finite: with values that are all finite it was their sum
-// that passed the largest float, and *v is the element with its sums in 64 bits (true); a value that
-// is not shows in the element as it is. By a warp, the head's (paged keys).
+// or NaN (odd) though the row's weights are finite. With values that are all finite it was their sum
+// that passed the largest float: the element with its sums in 64 bits. Else what is not finite among
+// them shows: NaN, or infinities of both signs, as NaN, of one sign as that. By a warp, the head's
+// (paged keys); returns the element.
 template <typename T>
-__device__ __noinline__ bool attn_element_again(const AttnArgs& a, int b, int h, int lo, int hi, int col, bool odd,
-                                                float* v, unsigned long long* beat) {
+__device__ __noinline__ float attn_element_again(const AttnArgs& a, int b, int h, int lo, int hi, int col, bool odd,
+                                                 unsigned long long* beat) {
   const AttnSeq s = attn_seq(a, b);
+  float v = 0.f;
+  bool up = false, down = false;  // (both for NaN)
 #pragma unroll 8
   for (int j = lo; j < hi; ++j) {
     if (beat && (threadIdx.x & 31) == 0 && ((j - lo) & 1023) == 0)
       *static_cast<volatile unsigned long long*>(beat) = global_timer_ns();
-    odd = odd && isfinite((float)attn_own_row<T>(a, s, true, j, h / (a.H_q / a.H_kv))[col]);
+    const float x = (float)attn_own_row<T>(a, s, true, j, h / (a.H_q / a.H_kv))[col];
+    up = up || !(x < INFINITY);
+    down = down || !(x > -INFINITY);
   }
-  if (!__any_sync(0xffffffffu, odd)) return false;
-  attn_row_plain<T, 1>(a, s, 0, 0, h, lo, hi, col, v, beat);
-  return odd;
+  if (__any_sync(0xffffffffu, odd && !up && !down)) attn_row_plain<T, 1>(a, s, 0, 0, h, lo, hi, col, &v, beat);
+  return up && down ? NAN : up ? INFINITY : down ? -INFINITY : v;
 }
 
 // Weighs n more parts of a row and adds them to s (by one warp): lse(p) in base 2 and 128 floats at part(p).

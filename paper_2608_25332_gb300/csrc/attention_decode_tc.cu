@@ -159,13 +159,10 @@ __device__ __noinline__ void elements_again(const AttnArgs& a, const AttnSpans& 
     __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out) + (size_t)x.b * a.o_stride + (size_t)(x.g * R + h) * kHeadDim + r;
     float* po = x.whole ? sp.whole_o + (row0 + h) * kHeadDim + r : sp.piece_o + (slot * R + h) * kHeadDim + r;
     const bool odd = isfinite(inv[h]) && !isfinite(last ? __bfloat162float(*op) : *po);
-    float v;
-    if (__any_sync(0xffffffffu, odd) && attn_element_again<__nv_bfloat16>(a, x.b, x.g * R + h, lo, hi, r, odd, &v, beat)) {
-      if (last)
-        *op = __float2bfloat16_rn(v);
-      else
-        *po = v;
-    }
+    if (!__any_sync(0xffffffffu, odd)) continue;
+    const float v = attn_element_again<__nv_bfloat16>(a, x.b, x.g * R + h, lo, hi, r, odd, beat);
+    if (odd && last) *op = __float2bfloat16_rn(v);
+    if (odd && !last) *po = v;
   }
 }
 

@@ -373,8 +373,10 @@ __global__ void __launch_bounds__(kDecThr) attn_token_simt(const __grid_constant
       const size_t row = (size_t)b * a.H_q + h0 + r;
       float val = sum == 0.f ? 0.f : acc / sum, lse = sum == 0.f ? -INFINITY : mx + log2f(sum);
       const bool odd = sum != 0.f && isfinite(sum) && !isfinite(val);
-      float v;
-      if (__any_sync(0xffffffffu, odd) && attn_element_again<T>(a, b, h0 + r, k_lo, k_hi, threadIdx.x, odd, &v, nullptr)) val = v;
+      if (__any_sync(0xffffffffu, odd)) {
+        const float v = attn_element_again<T>(a, b, h0 + r, k_lo, k_hi, threadIdx.x, odd, nullptr);
+        val = odd ? v : val;
+      }
       if (a.n_part > 1) {
         a.part_o[((size_t)part * a.T_q * a.H_q + row) * kHeadDim + threadIdx.x] = val;
         if (threadIdx.x == 0) a.part_lse[(size_t)part * a.T_q * a.H_q + row] = lse;

@@ -180,3 +180,24 @@ def test_decoding_infinite_values_that_are_seen(prefix, dtype, algo):
                                       DH ** -0.5, dtype, tc(dtype, algo))
             out = r["out"][b:b + 1, h].double()
             assert torch.isfinite(out[:, fine]).all() and ((out - o).abs() <= bound)[:, fine].all(), (b, h)
+
+
+@pytest.mark.parametrize("dtype,algo", FORMS, ids=IDS)
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_decoding_one_infinite_value_among_huge_ones(prefix, dtype, algo):
+    """the others' sum passes the largest float with the other sign: the infinite value shows all
+    the same"""
+    def values(g, *shape, dtype):
+        v = huge(g, *shape, dtype=dtype)
+        v[..., 5] = -v[..., 5]
+        if shape[0]:
+            v[-1, :, 3], v[-1, :, 5] = -math.inf, math.inf
+            v[-1, :, 90], v[0, :, 100] = math.inf, -math.inf
+        return v
+
+    args, kw, seqs = decode_case(gen(6), [40, 130, 700], 14, 2, prefix, dtype, values)
+    r = P.provip_decode_attention(*args, algo=algo, **kw)
+    torch.cuda.synchronize()
+    for at, want in ((3, -math.inf), (5, math.inf), (90, math.inf), (100, -math.inf)):
+        assert (r["out"][..., at] == want).all(), at
+    assert torch.isfinite(r["lse"]).all()
