@@ -23,7 +23,7 @@
 // of three 32 KiB stages that TMA fills across units.
 // Roles: warps 0-3 softmax (thread = key, then element), warp 4 MMAs, warp 5 TMA.
 // Every wait is bounded, from the last sign of elements computed again on (mbar_wait_beat); a timeout
-// sets the device error word and the roles drain.
+// sets the device error word, the roles end, and the block when what it has issued is done (drain).
 #include "attention_tc.cuh"
 
 namespace provip {
@@ -59,10 +59,12 @@ struct Ctl {
   uint64_t kv_full[kStages], kv_empty[kStages];
   uint64_t s_full[2], p_full[2];
   uint64_t o_done[2];  // by the tile's parity
+  uint64_t mma_done;   // (drain)
   unsigned long long beat;  // when elements were last known to be computed again (mbar_wait_beat)
   float red[4][kHeads], red_w[4][kHeads], inv[kHeads];
   uint32_t tmem;
-  volatile int fail;
+  uint32_t n_ld, n_q;  // loads issued
+  volatile int fail;   // a wait has given up
 };
 
 __device__ __forceinline__ int unit_tiles(int k_len) { return max((k_len + kT - 1) / kT, 1); }
@@ -146,6 +148,23 @@ __device__ __forceinline__ int tiles_before(int t, int lane, int& all) {
   return s - t;
 }
 
+// Where a wait has given up, loads into the block's shared memory and products in its tensor memory
+// may still be under way. The warps that issued them (role 0 the products, 1 the loads) wait for them
+// before the block ends, once more with a limit.
+__device__ __forceinline__ void drain(Ctl& ctl, unsigned* err) {
+  const int role = (int)(threadIdx.x >> 5) - 4;
+  if (role == 0) {
+    if (elect_one()) {  // the lane that issued the products
+      tc_commit(&ctl.mma_done);
+      mbar_wait(&ctl.mma_done, 0, err);
+    }
+  } else if (role == 1 && (threadIdx.x & 31) == 0) {
+    for (uint32_t i = ctl.n_q > 2 ? ctl.n_q - 2 : 0; i < ctl.n_q; ++i) mbar_wait(&ctl.q_full[i & 1], (i >> 1) & 1u, err);
+    for (uint32_t i = ctl.n_ld > kStages ? ctl.n_ld - kStages : 0; i < ctl.n_ld; ++i)
+      mbar_wait(&ctl.kv_full[i % kStages], (i / kStages) & 1u, err);
+  }
+}
+
 // Elements of a finished piece that are infinite or NaN though their weights are finite: again
 // (attn_element_again). Reads them back from where this thread has stored them, which keeps all of
 // it out of the unit's loop (inside, 64 requests of 32 heads on 4 had taken 26.4 us instead of 25.9).
@@ -200,6 +219,7 @@ __global__ void __launch_bounds__(kThr, 2)
       mbar_init(&ctl.p_full[n], 4);
       mbar_init(&ctl.o_done[n], 1);
     }
+    mbar_init(&ctl.mma_done, 1);
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&ctl.kv_full[s], 1);
       mbar_init(&ctl.kv_empty[s], 1);
@@ -280,7 +300,7 @@ __global__ void __launch_bounds__(kThr, 2)
     // ---- producer: the CTA's span, cut into pieces, and their loads ----
     const int box = min(a.page_size, kT);
     bool live = true;
-    uint32_t n_ld = 0, u = 0, tile0 = 0;
+    uint32_t n_ld = 0, n_q = 0, u = 0, tile0 = 0;
     long long f = 0, f_end = 1, f_b = 0, T = 0;  // this CTA's tiles; the first of request b
     int b = 0, k_len = 0, nt_b = 1;
     if (sp.by_unit) {
@@ -360,7 +380,10 @@ __global__ void __launch_bounds__(kThr, 2)
         if (ok) mbar_arrive_expect_tx(&ctl.kv_full[st], (uint32_t)(boxes * box * 256));
       }
       __syncwarp();
-      if (!__shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) return false;
+      if (!__shfl_sync(0xffffffffu, ok ? 1 : 0, 0)) {
+        --n_ld;
+        return false;
+      }
       uint8_t* dst = kv + st * kStage;
       const CUtensorMap* map = v ? &map_v : &map_k;
       if (lane < boxes) {
@@ -415,6 +438,7 @@ __global__ void __launch_bounds__(kThr, 2)
       }
       __syncwarp();
       live = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+      n_q += live;
       for (int j = 0; live && j < x.nt; ++j) {
         live = load(x, j, true);
         if (live && j + 1 < x.nt) live = load(x, j + 1, false);
@@ -437,6 +461,10 @@ __global__ void __launch_bounds__(kThr, 2)
       sp.cut[blockIdx.x] = make_int2(unit, last);
     }
     if (!live) ctl.fail = 1;
+    if (lane == 0) {
+      ctl.n_ld = n_ld;
+      ctl.n_q = n_q;
+    }
   } else {
     // ---- softmax: a thread per key; in the epilogue a thread per element ----
     const int r = threadIdx.x;
@@ -614,6 +642,10 @@ __global__ void __launch_bounds__(kThr, 2)
   }
   tc_fence_before();
   __syncthreads();
+  if (ctl.fail) {
+    drain(ctl, a.err);
+    __syncthreads();
+  }
   if (warp == 0) tmem_dealloc(tmem, kTmemCols);
   // where this kernel runs beside the prefix's, it does not complete before it: the joining
   // kernel waits for this one alone

@@ -24,7 +24,8 @@
 // Value rows of a tile past the sequence's end (another sequence's, padding, a page's unused
 // slots, a page not loaded) are zeroed in shared memory before the product.
 // Every wait is bounded, from the last sign of rows computed again on (mbar_wait_beat); one that gives
-// up sets the device error word and ends its role, and the other roles' waits then run out likewise.
+// up sets the device error word and ends its role, the other roles' waits then run out likewise, and
+// the block ends when what it has issued is done (drain).
 #include "attention_tc.cuh"
 
 namespace provip {
@@ -77,8 +78,11 @@ struct Ctl {
   uint64_t q_full, q_empty;
   uint64_t full[kSteps], empty[kSteps];
   uint64_t s_full[NQ], p_full[NQ], o_full[NQ];
+  uint64_t mma_done;  // (drain)
   unsigned long long beat;  // when rows were last known to be computed again (mbar_wait_beat)
   uint32_t tmem;
+  uint32_t armed, n_q;  // steps and queries that loads were issued for
+  volatile int fail;    // a wait has given up
 };
 
 constexpr uint32_t kIdescS = idesc_bf16_f32(kT, kT);
@@ -391,6 +395,25 @@ __device__ __noinline__ void finish_rows(const AttnArgs& a, const Unit<NQ>& x, i
   }
 }
 
+// Where a wait has given up, loads into the block's shared memory and products in its tensor memory
+// may still be under way. The warps that issued them (role 0 the products, 1 the loads) wait for them
+// before the block ends, once more with a limit. (A step whose loads were not all issued takes all
+// of it.)
+template <int NQ>
+__device__ __forceinline__ void drain(Ctl<NQ>& ctl, unsigned* err) {
+  const int role = (int)(threadIdx.x >> 5) - 4 * NQ;
+  if (role == 0) {
+    if (elect_one()) {  // the lane that issued the products
+      tc_commit(&ctl.mma_done);
+      mbar_wait(&ctl.mma_done, 0, err);
+    }
+  } else if (role == 1 && (threadIdx.x & 31) == 0) {
+    if (ctl.n_q > 0) mbar_wait(&ctl.q_full, (ctl.n_q - 1) & 1u, err);
+    for (uint32_t i = ctl.armed > kSteps ? ctl.armed - kSteps : 0; i < ctl.armed; ++i)
+      mbar_wait(&ctl.full[i % kSteps], (i / kSteps) & 1u, err);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // the kernel
 // ---------------------------------------------------------------------------
@@ -416,6 +439,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
     }
     mbar_init(&ctl.q_full, 1);
     mbar_init(&ctl.q_empty, 1);
+    mbar_init(&ctl.mma_done, 1);
     for (int s = 0; s < kSteps; ++s) {
       mbar_init(&ctl.full[s], 1);
       mbar_init(&ctl.empty[s], 1);
@@ -425,6 +449,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       mbar_init(&ctl.p_full[i], 4);
       mbar_init(&ctl.o_full[i], 1);
     }
+    ctl.fail = 0;
     ctl.beat = 0;
     fence_mbar_init();
   }
@@ -502,9 +527,10 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           if (j < ntm) two_on(sk);
         }
       }
+      if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 1) {
       // ---- TMA producer (the lanes share a tile's pages) ----
-      uint32_t n_q = 0, st = 0, step = 0;
+      uint32_t n_q = 0, st = 0, step = 0, armed = 0;  // armed: steps whose barrier expects loads
       uint32_t user[F::kStages];  // the step that the stage's tile is for, and one more
 #pragma unroll
       for (int i = 0; i < F::kStages; ++i) user[i] = 0;
@@ -556,6 +582,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         if (x.g < 0) break;
         if (x.ntm == 0) continue;
         // (a step's barrier is free: the stages handed over so far come from later steps than its last)
+        armed = step + 1;
         if (lane == 0) mbar_arrive_expect_tx(&ctl.full[step % kSteps], bytes_of(x, x.t_lo));
         __syncwarp();
         live = load(x, x.t_lo, false);
@@ -580,9 +607,10 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         }
         __syncwarp();
         live = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        ++n_q;
+        n_q += live;
         for (int j = 0; live && j < x.ntm; ++j, ++step) {
           const bool more = j + 1 < x.ntm;
+          armed = step + 1;
           if (lane == 0)
             mbar_arrive_expect_tx(&ctl.full[step % kSteps], bytes_of(x, x.t_lo + j) + (more ? bytes_of(x, x.t_lo + j + 1) : 0));
           __syncwarp();
@@ -590,6 +618,11 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
           if (live && more) live = load(x, x.t_lo + j + 1, false);
         }
       }
+      if (lane == 0) {
+        ctl.armed = armed;
+        ctl.n_q = n_q;
+      }
+      if (!live) ctl.fail = 1;
     } else if (warp == 4 * NQ + 2) {
       // ---- units of this CTA onto the board, ahead of those who work on them ----
       Walk w;
@@ -624,6 +657,7 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
         __syncwarp();
         if (!more) break;
       }
+      if (!live) ctl.fail = 1;
     }
   } else {
     // ---- softmax: a thread per row ----
@@ -737,9 +771,14 @@ __global__ void __launch_bounds__(Form<NQ>::kThreads, Form<NQ>::kCtas)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.u_empty[n % kBoard]);
     }
+    if (failed) ctl.fail = 1;
   }
   tc_fence_before();
   __syncthreads();
+  if (ctl.fail) {
+    drain<NQ>(ctl, a.err);
+    __syncthreads();
+  }
   if (warp == 0) tmem_dealloc(tmem, F::kCols);
 }
 

@@ -60,7 +60,9 @@ def test_waits_outlast_rows_that_are_computed_again(file):
     """A warp that computes rows again by the definition may take longer than a wait's limit (a
     microsecond a key and row): the others' waits start again while it gets on."""
     src = code(file)
-    assert not re.search(r"\bmbar_wait\(", src), "waits without the sign of rows under way"
+    drain = src.index("void drain(")
+    roles = src[:drain] + src[src.index("\n}\n", drain):]
+    assert not re.search(r"\bmbar_wait\(", roles), "waits without the sign of rows under way"
     assert "attn_row_plain" not in src or re.search(r"attn_row_plain<[^;]*&?(?:ctl\.)?beat\)", src)
     tc = code("attention_tc.cuh")
     wait = tc[tc.index("bool wait_over("):tc.index("bool warp_wait(")]
@@ -83,3 +85,28 @@ def test_a_flag_in_shared_memory_is_read(file):
     for name in re.findall(r"\b(?:int|uint32_t|float) (\w+)(?:\[\w+\])*;", struct):
         uses = re.findall(r"\bctl\." + name + r"\b(?!\s*(?:\[[^\]]*\])*\s*=[^=])", src)
         assert uses, f"{file}: {name} is written and never read"
+
+
+@pytest.mark.parametrize("file", FILES)
+def test_a_block_outlasts_what_it_has_issued(file):
+    """Where a wait gives up, loads into the block's shared memory and products in its tensor memory
+    may still be under way. The warps that issued them wait for them (once more with a limit)
+    before the release of tensor memory and the block's end."""
+    src = code(file)
+    end = src[src.rindex("if (ctl.fail) {"):]
+    assert re.match(r"if \(ctl\.fail\) \{\s*drain(?:<NQ>)?\(ctl, a\.err\);\s*__syncthreads\(\);\s*\}\s*if \(warp == 0\) tmem_dealloc\(", end)
+    assert src[:src.rindex("if (ctl.fail) {")].rstrip().endswith("__syncthreads();")
+    drain = src[src.index("void drain("):]
+    drain = drain[:drain.index("\n}\n")]
+    # the products: by the lane that issued them
+    assert re.search(r"if \(elect_one\(\)\) \{\s*tc_commit\(&ctl\.mma_done\);\s*mbar_wait\(&ctl\.mma_done, 0, err\);", drain)
+    assert "const bool lead = elect_one();" in src
+    # the loads: every barrier that one of them signals
+    loads = set(re.findall(r"tma_load_\dd\([^;]*&ctl\.(\w+)(?:\[[^\]]*\])?\);", src)) | ({"full"} if "uint64_t* full = &ctl.full[" in src else set())
+    assert len(loads) == 2
+    for bar in loads:
+        assert re.search(r"mbar_wait\(&ctl\." + bar + r"\b", drain), bar
+    # and every role that gives up says so
+    roles = src[src.index("__global__", src.index("void drain(")):]
+    assert len(re.findall(r"if \(!live\) ctl\.fail = 1;", roles)) == (3 if file == "attention_tc.cu" else 2)
+    assert len(re.findall(r"if \(failed\) ctl\.fail = 1;", roles)) == 1
