@@ -47,11 +47,14 @@ class QuestionCache:
         self.tables = torch.zeros(B, self.max_len // self.page_size, dtype=torch.int32, device=dev)
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=dev)
         self.planner = P.PageTables(B, page_size, B * self.max_len if max_new is None else max_new, dev)
+        self._slot_map = torch.full((self.planner.T_max + 1,), -1, dtype=torch.int32, device=dev)  # the last stays -1
+        self.planner.slot_map, self._first_row = self._slot_map[:-1], self.planner.row_start[:-1]
         self.prefix, self.prefix_len, self.prefix_table = [], 0, None
         self._prefix_held = torch.zeros(2, dtype=torch.int32, device=dev)  # rows that the prefix has in pages; 0
-        # a step's own tensors: its new tokens, prompt()'s rows, decode()'s slots and lengths (at one
-        # place for good, so that a layer's calls can be captured in a graph)
-        self.new_len, self.prompt_len, self.slots, self.decode_len = (torch.zeros_like(self.kv_len) for _ in range(4))
+        # the step's new tokens, and the tokens held before it (at one place for good, as all that the
+        # planner writes, so that a layer's calls can be captured in a graph)
+        self.new_len, self.held = torch.zeros_like(self.kv_len), torch.zeros_like(self.kv_len)
+        self._derived = {}
         self.plan = None
         self._prompt = self._decode = None  # the steps' buffers: of the last size only
 
@@ -96,12 +99,13 @@ class QuestionCache:
         if new_len.dtype is not torch.int32 or new_len.device != self.kv_len.device or not new_len.is_contiguous() or \
                 new_len.numel() < self.B:
             raise P.ProvipError(P.ERR_INVALID_ARG, f"begin: new_len must be a contiguous int32 tensor of {self.B} entries on {self.kv_len.device}")
-        self.new_len.copy_(new_len.view(-1)[:self.B])  # (the caller may write the next step's into it)
-        # -1, which is reported: more than prompt() and decode() can do
-        self.prompt_len.copy_(torch.where((self.new_len > 0) & (self.kv_len > 0), -1, self.new_len.clamp(min=0)))
+        self._drop(*self._derived.values())
+        self._derived.clear()
+        if new_len.numel() > self.B:
+            new_len = new_len.view(-1)[:self.B]
+        self.new_len.copy_(new_len)  # (the caller may write the next step's into it)
+        self.held.copy_(self.kv_len)
         self.plan = self.planner(self.kv_len, self.new_len, self.free, self.n_free, self.tables, inplace=True)
-        self.decode_len.copy_(torch.where(self.new_len > 1, -1, self.kv_len))
-        self.slots.copy_(self._token_slots())
         return self.plan
 
     def prompt(self, layer, Q, K, V, max_rows=None):
@@ -118,7 +122,7 @@ class QuestionCache:
             self._prompt = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len, True, None,
                                              self.dtype, self.device, self.algo, want_lse=False)
         self._check_rows("prompt", T, K, V)
-        start, n = self.plan["row_start"], self.prompt_len
+        start, n = self.plan["row_start"], self._once("rows", self._prompt_rows)
         kp, vp = self.pools[layer]
         rows = min(T, self.planner.T_max)  # (rows behind the last question have no slot)
         P.provip_kv_append(K[:rows], V[:rows], self.plan["slot_map"][:rows], kp, vp)
@@ -137,8 +141,9 @@ class QuestionCache:
             self._decode = P.DecodeAttention(self.B, self.H_q, self.H_kv, self.max_len, self.prefix_len, None, self.dtype,
                                              self.device, self.algo, want_lse=False)
         kp, vp = self.pools[layer]
-        P.provip_kv_append(K, V, self.slots, kp, vp)
-        return self._decode(Q, kp, vp, self.tables, self.decode_len, self.prefix_table if self.prefix_len else None)["out"]
+        P.provip_kv_append(K, V, self._once("slots", self._token_slots), kp, vp)
+        n = self._once("lengths", lambda: torch.where(self.new_len > 1, -1, self.kv_len))  # -1: reported
+        return self._decode(Q, kp, vp, self.tables, n, self.prefix_table if self.prefix_len else None)["out"]
 
     @staticmethod
     def _check_rows(what, n, *tensors):
@@ -149,17 +154,29 @@ class QuestionCache:
     def _drop(*held):
         """Tensors, or steps with theirs, that the cache lets go of: their memory is handed out again
         behind what the current stream has under way, whichever stream it was allocated on."""
-        for x in held:
-            for t in (x,) if isinstance(x, torch.Tensor) else () if x is None else (x.out, x.ws):
-                if t.is_cuda:
-                    t.record_stream(torch.cuda.current_stream(t.device))
+        held = [t for x in held if x is not None for t in ((x,) if isinstance(x, torch.Tensor) else (x.out, x.ws)) if t.is_cuda]
+        stream = torch.cuda.current_stream(held[0].device) if held else None
+        for t in held:
+            t.record_stream(stream)
+
+    def _once(self, name, make):
+        """What a step's layers share, worked out at its first use; in a graph at every use, as
+        its replays follow steps that are begun later."""
+        if self.device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            return make()
+        if name not in self._derived:
+            self._derived[name] = make()
+        return self._derived[name]
+
+    def _prompt_rows(self):
+        """The questions' rows for prompt(): -1, which is reported, where tokens are held already."""
+        return torch.where(torch.minimum(self.new_len, self.held) > 0, -1, self.new_len.clamp(min=0))
 
     def _token_slots(self):
         """Slots of the questions' new tokens in request order, -1 for a question without one.
         Packed rows skip such questions: the token of question b is row row_start[b], which for
-        those behind the step's last row may lie past the map's end (it has max_new slots)."""
-        rows, slots = self.plan["row_start"][:-1], self.plan["slot_map"]
-        n = slots.numel()
-        if n == 0:
-            return torch.full_like(rows, -1)
-        return torch.where((self.new_len > 0) & (rows < n), slots[rows.clamp(max=n - 1)], -1)
+        those behind the step's last row may lie past the map's end (it has max_new slots): they
+        take the entry behind it, -1."""
+        n = self.planner.T_max
+        rows = torch.where(self.new_len > 0, self._first_row, n).clamp_(max=n)
+        return self._slot_map.index_select(0, rows)

@@ -55,6 +55,7 @@ class Model:
             self.model, self.B, self.page, self.T_max = model, B, page_size, T_max
             self.kv_len = torch.zeros(B, dtype=torch.int32)
             self.free_count = torch.zeros(1, dtype=torch.int32)
+            self.slot_map, self.row_start = torch.zeros(T_max, dtype=torch.int32), torch.zeros(B + 1, dtype=torch.int32)
 
         def __call__(self, kv_len, new_len, free_pages, free_count, block_table, inplace=False):
             kv, new, n = kv_len.tolist(), new_len.tolist(), int(free_count)
@@ -80,12 +81,12 @@ class Model:
                 start.append(start[-1] + add)
                 kv[b] += add if ok else 0
             free_pages[:len(stack)] = torch.tensor(stack, dtype=torch.int32)
-            slots = (slots + [-1] * self.T_max)[:self.T_max]
+            self.slot_map[:] = torch.tensor((slots + [-1] * self.T_max)[:self.T_max], dtype=torch.int32)
             kv_out, fc_out = (kv_len, free_count) if inplace else (self.kv_len, self.free_count)
             kv_out[:] = torch.tensor(kv, dtype=torch.int32)
             fc_out[:] = len(stack)
-            return dict(kv_len=kv_out, row_start=torch.tensor(start, dtype=torch.int32),
-                        slot_map=torch.tensor(slots, dtype=torch.int32), free_count=fc_out)
+            self.row_start[:] = torch.tensor(start, dtype=torch.int32)
+            return dict(kv_len=kv_out, row_start=self.row_start, slot_map=self.slot_map, free_count=fc_out)
 
     @staticmethod
     def attend(q, k, v, scale):
