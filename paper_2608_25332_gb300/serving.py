@@ -85,7 +85,7 @@ class QuestionCache:
         for (kp, vp), k, v in zip(self.pools, K, V):
             P.provip_kv_append(k, v, plan["slot_map"], kp, vp)
         # prompts read rows of their own, not the caller's, which the next pruning may overwrite
-        self._drop(*(x for kv in self.prefix for x in kv))
+        self._drop(self.prefix_table, *(x for kv in self.prefix for x in kv))
         self.prefix = [(k.clone(), v.clone()) for k, v in zip(K, V)]
         self.prefix_len, self.prefix_table = n, table[1, :need]
         self._drop(self._prompt, self._decode)

@@ -179,14 +179,14 @@ def test_prompts_of_many_sizes_keep_one_set_of_buffers(dtype):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_buffers_that_are_dropped_wait_for_their_stream(dtype):
-    """A step's workspace was allocated on another stream than the one that uses it last: once
-    it is dropped, the allocating stream gets its memory only behind that use."""
-    r = Run(dtype, B=1, n_pages=400, max_len=64, prefix=5000)  # few rows, many keys: parts in the workspace
+    """The prefix was copied on another stream than the one that reads it last: once another takes
+    its place, the first stream gets its memory only behind that use."""
+    n = 5000
+    r = Run(dtype, B=1, n_pages=1000, max_len=64, prefix=n)
     r.begin([4])
     q, k, v = r.rand(4, H_Q), r.rand(4, H_KV), r.rand(4, H_KV)
     want = r.cache.prompt(0, q, k, v).clone()
-    new = [i32([x]) for x in (-1, 4, -1, 5)]
-    q5 = r.rand(5, H_Q)
+    new, other = [i32([x]) for x in (-1, 4)], [r.rand(n, H_KV) for _ in range(2)]
     side = torch.cuda.Stream(DEV)
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
@@ -194,10 +194,31 @@ def test_buffers_that_are_dropped_wait_for_their_stream(dtype):
         r.cache.begin(new[1])
         torch.cuda._sleep(200_000_000)  # about a tenth of a second
         got = r.cache.prompt(0, q, k, v)
+        r.cache.set_prefix([other[0]], [other[1]])
+    junk = [torch.full_like(other[0], 7.0) for _ in range(6)]  # (of the size that was dropped)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(junk)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_table_that_is_dropped_waits_for_its_stream(dtype):
+    """the same for the prefix's table, which decoding reads"""
+    n = 5000
+    r = Run(dtype, B=1, n_pages=1000, max_len=64, prefix=n)
+    new, other = [i32([x]) for x in (1, -1, 1)], [r.rand(n, H_KV) for _ in range(2)]
+    q, k, v = r.rand(1, H_Q), r.rand(1, H_KV), r.rand(1, H_KV)
+    r.cache.begin(new[0])
+    want = r.cache.decode(0, q, k, v).clone()
+    width = r.cache.prefix_table.numel()
+    side = torch.cuda.Stream(DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        r.cache.begin(new[1])
         r.cache.begin(new[2])
-        r.cache.begin(new[3])
-        r.cache.prompt(0, q5, q5[:, :H_KV], q5[:, :H_KV])  # drops the step of four rows
-    junk = [torch.full((1 << p,), 0xFF, dtype=torch.uint8, device=DEV) for p in range(9, 24) for _ in range(4)]
+        torch.cuda._sleep(200_000_000)
+        got = r.cache.decode(0, q, k, v)
+        r.cache.set_prefix([other[0]], [other[1]])
+    junk = [torch.zeros(2, width, dtype=torch.int32, device=DEV) for _ in range(200)]
     torch.cuda.synchronize()
     assert torch.equal(got, want) and len(junk)
 
