@@ -65,12 +65,16 @@ class QuestionCache:
         should have ended); more rows than the pool holds are refused. Where the questions leave
         too few pages, the prefix gets none: every decode() then reports it in the device status,
         and its result is meaningless."""
-        n = K[0].shape[0] if len(K) else 0
-        if len(K) != len(self.pools) or len(V) != len(K) or any(x.shape[0] != n for x in (*K, *V)):
-            raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: K and V must be {len(self.pools)} tensors each, of as many rows")
+        n, layers = K[0].shape[0] if len(K) else 0, len(self.pools)
+        if len(K) != layers or len(V) != layers or any(
+                x.shape != (n, self.H_kv, 128) or x.dtype is not self.dtype or x.device != self.kv_len.device for x in (*K, *V)):
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: K and V must be {layers} tensors [n, {self.H_kv}, 128] each, "
+                                                   f"of as many rows, {self.dtype} on {self.kv_len.device}")
         need, pages = -(-n // self.page_size), self.free.numel()
         if need > pages:
             raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: {n} rows take {need} pages, the pool has {pages}")
+        # prompts read rows of their own, not the caller's, which the next pruning may overwrite
+        prefix = [tuple(x.clone(memory_format=torch.contiguous_format) for x in kv) for kv in zip(K, V)]
         # two requests of the tables: the prefix before, which ends, and this one. (-1: no page.
         # Where the questions hold too many, the prefix gets none and decoding reports it)
         before = 0 if self.prefix_table is None else self.prefix_table.numel()
@@ -82,13 +86,10 @@ class QuestionCache:
         plan = P.PageTables(2, self.page_size, n, self.device)(self._prefix_held, new, self.free, self.n_free, table)
         self.n_free.copy_(plan["free_count"])
         self._prefix_held[0].copy_(plan["kv_len"][1])
-        for (kp, vp), k, v in zip(self.pools, K, V):
+        for (kp, vp), (k, v) in zip(self.pools, prefix):
             P.provip_kv_append(k, v, plan["slot_map"], kp, vp)
-        # prompts read rows of their own, not the caller's, which the next pruning may overwrite
-        self._drop(self.prefix_table, *(x for kv in self.prefix for x in kv))
-        self.prefix = [(k.clone(), v.clone()) for k, v in zip(K, V)]
-        self.prefix_len, self.prefix_table = n, table[1, :need]
-        self._drop(self._prompt, self._decode)
+        self._drop(self.prefix_table, self._prompt, self._decode, *(x for kv in self.prefix for x in kv))
+        self.prefix, self.prefix_len, self.prefix_table = prefix, n, table[1, :need]
         self._prompt = self._decode = None
 
     def begin(self, new_len):
@@ -98,7 +99,8 @@ class QuestionCache:
         that can happen."""
         if new_len.dtype is not torch.int32 or new_len.device != self.kv_len.device or not new_len.is_contiguous() or \
                 new_len.numel() < self.B:
-            raise P.ProvipError(P.ERR_INVALID_ARG, f"begin: new_len must be a contiguous int32 tensor of {self.B} entries on {self.kv_len.device}")
+            raise P.ProvipError(P.ERR_INVALID_ARG, f"begin: new_len must be a contiguous int32 tensor of {self.B} entries on "
+                                                   f"{self.kv_len.device}")
         self._drop(*self._derived.values())
         self._derived.clear()
         if new_len.numel() > self.B:
@@ -117,11 +119,11 @@ class QuestionCache:
         its rows go into the cache, and their output is left untouched. max_rows: the longest
         question (default max_len). The result is overwritten by the next call (another layer's)."""
         T, longest = Q.shape[0], min(self.max_len, Q.shape[0]) if max_rows is None else int(max_rows)
+        self._check_rows("prompt", T, K, V)
         if self._prompt is None or self._prompt.shape[0] != T or self._prompt.shape[4] != longest:
             self._drop(self._prompt)
             self._prompt = P.PromptAttention(T, self.B, self.H_q, self.H_kv, longest, longest, self.prefix_len, True, None,
                                              self.dtype, self.device, self.algo, want_lse=False)
-        self._check_rows("prompt", T, K, V)
         start, n = self.plan["row_start"], self._once("rows", self._prompt_rows)
         kp, vp = self.pools[layer]
         rows = min(T, self.planner.T_max)  # (rows behind the last question have no slot)

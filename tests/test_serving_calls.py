@@ -277,3 +277,18 @@ def test_a_steps_rows_are_checked(monkeypatch):
         with pytest.raises(P.ProvipError):
             r.cache.decode(0, qq, kk, vv)
     r.decode()
+
+
+def test_a_refused_prefix_leaves_the_one_before(monkeypatch):
+    """types and shapes are checked before any page changes hands"""
+    r = Run(monkeypatch, B=2, n_pages=12, prefix=30)
+    for bad in (r.rand(9, H_KV).double(), r.rand(9, H_KV + 1), r.rand(9, H_KV)[..., :64]):
+        fine = r.rand(9, H_KV)
+        for k, v in (([fine, bad], [fine, fine]), ([fine, fine], [bad, fine])):
+            with pytest.raises(P.ProvipError):
+                r.cache.set_prefix(k, v)
+    assert int(r.cache.n_free) == 8 and r.cache.prefix_len == 30
+    r.begin([3, 2])
+    r.prompt()
+    r.begin([1, 1])
+    r.decode()
