@@ -496,6 +496,88 @@ int provip_decode_attention(const void *Q, long long q_stride, int B, int H_q, i
                             float scale, int dtype, int algo, void *out, long long out_stride,
                             float *lse_or_null, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Position rotation on the way into the cache, and a cache held in 4 bits
+ *
+ * Pages of 4 bits: k_pages and v_pages [n_pages, H_kv, page_size * 72] bytes
+ * (72 for a head's row of 128 values; page_size a power of two from 8 to 256).
+ * For each 32 values of a row a bf16 scale d and codes n in 0..15 that stand for
+ * d (n - 8): d = -e / 8 rounded to bf16, e the value of largest magnitude (the
+ * positive one of two), n = round(x * (1 / d)) + 8, at most 15, reciprocal,
+ * product and rounding (ties to even) each once in fp32. So a value is off by
+ * |d| / 2, but one of the sign that e has not, past 7.5 |d|, by |x| - 7 |d|. A group with an
+ * infinity, a NaN or a magnitude of 2^100 or more stands for NaN, one below
+ * 2^-123 for zeros. A page of one head holds its rows' codes, 64 bytes each, then
+ * their scales, four bf16 each; the 16 bits at place 4 g + q (g < 8, q < 4) of a
+ * row's codes are values 32 q + 4 g .. + 3, the first in the lowest bits.
+ * Requires d_h == 128. Row strides as above.
+ * ---------------------------------------------------------------------- */
+
+/* Norm of every head's queries and keys, and their rotation by position ids, for
+ * packed rows: for head x of row t,
+ *   y = x * norm / sqrt(mean(x^2) + eps)   (y = x where that norm is NULL),
+ *   (y_i, y_{i+64}) turned by pos[axis_i][t] * inv_freq_i and times factor, i < 64,
+ * in fp32, rounded once at the end; angles are exact modulo a turn at every 32-bit
+ * position (also negative ones).
+ *   Q [T, H_q, d_h], K [T, H_kv, d_h]: rows q_stride, k_stride elements apart (may be
+ *   slices of one buffer); q_out, k_out alike. An output may be its input itself,
+ *   with the same stride (in place), and must not overlap any other row that is read.
+ *   n_rows_or_null [1] int32 (device): rows from there on are left untouched (a
+ *   count outside 0..T is reported; negative: none, larger: T).
+ *   pos [n_axes, T] int32 (device), axes pos_stride elements apart (the position ids
+ *   of a compaction: [P, B, L] with T = B L).
+ *   inv_freq [64] radians a position (host, in [-1e6, 1e6]), axis_or_null [64]
+ *   (host): the axis of each pair (NULL: 0). Read during the call.
+ *   q_norm_or_null, k_norm_or_null [d_h] dtype (device). */
+int provip_rotate(const void *Q, long long q_stride, const void *K, long long k_stride, int T,
+                  const int *n_rows_or_null, int H_q, int H_kv, int d_h, const int *pos,
+                  long long pos_stride, int n_axes, const double *inv_freq,
+                  const int *axis_or_null, float factor, const void *q_norm_or_null,
+                  const void *k_norm_or_null, float eps, int dtype, void *q_out,
+                  long long qo_stride, void *k_out, long long ko_stride, void *stream);
+
+/* provip_rotate with the rotated keys and the values V [T, H_kv, d_h] put into
+ * pages on the way, by slot_map [T] as in provip_kv_append: pages of dtype
+ * [n_pages, page_size, H_kv, d_h] (four_bits 0), or of 4 bits (four_bits 1), which
+ * take in the rotated keys as k_out would hold them. k_out_or_null receives them
+ * too (prompts attend over them). page_size is a power of two from 8 to 256. */
+int provip_rotate_append(const void *Q, long long q_stride, const void *K, long long k_stride,
+                         const void *V, long long v_stride, int T, const int *n_rows_or_null,
+                         int H_q, int H_kv, int d_h, const int *pos, long long pos_stride,
+                         int n_axes, const double *inv_freq, const int *axis_or_null,
+                         float factor, const void *q_norm_or_null, const void *k_norm_or_null,
+                         float eps, int dtype, void *q_out, long long qo_stride,
+                         void *k_out_or_null, long long ko_stride, const int *slot_map,
+                         int n_pages, int page_size, int four_bits, void *k_pages, void *v_pages,
+                         void *stream);
+
+/* provip_kv_append into pages of 4 bits: rows K and V [T, H_kv, d_h] dtype as they
+ * are (already rotated: a compaction's, or provip_rotate's). */
+int provip_kv_append4(const void *K, long long k_stride, const void *V, long long v_stride, int T,
+                      int H_kv, int d_h, const int *slot_map, int n_pages, int page_size,
+                      int dtype, void *k_pages, void *v_pages, void *stream);
+
+/* The values that the rows at slots slot_map [T] of 4-bit pages stand for, into
+ * k_out and v_out [T, H_kv, d_h] dtype (k_stride, v_stride elements apart; bf16:
+ * rounded), for prompts that attend over cached rows. Rows of a negative slot are left
+ * untouched, slots past the pool reported and left. The same slot may come twice. */
+int provip_kv_read4(const int *slot_map, int T, int H_kv, int d_h, const void *k_pages,
+                    const void *v_pages, int n_pages, int page_size, int dtype, void *k_out,
+                    long long k_stride, void *v_out, long long v_stride, void *stream);
+
+/* provip_decode_attention over pages of 4 bits: the values that codes and scales
+ * stand for are multiplied unrounded; Q and out have dtype. Queries' magnitudes stay below
+ * 2^100 (larger ones may give infinities or NaN); a row whose scores are finite and
+ * whose keys' groups are all finite is finite. Everything else as there. */
+size_t provip_decode_attention4_workspace_size(int B, int H_q, int H_kv, int kv_len_max,
+                                               int prefix_len, int dtype);
+int provip_decode_attention4(const void *Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
+                             const void *k_pages, const void *v_pages, int n_pages, int page_size,
+                             const int *block_table, int max_pages, const int *kv_len,
+                             int kv_len_max, const int *prefix_table_or_null, int prefix_len,
+                             float scale, int dtype, void *out, long long out_stride,
+                             float *lse_or_null, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1586,3 +1586,331 @@ extern "C" int provip_kv_append(const void* K, long long k_stride, const void* V
   cudaError_t e = kv_append_launch(a, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "kv_append launch");
 }
+
+// ===========================================================================
+// position rotation and the 4-bit cache
+// ===========================================================================
+namespace {
+
+// a fused buffer's or an output's rows of H heads
+int rows_check(const char* what, const char* name, const void* p, long long stride, int H, int dtype) {
+  if (!p) return fail(PROVIP_ERR_INVALID_ARG, "%s: null %s", what, name);
+  if (H < 1 || H > (1 << 20)) return fail(PROVIP_ERR_INVALID_ARG, "%s: %d heads in %s", what, H, name);
+  if (stride < (long long)H * kHeadDim) return fail(PROVIP_ERR_INVALID_ARG, "%s: row stride of %s shorter than a row", what, name);
+  if ((stride * esize(dtype)) % 16)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: row stride of %s must be a multiple of 16 bytes", what, name);
+  if (!aligned16(p)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: %s not 16-byte aligned", what, name);
+  return PROVIP_OK;
+}
+
+// an output that is an input's own memory must have its rows in the same places
+int inplace_check(const char* what, const char* name, const void* in, long long in_stride, const void* out, long long out_stride) {
+  if (in == out && in_stride != out_stride)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: %s in place with another row stride", what, name);
+  return PROVIP_OK;
+}
+
+// turns a position as a fraction of 2^64, from radians a position: f / (2 pi) with a product in two
+// doubles (1 / (2 pi) as two as well), of which only the fraction counts at whole positions
+unsigned long long turns_of(double f) {
+  const double hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
+  const double t = f * hi, rest = fma(f, hi, -t) + f * lo;
+  double frac = t - floor(t);  // exact below 1
+  if (frac >= 1.) frac = 0.;
+  return (unsigned long long)ldexp(frac, 64) + (unsigned long long)(long long)ldexp(rest, 64);
+}
+
+// what the rotating calls check alike, and their arguments
+int rotate_args(const char* what, RotateArgs& a, const void* Q, long long q_stride, const void* K, long long k_stride, int T,
+                const int* n_rows, int H_q, int H_kv, int d_h, const int* pos, long long pos_stride, int n_axes,
+                const double* inv_freq, const int* axis, float factor, const void* wq, const void* wk, float eps, int dtype,
+                void* q_out, long long qo_stride, void* k_out, long long ko_stride) {
+  memset(&a, 0, sizeof(a));
+  if (!dtype_ok(dtype)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: dtype %d", what, dtype);
+  if (d_h != kHeadDim) return fail(PROVIP_ERR_UNSUPPORTED, "%s: d_h must be 128", what);
+  int rc;
+  if ((rc = rows_check(what, "Q", Q, q_stride, H_q, dtype)) || (rc = rows_check(what, "K", K, k_stride, H_kv, dtype)) ||
+      (rc = rows_check(what, "q_out", q_out, qo_stride, H_q, dtype)) ||
+      (k_out && (rc = rows_check(what, "k_out", k_out, ko_stride, H_kv, dtype))) ||
+      (rc = inplace_check(what, "Q", Q, q_stride, q_out, qo_stride)) ||
+      (rc = inplace_check(what, "K", K, k_stride, k_out, ko_stride)))
+    return rc;
+  if (!pos || !inv_freq) return fail(PROVIP_ERR_INVALID_ARG, "%s: null positions or frequencies", what);
+  if (n_axes < 1 || n_axes > 255 || (n_axes > 1 && pos_stride < T) || pos_stride < 0)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: %d axes of positions, %lld apart", what, n_axes, pos_stride);
+  if (!isfinite(factor)) return fail(PROVIP_ERR_INVALID_ARG, "%s: factor must be finite", what);
+  if ((wq || wk) && !(eps >= 0.f && eps < INFINITY)) return fail(PROVIP_ERR_INVALID_ARG, "%s: eps must not be negative", what);
+  if ((wq && !aligned16(wq)) || (wk && !aligned16(wk)))
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: norm weights not 16-byte aligned", what);
+  for (int i = 0; i < kPairs; ++i) {
+    if (!(fabs(inv_freq[i]) <= 1e6)) return fail(PROVIP_ERR_INVALID_ARG, "%s: frequency %d is not in [-1e6, 1e6]", what, i);
+    const int x = axis ? axis[i] : 0;
+    if (x < 0 || x >= n_axes) return fail(PROVIP_ERR_INVALID_ARG, "%s: pair %d turns with axis %d of %d", what, i, x, n_axes);
+    a.turns[i] = turns_of(inv_freq[i]);
+    a.axis[i] = (unsigned char)x;
+  }
+  a.Q = Q;
+  a.K = K;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.T = T;
+  a.n_rows = n_rows;
+  a.H_q = H_q;
+  a.H_kv = H_kv;
+  a.turn = true;
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.factor = factor;
+  a.eps = eps;
+  a.wq = wq;
+  a.wk = wk;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.qo_stride = qo_stride;
+  a.ko_stride = ko_stride;
+  return PROVIP_OK;
+}
+
+// pages of rows of H_kv heads: of the rows' type, or of 4 bits
+int pages_check(const char* what, const void* k_pages, const void* v_pages, int n_pages, int page_size, int* shift) {
+  if (!k_pages || !v_pages) return fail(PROVIP_ERR_INVALID_ARG, "%s: null pages", what);
+  if (n_pages < 1) return fail(PROVIP_ERR_INVALID_ARG, "%s: %d pages", what, n_pages);
+  *shift = page_shift_of(page_size);
+  if (*shift < 0) return fail(PROVIP_ERR_UNSUPPORTED, "%s: page_size %d is no power of two from 8 to 256", what, page_size);
+  if ((long long)n_pages * page_size > 0x7fffffffll) return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many slots", what);
+  if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: pages not 16-byte aligned", what);
+  return PROVIP_OK;
+}
+
+// a warp's pieces of work: at least four heads each
+int pieces_check(const char* what, int T, long long heads) {
+  if (T < 0) return fail(PROVIP_ERR_INVALID_ARG, "%s: %d rows", what, T);
+  if ((heads / 4 + 3) * T > (1ll << 33)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows", what);
+  return PROVIP_OK;
+}
+
+}  // namespace
+
+extern "C" int provip_rotate(const void* Q, long long q_stride, const void* K, long long k_stride, int T,
+                             const int* n_rows_or_null, int H_q, int H_kv, int d_h, const int* pos, long long pos_stride,
+                             int n_axes, const double* inv_freq, const int* axis_or_null, float factor,
+                             const void* q_norm_or_null, const void* k_norm_or_null, float eps, int dtype, void* q_out,
+                             long long qo_stride, void* k_out, long long ko_stride, void* stream) {
+  NvtxRange nvtx_range("provip_rotate");
+  const char* what = "rotate";
+  int rc = pieces_check(what, T, (long long)H_q + H_kv);
+  if (rc) return rc;
+  if (T == 0) return PROVIP_OK;
+  if (!k_out) return fail(PROVIP_ERR_INVALID_ARG, "%s: null k_out", what);
+  RotateArgs a;
+  if ((rc = rotate_args(what, a, Q, q_stride, K, k_stride, T, n_rows_or_null, H_q, H_kv, d_h, pos, pos_stride, n_axes,
+                        inv_freq, axis_or_null, factor, q_norm_or_null, k_norm_or_null, eps, dtype, q_out, qo_stride, k_out,
+                        ko_stride)))
+    return rc;
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  a.err = d->status;
+  cudaError_t e = rotate_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "rotate launch");
+}
+
+extern "C" int provip_rotate_append(const void* Q, long long q_stride, const void* K, long long k_stride, const void* V,
+                                    long long v_stride, int T, const int* n_rows_or_null, int H_q, int H_kv, int d_h,
+                                    const int* pos, long long pos_stride, int n_axes, const double* inv_freq,
+                                    const int* axis_or_null, float factor, const void* q_norm_or_null,
+                                    const void* k_norm_or_null, float eps, int dtype, void* q_out, long long qo_stride,
+                                    void* k_out_or_null, long long ko_stride, const int* slot_map, int n_pages,
+                                    int page_size, int four_bits, void* k_pages, void* v_pages, void* stream) {
+  NvtxRange nvtx_range("provip_rotate_append");
+  const char* what = "rotate_append";
+  int rc = pieces_check(what, T, (long long)H_q + 2ll * H_kv);
+  if (rc) return rc;
+  if (T == 0) return PROVIP_OK;
+  RotateArgs a;
+  if ((rc = rotate_args(what, a, Q, q_stride, K, k_stride, T, n_rows_or_null, H_q, H_kv, d_h, pos, pos_stride, n_axes,
+                        inv_freq, axis_or_null, factor, q_norm_or_null, k_norm_or_null, eps, dtype, q_out, qo_stride,
+                        k_out_or_null, ko_stride)) ||
+      (rc = rows_check(what, "V", V, v_stride, H_kv, dtype)) ||
+      (rc = pages_check(what, k_pages, v_pages, n_pages, page_size, &a.page_shift)))
+    return rc;
+  if (!slot_map) return fail(PROVIP_ERR_INVALID_ARG, "%s: null slot_map", what);
+  if (four_bits != 0 && four_bits != 1) return fail(PROVIP_ERR_INVALID_ARG, "%s: four_bits %d", what, four_bits);
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  a.V = V;
+  a.v_stride = v_stride;
+  a.slot_map = slot_map;
+  a.n_slots = (long long)n_pages * page_size;
+  a.four = four_bits != 0;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.err = d->status;
+  cudaError_t e = rotate_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "rotate_append launch");
+}
+
+extern "C" int provip_kv_append4(const void* K, long long k_stride, const void* V, long long v_stride, int T, int H_kv,
+                                 int d_h, const int* slot_map, int n_pages, int page_size, int dtype, void* k_pages,
+                                 void* v_pages, void* stream) {
+  NvtxRange nvtx_range("provip_kv_append4");
+  const char* what = "kv_append4";
+  int rc = pieces_check(what, T, 2ll * H_kv);
+  if (rc) return rc;
+  if (T == 0) return PROVIP_OK;
+  if (!dtype_ok(dtype)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: dtype %d", what, dtype);
+  if (d_h != kHeadDim) return fail(PROVIP_ERR_UNSUPPORTED, "%s: d_h must be 128", what);
+  RotateArgs a;
+  memset(&a, 0, sizeof(a));
+  if ((rc = rows_check(what, "K", K, k_stride, H_kv, dtype)) || (rc = rows_check(what, "V", V, v_stride, H_kv, dtype)) ||
+      (rc = pages_check(what, k_pages, v_pages, n_pages, page_size, &a.page_shift)))
+    return rc;
+  if (!slot_map) return fail(PROVIP_ERR_INVALID_ARG, "%s: null slot_map", what);
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  a.K = K;
+  a.V = V;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.T = T;
+  a.H_kv = H_kv;
+  a.slot_map = slot_map;
+  a.n_slots = (long long)n_pages * page_size;
+  a.four = true;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.err = d->status;
+  cudaError_t e = rotate_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "kv_append4 launch");
+}
+
+extern "C" int provip_kv_read4(const int* slot_map, int T, int H_kv, int d_h, const void* k_pages, const void* v_pages,
+                               int n_pages, int page_size, int dtype, void* k_out, long long k_stride, void* v_out,
+                               long long v_stride, void* stream) {
+  NvtxRange nvtx_range("provip_kv_read4");
+  const char* what = "kv_read4";
+  int rc = pieces_check(what, T, 2ll * H_kv);
+  if (rc) return rc;
+  if (T == 0) return PROVIP_OK;
+  if (!dtype_ok(dtype)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: dtype %d", what, dtype);
+  if (d_h != kHeadDim) return fail(PROVIP_ERR_UNSUPPORTED, "%s: d_h must be 128", what);
+  Read4Args a;
+  memset(&a, 0, sizeof(a));
+  if ((rc = rows_check(what, "k_out", k_out, k_stride, H_kv, dtype)) ||
+      (rc = rows_check(what, "v_out", v_out, v_stride, H_kv, dtype)) ||
+      (rc = pages_check(what, k_pages, v_pages, n_pages, page_size, &a.page_shift)))
+    return rc;
+  if (!slot_map) return fail(PROVIP_ERR_INVALID_ARG, "%s: null slot_map", what);
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  a.k_pages = static_cast<const uint8_t*>(k_pages);
+  a.v_pages = static_cast<const uint8_t*>(v_pages);
+  a.slot_map = slot_map;
+  a.T = T;
+  a.H_kv = H_kv;
+  a.n_slots = (long long)n_pages * page_size;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.err = d->status;
+  cudaError_t e = read4_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "kv_read4 launch");
+}
+
+namespace {
+
+// Parts of at least 128 keys (32 a warp), as many as make `want` CTAs of `units`, at most `most`.
+void attn4_parts(long long units, int n_keys, long long want, int most, int* part_keys, int* n_part) {
+  long long n = (want + units - 1) / units;
+  if (n > most) n = most;
+  if (n < 1) n = 1;
+  const long long keys = (((long long)n_keys + n - 1) / n + 127) / 128 * 128;
+  *part_keys = (int)(keys < 128 ? 128 : keys);
+  *n_part = (int)(((long long)n_keys + *part_keys - 1) / *part_keys);
+}
+
+Attn4Plan attn4_plan(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int dtype) {
+  Attn4Plan p;
+  memset(&p, 0, sizeof(p));
+  const int R = H_q / H_kv, wide = dtype == PROVIP_BF16 ? 16 : 8;
+  p.n_cut = 1;
+  while (R % p.n_cut || R / p.n_cut > wide) ++p.n_cut;
+  p.own_cols = R / p.n_cut > 8 ? 16 : 8;
+  attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, 8 * kPlanSms, 512, &p.own_keys, &p.n_own);
+  if (p.n_own < 1) p.n_own = 1;  // rows without keys are written too
+  const long long rows = (long long)B * R;
+  p.pre_cols = rows > 8 ? wide : 8;
+  if (prefix_len > 0)
+    attn4_parts((rows + p.pre_cols - 1) / p.pre_cols * H_kv, prefix_len, 8 * kPlanSms, 256, &p.pre_keys, &p.n_pre);
+  return p;
+}
+
+}  // namespace
+
+extern "C" size_t provip_decode_attention4_workspace_size(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, int dtype) {
+  if (B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || kv_len_max < 0 || prefix_len < 0) return 0;
+  const Attn4Plan p = attn4_plan(B, H_q, H_kv, kv_len_max, prefix_len, dtype);
+  Carve c(nullptr);
+  float *po, *pl;
+  return attn_ws(c, p.n_pre + p.n_own, B, H_q, &po, &pl);
+}
+
+extern "C" int provip_decode_attention4(const void* Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
+                                        const void* k_pages, const void* v_pages, int n_pages, int page_size,
+                                        const int* block_table, int max_pages, const int* kv_len, int kv_len_max,
+                                        const int* prefix_table_or_null, int prefix_len, float scale, int dtype, void* out,
+                                        long long out_stride, float* lse_or_null, void* ws, size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_range("provip_decode_attention4");
+  const char* what = "decode_attention4";
+  if (B < 1 || max_pages < 0 || kv_len_max < 0 || prefix_len < 0) return fail(PROVIP_ERR_INVALID_ARG, "%s: bad sizes", what);
+  if (B > 65535) return fail(PROVIP_ERR_UNSUPPORTED, "%s: more than 65535 requests", what);
+  const long long row = (long long)H_kv * d_h;
+  int shift;
+  int rc = attn_validate(what, Q, q_stride, k_pages, row, v_pages, row, H_q, H_kv, d_h, scale, dtype, PROVIP_ALGO_AUTO, out,
+                         out_stride);
+  if (rc || (rc = pages_check(what, k_pages, v_pages, n_pages, page_size, &shift))) return rc;
+  if (!kv_len || (!block_table && max_pages > 0) || (!prefix_table_or_null && prefix_len > 0))
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: null lengths or tables", what);
+  if (kv_len_max > (long long)max_pages * page_size)
+    return fail(PROVIP_ERR_INVALID_ARG, "%s: kv_len_max %d does not fit %d pages", what, kv_len_max, max_pages);
+  if (prefix_len > 0x7fffffff - kv_len_max || kv_len_max > 0x7fffffff - 512 || prefix_len > 0x7fffffff - 512)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many keys", what);
+  const Attn4Plan p = attn4_plan(B, H_q, H_kv, kv_len_max, prefix_len, dtype);
+  if ((long long)B * H_q > 0x7fffffffll - 64 || (long long)B * H_kv * p.n_cut * p.n_own > 0x7fffffffll ||
+      ((long long)B * (H_q / H_kv) / p.pre_cols + 1) * H_kv * (p.n_pre + 1) > 0x7fffffffll)
+    return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
+  if ((rc = check_ws(provip_decode_attention4_workspace_size(B, H_q, H_kv, kv_len_max, prefix_len, dtype), ws, ws_bytes, what)))
+    return rc;
+  DevInfo* d;
+  if ((rc = dev_info(&d))) return rc;
+  AttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q;
+  a.K = a.Kp = k_pages;
+  a.V = a.Vp = v_pages;
+  a.q_stride = q_stride;
+  a.o_stride = out_stride;
+  a.T_q = B;
+  a.B = B;
+  attn_heads(a, H_q, H_kv);
+  a.k_len = kv_len;
+  a.q_len_max = 1;
+  a.k_len_max = kv_len_max;
+  a.prefix_len = prefix_len;
+  a.paged = 1;
+  a.page_size = page_size;
+  a.page_shift = shift;
+  a.n_pages = n_pages;
+  a.max_pages = max_pages;
+  a.block_table = block_table;
+  a.prefix_table = prefix_table_or_null;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.out = out;
+  a.lse = lse_or_null;
+  a.n_part = p.n_pre + p.n_own;
+  a.err = d->status;
+  Carve c(ws);
+  attn_ws(c, a.n_part, B, H_q, &a.part_o, &a.part_lse);
+  cudaError_t e = attn4_launch(a, p, dtype, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "decode_attention4 launch");
+}

@@ -382,6 +382,58 @@ struct KvAppendArgs {
 };
 cudaError_t kv_append_launch(const KvAppendArgs& a, cudaStream_t s);
 
+// ---------------------------------------------------------------------------
+// position rotation, and rows in and out of 4-bit pages (rotate.cu)
+// ---------------------------------------------------------------------------
+constexpr int kRow4 = 72;    // bytes of a head's row in 4 bits: 64 of codes, four bf16 scales
+constexpr int kCodes4 = 64;
+constexpr int kPairs = 64;   // pairs (i, i + 64) of a head
+struct RotateArgs {
+  const void *Q, *K, *V;     // rows of H_q, H_kv, H_kv heads, strides in elements (null: no such heads)
+  long long q_stride, k_stride, v_stride;
+  int T;                     // rows
+  const int* n_rows;         // device: rows to handle, or null (all T)
+  int H_q, H_kv;
+  bool turn;                 // norm and rotation of Q and K (else they are copied, as V is)
+  const int* pos;            // [axes][T], pos_stride apart
+  long long pos_stride;
+  unsigned long long turns[kPairs];  // turns of a pair per position, as a fraction of 2^64
+  unsigned char axis[kPairs];
+  float factor, eps;
+  const void *wq, *wk;       // norm weights [128] or null
+  void *q_out, *k_out;       // rows, strides in elements, or null
+  long long qo_stride, ko_stride;
+  const int* slot_map;       // [T], or null: no pages
+  long long n_slots;
+  int page_shift;
+  bool four;                 // 4-bit pages
+  void *k_pages, *v_pages;
+  unsigned* err;
+};
+cudaError_t rotate_launch(const RotateArgs& a, int dtype, cudaStream_t s);
+struct Read4Args {
+  const uint8_t *k_pages, *v_pages;
+  const int* slot_map;       // [T]
+  int T, H_kv, page_shift;
+  long long n_slots;
+  void *k_out, *v_out;       // rows, strides in elements
+  long long k_stride, v_stride;
+  unsigned* err;
+};
+cudaError_t read4_launch(const Read4Args& a, int dtype, cudaStream_t s);
+
+// One token per request over pages of 4 bits (attention_decode4.cu), with AttnArgs' paged fields.
+// Columns: the query rows that share keys. Own keys: the heads of a virtual key/value head (a
+// real one's group cut into n_cut equal ones); the prefix: blocks of packed (request, head) rows.
+struct Attn4Plan {
+  int n_cut;                 // virtual heads a key/value head
+  int own_keys, n_own;       // keys of a part, parts at most (own; 0: none)
+  int pre_keys, n_pre;       // the same for the prefix
+  int own_cols, pre_cols;    // columns a CTA: 8 or 16
+};
+// part_* of AttnArgs: the prefix's parts, then the own ones (n_part in all); used where a row has more than one
+cudaError_t attn4_launch(const AttnArgs& a, const Attn4Plan& plan, int dtype, cudaStream_t s);
+
 // host helper: encode a 2-D bf16 row table [rows, cols] (row stride in bytes)
 // as a tensor map with 64 x box_rows boxes and 128-byte swizzle.
 int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,

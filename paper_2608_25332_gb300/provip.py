@@ -83,6 +83,14 @@ _SIGS = {
     "provip_decode_attention_workspace_size": (_Z, [_I] * 7),
     "provip_decode_attention": (_I, [_P, _L, _I, _I, _I, _I, _P, _P, _I, _I, _P, _I, _P, _I, _P, _I, _F, _I, _I, _P, _L,
                                      _P, _P, _Z, _P]),
+    "provip_rotate": (_I, [_P, _L, _P, _L, _I, _P, _I, _I, _I, _P, _L, _I, _P, _P, _F, _P, _P, _F, _I, _P, _L, _P, _L, _P]),
+    "provip_rotate_append": (_I, [_P, _L, _P, _L, _P, _L, _I, _P, _I, _I, _I, _P, _L, _I, _P, _P, _F, _P, _P, _F, _I, _P, _L,
+                                  _P, _L, _P, _I, _I, _I, _P, _P, _P]),
+    "provip_kv_append4": (_I, [_P, _L, _P, _L, _I, _I, _I, _P, _I, _I, _I, _P, _P, _P]),
+    "provip_kv_read4": (_I, [_P, _I, _I, _I, _P, _P, _I, _I, _I, _P, _L, _P, _L, _P]),
+    "provip_decode_attention4_workspace_size": (_Z, [_I] * 6),
+    "provip_decode_attention4": (_I, [_P, _L, _I, _I, _I, _I, _P, _P, _I, _I, _P, _I, _P, _I, _P, _I, _F, _I, _P, _L, _P, _P,
+                                      _Z, _P]),
 }
 
 
@@ -734,4 +742,208 @@ def provip_decode_attention(Q, k_pages, v_pages, block_table, kv_len, kv_len_max
     """One call of DecodeAttention, its outputs and workspace allocated here."""
     step = DecodeAttention(Q.shape[0], Q.shape[1], k_pages.shape[2], kv_len_max, prefix_len, scale, Q.dtype, Q.device,
                            algo, want_lse)
+    return step(Q, k_pages, v_pages, block_table, kv_len, prefix_table)
+
+
+# ---------------------------------------------------------------------------
+# position rotation, and a cache held in 4 bits
+# ---------------------------------------------------------------------------
+ROW4 = 72  # bytes of a head's row of 128 values in 4 bits: 64 of codes, 8 of scales
+
+
+class Rotary:
+    """What a model's position rotation goes by: inv_freq, the 64 pairs' frequencies in radians a
+    position (default base^(-i/64)), axis, the axis of position ids that each pair turns with
+    (default: the first), or sections, the numbers of pairs that turn with each axis in order
+    (such as (16, 24, 24) for time, height and width), and factor, by which rotated queries and
+    keys are multiplied. Held on the host: one object serves every device and stream."""
+
+    def __init__(self, inv_freq=None, axis=None, sections=None, base=10000.0, factor=1.0):
+        freq = [float(base) ** (-i / 64) for i in range(64)] if inv_freq is None else \
+            [float(f) for f in (inv_freq.tolist() if hasattr(inv_freq, "tolist") else inv_freq)]
+        if axis is not None and sections is not None:
+            raise ProvipError(ERR_INVALID_ARG, "Rotary: axis or sections, not both")
+        if sections is not None:
+            axis = [a for a, n in enumerate(sections) for _ in range(n)]
+        axis = [0] * 64 if axis is None else [int(a) for a in (axis.tolist() if hasattr(axis, "tolist") else axis)]
+        if len(freq) != 64 or len(axis) != 64 or min(axis) < 0:
+            raise ProvipError(ERR_INVALID_ARG, "Rotary: 64 frequencies and 64 axes from 0 on, one a pair")
+        self.n_axes, self.factor = max(axis) + 1, float(factor)
+        self.inv_freq, self.axis = (ctypes.c_double * 64)(*freq), (ctypes.c_int * 64)(*axis)
+
+
+def _norm(w, dtype, what):
+    if w is None:
+        return None
+    if not w.is_cuda or w.dtype is not dtype or w.numel() != 128 or not w.is_contiguous():
+        raise ProvipError(ERR_INVALID_ARG, f"{what} must be a contiguous {dtype} GPU tensor of 128 entries")
+    return w.data_ptr()
+
+
+def _positions(pos, T, n_axes):
+    """pointer and axis stride of position ids [axes, T] (or [axes, B, L] with T = B L)"""
+    if pos.dim() == 3 and pos.is_contiguous():
+        pos = pos.view(pos.shape[0], -1)
+    if pos.dtype is not torch.int32 or not pos.is_cuda or pos.dim() != 2 or pos.shape[0] < n_axes or pos.shape[1] != T or \
+            (T > 1 and pos.stride(1) != 1):
+        raise ProvipError(ERR_INVALID_ARG, f"pos must be an int32 GPU tensor of at least {n_axes} axes by {T} rows")
+    # (one axis alone may have any stride)
+    return pos.data_ptr(), pos.stride(0) if n_axes > 1 and T > 0 else T
+
+
+def _same_device(what, *tensors):
+    dev = tensors[0].device
+    if any(t is not None and t.device != dev for t in tensors):
+        raise ProvipError(ERR_INVALID_ARG, f"{what}: tensors on different devices")
+    return dev
+
+
+def _on(dev, call, *args):
+    """a library call with its tensors' device current, whichever the caller's is"""
+    if dev.index == torch.cuda.current_device():
+        return call(*args)
+    with torch.cuda.device(dev):
+        return call(*args)
+
+
+def _rotate_head(what, Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out):
+    """the arguments that the rotating calls share: inputs, what goes by positions, outputs"""
+    dtype, T = Q.dtype, Q.shape[0]
+    q, qs = _rows(Q, Q.shape[1], dtype, "Q")
+    k, ks = _rows(K, K.shape[1], dtype, "K")
+    if K.shape[0] != T or q_out.shape[0] != T or (k_out is not None and k_out.shape[0] != T):
+        raise ProvipError(ERR_INVALID_ARG, f"{what}: Q, K or an output has another number of rows")
+    qo, qos = _rows(q_out, Q.shape[1], dtype, "q_out")
+    ko, kos = (None, 0) if k_out is None else _rows(k_out, K.shape[1], dtype, "k_out")
+    p, ps = _positions(pos, T, rotary.n_axes)
+    by = (None if n_rows is None else _ints(n_rows, 1, "n_rows"), Q.shape[1], K.shape[1], 128, p, ps, rotary.n_axes,
+          rotary.inv_freq, rotary.axis, rotary.factor, _norm(q_norm, dtype, "q_norm"), _norm(k_norm, dtype, "k_norm"),
+          float(eps), _dtype_of(dtype))
+    return (q, qs, k, ks), by, (qo, qos, ko, kos)
+
+
+def provip_rotate(Q, K, pos, rotary, q_norm=None, k_norm=None, eps=1e-6, out=None, n_rows=None):
+    """Norms (where given, [128]) and rotation of Q [T, H_q, 128] and K [T, H_kv, 128] by the position
+    ids pos [axes, T] (or a compaction's [axes, B, L]). out: (q_out, k_out) to write, which may be (Q, K)
+    themselves; n_rows: device count of rows (such as row_start[B:]), past which rows are left untouched.
+    Returns (q_out, k_out)."""
+    q_out, k_out = out if out is not None else (Q.new_empty(Q.shape), K.new_empty(K.shape))
+    ins, by, outs = _rotate_head("rotate", Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out)
+    dev = _same_device("rotate", Q, K, pos, q_norm, k_norm, n_rows, q_out, k_out)
+    rc = _on(dev, lib().provip_rotate, *ins, Q.shape[0], *by, *outs, _stream(dev))
+    _check(rc, "provip_rotate")
+    return q_out, k_out
+
+
+def pages4(n_pages, page_size, H_kv, device="cuda"):
+    """A pool of 4-bit pages [n_pages, H_kv, page_size * 72] bytes, whose rows stand for zeros."""
+    return torch.zeros(n_pages, H_kv, page_size * ROW4, dtype=torch.uint8, device=device)
+
+
+def _pages4(k_pages, v_pages, H):
+    """pointers of two 4-bit pools, their pages and rows a page"""
+    for t in (k_pages, v_pages):
+        if not t.is_cuda or not t.is_contiguous() or t.dim() != 3 or t.dtype is not torch.uint8 or t.shape[1] != H or \
+                t.shape[2] % ROW4 or t.shape != k_pages.shape:
+            raise ProvipError(ERR_INVALID_ARG, f"4-bit pages must be contiguous uint8 GPU tensors [n_pages, {H}, page_size * {ROW4}]")
+    return k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0], k_pages.shape[2] // ROW4
+
+
+def provip_rotate_append(Q, K, V, pos, rotary, slot_map, k_pages, v_pages, q_norm=None, k_norm=None, eps=1e-6, out=None,
+                         want_k=False, n_rows=None):
+    """provip_rotate, with the rotated keys and the values V [T, H_kv, 128] into the slots slot_map [T] of
+    pages on the way: [n_pages, page_size, H_kv, 128] of the rows' type, or 4-bit ones (uint8, see pages4).
+    out: (q_out, k_out or None) to write. Returns (q_out, k_out), the latter None unless given or want_k."""
+    q_out, k_out = out if out is not None else (Q.new_empty(Q.shape), K.new_empty(K.shape) if want_k else None)
+    ins, by, outs = _rotate_head("rotate_append", Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out)
+    T, H = K.shape[0], K.shape[1]
+    v, vs = _rows(V, H, Q.dtype, "V")
+    if V.shape[0] != T:
+        raise ProvipError(ERR_INVALID_ARG, "rotate_append: V has another number of rows")
+    four = k_pages.dtype is torch.uint8
+    if four:
+        kp, vp, n, ps = _pages4(k_pages, v_pages, H)
+    else:
+        kp, vp = _pages(k_pages, Q.dtype, "k_pages"), _pages(v_pages, Q.dtype, "v_pages")
+        if k_pages.shape[2:] != (H, 128) or v_pages.shape != k_pages.shape:
+            raise ProvipError(ERR_INVALID_ARG, f"rotate_append: pages must be [n_pages, page_size, {H}, 128]")
+        n, ps = k_pages.shape[:2]
+    dev = _same_device("rotate_append", Q, K, V, pos, q_norm, k_norm, n_rows, q_out, k_out, slot_map, k_pages, v_pages)
+    rc = _on(dev, lib().provip_rotate_append, *ins, v, vs, T, *by, *outs, _ints(slot_map, T, "slot_map"), n, ps, int(four), kp,
+             vp, _stream(dev))
+    _check(rc, "provip_rotate_append")
+    return q_out, k_out
+
+
+def provip_kv_append4(K, V, slot_map, k_pages, v_pages):
+    """Rows of K and V [T, H_kv, 128] into the slots slot_map [T] of 4-bit pages (uint8, see pages4);
+    negative slots are skipped."""
+    T, H = K.shape[0], K.shape[1]
+    k, ks = _rows(K, H, K.dtype, "K")
+    v, vs = _rows(V, H, K.dtype, "V")
+    if V.shape[0] != T:
+        raise ProvipError(ERR_INVALID_ARG, "kv_append4: V has another number of rows")
+    kp, vp, n, ps = _pages4(k_pages, v_pages, H)
+    dev = _same_device("kv_append4", K, V, slot_map, k_pages, v_pages)
+    rc = _on(dev, lib().provip_kv_append4, k, ks, v, vs, T, H, 128, _ints(slot_map, T, "slot_map"), n, ps, _dtype_of(K.dtype),
+             kp, vp, _stream(dev))
+    _check(rc, "provip_kv_append4")
+
+
+def provip_kv_read4(slot_map, k_pages, v_pages, dtype=torch.bfloat16, out=None):
+    """What the rows at the slots slot_map [T] of 4-bit pages stand for: K and V [T, H_kv, 128]. out: (K, V)
+    to write, whose type counts then; rows of a negative slot are left untouched (zeros, unless out is given)."""
+    T, H = slot_map.numel(), k_pages.shape[1]
+    if out is None:
+        out = tuple(torch.zeros(T, H, 128, dtype=dtype, device=k_pages.device) for _ in range(2))
+    k_out, v_out = out
+    if k_out.shape[0] != T or v_out.shape[0] != T:
+        raise ProvipError(ERR_INVALID_ARG, "kv_read4: an output has another number of rows")
+    k, ks = _rows(k_out, H, k_out.dtype, "K")
+    v, vs = _rows(v_out, H, k_out.dtype, "V")
+    kp, vp, n, ps = _pages4(k_pages, v_pages, H)
+    dev = _same_device("kv_read4", slot_map, k_pages, v_pages, k_out, v_out)
+    rc = _on(dev, lib().provip_kv_read4, _ints(slot_map, T, "slot_map"), T, H, 128, kp, vp, n, ps, _dtype_of(k_out.dtype), k, ks,
+             v, vs, _stream(dev))
+    _check(rc, "provip_kv_read4")
+    return k_out, v_out
+
+
+class DecodeAttention4:
+    """Pre-allocated outputs + workspace for repeated provip_decode_attention4 calls: DecodeAttention
+    over 4-bit pages (uint8, see pages4). dtype: of the queries and the output."""
+
+    def __init__(self, B, H_q, H_kv, kv_len_max, prefix_len=0, scale=None, dtype=torch.bfloat16, device="cuda", want_lse=True):
+        self.shape = (int(B), int(H_q), int(H_kv), int(kv_len_max), int(prefix_len))
+        self.dtype, self._dt = dtype, _dtype_of(dtype)
+        self.scale = 128 ** -0.5 if scale is None else float(scale)
+        dev = torch.device(device)
+        self.out = torch.empty((B, H_q, 128), dtype=dtype, device=dev)
+        self.lse = torch.empty((B, H_q), dtype=torch.float32, device=dev) if want_lse else None
+        self.ws = workspace(lib().provip_decode_attention4_workspace_size(*self.shape, self._dt), dev)
+
+    def __call__(self, Q, k_pages, v_pages, block_table, kv_len, prefix_table=None):
+        """Q [B, H_q, 128]; k_pages, v_pages [n_pages, H_kv, page_size * 72] bytes; block_table
+        [B, max_pages], kv_len [B] and the prefix's pages int32 on the device. Returns dict(out, lse)."""
+        B, H_q, H_kv, km, P = self.shape
+        if Q.shape[0] != B or block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ProvipError(ERR_INVALID_ARG, f"decode_attention4: Q and block_table must have {B} rows")
+        q, qs = _rows(Q, H_q, self.dtype, "Q")
+        kp, vp, n, ps = _pages4(k_pages, v_pages, H_kv)
+        if P and prefix_table is None:
+            raise ProvipError(ERR_INVALID_ARG, "decode_attention4: the prefix needs its pages' table")
+        dev = _same_device("decode_attention4", Q, k_pages, v_pages, block_table, kv_len, self.out, prefix_table if P else None)
+        rc = _on(dev, lib().provip_decode_attention4,
+                 q, qs, B, H_q, H_kv, 128, kp, vp, n, ps, _ints(block_table, 0, "block_table"), block_table.shape[1],
+                 _ints(kv_len, B, "kv_len"), km, _ints(prefix_table, -(-P // ps), "prefix_table") if P else None, P, self.scale,
+                 self._dt, self.out.data_ptr(), H_q * 128, None if self.lse is None else self.lse.data_ptr(),
+                 self.ws.data_ptr(), self.ws.numel(), _stream(dev))
+        _check(rc, "provip_decode_attention4")
+        return dict(out=self.out, lse=self.lse)
+
+
+def provip_decode_attention4(Q, k_pages, v_pages, block_table, kv_len, kv_len_max, prefix_table=None, prefix_len=0,
+                             scale=None, want_lse=True):
+    """One call of DecodeAttention4, its outputs and workspace allocated here."""
+    step = DecodeAttention4(Q.shape[0], Q.shape[1], k_pages.shape[1], kv_len_max, prefix_len, scale, Q.dtype, Q.device, want_lse)
     return step(Q, k_pages, v_pages, block_table, kv_len, prefix_table)
