@@ -1833,15 +1833,17 @@ Attn4Plan attn4_plan(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, i
   Attn4Plan p;
   memset(&p, 0, sizeof(p));
   const int R = H_q / H_kv, wide = dtype == PROVIP_BF16 ? 16 : 8;
+  const unsigned regs[3] = {0x64006400u, 0x43004300u, 0x2c002c00u};
+  memcpy(p.regs, regs, sizeof(regs));
   p.n_cut = 1;
   while (R % p.n_cut || R / p.n_cut > wide) ++p.n_cut;
-  p.own_cols = R / p.n_cut > 8 ? 16 : 8;
+  p.own_rows = R / p.n_cut > 8 ? 16 : R / p.n_cut > 2 ? 8 : 2;
   attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, 8 * kPlanSms, 512, &p.own_keys, &p.n_own);
   if (p.n_own < 1) p.n_own = 1;  // rows without keys are written too
   const long long rows = (long long)B * R;
-  p.pre_cols = rows > 8 ? wide : 8;
+  p.pre_rows = rows > 8 ? wide : rows > 2 ? 8 : 2;
   if (prefix_len > 0)
-    attn4_parts((rows + p.pre_cols - 1) / p.pre_cols * H_kv, prefix_len, 8 * kPlanSms, 256, &p.pre_keys, &p.n_pre);
+    attn4_parts((rows + p.pre_rows - 1) / p.pre_rows * H_kv, prefix_len, 8 * kPlanSms, 256, &p.pre_keys, &p.n_pre);
   return p;
 }
 
@@ -1876,8 +1878,7 @@ extern "C" int provip_decode_attention4(const void* Q, long long q_stride, int B
   if (prefix_len > 0x7fffffff - kv_len_max || kv_len_max > 0x7fffffff - 512 || prefix_len > 0x7fffffff - 512)
     return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many keys", what);
   const Attn4Plan p = attn4_plan(B, H_q, H_kv, kv_len_max, prefix_len, dtype);
-  if ((long long)B * H_q > 0x7fffffffll - 64 || (long long)B * H_kv * p.n_cut * p.n_own > 0x7fffffffll ||
-      ((long long)B * (H_q / H_kv) / p.pre_cols + 1) * H_kv * (p.n_pre + 1) > 0x7fffffffll)
+  if ((long long)B * H_q > 0x7fffffffll - 64 || H_kv > 65535)
     return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
   if ((rc = check_ws(provip_decode_attention4_workspace_size(B, H_q, H_kv, kv_len_max, prefix_len, dtype), ws, ws_bytes, what)))
     return rc;

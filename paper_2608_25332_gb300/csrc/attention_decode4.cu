@@ -21,28 +21,38 @@
 // the one before by 2^10. Statistics and sums are fp32; P dv is rounded to bf16 (2^-8 of each weight at most;
 // values then add up as integers times weights). For fp32 queries the queries and P dv are split into
 // three bf16 pieces each (24 bits), a product each.
+#include <cuda_fp16.h>
+
 #include "attention.cuh"
 
 namespace provip {
 namespace {
 
 constexpr int kWarps = 4, kThr = kWarps * 32;
-constexpr int kStep = 32;      // keys of a warp's stage
-constexpr int kStages = 3;
+constexpr int kStep = 64;      // keys of a warp's stage
+constexpr int kTiles = kStep / 16;
+constexpr int kStages = 2;
 constexpr int kCodeBytes = kStep * kCodes4, kScaleBytes = kStep * 8;
 constexpr int kStageBytes = 2 * (kCodeBytes + kScaleBytes);  // K codes, V codes, K scales, V scales
 constexpr int kRing = kStages * kStageBytes;
 constexpr size_t kSmem = (size_t)kWarps * kRing;
 
-__device__ __forceinline__ void mma_bf16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// D = C + A B, fp32 sums; both operands fp16 (F16) or both bf16; C is D, or zero (FIRST)
+template <bool F16, bool FIRST>
+__device__ __forceinline__ void mma16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  const float c0 = FIRST ? 0.f : d[0], c1 = FIRST ? 0.f : d[1], c2 = FIRST ? 0.f : d[2], c3 = FIRST ? 0.f : d[3];
+  if (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -50,17 +60,59 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                "r"(bytes), "r"(bar)
                : "memory");
 }
-// nibble t of each half of x, less 8, as bf16
-__device__ __forceinline__ uint32_t code_pair(uint32_t x, int t) {
-  const uint32_t v = ((x >> (4 * t)) & 0x000f000fu) | 0x43004300u;  // 128 + n
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __bfloat162bfloat162(__float2bfloat16_rn(136.f)));
-  return *reinterpret_cast<const uint32_t*>(&r);
+// (x & mask) | magic in one instruction: the mask an immediate, the magic a register
+template <uint32_t kMask>
+__device__ __forceinline__ uint32_t mask_or(uint32_t x, uint32_t magic) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "n"(kMask), "r"(magic));
+  return r;
+}
+// What the expansion of codes keeps in registers (as an instruction takes one constant, and of known ones the
+// compiler makes more instructions)
+struct CodeRegs {
+  uint32_t f16, bf16, sixteenth;  // 1024 as fp16, 128 as bf16, 1/16 as fp16, twice each
+};
+// The four nibbles of each half of x, less 8, as pairs of fp16: 1024 + n, or with the nibble at bit
+// 4 1024 + 16 n, by a mask-or, then a multiply-add. One shift for the four.
+__device__ __forceinline__ void codes_f16(uint32_t x, const CodeRegs& k, uint32_t* c) {
+#pragma unroll
+  for (int t = 0; t < 4; t += 2) {
+    const uint32_t w = t ? x >> 8 : x;
+    const uint32_t v0 = mask_or<0x000f000fu>(w, k.f16), v1 = mask_or<0x00f000f0u>(w, k.f16);
+    const __half2 h0 = __hadd2(*reinterpret_cast<const __half2*>(&v0), __float2half2_rn(-1032.f));
+    const __half2 h1 = __hfma2(*reinterpret_cast<const __half2*>(&v1), *reinterpret_cast<const __half2*>(&k.sixteenth), __float2half2_rn(-72.f));
+    c[t] = *reinterpret_cast<const uint32_t*>(&h0);
+    c[t + 1] = *reinterpret_cast<const uint32_t*>(&h1);
+  }
+}
+// The same as pairs of bf16, whose seven bits want each nibble at bit 0 (128 + n): three shifts. (Shifts by the
+// upper halves of products, to spare the integer pipe, took 94.9 us where these take 88.7.)
+__device__ __forceinline__ void codes_bf16(uint32_t x, const CodeRegs& k, uint32_t* c) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const uint32_t v = mask_or<0x000f000fu>(x >> (4 * t), k.bf16);
+    const __nv_bfloat162 h = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __bfloat162bfloat162(__float2bfloat16_rn(136.f)));
+    c[t] = *reinterpret_cast<const uint32_t*>(&h);
+  }
 }
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+// x, y as kP fp16 pairs that add up to them
+template <int kP>
+__device__ __forceinline__ void split2_f16(float x, float y, uint32_t* r) {
+#pragma unroll
+  for (int p = 0; p < kP; ++p) {
+    const __half2 h = __floats2half2_rn(x, y);
+    r[p] = *reinterpret_cast<const uint32_t*>(&h);
+    if (p + 1 < kP) {
+      x -= __low2float(h);
+      y -= __high2float(h);
+    }
+  }
 }
 // x, y as kP bf16 pairs that add up to them
 template <int kP>
@@ -75,34 +127,46 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t* r) {
   }
 }
 
-// which query row a column is (-1: none), as b * H_q + h
+// A column's query row: its request and head (h < 0: none). Own keys: head `block * R + c` of request
+// `unit`; the prefix: row `block` + c of the packed (request, head of the group) rows of head `unit`.
+struct Column {
+  int b, h;
+};
 template <bool kPrefix>
-__device__ __forceinline__ int column_row(const AttnArgs& a, int R, int block, int g, int c) {
-  if (!kPrefix) return c < R ? block * a.H_q + g * R + c : -1;  // (block: the request; g, R: virtual)
-  const long long r = (long long)block + c;
-  if (r >= (long long)a.B * R) return -1;
-  const int b = (int)(r / R);
-  return b * a.H_q + g * R + (int)(r - (long long)b * R);
+__device__ __forceinline__ Column column(const AttnArgs& a, int R, int unit, int block, int c) {
+  if (!kPrefix) return {unit, c < R ? block * R + c : -1};
+  const unsigned r = (unsigned)block + c, b = r / (unsigned)R;  // (B R fits 31 bits)
+  return {(int)b, b < (unsigned)a.B ? unit * R + (int)(r - b * R) : -1};
 }
 
-template <typename T, int NT, bool kPrefix>
-__global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Attn4Plan plan) {
-  constexpr int kP = sizeof(T) == 4 ? 3 : 1;  // bf16 pieces of a query and of a weight
-  constexpr int C = 8 * NT;
+// kHeads: query rows to a tile of eight columns. Eight: a column each, with the scores of the four groups of
+// dims from sums of their own. Two: four columns each, one a group (its queries are zero outside the group),
+// so that one sum over all dims leaves the groups' scores side by side, and the second product's columns carry a
+// weight for each group: a fifth of the instructions about scores and weights less where a head is alone
+// (or two are), and most of the columns are empty otherwise.
+template <typename T, int NT, int kHeads, bool kPrefix>
+__global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
+    attn4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Attn4Plan plan) {
+  constexpr bool kSplit = kHeads == 2;
+  constexpr int kE = kSplit ? 2 : 4;          // scores a lane and tile: its rows, by its columns' heads
+  constexpr int kH = kSplit ? 1 : 2;          // heads of a lane's columns
+  constexpr int kQ = sizeof(T) == 4 ? 2 : 1;  // fp16 pieces of a query
+  constexpr int kP = sizeof(T) == 4 ? 3 : 1;  // bf16 pieces of a weight
+  constexpr int C = kHeads * NT;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
   __shared__ float s_m[kWarps][C], s_l[kWarps][C];
+  __shared__ __align__(16) uint32_t s_q[NT][kQ][4][32][4];
+  __shared__ float s_most[4][C];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+  const bool first = threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0;
   if (kPrefix) pdl_allow_next();
 
-  // this CTA's piece: heads run fastest (their parts of a page lie next to each other)
-  const int R = kPrefix ? a.group : a.group / plan.n_cut, H = kPrefix ? a.H_kv : a.H_kv * plan.n_cut;
-  const long long id = blockIdx.x;
-  const int head = (int)(id % H);
-  const int n_part = kPrefix ? plan.n_pre : plan.n_own, part = (int)(id / H % n_part);
-  const int unit = (int)(id / H / n_part);
-  const int block = kPrefix ? unit * C : unit;
-  const int kv_head = kPrefix ? head : head / plan.n_cut;
+  // this CTA's piece. Own keys: x a virtual key/value head (their parts of a page lie next to each
+  // other), y a part, z the request; the prefix: x a block of rows, y a part, z the head
+  const int R = kPrefix ? a.group : a.group / plan.n_cut;
+  const int part = blockIdx.y, unit = blockIdx.z, block = kPrefix ? (int)blockIdx.x * C : (int)blockIdx.x;
+  const int kv_head = kPrefix ? unit : plan.n_cut == 1 ? block : block / plan.n_cut;
   int len = a.prefix_len;
   const int* table = a.prefix_table;
   if (!kPrefix) {
@@ -117,45 +181,42 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
   const int k_lo = part * part_keys;
   const bool alone = !kPrefix && a.prefix_len == 0 && len <= part_keys;  // the row's only part
   if (len <= k_lo && !(alone && part == 0)) {
-    if (!kPrefix && blockIdx.x == 0 && threadIdx.x == 0) pdl_wait_prior();
+    if (!kPrefix && first) pdl_wait_prior();
     return;
   }
   const int k_hi = k_lo + min(len - k_lo, part_keys);
   const int n_steps = max(0, (k_hi - k_lo + kStep - 1) / kStep);
 
+  // loads: a lane per copy of a stage (up to eight boxes of rows, K and V codes and scales of each)
+  const int box = min(a.page_size, kStep), kind = lane & 3, box_row = (lane >> 2) * box;
+  auto page_of = [&](int step) {
+    const int k = k_lo + step * kStep + box_row;
+    return box_row < kStep && step < n_steps && k < k_hi ? __ldg(table + (k >> a.page_shift)) : 0;
+  };
+  int page = page_of(warp);
   if (lane == 0) {
     for (int s = 0; s < kStages; ++s) mbar_init(&full[warp][s], 1);
     fence_mbar_init();
   }
   __syncwarp();
-
-  // loads: a lane per copy of a stage (up to four boxes of rows, K and V codes and scales of each)
-  const int box = min(a.page_size, kStep), kind = lane & 3, my_box = lane >> 2;
-  const uint32_t ring = smem_u32(smem) + warp * kRing;
-  const uint32_t dst = (kind < 2 ? kind * kCodeBytes + my_box * box * kCodes4
-                                 : 2 * kCodeBytes + (kind - 2) * kScaleBytes + my_box * box * 8);
-  const uint32_t bytes = box * (kind < 2 ? kCodes4 : 8);
-  const uint8_t* pool = static_cast<const uint8_t*>(kind & 1 ? a.V : a.K);
-  auto page_of = [&](int step) {
-    const int k = k_lo + step * kStep + my_box * box;
-    return my_box * box < kStep && step < n_steps && k < k_hi ? __ldg(table + (k >> a.page_shift)) : 0;
-  };
-  int page = page_of(warp);
+  const uint32_t ring = smem_u32(smem) + warp * kRing, bar = smem_u32(&full[warp][0]);
+  const uint32_t unit_bytes = kind < 2 ? kCodes4 : 8;  // of a row
+  const uint32_t dst = ring + box_row * unit_bytes + (kind < 2 ? kind * kCodeBytes : 2 * kCodeBytes + (kind - 2) * kScaleBytes);
+  const uint8_t* src = static_cast<const uint8_t*>(kind & 1 ? a.V : a.K) + (((size_t)kv_head * kRow4 + (kind < 2 ? 0 : kCodes4)) << a.page_shift);
+  const uint32_t page_bytes = (uint32_t)(a.H_kv * kRow4) << a.page_shift;
   auto load = [&](int step, int stage) {  // (steps: this warp's, in order)
-    const int k = k_lo + step * kStep, n = min(kStep, k_hi - k), boxes = (n + box - 1) / box;
+    const int k = k_lo + step * kStep, rows = min(kStep, k_hi - k);
     int p = page;
     page = page_of(step + kWarps);
-    if (lane == 0) mbar_arrive_expect_tx(&full[warp][stage], (uint32_t)(boxes * box * kRow4 * 2));
+    if (lane == 0) mbar_arrive_expect_tx(&full[warp][stage], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4 * 2));
     __syncwarp();
-    if (my_box < boxes) {
+    if (box_row < rows) {
       if ((unsigned)p >= (unsigned)a.n_pages) {
         set_error(a.err, kErrBadDeviceArg);
         p = 0;
       }
-      const int row = (k + my_box * box) & (a.page_size - 1);
-      const size_t base = ((size_t)((long long)p * a.H_kv + kv_head) << a.page_shift) * kRow4;
-      const size_t at = kind < 2 ? (size_t)row * kCodes4 : ((size_t)kCodes4 << a.page_shift) + (size_t)row * 8;
-      bulk_load(ring + stage * kStageBytes + dst, pool + base + at, bytes, smem_u32(&full[warp][stage]));
+      bulk_load(dst + stage * kStageBytes, src + (size_t)p * page_bytes + ((k + box_row) & (a.page_size - 1)) * unit_bytes,
+                box * unit_bytes, bar + stage * 8);
     }
     __syncwarp();
   };
@@ -169,39 +230,74 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
     }
   }
 
-  // queries: column g's dims 32 q + 8 j .. + 7, as B operands
-  uint32_t qf[NT][kP][4][4];
+  // Queries: column g's dims 32 q + 8 j .. + 7, as B operands in fp16: times a power of two that brings
+  // the column's largest into [2^14, 2^15), so that nothing is lost but what is below 2^-39 of that. The
+  // scale of a column's scores makes up for it. Warp q works out group q for all.
+  uint32_t qf[NT][kQ][4][4];
+  float cs[NT][kH];
+  {
+    float x[NT][8];
+    const bool mine = !kSplit || (g & 3) == warp;  // column g has this group
+    const int g_head = kSplit ? g >> 2 : g;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int row = column_row<kPrefix>(a, R, block, head, nt * 8 + g);
-    const T* qp = nullptr;
-    if (row >= 0) {
-      const int b = row / a.H_q;
-      qp = static_cast<const T*>(a.Q) + (size_t)b * a.q_stride + (size_t)(row - b * a.H_q) * kHeadDim + 8 * j;
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[nt][e] = 0.f;
+      const Column c = column<kPrefix>(a, R, unit, block, nt * kHeads + g_head);
+      if (c.h >= 0 && mine)
+        load8(static_cast<const T*>(a.Q) + (size_t)c.b * a.q_stride + (size_t)c.h * kHeadDim + 32 * warp + 8 * j, x[nt]);
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float x[8];
+    for (int nt = 0; nt < NT; ++nt) {
+      float most = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-      if (qp) load8(qp + 32 * q, x);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        uint32_t r[kP];
-        split2<kP>(x[t], x[t + 4], r);
-#pragma unroll
-        for (int p = 0; p < kP; ++p) qf[nt][p][q][t] = r[p];
-      }
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[nt][e]));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      if (j == 0 && mine) s_most[warp][nt * kHeads + g_head] = most;
     }
+    __syncthreads();
+    // 2^(14 - exponent), and its reciprocal (exponents from -100 on: smaller queries need no more)
+    auto up = [&](int c) {
+      const float most = fmaxf(fmaxf(s_most[0][c], s_most[1][c]), fmaxf(s_most[2][c], s_most[3][c]));
+      return 14 + 127 - max((int)(__float_as_uint(most) >> 23), 27);
+    };
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float mul = __uint_as_float((uint32_t)(127 + up(nt * kHeads + g_head)) << 23);
+      uint32_t r[4][kQ];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) split2_f16<kQ>(x[nt][t] * mul, x[nt][t + 4] * mul, r[t]);
+#pragma unroll
+      for (int p = 0; p < kQ; ++p)
+        *reinterpret_cast<uint4*>(s_q[nt][p][warp][lane]) = make_uint4(r[0][p], r[1][p], r[2][p], r[3][p]);
+#pragma unroll
+      for (int c = 0; c < kH; ++c)
+        cs[nt][c] = __uint_as_float((uint32_t)(127 - up(nt * kHeads + (kSplit ? j >> 1 : 2 * j + c))) << 23) * a.scale_log2;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int p = 0; p < kQ; ++p)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint4 v = *reinterpret_cast<const uint4*>(s_q[nt][p][q][lane]);
+          qf[nt][p][q][0] = v.x;
+          qf[nt][p][q][1] = v.y;
+          qf[nt][p][q][2] = v.z;
+          qf[nt][p][q][3] = v.w;
+        }
   }
 
-  float o[4][2][NT][4], m[NT][2], l[NT][2];
+  const CodeRegs regs = {plan.regs[0], plan.regs[1], plan.regs[2]};
+  float o[4][2][NT][4], m[NT][kH], base[NT][kH], l[NT][kH];  // base: the maximum, 0 for none
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < kH; ++c) {
       m[nt][c] = -INFINITY;
-      l[nt][c] = 0.f;
+      base[nt][c] = l[nt][c] = 0.f;
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -223,91 +319,126 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
     const uint8_t* st = smem + warp * kRing + stage * kStageBytes;
     const uint8_t *kc = st, *vc = st + kCodeBytes, *ks = st + 2 * kCodeBytes, *vs = ks + kScaleBytes;
     const int left = k_hi - k_lo - step * kStep;  // keys from this step's first on
-    float s[2][NT][4];
+    float s[kTiles][NT][kE];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
+    for (int mt = 0; mt < kTiles; ++mt) {
       const int r0 = mt * 16 + g, r1 = r0 + 8;
       const uint4 wa = *reinterpret_cast<const uint4*>(kc + r0 * kCodes4 + 16 * j);
       const uint4 wb = *reinterpret_cast<const uint4*>(kc + r1 * kCodes4 + 16 * j);
-      const uint2 da = *reinterpret_cast<const uint2*>(ks + r0 * 8), db = *reinterpret_cast<const uint2*>(ks + r1 * 8);
+      // scales of the rows: all four groups', or those of this lane's columns
+      uint2 da, db;
+      if (kSplit) {
+        da.x = *reinterpret_cast<const uint32_t*>(ks + r0 * 8 + 4 * (j & 1));
+        db.x = *reinterpret_cast<const uint32_t*>(ks + r1 * 8 + 4 * (j & 1));
+      } else {
+        da = *reinterpret_cast<const uint2*>(ks + r0 * 8);
+        db = *reinterpret_cast<const uint2*>(ks + r1 * 8);
+      }
+      float x[NT][4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
         const uint32_t xa = q < 2 ? __byte_perm(wa.x, wa.z, sel) : __byte_perm(wa.y, wa.w, sel);
         const uint32_t xb = q < 2 ? __byte_perm(wb.x, wb.z, sel) : __byte_perm(wb.y, wb.w, sel);
         uint32_t ca[4], cb[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          ca[t] = code_pair(xa, t);
-          cb[t] = code_pair(xb, t);
-        }
+        codes_f16(xa, regs, ca);
+        codes_f16(xb, regs, cb);
         const uint32_t ua = q < 2 ? da.x : da.y, ub = q < 2 ? db.x : db.y;
         const float fa = q & 1 ? hi_f(ua) : lo_f(ua), fb = q & 1 ? hi_f(ub) : lo_f(ub);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int p = kP - 1; p >= 0; --p) {
-            mma_bf16(x, ca[0], cb[0], ca[1], cb[1], qf[nt][p][q][0], qf[nt][p][q][1]);
-            mma_bf16(x, ca[2], cb[2], ca[3], cb[3], qf[nt][p][q][2], qf[nt][p][q][3]);
+          if (!kSplit || q == 0)
+            mma16<true, true>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][kQ - 1][q][0], qf[nt][kQ - 1][q][1]);
+          else
+            mma16<true, false>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][kQ - 1][q][0], qf[nt][kQ - 1][q][1]);
+          mma16<true, false>(x[nt], ca[2], cb[2], ca[3], cb[3], qf[nt][kQ - 1][q][2], qf[nt][kQ - 1][q][3]);
+          if (kQ > 1) {
+            mma16<true, false>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][0][q][0], qf[nt][0][q][1]);
+            mma16<true, false>(x[nt], ca[2], cb[2], ca[3], cb[3], qf[nt][0][q][2], qf[nt][0][q][3]);
           }
-          if (q == 0) {
-            s[mt][nt][0] = x[0] * fa;
-            s[mt][nt][1] = x[1] * fa;
-            s[mt][nt][2] = x[2] * fb;
-            s[mt][nt][3] = x[3] * fb;
-          } else {
-            s[mt][nt][0] = fmaf(x[0], fa, s[mt][nt][0]);
-            s[mt][nt][1] = fmaf(x[1], fa, s[mt][nt][1]);
-            s[mt][nt][2] = fmaf(x[2], fb, s[mt][nt][2]);
-            s[mt][nt][3] = fmaf(x[3], fb, s[mt][nt][3]);
+          if constexpr (!kSplit) {
+            if (q == 0) {
+              s[mt][nt][0] = x[nt][0] * fa;
+              s[mt][nt][1] = x[nt][1] * fa;
+              s[mt][nt][2] = x[nt][2] * fb;
+              s[mt][nt][3] = x[nt][3] * fb;
+            } else {
+              s[mt][nt][0] = fmaf(x[nt][0], fa, s[mt][nt][0]);
+              s[mt][nt][1] = fmaf(x[nt][1], fa, s[mt][nt][1]);
+              s[mt][nt][2] = fmaf(x[nt][2], fb, s[mt][nt][2]);
+              s[mt][nt][3] = fmaf(x[nt][3], fb, s[mt][nt][3]);
+            }
           }
         }
       }
-    }
-    // base 2, hidden keys out (rounded before a maximum is subtracted: no fma with that)
-    bool raise = false;
+      if constexpr (kSplit) {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+        for (int nt = 0; nt < NT; ++nt) {
+          const float ra = fmaf(x[nt][0], lo_f(da.x), x[nt][1] * hi_f(da.x)), rb = fmaf(x[nt][2], lo_f(db.x), x[nt][3] * hi_f(db.x));
+          s[mt][nt][0] = ra + __shfl_xor_sync(0xffffffffu, ra, 1);  // (the same bits in both lanes)
+          s[mt][nt][1] = rb + __shfl_xor_sync(0xffffffffu, rb, 1);
+        }
+      }
+    }
+    // base 2, hidden keys out (rounded before a maximum is subtracted: no fma with that). Score e: of head
+    // e % kH of the lane's, row g (+ 8 from kH on)
+#pragma unroll
+    for (int mt = 0; mt < kTiles; ++mt)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool seen = mt * 16 + (e >> 1) * 8 + g < left;
-          s[mt][nt][e] = seen ? __fmul_rn(s[mt][nt][e], a.scale_log2) : -INFINITY;
-          raise = raise || s[mt][nt][e] > m[nt][e & 1] + 10.f;
-        }
+        for (int e = 0; e < kE; ++e) s[mt][nt][e] = __fmul_rn(s[mt][nt][e], cs[nt][e % kH]);
+    if (left < kStep) {
+#pragma unroll
+      for (int mt = 0; mt < kTiles; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < kE; ++e)
+            if (mt * 16 + (e / kH) * 8 + g >= left) s[mt][nt][e] = -INFINITY;
+    }
+    bool raise = false;
+    float top[NT][kH];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < kH; ++c) {
+        top[nt][c] = fmaxf(s[0][nt][c], s[0][nt][c + kH]);
+#pragma unroll
+        for (int mt = 1; mt < kTiles; ++mt) top[nt][c] = fmaxf(top[nt][c], fmaxf(s[mt][nt][c], s[mt][nt][c + kH]));
+        raise = raise || top[nt][c] > m[nt][c] + 10.f;
+      }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float x = fmaxf(fmaxf(s[0][nt][c], s[0][nt][c + 2]), fmaxf(s[1][nt][c], s[1][nt][c + 2]));
+        for (int c = 0; c < kH; ++c) {
+          float x = top[nt][c];
 #pragma unroll
           for (int b = 4; b < 32; b <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, b));
           x = fmaxf(x, m[nt][c]);
           const float f = x == m[nt][c] ? 1.f : ex2_approx(m[nt][c] - x);
           m[nt][c] = x;
+          base[nt][c] = x == -INFINITY ? 0.f : x;
           l[nt][c] *= f;
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              o[q][h][nt][c] *= f;
-              o[q][h][nt][c + 2] *= f;
-            }
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (e % kH == c) o[q][h][nt][e] *= f;
         }
     }
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < kTiles; ++mt)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float mm = m[nt][e & 1];
-          const float p = ex2_approx(s[mt][nt][e] - (mm == -INFINITY ? 0.f : mm));
+        for (int e = 0; e < kE; ++e) {
+          const float p = ex2_approx(s[mt][nt][e] - base[nt][e % kH]);
           s[mt][nt][e] = p;
-          l[nt][e & 1] += p;
+          l[nt][e % kH] += p;
         }
     // (fp32: a step's sums start from zero and are added in fp32, as the MMAs' own sums truncate)
     float add[kP > 1 ? 4 : 1][2][NT][4];
@@ -316,12 +447,34 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
       for (int i = 0; i < 4 * 2 * NT * 4; ++i) (&add[0][0][0][0])[i] = 0.f;
     }
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
+    for (int mt = 0; mt < kTiles; ++mt) {
       const int r0 = mt * 16 + g, k0 = mt * 16 + 2 * j;
       // a row past the end has no scale, whatever lies there
-      uint2 da = *reinterpret_cast<const uint2*>(vs + r0 * 8), db = *reinterpret_cast<const uint2*>(vs + (r0 + 8) * 8);
-      if (r0 >= left) da = make_uint2(0u, 0u);
-      if (r0 + 8 >= left) db = make_uint2(0u, 0u);
+      uint2 da, db;
+      if (kSplit) {
+        da.x = *reinterpret_cast<const uint32_t*>(vs + r0 * 8 + 4 * (j & 1));
+        db.x = *reinterpret_cast<const uint32_t*>(vs + (r0 + 8) * 8 + 4 * (j & 1));
+      } else {
+        da = *reinterpret_cast<const uint2*>(vs + r0 * 8);
+        db = *reinterpret_cast<const uint2*>(vs + (r0 + 8) * 8);
+      }
+      if (left < kStep) {
+        if (r0 >= left) da = make_uint2(0u, 0u);
+        if (r0 + 8 >= left) db = make_uint2(0u, 0u);
+      }
+      uint32_t b0[NT][kP], b1[NT][kP];
+      if constexpr (kSplit) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          split2<kP>(s[mt][nt][0] * lo_f(da.x), s[mt][nt][0] * hi_f(da.x), b0[nt]);
+          split2<kP>(s[mt][nt][1] * lo_f(db.x), s[mt][nt][1] * hi_f(db.x), b1[nt]);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) {
+            b0[nt][p] = transpose8x8(b0[nt][p]);
+            b1[nt][p] = transpose8x8(b1[nt][p]);
+          }
+        }
+      }
       uint2 v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2*>(vc + (k0 + (i >> 1) * 8 + (i & 1)) * kCodes4 + 8 * g);
@@ -331,23 +484,25 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
         const uint32_t ya = q < 2 ? __byte_perm(v[0].x, v[1].x, sel) : __byte_perm(v[0].y, v[1].y, sel);
         const uint32_t yb = q < 2 ? __byte_perm(v[2].x, v[3].x, sel) : __byte_perm(v[2].y, v[3].y, sel);
         uint32_t ca[4], cb[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          ca[t] = code_pair(ya, t);
-          cb[t] = code_pair(yb, t);
-        }
+        codes_bf16(ya, regs, ca);
+        codes_bf16(yb, regs, cb);
         const uint32_t ua = q < 2 ? da.x : da.y, ub = q < 2 ? db.x : db.y;
         const float fa = q & 1 ? hi_f(ua) : lo_f(ua), fb = q & 1 ? hi_f(ub) : lo_f(ub);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          uint32_t wa[kP], wb[kP];
-          split2<kP>(s[mt][nt][0] * fa, s[mt][nt][1] * fa, wa);
-          split2<kP>(s[mt][nt][2] * fb, s[mt][nt][3] * fb, wb);
+          if constexpr (!kSplit) {
+            split2<kP>(s[mt][nt][0] * fa, s[mt][nt][1] * fa, b0[nt]);
+            split2<kP>(s[mt][nt][2] * fb, s[mt][nt][3] * fb, b1[nt]);
+#pragma unroll
+            for (int p = 0; p < kP; ++p) {
+              b0[nt][p] = transpose8x8(b0[nt][p]);
+              b1[nt][p] = transpose8x8(b1[nt][p]);
+            }
+          }
 #pragma unroll
           for (int p = kP - 1; p >= 0; --p) {
-            const uint32_t b0 = transpose8x8(wa[p]), b1 = transpose8x8(wb[p]);
-            mma_bf16(kP > 1 ? add[q][0][nt] : o[q][0][nt], ca[0], ca[1], cb[0], cb[1], b0, b1);
-            mma_bf16(kP > 1 ? add[q][1][nt] : o[q][1][nt], ca[2], ca[3], cb[2], cb[3], b0, b1);
+            mma16<false, false>(kP > 1 ? add[q][0][nt] : o[q][0][nt], ca[0], ca[1], cb[0], cb[1], b0[nt][p], b1[nt][p]);
+            mma16<false, false>(kP > 1 ? add[q][1][nt] : o[q][1][nt], ca[2], ca[3], cb[2], cb[3], b0[nt][p], b1[nt][p]);
           }
         }
       }
@@ -374,33 +529,42 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < kH; ++c)
 #pragma unroll
       for (int b = 4; b < 32; b <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], b);
 
   // the four warps' results: [warp][column][128] over the rings
+  const int n_cols = kPrefix ? C : R;
   __syncthreads();
   float* so = reinterpret_cast<float*>(smem);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int col = nt * 8 + 2 * j + c;
-      if (g == 0) {
-        s_m[warp][col] = m[nt][c];
-        s_l[warp][col] = l[nt][c];
+      const int col = nt * kHeads + (kSplit ? j >> 1 : 2 * j + c);
+      if (col >= n_cols) continue;
+      if (g == 0 && (!kSplit || c == (j & 1))) {
+        s_m[warp][col] = m[nt][kSplit ? 0 : c];
+        s_l[warp][col] = l[nt][kSplit ? 0 : c];
       }
+      float* to = so + (warp * C + col) * kHeadDim + 4 * g;
+      if constexpr (kSplit) {  // column 2 j + c has the sums of group 2 (j & 1) + c alone
+        const bool up = j & 1;
+        *reinterpret_cast<float4*>(to + 32 * c + (up ? 64 : 0)) =
+            make_float4(up ? o[2 + c][0][nt][c] : o[c][0][nt][c], up ? o[2 + c][0][nt][c + 2] : o[c][0][nt][c + 2],
+                        up ? o[2 + c][1][nt][c] : o[c][1][nt][c], up ? o[2 + c][1][nt][c + 2] : o[c][1][nt][c + 2]);
+      } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4*>(so + ((size_t)warp * C + col) * kHeadDim + 32 * q + 4 * g) =
-            make_float4(o[q][0][nt][c], o[q][0][nt][c + 2], o[q][1][nt][c], o[q][1][nt][c + 2]);
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(to + 32 * q) =
+              make_float4(o[q][0][nt][c], o[q][0][nt][c + 2], o[q][1][nt][c], o[q][1][nt][c + 2]);
+      }
     }
   __syncthreads();
   // a warp takes every fourth column, a lane four dims
-  const size_t slot = (size_t)((kPrefix ? 0 : plan.n_pre) + part) * a.B * a.H_q;
-  for (int col = warp; col < C; col += kWarps) {
-    const int row = column_row<kPrefix>(a, R, block, head, col);
-    if (row < 0) continue;
+  for (int col = warp; col < n_cols; col += kWarps) {
+    const Column at = column<kPrefix>(a, R, unit, block, col);
+    if (at.h < 0) continue;
     float M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][col]);
@@ -408,7 +572,7 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const float f = s_m[w][col] == -INFINITY ? 0.f : ex2_approx(s_m[w][col] - M);
-      const float4 v = *reinterpret_cast<const float4*>(so + ((size_t)w * C + col) * kHeadDim + 4 * lane);
+      const float4 v = *reinterpret_cast<const float4*>(so + (w * C + col) * kHeadDim + 4 * lane);
       // (a warp without keys, or one whose scores are all -inf, has weight 0; a NaN one shows)
       if (s_m[w][col] == -INFINITY && !(s_l[w][col] != 0.f)) continue;
       L += s_l[w][col] * f;
@@ -423,17 +587,18 @@ __global__ void __launch_bounds__(kThr) attn4_kernel(const __grid_constant__ Att
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= inv;
     const float lse = nil ? (alone && len > 0 ? NAN : -INFINITY) : M + log2f(L);
+    const size_t row = (size_t)at.b * a.H_q + at.h;
     if (alone) {
-      const int b = row / a.H_q;
-      store4(static_cast<T*>(a.out) + (size_t)b * a.o_stride + (size_t)(row - b * a.H_q) * kHeadDim + 4 * lane, x);
+      store4(static_cast<T*>(a.out) + (size_t)at.b * a.o_stride + (size_t)at.h * kHeadDim + 4 * lane, x);
       if (lane == 0 && a.lse) a.lse[row] = lse * kLn2;
     } else {
-      store4(a.part_o + (slot + row) * kHeadDim + 4 * lane, x);
-      if (lane == 0) a.part_lse[slot + row] = lse;
+      const size_t slot = (size_t)((kPrefix ? 0 : plan.n_pre) + part) * a.B * a.H_q + row;
+      store4(a.part_o + slot * kHeadDim + 4 * lane, x);
+      if (lane == 0) a.part_lse[slot] = lse;
     }
   }
   // beside the prefix's kernel: the joining one waits for this one alone
-  if (!kPrefix && blockIdx.x == 0 && threadIdx.x == 0) pdl_wait_prior();
+  if (!kPrefix && first) pdl_wait_prior();
 }
 
 // parts -> rows, a warp each
@@ -460,32 +625,39 @@ __global__ void __launch_bounds__(256) attn4_join(const __grid_constant__ AttnAr
   if (lane == 0 && a.lse) a.lse[row] = s.w == 0.f ? NAN : s.lse() * kLn2;
 }
 
-template <typename T, int NT, bool kPrefix>
+template <typename T, int NT, int kHeads, bool kPrefix>
 cudaError_t go(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
+  constexpr auto kernel = attn4_kernel<T, NT, kHeads, kPrefix>;
   static std::atomic<bool> configured[64];  // per device, zero-initialised
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev >= 0 && dev < 64 && !configured[dev]) {
-    cudaError_t e = cudaFuncSetAttribute(attn4_kernel<T, NT, kPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
+  constexpr int C = kHeads * NT;
   const long long rows = (long long)a.B * a.group;
-  const long long ctas = kPrefix ? (rows + 8 * NT - 1) / (8 * NT) * a.H_kv * plan.n_pre
-                                 : (long long)a.B * a.H_kv * plan.n_cut * plan.n_own;
-  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  const dim3 grid = kPrefix ? dim3((unsigned)((rows + C - 1) / C), plan.n_pre, a.H_kv) : dim3(a.H_kv * plan.n_cut, plan.n_own, a.B);
   if (!kPrefix && plan.n_pre > 0)  // beside the prefix's kernel, whose results it does not read
-    return launch_pdl(attn4_kernel<T, NT, kPrefix>, dim3((unsigned)ctas), dim3(kThr), kSmem, s, a, plan);
-  attn4_kernel<T, NT, kPrefix><<<(unsigned)ctas, kThr, kSmem, s>>>(a, plan);
+    return launch_pdl(kernel, grid, dim3(kThr), kSmem, s, a, plan);
+  kernel<<<grid, kThr, kSmem, s>>>(a, plan);
   return cudaGetLastError();
+}
+
+template <typename T, bool kPrefix>
+cudaError_t go_by_columns(int rows, const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
+  if (rows == 2) return go<T, 1, 2, kPrefix>(a, plan, s);
+  if (rows == 8) return go<T, 1, 8, kPrefix>(a, plan, s);
+  if constexpr (sizeof(T) == 2) return go<T, 2, 8, kPrefix>(a, plan, s);  // (fp32 at 16 columns spills registers)
+  return cudaErrorInvalidValue;
 }
 
 template <typename T>
 cudaError_t run(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  constexpr int kWide = sizeof(T) == 4 ? 1 : 2;  // (fp32 at 16 columns spills registers)
-  if (plan.n_pre > 0) e = plan.pre_cols == 16 ? go<T, kWide, true>(a, plan, s) : go<T, 1, true>(a, plan, s);
-  if (e == cudaSuccess) e = plan.own_cols == 16 ? go<T, kWide, false>(a, plan, s) : go<T, 1, false>(a, plan, s);
+  if (plan.n_pre > 0) e = go_by_columns<T, true>(plan.pre_rows, a, plan, s);
+  if (e == cudaSuccess) e = go_by_columns<T, false>(plan.own_rows, a, plan, s);
   if (e != cudaSuccess || plan.n_pre + plan.n_own <= 1) return e;
   return launch_pdl(attn4_join<T>, dim3((unsigned)(((long long)a.B * a.H_q + 7) / 8)), dim3(256), 0, s, a, plan);
 }

@@ -429,7 +429,8 @@ struct Attn4Plan {
   int n_cut;                 // virtual heads a key/value head
   int own_keys, n_own;       // keys of a part, parts at most (own; 0: none)
   int pre_keys, n_pre;       // the same for the prefix
-  int own_cols, pre_cols;    // columns a CTA: 8 or 16
+  int own_rows, pre_rows;    // query rows a CTA: 2, 8 or (bf16) 16
+  unsigned regs[3];          // constants of the codes' expansion (CodeRegs)
 };
 // part_* of AttnArgs: the prefix's parts, then the own ones (n_part in all); used where a row has more than one
 cudaError_t attn4_launch(const AttnArgs& a, const Attn4Plan& plan, int dtype, cudaStream_t s);
