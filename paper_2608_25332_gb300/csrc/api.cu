@@ -1617,7 +1617,7 @@ unsigned long long turns_of(double f) {
   const double t = f * hi, rest = fma(f, hi, -t) + f * lo;
   double frac = t - floor(t);  // exact below 1
   if (frac >= 1.) frac = 0.;
-  return (unsigned long long)ldexp(frac, 64) + (unsigned long long)(long long)ldexp(rest, 64);
+  return (unsigned long long)(frac * 0x1p64) + (unsigned long long)(long long)(rest * 0x1p64);
 }
 
 // what the rotating calls check alike, and their arguments
@@ -1682,10 +1682,10 @@ int pages_check(const char* what, const void* k_pages, const void* v_pages, int 
   return PROVIP_OK;
 }
 
-// a warp's pieces of work: at least four heads each
+// a grid's blocks: along y pieces of at least four heads, along x rows (strides of them stay below 2^31)
 int pieces_check(const char* what, int T, long long heads) {
   if (T < 0) return fail(PROVIP_ERR_INVALID_ARG, "%s: %d rows", what, T);
-  if ((heads / 4 + 3) * T > (1ll << 33)) return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows", what);
+  if (T > 0x7fffffff - (1 << 24) || heads > 4 * 65000) return fail(PROVIP_ERR_UNSUPPORTED, "%s: too many rows or heads", what);
   return PROVIP_OK;
 }
 
@@ -1710,7 +1710,7 @@ extern "C" int provip_rotate(const void* Q, long long q_stride, const void* K, l
   DevInfo* d;
   if ((rc = dev_info(&d))) return rc;
   a.err = d->status;
-  cudaError_t e = rotate_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  cudaError_t e = rotate_launch(a, dtype, d->sms, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "rotate launch");
 }
 
@@ -1745,7 +1745,7 @@ extern "C" int provip_rotate_append(const void* Q, long long q_stride, const voi
   a.k_pages = k_pages;
   a.v_pages = v_pages;
   a.err = d->status;
-  cudaError_t e = rotate_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  cudaError_t e = rotate_launch(a, dtype, d->sms, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "rotate_append launch");
 }
 
@@ -1779,7 +1779,7 @@ extern "C" int provip_kv_append4(const void* K, long long k_stride, const void* 
   a.k_pages = k_pages;
   a.v_pages = v_pages;
   a.err = d->status;
-  cudaError_t e = rotate_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  cudaError_t e = rotate_launch(a, dtype, d->sms, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "kv_append4 launch");
 }
 
@@ -1813,7 +1813,7 @@ extern "C" int provip_kv_read4(const int* slot_map, int T, int H_kv, int d_h, co
   a.k_stride = k_stride;
   a.v_stride = v_stride;
   a.err = d->status;
-  cudaError_t e = read4_launch(a, dtype, static_cast<cudaStream_t>(stream));
+  cudaError_t e = read4_launch(a, dtype, d->sms, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PROVIP_OK : cuda_fail(e, "kv_read4 launch");
 }
 

@@ -410,7 +410,7 @@ struct RotateArgs {
   void *k_pages, *v_pages;
   unsigned* err;
 };
-cudaError_t rotate_launch(const RotateArgs& a, int dtype, cudaStream_t s);
+cudaError_t rotate_launch(const RotateArgs& a, int dtype, int sms, cudaStream_t s);
 struct Read4Args {
   const uint8_t *k_pages, *v_pages;
   const int* slot_map;       // [T]
@@ -420,7 +420,7 @@ struct Read4Args {
   long long k_stride, v_stride;
   unsigned* err;
 };
-cudaError_t read4_launch(const Read4Args& a, int dtype, cudaStream_t s);
+cudaError_t read4_launch(const Read4Args& a, int dtype, int sms, cudaStream_t s);
 
 // One token per request over pages of 4 bits (attention_decode4.cu), with AttnArgs' paged fields.
 // Columns: the query rows that share keys. Own keys: the heads of a virtual key/value head (a

@@ -16,10 +16,12 @@
 // values 32 q + 4 g .. + 3, the first in the lowest bits. (So eight bytes hold four values of each
 // group, and a lane of the decoding kernel gets whole groups' operands from what it loads.)
 //
-// A warp handles up to kIter times four heads of a row: eight lanes a head, lane l with values 8 l
-// .. + 7 and 64 + 8 l .. + 7, which are pairs. A row's 64 sines are worked out two a lane and passed
-// round. Bound by HBM (each value is read and written once) from about a thousand rows on, below
-// that by the launch.
+// A warp handles four heads of a row at a time: eight lanes a head, lane l with values 8 l .. + 7 and
+// 64 + 8 l .. + 7, which are pairs. A row's 64 sines are worked out two a lane and passed round. Each value is
+// read and written once; what bounds that beyond a thousand rows is the SMs' issue slots rather than HBM where
+// heads are normed or brought to 4 bits (250 instructions for four heads): 8725 rows of 96 heads into pages in
+// 65 us (6.6 TB/s), 9379 of 32 heads with norms in 31 (5.0), 8725 of 64 heads to 4 bits in 45 (4.1 TB/s). Below
+// that it is the launch.
 #include "common.cuh"
 #include "kernels.h"
 
@@ -27,6 +29,12 @@ namespace provip {
 namespace {
 
 constexpr int kThr = 256;
+// Rotation: rows ahead a warp, bytes of a row's piece at most, blocks an SM (the registers' limit), rows from
+// which pieces are that large. (A video's 9379 rows of 32 heads, normed: pieces of 2 KiB 38 us, 4 KiB 31, 8 KiB 37;
+// three blocks an SM 33; four rows ahead instead of two, no change.)
+constexpr int kRing = 2, kPieceBytes = 4096, kRotateBlocks = 2, kRotateWide = 512;
+// Reading: blocks, an SM's.
+constexpr int kReadBlocks = 12;
 
 // 8 + 8 values of a head's lane
 template <typename T>
@@ -92,42 +100,84 @@ struct Raw<float> {
   }
 };
 
-// The scale of a group whose eight values a lane are x, over the four lanes that hold it.
-__device__ __forceinline__ float group_scale(const float* x, uint16_t& bits) {
-  // magnitude above the sign: the positive of two equal ones is the larger
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t b = __float_as_uint(x[i]);
-    m = max(m, ((b << 1) | (b >> 31)) ^ 1u);
-  }
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  const float mag = __uint_as_float(m >> 1);
-  float d = mag * 0.125f;
-  if (m & 1u) d = -d;
-  __nv_bfloat16 h = __float2bfloat16_rn(d);
+__device__ __forceinline__ float max_nan(float x, float y) {  // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+// A group's scale from its largest magnitude, the positive one of two.
+__device__ __forceinline__ float scale_of(float most, bool positive, uint16_t& bits) {
+  const __nv_bfloat16 h = __float2bfloat16_rn(positive ? most * -0.125f : most * 0.125f);
   bits = *reinterpret_cast<const uint16_t*>(&h);
-  if (!(mag < 0x1p100f)) bits = 0x7fff;
-  if (mag < 0x1p-123f) bits = 0;
+  if (!(most < 0x1p100f)) bits = 0x7fff;
+  if (most < 0x1p-123f) bits = 0;
   return __uint_as_float((uint32_t)bits << 16);
 }
-// codes of eight values: four of them in each half of the result
-__device__ __forceinline__ uint32_t group_codes(const float* x, float d) {
-  const float r = d == 0.f ? 0.f : __frcp_rn(d);
-  uint32_t w = 0;
+// The scale of group k of two (0: values 0 .. 7 of each lane) over the four lanes that hold it.
+__device__ __forceinline__ float group_scale(const Raw<float>& raw, int k, uint16_t& bits) {
+  float x[16];
+  raw.get(x);
+  float most = fabsf(x[8 * k]), top = x[8 * k];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = fminf(fmaxf(__fmul_rn(x[i], r), -8.f), 7.f);
-    w |= (__float_as_uint(__fadd_rn(y, 12582920.f)) & 15u) << (4 * i);  // 3 * 2^22 + 8: the sum's unit is 1
+  for (int i = 1; i < 8; ++i) {
+    most = max_nan(most, fabsf(x[8 * k + i]));
+    top = fmaxf(top, x[8 * k + i]);
   }
-  return w;
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  }
+  return scale_of(most, top == most, bits);
+}
+// bf16 as 16-bit integers: magnitudes order as unsigned ones (NaN above all), positive values as signed ones above
+// the negative, which is all that is asked of them. Both maxima go round in one word, the signed one shifted to be
+// unsigned.
+__device__ __forceinline__ float group_scale(const Raw<__nv_bfloat16>& raw, int k, uint16_t& bits) {
+  const uint32_t w[4] = {raw.u[k].x, raw.u[k].y, raw.u[k].z, raw.u[k].w};
+  uint32_t most = w[0] & 0x7fff7fffu, top = w[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    most = __vmaxu2(most, w[i] & 0x7fff7fffu);
+    top = __vmaxs2(top, w[i]);
+  }
+  most = __vmaxu2(most, most >> 16);
+  top = __vmaxs2(top, __byte_perm(top, top, 0x1032)) ^ 0x80008000u;
+  uint32_t both = __byte_perm(most, top, 0x5410);
+  both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 1));
+  both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 2));
+  return scale_of(__uint_as_float(both << 16), ((both >> 16) ^ 0x8000u) == (both & 0xffffu), bits);
+}
+// 1 / d rounded to nearest, for a normal d of eight bits whose reciprocal is normal: a step of Newton's iteration,
+// r + r (1 - d r), on the hardware's approximation (all 256 such fractions give __frcp_rn's result).
+__device__ __forceinline__ float reciprocal(float d) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  return fmaf(r, fmaf(-d, r, 1.f), r);
+}
+// Codes of eight values: four of them in each half of the result. No quotient is below -8.1, which rounds
+// to -8. A sum with 3 * 2^22 + 8 has a unit of 1, and so the code in its lowest bits, with nothing else below bit 22: multiplied
+// by 1, 16, 256 and 4096 and added up, four of them leave their codes side by side in the lower half.
+__device__ __forceinline__ uint32_t group_codes(const float* x, float d) {
+  const float r = d == 0.f ? 0.f : reciprocal(d);
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    uint32_t n[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n[i] = __float_as_uint(__fadd_rn(fminf(__fmul_rn(x[4 * k + i], r), 7.f), 12582920.f));
+    w[k] = n[0] + n[1] * 16u + n[2] * 256u + n[3] * 4096u;
+  }
+  return __byte_perm(w[0], w[1], 0x5410);
 }
 
 // A head's row (eight lanes with 16 values each) into its place in 4-bit pages.
-__device__ __forceinline__ void store4bit(const float* x, uint8_t* codes, uint8_t* scales, int l, bool on) {
+template <typename T>
+__device__ __forceinline__ void store4bit(const Raw<T>& raw, uint8_t* codes, uint8_t* scales, int l, bool on) {
   uint16_t b0, b1;
-  const float d0 = group_scale(x, b0), d1 = group_scale(x + 8, b1);
+  const float d0 = group_scale(raw, 0, b0), d1 = group_scale(raw, 1, b1);
+  float x[16];
+  raw.get(x);
   const uint32_t c0 = group_codes(x, d0), c1 = group_codes(x + 8, d1);
   // lanes 0-3 hold groups 0 and 2, lanes 4-7 groups 1 and 3 of the same places: one keeps its lower
   // four values of each, the other its upper ones
@@ -155,120 +205,202 @@ __device__ __forceinline__ size_t place4(long long slot, int h, int H_kv, int pa
   return ((size_t)(page * H_kv + h) << page_shift) * kRow4 + (size_t)row * kCodes4;
 }
 
-template <typename T, int ITER>
-__global__ void __launch_bounds__(kThr) rotate_kernel(const __grid_constant__ RotateArgs a, int per_row, int q_items, int k_items) {
-  const int lane = threadIdx.x & 31, l = lane & 7;
-  const long long item = (long long)blockIdx.x * (kThr / 32) + (threadIdx.x >> 5);
-  const long long t = item / per_row;
-  if (t >= a.T) return;
+// Blocks along y: pieces of up to kPieceBytes of heads, queries', then keys', then values'; along x: rows, a row a
+// warp at a time. A warp keeps what its piece needs of every row (frequencies, axes, norm weights) in registers;
+// the rows' values come through a ring of its own in shared memory, kRing rows ahead, by bulk copies (heads of a
+// row lie next to each other). Waits are bounded; one that gives up sets the error word and ends the warp once
+// its copies are done.
+template <typename T>
+__global__ void __launch_bounds__(kThr, kRotateBlocks) rotate_kernel(const __grid_constant__ RotateArgs a, int heads, int q_items, int k_items) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t full[kThr / 32][kRing];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane & 7;
+  int n = a.T;
   if (a.n_rows) {
-    const int n = *a.n_rows;
-    if (item == 0 && lane == 0 && (n < 0 || n > a.T)) set_error(a.err, kErrBadDeviceArg);
-    if (t >= n) return;
+    const int m = *a.n_rows;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && (m < 0 || m > a.T)) set_error(a.err, kErrBadDeviceArg);
+    n = min(m, a.T);
   }
-  int part = (int)(item - t * per_row);
+  const int step = gridDim.x * (kThr / 32);
+  int t = blockIdx.x * (kThr / 32) + warp;
+  if (t >= n) return;
+  int piece = blockIdx.y;
   // 0: queries, 1: keys, 2: values
-  const int kind = part < q_items ? 0 : part < q_items + k_items ? 1 : 2;
-  if (kind == 1) part -= q_items;
-  if (kind == 2) part -= q_items + k_items;
-  const int H = kind == 0 ? a.H_q : a.H_kv, h0 = part * (4 * ITER) + (lane >> 3);
-  const T* src = kind == 0 ? static_cast<const T*>(a.Q) + t * a.q_stride
-                 : kind == 1 ? static_cast<const T*>(a.K) + t * a.k_stride
-                             : static_cast<const T*>(a.V) + t * a.v_stride;
-  Raw<T> raw[ITER];
-#pragma unroll
-  for (int i = 0; i < ITER; ++i)
-    if (h0 + 4 * i < H) raw[i].load(src + (size_t)(h0 + 4 * i) * kHeadDim + l * 8);
-  // where the row goes
-  T* out = kind == 0 ? static_cast<T*>(a.q_out) + t * a.qo_stride
-           : kind == 1 && a.k_out ? static_cast<T*>(a.k_out) + t * a.ko_stride : nullptr;
-  long long slot = -1;
-  if (kind != 0 && a.slot_map) {
-    slot = a.slot_map[t];
-    if (slot >= a.n_slots) {
-      if (lane == 0) set_error(a.err, kErrBadDeviceArg);
-      slot = -1;
-    }
+  const int kind = piece < q_items ? 0 : piece < q_items + k_items ? 1 : 2;
+  piece -= kind == 0 ? 0 : kind == 1 ? q_items : q_items + k_items;
+  const int h_lo = piece * heads, n_heads = min(heads, (kind == 0 ? a.H_q : a.H_kv) - h_lo);
+  const long long stride = (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) * (long long)sizeof(T);
+  const uint8_t* src = static_cast<const uint8_t*>(kind == 0 ? a.Q : kind == 1 ? a.K : a.V) + (size_t)h_lo * kHeadDim * sizeof(T);
+  const uint32_t bytes = n_heads * kHeadDim * (int)sizeof(T);
+  uint8_t* ring = smem + warp * (kRing * kPieceBytes);
+  auto load = [&](int row, int stage) {  // (one lane)
+    mbar_arrive_expect_tx(&full[warp][stage], bytes);
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     smem_u32(ring + stage * kPieceBytes)),
+                 "l"(src + row * stride), "r"(bytes), "r"(smem_u32(&full[warp][stage]))
+                 : "memory");
+  };
+  if (lane == 0) {
+    for (int i = 0; i < kRing; ++i) mbar_init(&full[warp][i], 1);
+    fence_mbar_init();
+    for (int i = 0; i < kRing; ++i)
+      if ((long long)t + (long long)i * step < n) load(t + i * step, i);
   }
-  if (out == nullptr && slot < 0) return;
-  uint8_t* pages = static_cast<uint8_t*>(kind == 1 ? a.k_pages : a.v_pages);
-  const bool turn = a.turn && kind != 2;
-  float c[8], s[8];
+  __syncwarp();
+  T* out = kind == 0 ? static_cast<T*>(a.q_out) : kind == 1 ? static_cast<T*>(a.k_out) : nullptr;
+  const long long o_stride = kind == 0 ? a.qo_stride : a.ko_stride;
+  if (out) out += (size_t)h_lo * kHeadDim;
+  const bool paged = kind != 0 && a.slot_map != nullptr, turn = a.turn && kind != 2;
+  void* pages = kind == 1 ? a.k_pages : a.v_pages;
+  // pairs 2 lane, 2 lane + 1: this lane's sines and cosines
+  unsigned long long turns[2] = {0, 0};
+  const int* pos[2] = {nullptr, nullptr};
   if (turn) {
-    float s2[2], c2[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int p = 2 * lane + i;
-      const long long at = a.pos[a.axis[p] * a.pos_stride + t];
-      const int part_turn = (int)(((unsigned long long)at * a.turns[p]) >> 32);  // 2^-32 of a turn, signed
-      sincospif((float)part_turn * 0x1p-31f, &s2[i], &c2[i]);
-      s2[i] *= a.factor;
-      c2[i] *= a.factor;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s[i] = __shfl_sync(0xffffffffu, s2[i & 1], 4 * l + (i >> 1));
-      c[i] = __shfl_sync(0xffffffffu, c2[i & 1], 4 * l + (i >> 1));
+      turns[i] = a.turns[2 * lane + i];
+      pos[i] = a.pos + a.axis[2 * lane + i] * a.pos_stride;
     }
   }
   const T* w = turn ? static_cast<const T*>(kind == 0 ? a.wq : a.wk) : nullptr;
-  float g[16];
-  if (w) {
-    Raw<T> r;
-    r.load(w + l * 8);
-    r.get(g);
-  }
+  Raw<T> weights;
+  if (w) weights.load(w + l * 8);
+  // bytes of a head's row's places: in an output, and in pages from one head to the next
+  const uint32_t lane_at = (uint32_t)((lane >> 3) * kHeadDim + l * 8);
+  const size_t head4 = (size_t)kRow4 << a.page_shift;
+  int p[2] = {0, 0}, slot = -1;
+  auto fetch = [&](int row) {
+    if (turn) {
+      p[0] = __ldg(pos[0] + row);
+      p[1] = __ldg(pos[1] + row);
+    }
+    if (paged) slot = __ldg(a.slot_map + row);
+  };
+  fetch(t);
+  int stage = 0;
+  uint32_t phase = 0;
+  for (;;) {
+    // y_i = x_i c_i - x_{i+64} s_i and y_{i+64} = x_{i+64} c_i + x_i s_i, each x with its norm weight: the four factors
+    float c0[8], c1[8], s0[8], s1[8];
+    if (turn) {
+      float s2[2], c2[2];
 #pragma unroll
-  for (int i = 0; i < ITER; ++i) {
-    const int h = h0 + 4 * i;
-    const bool on = h < H;
-    if (h - (lane >> 3) >= H) break;  // (the whole warp)
-    if (turn || a.four) {
-      float x[16];
-      if (on) {
-        raw[i].get(x);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = 0.f;
+      for (int i = 0; i < 2; ++i) {
+        const int part = (int)(((unsigned long long)(long long)p[i] * turns[i]) >> 32);  // 2^-32 of a turn, signed
+        sincospif((float)part * 0x1p-31f, &s2[i], &c2[i]);
+        s2[i] *= a.factor;
+        c2[i] *= a.factor;
       }
-      if (turn) {
-        if (w) {
-          float ss = 0.f;
+      float g[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+      for (int e = 0; e < 16; ++e) g[e] = 1.f;
+      if (w) weights.get(g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float s = __shfl_sync(0xffffffffu, s2[i & 1], 4 * l + (i >> 1)), c = __shfl_sync(0xffffffffu, c2[i & 1], 4 * l + (i >> 1));
+        c0[i] = c * g[i];
+        s1[i] = s * g[i];
+        c1[i] = c * g[i + 8];
+        s0[i] = s * g[i + 8];
+      }
+    }
+    const int row = t;
+    long long at = slot;
+    if (at >= a.n_slots) {
+      if (paged && lane == 0) set_error(a.err, kErrBadDeviceArg);
+      at = -1;
+    }
+    t += step;
+    if (t < n) fetch(t);
+    if (__any_sync(0xffffffffu, !mbar_wait(&full[warp][stage], phase, a.err))) {
+      // the copies still in flight, from this row's on, once more with a limit
+      int st = stage;
+      uint32_t ph = phase;
+      for (int i = 0; i < kRing && (long long)row + (long long)i * step < n; ++i) {
+        mbar_wait(&full[warp][st], ph, a.err);
+        if (++st == kRing) {
+          st = 0;
+          ph ^= 1;
+        }
+      }
+      return;
+    }
+    const T* from = reinterpret_cast<const T*>(ring + stage * kPieceBytes);
+    T* to = out ? out + row * o_stride + lane_at : nullptr;
+    // this lane's head in pages: its row, or its codes and its scales
+    const bool keep = paged && at >= 0;
+    uint8_t* in_page = static_cast<uint8_t*>(pages);
+    size_t scales = 0;
+    if (keep) {
+      if (a.four)
+        in_page += place4(at, h_lo + (lane >> 3), a.H_kv, a.page_shift, &scales);
+      else
+        in_page += (((size_t)at * a.H_kv + h_lo) * kHeadDim + lane_at) * sizeof(T);
+    }
+#pragma unroll 1
+    for (int h4 = 0; h4 < n_heads; h4 += 4) {
+      const bool on = h4 + (lane >> 3) < n_heads;
+      Raw<T> now;
+      now.load(from + (on ? lane_at : (uint32_t)(l * 8)) + h4 * kHeadDim);
+      if (turn) {
+        float x[16], r = 1.f;
+        now.get(x);
+        if (w) {
+          float ss = 0.f, st = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            ss = fmaf(x[e], x[e], ss);
+            st = fmaf(x[e + 8], x[e + 8], st);
+          }
+          ss += st;
 #pragma unroll
           for (int o = 1; o < 8; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float r = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = x[e] * r * g[e];
+          r = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float u = x[e], v = x[e + 8];
-          x[e] = u * c[e] - v * s[e];
-          x[e + 8] = v * c[e] + u * s[e];
+          x[e] = u * c0[e] - v * s0[e];
+          x[e + 8] = v * c1[e] + u * s1[e];
         }
-        raw[i].set(x);
-        raw[i].get(x);  // the cache takes in what k_out holds
+        if (w) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] *= r;
+        }
+        now.set(x);
       }
-      if (a.four && slot >= 0 && kind != 0) {
-        size_t scales;
-        uint8_t* at = pages + place4(slot, on ? h : 0, a.H_kv, a.page_shift, &scales);
-        store4bit(x, at, at + scales, l, on);
-      }
+      // (4 bits take in what k_out holds)
+      if (keep && a.four) store4bit(now, in_page + (h4 * head4), in_page + (h4 * head4 + scales), l, on);
+      if (!on) continue;
+      if (to) now.store(to + h4 * kHeadDim);
+      if (keep && !a.four) now.store(reinterpret_cast<T*>(in_page) + h4 * kHeadDim);
     }
-    if (on && out) raw[i].store(out + (size_t)h * kHeadDim + l * 8);
-    if (on && !a.four && slot >= 0)
-      raw[i].store(reinterpret_cast<T*>(pages) + ((size_t)slot * a.H_kv + h) * kHeadDim + l * 8);
+    __syncwarp();  // every lane has read the stage
+    if (lane == 0 && (long long)row + (long long)kRing * step < n) load(row + kRing * step, stage);
+    if (++stage == kRing) {
+      stage = 0;
+      phase ^= 1;
+    }
+    if (t >= n) break;
   }
 }
 
-template <typename T, int ITER>
-cudaError_t rotate_go(const RotateArgs& a, cudaStream_t s) {
-  const int per = 4 * ITER;
-  const int q = a.Q ? (a.H_q + per - 1) / per : 0, k = a.K ? (a.H_kv + per - 1) / per : 0, v = a.V ? (a.H_kv + per - 1) / per : 0;
-  const long long items = (long long)(q + k + v) * a.T;
-  rotate_kernel<T, ITER><<<(unsigned)((items + kThr / 32 - 1) / (kThr / 32)), kThr, 0, s>>>(a, q + k + v, q, k);
+// Pieces of 4 KiB (sixteen heads in bf16, eight in fp32) where the rows fill the SMs with them, else of four heads.
+template <typename T>
+cudaError_t rotate_go(const RotateArgs& a, int sms, cudaStream_t s) {
+  static std::atomic<bool> configured[64];  // per device, zero-initialised
+  constexpr int smem = kThr / 32 * kRing * kPieceBytes;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    configured[dev] = true;
+  }
+  const int heads = a.T >= kRotateWide ? kPieceBytes / (kHeadDim * (int)sizeof(T)) : 4;
+  const int q = a.Q ? (a.H_q + heads - 1) / heads : 0, k = a.K ? (a.H_kv + heads - 1) / heads : 0, v = a.V ? (a.H_kv + heads - 1) / heads : 0;
+  const int all = (a.T + kThr / 32 - 1) / (kThr / 32), most = kRotateBlocks * sms / (q + k + v);
+  rotate_kernel<T><<<dim3((unsigned)min(all, max(most, 1)), q + k + v), kThr, smem, s>>>(a, heads, q, k);
   return cudaGetLastError();
 }
 
@@ -276,66 +408,58 @@ cudaError_t rotate_go(const RotateArgs& a, cudaStream_t s) {
 // rows out of 4-bit pages: the same eight lanes a head. Lane l's values lie in 16 bytes of codes,
 // which lanes l and l + 4 share.
 // ---------------------------------------------------------------------------
-template <typename T, int ITER>
-__global__ void __launch_bounds__(kThr) read4_kernel(const __grid_constant__ Read4Args a, int per_row) {
+template <typename T>
+__global__ void __launch_bounds__(kThr) read4_kernel(const __grid_constant__ Read4Args a) {
   const int lane = threadIdx.x & 31, l = lane & 7;
-  const long long item = (long long)blockIdx.x * (kThr / 32) + (threadIdx.x >> 5);
-  const long long t = item / per_row;
-  if (t >= a.T) return;
-  const int h0 = (int)(item - t * per_row) * (4 * ITER) + (lane >> 3);
-  const long long slot = a.slot_map[t];
-  if (slot < 0) return;
-  if (slot >= a.n_slots) {
-    if (lane == 0) set_error(a.err, kErrBadDeviceArg);
-    return;
-  }
-  const uint8_t* pages = blockIdx.y ? a.v_pages : a.k_pages;
-  T* out = static_cast<T*>(blockIdx.y ? a.v_out : a.k_out) + t * (blockIdx.y ? a.v_stride : a.k_stride);
-  uint4 codes[ITER];
-  uint2 scales[ITER];
-#pragma unroll
-  for (int i = 0; i < ITER; ++i) {
-    if (h0 + 4 * i >= a.H_kv) continue;
-    size_t behind;
-    const uint8_t* at = pages + place4(slot, h0 + 4 * i, a.H_kv, a.page_shift, &behind);
-    codes[i] = *reinterpret_cast<const uint4*>(at + (l & 3) * 16);
-    scales[i] = *reinterpret_cast<const uint2*>(at + behind);
-  }
+  const int h = blockIdx.y * 4 + (lane >> 3);
+  if (h >= a.H_kv) return;
+  const uint8_t* pages = blockIdx.z ? a.v_pages : a.k_pages;
+  const long long stride = blockIdx.z ? a.v_stride : a.k_stride;
+  T* out = static_cast<T*>(blockIdx.z ? a.v_out : a.k_out) + (size_t)h * kHeadDim + l * 8;
   const uint32_t half = l & 4 ? 0x7632 : 0x5410;
-#pragma unroll
-  for (int i = 0; i < ITER; ++i) {
-    if (h0 + 4 * i >= a.H_kv) continue;
-    const uint32_t c[2] = {__byte_perm(codes[i].x, codes[i].z, half), __byte_perm(codes[i].y, codes[i].w, half)};
-    const uint32_t b[2] = {scales[i].x, scales[i].y};
+  for (int t = blockIdx.x * (kThr / 32) + (threadIdx.x >> 5); t < a.T; t += gridDim.x * (kThr / 32)) {
+    const long long slot = __ldg(a.slot_map + t);
+    if (slot < 0) continue;
+    if (slot >= a.n_slots) {
+      if (lane == 0) set_error(a.err, kErrBadDeviceArg);
+      continue;
+    }
+    size_t behind;
+    const uint8_t* at = pages + place4(slot, h, a.H_kv, a.page_shift, &behind);
+    const uint4 codes = *reinterpret_cast<const uint4*>(at + (l & 3) * 16);
+    const uint2 scales = *reinterpret_cast<const uint2*>(at + behind);
+    const uint32_t c[2] = {__byte_perm(codes.x, codes.z, half), __byte_perm(codes.y, codes.w, half)};
+    const uint32_t b[2] = {scales.x, scales.y};
     float x[16];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const float d = __uint_as_float(l & 4 ? b[k] & 0xffff0000u : b[k] << 16);
+      // (2^23 + n less 2^23 + 8: n - 8 exactly)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[8 * k + e] = d * (float)((int)((c[k] >> (4 * e)) & 15u) - 8);
+      for (int e = 0; e < 8; ++e) x[8 * k + e] = d * (__uint_as_float(0x4b000000u | ((c[k] >> (4 * e)) & 15u)) - 8388616.f);
     }
     Raw<T> r;
     r.set(x);
-    r.store(out + (size_t)(h0 + 4 * i) * kHeadDim + l * 8);
+    r.store(out + t * stride);
   }
 }
 
-template <typename T, int ITER>
-cudaError_t read4_go(const Read4Args& a, cudaStream_t s) {
-  const int per_row = (a.H_kv + 4 * ITER - 1) / (4 * ITER);
-  const long long items = (long long)per_row * a.T;
-  read4_kernel<T, ITER><<<dim3((unsigned)((items + kThr / 32 - 1) / (kThr / 32)), 2), kThr, 0, s>>>(a, per_row);
+template <typename T>
+cudaError_t read4_go(const Read4Args& a, int blocks, cudaStream_t s) {
+  const int pieces = (a.H_kv + 3) / 4, all = (a.T + kThr / 32 - 1) / (kThr / 32), most = blocks / (2 * pieces);
+  read4_kernel<T><<<dim3((unsigned)min(all, max(most, 1)), pieces, 2), kThr, 0, s>>>(a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t rotate_launch(const RotateArgs& a, int dtype, cudaStream_t s) {
-  return dtype == 0 ? rotate_go<float, 1>(a, s) : rotate_go<__nv_bfloat16, 1>(a, s);
+cudaError_t rotate_launch(const RotateArgs& a, int dtype, int sms, cudaStream_t s) {
+  return dtype == 0 ? rotate_go<float>(a, sms, s) : rotate_go<__nv_bfloat16>(a, sms, s);
 }
 
-cudaError_t read4_launch(const Read4Args& a, int dtype, cudaStream_t s) {
-  return dtype == 0 ? read4_go<float, 1>(a, s) : read4_go<__nv_bfloat16, 1>(a, s);
+cudaError_t read4_launch(const Read4Args& a, int dtype, int sms, cudaStream_t s) {
+  const int blocks = kReadBlocks * sms;
+  return dtype == 0 ? read4_go<float>(a, blocks, s) : read4_go<__nv_bfloat16>(a, blocks, s);
 }
 
 }  // namespace provip

@@ -770,56 +770,72 @@ class Rotary:
             raise ProvipError(ERR_INVALID_ARG, "Rotary: 64 frequencies and 64 axes from 0 on, one a pair")
         self.n_axes, self.factor = max(axis) + 1, float(factor)
         self.inv_freq, self.axis = (ctypes.c_double * 64)(*freq), (ctypes.c_int * 64)(*axis)
+        self.args = (self.n_axes, ctypes.addressof(self.inv_freq), ctypes.addressof(self.axis), self.factor)
 
 
-def _norm(w, dtype, what):
+# (The checks below look at each property of a tensor once, and at its device by number: a property takes
+# 0.1 to 0.2 us, and a call has up to nine tensors and 8 us on the GPU's side.)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _heads(t, T, H, dtype, dev, what):
+    """pointer and row stride (elements) of rows [T, H, 128] as _rows takes them, on device number dev"""
+    if t.dtype is not dtype or t.get_device() != dev or dev < 0 or tuple(t.shape) != (T, H, 128):
+        raise ProvipError(ERR_INVALID_ARG, f"{what} must be {dtype} [{T}, {H}, 128] on GPU {dev}: got {t.dtype} {list(t.shape)} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 or (s1 != 128 and H > 1)) and T:
+        raise ProvipError(ERR_INVALID_ARG, f"{what}: the heads of a row must lie next to each other")
+    return t.data_ptr(), (s0 if T > 1 else H * 128)
+
+
+def _norm(w, dtype, dev, what):
     if w is None:
         return None
-    if not w.is_cuda or w.dtype is not dtype or w.numel() != 128 or not w.is_contiguous():
-        raise ProvipError(ERR_INVALID_ARG, f"{what} must be a contiguous {dtype} GPU tensor of 128 entries")
+    if w.dtype is not dtype or w.get_device() != dev or w.numel() != 128 or not w.is_contiguous():
+        raise ProvipError(ERR_INVALID_ARG, f"{what} must be a contiguous {dtype} tensor of 128 entries on GPU {dev}")
     return w.data_ptr()
 
 
-def _positions(pos, T, n_axes):
+def _positions(pos, T, n_axes, dev):
     """pointer and axis stride of position ids [axes, T] (or [axes, B, L] with T = B L)"""
     if pos.dim() == 3 and pos.is_contiguous():
         pos = pos.view(pos.shape[0], -1)
-    if pos.dtype is not torch.int32 or not pos.is_cuda or pos.dim() != 2 or pos.shape[0] < n_axes or pos.shape[1] != T or \
-            (T > 1 and pos.stride(1) != 1):
-        raise ProvipError(ERR_INVALID_ARG, f"pos must be an int32 GPU tensor of at least {n_axes} axes by {T} rows")
+    shape, stride = pos.shape, pos.stride()
+    if pos.dtype is not torch.int32 or pos.get_device() != dev or len(shape) != 2 or shape[0] < n_axes or shape[1] != T or \
+            (T > 1 and stride[1] != 1):
+        raise ProvipError(ERR_INVALID_ARG, f"pos must be an int32 tensor of at least {n_axes} axes by {T} rows on GPU {dev}")
     # (one axis alone may have any stride)
-    return pos.data_ptr(), pos.stride(0) if n_axes > 1 and T > 0 else T
+    return pos.data_ptr(), stride[0] if n_axes > 1 and T > 0 else T
 
 
-def _same_device(what, *tensors):
-    dev = tensors[0].device
-    if any(t is not None and t.device != dev for t in tensors):
-        raise ProvipError(ERR_INVALID_ARG, f"{what}: tensors on different devices")
-    return dev
+def _index(t, n, dev, what):
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous() or t.numel() < n:
+        raise ProvipError(ERR_INVALID_ARG, f"{what} must be a contiguous int32 tensor of {n} entries on GPU {dev}")
+    return t.data_ptr()
 
 
-def _on(dev, call, *args):
-    """a library call with its tensors' device current, whichever the caller's is"""
-    if dev.index == torch.cuda.current_device():
-        return call(*args)
-    with torch.cuda.device(dev):
-        return call(*args)
+def _call(dev, what, call, *args):
+    """a library call with its tensors' device current, whichever the caller's is, on that device's stream"""
+    if dev == _raw_device():
+        rc = call(*args, _raw_stream(dev) if _raw_stream is not None else _stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = call(*args, _stream(dev))
+    if rc != OK:
+        _check(rc, what)
 
 
-def _rotate_head(what, Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out):
-    """the arguments that the rotating calls share: inputs, what goes by positions, outputs"""
-    dtype, T = Q.dtype, Q.shape[0]
-    q, qs = _rows(Q, Q.shape[1], dtype, "Q")
-    k, ks = _rows(K, K.shape[1], dtype, "K")
-    if K.shape[0] != T or q_out.shape[0] != T or (k_out is not None and k_out.shape[0] != T):
-        raise ProvipError(ERR_INVALID_ARG, f"{what}: Q, K or an output has another number of rows")
-    qo, qos = _rows(q_out, Q.shape[1], dtype, "q_out")
-    ko, kos = (None, 0) if k_out is None else _rows(k_out, K.shape[1], dtype, "k_out")
-    p, ps = _positions(pos, T, rotary.n_axes)
-    by = (None if n_rows is None else _ints(n_rows, 1, "n_rows"), Q.shape[1], K.shape[1], 128, p, ps, rotary.n_axes,
-          rotary.inv_freq, rotary.axis, rotary.factor, _norm(q_norm, dtype, "q_norm"), _norm(k_norm, dtype, "k_norm"),
-          float(eps), _dtype_of(dtype))
-    return (q, qs, k, ks), by, (qo, qos, ko, kos)
+def _rotate_args(Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out):
+    """the arguments that the rotating calls share: inputs, what goes by positions, outputs, their device"""
+    dtype, dev, (T, H_q, _), H = Q.dtype, Q.get_device(), Q.shape, K.shape[1]
+    q, qs = _heads(Q, T, H_q, dtype, dev, "Q")
+    k, ks = _heads(K, T, H, dtype, dev, "K")
+    qo, qos = _heads(q_out, T, H_q, dtype, dev, "q_out")
+    ko, kos = (None, 0) if k_out is None else _heads(k_out, T, H, dtype, dev, "k_out")
+    p, ps = _positions(pos, T, rotary.n_axes, dev)
+    by = (None if n_rows is None else _index(n_rows, 1, dev, "n_rows"), H_q, H, 128, p, ps, *rotary.args,
+          _norm(q_norm, dtype, dev, "q_norm"), _norm(k_norm, dtype, dev, "k_norm"), eps, _dtype_of(dtype))
+    return (q, qs, k, ks), by, (qo, qos, ko, kos), dev
 
 
 def provip_rotate(Q, K, pos, rotary, q_norm=None, k_norm=None, eps=1e-6, out=None, n_rows=None):
@@ -828,10 +844,8 @@ def provip_rotate(Q, K, pos, rotary, q_norm=None, k_norm=None, eps=1e-6, out=Non
     themselves; n_rows: device count of rows (such as row_start[B:]), past which rows are left untouched.
     Returns (q_out, k_out)."""
     q_out, k_out = out if out is not None else (Q.new_empty(Q.shape), K.new_empty(K.shape))
-    ins, by, outs = _rotate_head("rotate", Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out)
-    dev = _same_device("rotate", Q, K, pos, q_norm, k_norm, n_rows, q_out, k_out)
-    rc = _on(dev, lib().provip_rotate, *ins, Q.shape[0], *by, *outs, _stream(dev))
-    _check(rc, "provip_rotate")
+    ins, by, outs, dev = _rotate_args(Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out)
+    _call(dev, "provip_rotate", lib().provip_rotate, *ins, Q.shape[0], *by, *outs)
     return q_out, k_out
 
 
@@ -840,13 +854,14 @@ def pages4(n_pages, page_size, H_kv, device="cuda"):
     return torch.zeros(n_pages, H_kv, page_size * ROW4, dtype=torch.uint8, device=device)
 
 
-def _pages4(k_pages, v_pages, H):
+def _pages4(k_pages, v_pages, H, dev):
     """pointers of two 4-bit pools, their pages and rows a page"""
+    shape = k_pages.shape
     for t in (k_pages, v_pages):
-        if not t.is_cuda or not t.is_contiguous() or t.dim() != 3 or t.dtype is not torch.uint8 or t.shape[1] != H or \
-                t.shape[2] % ROW4 or t.shape != k_pages.shape:
-            raise ProvipError(ERR_INVALID_ARG, f"4-bit pages must be contiguous uint8 GPU tensors [n_pages, {H}, page_size * {ROW4}]")
-    return k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0], k_pages.shape[2] // ROW4
+        if t.dtype is not torch.uint8 or t.get_device() != dev or dev < 0 or t.shape != shape or len(shape) != 3 or shape[1] != H or \
+                shape[2] % ROW4 or not t.is_contiguous():
+            raise ProvipError(ERR_INVALID_ARG, f"4-bit pages must be contiguous uint8 tensors [n_pages, {H}, page_size * {ROW4}] on GPU {dev}")
+    return k_pages.data_ptr(), v_pages.data_ptr(), shape[0], shape[2] // ROW4
 
 
 def provip_rotate_append(Q, K, V, pos, rotary, slot_map, k_pages, v_pages, q_norm=None, k_norm=None, eps=1e-6, out=None,
@@ -855,57 +870,46 @@ def provip_rotate_append(Q, K, V, pos, rotary, slot_map, k_pages, v_pages, q_nor
     pages on the way: [n_pages, page_size, H_kv, 128] of the rows' type, or 4-bit ones (uint8, see pages4).
     out: (q_out, k_out or None) to write. Returns (q_out, k_out), the latter None unless given or want_k."""
     q_out, k_out = out if out is not None else (Q.new_empty(Q.shape), K.new_empty(K.shape) if want_k else None)
-    ins, by, outs = _rotate_head("rotate_append", Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out)
-    T, H = K.shape[0], K.shape[1]
-    v, vs = _rows(V, H, Q.dtype, "V")
-    if V.shape[0] != T:
-        raise ProvipError(ERR_INVALID_ARG, "rotate_append: V has another number of rows")
+    ins, by, outs, dev = _rotate_args(Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out)
+    T, H, dtype = Q.shape[0], K.shape[1], Q.dtype
+    v, vs = _heads(V, T, H, dtype, dev, "V")
     four = k_pages.dtype is torch.uint8
     if four:
-        kp, vp, n, ps = _pages4(k_pages, v_pages, H)
+        kp, vp, n, ps = _pages4(k_pages, v_pages, H, dev)
     else:
-        kp, vp = _pages(k_pages, Q.dtype, "k_pages"), _pages(v_pages, Q.dtype, "v_pages")
-        if k_pages.shape[2:] != (H, 128) or v_pages.shape != k_pages.shape:
-            raise ProvipError(ERR_INVALID_ARG, f"rotate_append: pages must be [n_pages, page_size, {H}, 128]")
+        kp, vp = _pages(k_pages, dtype, "k_pages"), _pages(v_pages, dtype, "v_pages")
         n, ps = k_pages.shape[:2]
-    dev = _same_device("rotate_append", Q, K, V, pos, q_norm, k_norm, n_rows, q_out, k_out, slot_map, k_pages, v_pages)
-    rc = _on(dev, lib().provip_rotate_append, *ins, v, vs, T, *by, *outs, _ints(slot_map, T, "slot_map"), n, ps, int(four), kp,
-             vp, _stream(dev))
-    _check(rc, "provip_rotate_append")
+        if k_pages.shape[2:] != (H, 128) or v_pages.shape != k_pages.shape or k_pages.get_device() != dev or v_pages.get_device() != dev:
+            raise ProvipError(ERR_INVALID_ARG, f"rotate_append: pages must be [n_pages, page_size, {H}, 128] on GPU {dev}")
+    _call(dev, "provip_rotate_append", lib().provip_rotate_append, *ins, v, vs, T, *by, *outs, _index(slot_map, T, dev, "slot_map"), n,
+          ps, int(four), kp, vp)
     return q_out, k_out
 
 
 def provip_kv_append4(K, V, slot_map, k_pages, v_pages):
     """Rows of K and V [T, H_kv, 128] into the slots slot_map [T] of 4-bit pages (uint8, see pages4);
     negative slots are skipped."""
-    T, H = K.shape[0], K.shape[1]
-    k, ks = _rows(K, H, K.dtype, "K")
-    v, vs = _rows(V, H, K.dtype, "V")
-    if V.shape[0] != T:
-        raise ProvipError(ERR_INVALID_ARG, "kv_append4: V has another number of rows")
-    kp, vp, n, ps = _pages4(k_pages, v_pages, H)
-    dev = _same_device("kv_append4", K, V, slot_map, k_pages, v_pages)
-    rc = _on(dev, lib().provip_kv_append4, k, ks, v, vs, T, H, 128, _ints(slot_map, T, "slot_map"), n, ps, _dtype_of(K.dtype),
-             kp, vp, _stream(dev))
-    _check(rc, "provip_kv_append4")
+    (T, H, _), dtype, dev = K.shape, K.dtype, K.get_device()
+    k, ks = _heads(K, T, H, dtype, dev, "K")
+    v, vs = _heads(V, T, H, dtype, dev, "V")
+    kp, vp, n, ps = _pages4(k_pages, v_pages, H, dev)
+    _call(dev, "provip_kv_append4", lib().provip_kv_append4, k, ks, v, vs, T, H, 128, _index(slot_map, T, dev, "slot_map"), n, ps,
+          _dtype_of(dtype), kp, vp)
 
 
 def provip_kv_read4(slot_map, k_pages, v_pages, dtype=torch.bfloat16, out=None):
     """What the rows at the slots slot_map [T] of 4-bit pages stand for: K and V [T, H_kv, 128]. out: (K, V)
     to write, whose type counts then; rows of a negative slot are left untouched (zeros, unless out is given)."""
-    T, H = slot_map.numel(), k_pages.shape[1]
+    T, H, dev = slot_map.numel(), k_pages.shape[1], k_pages.get_device()
     if out is None:
         out = tuple(torch.zeros(T, H, 128, dtype=dtype, device=k_pages.device) for _ in range(2))
     k_out, v_out = out
-    if k_out.shape[0] != T or v_out.shape[0] != T:
-        raise ProvipError(ERR_INVALID_ARG, "kv_read4: an output has another number of rows")
-    k, ks = _rows(k_out, H, k_out.dtype, "K")
-    v, vs = _rows(v_out, H, k_out.dtype, "V")
-    kp, vp, n, ps = _pages4(k_pages, v_pages, H)
-    dev = _same_device("kv_read4", slot_map, k_pages, v_pages, k_out, v_out)
-    rc = _on(dev, lib().provip_kv_read4, _ints(slot_map, T, "slot_map"), T, H, 128, kp, vp, n, ps, _dtype_of(k_out.dtype), k, ks,
-             v, vs, _stream(dev))
-    _check(rc, "provip_kv_read4")
+    dtype = k_out.dtype
+    k, ks = _heads(k_out, T, H, dtype, dev, "K")
+    v, vs = _heads(v_out, T, H, dtype, dev, "V")
+    kp, vp, n, ps = _pages4(k_pages, v_pages, H, dev)
+    _call(dev, "provip_kv_read4", lib().provip_kv_read4, _index(slot_map, T, dev, "slot_map"), T, H, 128, kp, vp, n, ps,
+          _dtype_of(dtype), k, ks, v, vs)
     return k_out, v_out
 
 
@@ -921,24 +925,24 @@ class DecodeAttention4:
         self.out = torch.empty((B, H_q, 128), dtype=dtype, device=dev)
         self.lse = torch.empty((B, H_q), dtype=torch.float32, device=dev) if want_lse else None
         self.ws = workspace(lib().provip_decode_attention4_workspace_size(*self.shape, self._dt), dev)
+        self._outs = (self.out.data_ptr(), H_q * 128, None if self.lse is None else self.lse.data_ptr(), self.ws.data_ptr(),
+                      self.ws.numel())
 
     def __call__(self, Q, k_pages, v_pages, block_table, kv_len, prefix_table=None):
         """Q [B, H_q, 128]; k_pages, v_pages [n_pages, H_kv, page_size * 72] bytes; block_table
         [B, max_pages], kv_len [B] and the prefix's pages int32 on the device. Returns dict(out, lse)."""
         B, H_q, H_kv, km, P = self.shape
-        if Q.shape[0] != B or block_table.dim() != 2 or block_table.shape[0] != B:
-            raise ProvipError(ERR_INVALID_ARG, f"decode_attention4: Q and block_table must have {B} rows")
-        q, qs = _rows(Q, H_q, self.dtype, "Q")
-        kp, vp, n, ps = _pages4(k_pages, v_pages, H_kv)
+        dev = self.out.get_device()
+        q, qs = _heads(Q, B, H_q, self.dtype, dev, "Q")
+        kp, vp, n, ps = _pages4(k_pages, v_pages, H_kv, dev)
+        table = block_table.shape
+        if len(table) != 2 or table[0] != B:
+            raise ProvipError(ERR_INVALID_ARG, f"decode_attention4: block_table must have {B} rows")
         if P and prefix_table is None:
             raise ProvipError(ERR_INVALID_ARG, "decode_attention4: the prefix needs its pages' table")
-        dev = _same_device("decode_attention4", Q, k_pages, v_pages, block_table, kv_len, self.out, prefix_table if P else None)
-        rc = _on(dev, lib().provip_decode_attention4,
-                 q, qs, B, H_q, H_kv, 128, kp, vp, n, ps, _ints(block_table, 0, "block_table"), block_table.shape[1],
-                 _ints(kv_len, B, "kv_len"), km, _ints(prefix_table, -(-P // ps), "prefix_table") if P else None, P, self.scale,
-                 self._dt, self.out.data_ptr(), H_q * 128, None if self.lse is None else self.lse.data_ptr(),
-                 self.ws.data_ptr(), self.ws.numel(), _stream(dev))
-        _check(rc, "provip_decode_attention4")
+        _call(dev, "provip_decode_attention4", lib().provip_decode_attention4, q, qs, B, H_q, H_kv, 128, kp, vp, n, ps,
+              _index(block_table, 0, dev, "block_table"), table[1], _index(kv_len, B, dev, "kv_len"), km,
+              _index(prefix_table, -(-P // ps), dev, "prefix_table") if P else None, P, self.scale, self._dt, *self._outs)
         return dict(out=self.out, lse=self.lse)
 
 

@@ -122,6 +122,33 @@ def test_read_gives_what_codes_stand_for(dtype):
         assert torch.equal(out, torch.where(keep, torch.cat([k, v], 1), out.new_tensor(7.0)))
 
 
+def test_every_scale_fraction():
+    """groups whose largest value has each of the 256 fractions of a bf16, at several exponents, with values all
+    over the codes' range and next to their borders: codes as the reciprocal rounded to nearest gives them"""
+    g = gen(12)
+    frac = torch.arange(128, device=DEV).float() / 128 + 1
+    rows = []
+    for exp in (-100, -20, 0, 7, 60, 90):
+        for sign in (1.0, -1.0):
+            e = sign * frac * 2.0 ** exp
+            d = -e / 8
+            x = torch.rand(128, 32, device=DEV, generator=g) * 15.5 - 8
+            x[:, 1:16] = torch.round(x[:, 1:16]) + 0.5  # borders, and one step of fp32 off them
+            x[:, 4:8] *= 1 + 2.0 ** -23
+            x[:, 8:12] *= 1 - 2.0 ** -23
+            x = x.clamp(-7.9, 7.9) * d[:, None]
+            x[:, 0] = e
+            rows.append(x)
+    x = torch.cat(rows).view(-1, 1, 128)
+    n = x.shape[0]
+    pools = P.pages4(-(-n // 64), 64, 1, DEV), P.pages4(-(-n // 64), 64, 1, DEV)
+    P.provip_kv_append4(x, x, torch.arange(n, dtype=torch.int32, device=DEV), *pools)
+    codes, bits = ref.pack(x.cpu().numpy().reshape(-1, 128))
+    want = (codes.reshape(-1, 4, 32) - 8) * ref.bf16_value(bits).astype(np.float64)[..., None]
+    got = ref.values(pools[0], 64, torch.arange(n, device=DEV)).cpu().numpy().reshape(-1, 4, 32)
+    assert (got == want).all()
+
+
 def test_not_finite_and_huge_groups_stand_for_nan():
     x = torch.ones(4, 1, 128, device=DEV)
     x[0, 0, 40], x[1, 0, 3], x[2, 0, 100], x[3, 0, 127] = math.nan, math.inf, -math.inf, 2.0 ** 100

@@ -38,7 +38,7 @@ COMMON_BAD = [dict(Q=None), dict(K=None), dict(qo=None), dict(pos=None), dict(fr
               dict(freq=freq(63, math.inf)), dict(freq=freq(0, -1.1e6)), dict(axis=axis(3)), dict(axis=axis(-1)), dict(factor=math.nan),
               dict(factor=math.inf), dict(wq=FAKE, eps=-1.0), dict(wk=FAKE, eps=math.nan), dict(qo=FAKE, qos=1032)]
 COMMON_UNSUPPORTED = [dict(d_h=64), dict(dtype=2), dict(Q=OFF), dict(K=OFF), dict(qo=OFF), dict(ko=OFF), dict(qs=1028), dict(kos=516), dict(wq=OFF),
-                      dict(wk=OFF), dict(T=2 ** 31 - 1, ps=2 ** 31 - 1, H_q=64, qs=64 * 128, qos=64 * 128)]
+                      dict(wk=OFF), dict(T=2 ** 31 - 1, ps=2 ** 31 - 1)]
 
 
 def test_rotate_refusals(L):
@@ -127,4 +127,4 @@ def test_binding_refusals():
         with pytest.raises(P.ProvipError):
             call()  # not on the GPU
     with pytest.raises(P.ProvipError):
-        P._positions(i, 4, 1)
+        P._positions(i, 4, 1, 0)
