@@ -429,7 +429,7 @@ struct Attn4Plan {
   int n_cut;                 // virtual heads a key/value head
   int own_keys, n_own;       // keys of a part, parts at most (own; 0: none)
   int pre_keys, n_pre;       // the same for the prefix
-  int own_rows, pre_rows;    // query rows a CTA: 2, 8 or (bf16) 16
+  int own_rows, pre_rows;    // query rows a CTA: 2, 8 or (bf16) 16; the prefix's (bf16) also 64 or 128
   unsigned regs[3];          // constants of the codes' expansion (CodeRegs)
 };
 // part_* of AttnArgs: the prefix's parts, then the own ones (n_part in all); used where a row has more than one

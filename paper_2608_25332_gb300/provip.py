@@ -780,7 +780,7 @@ _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 def _heads(t, T, H, dtype, dev, what):
     """pointer and row stride (elements) of rows [T, H, 128] as _rows takes them, on device number dev"""
-    if t.dtype is not dtype or t.get_device() != dev or dev < 0 or tuple(t.shape) != (T, H, 128):
+    if t.dtype is not dtype or t.get_device() != dev or dev < 0 or t.shape != (T, H, 128):
         raise ProvipError(ERR_INVALID_ARG, f"{what} must be {dtype} [{T}, {H}, 128] on GPU {dev}: got {t.dtype} {list(t.shape)} on {t.device}")
     s0, s1, s2 = t.stride()
     if (s2 != 1 or (s1 != 128 and H > 1)) and T:

@@ -258,6 +258,73 @@ def test_long_rows(dtype):
     check(c, decode(c))
 
 
+@pytest.mark.parametrize("lens,H_q,H_kv,page,prefix", [
+    ([3, 0, 9], 28, 4, 16, 100), ([1] * 20, 28, 4, 64, 1000), ([2, 40] * 19, 8, 2, 8, 333), ([7] * 70, 4, 4, 32, 65), ([1] * 64, 28, 4, 64, 9251),
+    ([0] * 33, 2, 1, 256, 1), ([5] * 9, 64, 2, 128, 700), ([4] * 300, 1, 1, 16, 2000)])
+def test_a_prefix_for_many_rows(lens, H_q, H_kv, page, prefix):
+    """blocks of 32, 64 and 128 rows"""
+    c = case(len(lens) + page, lens, H_q, H_kv, page, prefix, torch.bfloat16)
+    check(c, decode(c), rows=range(0, len(lens), max(len(lens) // 5, 1)))
+
+
+@pytest.mark.parametrize("spread", [2.0 ** -110, 2.0 ** -40, 2.0 ** 12, 2.0 ** 90])
+def test_a_prefix_of_any_size(spread):
+    c = case(21, [5] * 12, 28, 4, 16, 300, torch.bfloat16, spread)
+    scale = 1.0 / (spread * 11.3)
+    check(c, decode(c, scale=scale), scale, rows=(0, 7))
+
+
+def test_a_prefix_whose_values_grow():
+    """keys' scales and values' scales over 2^24 along the list, and groups of a row 2^20 apart: each weight keeps
+    its bits next to the largest"""
+    c = case(22, [5] * 12, 28, 4, 16, 640, torch.bfloat16)
+    j = torch.arange(640, device=DEV)
+    slots = c["prefix_table"].long()[j // 16] * 16 + j % 16
+    s = c["v"][..., 16 * 64:].view(torch.bfloat16).view(-1, 4, 16, 4)
+    grow = torch.exp2((j % 320).float() / 320 * 24 - 12)
+    s[slots // 16, :, slots % 16] = (s[slots // 16, :, slots % 16].float() * grow[:, None, None]).to(torch.bfloat16)
+    s[..., 2] *= 2.0 ** -20
+    s = c["k"][..., 16 * 64:].view(torch.bfloat16).view(-1, 4, 16, 4)
+    s[slots // 16, :, slots % 16] = (s[slots // 16, :, slots % 16].float() * (0.05 + j.float()[:, None, None] / 300)).to(torch.bfloat16)
+    check(c, decode(c), rows=(0, 11))
+
+
+def test_a_prefix_with_keys_far_apart():
+    """a few keys' values, and a few groups of keys, 2^12 to 2^150 from the others, at the front and later"""
+    c = case(25, [5] * 12, 28, 4, 16, 640, torch.bfloat16)
+    s = c["v"][..., 16 * 64:].view(torch.bfloat16).view(-1, 4, 16, 4)
+    for at, f in ((0, 2.0 ** -70), (1, 2.0 ** -12), (100, 2.0 ** 12), (333, 2.0 ** 80), (500, 2.0 ** -60)):
+        s[c["prefix_table"][at // 16].long(), at % 4, at % 16] *= f
+    s[c["prefix_table"][5:9].long(), 3] *= 2.0 ** 15
+    s = c["k"][..., 16 * 64:].view(torch.bfloat16).view(-1, 4, 16, 4)
+    s[c["prefix_table"][3].long(), 1, 7, 2] *= 2.0 ** -14
+    s[c["prefix_table"][11:13].long(), :, :, 1] *= 2.0 ** -30
+    check(c, decode(c), rows=(0, 5, 11))
+
+
+def test_a_prefix_that_is_not_finite_shows_where_it_should():
+    c = case(23, [5] * 12, 28, 4, 16, 100, torch.bfloat16)
+    page = int(c["prefix_table"][3])
+    c["v"][..., 16 * 64:].view(torch.bfloat16).view(-1, 4, 16, 4)[page, 2, 5, 1] = math.nan
+    bad = ~torch.isfinite(decode(c)["out"]).view(12, 4, 7, 4, 32).all(-1)
+    want = torch.zeros(12, 4, 7, 4, dtype=torch.bool, device=DEV)
+    want[:, 2, :, 1] = True
+    assert torch.equal(bad, want)
+    c["k"][..., 16 * 64:].view(torch.bfloat16).view(-1, 4, 16, 4)[page, 0, 5, 1] = math.nan
+    r = decode(c)
+    want[:, 0] = True
+    assert torch.equal(~torch.isfinite(r["out"]).view(12, 4, 7, 4, 32).all(-1), want)
+    assert torch.isnan(r["lse"].view(12, 4, 7)[:, 0]).all() and torch.isfinite(r["lse"].view(12, 4, 7)[:, 1:]).all()
+
+
+def test_a_bad_prefix_page_is_reported():
+    c = case(24, [5] * 12, 28, 4, 16, 100, torch.bfloat16)
+    for bad in (-1, c["k"].shape[0]):
+        c["prefix_table"][2] = bad
+        decode(c)
+        assert P.provip_device_status(clear=True)[1] == P.DEVSTAT_BAD_ARG
+
+
 def test_many_requests():
     lens = [(i * 37) % 300 for i in range(300)]
     c = case(3, lens, 8, 2, 16, 0, torch.bfloat16)
