@@ -610,19 +610,23 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
 // with k_t relative to the largest scale of its row, and the values of group q to u_q, the largest scale in the
 // group among the first 64 keys. Five bits of exponent hold that while a row's scales lie within 2^10 of each
 // other, and a group's, over 16 keys, within 2^9 and at 2^u_q to a factor of 2^4. Sixteen keys that do not fit are
-// done as above, codes and scales apart. Eight warps, 64 keys at a time: four warps expand 16 keys of K each,
-// four of V, into one of two buffers, then all take the 64 keys before from the other against their 8 NT columns.
+// done as above, codes and scales apart. 64 keys at a time, four warps expand 16 of them each into one of two
+// buffers, while eight others take the 64 before from the other against their 8 NT columns.
 // Bound by the MMAs (half of one an SM and clock) and by their operands' way out of shared memory (128 bytes
 // a clock), which take equally long.
 // ---------------------------------------------------------------------------
-constexpr int kWideWarps = 8, kWideThr = kWideWarps * 32;
+constexpr int kWideWarps = 8, kExpand = 4, kWideThr = (kWideWarps + kExpand) * 32;
 constexpr int kFragBytes = kTiles * 8 * 32 * 16;  // operands of 64 keys, K's or V's
 constexpr int kWideStages = 3;
 constexpr size_t kWideSmem = 4 * (size_t)kFragBytes + (size_t)kWideStages * kStageBytes;
+constexpr int kAtOnce = 2;  // tiles of 16 keys a warp has scores of
 constexpr int kLift = 4;  // weights are 2^4 higher than they are, so that small ones keep their bits
 constexpr int kRowSpread = 10, kTileSpread = 9, kUnitSpread = 4, kUnitMost = 40;
 
-__device__ __forceinline__ void value_warps_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+// named barriers: 1 among the expanding warps; 2, 3 a buffer is whole, 4, 5 it may be overwritten
+__device__ __forceinline__ void expand_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kExpand * 32) : "memory"); }
+__device__ __forceinline__ void wide_sync(int id) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(kWideThr) : "memory"); }
+__device__ __forceinline__ void wide_arrive(int id) { asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "n"(kWideThr) : "memory"); }
 __device__ __forceinline__ float pow2(int biased) { return __uint_as_float((uint32_t)biased << 23); }
 // biased exponent of scale q of a row (0 for a scale of zero; infinite and NaN ones, which show in any case, too)
 __device__ __forceinline__ int exponent_of(uint2 d, int q) {
@@ -663,44 +667,171 @@ __global__ void __launch_bounds__(kWideThr, 1)
   const int n_steps = (k_hi - k_lo + kStep - 1) / kStep;
   uint8_t* ring = smem + 4 * kFragBytes;
 
-  // loads, by warp 0: a lane per copy of a stage
-  const int box = min(a.page_size, kStep), kind = lane & 3, box_row = (lane >> 2) * box;
-  auto page_of = [&](int step) {
-    const int k = k_lo + step * kStep + box_row;
-    return box_row < kStep && step < n_steps && k < k_hi ? __ldg(a.prefix_table + (k >> a.page_shift)) : 0;
-  };
-  int page = warp == 0 ? page_of(0) : 0;
-  const uint32_t unit_bytes = kind < 2 ? kCodes4 : 8;
-  const uint32_t dst = smem_u32(ring) + box_row * unit_bytes + (kind < 2 ? kind * kCodeBytes : 2 * kCodeBytes + (kind - 2) * kScaleBytes);
-  const uint8_t* src = static_cast<const uint8_t*>(kind & 1 ? a.V : a.K) + (((size_t)kv_head * kRow4 + (kind < 2 ? 0 : kCodes4)) << a.page_shift);
-  const uint32_t page_bytes = (uint32_t)(a.H_kv * kRow4) << a.page_shift;
-  int issued = 0;  // (steps in order: stage issued % kWideStages)
-  auto load = [&]() {
-    const int k = k_lo + issued * kStep, rows = min(kStep, k_hi - k), stage = issued % kWideStages;
-    int p = page;
-    page = page_of(issued + 1);
-    if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4 * 2));
-    __syncwarp();
-    if (box_row < rows) {
-      if ((unsigned)p >= (unsigned)a.n_pages) {
-        set_error(a.err, kErrBadDeviceArg);
-        p = 0;
-      }
-      bulk_load(dst + stage * kStageBytes, src + (size_t)p * page_bytes + ((k + box_row) & (a.page_size - 1)) * unit_bytes,
-                box * unit_bytes, smem_u32(&full[stage]));
-    }
-    __syncwarp();
-    ++issued;
-  };
   if (threadIdx.x == 0) {
     for (int s = 0; s < kWideStages; ++s) mbar_init(&full[s], 1);
     fence_mbar_init();
   }
-  if (warp == 0) {
-    __syncwarp();
-    while (issued < kWideStages && issued < n_steps) load();
-  }
   __syncthreads();
+  const CodeRegs regs = {plan.regs[0], plan.regs[1], plan.regs[2]};
+
+  if (warp >= kWideWarps) {
+    // ---- expanding warps: 16 keys each as operands. Rows past the end are zeros, whatever lies there ----
+    const int w = warp - kWideWarps;
+    const bool first = w == 0;
+    // loads, by the first of them: a lane per copy of a stage
+    const int box = min(a.page_size, kStep), kind = lane & 3, box_row = (lane >> 2) * box;
+    auto page_of = [&](int step) {
+      const int k = k_lo + step * kStep + box_row;
+      return box_row < kStep && step < n_steps && k < k_hi ? __ldg(a.prefix_table + (k >> a.page_shift)) : 0;
+    };
+    int page = first ? page_of(0) : 0;
+    const uint32_t unit_bytes = kind < 2 ? kCodes4 : 8;
+    const uint32_t dst = smem_u32(ring) + box_row * unit_bytes + (kind < 2 ? kind * kCodeBytes : 2 * kCodeBytes + (kind - 2) * kScaleBytes);
+    const uint8_t* src = static_cast<const uint8_t*>(kind & 1 ? a.V : a.K) + (((size_t)kv_head * kRow4 + (kind < 2 ? 0 : kCodes4)) << a.page_shift);
+    const uint32_t page_bytes = (uint32_t)(a.H_kv * kRow4) << a.page_shift;
+    int issued = 0;  // (steps in order: stage issued % kWideStages)
+    auto load = [&]() {
+      const int k = k_lo + issued * kStep, rows = min(kStep, k_hi - k), stage = issued % kWideStages;
+      int p = page;
+      page = page_of(issued + 1);
+      if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4 * 2));
+      __syncwarp();
+      if (box_row < rows) {
+        if ((unsigned)p >= (unsigned)a.n_pages) {
+          set_error(a.err, kErrBadDeviceArg);
+          p = 0;
+        }
+        bulk_load(dst + stage * kStageBytes, src + (size_t)p * page_bytes + ((k + box_row) & (a.page_size - 1)) * unit_bytes,
+                  box * unit_bytes, smem_u32(&full[stage]));
+      }
+      __syncwarp();
+      ++issued;
+    };
+    if (first)
+      while (issued < kWideStages && issued < n_steps) load();
+    int made[4] = {0, 0, 0, 0};  // exponents that the values are relative to
+    bool failed = false;
+    for (int step = 0; step < n_steps; ++step) {
+      const int stage = step % kWideStages, buf = step & 1, left = k_hi - k_lo - step * kStep;
+      // (a wait that gives up: no more waits, but every barrier is met)
+      if (!failed && __any_sync(0xffffffffu, !mbar_wait(&full[stage], (uint32_t)(step / kWideStages) & 1u, a.err))) failed = true;
+      if (step >= 2) wide_sync(4 + buf);
+      const uint8_t* st = ring + stage * kStageBytes;
+      uint4* to = reinterpret_cast<uint4*>(smem + buf * 2 * kFragBytes) + w * 8 * 32 + lane;
+      {
+        const uint8_t *kc = st, *ks = st + 2 * kCodeBytes;
+        const int r0 = w * 16 + g, r1 = r0 + 8;
+        uint2 da = *reinterpret_cast<const uint2*>(ks + r0 * 8), db = *reinterpret_cast<const uint2*>(ks + r1 * 8);
+        if (r0 >= left) da = make_uint2(0u, 0u);
+        if (r1 >= left) db = make_uint2(0u, 0u);
+        int ea = 1, eb = 1, la = 255, lb = 255;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int x = exponent_of(da, q), y = exponent_of(db, q);
+          ea = max(ea, x);
+          eb = max(eb, y);
+          la = min(la, x == 0 ? 255 : x);
+          lb = min(lb, y == 0 ? 255 : y);
+        }
+        const bool apart = __any_sync(0xffffffffu, ea - la > kRowSpread || eb - lb > kRowSpread);
+        if (lane == 0) s_apart[buf][0][w] = apart;
+        if (j == 0) {
+          s_ek[buf][r0] = ea;
+          s_ek[buf][r1] = eb;
+          s_d[buf][0][r0] = da;
+          s_d[buf][0][r1] = db;
+        }
+        const float fa = pow2(254 - ea), fb = pow2(254 - eb);  // 2^-(e - 127)
+        const uint4 wa = *reinterpret_cast<const uint4*>(kc + r0 * kCodes4 + 16 * j);
+        const uint4 wb = *reinterpret_cast<const uint4*>(kc + r1 * kCodes4 + 16 * j);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
+          uint32_t ca[4], cb[4];
+          codes_f16(q < 2 ? __byte_perm(wa.x, wa.z, sel) : __byte_perm(wa.y, wa.w, sel), regs, ca);
+          codes_f16(q < 2 ? __byte_perm(wb.x, wb.z, sel) : __byte_perm(wb.y, wb.w, sel), regs, cb);
+          const __half2 ha = __float2half2_rn(apart ? 1.f : scale_f(da, q) * fa), hb = __float2half2_rn(apart ? 1.f : scale_f(db, q) * fb);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            to[(2 * q + i) * 32] = make_uint4(times(ca[2 * i], ha), times(cb[2 * i], hb), times(ca[2 * i + 1], ha), times(cb[2 * i + 1], hb));
+        }
+      }
+      {
+        // keys 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of the sixteen, dims 4 g .. + 3 of each group
+        const uint8_t *vc = st + kCodeBytes, *vs = st + 2 * kCodeBytes + kScaleBytes;
+        to += kFragBytes / 16;
+        uint2 v[4], d[4];
+        int hi[4] = {0, 0, 0, 0}, lo[4] = {255, 255, 255, 255};  // a group's largest and smallest exponent
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = w * 16 + 2 * j + (i >> 1) * 8 + (i & 1);
+          v[i] = *reinterpret_cast<const uint2*>(vc + r * kCodes4 + 8 * g);
+          d[i] = *reinterpret_cast<const uint2*>(vs + r * 8);
+          if (r >= left) d[i] = make_uint2(0u, 0u);
+          if (g == 0) s_d[buf][1][r] = d[i];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int e = exponent_of(d[i], q);
+            hi[q] = max(hi[q], e);
+            lo[q] = min(lo[q], e == 0 ? 255 : e);
+          }
+        }
+        // (the eight lanes with another j have other keys, those with another g the same)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int b = 1; b < 4; b <<= 1) {
+            hi[q] = max(hi[q], __shfl_xor_sync(0xffffffffu, hi[q], b));
+            lo[q] = min(lo[q], __shfl_xor_sync(0xffffffffu, lo[q], b));
+          }
+        if (lane == 0) *reinterpret_cast<int4*>(s_top[buf][w]) = make_int4(hi[0], hi[1], hi[2], hi[3]);
+        expand_sync();
+        // (the stage before is read by all of them)
+        if (first && issued < n_steps && step > 0) load();
+        bool apart = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int top = max(max(max(s_top[buf][0][q], s_top[buf][1][q]), max(s_top[buf][2][q], s_top[buf][3][q])), 1);
+          if (step == 0 || top > made[q] + kUnitMost) made[q] = top;  // (or far larger than what was before)
+          apart = apart || hi[q] - lo[q] > kTileSpread || (hi[q] > 0 && abs(hi[q] - made[q]) > kUnitSpread);
+        }
+        if (lane == 0) {
+          s_apart[buf][1][w] = apart;
+          if (w == 0) *reinterpret_cast<int4*>(s_unit[buf]) = make_int4(made[0], made[1], made[2], made[3]);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
+          const uint32_t ya = q < 2 ? __byte_perm(v[0].x, v[1].x, sel) : __byte_perm(v[0].y, v[1].y, sel);
+          const uint32_t yb = q < 2 ? __byte_perm(v[2].x, v[3].x, sel) : __byte_perm(v[2].y, v[3].y, sel);
+          uint32_t ca[4], cb[4];
+          if (apart) {
+            codes_bf16(ya, regs, ca);
+            codes_bf16(yb, regs, cb);
+          } else {
+            codes_f16(ya, regs, ca);
+            codes_f16(yb, regs, cb);
+            const float f = pow2(254 - made[q]);
+            const __half2 ha = __floats2half2_rn(scale_f(d[0], q) * f, scale_f(d[1], q) * f);
+            const __half2 hb = __floats2half2_rn(scale_f(d[2], q) * f, scale_f(d[3], q) * f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              ca[i] = times(ca[i], ha);
+              cb[i] = times(cb[i], hb);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) to[(2 * q + i) * 32] = make_uint4(ca[2 * i], ca[2 * i + 1], cb[2 * i], cb[2 * i + 1]);
+        }
+      }
+      wide_arrive(2 + buf);
+    }
+    if (failed && first) {
+      // copies that may still be in flight into the block's shared memory: waited for once more, with a limit
+      for (int i = max(issued - kWideStages, 0); i < issued; ++i) mbar_wait(&full[i % kWideStages], (uint32_t)(i / kWideStages) & 1u, a.err);
+    }
+    return;
+  }
 
   // queries, as in the kernel above: a warp its own columns
   uint32_t qf[NT][4][4];
@@ -734,7 +865,6 @@ __global__ void __launch_bounds__(kWideThr, 1)
       }
   }
 
-  const CodeRegs regs = {plan.regs[0], plan.regs[1], plan.regs[2]};
   float o[8][NT][4], m[NT][2], base[NT][2], l[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -749,122 +879,6 @@ __global__ void __launch_bounds__(kWideThr, 1)
       for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
   }
   int unit[4] = {0, 0, 0, 0};  // of o's sums; warps 4-7: of the values expanded last
-  int made[4] = {0, 0, 0, 0};
-  bool failed = false;
-
-  // ---- 16 keys a warp as operands. Rows past the end are zeros, whatever lies there ----
-  auto expand = [&](int step) {
-    const int stage = step % kWideStages, buf = step & 1, left = k_hi - k_lo - step * kStep;
-    // (a wait that gives up: no more waits, but every barrier is met)
-    if (!failed && __any_sync(0xffffffffu, !mbar_wait(&full[stage], (uint32_t)(step / kWideStages) & 1u, a.err))) failed = true;
-    const uint8_t* st = ring + stage * kStageBytes;
-    uint4* to = reinterpret_cast<uint4*>(smem + buf * 2 * kFragBytes) + (warp & 3) * 8 * 32 + lane;
-    if (warp < 4) {
-      const uint8_t *kc = st, *ks = st + 2 * kCodeBytes;
-      const int r0 = warp * 16 + g, r1 = r0 + 8;
-      uint2 da = *reinterpret_cast<const uint2*>(ks + r0 * 8), db = *reinterpret_cast<const uint2*>(ks + r1 * 8);
-      if (r0 >= left) da = make_uint2(0u, 0u);
-      if (r1 >= left) db = make_uint2(0u, 0u);
-      int ea = 1, eb = 1, la = 255, lb = 255;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int x = exponent_of(da, q), y = exponent_of(db, q);
-        ea = max(ea, x);
-        eb = max(eb, y);
-        la = min(la, x == 0 ? 255 : x);
-        lb = min(lb, y == 0 ? 255 : y);
-      }
-      const bool apart = __any_sync(0xffffffffu, ea - la > kRowSpread || eb - lb > kRowSpread);
-      if (lane == 0) s_apart[buf][0][warp] = apart;
-      if (j == 0) {
-        s_ek[buf][r0] = ea;
-        s_ek[buf][r1] = eb;
-        s_d[buf][0][r0] = da;
-        s_d[buf][0][r1] = db;
-      }
-      const float fa = pow2(254 - ea), fb = pow2(254 - eb);  // 2^-(e - 127)
-      const uint4 wa = *reinterpret_cast<const uint4*>(kc + r0 * kCodes4 + 16 * j);
-      const uint4 wb = *reinterpret_cast<const uint4*>(kc + r1 * kCodes4 + 16 * j);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
-        uint32_t ca[4], cb[4];
-        codes_f16(q < 2 ? __byte_perm(wa.x, wa.z, sel) : __byte_perm(wa.y, wa.w, sel), regs, ca);
-        codes_f16(q < 2 ? __byte_perm(wb.x, wb.z, sel) : __byte_perm(wb.y, wb.w, sel), regs, cb);
-        const __half2 ha = __float2half2_rn(apart ? 1.f : scale_f(da, q) * fa), hb = __float2half2_rn(apart ? 1.f : scale_f(db, q) * fb);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          to[(2 * q + i) * 32] = make_uint4(times(ca[2 * i], ha), times(cb[2 * i], hb), times(ca[2 * i + 1], ha), times(cb[2 * i + 1], hb));
-      }
-    } else {
-      // keys 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of the sixteen, dims 4 g .. + 3 of each group
-      const uint8_t *vc = st + kCodeBytes, *vs = st + 2 * kCodeBytes + kScaleBytes;
-      const int w = warp - 4;
-      to += kFragBytes / 16;
-      uint2 v[4], d[4];
-      int hi[4] = {0, 0, 0, 0}, lo[4] = {255, 255, 255, 255};  // a group's largest and smallest exponent
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = w * 16 + 2 * j + (i >> 1) * 8 + (i & 1);
-        v[i] = *reinterpret_cast<const uint2*>(vc + r * kCodes4 + 8 * g);
-        d[i] = *reinterpret_cast<const uint2*>(vs + r * 8);
-        if (r >= left) d[i] = make_uint2(0u, 0u);
-        if (g == 0) s_d[buf][1][r] = d[i];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int e = exponent_of(d[i], q);
-          hi[q] = max(hi[q], e);
-          lo[q] = min(lo[q], e == 0 ? 255 : e);
-        }
-      }
-      // (the eight lanes with another j have other keys, those with another g the same)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int b = 1; b < 4; b <<= 1) {
-          hi[q] = max(hi[q], __shfl_xor_sync(0xffffffffu, hi[q], b));
-          lo[q] = min(lo[q], __shfl_xor_sync(0xffffffffu, lo[q], b));
-        }
-      if (lane == 0) *reinterpret_cast<int4*>(s_top[buf][w]) = make_int4(hi[0], hi[1], hi[2], hi[3]);
-      value_warps_sync();
-      bool apart = false;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int top = max(max(max(s_top[buf][0][q], s_top[buf][1][q]), max(s_top[buf][2][q], s_top[buf][3][q])), 1);
-        if (step == 0 || top > made[q] + kUnitMost) made[q] = top;  // (or far larger than what was before)
-        apart = apart || hi[q] - lo[q] > kTileSpread || (hi[q] > 0 && abs(hi[q] - made[q]) > kUnitSpread);
-      }
-      if (lane == 0) {
-        s_apart[buf][1][w] = apart;
-        if (w == 0) *reinterpret_cast<int4*>(s_unit[buf]) = make_int4(made[0], made[1], made[2], made[3]);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
-        const uint32_t ya = q < 2 ? __byte_perm(v[0].x, v[1].x, sel) : __byte_perm(v[0].y, v[1].y, sel);
-        const uint32_t yb = q < 2 ? __byte_perm(v[2].x, v[3].x, sel) : __byte_perm(v[2].y, v[3].y, sel);
-        uint32_t ca[4], cb[4];
-        if (apart) {
-          codes_bf16(ya, regs, ca);
-          codes_bf16(yb, regs, cb);
-        } else {
-          codes_f16(ya, regs, ca);
-          codes_f16(yb, regs, cb);
-          const float f = pow2(254 - made[q]);
-          const __half2 ha = __floats2half2_rn(scale_f(d[0], q) * f, scale_f(d[1], q) * f);
-          const __half2 hb = __floats2half2_rn(scale_f(d[2], q) * f, scale_f(d[3], q) * f);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            ca[i] = times(ca[i], ha);
-            cb[i] = times(cb[i], hb);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) to[(2 * q + i) * 32] = make_uint4(ca[2 * i], ca[2 * i + 1], cb[2 * i], cb[2 * i + 1]);
-      }
-    }
-  };
-
   // a new maximum, where a score passes the one before by 2^10
   auto raise_to = [&](const float (*top)[2]) {
 #pragma unroll
@@ -1007,45 +1021,35 @@ __global__ void __launch_bounds__(kWideThr, 1)
     }
   };
 
-  expand(0);
-  __syncthreads();
   for (int step = 0; step < n_steps; ++step) {
     const int buf = step & 1, left = k_hi - k_lo - step * kStep;
-    // (an SM quarter's two warps, one of each kind, expand at different times: one's MMAs fill the other's)
-    if (warp < 4 && step + 1 < n_steps) expand(step + 1);
-    if (!failed) {
+    wide_sync(2 + buf);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int u = s_unit[buf][q];
-        if (u != unit[q]) {  // larger values: what there is, relative to them
-          const float f = pow2(max(127 + unit[q] - u, 0));
+    for (int q = 0; q < 4; ++q) {
+      const int u = s_unit[buf][q];
+      if (u != unit[q]) {  // larger values: what there is, relative to them
+        const float f = pow2(max(127 + unit[q] - u, 0));
 #pragma unroll
-          for (int i = 2 * q; i < 2 * q + 2; ++i)
+        for (int i = 2 * q; i < 2 * q + 2; ++i)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[i][nt][e] *= f;
-          unit[q] = u;
-        }
-      }
-      int any = 0;
-#pragma unroll
-      for (int mt = 0; mt < kTiles; ++mt) any |= s_apart[buf][0][mt] | s_apart[buf][1][mt];
-      if (!any) {
-        attend(Tiles<kTiles>(), buf, 0, left, false, false);
-      } else {
-#pragma unroll 1
-        for (int mt = 0; mt < kTiles && mt * 16 < left; ++mt)
-          attend(Tiles<1>(), buf, mt, left, s_apart[buf][0][mt] != 0, s_apart[buf][1][mt] != 0);
+            for (int e = 0; e < 4; ++e) o[i][nt][e] *= f;
+        unit[q] = u;
       }
     }
-    if (warp >= 4 && step + 1 < n_steps) expand(step + 1);
-    __syncthreads();  // the next operands are whole, and these may be overwritten; the next stage is read
-    if (warp == 0 && !failed && issued < n_steps && issued < step + 2 + kWideStages) load();
-  }
-  if (failed && warp == 0) {
-    // copies that may still be in flight into the block's shared memory: waited for once more, with a limit
-    for (int i = max(issued - kWideStages, 0); i < issued; ++i) mbar_wait(&full[i % kWideStages], (uint32_t)(i / kWideStages) & 1u, a.err);
+    int any = 0;
+#pragma unroll
+    for (int mt = 0; mt < kTiles; ++mt) any |= s_apart[buf][0][mt] | s_apart[buf][1][mt];
+    if (!any) {
+#pragma unroll 1
+      for (int mt = 0; mt < kTiles && mt * 16 < left; mt += kAtOnce) attend(Tiles<kAtOnce>(), buf, mt, left, false, false);
+    } else {
+#pragma unroll 1
+      for (int mt = 0; mt < kTiles && mt * 16 < left; ++mt)
+        attend(Tiles<1>(), buf, mt, left, s_apart[buf][0][mt] != 0, s_apart[buf][1][mt] != 0);
+    }
+    if (step + 2 < n_steps) wide_arrive(4 + buf);  // these operands may be overwritten
   }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
