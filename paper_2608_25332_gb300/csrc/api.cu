@@ -1819,15 +1819,15 @@ extern "C" int provip_kv_read4(const int* slot_map, int T, int H_kv, int d_h, co
 
 namespace {
 
-// Parts of whole 64 keys (a warp's stage), as many as make `want` CTAs of `units`, at most `most` and, as a
-// CTA's four warps take 256 keys at a time, at most one for 256 keys.
-void attn4_parts(long long units, int n_keys, long long want, int most, int* part_keys, int* n_part) {
+// Parts of whole `tile` keys, as many as make `want` CTAs of `units`, at most `most` and at most one for `least`
+// keys.
+void attn4_parts(long long units, int n_keys, long long want, int most, int tile, int least, int* part_keys, int* n_part) {
   long long n = (want + units - 1) / units;
   if (n > most) n = most;
-  if (n > ((long long)n_keys + 255) / 256) n = ((long long)n_keys + 255) / 256;
+  if (n > ((long long)n_keys + least - 1) / least) n = ((long long)n_keys + least - 1) / least;
   if (n < 1) n = 1;
-  const long long keys = (((long long)n_keys + n - 1) / n + 63) / 64 * 64;
-  *part_keys = (int)(keys < 64 ? 64 : keys);
+  const long long keys = (((long long)n_keys + n - 1) / n + tile - 1) / tile * tile;
+  *part_keys = (int)(keys < tile ? tile : keys);
   *n_part = (int)(((long long)n_keys + *part_keys - 1) / *part_keys);
 }
 
@@ -1840,16 +1840,20 @@ Attn4Plan attn4_plan(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, i
   p.n_cut = 1;
   while (R % p.n_cut || R / p.n_cut > wide) ++p.n_cut;
   p.own_rows = R / p.n_cut > 8 ? 16 : R / p.n_cut > 2 ? 8 : 2;
-  attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, 8 * kPlanSms, 512, &p.own_keys, &p.n_own);
+  // (64 keys are a warp's stage, 256 what a CTA's four warps take at a time)
+  attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, 8 * kPlanSms, 512, 64, 256, &p.own_keys, &p.n_own);
   if (p.n_own < 1) p.n_own = 1;  // rows without keys are written too
   const long long rows = (long long)B * R;
   p.pre_rows = rows > 8 ? wide : rows > 2 ? 8 : 2;
-  // many rows of bf16 queries: blocks of 64 or 128, a CTA an SM
-  const bool blocks = dtype == PROVIP_BF16 && rows > 16;
-  if (blocks) p.pre_rows = rows > 64 ? 128 : 64;
+  // many rows of bf16 queries: blocks of two tiles of 128, a CTA an SM
+  const bool tc = dtype == PROVIP_BF16 && rows > 16;
+  if (tc) p.pre_rows = 256;
   if (prefix_len > 0) {
     const long long units = (rows + p.pre_rows - 1) / p.pre_rows * H_kv;
-    attn4_parts(units, prefix_len, blocks ? kPlanSms / units * units : 8 * kPlanSms, 256, &p.pre_keys, &p.n_pre);
+    if (tc)
+      attn4_parts(units, prefix_len, kPlanSms / units * units, 256, 128, 128, &p.pre_keys, &p.n_pre);
+    else
+      attn4_parts(units, prefix_len, 8 * kPlanSms, 256, 64, 256, &p.pre_keys, &p.n_pre);
   }
   return p;
 }

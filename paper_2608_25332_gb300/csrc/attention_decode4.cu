@@ -1145,7 +1145,8 @@ template <typename T>
 cudaError_t run(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (plan.n_pre > 0)
-    e = plan.pre_rows == 128 ? go_wide<2>(a, plan, s)
+    e = plan.pre_rows == 256 ? attn4_prefix_tc_launch(a, plan, s)
+        : plan.pre_rows == 128 ? go_wide<2>(a, plan, s)
         : plan.pre_rows == 64 ? go_wide<1>(a, plan, s) : go_by_columns<T, true>(plan.pre_rows, a, plan, s);
   if (e == cudaSuccess) e = go_by_columns<T, false>(plan.own_rows, a, plan, s);
   if (e != cudaSuccess || plan.n_pre + plan.n_own <= 1) return e;

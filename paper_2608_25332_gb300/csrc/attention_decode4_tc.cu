@@ -1,0 +1,384 @@
+// The shared prefix of a batch in pages of 4 bits, on the tensor cores (bf16 queries).
+//
+// Every request's query rows see the same keys, so there are rows enough for tcgen05.mma: a CTA takes two
+// tiles of 128 packed (request, head of the group) rows of one key/value head against a part of the prefix,
+// 128 keys at a time. A value d c (eight significant bits times four) has eleven: it is the sum of two bf16
+// values, hi = d c rounded and lo = d c - hi, each exact from one packed multiply and one multiply-add, whatever
+// the scales' range. So codes and scales become two bf16 operands of K and of V in shared memory, once for all
+// rows, and
+//   S = Q K_hi^T + Q K_lo^T    16 MMAs (M = N = 128, K = 16), S in tensor memory
+//   P = 2^(s - m)              a thread per row, to bf16 over S's own columns
+//   O += P V_hi + P V_lo       16 MMAs, P from tensor memory
+// lose nothing but P's rounding. The eight elements of a 16-byte chunk lie in the order 0 4 1 5 2 6 3 7, as the
+// codes give them: queries are staged in that order too, and the output's columns are read in it.
+// The maximum is raised only where a tile's sum passes 2^10, as for bf16 keys (attention_tc.cu).
+//
+// Roles (512 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
+// codes, a key's row a thread, K for the next tile while the softmax works, V when the product before has read
+// the buffer; one of them loads, by bulk copies. Two row tiles share every operand and keep the tensor
+// cores busy for one while the other's softmax runs. Every wait is bounded; one that gives up sets the error word
+// and ends its role, the other roles' waits then run out likewise, and the block ends when what it has issued is
+// done.
+#include "attention_tc.cuh"
+
+namespace provip {
+namespace {
+
+constexpr int kSoftWarps = 8, kMmaWarp = 8, kExpandWarp = 12;
+constexpr int kThr = 512;
+// registers a thread: what the softmax takes more than the launch's 128, the others leave (the sums are equal)
+constexpr int kSoftRegs = 176, kMmaRegs = 40, kExpandRegs = 120;
+static_assert(kSoftRegs * 256 + kMmaRegs * 128 + kExpandRegs * 128 == 128 * kThr, "register split");
+constexpr int kRawBytes = kT * (kCodes4 + 8);  // K's or V's codes and scales of a tile
+constexpr size_t kSmem = 6 * (size_t)kStage + 2 * kRawBytes + 1024;
+constexpr uint32_t kIdescS = idesc_bf16_f32(kT, kT);
+constexpr uint32_t kIdescO = idesc_bf16_f32(kT, kT) | (1u << 16);  // B's rows run along N
+constexpr float kMostSum = 1024.f;
+
+struct Ctl {
+  uint64_t raw_full[2];            // codes and scales: K, V
+  uint64_t full[2], empty[2];      // operands: K, V
+  uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t mma_done;               // (drain)
+  uint32_t tmem;
+  volatile int fail;
+};
+
+__device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, unsigned* err) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
+}
+__device__ __forceinline__ void expand_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ __nv_bfloat162 as_bf16(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+__device__ __forceinline__ void scale_o(uint32_t to, float f) {
+  for (int z = 0; z < kHeadDim / 32; ++z) {
+    uint32_t w[32];
+    tmem_ld32(to + z * 32, reinterpret_cast<float*>(w));
+    tc_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+    tmem_st32(to + z * 32, w);
+  }
+}
+
+// This thread's key: its 16 pieces of eight values, hi and lo, into the two operand tiles.
+__device__ __forceinline__ void expand_row(const uint8_t* raw, int r, bool on, uint32_t magic, uint8_t* to) {
+  uint2 d = *reinterpret_cast<const uint2*>(raw + kT * kCodes4 + r * 8);
+  if (!on) d = make_uint2(0u, 0u);  // past the end: zeros, whatever lies there
+  const __nv_bfloat162 scale[4] = {as_bf16(__byte_perm(d.x, d.x, 0x1010)), as_bf16(__byte_perm(d.x, d.x, 0x3232)),
+                                   as_bf16(__byte_perm(d.y, d.y, 0x1010)), as_bf16(__byte_perm(d.y, d.y, 0x3232))};
+  const __nv_bfloat162 bias = __bfloat162bfloat162(__float2bfloat16_rn(136.f));
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const uint4 w = *reinterpret_cast<const uint4*>(raw + r * kCodes4 + 16 * p);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t x = __byte_perm(q < 2 ? w.x : w.y, q < 2 ? w.z : w.w, q & 1 ? 0x7632 : 0x5410);
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t v;  // 128 + n
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(x >> (4 * t)), "n"(0x000f000fu), "r"(magic));
+        const __nv_bfloat162 c = __hsub2(as_bf16(v), bias), h = __hmul2(c, scale[q]);
+        hi[t] = as_word(h);
+        lo[t] = as_word(__hfma2(c, scale[q], __hneg2(h)));
+      }
+      // elements 32 q + 8 p .. + 7: chunk 4 q + p of the row, swizzled by the row
+      const int chunk = 4 * q + p;
+      uint8_t* at = to + (chunk >> 3) * kHalf + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
+      *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(at + kStage) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThr, 1)
+    attn4_prefix_tc(int part_keys, const __grid_constant__ AttnArgs a, uint32_t magic) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Ctl ctl;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem_raw);
+  uint8_t* qs = smem_raw + (((base + 1023u) & ~1023u) - base);
+  uint8_t* kb = qs + 2 * kStage;  // K_hi, K_lo
+  uint8_t* vb = kb + 2 * kStage;  // V_hi, V_lo
+  uint8_t* raw = vb + 2 * kStage;
+  const int R = a.group, kv_head = blockIdx.z, part = blockIdx.y;
+  const int k_lo = part * part_keys, n_keys = min(a.prefix_len - k_lo, part_keys);
+  const int nt = (n_keys + kT - 1) / kT;
+  const int row0 = (int)blockIdx.x * 2 * kT, n_rows = (int)min((long long)a.B * R - row0, 2ll * kT);  // rows of the block
+  const int n_live = n_rows > kT ? 2 : 1;  // row tiles
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.raw_full[i], 1);
+      mbar_init(&ctl.full[i], 4);
+      mbar_init(&ctl.empty[i], 1);
+      mbar_init(&ctl.s_full[i], 1);
+      mbar_init(&ctl.p_full[i], 4);
+      mbar_init(&ctl.o_full[i], 1);
+    }
+    mbar_init(&ctl.mma_done, 1);
+    ctl.fail = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(&ctl.tmem, 512);
+    tmem_relinquish();
+  }
+  // queries: a thread a row, in the chunks' order; rows past the last are zeros
+  const int qi = warp >> 2, r = (warp & 3) * 32 + lane;  // (softmax warps) row tile, row of it
+  const bool row_live = warp < kSoftWarps && qi * kT + r < n_rows;
+  int b = 0, h = 0;
+  if (row_live) {
+    const unsigned row = (unsigned)(row0 + qi * kT + r);
+    b = (int)(row / (unsigned)R);
+    h = kv_head * R + (int)(row - (unsigned)b * (unsigned)R);
+  }
+  if (warp < kSoftWarps) {
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + (size_t)b * a.q_stride + (size_t)h * kHeadDim);
+#pragma unroll 4
+    for (int ch = 0; ch < 16; ++ch) {
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (row_live) x = __ldg(src + ch);
+      const uint4 y = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                                 __byte_perm(x.y, x.w, 0x7632));
+      *reinterpret_cast<uint4*>(qs + qi * kStage + (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = y;
+    }
+    fence_proxy_async_smem();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_allow_next();  // the own keys' kernel and the joining one, which hold no tensor memory, may be scheduled
+  const uint32_t tmem = ctl.tmem;
+
+  if (warp >= kExpandWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
+    // ---- codes and scales to operands ----
+    const bool first = warp == kExpandWarp;
+    const int key = (int)threadIdx.x - kExpandWarp * 32;
+    const int box = min(a.page_size, kT), box_row = (lane >> 1) * box;
+    const bool codes = !(lane & 1);
+    const uint32_t unit = codes ? kCodes4 : 8, page_bytes = (uint32_t)(a.H_kv * kRow4) << a.page_shift;
+    const size_t at = ((size_t)kv_head * kRow4 + (codes ? 0 : kCodes4)) << a.page_shift;
+    uint32_t loads[2] = {0, 0};  // issued: K, V
+    // K's (v = 0) or V's codes and scales of tile t, by one warp: a lane a copy
+    auto load = [&](int v, int t) {
+      const int rows = min(kT, n_keys - t * kT), k = k_lo + t * kT + box_row;
+      if (lane == 0) mbar_arrive_expect_tx(&ctl.raw_full[v], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4));
+      __syncwarp();
+      if (box_row < rows) {
+        int p = __ldg(a.prefix_table + (k >> a.page_shift));
+        if ((unsigned)p >= (unsigned)a.n_pages) {
+          set_error(a.err, kErrBadDeviceArg);
+          p = 0;
+        }
+        const uint8_t* src = static_cast<const uint8_t*>(v ? a.V : a.K) + (size_t)p * page_bytes + at + (size_t)(k & (a.page_size - 1)) * unit;
+        uint8_t* dst = raw + v * kRawBytes + (codes ? 0 : kT * kCodes4) + box_row * unit;
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                     "l"(src), "r"(box * unit), "r"(smem_u32(&ctl.raw_full[v]))
+                     : "memory");
+      }
+      __syncwarp();
+      ++loads[v];
+    };
+    if (first) {
+      load(0, 0);
+      load(1, 0);
+    }
+    bool live = true;
+    for (int t = 0; t < nt; ++t) {
+#pragma unroll 1
+      for (int v = 0; v < 2; ++v) {
+        // the operands before are read: K's by tile t - 1's scores, V's by its product
+        if (live && t > 0) live = wait_all(&ctl.empty[v], (uint32_t)(t - 1) & 1u, a.err);
+        if (live) live = wait_all(&ctl.raw_full[v], (uint32_t)t & 1u, a.err);
+        expand_row(raw + v * kRawBytes, key, key < n_keys - t * kT, magic, v ? vb : kb);
+        fence_proxy_async_smem();
+        expand_sync();  // (met by all four warps, whatever their waits gave; the codes are read)
+        if (live && lane == 0) mbar_arrive(&ctl.full[v]);
+        if (first && live && t + 1 < nt) load(v, t + 1);
+      }
+    }
+    if (!live) ctl.fail = 1;
+    if (first && !live) {
+      // copies that may still be in flight: waited for once more, with a limit
+      for (int v = 0; v < 2; ++v)
+        if (lane == 0 && loads[v] > 0) mbar_wait(&ctl.raw_full[v], (loads[v] - 1) & 1u, a.err);
+      __syncwarp();
+    }
+  } else if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    if (warp == kMmaWarp) {
+      // ---- MMA issuer: the whole warp walks through the tiles, one lane issues ----
+      const bool lead = elect_one();
+      const uint64_t qd = smem_desc_sw128(smem_u32(qs)), kd = smem_desc_sw128(smem_u32(kb)), vd = smem_desc_mn_sw128(smem_u32(vb));
+      bool live = true;
+      for (int t = 0; live && t <= nt; ++t) {
+        if (t > 0) live = wait_all(&ctl.full[1], (uint32_t)(t - 1) & 1u, a.err);
+        if (live && t < nt) live = wait_all(&ctl.full[0], (uint32_t)t & 1u, a.err);
+        for (int i = 0; live && i < n_live; ++i) {
+          const uint32_t ts = tmem + i * kT, to = tmem + (2 + i) * kT;
+          if (t > 0) {
+            live = wait_all(&ctl.p_full[i], (uint32_t)(t - 1) & 1u, a.err);
+            tc_fence_after();
+            if (lead && live) {
+#pragma unroll
+              for (int ks = 0; ks < 16; ++ks)  // hi, then lo
+                tc_mma_bf16_ts(to, ts + (ks & 7) * 8, vd + (uint64_t)(((ks >> 3) * kStage + (ks & 7) * 2048) >> 4), kIdescO,
+                               ks > 0 || t > 1 ? 1u : 0u);
+              if (t == nt) tc_commit(&ctl.o_full[i]);
+            }
+          }
+          if (t < nt) {
+            tc_fence_after();
+            if (lead && live) {
+#pragma unroll
+              for (int ks = 0; ks < 16; ++ks) {
+                const uint32_t off = ((ks >> 2) & 1) * kHalf + (ks & 3) * 32;
+                tc_mma_bf16(ts, qd + (uint64_t)((i * kStage + off) >> 4), kd + (uint64_t)(((ks >> 3) * kStage + off) >> 4), kIdescS,
+                            ks > 0 ? 1u : 0u);
+              }
+              tc_commit(&ctl.s_full[i]);
+            }
+          }
+        }
+        if (lead && live) {
+          if (t > 0) tc_commit(&ctl.empty[1]);
+          if (t < nt) tc_commit(&ctl.empty[0]);
+        }
+        __syncwarp();
+      }
+      if (!live) {
+        ctl.fail = 1;
+        if (lead) {  // products under way
+          tc_commit(&ctl.mma_done);
+          mbar_wait(&ctl.mma_done, 0, a.err);
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    // ---- softmax: a thread per row ----
+    const uint32_t ts = tmem + qi * kT + ((uint32_t)((warp & 3) * 32) << 16), to = ts + 2 * kT;
+    const float sc = a.scale_log2;
+    float m = -INFINITY, l = 0.f;
+    bool live = true;
+    for (int t = 0; live && t < nt && qi < n_live; ++t) {
+      live = wait_all(&ctl.s_full[qi], (uint32_t)t & 1u, a.err);
+      if (!live) break;
+      tc_fence_after();
+      const int seen = n_keys - t * kT;
+      float sum;
+      uint32_t w[kT / 2];
+      // as for bf16 keys: P against the maximum so far, which is raised where the tile's sum is too large
+#pragma unroll 1
+      for (bool raise = t == 0, raised = false;;) {
+        float v[kT];
+        tmem_ld64(ts, v);
+        tmem_ld64(ts + 64, v + 64);
+        tc_wait_ld();
+        if (seen < kT) {
+#pragma unroll
+          for (int e = 0; e < kT; ++e) v[e] = e < seen ? v[e] : -INFINITY;
+        }
+        if (raise) {
+          raised = true;
+          float top[8];
+#pragma unroll
+          for (int z = 0; z < 8; ++z) top[z] = fmaxf(v[z], v[8 + z]);
+#pragma unroll
+          for (int e = 16; e < kT; e += 16)
+#pragma unroll
+            for (int z = 0; z < 8; ++z) top[z] = max3(top[z], v[e + z], v[e + 8 + z]);
+          const float mx = fmaxf(max3(top[0], top[1], top[2]), max3(max3(top[3], top[4], top[5]), top[6], top[7]));
+          const float mn = fmaxf(m, mx * sc);  // sc > 0: the maximum commutes with it
+          const float f = m == mn ? 1.f : ex2_approx(m - mn);
+          m = mn;
+          if (t > 0) {
+            l *= f;
+            scale_o(to, f);
+            tc_wait_st();
+            raise = false;
+            continue;  // the scores are read again rather than kept over the call
+          }
+        }
+        const float mb = m == -INFINITY ? 0.f : m;
+        // (scores are rounded before the maximum is subtracted, as that is: with the two in one fma, scores past 2^28
+        // would pass their own maximum by more than the exponent holds)
+        const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
+        uint64_t s2[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < kT / 2; ++e) {
+          float p0, p1;
+          unpack2(add2(fma2(pack2(v[2 * e], v[2 * e + 1]), sc2, 0), mb2), p0, p1);
+          p0 = ex2_approx(p0);
+          p1 = ex2_approx(p1);
+          s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
+          w[e] = pack_bf16(p0, p1);
+        }
+        float s0, s1;
+        unpack2(add2(s2[0], s2[1]), s0, s1);
+        sum = s0 + s1;
+        raise = !raised && __any_sync(0xffffffffu, row_live && sum > kMostSum);
+        if (!raise) break;
+      }
+      l += sum;
+      tmem_st32(ts, w);
+      tmem_st32(ts + 32, w + 32);
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.p_full[qi]);
+    }
+    if (live && qi < n_live) live = wait_all(&ctl.o_full[qi], 0, a.err);
+    if (!live) ctl.fail = 1;
+    if (live && qi < n_live) {
+      tc_fence_after();
+      const size_t row = ((size_t)part * a.B + b) * a.H_q + h;
+      // (every score -inf: no weight)
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+      for (int z = 0; z < kHeadDim; z += 32) {
+        float o[32];
+        tmem_ld32(to + z, o);
+        tc_wait_ld();
+        if (row_live) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            float4* dst = reinterpret_cast<float4*>(a.part_o + row * kHeadDim + z + e);
+            dst[0] = make_float4(o[e] * inv, o[e + 2] * inv, o[e + 4] * inv, o[e + 6] * inv);
+            dst[1] = make_float4(o[e + 1] * inv, o[e + 3] * inv, o[e + 5] * inv, o[e + 7] * inv);
+          }
+        }
+        __syncwarp();
+      }
+      if (row_live) a.part_lse[row] = l == 0.f ? -INFINITY : m == -INFINITY ? NAN : m + lg2_approx(l);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace
+
+cudaError_t attn4_prefix_tc_launch(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
+  static std::atomic<bool> configured[64];  // per device, zero-initialised
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    cudaError_t e = cudaFuncSetAttribute(attn4_prefix_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    cudaFuncAttributes at;
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, attn4_prefix_tc);
+    if (e != cudaSuccess) return e;
+    // a register split that the launch does not cover would wait for ever
+    if (at.numRegs != 128) return cudaErrorInvalidConfiguration;
+    configured[dev] = true;
+  }
+  const long long rows = (long long)a.B * a.group;
+  attn4_prefix_tc<<<dim3((unsigned)((rows + 2 * kT - 1) / (2 * kT)), plan.n_pre, a.H_kv), kThr, kSmem, s>>>(plan.pre_keys, a, plan.regs[1]);
+  return cudaGetLastError();
+}
+
+}  // namespace provip

@@ -429,11 +429,13 @@ struct Attn4Plan {
   int n_cut;                 // virtual heads a key/value head
   int own_keys, n_own;       // keys of a part, parts at most (own; 0: none)
   int pre_keys, n_pre;       // the same for the prefix
-  int own_rows, pre_rows;    // query rows a CTA: 2, 8 or (bf16) 16; the prefix's (bf16) also 64 or 128
+  int own_rows, pre_rows;    // query rows a CTA: 2, 8 or (bf16) 16; the prefix's (bf16) also 256
   unsigned regs[3];          // constants of the codes' expansion (CodeRegs)
 };
 // part_* of AttnArgs: the prefix's parts, then the own ones (n_part in all); used where a row has more than one
 cudaError_t attn4_launch(const AttnArgs& a, const Attn4Plan& plan, int dtype, cudaStream_t s);
+// the prefix's parts for many bf16 rows, on the tensor cores (attention_decode4_tc.cu)
+cudaError_t attn4_prefix_tc_launch(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s);
 
 // host helper: encode a 2-D bf16 row table [rows, cols] (row stride in bytes)
 // as a tensor map with 64 x box_rows boxes and 128-byte swizzle.
