@@ -185,9 +185,8 @@ struct Joined {
   float o[4], w, m;  // weighted sum of lane's elements, sum of the weights 2^(lse - m) kJoinUnit
   __device__ __forceinline__ float lse() const { return m + log2f(w * (1.f / kJoinUnit)); }  // (base 2)
 };
-template <typename Lse, typename Part>
+template <int kRound = 12, typename Lse, typename Part>
 __device__ __forceinline__ void join_parts(Joined& s, int n, Lse lse, Part part) {
-  constexpr int kRound = 12;
   const int lane = threadIdx.x & 31;
   for (int p0 = 0; p0 < n; p0 += kRound) {
     float x[kRound];

@@ -601,484 +601,13 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
   if (!kPrefix && first) pdl_wait_prior();
 }
 
-// ---------------------------------------------------------------------------
-// The prefix, for many rows (bf16 queries). The same products as above, but a key's codes are expanded once
-// for all columns of the CTA: c d is exact in fp16 (three bits of c, or a power of two, times eight of
-// d) next to a power of two, so values go into shared memory as fp16 MMA operands, each lane's registers at
-// its place, and neither product knows of groups:
-//   score_t = 2^{e_t} (Q . k_t)        o_q = 2^{u_q} sum_t p_t v_{t,q}
-// with k_t relative to the largest scale of its row, and the values of group q to u_q, the largest scale in the
-// group among the first 64 keys. Five bits of exponent hold that while a row's scales lie within 2^10 of each
-// other, and a group's, over 16 keys, within 2^9 and at 2^u_q to a factor of 2^4. Sixteen keys that do not fit are
-// done as above, codes and scales apart. 64 keys at a time, four warps expand 16 of them each into one of two
-// buffers, while eight others take the 64 before from the other against their 8 NT columns.
-// Bound by the MMAs (half of one an SM and clock) and by their operands' way out of shared memory (128 bytes
-// a clock), which take equally long.
-// ---------------------------------------------------------------------------
-constexpr int kWideWarps = 8, kExpand = 4, kWideThr = (kWideWarps + kExpand) * 32;
-constexpr int kFragBytes = kTiles * 8 * 32 * 16;  // operands of 64 keys, K's or V's
-constexpr int kWideStages = 3;
-constexpr size_t kWideSmem = 4 * (size_t)kFragBytes + (size_t)kWideStages * kStageBytes;
-constexpr int kAtOnce = 2;  // tiles of 16 keys a warp has scores of
-constexpr int kLift = 4;  // weights are 2^4 higher than they are, so that small ones keep their bits
-constexpr int kRowSpread = 10, kTileSpread = 9, kUnitSpread = 4, kUnitMost = 40;
-
-// named barriers: 1 among the expanding warps; 2, 3 a buffer is whole, 4, 5 it may be overwritten
-__device__ __forceinline__ void expand_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kExpand * 32) : "memory"); }
-__device__ __forceinline__ void wide_sync(int id) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(kWideThr) : "memory"); }
-__device__ __forceinline__ void wide_arrive(int id) { asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "n"(kWideThr) : "memory"); }
-__device__ __forceinline__ float pow2(int biased) { return __uint_as_float((uint32_t)biased << 23); }
-// biased exponent of scale q of a row (0 for a scale of zero; infinite and NaN ones, which show in any case, too)
-__device__ __forceinline__ int exponent_of(uint2 d, int q) {
-  const uint32_t w = (q < 2 ? d.x : d.y) >> (q & 1 ? 16 : 0);
-  const int x = (int)((w >> 7) & 255u);
-  return x == 255 ? 0 : (w & 0x7fffu) ? max(min(x, 253), 1) : 0;
-}
-__device__ __forceinline__ float scale_f(uint2 d, int q) {
-  const uint32_t w = q < 2 ? d.x : d.y;
-  return q & 1 ? hi_f(w) : lo_f(w);
-}
-__device__ __forceinline__ uint32_t times(uint32_t x, __half2 d) {
-  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x), d);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-
-template <int N>
-struct Tiles {
-  static constexpr int n = N;
-};
-
-template <int NT>
-__global__ void __launch_bounds__(kWideThr, 1)
-    attn4_prefix(const __grid_constant__ AttnArgs a, const __grid_constant__ Attn4Plan plan) {
-  constexpr int C = kWideWarps * 8 * NT;  // columns a CTA
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ uint64_t full[kWideStages];
-  __shared__ int s_ek[2][kStep];       // exponents of the keys' rows
-  __shared__ __align__(16) int s_top[2][4][4];  // largest exponents of 16 keys' groups of values
-  __shared__ __align__(16) int s_unit[2][4];    // exponents that the groups' values are relative to
-  __shared__ int s_apart[2][2][kTiles];  // 16 keys whose codes and scales stay apart: K's, V's
-  __shared__ uint2 s_d[2][2][kStep];   // scales
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
-  pdl_allow_next();
-  const int R = a.group, block = (int)blockIdx.x * C, part = blockIdx.y, kv_head = blockIdx.z;
-  const int k_lo = part * plan.pre_keys;
-  const int k_hi = k_lo + min(a.prefix_len - k_lo, plan.pre_keys);
-  const int n_steps = (k_hi - k_lo + kStep - 1) / kStep;
-  uint8_t* ring = smem + 4 * kFragBytes;
-
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kWideStages; ++s) mbar_init(&full[s], 1);
-    fence_mbar_init();
-  }
-  __syncthreads();
-  const CodeRegs regs = {plan.regs[0], plan.regs[1], plan.regs[2]};
-
-  if (warp >= kWideWarps) {
-    // ---- expanding warps: 16 keys each as operands. Rows past the end are zeros, whatever lies there ----
-    const int w = warp - kWideWarps;
-    const bool first = w == 0;
-    // loads, by the first of them: a lane per copy of a stage
-    const int box = min(a.page_size, kStep), kind = lane & 3, box_row = (lane >> 2) * box;
-    auto page_of = [&](int step) {
-      const int k = k_lo + step * kStep + box_row;
-      return box_row < kStep && step < n_steps && k < k_hi ? __ldg(a.prefix_table + (k >> a.page_shift)) : 0;
-    };
-    int page = first ? page_of(0) : 0;
-    const uint32_t unit_bytes = kind < 2 ? kCodes4 : 8;
-    const uint32_t dst = smem_u32(ring) + box_row * unit_bytes + (kind < 2 ? kind * kCodeBytes : 2 * kCodeBytes + (kind - 2) * kScaleBytes);
-    const uint8_t* src = static_cast<const uint8_t*>(kind & 1 ? a.V : a.K) + (((size_t)kv_head * kRow4 + (kind < 2 ? 0 : kCodes4)) << a.page_shift);
-    const uint32_t page_bytes = (uint32_t)(a.H_kv * kRow4) << a.page_shift;
-    int issued = 0;  // (steps in order: stage issued % kWideStages)
-    auto load = [&]() {
-      const int k = k_lo + issued * kStep, rows = min(kStep, k_hi - k), stage = issued % kWideStages;
-      int p = page;
-      page = page_of(issued + 1);
-      if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4 * 2));
-      __syncwarp();
-      if (box_row < rows) {
-        if ((unsigned)p >= (unsigned)a.n_pages) {
-          set_error(a.err, kErrBadDeviceArg);
-          p = 0;
-        }
-        bulk_load(dst + stage * kStageBytes, src + (size_t)p * page_bytes + ((k + box_row) & (a.page_size - 1)) * unit_bytes,
-                  box * unit_bytes, smem_u32(&full[stage]));
-      }
-      __syncwarp();
-      ++issued;
-    };
-    if (first)
-      while (issued < kWideStages && issued < n_steps) load();
-    int made[4] = {0, 0, 0, 0};  // exponents that the values are relative to
-    bool failed = false;
-    for (int step = 0; step < n_steps; ++step) {
-      const int stage = step % kWideStages, buf = step & 1, left = k_hi - k_lo - step * kStep;
-      // (a wait that gives up: no more waits, but every barrier is met)
-      if (!failed && __any_sync(0xffffffffu, !mbar_wait(&full[stage], (uint32_t)(step / kWideStages) & 1u, a.err))) failed = true;
-      if (step >= 2) wide_sync(4 + buf);
-      const uint8_t* st = ring + stage * kStageBytes;
-      uint4* to = reinterpret_cast<uint4*>(smem + buf * 2 * kFragBytes) + w * 8 * 32 + lane;
-      {
-        const uint8_t *kc = st, *ks = st + 2 * kCodeBytes;
-        const int r0 = w * 16 + g, r1 = r0 + 8;
-        uint2 da = *reinterpret_cast<const uint2*>(ks + r0 * 8), db = *reinterpret_cast<const uint2*>(ks + r1 * 8);
-        if (r0 >= left) da = make_uint2(0u, 0u);
-        if (r1 >= left) db = make_uint2(0u, 0u);
-        int ea = 1, eb = 1, la = 255, lb = 255;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int x = exponent_of(da, q), y = exponent_of(db, q);
-          ea = max(ea, x);
-          eb = max(eb, y);
-          la = min(la, x == 0 ? 255 : x);
-          lb = min(lb, y == 0 ? 255 : y);
-        }
-        const bool apart = __any_sync(0xffffffffu, ea - la > kRowSpread || eb - lb > kRowSpread);
-        if (lane == 0) s_apart[buf][0][w] = apart;
-        if (j == 0) {
-          s_ek[buf][r0] = ea;
-          s_ek[buf][r1] = eb;
-          s_d[buf][0][r0] = da;
-          s_d[buf][0][r1] = db;
-        }
-        const float fa = pow2(254 - ea), fb = pow2(254 - eb);  // 2^-(e - 127)
-        const uint4 wa = *reinterpret_cast<const uint4*>(kc + r0 * kCodes4 + 16 * j);
-        const uint4 wb = *reinterpret_cast<const uint4*>(kc + r1 * kCodes4 + 16 * j);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
-          uint32_t ca[4], cb[4];
-          codes_f16(q < 2 ? __byte_perm(wa.x, wa.z, sel) : __byte_perm(wa.y, wa.w, sel), regs, ca);
-          codes_f16(q < 2 ? __byte_perm(wb.x, wb.z, sel) : __byte_perm(wb.y, wb.w, sel), regs, cb);
-          const __half2 ha = __float2half2_rn(apart ? 1.f : scale_f(da, q) * fa), hb = __float2half2_rn(apart ? 1.f : scale_f(db, q) * fb);
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            to[(2 * q + i) * 32] = make_uint4(times(ca[2 * i], ha), times(cb[2 * i], hb), times(ca[2 * i + 1], ha), times(cb[2 * i + 1], hb));
-        }
-      }
-      {
-        // keys 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of the sixteen, dims 4 g .. + 3 of each group
-        const uint8_t *vc = st + kCodeBytes, *vs = st + 2 * kCodeBytes + kScaleBytes;
-        to += kFragBytes / 16;
-        uint2 v[4], d[4];
-        int hi[4] = {0, 0, 0, 0}, lo[4] = {255, 255, 255, 255};  // a group's largest and smallest exponent
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = w * 16 + 2 * j + (i >> 1) * 8 + (i & 1);
-          v[i] = *reinterpret_cast<const uint2*>(vc + r * kCodes4 + 8 * g);
-          d[i] = *reinterpret_cast<const uint2*>(vs + r * 8);
-          if (r >= left) d[i] = make_uint2(0u, 0u);
-          if (g == 0) s_d[buf][1][r] = d[i];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int e = exponent_of(d[i], q);
-            hi[q] = max(hi[q], e);
-            lo[q] = min(lo[q], e == 0 ? 255 : e);
-          }
-        }
-        // (the eight lanes with another j have other keys, those with another g the same)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int b = 1; b < 4; b <<= 1) {
-            hi[q] = max(hi[q], __shfl_xor_sync(0xffffffffu, hi[q], b));
-            lo[q] = min(lo[q], __shfl_xor_sync(0xffffffffu, lo[q], b));
-          }
-        if (lane == 0) *reinterpret_cast<int4*>(s_top[buf][w]) = make_int4(hi[0], hi[1], hi[2], hi[3]);
-        expand_sync();
-        // (the stage before is read by all of them)
-        if (first && issued < n_steps && step > 0) load();
-        bool apart = false;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int top = max(max(max(s_top[buf][0][q], s_top[buf][1][q]), max(s_top[buf][2][q], s_top[buf][3][q])), 1);
-          if (step == 0 || top > made[q] + kUnitMost) made[q] = top;  // (or far larger than what was before)
-          apart = apart || hi[q] - lo[q] > kTileSpread || (hi[q] > 0 && abs(hi[q] - made[q]) > kUnitSpread);
-        }
-        if (lane == 0) {
-          s_apart[buf][1][w] = apart;
-          if (w == 0) *reinterpret_cast<int4*>(s_unit[buf]) = make_int4(made[0], made[1], made[2], made[3]);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
-          const uint32_t ya = q < 2 ? __byte_perm(v[0].x, v[1].x, sel) : __byte_perm(v[0].y, v[1].y, sel);
-          const uint32_t yb = q < 2 ? __byte_perm(v[2].x, v[3].x, sel) : __byte_perm(v[2].y, v[3].y, sel);
-          uint32_t ca[4], cb[4];
-          if (apart) {
-            codes_bf16(ya, regs, ca);
-            codes_bf16(yb, regs, cb);
-          } else {
-            codes_f16(ya, regs, ca);
-            codes_f16(yb, regs, cb);
-            const float f = pow2(254 - made[q]);
-            const __half2 ha = __floats2half2_rn(scale_f(d[0], q) * f, scale_f(d[1], q) * f);
-            const __half2 hb = __floats2half2_rn(scale_f(d[2], q) * f, scale_f(d[3], q) * f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              ca[i] = times(ca[i], ha);
-              cb[i] = times(cb[i], hb);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i) to[(2 * q + i) * 32] = make_uint4(ca[2 * i], ca[2 * i + 1], cb[2 * i], cb[2 * i + 1]);
-        }
-      }
-      wide_arrive(2 + buf);
-    }
-    if (failed && first) {
-      // copies that may still be in flight into the block's shared memory: waited for once more, with a limit
-      for (int i = max(issued - kWideStages, 0); i < issued; ++i) mbar_wait(&full[i % kWideStages], (uint32_t)(i / kWideStages) & 1u, a.err);
-    }
-    return;
-  }
-
-  // queries, as in the kernel above: a warp its own columns
-  uint32_t qf[NT][4][4];
-  float cs[NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const Column c = column<true>(a, R, kv_head, block, (warp * NT + nt) * 8 + g);
-    float x[4][8], most = 0.f;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[q][e] = 0.f;
-      if (c.h >= 0)
-        load8(static_cast<const __nv_bfloat16*>(a.Q) + (size_t)c.b * a.q_stride + (size_t)c.h * kHeadDim + 32 * q + 8 * j, x[q]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[q][e]));
-    }
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    const int up = 14 + 127 - max((int)(__float_as_uint(most) >> 23), 27);
-    const float mul = pow2(127 + up), back = pow2(127 - up) * a.scale_log2;
-#pragma unroll
-    for (int c2 = 0; c2 < 2; ++c2) cs[nt][c2] = __shfl_sync(0xffffffffu, back, 4 * (2 * j + c2));
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        uint32_t r[1];
-        split2_f16<1>(x[q][t] * mul, x[q][t + 4] * mul, r);
-        qf[nt][q][t] = r[0];
-      }
-  }
-
-  float o[8][NT][4], m[NT][2], base[NT][2], l[NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      m[nt][c] = -INFINITY;
-      base[nt][c] = l[nt][c] = 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
-  }
-  int unit[4] = {0, 0, 0, 0};  // of o's sums; warps 4-7: of the values expanded last
-  // a new maximum, where a score passes the one before by 2^10
-  auto raise_to = [&](const float (*top)[2]) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float x = top[nt][c];
-#pragma unroll
-        for (int b = 4; b < 32; b <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, b));
-        x = fmaxf(x, m[nt][c]);
-        const float f = x == m[nt][c] ? 1.f : ex2_approx(m[nt][c] - x);
-        m[nt][c] = x;
-        base[nt][c] = x == -INFINITY ? 0.f : x;
-        l[nt][c] *= f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          o[i][nt][c] *= f;
-          o[i][nt][c + 2] *= f;
-        }
-      }
-  };
-
-  // ---- kN tiles of 16 keys from tile mt0 on against this warp's columns ----
-  auto attend = [&](auto tiles, int buf, int mt0, int left, bool k_apart, bool v_apart) {
-    constexpr int kN = decltype(tiles)::n;
-    const uint4* kf = reinterpret_cast<const uint4*>(smem + buf * 2 * kFragBytes) + mt0 * 8 * 32 + lane;
-    const uint4* vf = kf + kFragBytes / 16;
-    float s[kN][NT][4];
-    if (!k_apart) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int mt = 0; mt < kN; ++mt) {
-          const uint4 c = kf[(mt * 8 + i) * 32];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (i == 0)
-              mma16<true, true>(s[mt][nt], c.x, c.y, c.z, c.w, qf[nt][0][0], qf[nt][0][1]);
-            else
-              mma16<true, false>(s[mt][nt], c.x, c.y, c.z, c.w, qf[nt][i >> 1][2 * (i & 1)], qf[nt][i >> 1][2 * (i & 1) + 1]);
-          }
-        }
-#pragma unroll
-      for (int mt = 0; mt < kN; ++mt) {
-        const float ka = pow2(s_ek[buf][(mt0 + mt) * 16 + g]), kb = pow2(s_ek[buf][(mt0 + mt) * 16 + g + 8]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[mt][nt][e] *= e < 2 ? ka : kb;
-      }
-    } else {
-#pragma unroll
-      for (int mt = 0; mt < kN; ++mt) {
-        const uint2 da = s_d[buf][0][(mt0 + mt) * 16 + g], db = s_d[buf][0][(mt0 + mt) * 16 + g + 8];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint4 c0 = kf[(mt * 8 + 2 * q) * 32], c1 = kf[(mt * 8 + 2 * q + 1) * 32];
-          const float fa = scale_f(da, q), fb = scale_f(db, q);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float x[4];
-            mma16<true, true>(x, c0.x, c0.y, c0.z, c0.w, qf[nt][q][0], qf[nt][q][1]);
-            mma16<true, false>(x, c1.x, c1.y, c1.z, c1.w, qf[nt][q][2], qf[nt][q][3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[mt][nt][e] = q == 0 ? x[e] * (e < 2 ? fa : fb) : fmaf(x[e], e < 2 ? fa : fb, s[mt][nt][e]);
-          }
-        }
-      }
-    }
-    bool raise = false;
-    float top[NT][2];
-#pragma unroll
-    for (int mt = 0; mt < kN; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[mt][nt][e] = __fmul_rn(s[mt][nt][e], cs[nt][e & 1]);
-    if (left < kStep) {
-#pragma unroll
-      for (int mt = 0; mt < kN; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if ((mt0 + mt) * 16 + g + (e >> 1) * 8 >= left) s[mt][nt][e] = -INFINITY;
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        top[nt][c] = fmaxf(s[0][nt][c], s[0][nt][c + 2]);
-#pragma unroll
-        for (int mt = 1; mt < kN; ++mt) top[nt][c] = fmaxf(top[nt][c], fmaxf(s[mt][nt][c], s[mt][nt][c + 2]));
-        raise = raise || top[nt][c] > m[nt][c] + 10.f;
-      }
-    if (__any_sync(0xffffffffu, raise)) raise_to(top);
-#pragma unroll
-    for (int mt = 0; mt < kN; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = ex2_approx(s[mt][nt][e] - base[nt][e & 1]);
-          l[nt][e & 1] += p;
-          s[mt][nt][e] = p * (float)(1 << kLift);
-        }
-    if (!v_apart) {
-#pragma unroll
-      for (int mt = 0; mt < kN; ++mt) {
-        uint32_t b0[NT], b1[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const __half2 x = __floats2half2_rn(s[mt][nt][0], s[mt][nt][1]), y = __floats2half2_rn(s[mt][nt][2], s[mt][nt][3]);
-          b0[nt] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
-          b1[nt] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint4 c = vf[(mt * 8 + i) * 32];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16<true, false>(o[i][nt], c.x, c.y, c.z, c.w, b0[nt], b1[nt]);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int mt = 0; mt < kN; ++mt) {
-        const uint2 da = s_d[buf][1][(mt0 + mt) * 16 + g], db = s_d[buf][1][(mt0 + mt) * 16 + g + 8];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint4 c0 = vf[(mt * 8 + 2 * q) * 32], c1 = vf[(mt * 8 + 2 * q + 1) * 32];
-          const float f = pow2(254 - unit[q]), fa = scale_f(da, q) * f, fb = scale_f(db, q) * f;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const uint32_t b0 = transpose8x8(pack2(s[mt][nt][0] * fa, s[mt][nt][1] * fa)), b1 = transpose8x8(pack2(s[mt][nt][2] * fb, s[mt][nt][3] * fb));
-            mma16<false, false>(o[2 * q][nt], c0.x, c0.y, c0.z, c0.w, b0, b1);
-            mma16<false, false>(o[2 * q + 1][nt], c1.x, c1.y, c1.z, c1.w, b0, b1);
-          }
-        }
-      }
-    }
-  };
-
-  for (int step = 0; step < n_steps; ++step) {
-    const int buf = step & 1, left = k_hi - k_lo - step * kStep;
-    wide_sync(2 + buf);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int u = s_unit[buf][q];
-      if (u != unit[q]) {  // larger values: what there is, relative to them
-        const float f = pow2(max(127 + unit[q] - u, 0));
-#pragma unroll
-        for (int i = 2 * q; i < 2 * q + 2; ++i)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][nt][e] *= f;
-        unit[q] = u;
-      }
-    }
-    int any = 0;
-#pragma unroll
-    for (int mt = 0; mt < kTiles; ++mt) any |= s_apart[buf][0][mt] | s_apart[buf][1][mt];
-    if (!any) {
-#pragma unroll 1
-      for (int mt = 0; mt < kTiles && mt * 16 < left; mt += kAtOnce) attend(Tiles<kAtOnce>(), buf, mt, left, false, false);
-    } else {
-#pragma unroll 1
-      for (int mt = 0; mt < kTiles && mt * 16 < left; ++mt)
-        attend(Tiles<1>(), buf, mt, left, s_apart[buf][0][mt] != 0, s_apart[buf][1][mt] != 0);
-    }
-    if (step + 2 < n_steps) wide_arrive(4 + buf);  // these operands may be overwritten
-  }
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-      for (int b = 4; b < 32; b <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], b);
-      const Column at = column<true>(a, R, kv_head, block, (warp * NT + nt) * 8 + 2 * j + c);
-      if (at.h < 0) continue;
-      // (every score -inf: no weight)
-      const bool nil = l[nt][c] == 0.f;
-      const float inv = nil ? 0.f : (1.f / (1 << kLift)) / l[nt][c];
-      const size_t slot = (size_t)part * a.B * a.H_q + (size_t)at.b * a.H_q + at.h;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float f = pow2(max(unit[q], 1));
-        *reinterpret_cast<float4*>(a.part_o + slot * kHeadDim + 32 * q + 4 * g) =
-            make_float4(o[2 * q][nt][c] * inv * f, o[2 * q][nt][c + 2] * inv * f, o[2 * q + 1][nt][c] * inv * f, o[2 * q + 1][nt][c + 2] * inv * f);
-      }
-      if (g == 0) a.part_lse[slot] = nil ? -INFINITY : m[nt][c] == -INFINITY ? NAN : m[nt][c] + log2f(l[nt][c]);
-    }
-}
-
-// parts -> rows, a warp each
+// Parts -> rows, a warp each: up to 24 parts are under way at once (12 had taken 9.7 us for 1792 rows of 20).
+constexpr int kJoinThr = 128;
 template <typename T>
-__global__ void __launch_bounds__(256) attn4_join(const __grid_constant__ AttnArgs a, const __grid_constant__ Attn4Plan plan) {
+__global__ void __launch_bounds__(kJoinThr) attn4_join(const __grid_constant__ AttnArgs a, const __grid_constant__ Attn4Plan plan) {
   pdl_wait_prior();
   const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), n_rows = (long long)a.B * a.H_q;
+  const long long row = (long long)blockIdx.x * (kJoinThr / 32) + (threadIdx.x >> 5), n_rows = (long long)a.B * a.H_q;
   if (row >= n_rows) return;
   const int b = (int)(row / a.H_q);
   int len = a.k_len[b];
@@ -1086,7 +615,7 @@ __global__ void __launch_bounds__(256) attn4_join(const __grid_constant__ AttnAr
   if (a.prefix_len == 0 && len <= plan.own_keys) return;  // written by its only part
   const int n_own = plan.n_own > 0 ? (len + plan.own_keys - 1) / plan.own_keys : 0;
   Joined s = {{0.f, 0.f, 0.f, 0.f}, 0.f, -INFINITY};
-  join_parts(
+  join_parts<24>(
       s, plan.n_pre + n_own, [&](int p) { return a.part_lse[p * n_rows + row]; },
       [&](int p) { return a.part_o + (p * n_rows + row) * kHeadDim; });
   const float den = s.w == 0.f ? NAN : s.w;  // (there are keys: every score -inf is 0 / 0)
@@ -1125,32 +654,14 @@ cudaError_t go_by_columns(int rows, const AttnArgs& a, const Attn4Plan& plan, cu
   return cudaErrorInvalidValue;
 }
 
-template <int NT>
-cudaError_t go_wide(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
-  static std::atomic<bool> configured[64];  // per device, zero-initialised
-  int dev = 0;
-  cudaGetDevice(&dev);
-  if (dev >= 0 && dev < 64 && !configured[dev]) {
-    cudaError_t e = cudaFuncSetAttribute(attn4_prefix<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kWideSmem);
-    if (e != cudaSuccess) return e;
-    configured[dev] = true;
-  }
-  const long long rows = (long long)a.B * a.group;
-  constexpr int C = kWideWarps * 8 * NT;
-  attn4_prefix<NT><<<dim3((unsigned)((rows + C - 1) / C), plan.n_pre, a.H_kv), kWideThr, kWideSmem, s>>>(a, plan);
-  return cudaGetLastError();
-}
-
 template <typename T>
 cudaError_t run(const AttnArgs& a, const Attn4Plan& plan, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (plan.n_pre > 0)
-    e = plan.pre_rows == 256 ? attn4_prefix_tc_launch(a, plan, s)
-        : plan.pre_rows == 128 ? go_wide<2>(a, plan, s)
-        : plan.pre_rows == 64 ? go_wide<1>(a, plan, s) : go_by_columns<T, true>(plan.pre_rows, a, plan, s);
+    e = plan.pre_rows == 256 ? attn4_prefix_tc_launch(a, plan, s) : go_by_columns<T, true>(plan.pre_rows, a, plan, s);
   if (e == cudaSuccess) e = go_by_columns<T, false>(plan.own_rows, a, plan, s);
   if (e != cudaSuccess || plan.n_pre + plan.n_own <= 1) return e;
-  return launch_pdl(attn4_join<T>, dim3((unsigned)(((long long)a.B * a.H_q + 7) / 8)), dim3(256), 0, s, a, plan);
+  return launch_pdl(attn4_join<T>, dim3((unsigned)(((long long)a.B * a.H_q + kJoinThr / 32 - 1) / (kJoinThr / 32))), dim3(kJoinThr), 0, s, a, plan);
 }
 
 }  // namespace

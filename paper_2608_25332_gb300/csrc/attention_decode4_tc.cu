@@ -13,10 +13,10 @@
 // codes give them: queries are staged in that order too, and the output's columns are read in it.
 // The maximum is raised only where a tile's sum passes 2^10, as for bf16 keys (attention_tc.cu).
 //
-// Roles (512 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
-// codes, a key's row a thread, K for the next tile while the softmax works, V when the product before has read
-// the buffer; one of them loads, by bulk copies. Two row tiles share every operand and keep the tensor
-// cores busy for one while the other's softmax runs. Every wait is bounded; one that gives up sets the error word
+// Roles (640 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
+// K's codes, warps 16-19 V's, a key's row a thread, K for the next tile while the softmax works, V when the product
+// before has read the buffer; the first of each four loads, by bulk copies. Two row tiles share every operand
+// and keep the tensor cores busy for one while the other's softmax runs. Every wait is bounded; one that gives up sets the error word
 // and ends its role, the other roles' waits then run out likewise, and the block ends when what it has issued is
 // done.
 #include "attention_tc.cuh"
@@ -25,10 +25,10 @@ namespace provip {
 namespace {
 
 constexpr int kSoftWarps = 8, kMmaWarp = 8, kExpandWarp = 12;
-constexpr int kThr = 512;
-// registers a thread: what the softmax takes more than the launch's 128, the others leave (the sums are equal)
-constexpr int kSoftRegs = 176, kMmaRegs = 40, kExpandRegs = 120;
-static_assert(kSoftRegs * 256 + kMmaRegs * 128 + kExpandRegs * 128 == 128 * kThr, "register split");
+constexpr int kThr = 640;
+// registers a thread: what the softmax takes more than the launch's 96, the others leave
+constexpr int kLaunchRegs = 96, kSoftRegs = 152, kMmaRegs = 40, kExpandRegs = 64;
+static_assert(kSoftRegs * 256 + kMmaRegs * 128 + kExpandRegs * 256 <= kLaunchRegs * kThr, "register split");
 constexpr int kRawBytes = kT * (kCodes4 + 8);  // K's or V's codes and scales of a tile
 constexpr size_t kSmem = 6 * (size_t)kStage + 2 * kRawBytes + 1024;
 constexpr uint32_t kIdescS = idesc_bf16_f32(kT, kT);
@@ -47,7 +47,8 @@ struct Ctl {
 __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, unsigned* err) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
 }
-__device__ __forceinline__ void expand_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+// the four warps that expand K (v = 0) or V
+__device__ __forceinline__ void expand_sync(int v) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + v) : "memory"); }
 __device__ __forceinline__ __nv_bfloat162 as_bf16(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
 __device__ __forceinline__ uint32_t as_word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t*>(&v); }
 __device__ __forceinline__ void scale_o(uint32_t to, float f) {
@@ -68,7 +69,7 @@ __device__ __forceinline__ void expand_row(const uint8_t* raw, int r, bool on, u
   const __nv_bfloat162 scale[4] = {as_bf16(__byte_perm(d.x, d.x, 0x1010)), as_bf16(__byte_perm(d.x, d.x, 0x3232)),
                                    as_bf16(__byte_perm(d.y, d.y, 0x1010)), as_bf16(__byte_perm(d.y, d.y, 0x3232))};
   const __nv_bfloat162 bias = __bfloat162bfloat162(__float2bfloat16_rn(136.f));
-#pragma unroll
+#pragma unroll 1
   for (int p = 0; p < 4; ++p) {
     const uint4 w = *reinterpret_cast<const uint4*>(raw + r * kCodes4 + 16 * p);
 #pragma unroll
@@ -107,9 +108,49 @@ __global__ void __launch_bounds__(kThr, 1)
   const int nt = (n_keys + kT - 1) / kT;
   const int row0 = (int)blockIdx.x * 2 * kT, n_rows = (int)min((long long)a.B * R - row0, 2ll * kT);  // rows of the block
   const int n_live = n_rows > kT ? 2 : 1;  // row tiles
+  // codes and scales of a tile, K's (v = 0) or V's, by one warp: a lane a copy
+  const int v_role = warp >= kExpandWarp + 4 ? 1 : 0;
+  const bool loader = warp == kExpandWarp || warp == kExpandWarp + 4;
+  const int box = min(a.page_size, kT), box_row = (lane >> 1) * box;
+  const bool codes = !(lane & 1);
+  const uint32_t unit = codes ? kCodes4 : 8;
+  auto page_of = [&](int t) {
+    const int k = t * kT + box_row;
+    return box_row < kT && k < n_keys ? __ldg(a.prefix_table + ((k_lo + k) >> a.page_shift)) : 0;
+  };
+  int page = 0, loads = 0;
+  auto load = [&]() {
+    const int t = loads, rows = min(kT, n_keys - t * kT), k = k_lo + t * kT + box_row;
+    int p = page;
+    page = page_of(t + 1);
+    if (lane == 0) mbar_arrive_expect_tx(&ctl.raw_full[v_role], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4));
+    __syncwarp();
+    if (box_row < rows) {
+      if ((unsigned)p >= (unsigned)a.n_pages) {
+        set_error(a.err, kErrBadDeviceArg);
+        p = 0;
+      }
+      const uint8_t* src = static_cast<const uint8_t*>(v_role ? a.V : a.K) + (size_t)p * ((uint32_t)(a.H_kv * kRow4) << a.page_shift) +
+                           (((size_t)kv_head * kRow4 + (codes ? 0 : kCodes4)) << a.page_shift) + (size_t)(k & (a.page_size - 1)) * unit;
+      uint8_t* dst = raw + v_role * kRawBytes + (codes ? 0 : kT * kCodes4) + box_row * unit;
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                   "l"(src), "r"(box * unit), "r"(smem_u32(&ctl.raw_full[v_role]))
+                   : "memory");
+    }
+    __syncwarp();
+    ++loads;
+  };
+  if (loader) {  // the first tile's are asked for while the block is set up
+    page = page_of(0);
+    if (lane == 0) {
+      mbar_init(&ctl.raw_full[v_role], 1);
+      fence_mbar_init();
+    }
+    __syncwarp();
+    load();
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&ctl.raw_full[i], 1);
       mbar_init(&ctl.full[i], 4);
       mbar_init(&ctl.empty[i], 1);
       mbar_init(&ctl.s_full[i], 1);
@@ -154,56 +195,24 @@ __global__ void __launch_bounds__(kThr, 1)
   if (warp >= kExpandWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
     // ---- codes and scales to operands ----
-    const bool first = warp == kExpandWarp;
-    const int key = (int)threadIdx.x - kExpandWarp * 32;
-    const int box = min(a.page_size, kT), box_row = (lane >> 1) * box;
-    const bool codes = !(lane & 1);
-    const uint32_t unit = codes ? kCodes4 : 8, page_bytes = (uint32_t)(a.H_kv * kRow4) << a.page_shift;
-    const size_t at = ((size_t)kv_head * kRow4 + (codes ? 0 : kCodes4)) << a.page_shift;
-    uint32_t loads[2] = {0, 0};  // issued: K, V
-    // K's (v = 0) or V's codes and scales of tile t, by one warp: a lane a copy
-    auto load = [&](int v, int t) {
-      const int rows = min(kT, n_keys - t * kT), k = k_lo + t * kT + box_row;
-      if (lane == 0) mbar_arrive_expect_tx(&ctl.raw_full[v], (uint32_t)(((rows + box - 1) & ~(box - 1)) * kRow4));
-      __syncwarp();
-      if (box_row < rows) {
-        int p = __ldg(a.prefix_table + (k >> a.page_shift));
-        if ((unsigned)p >= (unsigned)a.n_pages) {
-          set_error(a.err, kErrBadDeviceArg);
-          p = 0;
-        }
-        const uint8_t* src = static_cast<const uint8_t*>(v ? a.V : a.K) + (size_t)p * page_bytes + at + (size_t)(k & (a.page_size - 1)) * unit;
-        uint8_t* dst = raw + v * kRawBytes + (codes ? 0 : kT * kCodes4) + box_row * unit;
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-                     "l"(src), "r"(box * unit), "r"(smem_u32(&ctl.raw_full[v]))
-                     : "memory");
-      }
-      __syncwarp();
-      ++loads[v];
-    };
-    if (first) {
-      load(0, 0);
-      load(1, 0);
-    }
+    const int key = ((int)threadIdx.x - kExpandWarp * 32) & 127;
+    const uint8_t* from = raw + v_role * kRawBytes;
+    uint8_t* to = v_role ? vb : kb;
     bool live = true;
     for (int t = 0; t < nt; ++t) {
-#pragma unroll 1
-      for (int v = 0; v < 2; ++v) {
-        // the operands before are read: K's by tile t - 1's scores, V's by its product
-        if (live && t > 0) live = wait_all(&ctl.empty[v], (uint32_t)(t - 1) & 1u, a.err);
-        if (live) live = wait_all(&ctl.raw_full[v], (uint32_t)t & 1u, a.err);
-        expand_row(raw + v * kRawBytes, key, key < n_keys - t * kT, magic, v ? vb : kb);
-        fence_proxy_async_smem();
-        expand_sync();  // (met by all four warps, whatever their waits gave; the codes are read)
-        if (live && lane == 0) mbar_arrive(&ctl.full[v]);
-        if (first && live && t + 1 < nt) load(v, t + 1);
-      }
+      // the operands before are read: K's by tile t - 1's scores, V's by its product
+      if (live && t > 0) live = wait_all(&ctl.empty[v_role], (uint32_t)(t - 1) & 1u, a.err);
+      if (live) live = wait_all(&ctl.raw_full[v_role], (uint32_t)t & 1u, a.err);
+      expand_row(from, key, key < n_keys - t * kT, magic, to);
+      fence_proxy_async_smem();
+      expand_sync(v_role);  // (met by all four warps, whatever their waits gave; the codes are read)
+      if (live && lane == 0) mbar_arrive(&ctl.full[v_role]);
+      if (loader && live && t + 1 < nt) load();
     }
     if (!live) ctl.fail = 1;
-    if (first && !live) {
+    if (loader && !live) {
       // copies that may still be in flight: waited for once more, with a limit
-      for (int v = 0; v < 2; ++v)
-        if (lane == 0 && loads[v] > 0) mbar_wait(&ctl.raw_full[v], (loads[v] - 1) & 1u, a.err);
+      mbar_wait(&ctl.raw_full[v_role], (uint32_t)(loads - 1) & 1u, a.err);
       __syncwarp();
     }
   } else if (warp >= kMmaWarp) {
@@ -274,24 +283,26 @@ __global__ void __launch_bounds__(kThr, 1)
       // as for bf16 keys: P against the maximum so far, which is raised where the tile's sum is too large
 #pragma unroll 1
       for (bool raise = t == 0, raised = false;;) {
-        float v[kT];
-        tmem_ld64(ts, v);
-        tmem_ld64(ts + 64, v + 64);
-        tc_wait_ld();
-        if (seen < kT) {
-#pragma unroll
-          for (int e = 0; e < kT; ++e) v[e] = e < seen ? v[e] : -INFINITY;
-        }
         if (raise) {
           raised = true;
-          float top[8];
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int z = 0; z < kT; z += 64) {
+            float v[64], top[8];
+            tmem_ld64(ts + z, v);
+            tc_wait_ld();
+            if (seen < kT) {
 #pragma unroll
-          for (int z = 0; z < 8; ++z) top[z] = fmaxf(v[z], v[8 + z]);
+              for (int e = 0; e < 64; ++e) v[e] = z + e < seen ? v[e] : -INFINITY;
+            }
 #pragma unroll
-          for (int e = 16; e < kT; e += 16)
+            for (int e = 0; e < 8; ++e) top[e] = fmaxf(v[e], v[8 + e]);
 #pragma unroll
-            for (int z = 0; z < 8; ++z) top[z] = max3(top[z], v[e + z], v[e + 8 + z]);
-          const float mx = fmaxf(max3(top[0], top[1], top[2]), max3(max3(top[3], top[4], top[5]), top[6], top[7]));
+            for (int e = 16; e < 64; e += 16)
+#pragma unroll
+              for (int k = 0; k < 8; ++k) top[k] = max3(top[k], v[e + k], v[e + 8 + k]);
+            mx = fmaxf(mx, fmaxf(max3(top[0], top[1], top[2]), max3(max3(top[3], top[4], top[5]), top[6], top[7])));
+          }
           const float mn = fmaxf(m, mx * sc);  // sc > 0: the maximum commutes with it
           const float f = m == mn ? 1.f : ex2_approx(m - mn);
           m = mn;
@@ -299,8 +310,6 @@ __global__ void __launch_bounds__(kThr, 1)
             l *= f;
             scale_o(to, f);
             tc_wait_st();
-            raise = false;
-            continue;  // the scores are read again rather than kept over the call
           }
         }
         const float mb = m == -INFINITY ? 0.f : m;
@@ -309,13 +318,23 @@ __global__ void __launch_bounds__(kThr, 1)
         const uint64_t sc2 = pack2(sc, sc), mb2 = pack2(-mb, -mb);
         uint64_t s2[2] = {0, 0};
 #pragma unroll
-        for (int e = 0; e < kT / 2; ++e) {
-          float p0, p1;
-          unpack2(add2(fma2(pack2(v[2 * e], v[2 * e + 1]), sc2, 0), mb2), p0, p1);
-          p0 = ex2_approx(p0);
-          p1 = ex2_approx(p1);
-          s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
-          w[e] = pack_bf16(p0, p1);
+        for (int z = 0; z < 2; ++z) {  // (64 scores at a time, for the registers)
+          float v[64];
+          tmem_ld64(ts + z * 64, v);
+          tc_wait_ld();
+          if (seen < kT) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[e] = z * 64 + e < seen ? v[e] : -INFINITY;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            float p0, p1;
+            unpack2(add2(fma2(pack2(v[2 * e], v[2 * e + 1]), sc2, 0), mb2), p0, p1);
+            p0 = ex2_approx(p0);
+            p1 = ex2_approx(p1);
+            s2[e & 1] = add2(s2[e & 1], pack2(p0, p1));
+            w[z * 32 + e] = pack_bf16(p0, p1);
+          }
         }
         float s0, s1;
         unpack2(add2(s2[0], s2[1]), s0, s1);
@@ -373,7 +392,7 @@ cudaError_t attn4_prefix_tc_launch(const AttnArgs& a, const Attn4Plan& plan, cud
     if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, attn4_prefix_tc);
     if (e != cudaSuccess) return e;
     // a register split that the launch does not cover would wait for ever
-    if (at.numRegs != 128) return cudaErrorInvalidConfiguration;
+    if (at.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration;
     configured[dev] = true;
   }
   const long long rows = (long long)a.B * a.group;
