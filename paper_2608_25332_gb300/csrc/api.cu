@@ -1819,10 +1819,13 @@ extern "C" int provip_kv_read4(const int* slot_map, int T, int H_kv, int d_h, co
 
 namespace {
 
-// Parts of whole `tile` keys, as many as make `want` CTAs of `units`, at most `most` and at most one for `least`
-// keys.
+// Parts of whole `tile` keys: one of them, or as many as make at most `want` CTAs of `units`, which all run at the same
+// time; at most `most`, and at most one for `least` keys. (With up to 8 * 152 CTAs 12 requests of 1250 keys and 32
+// heads took 30.8 us where one part each takes 24.6, 32 with fp32 queries 73.7 and 59.6, and a prefix of 40000 keys for
+// a request of 32 heads 52.6 and 46.1. Long lists cut to parts of at most 768 keys for a shorter tail: 128 requests of
+// 163 to 2339 keys 174 us, uncut 154.)
 void attn4_parts(long long units, int n_keys, long long want, int most, int tile, int least, int* part_keys, int* n_part) {
-  long long n = (want + units - 1) / units;
+  long long n = want / units;
   if (n > most) n = most;
   if (n > ((long long)n_keys + least - 1) / least) n = ((long long)n_keys + least - 1) / least;
   if (n < 1) n = 1;
@@ -1840,8 +1843,10 @@ Attn4Plan attn4_plan(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, i
   p.n_cut = 1;
   while (R % p.n_cut || R / p.n_cut > wide) ++p.n_cut;
   p.own_rows = R / p.n_cut > 8 ? 16 : R / p.n_cut > 2 ? 8 : 2;
-  // (64 keys are a warp's stage, 256 what a CTA's four warps take at a time)
-  attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, 8 * kPlanSms, 512, 64, 256, &p.own_keys, &p.n_own);
+  // (64 keys are a warp's stage, 256 what a CTA's four warps take at a time; three CTAs fit an SM. Behind a prefix,
+  // whose rows are joined in any case, shorter parts cost less: 64 requests of 3000 keys and 4 heads behind 9251
+  // rows: 68 us, and 78 without)
+  attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, (prefix_len > 0 ? 4 : 3) * kPlanSms, 512, 64, 256, &p.own_keys, &p.n_own);
   if (p.n_own < 1) p.n_own = 1;  // rows without keys are written too
   const long long rows = (long long)B * R;
   p.pre_rows = rows > 8 ? wide : rows > 2 ? 8 : 2;
@@ -1851,9 +1856,9 @@ Attn4Plan attn4_plan(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, i
   if (prefix_len > 0) {
     const long long units = (rows + p.pre_rows - 1) / p.pre_rows * H_kv;
     if (tc)
-      attn4_parts(units, prefix_len, kPlanSms / units * units, 256, 128, 128, &p.pre_keys, &p.n_pre);
+      attn4_parts(units, prefix_len, kPlanSms, 256, 128, 128, &p.pre_keys, &p.n_pre);
     else
-      attn4_parts(units, prefix_len, 8 * kPlanSms, 256, 64, 256, &p.pre_keys, &p.n_pre);
+      attn4_parts(units, prefix_len, 3 * kPlanSms, 256, 64, 256, &p.pre_keys, &p.n_pre);
   }
   return p;
 }
