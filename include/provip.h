@@ -525,7 +525,7 @@ int provip_decode_attention(const void *Q, long long q_stride, int B, int H_q, i
  *   n_rows_or_null [1] int32 (device): rows from there on are left untouched (a
  *   count outside 0..T is reported; negative: none, larger: T).
  *   pos [n_axes, T] int32 (device), axes pos_stride elements apart (the position ids
- *   of a compaction: [P, B, L] with T = B L).
+ *   of a compaction: [P, B, L] with T = B L; 0: one row of ids for every axis).
  *   inv_freq [64] radians a position (host, in [-1e6, 1e6]), axis_or_null [64]
  *   (host): the axis of each pair (NULL: 0). Read during the call.
  *   q_norm_or_null, k_norm_or_null [d_h] dtype (device). */

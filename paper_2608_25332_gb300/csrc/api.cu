@@ -1636,7 +1636,7 @@ int rotate_args(const char* what, RotateArgs& a, const void* Q, long long q_stri
       (rc = inplace_check(what, "K", K, k_stride, k_out, ko_stride)))
     return rc;
   if (!pos || !inv_freq) return fail(PROVIP_ERR_INVALID_ARG, "%s: null positions or frequencies", what);
-  if (n_axes < 1 || n_axes > 255 || (n_axes > 1 && pos_stride < T) || pos_stride < 0)
+  if (n_axes < 1 || n_axes > 255 || (n_axes > 1 && pos_stride != 0 && pos_stride < T) || pos_stride < 0)
     return fail(PROVIP_ERR_INVALID_ARG, "%s: %d axes of positions, %lld apart", what, n_axes, pos_stride);
   if (!isfinite(factor)) return fail(PROVIP_ERR_INVALID_ARG, "%s: factor must be finite", what);
   if ((wq || wk) && !(eps >= 0.f && eps < INFINITY)) return fail(PROVIP_ERR_INVALID_ARG, "%s: eps must not be negative", what);

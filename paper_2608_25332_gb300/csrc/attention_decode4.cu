@@ -1,26 +1,33 @@
 // One token per request against pages of 4 bits.
 //
 // A row of 128 values is d_q (n - 8) with codes n and a scale d_q for each 32 values q (rotate.cu),
-// so with integers c = n - 8, exact in bf16,
+// so with integers c = n - 8, exact in fp16 and in bf16,
 //   score_t = sum_q dk_{t,q} (Q_q . c_{t,q})        o_q = sum_t (p_t dv_{t,q}) c_{t,q}:
 // scales stay outside the first product and go into the weights of the second, and no value is
-// ever rounded to 16 bits. Both products run on mma.sync (m16n8k16, bf16 in, fp32 sums) with the codes
+// ever rounded to 16 bits. Both products run on mma.sync (m16n8k16, fp32 sums) with the codes
 // as the 16-row operand A straight from registers: eight query rows ("columns") are enough to fill
 // it, where a tcgen05 product would want the expanded codes written to shared memory first, four times
-// the bytes that come from HBM, on every one of them.
+// the bytes that come from HBM, for every key. (It pays for a prefix that more than 16 bf16 rows share:
+// attention_decode4_tc.cu. All else is here: own keys, few rows, fp32.)
 //   S[16 keys x 8] = 4 groups x 2 MMAs over the dims, then 4 FMAs a score with dk
 //   O^T[16 dims x 8] += 8 MMAs over 16 keys, with P dv from S's registers by movmatrix (a transpose)
 // The order of the dims in the codes (rotate.cu) is such that a lane's 16 bytes of a key hold whole
-// MMA operands of one group each: shifts and masks, no exchange. A nibble becomes c as bf16 in a mask-or
-// to 128 + n and a subtraction, two at a time.
+// MMA operands of one group each: shifts and masks, no exchange.
 //
 // Work: a CTA of four warps takes a part of one (request, key/value head)'s keys, or of the prefix's for
-// a block of rows of all requests; a warp 32 keys at a time, from a ring of its own that bulk copies
+// a block of rows of all requests; a warp 64 keys at a time, from a ring of its own that bulk copies
 // fill (a page of one head is contiguous), with its own softmax state; the four join in shared memory.
 // Rows of several parts are joined by a second kernel. No maximum is looked for while no score passes
-// the one before by 2^10. Statistics and sums are fp32; P dv is rounded to bf16 (2^-8 of each weight at most;
-// values then add up as integers times weights). For fp32 queries the queries and P dv are split into
-// three bf16 pieces each (24 bits), a product each.
+// the one before by 2^10. Statistics and sums are fp32.
+//
+// Roundings. A query is fp16 after a power of two a row (bf16's eight bits fit), fp32 ones two fp16 pieces
+// (2^-22 of a value at most); P dv is rounded to bf16 (2^-8 of each weight at most, as P is where keys are
+// bf16), for fp32 split into three bf16 pieces (24 bits), a product each.
+//
+// What bounds it: the SMs' issue slots and integer units, which take the codes apart, not HBM. 128 requests of
+// 163 to 2339 keys (32 heads, bf16): 154 us, 4.8 TB/s of codes and scales; 32 of 163 to 1091 (32 heads, fp32): 43 us;
+// one of 211: 9 us, of which the launch and the first loads' way are most. Stages of 32 keys, three stages,
+// eight warps a CTA or more CTAs an SM took as long or longer.
 #include <cuda_fp16.h>
 
 #include "attention.cuh"
@@ -613,7 +620,7 @@ __global__ void __launch_bounds__(kJoinThr) attn4_join(const __grid_constant__ A
   int len = a.k_len[b];
   if (len < 0 || len > a.k_len_max || len > (long long)a.max_pages * a.page_size) len = 0;
   if (a.prefix_len == 0 && len <= plan.own_keys) return;  // written by its only part
-  const int n_own = plan.n_own > 0 ? (len + plan.own_keys - 1) / plan.own_keys : 0;
+  const int n_own = len > 0 ? (len - 1) / plan.own_keys + 1 : 0;
   Joined s = {{0.f, 0.f, 0.f, 0.f}, 0.f, -INFINITY};
   join_parts<24>(
       s, plan.n_pre + n_own, [&](int p) { return a.part_lse[p * n_rows + row]; },

@@ -13,6 +13,12 @@
 // codes give them: queries are staged in that order too, and the output's columns are read in it.
 // The maximum is raised only where a tile's sum passes 2^10, as for bf16 keys (attention_tc.cu).
 //
+// What bounds it: 64 requests of 28 heads over 4 (448 rows a head), 9251 keys, 30 us: 13 of them set-up, first loads
+// and the last tile's way out, the rest 4.0 us for two tiles of rows and 128 keys, of which the MMAs are half (4.1
+// thousand clocks a tile of keys); the softmax and the expansion share the issue slots beside them. On
+// mma.sync the whole call took 76 us with the codes taken apart for every 16 rows, 51 with operands expanded once for
+// 128, and takes 41 here.
+//
 // Roles (640 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
 // K's codes, warps 16-19 V's, a key's row a thread, K for the next tile while the softmax works, V when the product
 // before has read the buffer; the first of each four loads, by bulk copies. Two row tiles share every operand
@@ -251,9 +257,9 @@ __global__ void __launch_bounds__(kThr, 1)
             }
           }
         }
-        if (lead && live) {
-          if (t > 0) tc_commit(&ctl.empty[1]);
-          if (t < nt) tc_commit(&ctl.empty[0]);
+        if (lead && live) {  // (only where a tile follows that waits for it: nothing arrives at the block's end)
+          if (t > 0 && t < nt) tc_commit(&ctl.empty[1]);
+          if (t + 1 < nt) tc_commit(&ctl.empty[0]);
         }
         __syncwarp();
       }

@@ -427,8 +427,8 @@ cudaError_t read4_launch(const Read4Args& a, int dtype, int sms, cudaStream_t s)
 // real one's group cut into n_cut equal ones); the prefix: blocks of packed (request, head) rows.
 struct Attn4Plan {
   int n_cut;                 // virtual heads a key/value head
-  int own_keys, n_own;       // keys of a part, parts at most (own; 0: none)
-  int pre_keys, n_pre;       // the same for the prefix
+  int own_keys, n_own;       // own keys of a part, parts at most (one at least)
+  int pre_keys, n_pre;       // the same for the prefix (0: none)
   int own_rows, pre_rows;    // query rows a CTA: 2, 8 or (bf16) 16; the prefix's (bf16) also 256
   unsigned regs[3];          // constants of the codes' expansion (CodeRegs)
 };

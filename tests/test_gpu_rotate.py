@@ -110,6 +110,15 @@ def test_one_axis_of_many():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_one_row_of_ids_for_every_axis():
+    """text behind a video: the same position on all three axes, as a view without a copy"""
+    Q, K, _, pos, w = inputs(14, 33, 6, 2, torch.bfloat16)
+    a = P.provip_rotate(Q, K, pos.expand(3, 33), rotary(3), *w, EPS)
+    b = P.provip_rotate(Q, K, pos.repeat(3, 1), rotary(3), *w, EPS)
+    c = P.provip_rotate(Q, K, pos, rotary(1), *w, EPS)  # (and with the same frequencies)
+    assert all(torch.equal(x, y) and torch.equal(x, z) for x, y, z in zip(a, b, c))
+
+
 def test_values_that_are_not_finite_stay_in_their_head():
     Q, K, _, pos, w = inputs(7, 4, 6, 2, torch.bfloat16, fused=False)
     Q[1, 2, 5], Q[2, 3, 70], K[3, 1, 0] = float("nan"), float("inf"), -float("inf")
