@@ -18,10 +18,10 @@
 //
 // A warp handles four heads of a row at a time: eight lanes a head, lane l with values 8 l .. + 7 and
 // 64 + 8 l .. + 7, which are pairs. A row's 64 sines are worked out two a lane and passed round. Each value is
-// read and written once; what bounds that beyond a thousand rows is the SMs' issue slots rather than HBM where
-// heads are normed or brought to 4 bits (250 instructions for four heads): 8725 rows of 96 heads into pages in
-// 65 us (6.6 TB/s), 9379 of 32 heads with norms in 31 (5.0), 8725 of 64 heads to 4 bits in 45 (4.1 TB/s). Below
-// that it is the launch.
+// read and written once; what bounds that beyond a thousand rows is the SMs' issue slots and integer units rather than
+// HBM where heads are normed or brought to 4 bits: 9379 rows of 32 heads with norms in 26 us (6.0 TB/s), 8725 of 64 heads
+// to 4 bits in 42 (4.4 TB/s). 8725 rows of 96 heads into pages take 64 us (6.7 TB/s, what HBM gives), 8725 of
+// 64 heads out of 4 bits 31 (5.9). Below that it is the launch.
 #include "common.cuh"
 #include "kernels.h"
 
@@ -29,10 +29,11 @@ namespace provip {
 namespace {
 
 constexpr int kThr = 256;
-// Rotation: rows ahead a warp, bytes of a row's piece at most, blocks an SM (the registers' limit), rows from
-// which pieces are that large. (A video's 9379 rows of 32 heads, normed: pieces of 2 KiB 38 us, 4 KiB 31, 8 KiB 37;
-// three blocks an SM 33; four rows ahead instead of two, no change.)
-constexpr int kRing = 2, kPieceBytes = 4096, kRotateBlocks = 2, kRotateWide = 512;
+// Rotation: rows ahead a warp, bytes of a row's piece at most, blocks an SM (the registers' limit; without rotation
+// three: 700 rows of 64 heads to 4 bits 10 us, with two 12), rows from which pieces are that large. (A video's 9379 rows
+// of 32 heads, normed, blocks shared out evenly: pieces of 2 KiB 38 us, 4 KiB 31, 8 KiB 37; three blocks an SM 33; four
+// rows ahead instead of two, no change.)
+constexpr int kRing = 2, kPieceBytes = 4096, kRotateBlocks = 2, kStoreBlocks = 3, kRotateWide = 512;
 // Reading: blocks, an SM's.
 constexpr int kReadBlocks = 12;
 
@@ -130,23 +131,21 @@ __device__ __forceinline__ float group_scale(const Raw<float>& raw, int k, uint1
   }
   return scale_of(most, top == most, bits);
 }
-// bf16 as 16-bit integers: magnitudes order as unsigned ones (NaN above all), positive values as signed ones above
-// the negative, which is all that is asked of them. Both maxima go round in one word, the signed one shifted to be
-// unsigned.
+// bf16 as 16-bit integers: the largest unsigned one is the negative value of largest magnitude, where there is one,
+// the largest signed one the positive value of largest magnitude, where there is one (NaN above all). Both go round
+// in one word, the signed one shifted to be unsigned.
 __device__ __forceinline__ float group_scale(const Raw<__nv_bfloat16>& raw, int k, uint16_t& bits) {
   const uint32_t w[4] = {raw.u[k].x, raw.u[k].y, raw.u[k].z, raw.u[k].w};
-  uint32_t most = w[0] & 0x7fff7fffu, top = w[0];
-#pragma unroll
-  for (int i = 1; i < 4; ++i) {
-    most = __vmaxu2(most, w[i] & 0x7fff7fffu);
-    top = __vmaxs2(top, w[i]);
-  }
-  most = __vmaxu2(most, most >> 16);
-  top = __vmaxs2(top, __byte_perm(top, top, 0x1032)) ^ 0x80008000u;
-  uint32_t both = __byte_perm(most, top, 0x5410);
+  uint32_t neg = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+  uint32_t pos = __vmaxs2(__vmaxs2(w[0], w[1]), __vmaxs2(w[2], w[3]));
+  neg = __vmaxu2(neg, neg >> 16);
+  pos = __vmaxs2(pos, __byte_perm(pos, pos, 0x1032)) ^ 0x80008000u;
+  uint32_t both = __byte_perm(neg, pos, 0x5410);
   both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 1));
   both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 2));
-  return scale_of(__uint_as_float(both << 16), ((both >> 16) ^ 0x8000u) == (both & 0xffffu), bits);
+  both = __vmaxu2(both, 0x80008000u) & 0x7fff7fffu;  // magnitudes, 0 where there is none of that sign
+  const uint32_t up = both & 0xffff0000u, down = both << 16;
+  return scale_of(__uint_as_float(max(up, down)), up >= down, bits);
 }
 // 1 / d rounded to nearest, for a normal d of eight bits whose reciprocal is normal: a step of Newton's iteration,
 // r + r (1 - d r), on the hardware's approximation (all 256 such fractions give __frcp_rn's result).
@@ -156,19 +155,21 @@ __device__ __forceinline__ float reciprocal(float d) {
   return fmaf(r, fmaf(-d, r, 1.f), r);
 }
 // Codes of eight values: four of them in each half of the result. No quotient is below -8.1, which rounds
-// to -8. A sum with 3 * 2^22 + 8 has a unit of 1, and so the code in its lowest bits, with nothing else below bit 22: multiplied
-// by 1, 16, 256 and 4096 and added up, four of them leave their codes side by side in the lower half.
+// to -8. A sum with 2^23 + 264 has a unit of 1, and so 256 and the code in its lower half, nothing else up to bit 24.
+// Two such sums side by side are cut off at 15 together; the next two, times 16, leave two codes in a byte of each half.
 __device__ __forceinline__ uint32_t group_codes(const float* x, float d) {
+  constexpr uint32_t most = 0x4c0f010fu;
   const float r = d == 0.f ? 0.f : reciprocal(d);
   uint32_t w[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     uint32_t n[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n[i] = __float_as_uint(__fadd_rn(fminf(__fmul_rn(x[4 * k + i], r), 7.f), 12582920.f));
-    w[k] = n[0] + n[1] * 16u + n[2] * 256u + n[3] * 4096u;
+    for (int i = 0; i < 4; ++i) n[i] = __float_as_uint(__fadd_rn(__fmul_rn(x[4 * k + i], r), 8388872.f));
+    // (upper halves: 2^23 as a float is 0x4b00 there, and the lower sum's 0x4b00.... moves out)
+    w[k] = __vminu2(n[0] + n[2] * 65536u, most) + __vminu2(n[1] + n[3] * 65536u, most) * 16u;
   }
-  return __byte_perm(w[0], w[1], 0x5410);
+  return __byte_perm(w[0], w[1], 0x6420);
 }
 
 // A head's row (eight lanes with 16 values each) into its place in 4-bit pages.
@@ -205,30 +206,40 @@ __device__ __forceinline__ size_t place4(long long slot, int h, int H_kv, int pa
   return ((size_t)(page * H_kv + h) << page_shift) * kRow4 + (size_t)row * kCodes4;
 }
 
-// Blocks along y: pieces of up to kPieceBytes of heads, queries', then keys', then values'; along x: rows, a row a
-// warp at a time. A warp keeps what its piece needs of every row (frequencies, axes, norm weights) in registers;
+// What a kind of rows (queries, keys, values) is cut into: pieces of `heads` heads, and blocks that share a piece's rows.
+struct Share {
+  int pieces, blocks;
+};
+struct Shares {
+  Share of[3];
+  int heads;
+};
+
+// Blocks: queries' pieces first, then keys', then values'; a row a warp at a time. A warp keeps what its piece needs of every row (frequencies, axes, norm weights) in registers;
 // the rows' values come through a ring of its own in shared memory, kRing rows ahead, by bulk copies (heads of a
 // row lie next to each other). Waits are bounded; one that gives up sets the error word and ends the warp once
 // its copies are done.
-template <typename T>
-__global__ void __launch_bounds__(kThr, kRotateBlocks) rotate_kernel(const __grid_constant__ RotateArgs a, int heads, int q_items, int k_items) {
+template <typename T, bool kTurn>
+__global__ void __launch_bounds__(kThr, kTurn ? kRotateBlocks : kStoreBlocks) rotate_kernel(const __grid_constant__ RotateArgs a, const __grid_constant__ Shares shares) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kThr / 32][kRing];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane & 7;
   int n = a.T;
   if (a.n_rows) {
     const int m = *a.n_rows;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && (m < 0 || m > a.T)) set_error(a.err, kErrBadDeviceArg);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && (m < 0 || m > a.T)) set_error(a.err, kErrBadDeviceArg);
     n = min(m, a.T);
   }
-  const int step = gridDim.x * (kThr / 32);
-  int t = blockIdx.x * (kThr / 32) + warp;
-  if (t >= n) return;
-  int piece = blockIdx.y;
   // 0: queries, 1: keys, 2: values
-  const int kind = piece < q_items ? 0 : piece < q_items + k_items ? 1 : 2;
-  piece -= kind == 0 ? 0 : kind == 1 ? q_items : q_items + k_items;
-  const int h_lo = piece * heads, n_heads = min(heads, (kind == 0 ? a.H_q : a.H_kv) - h_lo);
+  int block = blockIdx.x;
+  const int q_blocks = shares.of[0].pieces * shares.of[0].blocks, k_blocks = shares.of[1].pieces * shares.of[1].blocks;
+  const int kind = block < q_blocks ? 0 : block < q_blocks + k_blocks ? 1 : 2;
+  block -= kind == 0 ? 0 : kind == 1 ? q_blocks : q_blocks + k_blocks;
+  const int blocks = kind == 0 ? shares.of[0].blocks : kind == 1 ? shares.of[1].blocks : shares.of[2].blocks;
+  const int piece = block / blocks, step = blocks * (kThr / 32);
+  int t = (block - piece * blocks) * (kThr / 32) + warp;
+  if (t >= n) return;
+  const int h_lo = piece * shares.heads, n_heads = min(shares.heads, (kind == 0 ? a.H_q : a.H_kv) - h_lo);
   const long long stride = (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) * (long long)sizeof(T);
   const uint8_t* src = static_cast<const uint8_t*>(kind == 0 ? a.Q : kind == 1 ? a.K : a.V) + (size_t)h_lo * kHeadDim * sizeof(T);
   const uint32_t bytes = n_heads * kHeadDim * (int)sizeof(T);
@@ -250,7 +261,7 @@ __global__ void __launch_bounds__(kThr, kRotateBlocks) rotate_kernel(const __gri
   T* out = kind == 0 ? static_cast<T*>(a.q_out) : kind == 1 ? static_cast<T*>(a.k_out) : nullptr;
   const long long o_stride = kind == 0 ? a.qo_stride : a.ko_stride;
   if (out) out += (size_t)h_lo * kHeadDim;
-  const bool paged = kind != 0 && a.slot_map != nullptr, turn = a.turn && kind != 2;
+  const bool paged = kind != 0 && a.slot_map != nullptr, turn = kTurn && kind != 2;
   void* pages = kind == 1 ? a.k_pages : a.v_pages;
   // pairs 2 lane, 2 lane + 1: this lane's sines and cosines
   unsigned long long turns[2] = {0, 0};
@@ -386,21 +397,38 @@ __global__ void __launch_bounds__(kThr, kRotateBlocks) rotate_kernel(const __gri
 }
 
 // Pieces of 4 KiB (sixteen heads in bf16, eight in fp32) where the rows fill the SMs with them, else of four heads.
-template <typename T>
+// All blocks run at once and go through their piece's rows, so pieces get blocks by what a row of theirs costs, in
+// turns of four heads: the sines and the norm weights are worth two of them, bringing four heads to 4 bits one and a
+// half more, a copy's way through shared memory one. (9379 rows of 28 and 4 heads: rotated 31 us with blocks shared out
+// evenly, 27 so; with values into pages 39 and 33. Values' copies at no cost: 41.)
+template <typename T, bool kTurn>
 cudaError_t rotate_go(const RotateArgs& a, int sms, cudaStream_t s) {
   static std::atomic<bool> configured[64];  // per device, zero-initialised
   constexpr int smem = kThr / 32 * kRing * kPieceBytes;
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev >= 0 && dev < 64 && !configured[dev]) {
-    cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T, kTurn>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  const int heads = a.T >= kRotateWide ? kPieceBytes / (kHeadDim * (int)sizeof(T)) : 4;
-  const int q = a.Q ? (a.H_q + heads - 1) / heads : 0, k = a.K ? (a.H_kv + heads - 1) / heads : 0, v = a.V ? (a.H_kv + heads - 1) / heads : 0;
-  const int all = (a.T + kThr / 32 - 1) / (kThr / 32), most = kRotateBlocks * sms / (q + k + v);
-  rotate_kernel<T><<<dim3((unsigned)min(all, max(most, 1)), q + k + v), kThr, smem, s>>>(a, heads, q, k);
+  Shares n;
+  n.heads = a.T >= kRotateWide ? kPieceBytes / (kHeadDim * (int)sizeof(T)) : 4;
+  const int all = (a.T + kThr / 32 - 1) / (kThr / 32), most = (kTurn ? kRotateBlocks : kStoreBlocks) * sms;
+  long long cost[3], sum = 0;  // of a row, in half turns
+  for (int i = 0; i < 3; ++i) {
+    const int H = (i == 0 ? a.Q : i == 1 ? a.K : a.V) ? (i == 0 ? a.H_q : a.H_kv) : 0;
+    n.of[i].pieces = (H + n.heads - 1) / n.heads;
+    cost[i] = (H + 3) / 4 * (i > 0 && a.four ? 5 : 2) + (kTurn && i < 2 ? 4 : a.four ? 0 : 2) * n.of[i].pieces;
+    sum += cost[i];
+  }
+  int blocks = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (n.of[i].pieces) n.of[i].blocks = (int)min((long long)all, max(cost[i] * most / (sum * n.of[i].pieces), 1ll));
+    else n.of[i].blocks = 0;
+    blocks += n.of[i].pieces * n.of[i].blocks;
+  }
+  rotate_kernel<T, kTurn><<<blocks, kThr, smem, s>>>(a, n);
   return cudaGetLastError();
 }
 
@@ -454,7 +482,8 @@ cudaError_t read4_go(const Read4Args& a, int blocks, cudaStream_t s) {
 }  // namespace
 
 cudaError_t rotate_launch(const RotateArgs& a, int dtype, int sms, cudaStream_t s) {
-  return dtype == 0 ? rotate_go<float>(a, sms, s) : rotate_go<__nv_bfloat16>(a, sms, s);
+  if (a.turn) return dtype == 0 ? rotate_go<float, true>(a, sms, s) : rotate_go<__nv_bfloat16, true>(a, sms, s);
+  return dtype == 0 ? rotate_go<float, false>(a, sms, s) : rotate_go<__nv_bfloat16, false>(a, sms, s);
 }
 
 cudaError_t read4_launch(const Read4Args& a, int dtype, int sms, cudaStream_t s) {
