@@ -13,18 +13,18 @@
 // codes give them: queries are staged in that order too, and the output's columns are read in it.
 // The maximum is raised only where a tile's sum passes 2^10, as for bf16 keys (attention_tc.cu).
 //
-// What bounds it: 64 requests of 28 heads over 4 (448 rows a head), 9251 keys, 30 us: 13 of them set-up, first loads
-// and the last tile's way out, the rest 4.0 us for two tiles of rows and 128 keys, of which the MMAs are half (4.1
-// thousand clocks a tile of keys); the softmax and the expansion share the issue slots beside them. On
-// mma.sync the whole call took 76 us with the codes taken apart for every 16 rows, 51 with operands expanded once for
-// 128, and takes 41 here.
+// What bounds it: 64 requests of 28 heads over 4 (448 rows a head), 9251 keys, 26 us: 15 of them set-up, first loads
+// and the last tile's way out, the rest 2.7 us for two tiles of rows and 128 keys, of which the MMAs are 2.1; the
+// softmax and the expansion share the issue slots beside them. (With the scores of a row tile issued behind its own values'
+// product, before the other tile's, K's operands were waited for: 4.0 us.) On mma.sync the whole call took 76 us with the
+// codes taken apart for every 16 rows, 51 with operands expanded once for 128, and takes 37 here.
 //
 // Roles (640 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
 // K's codes, warps 16-19 V's, a key's row a thread, K for the next tile while the softmax works, V when the product
 // before has read the buffer; the first of each four loads, by bulk copies. Two row tiles share every operand
-// and keep the tensor cores busy for one while the other's softmax runs. Every wait is bounded; one that gives up sets the error word
-// and ends its role, the other roles' waits then run out likewise, and the block ends when what it has issued is
-// done.
+// and keep the tensor cores busy for one while the other's softmax runs. Every wait is bounded; one that gives up
+// sets the error word and ends its role, the other roles' waits then run out likewise, and the block ends when what it
+// has issued is done.
 #include "attention_tc.cuh"
 
 namespace provip {
@@ -228,38 +228,39 @@ __global__ void __launch_bounds__(kThr, 1)
       const bool lead = elect_one();
       const uint64_t qd = smem_desc_sw128(smem_u32(qs)), kd = smem_desc_sw128(smem_u32(kb)), vd = smem_desc_mn_sw128(smem_u32(vb));
       bool live = true;
+      // the values' products of tile t - 1 before the scores of tile t: K's next operands are still being written then
       for (int t = 0; live && t <= nt; ++t) {
-        if (t > 0) live = wait_all(&ctl.full[1], (uint32_t)(t - 1) & 1u, a.err);
-        if (live && t < nt) live = wait_all(&ctl.full[0], (uint32_t)t & 1u, a.err);
-        for (int i = 0; live && i < n_live; ++i) {
-          const uint32_t ts = tmem + i * kT, to = tmem + (2 + i) * kT;
-          if (t > 0) {
+        if (t > 0) {
+          live = wait_all(&ctl.full[1], (uint32_t)(t - 1) & 1u, a.err);
+          for (int i = 0; live && i < n_live; ++i) {
             live = wait_all(&ctl.p_full[i], (uint32_t)(t - 1) & 1u, a.err);
             tc_fence_after();
             if (lead && live) {
 #pragma unroll
               for (int ks = 0; ks < 16; ++ks)  // hi, then lo
-                tc_mma_bf16_ts(to, ts + (ks & 7) * 8, vd + (uint64_t)(((ks >> 3) * kStage + (ks & 7) * 2048) >> 4), kIdescO,
-                               ks > 0 || t > 1 ? 1u : 0u);
+                tc_mma_bf16_ts(tmem + (2 + i) * kT, tmem + i * kT + (ks & 7) * 8,
+                               vd + (uint64_t)(((ks >> 3) * kStage + (ks & 7) * 2048) >> 4), kIdescO, ks > 0 || t > 1 ? 1u : 0u);
               if (t == nt) tc_commit(&ctl.o_full[i]);
             }
           }
-          if (t < nt) {
-            tc_fence_after();
-            if (lead && live) {
+          // (only where a tile follows that waits for it, here and below: nothing arrives at the block's end)
+          if (lead && live && t < nt) tc_commit(&ctl.empty[1]);
+        }
+        if (live && t < nt) {
+          live = wait_all(&ctl.full[0], (uint32_t)t & 1u, a.err);
+          tc_fence_after();
+          if (lead && live) {
+            for (int i = 0; i < n_live; ++i) {
 #pragma unroll
               for (int ks = 0; ks < 16; ++ks) {
                 const uint32_t off = ((ks >> 2) & 1) * kHalf + (ks & 3) * 32;
-                tc_mma_bf16(ts, qd + (uint64_t)((i * kStage + off) >> 4), kd + (uint64_t)(((ks >> 3) * kStage + off) >> 4), kIdescS,
-                            ks > 0 ? 1u : 0u);
+                tc_mma_bf16(tmem + i * kT, qd + (uint64_t)((i * kStage + off) >> 4), kd + (uint64_t)(((ks >> 3) * kStage + off) >> 4),
+                            kIdescS, ks > 0 ? 1u : 0u);
               }
               tc_commit(&ctl.s_full[i]);
             }
+            if (t + 1 < nt) tc_commit(&ctl.empty[0]);
           }
-        }
-        if (lead && live) {  // (only where a tile follows that waits for it: nothing arrives at the block's end)
-          if (t > 0 && t < nt) tc_commit(&ctl.empty[1]);
-          if (t + 1 < nt) tc_commit(&ctl.empty[0]);
         }
         __syncwarp();
       }

@@ -67,7 +67,7 @@ def test_named_barriers_are_met_by_all_of_their_warps():
 def test_commits_are_waited_for():
     """nothing arrives at a barrier of a block that has ended: operands are given back only to a tile that follows"""
     b = body(TC, "attn4_prefix_tc")
-    assert "if (t > 0 && t < nt) tc_commit(&ctl.empty[1]);" in b and "if (t + 1 < nt) tc_commit(&ctl.empty[0]);" in b
+    assert "if (lead && live && t < nt) tc_commit(&ctl.empty[1]);" in b and "if (t + 1 < nt) tc_commit(&ctl.empty[0]);" in b
     assert b.count("tc_commit(&ctl.empty") == 2
 
 
