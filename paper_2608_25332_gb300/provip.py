@@ -770,7 +770,10 @@ class Rotary:
             raise ProvipError(ERR_INVALID_ARG, "Rotary: 64 frequencies and 64 axes from 0 on, one a pair")
         self.n_axes, self.factor = max(axis) + 1, float(factor)
         self.inv_freq, self.axis = (ctypes.c_double * 64)(*freq), (ctypes.c_int * 64)(*axis)
-        self.args = (self.n_axes, ctypes.addressof(self.inv_freq), ctypes.addressof(self.axis), self.factor)
+        self.args = (self.n_axes, self.inv_freq, self.axis, self.factor)
+
+    def __reduce__(self):  # (copies and pickles: with arrays of their own)
+        return Rotary, (list(self.inv_freq), list(self.axis), None, 1.0, self.factor)
 
 
 # (The checks below look at each property of a tensor once, and at its device by number: a property takes
@@ -925,8 +928,6 @@ class DecodeAttention4:
         self.out = torch.empty((B, H_q, 128), dtype=dtype, device=dev)
         self.lse = torch.empty((B, H_q), dtype=torch.float32, device=dev) if want_lse else None
         self.ws = workspace(lib().provip_decode_attention4_workspace_size(*self.shape, self._dt), dev)
-        self._outs = (self.out.data_ptr(), H_q * 128, None if self.lse is None else self.lse.data_ptr(), self.ws.data_ptr(),
-                      self.ws.numel())
 
     def __call__(self, Q, k_pages, v_pages, block_table, kv_len, prefix_table=None):
         """Q [B, H_q, 128]; k_pages, v_pages [n_pages, H_kv, page_size * 72] bytes; block_table
@@ -942,7 +943,8 @@ class DecodeAttention4:
             raise ProvipError(ERR_INVALID_ARG, "decode_attention4: the prefix needs its pages' table")
         _call(dev, "provip_decode_attention4", lib().provip_decode_attention4, q, qs, B, H_q, H_kv, 128, kp, vp, n, ps,
               _index(block_table, 0, dev, "block_table"), table[1], _index(kv_len, B, dev, "kv_len"), km,
-              _index(prefix_table, -(-P // ps), dev, "prefix_table") if P else None, P, self.scale, self._dt, *self._outs)
+              _index(prefix_table, -(-P // ps), dev, "prefix_table") if P else None, P, self.scale, self._dt,
+              self.out.data_ptr(), H_q * 128, None if self.lse is None else self.lse.data_ptr(), self.ws.data_ptr(), self.ws.numel())
         return dict(out=self.out, lse=self.lse)
 
 

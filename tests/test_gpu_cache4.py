@@ -1,4 +1,5 @@
 """Rows in and out of 4-bit pages, and decoding from them, against their definition."""
+import copy
 import math
 import random
 
@@ -449,3 +450,16 @@ def test_a_cache_past_32_bits():
     want = decode(small)
     got = P.provip_decode_attention4(small["Q"], *pools, table, small["kv"], 600)
     assert torch.equal(want["out"], got["out"]) and torch.equal(want["lse"], got["lse"])
+
+
+def test_a_step_copied_or_given_another_output():
+    """outputs and workspace are those that the step has at the call"""
+    c = case(12, [70, 300], 8, 2, 16, 40, torch.bfloat16)
+    want = decode(c)
+    step = P.DecodeAttention4(2, 8, 2, 300, 40, device=DEV)
+    other = copy.deepcopy(step)
+    del step
+    r = other(c["Q"], c["k"], c["v"], c["table"], c["kv"], c["prefix_table"])
+    assert torch.equal(r["out"], want["out"]) and torch.equal(r["lse"], want["lse"])
+    other.out = torch.zeros_like(want["out"])
+    assert torch.equal(other(c["Q"], c["k"], c["v"], c["table"], c["kv"], c["prefix_table"])["out"], want["out"])

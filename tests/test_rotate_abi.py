@@ -1,6 +1,8 @@
 """Refusals of the rotation's and the 4-bit cache's calls (CPU: all of them come before any CUDA call)."""
+import copy
 import ctypes
 import math
+import pickle
 
 import pytest
 import torch
@@ -119,6 +121,9 @@ def test_binding_refusals():
             P.Rotary(**kw)
     r = P.Rotary(sections=(16, 24, 24), base=1e6)
     assert r.n_axes == 3 and list(r.axis) == [0] * 16 + [1] * 24 + [2] * 24 and r.inv_freq[0] == 1.0 and r.inv_freq[32] == 1e6 ** -0.5
+    for c in (copy.copy(r), copy.deepcopy(r), pickle.loads(pickle.dumps(r))):  # of their own: the first may be gone
+        assert c.args[1] is c.inv_freq is not r.inv_freq and c.args[2] is c.axis and (c.n_axes, c.factor) == (r.n_axes, r.factor)
+        assert list(c.inv_freq) == list(r.inv_freq) and list(c.axis) == list(r.axis)
     assert P.pages4(3, 16, 2, "cpu").shape == (3, 2, 16 * 72)
     t, i = torch.zeros(4, 2, 128), torch.zeros(1, 4, dtype=torch.int32)
     pool = P.pages4(3, 16, 2, "cpu")
