@@ -463,3 +463,22 @@ def test_a_step_copied_or_given_another_output():
     assert torch.equal(r["out"], want["out"]) and torch.equal(r["lse"], want["lse"])
     other.out = torch.zeros_like(want["out"])
     assert torch.equal(other(c["Q"], c["k"], c["v"], c["table"], c["kv"], c["prefix_table"])["out"], want["out"])
+
+
+@pytest.mark.parametrize("B,H_q,H_kv,most", [(15, 32, 32, 900), (33, 16, 16, 300), (130, 4, 4, 40), (512, 1, 1, 17), (513, 1, 1, 17), (129, 37, 1, 9)])
+def test_more_units_than_run_at_once(B, H_q, H_kv, most):
+    """requests of all lengths in any order, none and the longest among them, and one out of range"""
+    rng = random.Random(B)
+    lens = [rng.randint(0, most) for _ in range(B)]
+    lens[B // 2], lens[B // 3], lens[0], lens[-1] = most, 0, most // 2, most
+    c = case(B, lens, H_q, H_kv, 8)
+    r = decode(c)
+    check(c, r, rows=rng.sample(range(B), min(B, 30)) + [0, B // 3, B // 2, B - 1])
+    for bad in (-1, most + 1, 2 ** 31 - 1, -2 ** 31):
+        kv = c["kv"].clone()
+        kv[3] = bad
+        again = P.provip_decode_attention4(c["Q"], c["k"], c["v"], c["table"], kv, most)
+        assert P.provip_device_status(clear=True)[1] == P.DEVSTAT_BAD_ARG
+        assert not again["out"][3].any() and (again["lse"][3] == -math.inf).all()
+        rest = [b for b in range(B) if b != 3]
+        assert torch.equal(again["out"][rest], r["out"][rest]) and torch.equal(again["lse"][rest], r["lse"][rest])
