@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
   __shared__ float s_m[kWarps][C], s_l[kWarps][C];
-  __shared__ __align__(16) uint32_t s_q[NT][kQ][4][32][4];
+  __shared__ __align__(16) uint32_t s_q[kSplit ? 1 : NT][kQ][kSplit ? 1 : 4][32][4];
   __shared__ float s_most[4][C];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
   const bool first = threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0;
@@ -237,21 +237,53 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
     }
   }
 
-  // Queries: column g's dims 32 q + 8 j .. + 7, as B operands in fp16: times a power of two that brings
+  // Queries: dims 8 j .. + 7 of a column's groups, as B operands in fp16: times a power of two that brings
   // the column's largest into [2^14, 2^15), so that nothing is lost but what is below 2^-39 of that. The
-  // scale of a column's scores makes up for it. Warp q works out group q for all.
+  // scale of a column's scores makes up for it.
+  // Of a lane's 16 bytes of codes a word holds four values of two groups, side by side. Columns of one group each take
+  // the words as they are: a pair of values meets a query and a zero. For columns of all groups the words' halves are put
+  // together by group, and warp q works out group q's queries for all.
   uint32_t qf[NT][kQ][4][4];
   float cs[NT][kH];
-  {
+  // 2^(14 - exponent), and its reciprocal (exponents from -100 on: smaller queries need no more)
+  auto up = [](float most) { return 14 + 127 - max((int)(__float_as_uint(most) >> 23), 27); };
+  auto pow2 = [](int e) { return __uint_as_float((uint32_t)(127 + e) << 23); };
+  if constexpr (kSplit) {
+    const int q = g & 3;  // column g's group
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float x[8], most = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      const Column c = column<kPrefix>(a, R, unit, block, nt * kHeads + (g >> 2));
+      if (c.h >= 0) load8(static_cast<const T*>(a.Q) + (size_t)c.b * a.q_stride + (size_t)c.h * kHeadDim + 32 * q + 8 * j, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+#pragma unroll
+      for (int b = 1; b < 16; b <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, b));
+      const float mul = pow2(up(most));
+      uint32_t r[4][kQ];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) split2_f16<kQ>(x[t] * mul, x[t + 4] * mul, r[t]);
+#pragma unroll
+      for (int p = 0; p < kQ; ++p)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t v = w < 2 ? r[t][p] & 0xffffu : r[t][p] >> 16;
+            qf[nt][p][w][t] = (w & 1) != (q >> 1) ? 0u : q & 1 ? v << 16 : v;
+          }
+      cs[nt][0] = pow2(-up(__shfl_sync(0xffffffffu, most, (j >> 1) * 16))) * a.scale_log2;
+    }
+  } else {
     float x[NT][8];
-    const bool mine = !kSplit || (g & 3) == warp;  // column g has this group
-    const int g_head = kSplit ? g >> 2 : g;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[nt][e] = 0.f;
-      const Column c = column<kPrefix>(a, R, unit, block, nt * kHeads + g_head);
-      if (c.h >= 0 && mine)
+      const Column c = column<kPrefix>(a, R, unit, block, nt * kHeads + g);
+      if (c.h >= 0)
         load8(static_cast<const T*>(a.Q) + (size_t)c.b * a.q_stride + (size_t)c.h * kHeadDim + 32 * warp + 8 * j, x[nt]);
     }
 #pragma unroll
@@ -261,17 +293,13 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
       for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[nt][e]));
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      if (j == 0 && mine) s_most[warp][nt * kHeads + g_head] = most;
+      if (j == 0) s_most[warp][nt * kHeads + g] = most;
     }
     __syncthreads();
-    // 2^(14 - exponent), and its reciprocal (exponents from -100 on: smaller queries need no more)
-    auto up = [&](int c) {
-      const float most = fmaxf(fmaxf(s_most[0][c], s_most[1][c]), fmaxf(s_most[2][c], s_most[3][c]));
-      return 14 + 127 - max((int)(__float_as_uint(most) >> 23), 27);
-    };
+    auto most_of = [&](int c) { return fmaxf(fmaxf(s_most[0][c], s_most[1][c]), fmaxf(s_most[2][c], s_most[3][c])); };
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const float mul = __uint_as_float((uint32_t)(127 + up(nt * kHeads + g_head)) << 23);
+      const float mul = pow2(up(most_of(nt * kHeads + g)));
       uint32_t r[4][kQ];
 #pragma unroll
       for (int t = 0; t < 4; ++t) split2_f16<kQ>(x[nt][t] * mul, x[nt][t + 4] * mul, r[t]);
@@ -279,8 +307,7 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
       for (int p = 0; p < kQ; ++p)
         *reinterpret_cast<uint4*>(s_q[nt][p][warp][lane]) = make_uint4(r[0][p], r[1][p], r[2][p], r[3][p]);
 #pragma unroll
-      for (int c = 0; c < kH; ++c)
-        cs[nt][c] = __uint_as_float((uint32_t)(127 - up(nt * kHeads + (kSplit ? j >> 1 : 2 * j + c))) << 23) * a.scale_log2;
+      for (int c = 0; c < kH; ++c) cs[nt][c] = pow2(-up(most_of(nt * kHeads + 2 * j + c))) * a.scale_log2;
     }
     __syncthreads();
 #pragma unroll
@@ -344,9 +371,15 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
       float x[NT][4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
-        const uint32_t xa = q < 2 ? __byte_perm(wa.x, wa.z, sel) : __byte_perm(wa.y, wa.w, sel);
-        const uint32_t xb = q < 2 ? __byte_perm(wb.x, wb.z, sel) : __byte_perm(wb.y, wb.w, sel);
+        uint32_t xa, xb;  // a word (columns of a group each), or a group's halves of two
+        if (kSplit) {
+          xa = q == 0 ? wa.x : q == 1 ? wa.y : q == 2 ? wa.z : wa.w;
+          xb = q == 0 ? wb.x : q == 1 ? wb.y : q == 2 ? wb.z : wb.w;
+        } else {
+          const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
+          xa = q < 2 ? __byte_perm(wa.x, wa.z, sel) : __byte_perm(wa.y, wa.w, sel);
+          xb = q < 2 ? __byte_perm(wb.x, wb.z, sel) : __byte_perm(wb.y, wb.w, sel);
+        }
         uint32_t ca[4], cb[4];
         codes_f16(xa, regs, ca);
         codes_f16(xb, regs, cb);
