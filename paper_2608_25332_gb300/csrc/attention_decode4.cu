@@ -25,9 +25,10 @@
 // bf16), for fp32 split into three bf16 pieces (24 bits), a product each.
 //
 // What bounds it: the SMs' issue slots and integer units, which take the codes apart, not HBM. 128 requests of
-// 163 to 2339 keys (32 heads, bf16): 154 us, 4.8 TB/s of codes and scales; 32 of 163 to 1091 (32 heads, fp32): 43 us;
+// 163 to 2339 keys (32 heads, bf16): 145 us, 5.1 TB/s of codes and scales; 32 of 163 to 1091 (32 heads, fp32): 39 us;
 // one of 211: 9 us, of which the launch and the first loads' way are most. Stages of 32 keys, three stages,
-// eight warps a CTA or more CTAs an SM took as long or longer.
+// eight warps a CTA or more CTAs an SM took as long or longer; so did requests taken longest first, the first pages
+// asked for beside the length, and scores summed in two chains.
 #include <cuda_fp16.h>
 
 #include "attention.cuh"
@@ -150,13 +151,16 @@ __device__ __forceinline__ Column column(const AttnArgs& a, int R, int unit, int
 // dims from sums of their own. Two: four columns each, one a group (its queries are zero outside the group),
 // so that one sum over all dims leaves the groups' scores side by side, and the second product's columns carry a
 // weight for each group: a fifth of the instructions about scores and weights less where a head is alone
-// (or two are), and most of the columns are empty otherwise.
+// (or two are), and most of the columns are empty otherwise. A word of codes, which holds two groups' values side by side,
+// is an operand as it is then, in both products: a pair meets a column's query or weight and a zero (128 requests:
+// 154 -> 145 us with that). fp32 at three CTAs an SM: 64 requests of 1250 keys 108 -> 100 us.
 template <typename T, int NT, int kHeads, bool kPrefix>
-__global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
+__global__ void __launch_bounds__(kThr, NT > 1 || (sizeof(T) == 4 && kHeads == 8) ? 2 : 3)
     attn4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Attn4Plan plan) {
   constexpr bool kSplit = kHeads == 2;
   constexpr int kE = kSplit ? 2 : 4;          // scores a lane and tile: its rows, by its columns' heads
   constexpr int kH = kSplit ? 1 : 2;          // heads of a lane's columns
+  constexpr int kG = kSplit ? 2 : 4;          // sums a column: by word of the codes, or by group
   constexpr int kQ = sizeof(T) == 4 ? 2 : 1;  // fp16 pieces of a query
   constexpr int kP = sizeof(T) == 4 ? 3 : 1;  // bf16 pieces of a weight
   constexpr int C = kHeads * NT;
@@ -325,7 +329,7 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
   }
 
   const CodeRegs regs = {plan.regs[0], plan.regs[1], plan.regs[2]};
-  float o[4][2][NT][4], m[NT][kH], base[NT][kH], l[NT][kH];  // base: the maximum, 0 for none
+  float o[kG][2][NT][4], m[NT][kH], base[NT][kH], l[NT][kH];  // base: the maximum, 0 for none
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -334,7 +338,7 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
       base[nt][c] = l[nt][c] = 0.f;
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < kG; ++q)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -368,7 +372,7 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
         da = *reinterpret_cast<const uint2*>(ks + r0 * 8);
         db = *reinterpret_cast<const uint2*>(ks + r1 * 8);
       }
-      float x[NT][4];
+      float x[NT][4], y[NT][4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         uint32_t xa, xb;  // a word (columns of a group each), or a group's halves of two
@@ -387,13 +391,18 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
         const float fa = q & 1 ? hi_f(ua) : lo_f(ua), fb = q & 1 ? hi_f(ub) : lo_f(ub);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          // (a lone head's smaller pieces have a sum of their own: MMAs' sums truncate, at the size of what they hold)
+          float* const lo = kSplit && kQ > 1 ? y[nt] : x[nt];
           if (!kSplit || q == 0)
-            mma16<true, true>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][kQ - 1][q][0], qf[nt][kQ - 1][q][1]);
+            mma16<true, true>(lo, ca[0], cb[0], ca[1], cb[1], qf[nt][kQ - 1][q][0], qf[nt][kQ - 1][q][1]);
           else
-            mma16<true, false>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][kQ - 1][q][0], qf[nt][kQ - 1][q][1]);
-          mma16<true, false>(x[nt], ca[2], cb[2], ca[3], cb[3], qf[nt][kQ - 1][q][2], qf[nt][kQ - 1][q][3]);
+            mma16<true, false>(lo, ca[0], cb[0], ca[1], cb[1], qf[nt][kQ - 1][q][0], qf[nt][kQ - 1][q][1]);
+          mma16<true, false>(lo, ca[2], cb[2], ca[3], cb[3], qf[nt][kQ - 1][q][2], qf[nt][kQ - 1][q][3]);
           if (kQ > 1) {
-            mma16<true, false>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][0][q][0], qf[nt][0][q][1]);
+            if (kSplit && q == 0)
+              mma16<true, true>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][0][q][0], qf[nt][0][q][1]);
+            else
+              mma16<true, false>(x[nt], ca[0], cb[0], ca[1], cb[1], qf[nt][0][q][0], qf[nt][0][q][1]);
             mma16<true, false>(x[nt], ca[2], cb[2], ca[3], cb[3], qf[nt][0][q][2], qf[nt][0][q][3]);
           }
           if constexpr (!kSplit) {
@@ -414,6 +423,10 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
       if constexpr (kSplit) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          if (kQ > 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[nt][e] += y[nt][e];
+          }
           const float ra = fmaf(x[nt][0], lo_f(da.x), x[nt][1] * hi_f(da.x)), rb = fmaf(x[nt][2], lo_f(db.x), x[nt][3] * hi_f(db.x));
           s[mt][nt][0] = ra + __shfl_xor_sync(0xffffffffu, ra, 1);  // (the same bits in both lanes)
           s[mt][nt][1] = rb + __shfl_xor_sync(0xffffffffu, rb, 1);
@@ -462,7 +475,7 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
           base[nt][c] = x == -INFINITY ? 0.f : x;
           l[nt][c] *= f;
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < kG; ++q)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -480,11 +493,11 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
           s[mt][nt][e] = p;
           l[nt][e % kH] += p;
         }
-    // (fp32: a step's sums start from zero and are added in fp32, as the MMAs' own sums truncate)
-    float add[kP > 1 ? 4 : 1][2][NT][4];
+    // (fp32: sums of 64 keys, or of 32 with twice the MMAs, start from zero and are added in fp32, as MMAs' sums truncate)
+    float add[kP > 1 ? kG : 1][2][NT][4];
     if (kP > 1) {
 #pragma unroll
-      for (int i = 0; i < 4 * 2 * NT * 4; ++i) (&add[0][0][0][0])[i] = 0.f;
+      for (int i = 0; i < kG * 2 * NT * 4; ++i) (&add[0][0][0][0])[i] = 0.f;
     }
 #pragma unroll
     for (int mt = 0; mt < kTiles; ++mt) {
@@ -502,54 +515,78 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
         if (r0 >= left) da = make_uint2(0u, 0u);
         if (r0 + 8 >= left) db = make_uint2(0u, 0u);
       }
-      uint32_t b0[NT][kP], b1[NT][kP];
-      if constexpr (kSplit) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          split2<kP>(s[mt][nt][0] * lo_f(da.x), s[mt][nt][0] * hi_f(da.x), b0[nt]);
-          split2<kP>(s[mt][nt][1] * lo_f(db.x), s[mt][nt][1] * hi_f(db.x), b1[nt]);
-#pragma unroll
-          for (int p = 0; p < kP; ++p) {
-            b0[nt][p] = transpose8x8(b0[nt][p]);
-            b1[nt][p] = transpose8x8(b1[nt][p]);
-          }
-        }
-      }
       uint2 v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2*>(vc + (k0 + (i >> 1) * 8 + (i & 1)) * kCodes4 + 8 * g);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
-        const uint32_t ya = q < 2 ? __byte_perm(v[0].x, v[1].x, sel) : __byte_perm(v[0].y, v[1].y, sel);
-        const uint32_t yb = q < 2 ? __byte_perm(v[2].x, v[3].x, sel) : __byte_perm(v[2].y, v[3].y, sel);
-        uint32_t ca[4], cb[4];
-        codes_bf16(ya, regs, ca);
-        codes_bf16(yb, regs, cb);
-        const uint32_t ua = q < 2 ? da.x : da.y, ub = q < 2 ? db.x : db.y;
-        const float fa = q & 1 ? hi_f(ua) : lo_f(ua), fb = q & 1 ? hi_f(ub) : lo_f(ub);
+      if constexpr (kSplit) {
+        // a word holds two groups' values of a key: operands of eight keys twice, whose columns of the one
+        // group have zeros against the other's (sums of the other word's columns mean nothing)
+        uint32_t b[NT][2][2][kP];  // of eight keys; keys 2 j, 2 j + 1
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          if constexpr (!kSplit) {
-            split2<kP>(s[mt][nt][0] * fa, s[mt][nt][1] * fa, b0[nt]);
-            split2<kP>(s[mt][nt][2] * fb, s[mt][nt][3] * fb, b1[nt]);
+          uint32_t w[2][kP];
+          split2<kP>(s[mt][nt][0] * lo_f(da.x), s[mt][nt][0] * hi_f(da.x), w[0]);
+          split2<kP>(s[mt][nt][1] * lo_f(db.x), s[mt][nt][1] * hi_f(db.x), w[1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int p = 0; p < kP; ++p) {
-              b0[nt][p] = transpose8x8(b0[nt][p]);
-              b1[nt][p] = transpose8x8(b1[nt][p]);
+              const uint32_t t = transpose8x8(w[i][p]);
+              b[nt][i][0][p] = __byte_perm(t, 0u, g & 1 ? 0x1044 : 0x4410);
+              b[nt][i][1][p] = __byte_perm(t, 0u, g & 1 ? 0x3244 : 0x4432);
             }
-          }
+        }
 #pragma unroll
-          for (int p = kP - 1; p >= 0; --p) {
-            mma16<false, false>(kP > 1 ? add[q][0][nt] : o[q][0][nt], ca[0], ca[1], cb[0], cb[1], b0[nt][p], b1[nt][p]);
-            mma16<false, false>(kP > 1 ? add[q][1][nt] : o[q][1][nt], ca[2], ca[3], cb[2], cb[3], b0[nt][p], b1[nt][p]);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint32_t ca[4], cb[4];
+            codes_bf16(q ? v[2 * i].y : v[2 * i].x, regs, ca);
+            codes_bf16(q ? v[2 * i + 1].y : v[2 * i + 1].x, regs, cb);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int p = kP - 1; p >= 0; --p) {
+                mma16<false, false>(kP > 1 ? add[q][0][nt] : o[q][0][nt], ca[0], ca[1], cb[0], cb[1], b[nt][i][0][p], b[nt][i][1][p]);
+                mma16<false, false>(kP > 1 ? add[q][1][nt] : o[q][1][nt], ca[2], ca[3], cb[2], cb[3], b[nt][i][0][p], b[nt][i][1][p]);
+              }
+          }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t sel = q & 1 ? 0x7632 : 0x5410;
+          const uint32_t ya = q < 2 ? __byte_perm(v[0].x, v[1].x, sel) : __byte_perm(v[0].y, v[1].y, sel);
+          const uint32_t yb = q < 2 ? __byte_perm(v[2].x, v[3].x, sel) : __byte_perm(v[2].y, v[3].y, sel);
+          uint32_t ca[4], cb[4];
+          codes_bf16(ya, regs, ca);
+          codes_bf16(yb, regs, cb);
+          const uint32_t ua = q < 2 ? da.x : da.y, ub = q < 2 ? db.x : db.y;
+          const float fa = q & 1 ? hi_f(ua) : lo_f(ua), fb = q & 1 ? hi_f(ub) : lo_f(ub);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            uint32_t b0[kP], b1[kP];
+            split2<kP>(s[mt][nt][0] * fa, s[mt][nt][1] * fa, b0);
+            split2<kP>(s[mt][nt][2] * fb, s[mt][nt][3] * fb, b1);
+#pragma unroll
+            for (int p = 0; p < kP; ++p) {
+              b0[p] = transpose8x8(b0[p]);
+              b1[p] = transpose8x8(b1[p]);
+            }
+#pragma unroll
+            for (int p = kP - 1; p >= 0; --p) {
+              mma16<false, false>(kP > 1 ? add[q][0][nt] : o[q][0][nt], ca[0], ca[1], cb[0], cb[1], b0[p], b1[p]);
+              mma16<false, false>(kP > 1 ? add[q][1][nt] : o[q][1][nt], ca[2], ca[3], cb[2], cb[3], b0[p], b1[p]);
+            }
           }
         }
       }
-    }
-    if (kP > 1) {
+      if (kP > 1 && (mt == kTiles - 1 || (kSplit && (mt & 1)))) {
 #pragma unroll
-      for (int i = 0; i < 4 * 2 * NT * 4; ++i) (&o[0][0][0][0])[i] += (&add[0][0][0][0])[i];
+        for (int i = 0; i < kG * 2 * NT * 4; ++i) {
+          (&o[0][0][0][0])[i] += (&add[0][0][0][0])[i];
+          (&add[0][0][0][0])[i] = 0.f;
+        }
+      }
     }
     __syncwarp();  // every lane has read the stage
     const int next = step + kStages * kWarps;
@@ -591,8 +628,8 @@ __global__ void __launch_bounds__(kThr, sizeof(T) == 4 || NT > 1 ? 2 : 3)
       if constexpr (kSplit) {  // column 2 j + c has the sums of group 2 (j & 1) + c alone
         const bool up = j & 1;
         *reinterpret_cast<float4*>(to + 32 * c + (up ? 64 : 0)) =
-            make_float4(up ? o[2 + c][0][nt][c] : o[c][0][nt][c], up ? o[2 + c][0][nt][c + 2] : o[c][0][nt][c + 2],
-                        up ? o[2 + c][1][nt][c] : o[c][1][nt][c], up ? o[2 + c][1][nt][c + 2] : o[c][1][nt][c + 2]);
+            make_float4(up ? o[1][0][nt][c] : o[0][0][nt][c], up ? o[1][0][nt][c + 2] : o[0][0][nt][c + 2],
+                        up ? o[1][1][nt][c] : o[0][1][nt][c], up ? o[1][1][nt][c + 2] : o[0][1][nt][c + 2]);
       } else {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
