@@ -13,11 +13,12 @@
 // codes give them: queries are staged in that order too, and the output's columns are read in it.
 // The maximum is raised only where a tile's sum passes 2^10, as for bf16 keys (attention_tc.cu).
 //
-// What bounds it: 64 requests of 28 heads over 4 (448 rows a head), 9251 keys, 26 us: 15 of them set-up, first loads
+// What bounds it: 64 requests of 28 heads over 4 (448 rows a head), 9251 keys, 23 us: 12 of them set-up, first loads
 // and the last tile's way out, the rest 2.7 us for two tiles of rows and 128 keys, of which the MMAs are 2.1; the
-// softmax and the expansion share the issue slots beside them. (With the scores of a row tile issued behind its own values'
-// product, before the other tile's, K's operands were waited for: 4.0 us.) On mma.sync the whole call took 76 us with the
-// codes taken apart for every 16 rows, 51 with operands expanded once for 128, and takes 37 here.
+// softmax and the expansion share the issue slots beside them. (With the scores of a row tile issued behind its own
+// values' product, before the other tile's, K's operands were waited for: 4.0 us a tile; with a thread storing its row
+// by itself, 26 in all; queries staged by half a warp a row, no change.) On mma.sync the whole call took 76 us with
+// the codes taken apart for every 16 rows, 51 with operands expanded once for 128, and takes 35 here.
 //
 // Roles (640 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
 // K's codes, warps 16-19 V's, a key's row a thread, K for the next tile while the softmax works, V when the product
@@ -361,21 +362,33 @@ __global__ void __launch_bounds__(kThr, 1)
     if (!live) ctl.fail = 1;
     if (live && qi < n_live) {
       tc_fence_after();
-      const size_t row = ((size_t)part * a.B + b) * a.H_q + h;
+      // this thread's row of the parts (~0: none)
+      const unsigned long long row = row_live ? ((size_t)part * a.B + b) * a.H_q + h : ~0ull;
       // (every score -inf: no weight)
       const float inv = l == 0.f ? 0.f : 1.f / l;
+      // 64 columns of the warp's 32 rows at a time go through shared memory, where this tile's queries have been
+      // read for the last time, so that half a warp stores a row's 256 bytes side by side
+      float4* st = reinterpret_cast<float4*>(qs + qi * kStage) + (warp & 3) * 512;
 #pragma unroll 1
-      for (int z = 0; z < kHeadDim; z += 32) {
-        float o[32];
-        tmem_ld32(to + z, o);
-        tc_wait_ld();
-        if (row_live) {
+      for (int z = 0; z < kHeadDim; z += 64) {
+#pragma unroll
+        for (int y = 0; y < 64; y += 32) {
+          float o[32];
+          tmem_ld32(to + z + y, o);
+          tc_wait_ld();
 #pragma unroll
           for (int e = 0; e < 32; e += 8) {
-            float4* dst = reinterpret_cast<float4*>(a.part_o + row * kHeadDim + z + e);
-            dst[0] = make_float4(o[e] * inv, o[e + 2] * inv, o[e + 4] * inv, o[e + 6] * inv);
-            dst[1] = make_float4(o[e + 1] * inv, o[e + 3] * inv, o[e + 5] * inv, o[e + 7] * inv);
+            const int c = (y + e) / 4;
+            st[lane * 16 + (c ^ (lane & 7))] = make_float4(o[e] * inv, o[e + 2] * inv, o[e + 4] * inv, o[e + 6] * inv);
+            st[lane * 16 + ((c + 1) ^ (lane & 7))] = make_float4(o[e + 1] * inv, o[e + 3] * inv, o[e + 5] * inv, o[e + 7] * inv);
           }
+        }
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < 32; i += 2) {
+          const int at = i + (lane >> 4), c = lane & 15;
+          const unsigned long long to_row = __shfl_sync(0xffffffffu, row, at);
+          if (to_row != ~0ull) *reinterpret_cast<float4*>(a.part_o + to_row * kHeadDim + z + c * 4) = st[at * 16 + (c ^ (at & 7))];
         }
         __syncwarp();
       }
