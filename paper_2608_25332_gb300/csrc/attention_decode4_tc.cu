@@ -11,7 +11,8 @@
 //   O += P V_hi + P V_lo       16 MMAs, P from tensor memory
 // lose nothing but P's rounding. The eight elements of a 16-byte chunk lie in the order 0 4 1 5 2 6 3 7, as the
 // codes give them: queries are staged in that order too, and the output's columns are read in it.
-// The maximum is raised only where a tile's sum passes 2^10, as for bf16 keys (attention_tc.cu).
+// The maximum is raised only where a tile's sum passes 2^10, or where a row has none yet (every score so far -inf),
+// as for bf16 keys (attention_tc.cu).
 //
 // What bounds it: 64 requests of 28 heads over 4 (448 rows a head), 9251 keys, 23 us: 12 of them set-up, first loads
 // and the last tile's way out, the rest 2.7 us for two tiles of rows and 128 keys, of which the MMAs are 2.1; the
@@ -288,9 +289,10 @@ __global__ void __launch_bounds__(kThr, 1)
       const int seen = n_keys - t * kT;
       float sum;
       uint32_t w[kT / 2];
-      // as for bf16 keys: P against the maximum so far, which is raised where the tile's sum is too large
+      // as for bf16 keys: P against the maximum so far, which is raised where the tile's sum is too large, and looked
+      // for where a row has none (the first tile's; later ones' where all scores before were -inf)
 #pragma unroll 1
-      for (bool raise = t == 0, raised = false;;) {
+      for (bool raise = __any_sync(0xffffffffu, row_live && m == -INFINITY), raised = false;;) {
         if (raise) {
           raised = true;
           float mx = -INFINITY;
