@@ -566,9 +566,10 @@ int provip_kv_read4(const int *slot_map, int T, int H_kv, int d_h, const void *k
                     long long k_stride, void *v_out, long long v_stride, void *stream);
 
 /* provip_decode_attention over pages of 4 bits: the values that codes and scales
- * stand for are multiplied unrounded; Q and out have dtype. Queries' magnitudes stay below
- * 2^100 (larger ones may give infinities or NaN); a row whose scores are finite and
- * whose keys' groups are all finite is finite. Everything else as there. */
+ * stand for are multiplied unrounded; Q and out have dtype. Queries' magnitudes, and those
+ * times the scale, stay below 2^100 (larger ones may give infinities or NaN), and of a
+ * query row what lies below 2^-39 of its largest value may count as zero; a row whose
+ * scores are finite and whose keys' groups are all finite is finite. Everything else as there. */
 size_t provip_decode_attention4_workspace_size(int B, int H_q, int H_kv, int kv_len_max,
                                                int prefix_len, int dtype);
 int provip_decode_attention4(const void *Q, long long q_stride, int B, int H_q, int H_kv, int d_h,

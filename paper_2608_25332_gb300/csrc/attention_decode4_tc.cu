@@ -9,7 +9,8 @@
 //   S = Q K_hi^T + Q K_lo^T    16 MMAs (M = N = 128, K = 16), S in tensor memory
 //   P = 2^(s - m)              a thread per row, to bf16 over S's own columns
 //   O += P V_hi + P V_lo       16 MMAs, P from tensor memory
-// lose nothing but P's rounding. The eight elements of a 16-byte chunk lie in the order 0 4 1 5 2 6 3 7, as the
+// lose nothing but P's rounding. (Queries of 2^20 and more go in with a power of two of their row, so that S stays a
+// float whatever the scales.) The eight elements of a 16-byte chunk lie in the order 0 4 1 5 2 6 3 7, as the
 // codes give them: queries are staged in that order too, and the output's columns are read in it.
 // The maximum is raised only where a tile's sum passes 2^10, or where a row has none yet (every score so far -inf),
 // as for bf16 keys (attention_tc.cu).
@@ -182,15 +183,34 @@ __global__ void __launch_bounds__(kThr, 1)
     b = (int)(row / (unsigned)R);
     h = kv_head * R + (int)(row - (unsigned)b * (unsigned)R);
   }
+  float sc = a.scale_log2;
   if (warp < kSoftWarps) {
     const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + (size_t)b * a.q_stride + (size_t)h * kHeadDim);
+    auto stage = [&](int ch, uint4 x) {
+      const uint4 y = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                                 __byte_perm(x.y, x.w, 0x7632));
+      *reinterpret_cast<uint4*>(qs + qi * kStage + (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = y;
+    };
+    uint32_t most = 0;  // largest magnitude, as bits, in each half
 #pragma unroll 4
     for (int ch = 0; ch < 16; ++ch) {
       uint4 x = make_uint4(0u, 0u, 0u, 0u);
       if (row_live) x = __ldg(src + ch);
-      const uint4 y = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
-                                 __byte_perm(x.y, x.w, 0x7632));
-      *reinterpret_cast<uint4*>(qs + qi * kStage + (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = y;
+      stage(ch, x);
+      most = __vmaxu2(most, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+    }
+    // 128 products of less than 2^20 and 2^100 sum up to a float. A row with larger queries is staged again, times a
+    // power of two (exact but for what then lies below 2^-133), which its scores' scale makes up for.
+    const int over = (int)(max(most & 0xffffu, most >> 16) >> 7) - (127 + 19);
+    if (over > 0) {
+      const __nv_bfloat162 down = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((127 - over) << 7)));
+      auto times = [&](uint32_t w) { return as_word(__hmul2(as_bf16(w), down)); };
+#pragma unroll 1
+      for (int ch = 0; ch < 16; ++ch) {
+        const uint4 x = __ldg(src + ch);
+        stage(ch, make_uint4(times(x.x), times(x.y), times(x.z), times(x.w)));
+      }
+      sc *= __uint_as_float((uint32_t)(127 + over) << 23);
     }
     fence_proxy_async_smem();
   }
@@ -279,7 +299,6 @@ __global__ void __launch_bounds__(kThr, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     // ---- softmax: a thread per row ----
     const uint32_t ts = tmem + qi * kT + ((uint32_t)((warp & 3) * 32) << 16), to = ts + 2 * kT;
-    const float sc = a.scale_log2;
     float m = -INFINITY, l = 0.f;
     bool live = true;
     for (int t = 0; live && t < nt && qi < n_live; ++t) {

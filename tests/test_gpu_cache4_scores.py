@@ -1,10 +1,11 @@
-"""Decoding from 4-bit pages where scores leave the range of a float: keys out of sight at a list's front."""
+"""Decoding from 4-bit pages where scores leave the range of a float: keys out of sight at a list's front, and
+products of queries and keys that pass the largest float before the scale brings them back."""
 import pytest
 import torch
 
 import cache4_ref as ref
 from paper_2608_25332_gb300 import provip as P
-from test_gpu_cache4 import _lib, case, decode, rows_of  # noqa: F401 (_lib: this module's fixture too)
+from test_gpu_cache4 import _lib, case, check, decode, rows_of  # noqa: F401 (_lib: this module's fixture too)
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -64,3 +65,35 @@ def test_keys_out_of_sight_at_the_front(dtype, B, H_q, H_kv, hidden, level):
             got, gl = r["out"][b, h].double(), r["lse"][b, h].double()
             assert ((got - o).abs() <= bo).all(), (b, h)
             assert abs(float(gl - lse)) <= bl, (b, h)
+
+
+@pytest.mark.parametrize("dtype,lens", [(torch.bfloat16, [5] * 12), (torch.bfloat16, [40]), (torch.float32, [5] * 12)])
+def test_products_past_the_largest_float(dtype, lens):
+    """queries around 2^56 and keys around 2^70, whose products' sums pass 2^128, under a scale of 2^-122"""
+    c = case(31, lens, 28, 4, PAGE, 300, dtype, spread=2.0 ** 70)
+    c["Q"] *= 2.0 ** 56
+    scale = 2.0 ** -122
+    r = decode(c, scale=scale)
+    for b in (0, len(lens) - 1):
+        K, V = rows_of(c, b)
+        for h in range(28):
+            o, lse, bo, bl = ref.attend(c["Q"][b, h], K[:, h // 7], V[:, h // 7], scale, dtype)
+            # Scores lie hundreds apart, and a weight below 2^-126 of the largest is no normal float: it may be zero,
+            # by the exponential, by the factor of a raised maximum, and by that of the join. Here values are
+            # around 2^70, so that is not below the bound's own 1e-30.
+            bo = bo + 3 * 2.0 ** -126 * V[:, h // 7].abs().sum(0)
+            got, gl = r["out"][b, h].double(), r["lse"][b, h].double()
+            assert ((got - o).abs() <= bo).all(), (b, h)
+            assert abs(float(gl - lse)) <= bl, (b, h)
+
+
+def test_a_large_query_beside_small_ones():
+    """rows of very different size in one call: each as it is by itself"""
+    c = case(32, [5] * 12, 28, 4, PAGE, 300, torch.bfloat16)
+    sizes = torch.tensor([1.0, 2.0 ** 18, 2.0 ** 19, 2.0 ** 20, 2.0 ** 21, 2.0 ** 60, 2.0 ** 90, 2.0 ** -90, 0.0, 2.0 ** -20, 1.5, 2.0 ** 33])
+    for scale in (2.0 ** -21, 2.0 ** -40):
+        for b, s in enumerate(sizes.tolist()):
+            alone = dict(c, Q=c["Q"][b:b + 1] * s, table=c["table"][b:b + 1], kv=c["kv"][b:b + 1], lens=c["lens"][:1])
+            check(alone, decode(alone, scale=scale), scale)
+        all_of = dict(c, Q=(c["Q"].float() * sizes.to(DEV)[:, None, None]).to(torch.bfloat16))
+        check(all_of, decode(all_of, scale=scale), scale)
