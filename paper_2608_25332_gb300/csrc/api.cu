@@ -15,6 +15,7 @@
 #include "../../include/provip.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "turns.h"
 
 using namespace provip;
 
@@ -1608,16 +1609,6 @@ int inplace_check(const char* what, const char* name, const void* in, long long 
   if (in == out && in_stride != out_stride)
     return fail(PROVIP_ERR_INVALID_ARG, "%s: %s in place with another row stride", what, name);
   return PROVIP_OK;
-}
-
-// turns a position as a fraction of 2^64, from radians a position: f / (2 pi) with a product in two
-// doubles (1 / (2 pi) as two as well), of which only the fraction counts at whole positions
-unsigned long long turns_of(double f) {
-  const double hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
-  const double t = f * hi, rest = fma(f, hi, -t) + f * lo;
-  double frac = t - floor(t);  // exact below 1
-  if (frac >= 1.) frac = 0.;
-  return (unsigned long long)(frac * 0x1p64) + (unsigned long long)(long long)(rest * 0x1p64);
 }
 
 // what the rotating calls check alike, and their arguments
