@@ -45,6 +45,7 @@ class QuestionCache:
     def __init__(self, layers, B, H_q, H_kv, page_size, n_pages, max_len, dtype=torch.bfloat16, device="cuda",
                  max_new=None, algo=P.ALGO_AUTO, bits=16, rotary=None, norms=None, eps=1e-6):
         dev = torch.device(device)
+        P._dtype_of(dtype)  # (refused here, not by the first append)
         if bits not in (4, 16):
             raise P.ProvipError(P.ERR_INVALID_ARG, f"QuestionCache: pages of {bits} bits")
         if norms is not None and (rotary is None or len(norms) != layers):
@@ -90,8 +91,11 @@ class QuestionCache:
         need, pages = -(-n // self.page_size), self.free.numel()
         if need > pages:
             raise P.ProvipError(P.ERR_INVALID_ARG, f"set_prefix: {n} rows take {need} pages, the pool has {pages}")
-        # prompts read rows of their own, not the caller's, which the next pruning may overwrite (4 bits: from pages)
-        prefix = [tuple(x if self.bits == 4 else x.clone(memory_format=torch.contiguous_format) for x in kv) for kv in zip(K, V)]
+        # prompts read rows of their own, not the caller's, which the next pruning may overwrite (4 bits: from pages). All
+        # that may be refused or lack memory comes before any page changes hands
+        prefix = [tuple(x if self.bits == 4 and self._packed(x) else x.clone(memory_format=torch.contiguous_format) for x in kv)
+                  for kv in zip(K, V)]
+        read = tuple(torch.zeros(n, self.H_kv, 128, dtype=self.dtype, device=self.device) for _ in range(2)) if self.bits == 4 else ()
         # two requests of the tables: the prefix before, which ends, and this one. (-1: no page.
         # Where the questions hold too many, the prefix gets none and decoding reports it)
         before = 0 if self.prefix_table is None else self.prefix_table.numel()
@@ -106,11 +110,9 @@ class QuestionCache:
         for (kp, vp), (k, v) in zip(self.pools, prefix):
             (P.provip_kv_append4 if self.bits == 4 else P.provip_kv_append)(k, v, plan["slot_map"], kp, vp)
         self._drop(self.prefix_table, self._prompt, self._decode, *(x for kv in self.prefix for x in kv), *self._read)
-        read = ()
         if self.bits == 4:
             # prompts read the rows back from the pages, one layer's at a time (a row without a slot is reported there)
-            slots = torch.where(plan["slot_map"] < 0, 2 ** 31 - 1, plan["slot_map"])
-            read = (*(torch.zeros(n, self.H_kv, 128, dtype=self.dtype, device=self.device) for _ in range(2)), slots)
+            read = (*read, torch.where(plan["slot_map"] < 0, 2 ** 31 - 1, plan["slot_map"]))
             prefix = []
         self.prefix, self.prefix_len, self.prefix_table, self._read = prefix, n, table[1, :need], read
         self._prompt = self._decode = None
@@ -176,6 +178,14 @@ class QuestionCache:
         Q, _ = self._append(layer, Q, K, V, self._once("slots", self._token_slots), pos, self.B, False)
         n = self._once("lengths", lambda: torch.where(self.new_len > 1, -1, self.kv_len))  # -1: reported
         return self._decode(Q, kp, vp, self.tables, n, self.prefix_table if self.prefix_len else None)["out"]
+
+    @staticmethod
+    def _packed(x):
+        """whether rows [n, H, 128] lie as the 4-bit append takes them: a row's heads side by side, at 16 bytes"""
+        n, H, _ = x.shape
+        s0, s1, s2 = x.stride()
+        return s2 == 1 and (H == 1 or s1 == 128) and x.data_ptr() % 16 == 0 and \
+            (n <= 1 or (s0 >= H * 128 and s0 * x.element_size() % 16 == 0))
 
     @staticmethod
     def _check_rows(what, n, *tensors):
