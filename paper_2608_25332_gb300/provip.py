@@ -781,6 +781,13 @@ class Rotary:
 _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
+def _three(what, *tensors):
+    """rows [T, H, 128] (or pages of three or four dimensions), whose first two sizes are looked at"""
+    for t in tensors:
+        if t.dim() < 3:
+            raise ProvipError(ERR_INVALID_ARG, f"{what}: rows must be [T, H, 128], pages three- or four-dimensional: got {list(t.shape)}")
+
+
 def _heads(t, T, H, dtype, dev, what):
     """pointer and row stride (elements) of rows [T, H, 128] as _rows takes them, on device number dev"""
     if t.dtype is not dtype or t.get_device() != dev or dev < 0 or t.shape != (T, H, 128):
@@ -830,7 +837,8 @@ def _call(dev, what, call, *args):
 
 def _rotate_args(Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out):
     """the arguments that the rotating calls share: inputs, what goes by positions, outputs, their device"""
-    dtype, dev, (T, H_q, _), H = Q.dtype, Q.get_device(), Q.shape, K.shape[1]
+    _three("rotate", Q, K)
+    dtype, dev, T, H_q, H = Q.dtype, Q.get_device(), Q.shape[0], Q.shape[1], K.shape[1]
     q, qs = _heads(Q, T, H_q, dtype, dev, "Q")
     k, ks = _heads(K, T, H, dtype, dev, "K")
     qo, qos = _heads(q_out, T, H_q, dtype, dev, "q_out")
@@ -881,7 +889,7 @@ def provip_rotate_append(Q, K, V, pos, rotary, slot_map, k_pages, v_pages, q_nor
         kp, vp, n, ps = _pages4(k_pages, v_pages, H, dev)
     else:
         kp, vp = _pages(k_pages, dtype, "k_pages"), _pages(v_pages, dtype, "v_pages")
-        n, ps = k_pages.shape[:2]
+        n, ps = k_pages.shape[:2]  # (four dimensions: checked there)
         if k_pages.shape[2:] != (H, 128) or v_pages.shape != k_pages.shape or k_pages.get_device() != dev or v_pages.get_device() != dev:
             raise ProvipError(ERR_INVALID_ARG, f"rotate_append: pages must be [n_pages, page_size, {H}, 128] on GPU {dev}")
     _call(dev, "provip_rotate_append", lib().provip_rotate_append, *ins, v, vs, T, *by, *outs, _index(slot_map, T, dev, "slot_map"), n,
@@ -892,7 +900,8 @@ def provip_rotate_append(Q, K, V, pos, rotary, slot_map, k_pages, v_pages, q_nor
 def provip_kv_append4(K, V, slot_map, k_pages, v_pages):
     """Rows of K and V [T, H_kv, 128] into the slots slot_map [T] of 4-bit pages (uint8, see pages4);
     negative slots are skipped."""
-    (T, H, _), dtype, dev = K.shape, K.dtype, K.get_device()
+    _three("kv_append4", K)
+    T, H, dtype, dev = K.shape[0], K.shape[1], K.dtype, K.get_device()
     k, ks = _heads(K, T, H, dtype, dev, "K")
     v, vs = _heads(V, T, H, dtype, dev, "V")
     kp, vp, n, ps = _pages4(k_pages, v_pages, H, dev)
@@ -903,6 +912,7 @@ def provip_kv_append4(K, V, slot_map, k_pages, v_pages):
 def provip_kv_read4(slot_map, k_pages, v_pages, dtype=torch.bfloat16, out=None):
     """What the rows at the slots slot_map [T] of 4-bit pages stand for: K and V [T, H_kv, 128]. out: (K, V)
     to write, whose type counts then; rows of a negative slot are left untouched (zeros, unless out is given)."""
+    _three("kv_read4", k_pages)
     T, H, dev = slot_map.numel(), k_pages.shape[1], k_pages.get_device()
     if out is None:
         out = tuple(torch.zeros(T, H, 128, dtype=dtype, device=k_pages.device) for _ in range(2))
@@ -951,5 +961,6 @@ class DecodeAttention4:
 def provip_decode_attention4(Q, k_pages, v_pages, block_table, kv_len, kv_len_max, prefix_table=None, prefix_len=0,
                              scale=None, want_lse=True):
     """One call of DecodeAttention4, its outputs and workspace allocated here."""
+    _three("decode_attention4", Q, k_pages)
     step = DecodeAttention4(Q.shape[0], Q.shape[1], k_pages.shape[1], kv_len_max, prefix_len, scale, Q.dtype, Q.device, want_lse)
     return step(Q, k_pages, v_pages, block_table, kv_len, prefix_table)
