@@ -756,7 +756,8 @@ class Rotary:
     position (default base^(-i/64)), axis, the axis of position ids that each pair turns with
     (default: the first), or sections, the numbers of pairs that turn with each axis in order
     (such as (16, 24, 24) for time, height and width), and factor, by which rotated queries and
-    keys are multiplied. Held on the host: one object serves every device and stream."""
+    keys are multiplied. Held on the host: one object serves every device and stream. Its values stay as
+    they are made (calls, and graphs of them, hold what they were given): another plan is another object."""
 
     def __init__(self, inv_freq=None, axis=None, sections=None, base=10000.0, factor=1.0):
         freq = [float(base) ** (-i / 64) for i in range(64)] if inv_freq is None else \
@@ -768,9 +769,11 @@ class Rotary:
         axis = [0] * 64 if axis is None else [int(a) for a in (axis.tolist() if hasattr(axis, "tolist") else axis)]
         if len(freq) != 64 or len(axis) != 64 or min(axis) < 0:
             raise ProvipError(ERR_INVALID_ARG, "Rotary: 64 frequencies and 64 axes from 0 on, one a pair")
-        self.n_axes, self.factor = max(axis) + 1, float(factor)
-        self.inv_freq, self.axis = (ctypes.c_double * 64)(*freq), (ctypes.c_int * 64)(*axis)
-        self.args = (self.n_axes, self.inv_freq, self.axis, self.factor)
+        n_axes, factor, inv_freq, axis = max(axis) + 1, float(factor), (ctypes.c_double * 64)(*freq), (ctypes.c_int * 64)(*axis)
+        self.__dict__.update(n_axes=n_axes, factor=factor, inv_freq=inv_freq, axis=axis, args=(n_axes, inv_freq, axis, factor))
+
+    def __setattr__(self, name, value):
+        raise ProvipError(ERR_INVALID_ARG, f"Rotary: {name} is set when it is made")
 
     def __reduce__(self):  # (copies and pickles: with arrays of their own)
         return Rotary, (list(self.inv_freq), list(self.axis), None, 1.0, self.factor)

@@ -62,3 +62,12 @@ def test_position_ids():
         with pytest.raises(P.ProvipError):
             P._positions(t, 4, 1, -1)  # (the device's number of a CPU tensor)
     assert P._positions(IDS[None], 4, 1, -1)[0] == IDS.data_ptr()
+
+
+def test_a_plan_stays_as_it_is_made():
+    """an attribute set afterwards would change nothing of the calls: it is refused"""
+    r = P.Rotary(factor=0.5)
+    for name, value in (("factor", 2.0), ("n_axes", 3), ("inv_freq", [1.0] * 64), ("axis", [0] * 64), ("args", ()), ("scale", 1.0)):
+        with pytest.raises(P.ProvipError):
+            setattr(r, name, value)
+    assert r.factor == 0.5 and r.args == (1, r.inv_freq, r.axis, 0.5)
