@@ -51,6 +51,7 @@ struct Ctl {
   uint64_t mma_done;               // (drain)
   uint32_t tmem;
   volatile int fail;
+  float scale[2 * kT];             // of a row's scores (kept here over the roles' split: in registers it cost 0.5 us)
 };
 
 __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, unsigned* err) {
@@ -183,8 +184,8 @@ __global__ void __launch_bounds__(kThr, 1)
     b = (int)(row / (unsigned)R);
     h = kv_head * R + (int)(row - (unsigned)b * (unsigned)R);
   }
-  float sc = a.scale_log2;
   if (warp < kSoftWarps) {
+    float sc = a.scale_log2;
     const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + (size_t)b * a.q_stride + (size_t)h * kHeadDim);
     auto stage = [&](int ch, uint4 x) {
       const uint4 y = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
@@ -212,6 +213,7 @@ __global__ void __launch_bounds__(kThr, 1)
       }
       sc *= __uint_as_float((uint32_t)(127 + over) << 23);
     }
+    ctl.scale[qi * kT + r] = sc;
     fence_proxy_async_smem();
   }
   tc_fence_before();
@@ -299,6 +301,7 @@ __global__ void __launch_bounds__(kThr, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     // ---- softmax: a thread per row ----
     const uint32_t ts = tmem + qi * kT + ((uint32_t)((warp & 3) * 32) << 16), to = ts + 2 * kT;
+    const float sc = ctl.scale[qi * kT + r];
     float m = -INFINITY, l = 0.f;
     bool live = true;
     for (int t = 0; live && t < nt && qi < n_live; ++t) {
