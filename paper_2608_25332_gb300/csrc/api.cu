@@ -1810,11 +1810,11 @@ extern "C" int provip_kv_read4(const int* slot_map, int T, int H_kv, int d_h, co
 
 namespace {
 
-// Parts of whole `tile` keys: one of them, or as many as make at most `want` CTAs of `units`, which all run at the same
-// time; at most `most`, and at most one for `least` keys. (With up to 8 * 152 CTAs 12 requests of 1250 keys and 32
-// heads took 30.8 us where one part each takes 24.6, 32 with fp32 queries 73.7 and 59.6, and a prefix of 40000 keys for
-// a request of 32 heads 52.6 and 46.1. Long lists cut to parts of at most 768 keys for a shorter tail: 128 requests of
-// 163 to 2339 keys 174 us, uncut 154.)
+// Parts of whole `tile` keys: one of them, or as many as make at most `want` CTAs of `units`; at most `most`, and at
+// most one for `least` keys. (With up to 8 * 152 CTAs instead of three an SM, in a graph: 12 requests of 1250 keys and 32
+// heads 20.9 us for 16.7, 64 with fp32 queries and 28 heads over 4 34.0 for 20.5, a prefix of 40000 keys for a request of
+// 32 heads 45.7 for 39.5; 32 requests of 163 to 1091 keys and 32 heads, fp32, 36 either way. In an earlier build long
+// lists cut to parts of at most 768 keys for a shorter tail: 128 requests of 163 to 2339 keys 174 us, uncut 154.)
 void attn4_parts(long long units, int n_keys, long long want, int most, int tile, int least, int* part_keys, int* n_part) {
   long long n = want / units;
   if (n > most) n = most;
@@ -1834,14 +1834,20 @@ Attn4Plan attn4_plan(int B, int H_q, int H_kv, int kv_len_max, int prefix_len, i
   p.n_cut = 1;
   while (R % p.n_cut || R / p.n_cut > wide) ++p.n_cut;
   p.own_rows = R / p.n_cut > 8 ? 16 : R / p.n_cut > 2 ? 8 : 2;
-  // (64 keys are a warp's stage, 256 what a CTA's four warps take at a time; three CTAs fit an SM. Behind a prefix,
-  // whose rows are joined in any case, shorter parts cost less: 64 requests of 3000 keys and 4 heads behind 9251
-  // rows: 68 us, and 78 without)
+  // (64 keys are a warp's stage, 256 what a CTA's four warps take at a time. Three CTAs fit an SM where a head is alone or
+  // bf16 rows fill eight columns; sixteen columns, and eight of fp32, fit two: there a third of the CTAs runs behind the
+  // others. Behind a prefix, whose rows are joined in any case, shorter parts cost less: 64 requests of 3000 keys and 28
+  // heads over 4 behind 9251 rows 62.5 us, with three CTAs an SM 67.8, with eight 59.0)
   attn4_parts((long long)B * H_kv * p.n_cut, kv_len_max, (prefix_len > 0 ? 4 : 3) * kPlanSms, 512, 64, 256, &p.own_keys, &p.n_own);
   if (p.n_own < 1) p.n_own = 1;  // rows without keys are written too
   const long long rows = (long long)B * R;
   p.pre_rows = rows > 8 ? wide : rows > 2 ? 8 : 2;
-  // many rows of bf16 queries: blocks of two tiles of 128, a CTA an SM
+  // Many rows of bf16 queries: blocks of two tiles of 128, a CTA an SM. (A whole call with 64 own keys a request in this
+  // form, and in the other one, us. 4 key/value heads, 17 rows: 12.0, 9.2 behind 35 keys, 12.6, 9.9 behind 2339, 17.9, 14.2
+  // behind 9251; 64 rows: 12.6, 9.7, then 13.1, 13.0, then 19.1, 23.3; 448 rows: 16.3, 14.0, then 22.0, 27.8, then 30.0,
+  // 63.1. 32 of them, 17 rows: 13.0, 11.4, then 23.5, 23.9, then 52.1, 44.7; 128 rows: 38.9, 40.9, then 50.2, 62.2, then
+  // 77.4, 127. So it costs 2 to 3 us where rows are few or the prefix is short, up to 7 for 17 rows of 32 heads behind a
+  // long one, and saves 3 to 50 where both are large.)
   const bool tc = dtype == PROVIP_BF16 && rows > 16;
   if (tc) p.pre_rows = 256;
   if (prefix_len > 0) {

@@ -178,8 +178,8 @@ __device__ __noinline__ float attn_element_again(const AttnArgs& a, int b, int h
 
 // Weighs n more parts of a row and adds them to s (by one warp): lse(p) in base 2 and 128 floats at part(p).
 // A round's loads are all under way before the first is used. The weights carry a factor of 2^-10:
-// a row has fewer than 2^10 parts (128 shared out, or 64 and the pieces of 304 spans), so they add up
-// to less than one and no sum of parts passes the largest float where their mean does not.
+// a row has fewer than 2^10 parts (128 shared out, or 64 and the pieces of 304 spans; over 4-bit pages a
+// prefix's 256 and 512), so they add up to less than one and no sum of parts passes the largest float where their mean does not.
 constexpr float kJoinUnit = 1.f / 1024.f;
 struct Joined {
   float o[4], w, m;  // weighted sum of lane's elements, sum of the weights 2^(lse - m) kJoinUnit

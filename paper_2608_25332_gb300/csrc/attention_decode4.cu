@@ -24,9 +24,12 @@
 // (2^-22 of a value at most); P dv is rounded to bf16 (2^-8 of each weight at most, as P is where keys are
 // bf16), for fp32 split into three bf16 pieces (24 bits), a product each.
 //
-// What bounds it: the SMs' issue slots and integer units, which take the codes apart, not HBM. 128 requests of
-// 163 to 2339 keys (32 heads, bf16): 145 us, 5.1 TB/s of codes and scales; 32 of 163 to 1091 (32 heads, fp32): 39 us;
-// one of 211: 9 us, of which the launch and the first loads' way are most. Stages of 32 keys, three stages,
+// What bounds it: no unit by itself. A lone head's kernel issues 2.3 of 4 instructions a clock (most of them take the codes
+// apart), the integer units are busy for 56%, the tensor cores for 26 (fp32 48), HBM for 66: with twelve warps an SM it
+// waits for its own chains of expansion, products and weights, and a CTA takes a whole list, so that the last ones
+// leave SMs idle. 128 requests of 163 to 2339 keys (32 heads, bf16): 145 us, 5.1 TB/s of codes and scales; 32 of 163 to
+// 1091 (32 heads, fp32): 39 us; one of 211: 9 us, of which the launch and the first loads' way are most; 64 of 3000 with 28
+// heads over 4: 32 us, 3.5 TB/s. Stages of 32 keys, three stages,
 // eight warps a CTA or more CTAs an SM took as long or longer; so did requests taken longest first, the first pages
 // asked for beside the length, and scores summed in two chains.
 #include <cuda_fp16.h>
@@ -94,7 +97,8 @@ __device__ __forceinline__ void codes_f16(uint32_t x, const CodeRegs& k, uint32_
   }
 }
 // The same as pairs of bf16, whose seven bits want each nibble at bit 0 (128 + n): three shifts. (Shifts by the
-// upper halves of products, to spare the integer pipe, took 94.9 us where these take 88.7.)
+// upper halves of products, to spare the integer pipe, took 94.9 us where these took 88.7, in an earlier build: 64 requests
+// of 1250 keys, 32 heads, 71 now.)
 __device__ __forceinline__ void codes_bf16(uint32_t x, const CodeRegs& k, uint32_t* c) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) {

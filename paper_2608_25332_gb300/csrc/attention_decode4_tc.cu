@@ -20,7 +20,8 @@
 // softmax and the expansion share the issue slots beside them. (With the scores of a row tile issued behind its own
 // values' product, before the other tile's, K's operands were waited for: 4.0 us a tile; with a thread storing its row
 // by itself, 26 in all; queries staged by half a warp a row, no change.) On mma.sync the whole call took 76 us with
-// the codes taken apart for every 16 rows, 51 with operands expanded once for 128, and takes 35 here.
+// the codes taken apart for every 16 rows, 51 with operands expanded once for 128, and takes 35 here (31 in a graph). What
+// the registers do not hold is 48 bytes a thread in places (416 instructions a CTA go there, of tens of thousands).
 //
 // Roles (640 threads): warps 0-7 softmax, a tile of rows to each four; warp 8 issues the MMAs; warps 12-15 expand
 // K's codes, warps 16-19 V's, a key's row a thread, K for the next tile while the softmax works, V when the product

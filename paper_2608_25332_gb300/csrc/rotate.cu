@@ -19,9 +19,9 @@
 // A warp handles four heads of a row at a time: eight lanes a head, lane l with values 8 l .. + 7 and
 // 64 + 8 l .. + 7, which are pairs. A row's 64 sines are worked out two a lane and passed round. Each value is
 // read and written once; what bounds that beyond a thousand rows is the SMs' issue slots and integer units rather than
-// HBM where heads are normed or brought to 4 bits: 9379 rows of 32 heads with norms in 26 us (6.0 TB/s), 8725 of 64 heads
-// to 4 bits in 39 (4.7 TB/s). 8725 rows of 96 heads into pages take 64 us (6.7 TB/s, what HBM gives), 8725 of
-// 64 heads out of 4 bits 31 (5.9). Below that it is the launch.
+// HBM where heads are normed or brought to 4 bits. In a graph over inputs in turn: 9379 rows of 32 heads with norms 27 us
+// (5.7 TB/s), 8725 of 64 heads to 4 bits 38 (4.8). 8725 rows of 96 heads into pages take 72 us (5.9 TB/s; 66 alone, with
+// nothing of a pass before to be written back), 8725 of 64 heads out of 4 bits 33 (5.5). Below that it is the launch.
 #include "common.cuh"
 #include "kernels.h"
 
