@@ -569,7 +569,8 @@ int provip_kv_read4(const int *slot_map, int T, int H_kv, int d_h, const void *k
  * stand for are multiplied unrounded; Q and out have dtype. Queries' magnitudes, and those
  * times the scale, stay below 2^100 (larger ones may give infinities or NaN), and of a
  * query row what lies below 2^-39 of its largest value may count as zero; a row whose
- * scores are finite and whose keys' groups are all finite is finite. Everything else as there. */
+ * scores stay below 2^127 and whose keys' groups are all finite is finite (scores are taken
+ * times log2 e). Everything else as there. */
 size_t provip_decode_attention4_workspace_size(int B, int H_q, int H_kv, int kv_len_max,
                                                int prefix_len, int dtype);
 int provip_decode_attention4(const void *Q, long long q_stride, int B, int H_q, int H_kv, int d_h,
