@@ -567,8 +567,8 @@ int provip_kv_read4(const int *slot_map, int T, int H_kv, int d_h, const void *k
 
 /* provip_decode_attention over pages of 4 bits: the values that codes and scales
  * stand for are multiplied unrounded; Q and out have dtype. Queries' magnitudes, and those
- * times the scale, stay below 2^100 (larger ones may give infinities or NaN), and of a
- * query row what lies below 2^-39 of its largest value may count as zero; a row whose
+ * times the scale, stay below 2^100 (larger ones may give infinities or NaN), and each
+ * query is taken to 2^-39 of its row's largest (a smaller one may count as zero); a row whose
  * scores stay below 2^127 and whose keys' groups are all finite is finite (scores are taken
  * times log2 e). Everything else as there. */
 size_t provip_decode_attention4_workspace_size(int B, int H_q, int H_kv, int kv_len_max,

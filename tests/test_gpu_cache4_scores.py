@@ -97,3 +97,25 @@ def test_a_large_query_beside_small_ones():
             check(alone, decode(alone, scale=scale), scale)
         all_of = dict(c, Q=(c["Q"].float() * sizes.to(DEV)[:, None, None]).to(torch.bfloat16))
         check(all_of, decode(all_of, scale=scale), scale)
+
+
+@pytest.mark.parametrize("dtype,lens", [(torch.bfloat16, [5] * 12), (torch.bfloat16, [300]), (torch.float32, [5] * 12), (torch.float32, [300])])
+@pytest.mark.parametrize("large", [2.0 ** 12, 2.0 ** 25])
+def test_a_query_value_far_above_the_others(dtype, lens, large):
+    """one that meets zeros in every key: scores are the others', each taken to 2^-39 of it"""
+    c = case(33, lens, 28, 4, PAGE, 200, dtype)
+    first_value(c["k"], torch.cat([prefix_slots(c), own_slots(c)]), 0.0)
+    c["Q"][:, :, 5] = large
+    scale = 1 / 11.3
+    r = decode(c, scale=scale)
+    for b in (0, len(lens) - 1):
+        K, V = rows_of(c, b)
+        for h in range(0, 28, 3):
+            k, v = K[:, h // 7], V[:, h // 7]
+            o, lse, bo, bl = ref.attend(c["Q"][b, h], k, v, scale, dtype)
+            # a score is off by that much of each key's magnitudes more; it moves the output by twice as much of the mean of |v|
+            e = float(k.abs().sum(1).max()) * scale * large * 2.0 ** -39
+            p = torch.softmax(k @ c["Q"][b, h].double() * scale, 0)
+            got, gl = r["out"][b, h].double(), r["lse"][b, h].double()
+            assert ((got - o).abs() <= bo + 2 * e * (p @ v.abs())).all(), (b, h)
+            assert abs(float(gl - lse)) <= bl + e, (b, h)
