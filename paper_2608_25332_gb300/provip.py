@@ -784,11 +784,10 @@ class Rotary:
 _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _three(what, *tensors):
-    """rows [T, H, 128] (or pages of three or four dimensions), whose first two sizes are looked at"""
-    for t in tensors:
-        if t.dim() < 3:
-            raise ProvipError(ERR_INVALID_ARG, f"{what}: rows must be [T, H, 128], pages three- or four-dimensional: got {list(t.shape)}")
+def _dims(what, *tensors):
+    """the refusal of tensors whose sizes could not even be taken apart (the others are refused one by one)"""
+    return ProvipError(ERR_INVALID_ARG, f"{what}: rows must be [T, H, 128], pages three- or four-dimensional: got " +
+                       " and ".join(str(list(t.shape)) for t in tensors))
 
 
 def _heads(t, T, H, dtype, dev, what):
@@ -840,8 +839,10 @@ def _call(dev, what, call, *args):
 
 def _rotate_args(Q, K, pos, rotary, q_norm, k_norm, eps, n_rows, q_out, k_out):
     """the arguments that the rotating calls share: inputs, what goes by positions, outputs, their device"""
-    _three("rotate", Q, K)
-    dtype, dev, T, H_q, H = Q.dtype, Q.get_device(), Q.shape[0], Q.shape[1], K.shape[1]
+    try:
+        dtype, dev, (T, H_q, _), H = Q.dtype, Q.get_device(), Q.shape, K.shape[1]
+    except (ValueError, IndexError):
+        raise _dims("rotate", Q, K) from None
     q, qs = _heads(Q, T, H_q, dtype, dev, "Q")
     k, ks = _heads(K, T, H, dtype, dev, "K")
     qo, qos = _heads(q_out, T, H_q, dtype, dev, "q_out")
@@ -903,8 +904,10 @@ def provip_rotate_append(Q, K, V, pos, rotary, slot_map, k_pages, v_pages, q_nor
 def provip_kv_append4(K, V, slot_map, k_pages, v_pages):
     """Rows of K and V [T, H_kv, 128] into the slots slot_map [T] of 4-bit pages (uint8, see pages4);
     negative slots are skipped."""
-    _three("kv_append4", K)
-    T, H, dtype, dev = K.shape[0], K.shape[1], K.dtype, K.get_device()
+    try:
+        (T, H, _), dtype, dev = K.shape, K.dtype, K.get_device()
+    except ValueError:
+        raise _dims("kv_append4", K) from None
     k, ks = _heads(K, T, H, dtype, dev, "K")
     v, vs = _heads(V, T, H, dtype, dev, "V")
     kp, vp, n, ps = _pages4(k_pages, v_pages, H, dev)
@@ -915,7 +918,8 @@ def provip_kv_append4(K, V, slot_map, k_pages, v_pages):
 def provip_kv_read4(slot_map, k_pages, v_pages, dtype=torch.bfloat16, out=None):
     """What the rows at the slots slot_map [T] of 4-bit pages stand for: K and V [T, H_kv, 128]. out: (K, V)
     to write, whose type counts then; rows of a negative slot are left untouched (zeros, unless out is given)."""
-    _three("kv_read4", k_pages)
+    if k_pages.dim() != 3:
+        raise _dims("kv_read4", k_pages)
     T, H, dev = slot_map.numel(), k_pages.shape[1], k_pages.get_device()
     if out is None:
         out = tuple(torch.zeros(T, H, 128, dtype=dtype, device=k_pages.device) for _ in range(2))
@@ -964,6 +968,7 @@ class DecodeAttention4:
 def provip_decode_attention4(Q, k_pages, v_pages, block_table, kv_len, kv_len_max, prefix_table=None, prefix_len=0,
                              scale=None, want_lse=True):
     """One call of DecodeAttention4, its outputs and workspace allocated here."""
-    _three("decode_attention4", Q, k_pages)
+    if Q.dim() != 3 or k_pages.dim() != 3:
+        raise _dims("decode_attention4", Q, k_pages)
     step = DecodeAttention4(Q.shape[0], Q.shape[1], k_pages.shape[1], kv_len_max, prefix_len, scale, Q.dtype, Q.device, want_lse)
     return step(Q, k_pages, v_pages, block_table, kv_len, prefix_table)
